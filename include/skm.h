@@ -62,7 +62,8 @@ typedef enum skm_repr {
                           0) + per-point terms `lvq` (Section 3.1 "LVQ4")   */
 } skm_repr;
 
-typedef enum skm_dtype { SKM_DTYPE_F32 = 0, SKM_DTYPE_BF16 = 1 } skm_dtype;
+/* SKM_DTYPE_F16: the key/value cache's entry points only. */
+typedef enum skm_dtype { SKM_DTYPE_F32 = 0, SKM_DTYPE_BF16 = 1, SKM_DTYPE_F16 = 2 } skm_dtype;
 
 /* skm_data.flags */
 enum {
@@ -742,6 +743,117 @@ int skm_objective(const void *X, int x_is_bf16, int64_t n, int d, const float *C
 /* SQ8 reconstruction x ~ code * s + b (fp32): codes uint8[n][d] -> Y float[n][d]. */
 int skm_sq8_decode(const uint8_t *codes, int64_t n, int d, const float *b, const float *s,
                    float *Y, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Key/value cache in 8 bits, and attention that computes on its codes (the
+ * paper has no counterpart: its scalar quantizer and its products in the code
+ * domain, applied to the vectors that a language model keeps of a context;
+ * the values read back are points for skm_fit like any others).
+ *
+ * A cache is a pool of pages.  A page holds `page` consecutive token
+ * positions of all `heads` key/value heads, cut into blocks of SKM_KV_BLOCK =
+ * 16 tokens; every block of a head has one fp32 scale for its keys and one for
+ * its values: value = scale (code - 128), codes 1..255 in uint8.
+ *  k       uint8 [pages][heads][page / 16][d / 16][16 tokens][16 dims]
+ *  v       uint8 [pages][heads][page / 16][d][16 bytes], token t of the block
+ *          at byte 4 ((t mod 8) div 2) + 2 (t div 8) + t mod 2 (the order in
+ *          which a tensor-core operand takes them)
+ *  scales  float32 [pages][heads][page / 16][2] (key, value)
+ * 16 <= d <= 256 and a multiple of 16, page a multiple of 16; pages * heads *
+ * page / 16 < 2^31; k and v 16-byte, scales 8-byte aligned.  Nothing needs
+ * initialising: only positions that were written are read, and codes hold no
+ * infinities or NaN.
+ *
+ * The sequences of a call: position t of sequence b lies in page
+ * table[b][t div page] at t mod page.  A table entry outside [0, pages) is an
+ * absent page: nothing is written there, it reads as zeros, attention does not
+ * see its tokens.  Rows of a call's token tensors belong to sequence b from
+ * cu[b] up to cu[b + 1] (clamped to [0, tokens]); sequences may have none.
+ * All arrays are device arrays; max_tokens and max_len are host bounds that
+ * launches are planned with: rows of a sequence beyond max_tokens are left
+ * alone, so they must not be below the true maxima.  A sequence ends at cols *
+ * page positions.  Pages of two sequences of one call may coincide when they are only read.
+ * ------------------------------------------------------------------------ */
+enum { SKM_KV_BLOCK = 16 };
+
+typedef struct skm_kv_cache {
+    int32_t heads;
+    int32_t d;
+    int32_t page;     /* tokens of a page                                     */
+    int32_t pages;    /* pages of the pool                                    */
+    uint8_t *k;
+    uint8_t *v;
+    float *scales;
+} skm_kv_cache;
+
+typedef struct skm_kv_seqs {
+    int32_t batch;
+    int32_t cols;         /* entries of a table row                               */
+    const int32_t *table; /* [batch][cols]                                        */
+    const int32_t *pos;   /* [batch]: skm_kv_write, skm_kv_read: the position of
+                             each sequence's first row; skm_kv_attend: the tokens
+                             that the cache holds of it, the rows' own included   */
+    const int32_t *cu;    /* [batch + 1]                                          */
+    int32_t tokens;       /* rows of the token tensors                            */
+    int32_t max_tokens;   /* most rows of one sequence                            */
+    int32_t max_len;      /* skm_kv_attend: largest pos; else not read            */
+} skm_kv_seqs;
+
+/* Quantises new keys and values as they enter the cache.  K, V (dtype F32,
+ * BF16 or F16): rows [tokens] of [heads][d], d contiguous, with strides in
+ * elements from token to token and head to head (slices of a fused projection
+ * need no copy).  Per block, head and tensor, with a the largest finite |x| of
+ * the block's new values: scale = max(the old scale if the block holds tokens
+ * before the first new one, fl32(a fl32(1/127))), code = 128 +
+ * clip(round(x / scale), -127, 127) in fp32, rounding half to even (NaN: 128;
+ * scale 0: 128).  When the scale of a block that holds tokens grows, their
+ * codes become 128 + round((code - 128) fl32(old / scale)).  Positions from
+ * pos[b] on that were written before are overwritten (a rolled back tail).  Two
+ * sequences of a call must not write to the same page.  One kernel, no
+ * workspace.  Asynchronous. */
+int skm_kv_write(const skm_kv_cache *c, const skm_kv_seqs *s, int dtype, const void *K, int64_t k_token,
+                 int64_t k_head, const void *V, int64_t v_token, int64_t v_head, void *stream);
+
+/* Values of positions pos[b], pos[b] + 1, ... back: K and V (device, either may
+ * be NULL) dtype [tokens][heads][d], contiguous, 16-byte aligned: scale (code -
+ * 128) in fp32, rounded once to dtype.  Absent pages and positions past the
+ * table's end: zeros.  One kernel, no workspace.  Asynchronous. */
+int skm_kv_read(const skm_kv_cache *c, const skm_kv_seqs *s, int dtype, void *K, void *V, void *stream);
+
+/* Attention of query rows over the cache.  Row i (of n) of sequence b stands at
+ * position p = pos[b] - n + i.  Query head h reads key/value head h div
+ * (heads_q / heads).  It sees the positions j < pos[b] in present pages with, if
+ * causal, j <= p, and with a window w > 0 (causal only), j > p - w:
+ *   lse = log sum_j exp(scale <q, k_j>),  out = sum_j exp(scale <q, k_j> - lse) v_j,
+ * and out = 0, lse = -infinity for a row that sees nothing.
+ *  Q   dtype rows [tokens] of [heads_q][d], d contiguous, strides in elements
+ *  out dtype [tokens][heads_q][d], lse float32 [tokens][heads_q] or NULL: contiguous
+ * dtype BF16 or F16: products on tensor cores of codes (exact in f16) and of the
+ * queries (bf16 rows scaled by a power of two to f16), sums and softmax in fp32,
+ * the probabilities rounded to f16; F32: fp32 arithmetic throughout.
+ *  status: device int32 or NULL; set to 1 when a bounded device wait gave up
+ *  (some rows are then NaN or not written), otherwise left alone.
+ *  ws: skm_kv_attend_workspace_size(c, s, a) bytes, 256-byte aligned (0 bytes: may be
+ *  NULL; it returns (size_t)-1 with skm_last_error() set for invalid arguments).
+ * The result does not depend on timing.  Asynchronous. */
+typedef struct skm_kv_attn {
+    int32_t heads_q;   /* a multiple of the cache's heads */
+    int32_t dtype;
+    int32_t causal;
+    int32_t window;    /* 0: none */
+    float scale;
+    int32_t reserved;
+    const void *Q;
+    int64_t q_token;
+    int64_t q_head;
+    void *out;
+    float *lse;
+    int32_t *status;
+} skm_kv_attn;
+
+size_t skm_kv_attend_workspace_size(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a);
+int skm_kv_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws, size_t ws_bytes,
+                  void *stream);
 
 #ifdef __cplusplus
 }

@@ -8,6 +8,7 @@ raises.  Function names match the C entry points.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -20,12 +21,13 @@ __all__ = [
     "skm_quantize", "skm_rbq1_exponent", "skm_lvq4_exponent", "skm_assign", "skm_update", "skm_merge_partials",
     "skm_update_finalize", "skm_fit", "skm_split_empty", "skm_objective", "skm_sq8_decode", "EXPORTED_SYMBOLS",
     "EMPTY_KEEP", "EMPTY_SPLIT",
-    "skm_assign_prune_stats",
+    "skm_assign_prune_stats", "DTYPE_F32", "DTYPE_BF16", "DTYPE_F16", "KVCache", "kv_workspace", "skm_kv_write",
+    "skm_kv_read", "skm_kv_attend",
 ]
 
 REPR_F32, REPR_SQ8, REPR_RBQ1, REPR_BF16, REPR_LVQ4 = 0, 1, 2, 3, 4
 FLAG_PRUNE, FLAG_SYMMETRIC, FLAG_WARM, FLAG_PRUNE_CUDA_CORES = 1, 2, 4, 8
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 EMPTY_KEEP, EMPTY_SPLIT = 0, 1
 OP_ASSIGN, OP_UPDATE, OP_FIT, OP_QUANTIZE, OP_PCA, OP_ASSIGN_SEG = 0, 1, 2, 3, 4, 5
 
@@ -46,7 +48,7 @@ EXPORTED_SYMBOLS = [
     "skm_fit_hierarchical", "skm_objective", "skm_sq8_decode", "skm_step_host_workspace_size",
     "skm_lloyd_step_host", "skm_inject_fault", "skm_fault_armed", "skm_forgy_indices", "skm_column_absmax",
     "skm_mean_scale", "skm_column_sums_fixed", "skm_mean_from_sums", "skm_rbq1_segment_bounds",
-    "skm_rbq1_segments",
+    "skm_rbq1_segments", "skm_kv_write", "skm_kv_read", "skm_kv_attend_workspace_size", "skm_kv_attend",
 ]
 
 
@@ -93,6 +95,30 @@ class HierConfig(ctypes.Structure):
 class FitConfig(ctypes.Structure):
     _fields_ = [("k", ctypes.c_int32), ("iters", ctypes.c_int32), ("empty_policy", ctypes.c_int32),
                 ("reserved0", ctypes.c_int32), ("seed", ctypes.c_uint64), ("reserved", ctypes.c_int32 * 2)]
+
+
+class KVCacheRef(ctypes.Structure):
+    """skm_kv_cache (include/skm.h)."""
+
+    _fields_ = [("heads", ctypes.c_int32), ("d", ctypes.c_int32), ("page", ctypes.c_int32), ("pages", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class KVSeqs(ctypes.Structure):
+    """skm_kv_seqs (include/skm.h)."""
+
+    _fields_ = [("batch", ctypes.c_int32), ("cols", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("pos", ctypes.c_void_p), ("cu", ctypes.c_void_p), ("tokens", ctypes.c_int32),
+                ("max_tokens", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class KVAttn(ctypes.Structure):
+    """skm_kv_attn (include/skm.h)."""
+
+    _fields_ = [("heads_q", ctypes.c_int32), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("Q", ctypes.c_void_p), ("q_token", ctypes.c_int64), ("q_head", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("status", ctypes.c_void_p)]
 
 
 EXCHANGE_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p)
@@ -160,6 +186,10 @@ def lib():
             "skm_mean_from_sums": ([vp, i64, i32, i32, vp, vp], i32),
             "skm_fault_armed": ([i32], i32),
             "skm_step_host_workspace_size": ([vp, vp], sz),
+            "skm_kv_write": ([vp, vp, i32, vp, i64, i64, vp, i64, i64, vp], i32),
+            "skm_kv_read": ([vp, vp, i32, vp, vp, vp], i32),
+            "skm_kv_attend_workspace_size": ([vp, vp, vp], sz),
+            "skm_kv_attend": ([vp, vp, vp, vp, sz, vp], i32),
             "skm_lloyd_step_host": ([vp, vp, vp, vp, vp, vp, vp, vp, sz, vp], i32),
         }
         for name, (args, res) in sig.items():
@@ -701,3 +731,151 @@ def skm_rbq1_segments(X, m, stream=None):
     pc = torch.empty(n, 3, device=X.device, dtype=torch.int32)
     _check(lib().skm_rbq1_segments(_ptr(X), n, d, _ptr(m), _ptr(nx2), _ptr(F), _ptr(pc), _stream(stream)))
     return nx2, F, pc
+
+
+# ---- 8-bit key/value cache
+
+_KV_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+_KV_TORCH = {v: k for k, v in _KV_DTYPES.items()}
+KV_BLOCK = 16
+
+
+class KVCache:
+    """The tensors of one skm_kv_cache: uint8 codes k and v [pages, heads,
+    page / 16, 16 d] and float32 scales [pages, heads, page / 16, 2] (layouts in
+    include/skm.h), allocated here for `pages` pages unless given."""
+
+    def __init__(self, heads, d, page, k=None, v=None, scales=None, pages=None, device="cuda"):
+        if k is None:
+            shape = (int(pages), int(heads), int(page) // KV_BLOCK)
+            k = torch.empty(*shape, KV_BLOCK * int(d), dtype=torch.uint8, device=device)
+            v = torch.empty_like(k)
+            scales = torch.empty(*shape, 2, dtype=torch.float32, device=device)
+        n = int(k.shape[0]) if k.dim() else 0
+        shape = (n, int(heads), int(page) // KV_BLOCK)
+        for name, t, last, dt in (("k", k, KV_BLOCK * int(d), torch.uint8), ("v", v, KV_BLOCK * int(d), torch.uint8),
+                                  ("scales", scales, 2, torch.float32)):
+            if t is None or t.dtype != dt or tuple(t.shape) != shape + (last,) or not t.is_contiguous():
+                raise ValueError(f"KVCache: {name} must be contiguous {dt} {list(shape + (last,))}")
+            if t.device != k.device:
+                raise ValueError("KVCache: k, v and scales must be on one device")
+        self.k, self.v, self.scales = k, v, scales
+        self.heads, self.d, self.page, self.pages = int(heads), int(d), int(page), n
+        self.ref = KVCacheRef(self.heads, self.d, self.page, n, k.data_ptr(), v.data_ptr(), scales.data_ptr())
+
+    @property
+    def device(self):
+        return self.k.device
+
+
+def _kv_ints(name, t, shape, device):
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+
+
+def _kv_seqs(cache, table, pos, cu, tokens, max_tokens, max_len=0):
+    if table.dim() != 2:
+        raise ValueError("table must be [batch, cols]")
+    batch, cols = table.shape
+    _kv_ints("table", table, (batch, cols), cache.device)
+    _kv_ints("positions", pos, (batch,), cache.device)
+    _kv_ints("cu", cu, (batch + 1,), cache.device)
+    return KVSeqs(batch, cols, table.data_ptr(), pos.data_ptr(), cu.data_ptr(), tokens, int(max_tokens), int(max_len))
+
+
+def _kv_rows(name, t, heads, cache):
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != cache.d or t.device != cache.device:
+        raise ValueError(f"{name} must be [tokens, {heads}, {cache.d}] on {cache.device}")
+    if t.dtype not in _KV_DTYPES:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+
+
+def _kv_on(cache, stream):
+    """What a call allocates belongs to the stream that it runs on."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def skm_kv_write(cache: KVCache, table, start, cu, K, V, max_tokens, stream=None):
+    """Quantises rows cu[b]:cu[b + 1] of K and V ([tokens, heads, d], any strides
+    with d contiguous) into the cache at positions start[b], start[b] + 1, ... of
+    sequence b; table int32 [batch, cols], start [batch], cu [batch + 1]."""
+    _kv_rows("K", K, cache.heads, cache)
+    _kv_rows("V", V, cache.heads, cache)
+    if V.dtype != K.dtype or V.shape[0] != K.shape[0]:
+        raise ValueError("K and V must have one type and length")
+    s = _kv_seqs(cache, table, start, cu, K.shape[0], max_tokens)
+    _check(lib().skm_kv_write(ctypes.byref(cache.ref), ctypes.byref(s), _KV_DTYPES[K.dtype], K.data_ptr(), K.stride(0),
+                              K.stride(1), V.data_ptr(), V.stride(0), V.stride(1), _stream(stream)))
+
+
+def skm_kv_read(cache: KVCache, table, start, cu, tokens, max_tokens, dtype=DTYPE_BF16, out=None, stream=None):
+    """(K, V), each [tokens, heads, d]: rows cu[b]:cu[b + 1] are the values at
+    positions start[b], start[b] + 1, ... of sequence b.  out: a pair of
+    contiguous tensors, either may be None (not read)."""
+    if out is None:
+        if dtype not in _KV_TORCH:
+            raise ValueError(f"unknown dtype {dtype}")
+        with _kv_on(cache, stream):
+            out = tuple(torch.empty(tokens, cache.heads, cache.d, dtype=_KV_TORCH[dtype], device=cache.device)
+                        for _ in range(2))
+    else:
+        for t in out:
+            if t is not None:
+                _kv_rows("out", t, cache.heads, cache)
+                if t.shape[0] != tokens or not t.is_contiguous() or _KV_DTYPES[t.dtype] != dtype:
+                    raise ValueError("out: contiguous tensors of `tokens` rows and the given dtype")
+    s = _kv_seqs(cache, table, start, cu, int(tokens), max_tokens)
+    _check(lib().skm_kv_read(ctypes.byref(cache.ref), ctypes.byref(s), dtype, _ptr(out[0]), _ptr(out[1]),
+                             _stream(stream)))
+    return out
+
+
+def _kv_attn(heads_q, dtype, causal, window, scale):
+    return KVAttn(int(heads_q), dtype, int(bool(causal)), int(window), scale, 0, None, 0, 0, None, None, None)
+
+
+def kv_workspace(cache: KVCache, batch, heads_q, tokens, max_tokens, max_len, dtype=DTYPE_BF16, cols=None, causal=True,
+                 window=0):
+    """A workspace for skm_kv_attend calls of at most these sizes."""
+    cols = -(-int(max_len) // cache.page) if cols is None else int(cols)
+    dummy = cache.k.data_ptr()
+    s = KVSeqs(int(batch), max(cols, 1), dummy, dummy, dummy, int(tokens), int(max_tokens), int(max_len))
+    a = _kv_attn(heads_q, dtype, causal, window, 1.0)
+    n = lib().skm_kv_attend_workspace_size(ctypes.byref(cache.ref), ctypes.byref(s), ctypes.byref(a))
+    if n == ctypes.c_size_t(-1).value:
+        raise SkmError(1, lib().skm_last_error().decode())
+    return _ws(n, cache.device)
+
+
+def skm_kv_attend(cache: KVCache, table, length, cu, Q, max_tokens, max_len, scale=None, causal=True, window=0,
+                  want_lse=False, out=None, ws=None, status=None, stream=None):
+    """(out, lse or None): attention of the query rows Q [tokens, heads_q, d]
+    over the cache.  length[b]: the tokens the cache holds of sequence b, its
+    own query tokens included; scale: 1 / sqrt(d) unless given."""
+    heads_q = Q.shape[1] if Q.dim() == 3 else 0
+    _kv_rows("Q", Q, heads_q, cache)
+    tokens = Q.shape[0]
+    s = _kv_seqs(cache, table, length, cu, tokens, max_tokens, max_len)
+    a = _kv_attn(heads_q, _KV_DTYPES[Q.dtype], causal, window, cache.d ** -0.5 if scale is None else float(scale))
+    if status is not None and (status.dtype != torch.int32 or status.device != cache.device or status.numel() < 1):
+        raise ValueError(f"status must be an int32 tensor on {cache.device}")
+    with _kv_on(cache, stream):
+        if out is None:
+            out = torch.empty(tokens, heads_q, cache.d, dtype=Q.dtype, device=cache.device)
+        elif out.shape != Q.shape or out.dtype != Q.dtype or not out.is_contiguous() or out.device != cache.device:
+            raise ValueError("out: contiguous, of Q's shape and type")
+        lse = torch.empty(tokens, heads_q, dtype=torch.float32, device=cache.device) if want_lse else None
+        if ws is None:
+            n = lib().skm_kv_attend_workspace_size(ctypes.byref(cache.ref), ctypes.byref(s), ctypes.byref(a))
+            if n == ctypes.c_size_t(-1).value:
+                raise SkmError(1, lib().skm_last_error().decode())
+            ws = _ws(n, cache.device) if n else None
+    a.Q, a.q_token, a.q_head = Q.data_ptr(), Q.stride(0), Q.stride(1)
+    a.out = out.data_ptr()
+    a.lse = None if lse is None else lse.data_ptr()
+    a.status = None if status is None else status.data_ptr()
+    _check(lib().skm_kv_attend(ctypes.byref(cache.ref), ctypes.byref(s), ctypes.byref(a), _ptr(ws),
+                               0 if ws is None else ws.numel(), _stream(stream)))
+    return out, lse

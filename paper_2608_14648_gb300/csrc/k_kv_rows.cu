@@ -1,0 +1,724 @@
+// Attention over the 8-bit cache for few query rows (single tokens, a few
+// tokens): the codes cross HBM once and everything else hides behind them.
+//
+// Work.  A unit is a sequence's tile of RT query rows (token-major, then the
+// heads of one group) and a key/value head; its blocks of 16 tokens are its
+// items.  All items of a launch form one line, units in order (sequence, row
+// tile, head), and each CTA takes an equal stretch of it, each warp an equal
+// stretch of its CTA's: short and long sequences balance without a plan on the
+// host, and a warp crosses at most two cuts.  (With `whole`, a CTA's stretch
+// is one unit: short sequences then need no second kernel.)  A warp runs alone: lane 0
+// keeps a ring of cp.async.bulk copies (a block's keys and values, 16 d bytes
+// each, contiguous in the cache) going across unit boundaries; the table
+// entries and scales of 32 items are fetched at once, a window ahead.
+//
+// Mathematics.  With S = scale log2(e) q.k, codes c and scales s_k, s_v, the
+// block's logits are t = S + log2 s_v, S = (scale log2(e) s_k) q.c_k; p = 2^(t - m),
+// o = sum p c_v, l = sum p / s_v: the value scale costs one addition a logit
+// and o needs none.  m is a running reference that moves only when a logit
+// exceeds it by 15 (then to 7 below the maximum), so p < 2^15 and the sums are rarely
+// rescaled.  out = o / l, lse = ln2 (m + log2 l).
+//
+// Joining.  Partial (m, l, o) of units that warps share are merged by their
+// CTA, those that CTAs share by kv_join_kernel; both in the line's order, so
+// the result does not depend on timing.
+#include "skm_kv.cuh"
+
+namespace skm {
+
+namespace {
+
+constexpr unsigned long long WAIT_NS = 2000000000ull;
+constexpr float M_NONE = -3.0e38f;  // the reference before the first logit
+constexpr float M_SLACK = 15.0f, M_BELOW = 7.0f;
+constexpr float LN2 = 0.69314718055994531f;
+
+__device__ __forceinline__ uint32_t su32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ bool bar_try(uint32_t b, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}\n"
+        : "=r"(ok)
+        : "r"(b), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity) {
+    if (bar_try(b, parity)) return true;
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    for (uint32_t i = 1;; ++i) {
+        if (bar_try(b, parity)) return true;
+        if ((i & 63) == 0) {
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+            if (t - t0 > WAIT_NS) return false;
+        }
+    }
+}
+__device__ __forceinline__ void bulk_g2s(uint32_t dst, const void *src, uint32_t bytes, uint32_t b) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+        "l"(src), "r"(bytes), "r"(b)
+        : "memory");
+}
+
+// ---- a sequence as this launch sees it
+struct Seq {
+    int lo, cnt;  // first block that a row sees, blocks
+    int len, n;   // tokens held, rows
+};
+__device__ __forceinline__ Seq seq_of(const KvAttnArgs &a, int b) {
+    Seq s;
+    s.len = kv_clamp(a.pos[b], 0, a.cols * a.page);
+    s.n = kv_rows_of(a.cu, b, a.tokens, a.max_tokens).y;
+    s.lo = a.window > 0 ? max(0, s.len - s.n - a.window + 1) / KV_B : 0;
+    s.cnt = s.n > 0 ? (s.len + KV_B - 1) / KV_B - s.lo : 0;
+    if (s.cnt < 0) s.cnt = 0;
+    return s;
+}
+__device__ __forceinline__ int tiles_of(const KvAttnArgs &a, const Seq &s, int rt) {
+    return (int)(((int64_t)s.n * a.group + rt - 1) / rt);
+}
+// the last / first position that row r of a sequence may see (last < first: none)
+__device__ __forceinline__ int last_of(const KvAttnArgs &a, const Seq &s, int r) {
+    const int i = r / a.group;
+    if (i >= s.n) return -1;
+    return a.causal ? min(s.len - 1, s.len - s.n + i) : s.len - 1;
+}
+__device__ __forceinline__ int first_of(const KvAttnArgs &a, const Seq &s, int r) {
+    return a.window > 0 ? max(0, s.len - s.n + r / a.group - a.window + 1) : 0;
+}
+
+// Where a row's result goes
+__device__ __forceinline__ int64_t row_index(const KvAttnArgs &a, int row0, int h, int r) {
+    return ((int64_t)row0 + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group;
+}
+
+// The line of items.  cum[i] (shared memory): items of sequences before b0 + i.
+struct Line {
+    const int64_t *cum;
+    const Seq *seq;
+    int b0, nb;
+    __device__ __forceinline__ int find(int64_t item) const {  // the sequence that holds an item
+        int lo = 0, hi = nb;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (cum[mid] <= item) lo = mid;
+            else hi = mid;
+        }
+        return lo;
+    }
+};
+
+// CTAs that share W items: no more than leave every warp two items
+__host__ __device__ __forceinline__ int64_t active_ctas(int64_t W, int nw, int64_t grid) {
+    const int64_t c = (W + 2 * nw - 1) / (2 * nw);
+    return c < 1 ? 1 : (c > grid ? grid : c);
+}
+
+// 32 items, one a lane: where the block is, its scales, the item's unit
+struct Window {
+    int at;  // block of the pool, -1: nothing to do
+    int blk, seq, unit;
+    float ks, lvs, ivs;
+    uint32_t todo, starts;  // (all lanes the same) items with work, items that begin a unit
+    int n;
+};
+
+template <int RT>
+__device__ __forceinline__ void window_fill(const KvAttnArgs &a, const Line &ln, int64_t base, int64_t end, int lane,
+                                            Window &w) {
+    w.n = end - base > 32 ? 32 : (int)(end > base ? end - base : 0);
+    w.at = -1;
+    w.blk = w.seq = w.unit = 0;
+    w.ks = 0.0f, w.lvs = 0.0f, w.ivs = 1.0f;
+    bool starts = false;
+    if (lane < w.n) {
+        const int64_t item = base + lane;
+        const int b = ln.find(item);
+        const Seq s = ln.seq[b];
+        const uint64_t rem = (uint64_t)(item - ln.cum[b]);
+        uint32_t u, k;
+        if (rem >> 32) {
+            u = (uint32_t)(rem / (uint32_t)s.cnt);
+            k = (uint32_t)(rem % (uint32_t)s.cnt);
+        } else {
+            u = (uint32_t)rem / (uint32_t)s.cnt;
+            k = (uint32_t)rem - u * (uint32_t)s.cnt;
+        }
+        starts = k == 0;
+        w.seq = b;
+        w.unit = (int)u;
+        w.blk = s.lo + (int)k;
+        const int r0 = (int)(u / a.heads) * RT, r1 = min(r0 + RT, s.n * a.group) - 1;
+        const bool seen = w.blk * KV_B <= last_of(a, s, r1) && w.blk * KV_B + KV_B > first_of(a, s, r0);
+        const int pg = a.table[(int64_t)(ln.b0 + b) * a.cols + w.blk / a.bpp];
+        if (seen && pg >= 0 && pg < a.pages) {
+            w.at = (pg * a.heads + (int)(u % a.heads)) * a.bpp + w.blk % a.bpp;
+            const float2 sc = a.scales[w.at];
+            w.ks = sc.x;
+            if (sc.y > 0.0f) {  // a block of zeros has scale 0: any scale will do
+                w.lvs = log2f(sc.y);
+                w.ivs = 1.0f / sc.y;
+            }
+        }
+    }
+    w.todo = __ballot_sync(0xffffffffu, w.at >= 0);
+    w.starts = __ballot_sync(0xffffffffu, starts);
+}
+
+// A partial result: RT x (m, l), padded to 16 bytes, then RT rows of d sums.
+template <int RT>
+__host__ __device__ constexpr int part_head() {
+    return (2 * RT + 3) & ~3;
+}
+template <int RT>
+__host__ __device__ __forceinline__ int64_t part_floats(int d) {
+    return part_head<RT>() + (int64_t)RT * d;
+}
+
+// Merges parts of one unit, the threads of a group working together: to the
+// outputs (dst NULL) or as a part again.
+template <int RT>
+__device__ __forceinline__ void merge_parts(const KvAttnArgs &a, const float *const *parts, int np, const Seq &s, int row0,
+                                            int unit, float *dst, int tid, int threads) {
+    const int d4 = a.d / 4, h = unit % a.heads, r0 = unit / a.heads * RT;
+    const int rows = min(RT, s.n * a.group - r0);
+    for (int e = tid; e < rows * d4; e += threads) {
+        const int r = e / d4, c = e - r * d4;
+        float m = M_NONE;
+        for (int i = 0; i < np; ++i) m = fmaxf(m, parts[i][2 * r]);
+        float l = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int i = 0; i < np; ++i) {
+            const float w = exp2f(parts[i][2 * r] - m);
+            const float4 v = *reinterpret_cast<const float4 *>(parts[i] + part_head<RT>() + r * a.d + 4 * c);
+            l = fmaf(parts[i][2 * r + 1], w, l);
+            o.x = fmaf(v.x, w, o.x), o.y = fmaf(v.y, w, o.y), o.z = fmaf(v.z, w, o.z), o.w = fmaf(v.w, w, o.w);
+        }
+        if (dst) {
+            if (c == 0) dst[2 * r] = m, dst[2 * r + 1] = l;
+            *reinterpret_cast<float4 *>(dst + part_head<RT>() + r * a.d + 4 * c) = o;
+        } else {
+            const int64_t row = row_index(a, row0, h, r0 + r);
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            kv_store(a.out, row * a.d + 4 * c, o.x * inv, a.dtype);
+            kv_store(a.out, row * a.d + 4 * c + 1, o.y * inv, a.dtype);
+            kv_store(a.out, row * a.d + 4 * c + 2, o.z * inv, a.dtype);
+            kv_store(a.out, row * a.d + 4 * c + 3, o.w * inv, a.dtype);
+            if (c == 0 && a.lse) a.lse[row] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
+        }
+    }
+}
+
+// Rows of one warp in fp32 on CUDA cores.  Scores: lane = (half, token), a
+// half takes every other 16-dim chunk of the keys; sums: lane = dims lane,
+// lane + 32, ...  q and p pass through the warp's shared memory.
+template <int R, int DPL>
+struct Fp32Rows {
+    static constexpr int RT = R;
+    static size_t __host__ __device__ scratch(int d) { return (size_t)R * (d + KV_B) * 4; }
+    float o[R][DPL], m[R], l[R];
+    float *q, *p;
+
+    __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int row0, int h, int r0, uint8_t *mem,
+                                          int lane) {
+        q = reinterpret_cast<float *>(mem);
+        p = q + R * a.d;
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            m[r] = M_NONE, l[r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < DPL; ++i) o[r][i] = 0.0f;
+            const int rr = r0 + r;
+            const bool in = rr < s.n * a.group;
+            const int64_t at = in ? (int64_t)(row0 + rr / a.group) * a.q_token + (int64_t)(h * a.group + rr % a.group) * a.q_head : 0;
+            for (int i = lane; i < a.d; i += 32) q[r * a.d + i] = in ? kv_load(a.Q, at + i, a.dtype) * a.scale_log2 : 0.0f;
+        }
+        __syncwarp();
+    }
+
+    __device__ __forceinline__ void block(const KvAttnArgs &a, const Seq &s, int r0, const uint8_t *K, const uint8_t *V,
+                                          int blk, float ks, float lvs, float ivs, bool mask, int lane) {
+        const int t = lane & 15, half = lane >> 4, nc = a.d / KV_B;
+        float x[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r] = 0.0f;
+        for (int w = half; w < nc; w += 2) {
+            const uint4 c = *reinterpret_cast<const uint4 *>(K + w * 256 + t * 16);
+            const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float k0 = kv_code(word[i], 0), k1 = kv_code(word[i], 1), k2 = kv_code(word[i], 2), k3 = kv_code(word[i], 3);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float4 qq = *reinterpret_cast<const float4 *>(q + r * a.d + 16 * w + 4 * i);
+                    x[r] = fmaf(k0, qq.x, x[r]);
+                    x[r] = fmaf(k1, qq.y, x[r]);
+                    x[r] = fmaf(k2, qq.z, x[r]);
+                    x[r] = fmaf(k3, qq.w, x[r]);
+                }
+            }
+        }
+        const int place = 4 * ((t & 7) >> 1) + 2 * (t >> 3) + (t & 1);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            x[r] += __shfl_xor_sync(0xffffffffu, x[r], 16);
+            x[r] = fmaf(x[r], ks, lvs);
+            if (mask) {
+                const int j = blk * KV_B + t;
+                if (j > last_of(a, s, r0 + r) || j < first_of(a, s, r0 + r)) x[r] = -INFINITY;
+            }
+            if (__any_sync(0xffffffffu, x[r] > m[r] + M_SLACK)) {
+                float top = x[r];
+#pragma unroll
+                for (int b = 8; b > 0; b >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, b));
+                const float to = top - M_BELOW, f = exp2f(m[r] - to);
+                m[r] = to;
+                l[r] *= f;
+#pragma unroll
+                for (int i = 0; i < DPL; ++i) o[r][i] *= f;
+            }
+            const float e = exp2f(x[r] - m[r]);
+            if (half == 0) {
+                l[r] = fmaf(e, ivs, l[r]);
+                p[r * KV_B + place] = e;
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < DPL; ++i) {
+            const int dim = lane + 32 * i;
+            if (dim >= a.d) break;
+            const uint4 c = *reinterpret_cast<const uint4 *>(V + dim * 16);
+            const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float k0 = kv_code(word[w], 0), k1 = kv_code(word[w], 1), k2 = kv_code(word[w], 2), k3 = kv_code(word[w], 3);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float4 pp = *reinterpret_cast<const float4 *>(p + r * KV_B + 4 * w);
+                    o[r][i] = fmaf(k0, pp.x, o[r][i]);
+                    o[r][i] = fmaf(k1, pp.y, o[r][i]);
+                    o[r][i] = fmaf(k2, pp.z, o[r][i]);
+                    o[r][i] = fmaf(k3, pp.w, o[r][i]);
+                }
+            }
+        }
+        __syncwarp();
+    }
+
+    __device__ __forceinline__ void close(int) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int b = 16; b > 0; b >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], b);
+    }
+    __device__ __forceinline__ void poison() {
+#pragma unroll
+        for (int r = 0; r < R; ++r) l[r] = NAN;
+    }
+    __device__ __forceinline__ void put(const KvAttnArgs &a, float *dst, int lane) const {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (lane == 0) dst[2 * r] = m[r], dst[2 * r + 1] = l[r];
+#pragma unroll
+            for (int i = 0; i < DPL; ++i)
+                if (lane + 32 * i < a.d) dst[part_head<R>() + r * a.d + lane + 32 * i] = o[r][i];
+        }
+    }
+    __device__ __forceinline__ void finish(const KvAttnArgs &a, const Seq &s, int row0, int h, int r0, int lane) const {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (r0 + r >= s.n * a.group) break;
+            const int64_t row = row_index(a, row0, h, r0 + r);
+            const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+#pragma unroll
+            for (int i = 0; i < DPL; ++i)
+                if (lane + 32 * i < a.d) kv_store(a.out, row * a.d + lane + 32 * i, o[r][i] * inv, a.dtype);
+            if (lane == 0 && a.lse) a.lse[row] = l[r] == 0.0f ? -INFINITY : LN2 * (m[r] + log2f(l[r]));
+        }
+    }
+};
+
+// A CTA's records of the units that its warps did not finish alone, in the
+// line's order: [2 w] the unit that warp w found begun and left (part_warp), [2 w +
+// 1] the one open at its end.
+struct Record {
+    int seq, unit;  // unit -1: none
+    float *part;
+};
+
+// Shared memory of a CTA
+struct Smem {
+    size_t cum, seq, rec, bars, scratch, ring, total;
+};
+template <class Rows>
+__host__ __device__ __forceinline__ Smem smem_of(int nb, int d, int nw, int ns) {
+    Smem s;
+    s.cum = 0;
+    s.seq = s.cum + 8 * (size_t)(nb + 1);
+    s.seq = (s.seq + 15) & ~size_t(15);
+    s.rec = s.seq + 16 * (size_t)nb;
+    s.bars = s.rec + sizeof(Record) * 2 * nw;
+    s.scratch = (s.bars + 8 * (size_t)nw * ns + 127) & ~size_t(127);
+    s.ring = (s.scratch + nw * Rows::scratch(d) + 127) & ~size_t(127);
+    // after the loop the ring's memory holds a part of every warp
+    const size_t ring = (size_t)nw * ns * 2 * KV_B * d, parts = (size_t)nw * part_floats<Rows::RT>(d) * 4;
+    s.total = s.ring + (ring > parts ? ring : parts);
+    return s;
+}
+
+// cum and seq of the launch's sequences (one sequence with `whole`)
+template <int RT>
+__device__ void line_up(const KvAttnArgs &a, int b0, int nb, int64_t *cum, Seq *seq) {
+    __shared__ int64_t warp_sum[32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = blockDim.x >> 5;
+    int64_t before = 0;
+    for (int base = 0; base < nb; base += blockDim.x) {
+        const int i = base + tid;
+        int64_t v = 0;
+        if (i < nb) {
+            const Seq s = seq_of(a, b0 + i);
+            seq[i] = s;
+            v = (int64_t)s.cnt * tiles_of(a, s, RT) * a.heads;
+        }
+        int64_t x = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) warp_sum[warp] = x;
+        __syncthreads();
+        int64_t all = 0, mine = 0;
+        for (int w = 0; w < nw; ++w) {
+            if (w == warp) mine = all;
+            all += warp_sum[w];
+        }
+        if (i < nb) cum[i] = before + mine + x - v;
+        before += all;
+        __syncthreads();
+    }
+    if (tid == 0) cum[nb] = before;
+    __syncthreads();
+}
+
+template <class Rows, int NW>
+__global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_constant__ KvAttnArgs a, int ns) {
+    constexpr int RT = Rows::RT;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // the sequences this CTA looks at, and its stretch of their line
+    int nb = a.nb, b0 = a.b0, whole_unit = 0;
+    if (a.whole) {
+        const int per = a.max_tiles * a.heads;
+        b0 += blockIdx.x / per;
+        whole_unit = blockIdx.x % per;
+        nb = 1;
+    }
+    const Smem sm = smem_of<Rows>(nb, a.d, NW, ns);
+    int64_t *cum = reinterpret_cast<int64_t *>(smem + sm.cum);
+    Seq *seq = reinterpret_cast<Seq *>(smem + sm.seq);
+    Record *rec = reinterpret_cast<Record *>(smem + sm.rec);
+    const uint32_t bars = su32(smem + sm.bars) + 8 * warp * ns;
+    uint8_t *scratch = smem + sm.scratch + warp * Rows::scratch(a.d);
+    const int half = KV_B * a.d;  // bytes of a block's keys
+    uint8_t *ring = smem + sm.ring + (size_t)warp * ns * 2 * half;
+
+    if (lane == 0)
+        for (int i = 0; i < ns; ++i)
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bars + 8 * i), "r"(1) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (lane < 2) rec[2 * warp + lane].unit = -1;
+    line_up<RT>(a, b0, nb, cum, seq);
+    const Line line{cum, seq, b0, nb};
+    const int64_t W = cum[nb];
+    int64_t c0, c1;  // this CTA's items
+    if (a.whole) {
+        const bool there = whole_unit < tiles_of(a, seq[0], RT) * a.heads;
+        c0 = there ? (int64_t)whole_unit * seq[0].cnt : 0;
+        c1 = there ? c0 + seq[0].cnt : 0;
+    } else {
+        const int64_t C = active_ctas(W, NW, gridDim.x), c = blockIdx.x;
+        c0 = c < C ? W * c / C : 0;
+        c1 = c < C ? W * (c + 1) / C : 0;
+    }
+    // rows of sequences without items: no key to see
+    for (int i = a.whole ? 0 : blockIdx.x; i < nb; i += a.whole ? 1 : gridDim.x) {
+        const Seq s = seq[i];
+        if (s.cnt > 0 || s.n == 0 || (a.whole && whole_unit != 0)) continue;
+        const int64_t row = kv_rows_of(a.cu, b0 + i, a.tokens, a.max_tokens).x, hq = a.heads * a.group;
+        for (int64_t e = tid; e < s.n * hq * a.d; e += NW * 32) kv_store(a.out, row * hq * a.d + e, 0.0f, a.dtype);
+        if (a.lse)
+            for (int64_t e = tid; e < s.n * hq; e += NW * 32) a.lse[row * hq + e] = -INFINITY;
+    }
+
+    const int64_t i0 = c0 + (c1 - c0) * warp / NW, i1 = c0 + (c1 - c0) * (warp + 1) / NW;
+    Rows rows;
+    bool open = false, ok = true;
+    int useq = 0, uunit = 0;       // the open unit
+    int urow0 = 0, ur0 = 0;        // ... its sequence's first row in the token tensors, its first row
+    int safe_last = 0, safe_first = 0;  // blocks within [first, last] need no mask
+    if (i1 > i0) {
+        Window cur, next;
+        window_fill<RT>(a, line, i0, i1, lane, cur);
+        int64_t base = i0;
+        uint32_t to_issue = cur.todo;
+        bool ahead = false;  // to_issue belongs to `next`
+        uint32_t issued = 0, taken = 0;
+        const auto issue = [&](int at) {
+            const uint32_t st = issued % ns;
+            if (lane == 0) {
+                const uint32_t b = bars + 8 * st, dst = su32(ring + (size_t)st * 2 * half);
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(2u * half) : "memory");
+                bulk_g2s(dst, a.k + (int64_t)at * half, half, b);
+                bulk_g2s(dst + half, a.v + (int64_t)at * half, half, b);
+            }
+            ++issued;
+        };
+        const auto fill_ring = [&] {
+            while (issued - taken < (uint32_t)ns) {
+                if (!to_issue) {
+                    if (ahead) break;
+                    ahead = true;
+                    to_issue = next.todo;
+                    continue;
+                }
+                const int i = __ffs(to_issue) - 1;
+                to_issue &= to_issue - 1;
+                issue(__shfl_sync(0xffffffffu, ahead ? next.at : cur.at, i));
+            }
+        };
+        next.todo = 0;
+        while (to_issue && issued < (uint32_t)ns) {  // the first copies go out before the next window is known
+            const int i = __ffs(to_issue) - 1;
+            to_issue &= to_issue - 1;
+            issue(__shfl_sync(0xffffffffu, cur.at, i));
+        }
+        window_fill<RT>(a, line, base + 32, i1, lane, next);
+        const auto leave = [&](bool last) {  // the open unit ends here, for this warp
+            const Seq s = seq[useq];
+            rows.close(lane);
+            if (!ok) rows.poison();
+            const int64_t u0 = cum[useq] + (int64_t)uunit * s.cnt;
+            if (u0 >= i0 && u0 + s.cnt <= i1) {
+                rows.finish(a, s, urow0, uunit % a.heads, ur0, lane);
+            } else if (!last) {
+                float *dst = a.part_warp + ((int64_t)blockIdx.x * NW + warp) * part_floats<RT>(a.d);
+                rows.put(a, dst, lane);
+                if (lane == 0) rec[2 * warp] = Record{useq, uunit, dst};
+            }
+            return !(u0 >= i0 && u0 + s.cnt <= i1);
+        };
+        for (;;) {
+            for (int i = 0; i < cur.n && ok; ++i) {
+                if (!open || ((cur.starts >> i) & 1)) {
+                    if (open) leave(false);
+                    open = true;
+                    useq = __shfl_sync(0xffffffffu, cur.seq, i);
+                    uunit = __shfl_sync(0xffffffffu, cur.unit, i);
+                    const Seq s = seq[useq];
+                    urow0 = kv_rows_of(a.cu, b0 + useq, a.tokens, a.max_tokens).x;
+                    ur0 = uunit / a.heads * RT;
+                    safe_last = last_of(a, s, ur0);
+                    safe_first = first_of(a, s, min(ur0 + RT, s.n * a.group) - 1);
+                    rows.begin(a, s, urow0, uunit % a.heads, ur0, scratch, lane);
+                }
+                if (!((cur.todo >> i) & 1)) continue;
+                const int blk = __shfl_sync(0xffffffffu, cur.blk, i);
+                const float ks = __shfl_sync(0xffffffffu, cur.ks, i);
+                const float lvs = __shfl_sync(0xffffffffu, cur.lvs, i);
+                const float ivs = __shfl_sync(0xffffffffu, cur.ivs, i);
+                const uint32_t st = taken % ns;
+                if (!bar_wait(bars + 8 * st, (taken / ns) & 1u)) {
+                    ok = false;
+                    break;
+                }
+                const uint8_t *K = ring + (size_t)st * 2 * half;
+                const bool mask = blk * KV_B < safe_first || blk * KV_B + KV_B - 1 > safe_last;
+                rows.block(a, seq[useq], ur0, K, K + half, blk, ks, lvs, ivs, mask, lane);
+                __syncwarp();
+                ++taken;
+                fill_ring();
+            }
+            base += 32;
+            if (base >= i1 || !ok) break;
+            cur = next;
+            if (ahead) ahead = false;
+            else to_issue = cur.todo;
+            window_fill<RT>(a, line, base + 32, i1, lane, next);
+            fill_ring();
+        }
+        if (!ok) {  // a copy did not arrive: let the others land before the memory is given up
+            for (; taken < issued; ++taken) bar_wait(bars + 8 * (taken % ns), (taken / ns) & 1u);
+            if (lane == 0 && a.status) *a.status = 1;
+        }
+        open = leave(true);
+    }
+    __syncthreads();
+    // the parts of units still open go to the ring's memory
+    const int64_t pf = part_floats<RT>(a.d);
+    if (open) {
+        float *dst = reinterpret_cast<float *>(smem + sm.ring) + warp * pf;
+        rows.put(a, dst, lane);
+        if (lane == 0) rec[2 * warp + 1] = Record{useq, uunit, dst};
+    }
+    __syncthreads();
+    for (int i = 0; i < 2 * NW;) {
+        const Record r = rec[i];
+        if (r.unit < 0) {
+            ++i;
+            continue;
+        }
+        const float *parts[2 * NW];
+        int np = 0;
+        for (; i < 2 * NW; ++i) {
+            const Record n = rec[i];
+            if (n.unit < 0) continue;
+            if (n.seq != r.seq || n.unit != r.unit) break;
+            parts[np++] = n.part;
+        }
+        const Seq s = seq[r.seq];
+        const int64_t u0 = cum[r.seq] + (int64_t)r.unit * s.cnt, u1 = u0 + s.cnt;
+        float *dst = u0 >= c0 && u1 <= c1 ? nullptr : a.part_cta + ((int64_t)blockIdx.x * 2 + (u0 < c0 ? 0 : 1)) * pf;
+        const int row0 = kv_rows_of(a.cu, b0 + r.seq, a.tokens, a.max_tokens).x;
+        merge_parts<RT>(a, parts, np, s, row0, r.unit, dst, tid, NW * 32);
+    }
+}
+
+// One CTA a unit: merges what the CTAs of kv_rows_kernel left of it.  grid:
+// that kernel's CTAs.
+template <int RT>
+__global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ KvAttnArgs a, int nw, int64_t grid) {
+    __shared__ int64_t sums[2][4];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int per = a.max_tiles * a.heads;
+    const int mine = blockIdx.x / per, unit = blockIdx.x % per;
+    // items before this sequence, and all of them
+    int64_t before = 0, all = 0;
+    for (int i = threadIdx.x; i < a.nb; i += 128) {
+        const Seq s = seq_of(a, a.b0 + i);
+        const int64_t v = (int64_t)s.cnt * tiles_of(a, s, RT) * a.heads;
+        all += v;
+        if (i < mine) before += v;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        before += __shfl_xor_sync(0xffffffffu, before, o);
+        all += __shfl_xor_sync(0xffffffffu, all, o);
+    }
+    if ((threadIdx.x & 31) == 0) sums[0][threadIdx.x >> 5] = before, sums[1][threadIdx.x >> 5] = all;
+    __syncthreads();
+    before = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+    all = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+    const Seq s = seq_of(a, a.b0 + mine);
+    if (s.cnt == 0 || unit >= tiles_of(a, s, RT) * a.heads) return;
+    const int64_t u0 = before + (int64_t)unit * s.cnt, u1 = u0 + s.cnt;
+    const int64_t C = active_ctas(all, nw, grid);
+    // CTA c takes [all c / C, all (c + 1) / C): the one that holds an item
+    const auto holder = [&](int64_t item) {
+        int64_t c = item * C / all;
+        while (all * (c + 1) / C <= item) ++c;
+        while (all * c / C > item) --c;
+        return c;
+    };
+    const int64_t first = holder(u0), last = holder(u1 - 1);
+    if (first == last) return;
+    const int64_t pf = part_floats<RT>(a.d);
+    const int64_t row0 = kv_rows_of(a.cu, a.b0 + mine, a.tokens, a.max_tokens).x;
+    const int h = unit % a.heads, r0 = unit / a.heads * RT;
+    const int rows = min(RT, s.n * a.group - r0), d4 = a.d / 4;
+    const auto part = [&](int64_t c) {
+        // the first CTA left it open at its end (slot 1) unless it begins exactly with it
+        return a.part_cta + (c * 2 + (all * c / C > u0 ? 0 : 1)) * pf;
+    };
+    for (int e = threadIdx.x; e < rows * d4; e += 128) {
+        const int r = e / d4, c4 = e - r * d4;
+        float m = M_NONE, l = 0.0f;
+        for (int64_t c = first; c <= last; ++c) m = fmaxf(m, part(c)[2 * r]);
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int64_t c = first; c <= last; ++c) {
+            const float *p = part(c);
+            const float w = exp2f(p[2 * r] - m);
+            const float4 v = *reinterpret_cast<const float4 *>(p + part_head<RT>() + r * a.d + 4 * c4);
+            l = fmaf(p[2 * r + 1], w, l);
+            o.x = fmaf(v.x, w, o.x), o.y = fmaf(v.y, w, o.y), o.z = fmaf(v.z, w, o.z), o.w = fmaf(v.w, w, o.w);
+        }
+        const int64_t row = row_index(a, (int)row0, h, r0 + r);
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        kv_store(a.out, row * a.d + 4 * c4, o.x * inv, a.dtype);
+        kv_store(a.out, row * a.d + 4 * c4 + 1, o.y * inv, a.dtype);
+        kv_store(a.out, row * a.d + 4 * c4 + 2, o.z * inv, a.dtype);
+        kv_store(a.out, row * a.d + 4 * c4 + 3, o.w * inv, a.dtype);
+        if (c4 == 0 && a.lse) a.lse[row] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
+    }
+}
+
+constexpr size_t SMEM_MOST = 226 * 1024;  // the static part aside
+
+template <class Rows, int NW>
+cudaError_t run_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) {
+    auto kern = kv_rows_kernel<Rows, NW>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_MOST);
+    if (e != cudaSuccess) return e;
+    kern<<<(unsigned)p.grid, NW * 32, p.smem, st>>>(a, p.ns);
+    e = launched();
+    if (e != cudaSuccess || p.whole) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)p.units);
+    cfg.blockDim = dim3(128);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, kv_join_kernel<Rows::RT>, a, NW, p.grid);
+    return e != cudaSuccess ? e : launched();
+}
+
+template <class Rows>
+KvRowsPlan plan_rows(int nb, int heads, int group, int d, int max_tokens, int64_t span, int nw) {
+    KvRowsPlan p = {};
+    p.rt = Rows::RT;
+    p.nw = nw;
+    p.units = (int64_t)nb * cdiv((int64_t)max_tokens * group, p.rt) * heads;
+    p.whole = span <= 1024;
+    p.ns = 4;
+    const int seqs = p.whole ? 1 : nb;
+    while (p.ns > 1 && smem_of<Rows>(seqs, d, nw, p.ns).total > SMEM_MOST) --p.ns;
+    p.smem = smem_of<Rows>(seqs, d, nw, p.ns).total;
+    p.grid = p.whole ? p.units : KV_SMS;
+    p.part_cta = p.whole ? 0 : (size_t)p.grid * 2 * part_floats<Rows::RT>(d) * 4;
+    p.part_warp = p.whole ? 0 : (size_t)p.grid * nw * part_floats<Rows::RT>(d) * 4;
+    return p;
+}
+
+}  // namespace
+
+// span: blocks times 16 that a unit may cover
+KvRowsPlan kv_rows_plan(int nb, int heads, int group, int d, int dtype, int max_tokens, int64_t span) {
+    KvRowsPlan p;
+    const int nw = d <= 128 ? 16 : 8;
+    if ((int64_t)max_tokens * group == 1) p = plan_rows<Fp32Rows<1, 8>>(nb, heads, group, d, max_tokens, span, nw);
+    else p = plan_rows<Fp32Rows<4, 8>>(nb, heads, group, d, max_tokens, span, nw);
+    p.fp32 = 1;
+    return p;
+}
+
+cudaError_t launch_kv_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) {
+    if (p.rt == 1) {
+        if (a.d <= 64) return run_rows<Fp32Rows<1, 2>, 16>(a, p, st);
+        if (a.d <= 128) return run_rows<Fp32Rows<1, 4>, 16>(a, p, st);
+        return run_rows<Fp32Rows<1, 8>, 8>(a, p, st);
+    }
+    if (a.d <= 64) return run_rows<Fp32Rows<4, 2>, 16>(a, p, st);
+    if (a.d <= 128) return run_rows<Fp32Rows<4, 4>, 16>(a, p, st);
+    return run_rows<Fp32Rows<4, 8>, 8>(a, p, st);
+}
+
+}  // namespace skm

@@ -1,0 +1,87 @@
+// 8-bit key/value cache: shared by the kernels (k_kv_*.cu) and their entry
+// points (skm_kv.cu).
+#pragma once
+#include <cuda_fp16.h>
+
+#include "skm_internal.cuh"
+
+namespace skm {
+
+constexpr int KV_B = SKM_KV_BLOCK;
+constexpr int KV_SMS = 152;
+// sequences whose prefix sums one launch keeps in shared memory; larger
+// batches take several launches
+constexpr int KV_MAX_SEQS = 1024;
+
+struct KvTokens {
+    const void *x;
+    int64_t token, head;  // strides, elements
+    int wide;             // 16-byte vectors of it are aligned
+};
+
+struct KvCacheArgs {
+    uint8_t *k, *v;
+    float2 *scales;
+    const int32_t *table, *pos, *cu;
+    int heads, d, page, pages, bpp;  // bpp: blocks of a page
+    int batch, cols, tokens, max_tokens;
+    KvTokens K, V;    // write: sources
+    void *outk, *outv;  // read: destinations
+};
+
+cudaError_t launch_kv_write(const KvCacheArgs &a, int dtype, cudaStream_t st);
+cudaError_t launch_kv_read(const KvCacheArgs &a, int dtype, cudaStream_t st);
+
+struct KvAttnArgs {
+    const uint8_t *k, *v;
+    const float2 *scales;
+    const int32_t *table, *pos, *cu;
+    int heads, d, page, pages, bpp, cols, tokens, max_tokens;
+    int b0, nb;  // sequences of this launch
+    int group, causal, window, dtype;
+    float scale_log2;
+    const void *Q;
+    int64_t q_token, q_head;
+    int q_wide;  // 8-byte (f32: 16-byte) vectors of Q are aligned
+    void *out;
+    float *lse;
+    int32_t *status;
+    float *part_cta;   // [grid][2] partial rows of units that CTAs share
+    float *part_warp;  // [grid][warps] rows of the unit that a warp found begun and left
+    int max_tiles;     // row tiles of the longest sequence
+    int whole;         // one CTA a unit (a sequence's row tile and head)
+};
+
+// How one call is run: rows a tile holds, warps, ring stages, CTAs, workspace.
+struct KvRowsPlan {
+    int fp32, rt, nw, ns, whole;
+    int64_t units, grid;
+    size_t smem, part_cta, part_warp;  // bytes
+};
+KvRowsPlan kv_rows_plan(int nb, int heads, int group, int d, int dtype, int max_tokens, int64_t span);
+cudaError_t launch_kv_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st);
+
+// ---- device helpers
+__device__ __forceinline__ float kv_code(uint32_t word, int byte) {
+    // 2^23 + u as a float's bits, minus 2^23 + 128
+    return __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7440 | byte)) - 8388736.0f;
+}
+__device__ __forceinline__ float kv_load(const void *x, int64_t i, int dtype) {
+    if (dtype == SKM_DTYPE_F32) return static_cast<const float *>(x)[i];
+    if (dtype == SKM_DTYPE_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(x)[i]);
+    return __half2float(static_cast<const __half *>(x)[i]);
+}
+__device__ __forceinline__ void kv_store(void *x, int64_t i, float v, int dtype) {
+    if (dtype == SKM_DTYPE_F32) static_cast<float *>(x)[i] = v;
+    else if (dtype == SKM_DTYPE_BF16) static_cast<__nv_bfloat16 *>(x)[i] = __float2bfloat16_rn(v);
+    else static_cast<__half *>(x)[i] = __float2half_rn(v);
+}
+__device__ __forceinline__ int kv_clamp(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
+
+// the rows [x, x + y) of sequence b in the token tensors
+__device__ __forceinline__ int2 kv_rows_of(const int32_t *cu, int b, int tokens, int most) {
+    const int c0 = kv_clamp(cu[b], 0, tokens), c1 = kv_clamp(cu[b + 1], c0, tokens);
+    return make_int2(c0, min(c1 - c0, most));
+}
+
+}  // namespace skm
