@@ -33,6 +33,11 @@ constexpr float M_NONE = -3.0e38f;  // the reference before the first logit
 constexpr float M_SLACK = 15.0f, M_BELOW = 7.0f;
 constexpr float LN2 = 0.69314718055994531f;
 
+__device__ __forceinline__ float ex2(float x) {  // 2^x, 2 units in the last place, subnormal results 0
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 __device__ __forceinline__ uint32_t su32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ bool bar_try(uint32_t b, uint32_t parity) {
     uint32_t ok;
@@ -344,6 +349,264 @@ struct Fp32Rows {
     }
 };
 
+// ---- 16-bit queries: mma.m16n8k16, f16 operands, fp32 sums
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// codes of bytes 0, 1 / 2, 3 of a word as two f16: 1024 + u as bits, minus 1152
+__device__ __forceinline__ uint32_t codes_f16(uint32_t word, uint32_t sel) {
+    const uint32_t x = __byte_perm(word, 0x64646464u, sel);
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&x), __half2half2(__ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+// operand A of a 16 x 16 tile of codes: x rows 0..7, y rows 8..15, four
+// consecutive bytes a lane (columns 2c, 2c + 1, 2c + 8, 2c + 9 of the tile)
+__device__ __forceinline__ void codes_a(uint32_t x, uint32_t y, uint32_t (&a)[4]) {
+    a[0] = codes_f16(x, 0x4140);
+    a[1] = codes_f16(y, 0x4140);
+    a[2] = codes_f16(x, 0x4342);
+    a[3] = codes_f16(y, 0x4342);
+}
+
+// Rows of one warp on tensor cores, transposed: S^T = K q^T and o^T = V^T p^T
+// (16 tokens or dims x 8 rows x 16), so a tile of 8 rows wastes nothing when
+// the heads of a group are 8.  Both cache layouts are read by ldmatrix, 512
+// consecutive bytes at a time, and a lane's word is the operand's columns: of
+// the dims of a 16-dim chunk, lane column c holds 4c .. 4c + 3 (the queries
+// are laid out to match); of the tokens, the cache's byte order makes it 2c,
+// 2c + 1, 2c + 8, 2c + 9, the operand's own.  p^T comes from S^T by movmatrix.
+// bf16 queries become f16 exactly after scaling a row by a power of two (values
+// below 2^-25 of the row's largest, whose products round away, aside).
+// DC: 16-dim chunks at most, NT: tiles of 8 rows.
+template <int DC, int NT>
+struct MmaRows {
+    static constexpr int RT = 8 * NT;
+    static constexpr bool QMEM = NT * DC >= 32;  // the queries' operands wait in shared memory
+    static size_t __host__ __device__ scratch(int) { return QMEM ? (size_t)NT * DC * 2 * 32 * 4 : 0; }
+    float o[NT][DC][4], m[NT][2], l[NT][2], fac[NT][2];
+    uint32_t q[QMEM ? 1 : NT][QMEM ? 1 : DC][2];
+    uint2 *qmem;
+
+    __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int row0, int h, int r0, uint8_t *mem,
+                                          int lane) {
+        const int g = lane >> 2, c = lane & 3, nc = a.d / KV_B;
+        qmem = reinterpret_cast<uint2 *>(mem);
+        __syncwarp();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int rr = r0 + 8 * t + g;
+            const bool in = rr < s.n * a.group;
+            const uint16_t *x = static_cast<const uint16_t *>(a.Q);
+            if (in) x += (int64_t)(row0 + rr / a.group) * a.q_token + (int64_t)(h * a.group + rr % a.group) * a.q_head + 4 * c;
+            uint2 raw[DC];
+            float top = 0.0f;
+#pragma unroll
+            for (int w = 0; w < DC; ++w) {
+                raw[w] = make_uint2(0, 0);
+                if (in && w < nc) {
+                    if (a.q_wide) {
+                        raw[w] = *reinterpret_cast<const uint2 *>(x + 16 * w);
+                    } else {
+                        raw[w].x = x[16 * w] | (uint32_t)x[16 * w + 1] << 16;
+                        raw[w].y = x[16 * w + 2] | (uint32_t)x[16 * w + 3] << 16;
+                    }
+                }
+            }
+            float mul = 1.0f, back = 1.0f;
+            if (a.dtype == SKM_DTYPE_BF16) {
+#pragma unroll
+                for (int w = 0; w < DC; ++w) {
+                    top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw[w].x << 16)), fabsf(__uint_as_float(raw[w].x & 0xffff0000u))));
+                    top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw[w].y << 16)), fabsf(__uint_as_float(raw[w].y & 0xffff0000u))));
+                }
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const uint32_t ex = __float_as_uint(top) >> 23;
+                if (ex > 0 && ex < 255) {
+                    const uint32_t e = ex > 253 ? 253 : ex;
+                    mul = __uint_as_float((254 - e) << 23);
+                    back = __uint_as_float(e << 23);
+                }
+            }
+#pragma unroll
+            for (int w = 0; w < DC; ++w) {
+                uint32_t b0 = raw[w].x, b1 = raw[w].y;
+                if (a.dtype == SKM_DTYPE_BF16) {
+                    const __half2 x0 = __floats2half2_rn(__uint_as_float(b0 << 16) * mul, __uint_as_float(b0 & 0xffff0000u) * mul);
+                    const __half2 x1 = __floats2half2_rn(__uint_as_float(b1 << 16) * mul, __uint_as_float(b1 & 0xffff0000u) * mul);
+                    b0 = *reinterpret_cast<const uint32_t *>(&x0);
+                    b1 = *reinterpret_cast<const uint32_t *>(&x1);
+                }
+                if constexpr (QMEM) qmem[(t * DC + w) * 32 + lane] = make_uint2(b0, b1);
+                else q[t][w][0] = b0, q[t][w][1] = b1;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[t][w][i] = 0.0f;
+            }
+            back *= a.scale_log2;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                fac[t][i] = __shfl_sync(0xffffffffu, back, (2 * c + i) * 4);
+                m[t][i] = M_NONE;
+                l[t][i] = 0.0f;
+            }
+        }
+        __syncwarp();
+    }
+
+    __device__ __forceinline__ void block(const KvAttnArgs &a, const Seq &s, int r0, const uint8_t *K, const uint8_t *V,
+                                          int blk, float ks, float lvs, float ivs, bool mask, int lane) {
+        const int g = lane >> 2, c = lane & 3, nc = a.d / KV_B;
+        float x[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[t][i] = 0.0f;
+        const uint32_t ka = su32(K) + lane * 16, va = su32(V) + lane * 16;
+#pragma unroll
+        for (int w = 0; w < DC; w += 2) {
+            if (w >= nc) break;
+            uint32_t r[4], f[4];
+            ldsm4(ka + w * 256, r);
+            codes_a(r[0], r[1], f);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if constexpr (QMEM) {
+                    const uint2 b = qmem[(t * DC + w) * 32 + lane];
+                    mma16816(x[t], f, b.x, b.y);
+                } else {
+                    mma16816(x[t], f, q[t][w][0], q[t][w][1]);
+                }
+            }
+            if (w + 1 >= nc) break;
+            codes_a(r[2], r[3], f);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                if constexpr (QMEM) {
+                    const uint2 b = qmem[(t * DC + w + 1) * 32 + lane];
+                    mma16816(x[t], f, b.x, b.y);
+                } else {
+                    mma16816(x[t], f, q[t][w + 1][0], q[t][w + 1][1]);
+                }
+            }
+        }
+        bool over = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[t][i] = fmaf(x[t][i], fac[t][i & 1] * ks, lvs);
+                if (mask) {
+                    const int j = blk * KV_B + g + 8 * (i >> 1), rr = r0 + 8 * t + 2 * c + (i & 1);
+                    if (j > last_of(a, s, rr) || j < first_of(a, s, rr)) x[t][i] = -INFINITY;
+                }
+                over |= x[t][i] > m[t][i & 1] + M_SLACK;
+            }
+        if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float top = fmaxf(x[t][i], x[t][i + 2]);
+#pragma unroll
+                    for (int b = 4; b < 32; b <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, b));
+                    const float to = top > m[t][i] + M_SLACK ? top - M_BELOW : m[t][i];
+                    const float f = exp2f(m[t][i] - to);
+                    m[t][i] = to;
+                    l[t][i] *= f;
+#pragma unroll
+                    for (int w = 0; w < DC; ++w) o[t][w][i] *= f, o[t][w][i + 2] *= f;
+                }
+        }
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = ex2(x[t][i] - m[t][i & 1]);
+            l[t][0] = fmaf(p[0] + p[2], ivs, l[t][0]);
+            l[t][1] = fmaf(p[1] + p[3], ivs, l[t][1]);
+            const __half2 lo = __floats2half2_rn(p[0], p[1]), hi = __floats2half2_rn(p[2], p[3]);
+            pb[t][0] = transpose8x8(*reinterpret_cast<const uint32_t *>(&lo));
+            pb[t][1] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hi));
+        }
+#pragma unroll
+        for (int w = 0; w < DC; w += 2) {
+            if (w >= nc) break;
+            uint32_t r[4], f[4];
+            ldsm4(va + w * 256, r);  // of an odd last chunk the second half is not used
+            codes_a(r[0], r[1], f);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16816(o[t][w], f, pb[t][0], pb[t][1]);
+            if (w + 1 >= nc) break;
+            codes_a(r[2], r[3], f);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) mma16816(o[t][w + 1], f, pb[t][0], pb[t][1]);
+        }
+    }
+
+    __device__ __forceinline__ void close(int) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int b = 4; b < 32; b <<= 1) l[t][i] += __shfl_xor_sync(0xffffffffu, l[t][i], b);
+    }
+    __device__ __forceinline__ void poison() {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) l[t][0] = l[t][1] = NAN;
+    }
+    __device__ __forceinline__ void put(const KvAttnArgs &a, float *dst, int lane) const {
+        const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = 8 * t + 2 * c + i;
+                if (g == 0) dst[2 * r] = m[t][i], dst[2 * r + 1] = l[t][i];
+#pragma unroll
+                for (int w = 0; w < DC; ++w) {
+                    if (w >= a.d / KV_B) break;
+                    dst[part_head<RT>() + r * a.d + 16 * w + g] = o[t][w][i];
+                    dst[part_head<RT>() + r * a.d + 16 * w + g + 8] = o[t][w][i + 2];
+                }
+            }
+    }
+    __device__ __forceinline__ void finish(const KvAttnArgs &a, const Seq &s, int row0, int h, int r0, int lane) const {
+        const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int rr = r0 + 8 * t + 2 * c + i;
+                if (rr >= s.n * a.group) continue;
+                const int64_t row = row_index(a, row0, h, rr);
+                const float inv = l[t][i] == 0.0f ? 0.0f : 1.0f / l[t][i];
+#pragma unroll
+                for (int w = 0; w < DC; ++w) {
+                    if (w >= a.d / KV_B) break;
+                    kv_store(a.out, row * a.d + 16 * w + g, o[t][w][i] * inv, a.dtype);
+                    kv_store(a.out, row * a.d + 16 * w + g + 8, o[t][w][i + 2] * inv, a.dtype);
+                }
+                if (g == 0 && a.lse) a.lse[row] = l[t][i] == 0.0f ? -INFINITY : LN2 * (m[t][i] + log2f(l[t][i]));
+            }
+    }
+};
+
 // A CTA's records of the units that its warps did not finish alone, in the
 // line's order: [2 w] the unit that warp w found begun and left (part_warp), [2 w +
 // 1] the one open at its end.
@@ -368,7 +631,7 @@ __host__ __device__ __forceinline__ Smem smem_of(int nb, int d, int nw, int ns) 
     s.ring = (s.scratch + nw * Rows::scratch(d) + 127) & ~size_t(127);
     // after the loop the ring's memory holds a part of every warp
     const size_t ring = (size_t)nw * ns * 2 * KV_B * d, parts = (size_t)nw * part_floats<Rows::RT>(d) * 4;
-    s.total = s.ring + (ring > parts ? ring : parts);
+    s.total = s.ring + (ring > parts ? ring : parts) + 256;  // ldmatrix reads chunks in pairs
     return s;
 }
 
@@ -700,25 +963,42 @@ KvRowsPlan plan_rows(int nb, int heads, int group, int d, int max_tokens, int64_
 
 }  // namespace
 
-// span: blocks times 16 that a unit may cover
+// The variants.  fp32 queries: one row or four.  16-bit queries: tiles of 8,
+// 16 or 32 rows (d > 128: 8 or 16, the sums of a tile are held in registers);
+// warps as many as the registers of that tile allow.
+#define KV_ROWS_VARIANTS(X)                                                                              \
+    X(1, 1, 64, (Fp32Rows<1, 2>), 16) X(1, 1, 128, (Fp32Rows<1, 4>), 16) X(1, 1, 256, (Fp32Rows<1, 8>), 8)  \
+    X(1, 4, 64, (Fp32Rows<4, 2>), 16) X(1, 4, 128, (Fp32Rows<4, 4>), 16) X(1, 4, 256, (Fp32Rows<4, 8>), 8)  \
+    X(0, 8, 64, (MmaRows<4, 1>), 16) X(0, 8, 128, (MmaRows<8, 1>), 16) X(0, 8, 256, (MmaRows<16, 1>), 8)    \
+    X(0, 16, 64, (MmaRows<4, 2>), 16) X(0, 16, 128, (MmaRows<8, 2>), 8) X(0, 16, 256, (MmaRows<16, 2>), 8)  \
+    X(0, 32, 64, (MmaRows<4, 4>), 8) X(0, 32, 128, (MmaRows<8, 4>), 8)
+
+#define KV_UNPACK(...) __VA_ARGS__
+
+// span: positions that a unit's items may cover
 KvRowsPlan kv_rows_plan(int nb, int heads, int group, int d, int dtype, int max_tokens, int64_t span) {
-    KvRowsPlan p;
-    const int nw = d <= 128 ? 16 : 8;
-    if ((int64_t)max_tokens * group == 1) p = plan_rows<Fp32Rows<1, 8>>(nb, heads, group, d, max_tokens, span, nw);
-    else p = plan_rows<Fp32Rows<4, 8>>(nb, heads, group, d, max_tokens, span, nw);
-    p.fp32 = 1;
-    return p;
+    const int64_t rows = (int64_t)max_tokens * group;
+    const int fp32 = dtype == SKM_DTYPE_F32;
+    const int rt = fp32 ? (rows == 1 ? 1 : 4) : (rows <= 8 ? 8 : rows <= 16 || d > 128 ? 16 : 32);
+    const int dmax = d <= 64 ? 64 : d <= 128 ? 128 : 256;
+#define KV_PLAN(FP32, RT, D, ROWS, NW)                                                          \
+    if (fp32 == FP32 && rt == RT && dmax == D) {                                                \
+        KvRowsPlan p = plan_rows<KV_UNPACK ROWS>(nb, heads, group, d, max_tokens, span, NW);    \
+        p.fp32 = FP32;                                                                          \
+        return p;                                                                               \
+    }
+    KV_ROWS_VARIANTS(KV_PLAN)
+#undef KV_PLAN
+    return KvRowsPlan{};
 }
 
 cudaError_t launch_kv_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) {
-    if (p.rt == 1) {
-        if (a.d <= 64) return run_rows<Fp32Rows<1, 2>, 16>(a, p, st);
-        if (a.d <= 128) return run_rows<Fp32Rows<1, 4>, 16>(a, p, st);
-        return run_rows<Fp32Rows<1, 8>, 8>(a, p, st);
-    }
-    if (a.d <= 64) return run_rows<Fp32Rows<4, 2>, 16>(a, p, st);
-    if (a.d <= 128) return run_rows<Fp32Rows<4, 4>, 16>(a, p, st);
-    return run_rows<Fp32Rows<4, 8>, 8>(a, p, st);
+    const int dmax = a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256;
+#define KV_RUN(FP32, RT, D, ROWS, NW) \
+    if (p.fp32 == FP32 && p.rt == RT && dmax == D) return run_rows<KV_UNPACK ROWS, NW>(a, p, st);
+    KV_ROWS_VARIANTS(KV_RUN)
+#undef KV_RUN
+    return cudaErrorInvalidValue;
 }
 
 }  // namespace skm
