@@ -1,0 +1,646 @@
+// Attention over the 8-bit cache for many query rows (prompt chunks) on
+// tcgen05: 16-bit queries, d <= 128.
+//
+// A CTA takes 256 query rows (token-major, then the heads of a group) of one
+// sequence and key/value head as two tiles of 128, and walks the keys they see in
+// tiles of 128 positions (8 blocks of the cache).  The codes are exact in f16, so
+// both products run in kind::f16 and the block scales stay out of the
+// operands: the key scale multiplies the logits of its block, the value scale
+// is added to them as log2 s_v (o = sum p c_v, l = sum p / s_v; the formulas of
+// k_kv_rows.cu, the running reference m included).
+//
+//   warps 0-3, 4-7  softmax of tile 0 / 1, one thread a row: S from TMEM in
+//                   pieces of a block, p = 2^(s f + c) to f16, P back to TMEM
+//                   over the columns S held (the A operand of the next product)
+//   warps 8-14      converters: a block of keys (or values) at a time from
+//                   global memory, one block ahead in registers, to f16 in the
+//                   128-byte-swizzled operand layout
+//   warp 15         MMA issuer: P0 V, Q0 K', P1 V, Q1 K' in turn, so the tensor
+//                   cores work on one tile while the other's softmax runs
+//
+// TMEM: S0/P0, S1/P1 (128 columns each), O0, O1 (DH columns each).  The first
+// pass over a tile's logits assumes that m need not move and keeps P in
+// registers; a block whose sum exceeds 2^15 (m has to be set or moved, at a row's first
+// tile and rarely after it) sends the warp through a maximum, a rescaling of O
+// and a second pass.  Shared memory: Q, and rings of K and V tiles.
+//
+// Few CTAs (short prompts): the keys are split over CTAs as well, and
+// kv_prompt_join_kernel merges the parts in order.
+#include "skm_kv_dev.cuh"
+
+namespace skm {
+
+namespace {
+
+constexpr int QT = 128, KT = 128, KBLK = KT / KV_B;  // rows of a tile, keys of a tile, blocks of it
+constexpr int CONV = 7, CONV_WARP0 = 8, MMA_WARP = 15, THREADS = 512;
+constexpr int INFO = 8;  // tiles whose scales are kept (more than the K ring holds)
+
+template <int DH>
+struct Lay {
+    static constexpr int STAGES = DH <= 64 ? 4 : 2;
+    static constexpr int TILE = QT * DH * 2;  // bytes of a Q, K or V tile
+    static constexpr int q = 0, k = 2 * TILE, v = k + STAGES * TILE, info = v + STAGES * TILE;
+    static constexpr int bars = info + INFO * KBLK * 16, slots = bars + 8 * (4 * STAGES + 8), total = slots + 16 + 1024;
+    static constexpr uint32_t O = 2 * KT;  // TMEM column of O0
+};
+
+__device__ __forceinline__ void arrive(uint32_t b) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(b) : "memory");
+}
+// bounded, and cut short when another role gave up
+__device__ __forceinline__ bool wait(uint32_t b, uint32_t parity, volatile int32_t *gone) {
+    if (bar_try(b, parity)) return true;
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    for (uint32_t i = 1;; ++i) {
+        if (bar_try(b, parity)) return true;
+        if ((i & 63) == 0) {
+            if (*gone) return false;
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+            if (t - t0 > WAIT_NS) {
+                *gone = 1;
+                return false;
+            }
+        }
+    }
+}
+// by a whole warp, with one answer
+__device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, volatile int32_t *gone) {
+    return __all_sync(0xffffffffu, wait(b, parity, gone));
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void commit(uint32_t b) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(b) : "memory");
+}
+// K-major operand, 128-byte swizzle: rows of 128 bytes, groups of 8 rows
+__device__ __forceinline__ uint64_t operand(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+           (uint64_t)2 << 61;
+}
+constexpr uint32_t idesc(int n) {  // f16 x f16 -> f32, M = 128, both K-major
+    return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(QT >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(id), "r"(add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(id), "r"(add)
+        : "memory");
+}
+// 16 columns; valid after ld_wait on the same registers
+__device__ __forceinline__ void ld16(uint32_t addr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void ld_wait(uint32_t (&v)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]),
+                   "+r"(v[15])
+                 :
+                 : "memory");
+}
+__device__ __forceinline__ void st16(uint32_t addr, const uint32_t *v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n\t.reg .b64 ra, rb, rc, rd;\n\t"
+        "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmov.b64 rc, {%6, %7};\n\t"
+        "fma.rn.f32x2 rd, ra, rb, rc;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 ra, rb, rd;\n\t"
+        "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+        "add.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ void st_shared(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// A part: 256 x (m, l), then 256 rows of d sums
+__host__ __device__ __forceinline__ int64_t prompt_part(int d) { return 2 * QT * (int64_t)(2 + d); }
+
+// A query row to f16 in its tile's operand; returns what its logits are
+// multiplied by (k_kv_rows.cu: bf16 rows are scaled by a power of two)
+template <int DH>
+__device__ __forceinline__ float load_row(const KvAttnArgs &a, const uint16_t *x, bool in, uint32_t tile, int row) {
+    float top = 0.0f, mul = 1.0f, back = 1.0f;
+    const auto get = [&](int i, uint32_t (&w)[4]) {  // dims 8 i .. 8 i + 7
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = 0;
+        if (!in || 8 * i >= a.d) return;
+        if (a.q_wide) {
+            const uint2 u = *reinterpret_cast<const uint2 *>(x + 8 * i), v = *reinterpret_cast<const uint2 *>(x + 8 * i + 4);
+            w[0] = u.x, w[1] = u.y, w[2] = v.x, w[3] = v.y;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = x[8 * i + 2 * j] | (uint32_t)x[8 * i + 2 * j + 1] << 16;
+        }
+    };
+    const bool bf = a.dtype == SKM_DTYPE_BF16;
+    if (bf) {
+#pragma unroll 4
+        for (int i = 0; i < DH / 8; ++i) {
+            uint32_t w[4];
+            get(i, w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[j] << 16)), fabsf(__uint_as_float(w[j] & 0xffff0000u))));
+        }
+        const uint32_t ex = __float_as_uint(top) >> 23;
+        if (ex > 0 && ex < 255) {
+            const uint32_t e = ex > 253 ? 253 : ex;
+            mul = __uint_as_float((254 - e) << 23);
+            back = __uint_as_float(e << 23);
+        }
+    }
+#pragma unroll 4
+    for (int i = 0; i < DH / 8; ++i) {
+        uint32_t w[4];
+        get(i, w);
+        if (bf) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[j] = pack(__uint_as_float(w[j] << 16) * mul, __uint_as_float(w[j] & 0xffff0000u) * mul);
+        }
+        st_shared(tile + (i >> 3) * (QT * 128) + row * 128 + (((i & 7) ^ (row & 7)) << 4), w[0], w[1], w[2], w[3]);
+    }
+    return back * a.scale_log2;
+}
+
+template <int DH>
+__global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_constant__ KvAttnArgs a, int splits, float *parts) {
+    using L = Lay<DH>;
+    constexpr int ST = L::STAGES;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint8_t *smem = smem_raw + ((1024 - (su32(smem_raw) & 1023)) & 1023);  // swizzle atoms
+    const uint32_t sm = su32(smem);
+    const auto bar = [&](int i) { return sm + L::bars + 8 * i; };
+    const auto k_full = [&](int s) { return bar(s); };
+    const auto k_free = [&](int s) { return bar(ST + s); };
+    const auto v_full = [&](int s) { return bar(2 * ST + s); };
+    const auto v_free = [&](int s) { return bar(3 * ST + s); };
+    const auto s_full = [&](int q) { return bar(4 * ST + q); };
+    const auto p_full = [&](int q) { return bar(4 * ST + 2 + q); };
+    const auto o_done = [&](int q) { return bar(4 * ST + 4 + q); };
+    const uint32_t q_full = bar(4 * ST + 6), drain = bar(4 * ST + 7);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::slots);
+    volatile int32_t *gone = reinterpret_cast<volatile int32_t *>(smem + L::slots + 4);
+    float4 *info = reinterpret_cast<float4 *>(smem + L::info);  // (k scale, log2 v scale, 1 / v scale, there)
+
+    // the unit: later rows first (causal: they see the most)
+    const int tiles = (a.max_tiles + 1) / 2;  // pairs of row tiles
+    int u = blockIdx.x;
+    const int split = u % splits;
+    u /= splits;
+    const int h = u % a.heads;
+    u /= a.heads;
+    const int bi = u % a.nb, pair = tiles - 1 - u / a.nb, b = a.b0 + bi;
+    const Seq s = seq_of(a, b);
+    const int rows = s.n * a.group, r0 = pair * 2 * QT;
+    if (r0 >= rows) return;
+    const int row0 = kv_rows_of(a.cu, b, a.tokens, a.max_tokens).x;
+    const int r1 = min(r0 + 2 * QT, rows) - 1;
+    const int nq = r1 - r0 >= QT ? 2 : 1;
+    // positions that some row sees, the tiles of them, this split's tiles
+    const int first = first_of(a, s, r0), last = last_of(a, s, r1);
+    const int t_lo = first / KT, t_all = last >= first ? last / KT + 1 - t_lo : 0;
+    const int t0 = t_lo + (int)((int64_t)t_all * split / splits);
+    const int n = t_lo + (int)((int64_t)t_all * (split + 1) / splits) - t0;
+
+    if (tid == 0) {
+        for (int i = 0; i < ST; ++i) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(k_full(i)), "r"(KBLK) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(v_full(i)), "r"(KBLK) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(k_free(i)), "r"(1) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(v_free(i)), "r"(1) : "memory");
+        }
+        for (int q = 0; q < 2; ++q) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s_full(q)), "r"(1) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(p_full(q)), "r"(4) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(o_done(q)), "r"(1) : "memory");
+        }
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(q_full), "r"(8) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(drain), "r"(1) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *gone = 0;
+    }
+    // blocks that are not there leave their operand rows as they are: finite
+    for (int i = tid * 16; i < 2 * ST * L::TILE; i += THREADS * 16) st_shared(sm + L::k + i, 0, 0, 0, 0);
+    fence_async();
+    if (warp == MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(tmem_slot)), "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp < CONV_WARP0) {  // ------------------------------------------ softmax
+        const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row;
+        const bool in = r < rows;
+        const uint16_t *x = static_cast<const uint16_t *>(a.Q);
+        if (in) x += (int64_t)(row0 + r / a.group) * a.q_token + (int64_t)(h * a.group + r % a.group) * a.q_head;
+        const float fac = load_row<DH>(a, x, in, sm + L::q + q * L::TILE, row);
+        fence_async();
+        __syncwarp();
+        if (lane == 0) arrive(q_full);
+        const int hi = in ? last_of(a, s, r) : -1, lo = in ? first_of(a, s, r) : 0;
+        // rows of the warp see [low, high] whole
+        const int high = __shfl_sync(0xffffffffu, hi, 0), low = __reduce_max_sync(0xffffffffu, lo);
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t S = tmem + lanes + q * KT, O = tmem + lanes + L::O + q * DH;
+        float m = M_NONE, l = 0.0f;
+        bool ok = true;
+        for (int j = 0; j < n && q < nq; ++j) {
+            if (!warp_wait(s_full(q), j & 1, gone)) {
+                ok = false;
+                break;
+            }
+            fence_after();
+            const float4 *inf = info + (j & (INFO - 1)) * KBLK;
+            const int c0 = (t0 + j) * KT;
+            const bool whole = c0 >= low && c0 + KT - 1 <= high &&
+                               __all_sync(0xffffffffu, inf[lane & (KBLK - 1)].w != 0.0f);
+            uint32_t P[KT / 2];
+            float add = 0.0f;
+            for (int pass = 0;; ++pass) {
+                uint32_t v[2][16];
+                float most = 0.0f;
+                add = 0.0f;
+                ld16(S, v[0]);
+#pragma unroll
+                for (int k = 0; k < KBLK; ++k) {
+                    ld_wait(v[k & 1]);
+                    if (k + 1 < KBLK) ld16(S + (k + 1) * KV_B, v[(k + 1) & 1]);
+                    const float4 f4 = inf[k];
+                    const float f = fac * f4.x, c = f4.y - m;
+                    float p[16];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        const float2 t = fma2(make_float2(__uint_as_float(v[k & 1][i]), __uint_as_float(v[k & 1][i + 1])),
+                                              make_float2(f, f), make_float2(c, c));
+                        p[i] = t.x, p[i + 1] = t.y;
+                    }
+                    if (!whole) {
+                        const int at = c0 + k * KV_B;
+                        const int upto = f4.w != 0.0f ? hi - at : -1, from = lo - at;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) p[i] = i <= upto && i >= from ? p[i] : -INFINITY;
+                    }
+                    float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        const float2 e = make_float2(ex2(p[i]), ex2(p[i + 1]));
+                        sum = add2(sum, e);
+                        P[k * 8 + i / 2] = pack(e.x, e.y);
+                    }
+                    const float all = sum.x + sum.y;
+                    most = fmaxf(most, all);
+                    add = fmaf(all, f4.z, add);
+                }
+                if (pass == 1 || !__any_sync(0xffffffffu, most > 32768.0f)) break;
+                // the rows' maxima, and with them new references
+                float top = -INFINITY;
+                for (int k = 0; k < KBLK; ++k) {
+                    ld16(S + k * KV_B, v[0]);
+                    ld_wait(v[0]);
+                    const float4 f4 = inf[k];
+                    const int at = c0 + k * KV_B, upto = f4.w != 0.0f ? hi - at : -1, from = lo - at;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (i <= upto && i >= from) top = fmaxf(top, fmaf(__uint_as_float(v[0][i]), fac * f4.x, f4.y));
+                }
+                const float to = top > m + 8.0f ? top - M_BELOW : m;
+                const float f = ex2(m - to);
+                m = to;
+                l *= f;
+                if (j > 0) {
+                    if (!warp_wait(o_done(q), (j - 1) & 1, gone)) {
+                        ok = false;
+                        break;
+                    }
+                    fence_after();
+                    for (int k = 0; k < DH / 16; ++k) {
+                        ld16(O + k * 16, v[0]);
+                        ld_wait(v[0]);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[0][i] = __float_as_uint(__uint_as_float(v[0][i]) * f);
+                        st16(O + k * 16, v[0]);
+                    }
+                    st_wait();
+                }
+            }
+            if (!ok) break;
+            l += add;
+#pragma unroll
+            for (int k = 0; k < KT / 2; k += 16) st16(S + k, P + k);
+            st_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(p_full(q));
+        }
+        if (q < nq) {
+            if (ok && n > 0) {
+                ok = warp_wait(o_done(q), (n - 1) & 1, gone);
+                fence_after();
+            }
+            if (!ok) {
+                l = NAN;
+                if (lane == 0 && a.status) *a.status = 1;
+            }
+            float *part = parts ? parts + (int64_t)blockIdx.x * prompt_part(a.d) : nullptr;
+            const int pr = q * QT + row;
+            if (part) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);
+            const int64_t at = in ? row_index(a, row0, h, r) : 0;
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            for (int k = 0; k < DH / 16; ++k) {
+                if (16 * k >= a.d) break;
+                uint32_t v[16];
+                if (ok && n > 0) {
+                    ld16(O + k * 16, v);
+                    ld_wait(v);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = 0;
+                }
+                if (!in) continue;
+                if (part) {
+                    float4 *dst = reinterpret_cast<float4 *>(part + 4 * QT + (int64_t)pr * a.d + 16 * k);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        dst[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
+                                             __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+                    continue;
+                }
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float x0 = __uint_as_float(v[2 * i]) * inv, x1 = __uint_as_float(v[2 * i + 1]) * inv;
+                    if (a.dtype == SKM_DTYPE_BF16) {
+                        const __nv_bfloat162 y = __floats2bfloat162_rn(x0, x1);
+                        w[i] = *reinterpret_cast<const uint32_t *>(&y);
+                    } else {
+                        w[i] = pack(x0, x1);
+                    }
+                }
+                uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + at * a.d + 16 * k);
+                dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            }
+            if (in && !part && a.lse) a.lse[at] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
+        }
+    } else if (warp < MMA_WARP) {  // ------------------------------------- converters
+        // tasks: per tile 8 blocks of keys, then 8 of values; warp w takes w, w + 7, ...
+        const int tasks = n * 2 * KBLK, cw = warp - CONV_WARP0;
+        constexpr int NV = DH / 32;
+        struct Ahead {  // 32 of the warp's tasks, one a lane
+            int at;
+            float2 sc;
+        };
+        const auto look = [&](int task) {
+            Ahead w;
+            w.at = -1;
+            w.sc = make_float2(0.0f, 0.0f);
+            if (task < tasks) {
+                const int blk = (t0 + task / (2 * KBLK)) * KBLK + task % KBLK;
+                if (blk * KV_B <= last && blk * KV_B + KV_B > first) {
+                    const int pg = a.table[(int64_t)b * a.cols + blk / a.bpp];
+                    if (pg >= 0 && pg < a.pages) {
+                        w.at = (pg * a.heads + h) * a.bpp + blk % a.bpp;
+                        w.sc = a.scales[w.at];
+                    }
+                }
+            }
+            return w;
+        };
+        const auto load = [&](int task, int at, uint4 (&raw)[NV]) {
+            const uint4 *p = reinterpret_cast<const uint4 *>((task & KBLK ? a.v : a.k) + (int64_t)at * (KV_B * a.d));
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (at >= 0 && lane + 32 * i < a.d) raw[i] = __ldg(p + lane + 32 * i);
+        };
+        Ahead cur = look(cw + CONV * lane), next = look(cw + CONV * (32 + lane));
+        uint4 raw[NV], coming[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[i] = coming[i] = make_uint4(0, 0, 0, 0);
+        int at = __shfl_sync(0xffffffffu, cur.at, 0);
+        if (cw < tasks) load(cw, at, raw);
+        for (int task = cw, i = 0; task < tasks; task += CONV, ++i) {
+            const int slot = i & 31;
+            const float2 sc = make_float2(__shfl_sync(0xffffffffu, cur.sc.x, slot), __shfl_sync(0xffffffffu, cur.sc.y, slot));
+            if (slot == 31) {
+                cur = next;
+                next = look(task + CONV * (33 + lane));
+            }
+            const int at_next = __shfl_sync(0xffffffffu, cur.at, (i + 1) & 31);
+            if (task + CONV < tasks) load(task + CONV, at_next, coming);
+            const int j = task / (2 * KBLK), st = j % ST, blk = task % KBLK;
+            const bool vals = task & KBLK;
+            if (!warp_wait(vals ? v_free(st) : k_free(st), ((j / ST) & 1) ^ 1, gone)) break;
+            if (!vals) {
+                if (lane == 0)
+                    info[(j & (INFO - 1)) * KBLK + blk] =
+                        at >= 0 ? make_float4(sc.x, sc.y > 0.0f ? log2f(sc.y) : 0.0f, sc.y > 0.0f ? 1.0f / sc.y : 1.0f, 1.0f)
+                                : make_float4(0.0f, 0.0f, 1.0f, 0.0f);
+            }
+            if (at >= 0) {
+                const uint32_t base = sm + (vals ? L::v : L::k) + st * L::TILE;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    const int e = lane + 32 * k;
+                    if (e >= a.d) break;
+                    const uint4 c = raw[k];
+                    uint32_t f[8];
+                    f[0] = codes_f16(c.x, 0x4140), f[1] = codes_f16(c.x, 0x4342);
+                    f[2] = codes_f16(c.y, 0x4140), f[3] = codes_f16(c.y, 0x4342);
+                    f[4] = codes_f16(c.z, 0x4140), f[5] = codes_f16(c.z, 0x4342);
+                    f[6] = codes_f16(c.w, 0x4140), f[7] = codes_f16(c.w, 0x4342);
+                    if (!vals) {  // e: chunk e / 16 of dims, token e % 16
+                        const int row = blk * KV_B + (e & 15), w = e >> 4, ch = (w & 3) * 2;
+                        const uint32_t p = base + (w >> 2) * (KT * 128) + row * 128;
+                        st_shared(p + ((ch ^ (row & 7)) << 4), f[0], f[1], f[2], f[3]);
+                        st_shared(p + (((ch + 1) ^ (row & 7)) << 4), f[4], f[5], f[6], f[7]);
+                    } else {  // e: dim; even words tokens 0..7, odd 8..15
+                        const int ch = (blk & 3) * 2;
+                        const uint32_t p = base + (blk >> 2) * (DH * 128) + e * 128;
+                        st_shared(p + ((ch ^ (e & 7)) << 4), f[0], f[2], f[4], f[6]);
+                        st_shared(p + (((ch + 1) ^ (e & 7)) << 4), f[1], f[3], f[5], f[7]);
+                    }
+                }
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) arrive(vals ? v_full(st) : k_full(st));
+            at = at_next;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) raw[k] = coming[k];
+        }
+    } else if (lane == 0 && n > 0) {  // ------------------------------------ MMA issuer
+        bool ok = wait(q_full, 0, gone), issued = false;
+        const auto qk = [&](int q, int st) {
+#pragma unroll
+            for (int k = 0; k < DH / 16; ++k)
+                mma_ss(tmem + q * KT, operand(sm + L::q + q * L::TILE + (k >> 2) * (QT * 128)) + 2 * (k & 3),
+                       operand(sm + L::k + st * L::TILE + (k >> 2) * (KT * 128)) + 2 * (k & 3), idesc(KT), k > 0);
+            issued = true;
+            commit(s_full(q));
+        };
+        if (ok) ok = wait(k_full(0), 0, gone);
+        if (ok) {
+            fence_after();
+            for (int q = 0; q < nq; ++q) qk(q, 0);
+            commit(k_free(0));
+        }
+        for (int j = 0; j < n && ok; ++j) {
+            const int st = j % ST, kst = (j + 1) % ST;
+            for (int q = 0; q < nq; ++q) {
+                if (!(ok = wait(p_full(q), j & 1, gone))) break;
+                if (q == 0 && !(ok = wait(v_full(st), (j / ST) & 1, gone))) break;
+                fence_after();
+#pragma unroll
+                for (int k = 0; k < KT / 16; ++k)
+                    mma_ts(tmem + L::O + q * DH, tmem + q * KT + 8 * k,
+                           operand(sm + L::v + st * L::TILE + (k >> 2) * (DH * 128)) + 2 * (k & 3), idesc(DH), j > 0 || k > 0);
+                if (q == nq - 1) commit(v_free(st));
+                commit(o_done(q));  // last, so that nothing arrives after the tile's rows are out
+                if (j + 1 < n) {
+                    if (q == 0) {
+                        if (!(ok = wait(k_full(kst), ((j + 1) / ST) & 1, gone))) break;
+                        fence_after();
+                    }
+                    qk(q, kst);
+                    if (q == nq - 1) commit(k_free(kst));
+                }
+            }
+        }
+        if (!ok && issued) {  // what was issued ends before the memory is given up
+            commit(drain);
+            bar_wait(drain, 0);
+        }
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    if (warp == MMA_WARP) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// A CTA takes 8 rows of a unit; the threads of a row its dims.
+__global__ void __launch_bounds__(256) kv_prompt_join_kernel(const __grid_constant__ KvAttnArgs a, int splits, const float *parts) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int tiles = (a.max_tiles + 1) / 2;
+    const int unit = blockIdx.x / (2 * QT / 8), pr = blockIdx.x % (2 * QT / 8) * 8 + (threadIdx.x >> 5);
+    int u = unit;
+    const int h = u % a.heads;
+    u /= a.heads;
+    const int b = a.b0 + u % a.nb, r = (tiles - 1 - u / a.nb) * 2 * QT + pr;
+    const Seq s = seq_of(a, b);
+    if (r >= s.n * a.group) return;
+    const float *base = parts + (int64_t)unit * splits * prompt_part(a.d);
+    float m = M_NONE, l = 0.0f;
+    for (int i = 0; i < splits; ++i) m = fmaxf(m, base[i * prompt_part(a.d) + 2 * pr]);
+    const int64_t row = row_index(a, kv_rows_of(a.cu, b, a.tokens, a.max_tokens).x, h, r);
+    for (int i = 0; i < splits; ++i) {
+        const float *p = base + i * prompt_part(a.d) + 2 * pr;
+        l = fmaf(p[1], exp2f(p[0] - m), l);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    for (int c = threadIdx.x & 31; c < a.d / 4; c += 32) {
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int i = 0; i < splits; ++i) {
+            const float *p = base + i * prompt_part(a.d);
+            const float w = exp2f(p[2 * pr] - m);
+            const float4 v = *reinterpret_cast<const float4 *>(p + 4 * QT + (int64_t)pr * a.d + 4 * c);
+            o.x = fmaf(v.x, w, o.x), o.y = fmaf(v.y, w, o.y), o.z = fmaf(v.z, w, o.z), o.w = fmaf(v.w, w, o.w);
+        }
+        kv_store(a.out, row * a.d + 4 * c, o.x * inv, a.dtype);
+        kv_store(a.out, row * a.d + 4 * c + 1, o.y * inv, a.dtype);
+        kv_store(a.out, row * a.d + 4 * c + 2, o.z * inv, a.dtype);
+        kv_store(a.out, row * a.d + 4 * c + 3, o.w * inv, a.dtype);
+    }
+    if ((threadIdx.x & 31) == 0 && a.lse) a.lse[row] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
+}
+
+template <int DH>
+cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
+    auto kern = kv_prompt_kernel<DH>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay<DH>::total);
+    if (e != cudaSuccess) return e;
+    kern<<<(unsigned)(p.units * p.splits), THREADS, Lay<DH>::total, st>>>(a, p.splits, p.splits > 1 ? a.part_cta : nullptr);
+    e = launched();
+    if (e != cudaSuccess || p.splits == 1) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p.units * (2 * QT / 8)));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, kv_prompt_join_kernel, a, p.splits, (const float *)a.part_cta);
+    return e != cudaSuccess ? e : launched();
+}
+
+}  // namespace
+
+// 16-bit queries with d <= 128 and more rows a sequence than a warp tile of
+// k_kv_rows.cu holds
+bool kv_prompt_ok(int d, int dtype, int64_t rows) { return dtype != SKM_DTYPE_F32 && d <= 128 && rows > 32; }
+
+KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens, int64_t span) {
+    KvPromptPlan p = {};
+    p.max_tiles = (int)cdiv((int64_t)max_tokens * group, QT);
+    p.units = (int64_t)nb * heads * ((p.max_tiles + 1) / 2);
+    p.splits = 1;
+    // one CTA an SM: split the keys while CTAs are missing, 4 tiles a split at least
+    const int64_t room = KV_SMS / p.units, worth = span / (4 * KT);
+    p.splits = (int)(room < 1 || worth < 1 ? 1 : (room < worth ? room : worth));
+    p.part = p.splits > 1 ? (size_t)p.units * p.splits * prompt_part(d) * 4 : 0;
+    return p;
+}
+
+cudaError_t launch_kv_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
+    return a.d <= 64 ? run_prompt<64>(a, p, st) : run_prompt<128>(a, p, st);
+}
+
+}  // namespace skm

@@ -22,84 +22,11 @@
 // Joining.  Partial (m, l, o) of units that warps share are merged by their
 // CTA, those that CTAs share by kv_join_kernel; both in the line's order, so
 // the result does not depend on timing.
-#include "skm_kv.cuh"
+#include "skm_kv_dev.cuh"
 
 namespace skm {
 
 namespace {
-
-constexpr unsigned long long WAIT_NS = 2000000000ull;
-constexpr float M_NONE = -3.0e38f;  // the reference before the first logit
-constexpr float M_SLACK = 15.0f, M_BELOW = 7.0f;
-constexpr float LN2 = 0.69314718055994531f;
-
-__device__ __forceinline__ float ex2(float x) {  // 2^x, 2 units in the last place, subnormal results 0
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-__device__ __forceinline__ uint32_t su32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ bool bar_try(uint32_t b, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}\n"
-        : "=r"(ok)
-        : "r"(b), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity) {
-    if (bar_try(b, parity)) return true;
-    unsigned long long t0, t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
-    for (uint32_t i = 1;; ++i) {
-        if (bar_try(b, parity)) return true;
-        if ((i & 63) == 0) {
-            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-            if (t - t0 > WAIT_NS) return false;
-        }
-    }
-}
-__device__ __forceinline__ void bulk_g2s(uint32_t dst, const void *src, uint32_t bytes, uint32_t b) {
-    asm volatile(
-        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-        "l"(src), "r"(bytes), "r"(b)
-        : "memory");
-}
-
-// ---- a sequence as this launch sees it
-struct Seq {
-    int lo, cnt;  // first block that a row sees, blocks
-    int len, n;   // tokens held, rows
-};
-__device__ __forceinline__ Seq seq_of(const KvAttnArgs &a, int b) {
-    Seq s;
-    s.len = kv_clamp(a.pos[b], 0, a.cols * a.page);
-    s.n = kv_rows_of(a.cu, b, a.tokens, a.max_tokens).y;
-    s.lo = a.window > 0 ? max(0, s.len - s.n - a.window + 1) / KV_B : 0;
-    s.cnt = s.n > 0 ? (s.len + KV_B - 1) / KV_B - s.lo : 0;
-    if (s.cnt < 0) s.cnt = 0;
-    return s;
-}
-__device__ __forceinline__ int tiles_of(const KvAttnArgs &a, const Seq &s, int rt) {
-    return (int)(((int64_t)s.n * a.group + rt - 1) / rt);
-}
-// the last / first position that row r of a sequence may see (last < first: none)
-__device__ __forceinline__ int last_of(const KvAttnArgs &a, const Seq &s, int r) {
-    const int i = r / a.group;
-    if (i >= s.n) return -1;
-    return a.causal ? min(s.len - 1, s.len - s.n + i) : s.len - 1;
-}
-__device__ __forceinline__ int first_of(const KvAttnArgs &a, const Seq &s, int r) {
-    return a.window > 0 ? max(0, s.len - s.n + r / a.group - a.window + 1) : 0;
-}
-
-// Where a row's result goes
-__device__ __forceinline__ int64_t row_index(const KvAttnArgs &a, int row0, int h, int r) {
-    return ((int64_t)row0 + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group;
-}
 
 // The line of items.  cum[i] (shared memory): items of sequences before b0 + i.
 struct Line {
@@ -366,12 +293,6 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
         "{%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// codes of bytes 0, 1 / 2, 3 of a word as two f16: 1024 + u as bits, minus 1152
-__device__ __forceinline__ uint32_t codes_f16(uint32_t word, uint32_t sel) {
-    const uint32_t x = __byte_perm(word, 0x64646464u, sel);
-    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&x), __half2half2(__ushort_as_half(0x6480)));
-    return *reinterpret_cast<const uint32_t *>(&r);
 }
 // operand A of a 16 x 16 tile of codes: x rows 0..7, y rows 8..15, four
 // consecutive bytes a lane (columns 2c, 2c + 1, 2c + 8, 2c + 9 of the tile)
@@ -797,7 +718,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
                 const float lvs = __shfl_sync(0xffffffffu, cur.lvs, i);
                 const float ivs = __shfl_sync(0xffffffffu, cur.ivs, i);
                 const uint32_t st = taken % ns;
-                if (!bar_wait(bars + 8 * st, (taken / ns) & 1u)) {
+                if (!__all_sync(0xffffffffu, bar_wait(bars + 8 * st, (taken / ns) & 1u))) {
                     ok = false;
                     break;
                 }

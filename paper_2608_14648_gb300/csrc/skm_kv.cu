@@ -105,15 +105,26 @@ int64_t span_of(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn *
     return span;
 }
 
-struct AttendBufs {
+// How a call runs, and its parts of the workspace
+struct AttendPlan {
+    bool prompt;
+    KvRowsPlan rows = {};
+    KvPromptPlan many = {};
     float *part_cta = nullptr, *part_warp = nullptr;
 };
 
-KvRowsPlan plan_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, Carver &cv, AttendBufs &b) {
-    const KvRowsPlan p = kv_rows_plan(std::min<int>(s->batch, KV_MAX_SEQS), c->heads, a->heads_q / c->heads, c->d,
-                                      a->dtype, most_tokens(s), span_of(c, s, a));
-    if (p.part_cta) b.part_cta = cv.take<float>(p.part_cta / 4);
-    if (p.part_warp) b.part_warp = cv.take<float>(p.part_warp / 4);
+AttendPlan plan_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, Carver &cv) {
+    AttendPlan p;
+    const int nb = std::min<int>(s->batch, KV_MAX_SEQS), group = a->heads_q / c->heads, most = most_tokens(s);
+    p.prompt = kv_prompt_ok(c->d, a->dtype, (int64_t)most * group);
+    if (p.prompt) {
+        p.many = kv_prompt_plan(nb, c->heads, group, c->d, most, span_of(c, s, a));
+        if (p.many.part) p.part_cta = cv.take<float>(p.many.part / 4);
+    } else {
+        p.rows = kv_rows_plan(nb, c->heads, group, c->d, a->dtype, most, span_of(c, s, a));
+        if (p.rows.part_cta) p.part_cta = cv.take<float>(p.rows.part_cta / 4);
+        if (p.rows.part_warp) p.part_warp = cv.take<float>(p.rows.part_warp / 4);
+    }
     return p;
 }
 
@@ -167,8 +178,7 @@ size_t skm_kv_attend_workspace_size(const skm_kv_cache *c, const skm_kv_seqs *s,
     if (check_attend(c, s, a) != SKM_OK) return (size_t)-1;
     if (most_tokens(s) == 0) return 0;
     Carver cv(nullptr, 0);
-    AttendBufs b;
-    plan_attend(c, s, a, cv, b);
+    plan_attend(c, s, a, cv);
     return cv.off;
 }
 
@@ -181,13 +191,13 @@ int skm_kv_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn
     if (!aligned(a->Q, e) || !aligned(a->out, 16) || !aligned(a->lse, 4) || !aligned(a->status, 4))
         return set_error(SKM_ERR_INVALID_ARG, "out must be 16-byte aligned, Q, lse and status to their elements");
     Carver cv(ws, ws_bytes);
-    AttendBufs b;
-    const KvRowsPlan p = plan_attend(c, s, a, cv, b);
+    const AttendPlan p = plan_attend(c, s, a, cv);
     if (cv.off && !ws) return set_error(SKM_ERR_INVALID_ARG, "workspace is NULL (%zu bytes needed)", cv.off);
     if (!aligned(ws, 256)) return set_error(SKM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
     if (!cv.fits() || fault_take(SKM_FAULT_WORKSPACE))
         return set_error(SKM_ERR_NO_MEMORY, "workspace of %zu bytes, %zu needed", ws_bytes, cv.off);
-    if (p.units > 0x7fffffff) return set_error(SKM_ERR_UNSUPPORTED, "too many row tiles");
+    const int64_t ctas = p.prompt ? p.many.units * std::max(p.many.splits, 32) : p.rows.units;
+    if (ctas > 0x7fffffff) return set_error(SKM_ERR_UNSUPPORTED, "too many row tiles");
     KvAttnArgs k = {};
     k.k = c->k;
     k.v = c->v;
@@ -215,17 +225,22 @@ int skm_kv_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn
     k.out = a->out;
     k.lse = a->lse;
     k.status = a->status;
-    k.part_cta = b.part_cta;
-    k.part_warp = b.part_warp;
-    k.max_tiles = (int)cdiv((int64_t)k.max_tokens * k.group, p.rt);
-    k.whole = p.whole;
-    for (int b0 = 0; b0 < s->batch; b0 += KV_MAX_SEQS) {
-        k.b0 = b0;
-        k.nb = std::min(s->batch - b0, KV_MAX_SEQS);
-        KvRowsPlan q = p;
-        q.units = (int64_t)k.nb * k.max_tiles * k.heads;
-        if (p.whole) q.grid = q.units;
-        SKM_CUDA_TRY(launch_kv_rows(k, q, S(stream)));
+    k.part_cta = p.part_cta;
+    k.part_warp = p.part_warp;
+    k.max_tiles = p.prompt ? p.many.max_tiles : (int)cdiv((int64_t)k.max_tokens * k.group, p.rows.rt);
+    k.whole = p.rows.whole;
+    for (k.b0 = 0; k.b0 < s->batch; k.b0 += KV_MAX_SEQS) {
+        k.nb = std::min(s->batch - k.b0, KV_MAX_SEQS);
+        if (p.prompt) {
+            KvPromptPlan q = p.many;
+            q.units = (int64_t)k.nb * k.heads * ((k.max_tiles + 1) / 2);
+            SKM_CUDA_TRY(launch_kv_prompt(k, q, S(stream)));
+        } else {
+            KvRowsPlan q = p.rows;
+            q.units = (int64_t)k.nb * k.max_tiles * k.heads;
+            if (q.whole) q.grid = q.units;
+            SKM_CUDA_TRY(launch_kv_rows(k, q, S(stream)));
+        }
     }
     return SKM_OK;
 }
