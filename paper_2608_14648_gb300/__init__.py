@@ -8,7 +8,6 @@ raises.  Function names match the C entry points.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
@@ -761,6 +760,7 @@ class KVCache:
                 raise ValueError("KVCache: k, v and scales must be on one device")
         self.k, self.v, self.scales = k, v, scales
         self.heads, self.d, self.page, self.pages = int(heads), int(d), int(page), n
+        self.index = k.get_device()
         self.ref = KVCacheRef(self.heads, self.d, self.page, n, k.data_ptr(), v.data_ptr(), scales.data_ptr())
 
     @property
@@ -768,46 +768,62 @@ class KVCache:
         return self.k.device
 
 
-def _kv_ints(name, t, shape, device):
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on {device}")
+def _kv_ints(name, t, n, index):
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != index:
+        raise ValueError(f"{name} must be a contiguous int32 tensor [{n}] on the cache's device")
+    return t.data_ptr()
 
 
 def _kv_seqs(cache, table, pos, cu, tokens, max_tokens, max_len=0):
-    if table.dim() != 2:
-        raise ValueError("table must be [batch, cols]")
+    index = cache.index
+    if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_contiguous() or table.get_device() != index:
+        raise ValueError("table must be a contiguous int32 tensor [batch, cols] on the cache's device")
     batch, cols = table.shape
-    _kv_ints("table", table, (batch, cols), cache.device)
-    _kv_ints("positions", pos, (batch,), cache.device)
-    _kv_ints("cu", cu, (batch + 1,), cache.device)
-    return KVSeqs(batch, cols, table.data_ptr(), pos.data_ptr(), cu.data_ptr(), tokens, int(max_tokens), int(max_len))
+    return KVSeqs(batch, cols, table.data_ptr(), _kv_ints("positions", pos, batch, index),
+                  _kv_ints("cu", cu, batch + 1, index), tokens, max_tokens, max_len)
 
 
 def _kv_rows(name, t, heads, cache):
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != cache.d or t.device != cache.device:
-        raise ValueError(f"{name} must be [tokens, {heads}, {cache.d}] on {cache.device}")
-    if t.dtype not in _KV_DTYPES:
+    """The C type of rows [tokens, heads, d]."""
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != cache.d or t.get_device() != cache.index:
+        raise ValueError(f"{name} must be [tokens, {heads}, {cache.d}] on the cache's device")
+    dtype = _KV_DTYPES.get(t.dtype)
+    if dtype is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16")
     if t.stride(2) != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
+    return dtype
 
 
-def _kv_on(cache, stream):
+def _kv_stream(cache, stream):
+    """The raw stream: the current one of the cache's device unless given (the
+    lookup without a Stream object, whose construction costs 3 us)."""
+    if cache.index < 0:
+        raise ValueError("the cache is not on a GPU")
+    return torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream
+
+
+def _kv_empty(cache, stream, *shape, dtype):
     """What a call allocates belongs to the stream that it runs on."""
-    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=cache.k.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=cache.k.device)
 
 
 def skm_kv_write(cache: KVCache, table, start, cu, K, V, max_tokens, stream=None):
     """Quantises rows cu[b]:cu[b + 1] of K and V ([tokens, heads, d], any strides
     with d contiguous) into the cache at positions start[b], start[b] + 1, ... of
     sequence b; table int32 [batch, cols], start [batch], cu [batch + 1]."""
-    _kv_rows("K", K, cache.heads, cache)
-    _kv_rows("V", V, cache.heads, cache)
-    if V.dtype != K.dtype or V.shape[0] != K.shape[0]:
+    dtype = _kv_rows("K", K, cache.heads, cache)
+    if _kv_rows("V", V, cache.heads, cache) != dtype or V.shape[0] != K.shape[0]:
         raise ValueError("K and V must have one type and length")
     s = _kv_seqs(cache, table, start, cu, K.shape[0], max_tokens)
-    _check(lib().skm_kv_write(ctypes.byref(cache.ref), ctypes.byref(s), _KV_DTYPES[K.dtype], K.data_ptr(), K.stride(0),
-                              K.stride(1), V.data_ptr(), V.stride(0), V.stride(1), _stream(stream)))
+    rc = lib().skm_kv_write(ctypes.byref(cache.ref), ctypes.byref(s), dtype, K.data_ptr(), K.stride(0), K.stride(1),
+                            V.data_ptr(), V.stride(0), V.stride(1), _kv_stream(cache, stream))
+    if rc:
+        _check(rc)
 
 
 def skm_kv_read(cache: KVCache, table, start, cu, tokens, max_tokens, dtype=DTYPE_BF16, out=None, stream=None):
@@ -815,38 +831,40 @@ def skm_kv_read(cache: KVCache, table, start, cu, tokens, max_tokens, dtype=DTYP
     positions start[b], start[b] + 1, ... of sequence b.  out: a pair of
     contiguous tensors, either may be None (not read)."""
     if out is None:
-        if dtype not in _KV_TORCH:
+        t = _KV_TORCH.get(dtype)
+        if t is None:
             raise ValueError(f"unknown dtype {dtype}")
-        with _kv_on(cache, stream):
-            out = tuple(torch.empty(tokens, cache.heads, cache.d, dtype=_KV_TORCH[dtype], device=cache.device)
-                        for _ in range(2))
+        out = (_kv_empty(cache, stream, tokens, cache.heads, cache.d, dtype=t),
+               _kv_empty(cache, stream, tokens, cache.heads, cache.d, dtype=t))
     else:
         for t in out:
-            if t is not None:
-                _kv_rows("out", t, cache.heads, cache)
-                if t.shape[0] != tokens or not t.is_contiguous() or _KV_DTYPES[t.dtype] != dtype:
-                    raise ValueError("out: contiguous tensors of `tokens` rows and the given dtype")
-    s = _kv_seqs(cache, table, start, cu, int(tokens), max_tokens)
-    _check(lib().skm_kv_read(ctypes.byref(cache.ref), ctypes.byref(s), dtype, _ptr(out[0]), _ptr(out[1]),
-                             _stream(stream)))
+            if t is not None and (_kv_rows("out", t, cache.heads, cache) != dtype or t.shape[0] != tokens
+                                  or not t.is_contiguous()):
+                raise ValueError("out: contiguous tensors of `tokens` rows and the given dtype")
+    K, V = out
+    s = _kv_seqs(cache, table, start, cu, tokens, max_tokens)
+    rc = lib().skm_kv_read(ctypes.byref(cache.ref), ctypes.byref(s), dtype, None if K is None else K.data_ptr(),
+                           None if V is None else V.data_ptr(), _kv_stream(cache, stream))
+    if rc:
+        _check(rc)
     return out
 
 
-def _kv_attn(heads_q, dtype, causal, window, scale):
-    return KVAttn(int(heads_q), dtype, int(bool(causal)), int(window), scale, 0, None, 0, 0, None, None, None)
+def _kv_ws_bytes(cache, s, a):
+    n = lib().skm_kv_attend_workspace_size(ctypes.byref(cache.ref), ctypes.byref(s), ctypes.byref(a))
+    if n == ctypes.c_size_t(-1).value:
+        raise SkmError(1, lib().skm_last_error().decode())
+    return n
 
 
 def kv_workspace(cache: KVCache, batch, heads_q, tokens, max_tokens, max_len, dtype=DTYPE_BF16, cols=None, causal=True,
                  window=0):
-    """A workspace for skm_kv_attend calls of at most these sizes."""
-    cols = -(-int(max_len) // cache.page) if cols is None else int(cols)
+    """A workspace for skm_kv_attend calls of these sizes."""
+    cols = -(-max_len // cache.page) if cols is None else cols
     dummy = cache.k.data_ptr()
-    s = KVSeqs(int(batch), max(cols, 1), dummy, dummy, dummy, int(tokens), int(max_tokens), int(max_len))
-    a = _kv_attn(heads_q, dtype, causal, window, 1.0)
-    n = lib().skm_kv_attend_workspace_size(ctypes.byref(cache.ref), ctypes.byref(s), ctypes.byref(a))
-    if n == ctypes.c_size_t(-1).value:
-        raise SkmError(1, lib().skm_last_error().decode())
-    return _ws(n, cache.device)
+    s = KVSeqs(batch, max(cols, 1), dummy, dummy, dummy, tokens, max_tokens, max_len)
+    a = KVAttn(heads_q, dtype, bool(causal), window, 1.0, 0, None, 0, 0, None, None, None)
+    return _ws(_kv_ws_bytes(cache, s, a), cache.device)
 
 
 def skm_kv_attend(cache: KVCache, table, length, cu, Q, max_tokens, max_len, scale=None, causal=True, window=0,
@@ -854,28 +872,26 @@ def skm_kv_attend(cache: KVCache, table, length, cu, Q, max_tokens, max_len, sca
     """(out, lse or None): attention of the query rows Q [tokens, heads_q, d]
     over the cache.  length[b]: the tokens the cache holds of sequence b, its
     own query tokens included; scale: 1 / sqrt(d) unless given."""
-    heads_q = Q.shape[1] if Q.dim() == 3 else 0
-    _kv_rows("Q", Q, heads_q, cache)
-    tokens = Q.shape[0]
+    tokens, heads_q = Q.shape[0], Q.shape[1]
+    dtype = _kv_rows("Q", Q, heads_q, cache)
     s = _kv_seqs(cache, table, length, cu, tokens, max_tokens, max_len)
-    a = _kv_attn(heads_q, _KV_DTYPES[Q.dtype], causal, window, cache.d ** -0.5 if scale is None else float(scale))
-    if status is not None and (status.dtype != torch.int32 or status.device != cache.device or status.numel() < 1):
-        raise ValueError(f"status must be an int32 tensor on {cache.device}")
-    with _kv_on(cache, stream):
-        if out is None:
-            out = torch.empty(tokens, heads_q, cache.d, dtype=Q.dtype, device=cache.device)
-        elif out.shape != Q.shape or out.dtype != Q.dtype or not out.is_contiguous() or out.device != cache.device:
-            raise ValueError("out: contiguous, of Q's shape and type")
-        lse = torch.empty(tokens, heads_q, dtype=torch.float32, device=cache.device) if want_lse else None
-        if ws is None:
-            n = lib().skm_kv_attend_workspace_size(ctypes.byref(cache.ref), ctypes.byref(s), ctypes.byref(a))
-            if n == ctypes.c_size_t(-1).value:
-                raise SkmError(1, lib().skm_last_error().decode())
-            ws = _ws(n, cache.device) if n else None
-    a.Q, a.q_token, a.q_head = Q.data_ptr(), Q.stride(0), Q.stride(1)
-    a.out = out.data_ptr()
-    a.lse = None if lse is None else lse.data_ptr()
-    a.status = None if status is None else status.data_ptr()
-    _check(lib().skm_kv_attend(ctypes.byref(cache.ref), ctypes.byref(s), ctypes.byref(a), _ptr(ws),
-                               0 if ws is None else ws.numel(), _stream(stream)))
+    if out is None:
+        out = _kv_empty(cache, stream, tokens, heads_q, cache.d, dtype=Q.dtype)
+    elif out.shape != Q.shape or out.dtype != Q.dtype or not out.is_contiguous() or out.get_device() != cache.index:
+        raise ValueError("out: contiguous, of Q's shape, type and device")
+    if status is not None and (status.dtype is not torch.int32 or status.get_device() != cache.index or not status.numel()):
+        raise ValueError("status must be an int32 tensor on the cache's device")
+    lse = _kv_empty(cache, stream, tokens, heads_q, dtype=torch.float32) if want_lse else None
+    a = KVAttn(heads_q, dtype, bool(causal), window, cache.d ** -0.5 if scale is None else scale, 0, Q.data_ptr(),
+               Q.stride(0), Q.stride(1), out.data_ptr(), None if lse is None else lse.data_ptr(),
+               None if status is None else status.data_ptr())
+    if ws is None:
+        n = _kv_ws_bytes(cache, s, a)
+        ws = _kv_empty(cache, stream, n, dtype=torch.uint8) if n else None
+    elif ws.get_device() != cache.index or not ws.is_contiguous():
+        raise ValueError("ws must be contiguous, on the cache's device")
+    rc = lib().skm_kv_attend(ctypes.byref(cache.ref), ctypes.byref(s), ctypes.byref(a), None if ws is None else ws.data_ptr(),
+                             0 if ws is None else ws.nbytes, _kv_stream(cache, stream))
+    if rc:
+        _check(rc)
     return out, lse

@@ -227,13 +227,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
     int u = blockIdx.x;
     const int split = u % splits;
     u /= splits;
-    const int h = u % a.heads;
-    u /= a.heads;
+    const int h = a.by_heads.mod(u);
+    u = a.by_heads.div(u);
     const int bi = u % a.nb, pair = tiles - 1 - u / a.nb, b = a.b0 + bi;
     const Seq s = seq_of(a, b);
     const int rows = s.n * a.group, r0 = pair * 2 * QT;
     if (r0 >= rows) return;
-    const int row0 = kv_rows_of(a.cu, b, a.tokens, a.max_tokens).x;
     const int r1 = min(r0 + 2 * QT, rows) - 1;
     const int nq = r1 - r0 >= QT ? 2 : 1;
     // positions that some row sees, the tiles of them, this split's tiles
@@ -276,7 +275,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row;
         const bool in = r < rows;
         const uint16_t *x = static_cast<const uint16_t *>(a.Q);
-        if (in) x += (int64_t)(row0 + r / a.group) * a.q_token + (int64_t)(h * a.group + r % a.group) * a.q_head;
+        if (in) x += (int64_t)(s.row0 + a.by_group.div(r)) * a.q_token + (int64_t)(h * a.group + a.by_group.mod(r)) * a.q_head;
         const float fac = load_row<DH>(a, x, in, sm + L::q + q * L::TILE, row);
         fence_async();
         __syncwarp();
@@ -335,7 +334,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                     most = fmaxf(most, all);
                     add = fmaf(all, f4.z, add);
                 }
-                if (pass == 1 || !__any_sync(0xffffffffu, most > 32768.0f)) break;
+                if (pass == 1 || !__any_sync(0xffffffffu, most > M_MOST)) break;
                 // the rows' maxima, and with them new references
                 float top = -INFINITY;
                 for (int k = 0; k < KBLK; ++k) {
@@ -388,7 +387,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
             float *part = parts ? parts + (int64_t)blockIdx.x * prompt_part(a.d) : nullptr;
             const int pr = q * QT + row;
             if (part) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);
-            const int64_t at = in ? row_index(a, row0, h, r) : 0;
+            const int64_t at = in ? row_index(a, s, h, r) : 0;
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
             for (int k = 0; k < DH / 16; ++k) {
                 if (16 * k >= a.d) break;
@@ -441,9 +440,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
             if (task < tasks) {
                 const int blk = (t0 + task / (2 * KBLK)) * KBLK + task % KBLK;
                 if (blk * KV_B <= last && blk * KV_B + KV_B > first) {
-                    const int pg = a.table[(int64_t)b * a.cols + blk / a.bpp];
+                    const int pg = a.table[(int64_t)b * a.cols + a.by_bpp.div(blk)];
                     if (pg >= 0 && pg < a.pages) {
-                        w.at = (pg * a.heads + h) * a.bpp + blk % a.bpp;
+                        w.at = (pg * a.heads + h) * a.bpp + a.by_bpp.mod(blk);
                         w.sc = a.scales[w.at];
                     }
                 }
@@ -570,15 +569,15 @@ __global__ void __launch_bounds__(256) kv_prompt_join_kernel(const __grid_consta
     const int tiles = (a.max_tiles + 1) / 2;
     const int unit = blockIdx.x / (2 * QT / 8), pr = blockIdx.x % (2 * QT / 8) * 8 + (threadIdx.x >> 5);
     int u = unit;
-    const int h = u % a.heads;
-    u /= a.heads;
+    const int h = a.by_heads.mod(u);
+    u = a.by_heads.div(u);
     const int b = a.b0 + u % a.nb, r = (tiles - 1 - u / a.nb) * 2 * QT + pr;
     const Seq s = seq_of(a, b);
     if (r >= s.n * a.group) return;
     const float *base = parts + (int64_t)unit * splits * prompt_part(a.d);
     float m = M_NONE, l = 0.0f;
     for (int i = 0; i < splits; ++i) m = fmaxf(m, base[i * prompt_part(a.d) + 2 * pr]);
-    const int64_t row = row_index(a, kv_rows_of(a.cu, b, a.tokens, a.max_tokens).x, h, r);
+    const int64_t row = row_index(a, s, h, r);
     for (int i = 0; i < splits; ++i) {
         const float *p = base + i * prompt_part(a.d) + 2 * pr;
         l = fmaf(p[1], exp2f(p[0] - m), l);
@@ -602,11 +601,11 @@ __global__ void __launch_bounds__(256) kv_prompt_join_kernel(const __grid_consta
 
 template <int DH>
 cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
-    auto kern = kv_prompt_kernel<DH>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay<DH>::total);
-    if (e != cudaSuccess) return e;
-    kern<<<(unsigned)(p.units * p.splits), THREADS, Lay<DH>::total, st>>>(a, p.splits, p.splits > 1 ? a.part_cta : nullptr);
-    e = launched();
+    static SmemLimit limit;
+    cudaError_t e = limit.launch(kv_prompt_kernel<DH>, Lay<DH>::total, [&] {
+        kv_prompt_kernel<DH><<<(unsigned)(p.units * p.splits), THREADS, Lay<DH>::total, st>>>(
+            a, p.splits, p.splits > 1 ? a.part_cta : nullptr);
+    });
     if (e != cudaSuccess || p.splits == 1) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(p.units * (2 * QT / 8)));

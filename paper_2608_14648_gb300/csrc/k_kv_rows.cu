@@ -50,22 +50,23 @@ __host__ __device__ __forceinline__ int64_t active_ctas(int64_t W, int nw, int64
     return c < 1 ? 1 : (c > grid ? grid : c);
 }
 
-// 32 items, one a lane: where the block is, its scales, the item's unit
+// 32 items, one a lane.  Three steps, so that the two dependent loads behind
+// an item (its page, then the block's scales) are waited for long after they
+// were issued: where the item is, its block, its scales to shared memory.
 struct Window {
-    int at;  // block of the pool, -1: nothing to do
+    int pg, at;  // page; block of the pool, -1: nothing to do
     int blk, seq, unit;
-    float ks, lvs, ivs;
+    float2 sc;
     uint32_t todo, starts;  // (all lanes the same) items with work, items that begin a unit
     int n;
 };
 
 template <int RT>
-__device__ __forceinline__ void window_fill(const KvAttnArgs &a, const Line &ln, int64_t base, int64_t end, int lane,
-                                            Window &w) {
+__device__ __forceinline__ void window_pages(const KvAttnArgs &a, const Line &ln, int64_t base, int64_t end, int lane,
+                                             Window &w) {
     w.n = end - base > 32 ? 32 : (int)(end > base ? end - base : 0);
-    w.at = -1;
+    w.pg = -1;
     w.blk = w.seq = w.unit = 0;
-    w.ks = 0.0f, w.lvs = 0.0f, w.ivs = 1.0f;
     bool starts = false;
     if (lane < w.n) {
         const int64_t item = base + lane;
@@ -84,21 +85,40 @@ __device__ __forceinline__ void window_fill(const KvAttnArgs &a, const Line &ln,
         w.seq = b;
         w.unit = (int)u;
         w.blk = s.lo + (int)k;
-        const int r0 = (int)(u / a.heads) * RT, r1 = min(r0 + RT, s.n * a.group) - 1;
-        const bool seen = w.blk * KV_B <= last_of(a, s, r1) && w.blk * KV_B + KV_B > first_of(a, s, r0);
-        const int pg = a.table[(int64_t)(ln.b0 + b) * a.cols + w.blk / a.bpp];
-        if (seen && pg >= 0 && pg < a.pages) {
-            w.at = (pg * a.heads + (int)(u % a.heads)) * a.bpp + w.blk % a.bpp;
-            const float2 sc = a.scales[w.at];
-            w.ks = sc.x;
-            if (sc.y > 0.0f) {  // a block of zeros has scale 0: any scale will do
-                w.lvs = log2f(sc.y);
-                w.ivs = 1.0f / sc.y;
-            }
-        }
+        const int r0 = a.by_heads.div((int)u) * RT, r1 = min(r0 + RT, s.n * a.group) - 1;
+        if (w.blk * KV_B <= last_of(a, s, r1) && w.blk * KV_B + KV_B > first_of(a, s, r0))
+            w.pg = a.table[(int64_t)(ln.b0 + b) * a.cols + a.by_bpp.div(w.blk)];
     }
-    w.todo = __ballot_sync(0xffffffffu, w.at >= 0);
     w.starts = __ballot_sync(0xffffffffu, starts);
+    w.todo = 0;
+}
+__device__ __forceinline__ void window_blocks(const KvAttnArgs &a, Window &w) {
+    const bool there = w.pg >= 0 && w.pg < a.pages;
+    w.at = there ? (w.pg * a.heads + a.by_heads.mod(w.unit)) * a.bpp + a.by_bpp.mod(w.blk) : -1;
+    w.sc = there ? a.scales[w.at] : make_float2(0.0f, 0.0f);
+    w.todo = __ballot_sync(0xffffffffu, there);
+}
+__device__ __forceinline__ void window_scales(const Window &w, float4 *mem, int lane) {
+    // a block of zeros has scale 0: any value scale will do
+    const float vs = w.sc.y > 0.0f ? w.sc.y : 1.0f;
+    mem[lane] = make_float4(w.sc.x, log2f(vs), 1.0f / vs, 0.0f);
+    __syncwarp();
+}
+
+// dims 4 c .. 4 c + 3 of an output row
+__device__ __forceinline__ void store_row4(const KvAttnArgs &a, int64_t row, int c, float4 o, float inv) {
+    o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (a.dtype == SKM_DTYPE_F32) {
+        reinterpret_cast<float4 *>(static_cast<float *>(a.out) + row * a.d)[c] = o;
+    } else if (a.dtype == SKM_DTYPE_BF16) {
+        const __nv_bfloat162 x = __floats2bfloat162_rn(o.x, o.y), y = __floats2bfloat162_rn(o.z, o.w);
+        reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row * a.d)[c] =
+            make_uint2(*reinterpret_cast<const uint32_t *>(&x), *reinterpret_cast<const uint32_t *>(&y));
+    } else {
+        const __half2 x = __floats2half2_rn(o.x, o.y), y = __floats2half2_rn(o.z, o.w);
+        reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row * a.d)[c] =
+            make_uint2(*reinterpret_cast<const uint32_t *>(&x), *reinterpret_cast<const uint32_t *>(&y));
+    }
 }
 
 // A partial result: RT x (m, l), padded to 16 bytes, then RT rows of d sums.
@@ -111,36 +131,61 @@ __host__ __device__ __forceinline__ int64_t part_floats(int d) {
     return part_head<RT>() + (int64_t)RT * d;
 }
 
-// Merges parts of one unit, the threads of a group working together: to the
-// outputs (dst NULL) or as a part again.
+// Merges parts of one unit: the lanes in `same` hold one each, in order.  A
+// warp takes a row: a lane its part's (m, l), then all lanes the row's dims.  To
+// the outputs (dst NULL) or as a part again.
 template <int RT>
-__device__ __forceinline__ void merge_parts(const KvAttnArgs &a, const float *const *parts, int np, const Seq &s, int row0,
-                                            int unit, float *dst, int tid, int threads) {
-    const int d4 = a.d / 4, h = unit % a.heads, r0 = unit / a.heads * RT;
+__device__ __forceinline__ void merge_parts(const KvAttnArgs &a, const float *part, uint32_t same, const Seq &s, int unit,
+                                            float *dst, int warp, int warps, int lane) {
+    const int d4 = a.d / 4, h = a.by_heads.mod(unit), r0 = a.by_heads.div(unit) * RT;
     const int rows = min(RT, s.n * a.group - r0);
-    for (int e = tid; e < rows * d4; e += threads) {
-        const int r = e / d4, c = e - r * d4;
-        float m = M_NONE;
-        for (int i = 0; i < np; ++i) m = fmaxf(m, parts[i][2 * r]);
-        float l = 0.0f;
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int i = 0; i < np; ++i) {
-            const float w = exp2f(parts[i][2 * r] - m);
-            const float4 v = *reinterpret_cast<const float4 *>(parts[i] + part_head<RT>() + r * a.d + 4 * c);
-            l = fmaf(parts[i][2 * r + 1], w, l);
-            o.x = fmaf(v.x, w, o.x), o.y = fmaf(v.y, w, o.y), o.z = fmaf(v.z, w, o.z), o.w = fmaf(v.w, w, o.w);
+    const bool mine = (same >> lane) & 1;
+    for (int r = warp; r < rows; r += warps) {
+        const float2 ml = mine ? *reinterpret_cast<const float2 *>(part + 2 * r) : make_float2(M_NONE, 0.0f);
+        float m = ml.x;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const float f = mine ? ex2(ml.x - m) : 0.0f;
+        float l = ml.y * f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        float4 o[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
+        for (uint32_t bits = same; bits;) {
+            float w[4];
+            const float4 *p[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {  // past the last: the first again, weight 0
+                const int j = __ffs(bits ? bits : same) - 1;
+                const float fj = __shfl_sync(0xffffffffu, f, j);
+                w[k] = bits ? fj : 0.0f;
+                p[k] = reinterpret_cast<const float4 *>(
+                    __shfl_sync(0xffffffffu, (unsigned long long)part, j) + 4ull * (part_head<RT>() + r * a.d));
+                bits &= bits - 1;
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                if (lane + 32 * q >= d4) break;
+                float4 v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = p[k][lane + 32 * q];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    o[q].x = fmaf(v[k].x, w[k], o[q].x), o[q].y = fmaf(v[k].y, w[k], o[q].y);
+                    o[q].z = fmaf(v[k].z, w[k], o[q].z), o[q].w = fmaf(v[k].w, w[k], o[q].w);
+                }
+            }
         }
-        if (dst) {
-            if (c == 0) dst[2 * r] = m, dst[2 * r + 1] = l;
-            *reinterpret_cast<float4 *>(dst + part_head<RT>() + r * a.d + 4 * c) = o;
-        } else {
-            const int64_t row = row_index(a, row0, h, r0 + r);
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            kv_store(a.out, row * a.d + 4 * c, o.x * inv, a.dtype);
-            kv_store(a.out, row * a.d + 4 * c + 1, o.y * inv, a.dtype);
-            kv_store(a.out, row * a.d + 4 * c + 2, o.z * inv, a.dtype);
-            kv_store(a.out, row * a.d + 4 * c + 3, o.w * inv, a.dtype);
-            if (c == 0 && a.lse) a.lse[row] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
+        const int64_t row = row_index(a, s, h, r0 + r);
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            if (lane + 32 * q >= d4) break;
+            if (dst) reinterpret_cast<float4 *>(dst + part_head<RT>() + r * a.d)[lane + 32 * q] = o[q];
+            else store_row4(a, row, lane + 32 * q, o[q], inv);
+        }
+        if (lane == 0) {
+            if (dst) dst[2 * r] = m, dst[2 * r + 1] = l;
+            else if (a.lse) a.lse[row] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
         }
     }
 }
@@ -151,11 +196,12 @@ __device__ __forceinline__ void merge_parts(const KvAttnArgs &a, const float *co
 template <int R, int DPL>
 struct Fp32Rows {
     static constexpr int RT = R;
+    static constexpr bool ONE_D = false;
     static size_t __host__ __device__ scratch(int d) { return (size_t)R * (d + KV_B) * 4; }
     float o[R][DPL], m[R], l[R];
     float *q, *p;
 
-    __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int row0, int h, int r0, uint8_t *mem,
+    __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int h, int r0, uint8_t *mem,
                                           int lane) {
         q = reinterpret_cast<float *>(mem);
         p = q + R * a.d;
@@ -167,7 +213,7 @@ struct Fp32Rows {
             for (int i = 0; i < DPL; ++i) o[r][i] = 0.0f;
             const int rr = r0 + r;
             const bool in = rr < s.n * a.group;
-            const int64_t at = in ? (int64_t)(row0 + rr / a.group) * a.q_token + (int64_t)(h * a.group + rr % a.group) * a.q_head : 0;
+            const int64_t at = in ? (int64_t)(s.row0 + a.by_group.div(rr)) * a.q_token + (int64_t)(h * a.group + a.by_group.mod(rr)) * a.q_head : 0;
             for (int i = lane; i < a.d; i += 32) q[r * a.d + i] = in ? kv_load(a.Q, at + i, a.dtype) * a.scale_log2 : 0.0f;
         }
         __syncwarp();
@@ -262,11 +308,11 @@ struct Fp32Rows {
                 if (lane + 32 * i < a.d) dst[part_head<R>() + r * a.d + lane + 32 * i] = o[r][i];
         }
     }
-    __device__ __forceinline__ void finish(const KvAttnArgs &a, const Seq &s, int row0, int h, int r0, int lane) const {
+    __device__ __forceinline__ void finish(const KvAttnArgs &a, const Seq &s, int h, int r0, int lane) const {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (r0 + r >= s.n * a.group) break;
-            const int64_t row = row_index(a, row0, h, r0 + r);
+            const int64_t row = row_index(a, s, h, r0 + r);
             const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
 #pragma unroll
             for (int i = 0; i < DPL; ++i)
@@ -312,19 +358,20 @@ __device__ __forceinline__ void codes_a(uint32_t x, uint32_t y, uint32_t (&a)[4]
 // 2c + 1, 2c + 8, 2c + 9, the operand's own.  p^T comes from S^T by movmatrix.
 // bf16 queries become f16 exactly after scaling a row by a power of two (values
 // below 2^-25 of the row's largest, whose products round away, aside).
-// DC: 16-dim chunks at most, NT: tiles of 8 rows.
-template <int DC, int NT>
+// DC: 16-dim chunks at most (FULL: exactly), NT: tiles of 8 rows.
+template <int DC, int NT, bool FULL>
 struct MmaRows {
     static constexpr int RT = 8 * NT;
+    static constexpr bool ONE_D = FULL;
     static constexpr bool QMEM = NT * DC >= 32;  // the queries' operands wait in shared memory
     static size_t __host__ __device__ scratch(int) { return QMEM ? (size_t)NT * DC * 2 * 32 * 4 : 0; }
     float o[NT][DC][4], m[NT][2], l[NT][2], fac[NT][2];
     uint32_t q[QMEM ? 1 : NT][QMEM ? 1 : DC][2];
     uint2 *qmem;
 
-    __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int row0, int h, int r0, uint8_t *mem,
+    __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int h, int r0, uint8_t *mem,
                                           int lane) {
-        const int g = lane >> 2, c = lane & 3, nc = a.d / KV_B;
+        const int g = lane >> 2, c = lane & 3, nc = FULL ? DC : a.d / KV_B;
         qmem = reinterpret_cast<uint2 *>(mem);
         __syncwarp();
 #pragma unroll
@@ -332,7 +379,7 @@ struct MmaRows {
             const int rr = r0 + 8 * t + g;
             const bool in = rr < s.n * a.group;
             const uint16_t *x = static_cast<const uint16_t *>(a.Q);
-            if (in) x += (int64_t)(row0 + rr / a.group) * a.q_token + (int64_t)(h * a.group + rr % a.group) * a.q_head + 4 * c;
+            if (in) x += (int64_t)(s.row0 + a.by_group.div(rr)) * a.q_token + (int64_t)(h * a.group + a.by_group.mod(rr)) * a.q_head + 4 * c;
             uint2 raw[DC];
             float top = 0.0f;
 #pragma unroll
@@ -390,7 +437,7 @@ struct MmaRows {
 
     __device__ __forceinline__ void block(const KvAttnArgs &a, const Seq &s, int r0, const uint8_t *K, const uint8_t *V,
                                           int blk, float ks, float lvs, float ivs, bool mask, int lane) {
-        const int g = lane >> 2, c = lane & 3, nc = a.d / KV_B;
+        const int g = lane >> 2, c = lane & 3, nc = FULL ? DC : a.d / KV_B;
         float x[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -424,19 +471,33 @@ struct MmaRows {
                 }
             }
         }
-        bool over = false;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
+            const float f[2] = {fac[t][0] * ks, fac[t][1] * ks};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[t][i] = fmaf(x[t][i], fac[t][i & 1] * ks, lvs);
-                if (mask) {
+            for (int i = 0; i < 4; ++i) x[t][i] = fmaf(x[t][i], f[i & 1], lvs);
+        }
+        if (mask) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
                     const int j = blk * KV_B + g + 8 * (i >> 1), rr = r0 + 8 * t + 2 * c + (i & 1);
                     if (j > last_of(a, s, rr) || j < first_of(a, s, rr)) x[t][i] = -INFINITY;
                 }
-                over |= x[t][i] > m[t][i & 1] + M_SLACK;
+        }
+        float p[NT][4];
+        const auto weigh = [&] {  // weights, and the largest sum of two
+            float most = 0.0f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[t][i] = ex2(x[t][i] - m[t][i & 1]);
+                most = fmaxf(most, fmaxf(p[t][0] + p[t][2], p[t][1] + p[t][3]));
             }
-        if (__any_sync(0xffffffffu, over)) {
+            return most;
+        };
+        if (__any_sync(0xffffffffu, weigh() > M_MOST)) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -444,23 +505,21 @@ struct MmaRows {
                     float top = fmaxf(x[t][i], x[t][i + 2]);
 #pragma unroll
                     for (int b = 4; b < 32; b <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, b));
-                    const float to = top > m[t][i] + M_SLACK ? top - M_BELOW : m[t][i];
-                    const float f = exp2f(m[t][i] - to);
+                    const float to = top > m[t][i] + M_BELOW ? top - M_BELOW : m[t][i];
+                    const float f = ex2(m[t][i] - to);
                     m[t][i] = to;
                     l[t][i] *= f;
 #pragma unroll
                     for (int w = 0; w < DC; ++w) o[t][w][i] *= f, o[t][w][i + 2] *= f;
                 }
+            weigh();
         }
         uint32_t pb[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            float p[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = ex2(x[t][i] - m[t][i & 1]);
-            l[t][0] = fmaf(p[0] + p[2], ivs, l[t][0]);
-            l[t][1] = fmaf(p[1] + p[3], ivs, l[t][1]);
-            const __half2 lo = __floats2half2_rn(p[0], p[1]), hi = __floats2half2_rn(p[2], p[3]);
+            l[t][0] = fmaf(p[t][0] + p[t][2], ivs, l[t][0]);
+            l[t][1] = fmaf(p[t][1] + p[t][3], ivs, l[t][1]);
+            const __half2 lo = __floats2half2_rn(p[t][0], p[t][1]), hi = __floats2half2_rn(p[t][2], p[t][3]);
             pb[t][0] = transpose8x8(*reinterpret_cast<const uint32_t *>(&lo));
             pb[t][1] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hi));
         }
@@ -501,13 +560,13 @@ struct MmaRows {
                 if (g == 0) dst[2 * r] = m[t][i], dst[2 * r + 1] = l[t][i];
 #pragma unroll
                 for (int w = 0; w < DC; ++w) {
-                    if (w >= a.d / KV_B) break;
+                    if (!FULL && w >= a.d / KV_B) break;
                     dst[part_head<RT>() + r * a.d + 16 * w + g] = o[t][w][i];
                     dst[part_head<RT>() + r * a.d + 16 * w + g + 8] = o[t][w][i + 2];
                 }
             }
     }
-    __device__ __forceinline__ void finish(const KvAttnArgs &a, const Seq &s, int row0, int h, int r0, int lane) const {
+    __device__ __forceinline__ void finish(const KvAttnArgs &a, const Seq &s, int h, int r0, int lane) const {
         const int g = lane >> 2, c = lane & 3;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -515,11 +574,11 @@ struct MmaRows {
             for (int i = 0; i < 2; ++i) {
                 const int rr = r0 + 8 * t + 2 * c + i;
                 if (rr >= s.n * a.group) continue;
-                const int64_t row = row_index(a, row0, h, rr);
+                const int64_t row = row_index(a, s, h, rr);
                 const float inv = l[t][i] == 0.0f ? 0.0f : 1.0f / l[t][i];
 #pragma unroll
                 for (int w = 0; w < DC; ++w) {
-                    if (w >= a.d / KV_B) break;
+                    if (!FULL && w >= a.d / KV_B) break;
                     kv_store(a.out, row * a.d + 16 * w + g, o[t][w][i] * inv, a.dtype);
                     kv_store(a.out, row * a.d + 16 * w + g + 8, o[t][w][i + 2] * inv, a.dtype);
                 }
@@ -538,7 +597,7 @@ struct Record {
 
 // Shared memory of a CTA
 struct Smem {
-    size_t cum, seq, rec, bars, scratch, ring, total;
+    size_t cum, seq, rec, win, bars, scratch, ring, warp_ring, total;
 };
 template <class Rows>
 __host__ __device__ __forceinline__ Smem smem_of(int nb, int d, int nw, int ns) {
@@ -546,45 +605,58 @@ __host__ __device__ __forceinline__ Smem smem_of(int nb, int d, int nw, int ns) 
     s.cum = 0;
     s.seq = s.cum + 8 * (size_t)(nb + 1);
     s.seq = (s.seq + 15) & ~size_t(15);
-    s.rec = s.seq + 16 * (size_t)nb;
-    s.bars = s.rec + sizeof(Record) * 2 * nw;
+    s.rec = (s.seq + sizeof(Seq) * nb + 15) & ~size_t(15);
+    s.win = s.rec + sizeof(Record) * 2 * nw;
+    s.bars = s.win + sizeof(float4) * 64 * nw;
     s.scratch = (s.bars + 8 * (size_t)nw * ns + 127) & ~size_t(127);
     s.ring = (s.scratch + nw * Rows::scratch(d) + 127) & ~size_t(127);
-    // after the loop the ring's memory holds a part of every warp
-    const size_t ring = (size_t)nw * ns * 2 * KV_B * d, parts = (size_t)nw * part_floats<Rows::RT>(d) * 4;
-    s.total = s.ring + (ring > parts ? ring : parts) + 256;  // ldmatrix reads chunks in pairs
+    // a warp's ring, and after the loop its part of the unit still open
+    const size_t ring = (size_t)ns * 2 * KV_B * d, part = (size_t)part_floats<Rows::RT>(d) * 4;
+    s.warp_ring = ((ring > part ? ring : part) + 127) & ~size_t(127);
+    s.total = s.ring + nw * s.warp_ring + 256;  // ldmatrix reads chunks in pairs
     return s;
 }
 
-// cum and seq of the launch's sequences (one sequence with `whole`)
+__device__ __forceinline__ int64_t scan_add(int64_t x, int lane) {  // inclusive, over a warp
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
+
+// cum and seq of the launch's sequences (one sequence with `whole`); ends with
+// a barrier
 template <int RT>
 __device__ void line_up(const KvAttnArgs &a, int b0, int nb, int64_t *cum, Seq *seq) {
     __shared__ int64_t warp_sum[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = blockDim.x >> 5;
+    const auto items = [&](int i) {
+        if (i >= nb) return int64_t(0);
+        const Seq s = seq_of(a, b0 + i);
+        seq[i] = s;
+        return (int64_t)s.cnt * tiles_of(a, s, RT) * a.heads;
+    };
+    if (nb <= 32) {
+        if (warp == 0) {
+            const int64_t v = items(lane), x = scan_add(v, lane);
+            if (lane < nb) cum[lane] = x - v;
+            if (lane == 31) cum[nb] = x;
+        }
+        __syncthreads();
+        return;
+    }
     int64_t before = 0;
     for (int base = 0; base < nb; base += blockDim.x) {
         const int i = base + tid;
-        int64_t v = 0;
-        if (i < nb) {
-            const Seq s = seq_of(a, b0 + i);
-            seq[i] = s;
-            v = (int64_t)s.cnt * tiles_of(a, s, RT) * a.heads;
-        }
-        int64_t x = v;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
-        }
+        const int64_t v = items(i), x = scan_add(v, lane);
         if (lane == 31) warp_sum[warp] = x;
         __syncthreads();
-        int64_t all = 0, mine = 0;
-        for (int w = 0; w < nw; ++w) {
-            if (w == warp) mine = all;
-            all += warp_sum[w];
-        }
+        const int64_t sums = scan_add(lane < nw ? warp_sum[lane] : 0, lane);
+        const int64_t mine = warp ? __shfl_sync(0xffffffffu, sums, warp - 1) : 0;
         if (i < nb) cum[i] = before + mine + x - v;
-        before += all;
+        before += __shfl_sync(0xffffffffu, sums, 31);
         __syncthreads();
     }
     if (tid == 0) cum[nb] = before;
@@ -611,7 +683,8 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
     const uint32_t bars = su32(smem + sm.bars) + 8 * warp * ns;
     uint8_t *scratch = smem + sm.scratch + warp * Rows::scratch(a.d);
     const int half = KV_B * a.d;  // bytes of a block's keys
-    uint8_t *ring = smem + sm.ring + (size_t)warp * ns * 2 * half;
+    uint8_t *ring = smem + sm.ring + warp * sm.warp_ring;
+    const uint32_t ring_u = su32(ring);
 
     if (lane == 0)
         for (int i = 0; i < ns; ++i)
@@ -635,7 +708,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
     for (int i = a.whole ? 0 : blockIdx.x; i < nb; i += a.whole ? 1 : gridDim.x) {
         const Seq s = seq[i];
         if (s.cnt > 0 || s.n == 0 || (a.whole && whole_unit != 0)) continue;
-        const int64_t row = kv_rows_of(a.cu, b0 + i, a.tokens, a.max_tokens).x, hq = a.heads * a.group;
+        const int64_t row = s.row0, hq = a.heads * a.group;
         for (int64_t e = tid; e < s.n * hq * a.d; e += NW * 32) kv_store(a.out, row * hq * a.d + e, 0.0f, a.dtype);
         if (a.lse)
             for (int64_t e = tid; e < s.n * hq; e += NW * 32) a.lse[row * hq + e] = -INFINITY;
@@ -645,29 +718,39 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
     Rows rows;
     bool open = false, ok = true;
     int useq = 0, uunit = 0;       // the open unit
-    int urow0 = 0, ur0 = 0;        // ... its sequence's first row in the token tensors, its first row
+    int ur0 = 0;                   // ... its first row of its sequence's
+    int ublk = 0;                  // ... the block of the window's item 0, were it of this unit
     int safe_last = 0, safe_first = 0;  // blocks within [first, last] need no mask
     if (i1 > i0) {
+        float4 *win = reinterpret_cast<float4 *>(smem + sm.win) + 64 * warp;
+        int side = 0;  // half of win that holds cur's scales
         Window cur, next;
-        window_fill<RT>(a, line, i0, i1, lane, cur);
+        window_pages<RT>(a, line, i0, i1, lane, cur);
+        window_blocks(a, cur);
         int64_t base = i0;
-        uint32_t to_issue = cur.todo;
-        bool ahead = false;  // to_issue belongs to `next`
-        uint32_t issued = 0, taken = 0;
+        uint32_t to_issue = cur.todo, flying = 0;
+        bool ahead = false, known = false;  // to_issue belongs to `next`; next's blocks are known
+        int put_at = 0, take_at = 0;
+        uint32_t phase = 0;  // parity of the stage taken next
         const auto issue = [&](int at) {
-            const uint32_t st = issued % ns;
             if (lane == 0) {
-                const uint32_t b = bars + 8 * st, dst = su32(ring + (size_t)st * 2 * half);
+                const uint32_t b = bars + 8 * put_at, dst = ring_u + put_at * 2 * half;
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(2u * half) : "memory");
                 bulk_g2s(dst, a.k + (int64_t)at * half, half, b);
                 bulk_g2s(dst + half, a.v + (int64_t)at * half, half, b);
             }
-            ++issued;
+            put_at = put_at + 1 == ns ? 0 : put_at + 1;
+            ++flying;
         };
+        while (to_issue && flying < (uint32_t)ns) {  // the first copies go out before the next window is known
+            const int i = __ffs(to_issue) - 1;
+            to_issue &= to_issue - 1;
+            issue(__shfl_sync(0xffffffffu, cur.at, i));
+        }
         const auto fill_ring = [&] {
-            while (issued - taken < (uint32_t)ns) {
+            while (flying < (uint32_t)ns) {
                 if (!to_issue) {
-                    if (ahead) break;
+                    if (ahead || !known) break;
                     ahead = true;
                     to_issue = next.todo;
                     continue;
@@ -677,116 +760,119 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
                 issue(__shfl_sync(0xffffffffu, ahead ? next.at : cur.at, i));
             }
         };
-        next.todo = 0;
-        while (to_issue && issued < (uint32_t)ns) {  // the first copies go out before the next window is known
-            const int i = __ffs(to_issue) - 1;
-            to_issue &= to_issue - 1;
-            issue(__shfl_sync(0xffffffffu, cur.at, i));
-        }
-        window_fill<RT>(a, line, base + 32, i1, lane, next);
+        window_pages<RT>(a, line, base + 32, i1, lane, next);
+        window_scales(cur, win, lane);
         const auto leave = [&](bool last) {  // the open unit ends here, for this warp
             const Seq s = seq[useq];
             rows.close(lane);
             if (!ok) rows.poison();
             const int64_t u0 = cum[useq] + (int64_t)uunit * s.cnt;
-            if (u0 >= i0 && u0 + s.cnt <= i1) {
-                rows.finish(a, s, urow0, uunit % a.heads, ur0, lane);
+            const bool done = u0 >= i0 && u0 + s.cnt <= i1;
+            if (done) {
+                rows.finish(a, s, a.by_heads.mod(uunit), ur0, lane);
             } else if (!last) {
                 float *dst = a.part_warp + ((int64_t)blockIdx.x * NW + warp) * part_floats<RT>(a.d);
                 rows.put(a, dst, lane);
                 if (lane == 0) rec[2 * warp] = Record{useq, uunit, dst};
             }
-            return !(u0 >= i0 && u0 + s.cnt <= i1);
+            return !done;
         };
         for (;;) {
-            for (int i = 0; i < cur.n && ok; ++i) {
+            // next: its blocks a few items into this window, its scales some later
+            for (int i = 0; i < cur.n; ++i) {
+                if (i == 8) {
+                    window_blocks(a, next);
+                    known = true;
+                    fill_ring();
+                }
+                if (i == 20) window_scales(next, win + 32 * (side ^ 1), lane);
                 if (!open || ((cur.starts >> i) & 1)) {
                     if (open) leave(false);
                     open = true;
                     useq = __shfl_sync(0xffffffffu, cur.seq, i);
                     uunit = __shfl_sync(0xffffffffu, cur.unit, i);
+                    ublk = __shfl_sync(0xffffffffu, cur.blk, i) - i;
                     const Seq s = seq[useq];
-                    urow0 = kv_rows_of(a.cu, b0 + useq, a.tokens, a.max_tokens).x;
-                    ur0 = uunit / a.heads * RT;
+                    ur0 = a.by_heads.div(uunit) * RT;
                     safe_last = last_of(a, s, ur0);
                     safe_first = first_of(a, s, min(ur0 + RT, s.n * a.group) - 1);
-                    rows.begin(a, s, urow0, uunit % a.heads, ur0, scratch, lane);
+                    rows.begin(a, s, a.by_heads.mod(uunit), ur0, scratch, lane);
                 }
                 if (!((cur.todo >> i) & 1)) continue;
-                const int blk = __shfl_sync(0xffffffffu, cur.blk, i);
-                const float ks = __shfl_sync(0xffffffffu, cur.ks, i);
-                const float lvs = __shfl_sync(0xffffffffu, cur.lvs, i);
-                const float ivs = __shfl_sync(0xffffffffu, cur.ivs, i);
-                const uint32_t st = taken % ns;
-                if (!__all_sync(0xffffffffu, bar_wait(bars + 8 * st, (taken / ns) & 1u))) {
+                const int blk = ublk + i;
+                const float4 sc = win[32 * side + i];
+                if (!__all_sync(0xffffffffu, bar_wait(bars + 8 * take_at, phase))) {
                     ok = false;
                     break;
                 }
-                const uint8_t *K = ring + (size_t)st * 2 * half;
+                const uint8_t *K = ring + take_at * 2 * half;
                 const bool mask = blk * KV_B < safe_first || blk * KV_B + KV_B - 1 > safe_last;
-                rows.block(a, seq[useq], ur0, K, K + half, blk, ks, lvs, ivs, mask, lane);
+                rows.block(a, seq[useq], ur0, K, K + half, blk, sc.x, sc.y, sc.z, mask, lane);
                 __syncwarp();
-                ++taken;
+                if (++take_at == ns) take_at = 0, phase ^= 1u;
+                --flying;
                 fill_ring();
             }
             base += 32;
             if (base >= i1 || !ok) break;
             cur = next;
+            side ^= 1;
+            ublk += 32;
             if (ahead) ahead = false;
             else to_issue = cur.todo;
-            window_fill<RT>(a, line, base + 32, i1, lane, next);
+            known = false;
+            window_pages<RT>(a, line, base + 32, i1, lane, next);
             fill_ring();
         }
         if (!ok) {  // a copy did not arrive: let the others land before the memory is given up
-            for (; taken < issued; ++taken) bar_wait(bars + 8 * (taken % ns), (taken / ns) & 1u);
+            for (; flying > 0; --flying) {
+                bar_wait(bars + 8 * take_at, phase);
+                if (++take_at == ns) take_at = 0, phase ^= 1u;
+            }
             if (lane == 0 && a.status) *a.status = 1;
         }
         open = leave(true);
     }
-    __syncthreads();
-    // the parts of units still open go to the ring's memory
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // a unit still open leaves its part where the warp's ring was
     const int64_t pf = part_floats<RT>(a.d);
     if (open) {
-        float *dst = reinterpret_cast<float *>(smem + sm.ring) + warp * pf;
+        float *dst = reinterpret_cast<float *>(ring);
+        __syncwarp();
         rows.put(a, dst, lane);
         if (lane == 0) rec[2 * warp + 1] = Record{useq, uunit, dst};
     }
     __syncthreads();
-    for (int i = 0; i < 2 * NW;) {
-        const Record r = rec[i];
-        if (r.unit < 0) {
-            ++i;
-            continue;
-        }
-        const float *parts[2 * NW];
-        int np = 0;
-        for (; i < 2 * NW; ++i) {
-            const Record n = rec[i];
-            if (n.unit < 0) continue;
-            if (n.seq != r.seq || n.unit != r.unit) break;
-            parts[np++] = n.part;
-        }
-        const Seq s = seq[r.seq];
-        const int64_t u0 = cum[r.seq] + (int64_t)r.unit * s.cnt, u1 = u0 + s.cnt;
+    const Record mine = lane < 2 * NW ? rec[lane] : Record{0, -1, nullptr};
+    for (uint32_t left = __ballot_sync(0xffffffffu, mine.unit >= 0); left;) {
+        const int f = __ffs(left) - 1;
+        const int rs = __shfl_sync(0xffffffffu, mine.seq, f), ru = __shfl_sync(0xffffffffu, mine.unit, f);
+        const uint32_t same = __ballot_sync(0xffffffffu, mine.unit == ru && mine.seq == rs);
+        left &= ~same;
+        const Seq s = seq[rs];
+        const int64_t u0 = cum[rs] + (int64_t)ru * s.cnt, u1 = u0 + s.cnt;
         float *dst = u0 >= c0 && u1 <= c1 ? nullptr : a.part_cta + ((int64_t)blockIdx.x * 2 + (u0 < c0 ? 0 : 1)) * pf;
-        const int row0 = kv_rows_of(a.cu, b0 + r.seq, a.tokens, a.max_tokens).x;
-        merge_parts<RT>(a, parts, np, s, row0, r.unit, dst, tid, NW * 32);
+        merge_parts<RT>(a, mine.part, same, s, ru, dst, warp, NW, lane);
     }
 }
 
-// One CTA a unit: merges what the CTAs of kv_rows_kernel left of it.  grid:
-// that kernel's CTAs.
+// One CTA a row of a unit: merges what the CTAs of kv_rows_kernel left of it,
+// a warp every fourth part, then the warps' sums.  grid: that kernel's CTAs.
 template <int RT>
 __global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ KvAttnArgs a, int nw, int64_t grid) {
     __shared__ int64_t sums[2][4];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int per = a.max_tiles * a.heads;
-    const int mine = blockIdx.x / per, unit = blockIdx.x % per;
+    __shared__ float tops[4], sl[4], weight[KV_SMS];
+    __shared__ float4 so[3][64];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = a.max_tiles * a.heads, r = blockIdx.x % RT;
+    const int mine = blockIdx.x / RT / per, unit = blockIdx.x / RT % per;
+    const Seq s = seq_of(a, a.b0 + mine);
+    if (s.cnt == 0 || unit >= tiles_of(a, s, RT) * a.heads || a.by_heads.div(unit) * RT + r >= s.n * a.group) return;
     // items before this sequence, and all of them
     int64_t before = 0, all = 0;
-    for (int i = threadIdx.x; i < a.nb; i += 128) {
-        const Seq s = seq_of(a, a.b0 + i);
-        const int64_t v = (int64_t)s.cnt * tiles_of(a, s, RT) * a.heads;
+    for (int i = tid; i < a.nb; i += 128) {
+        const Seq q = seq_of(a, a.b0 + i);
+        const int64_t v = (int64_t)q.cnt * tiles_of(a, q, RT) * a.heads;
         all += v;
         if (i < mine) before += v;
     }
@@ -795,12 +881,10 @@ __global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ Kv
         before += __shfl_xor_sync(0xffffffffu, before, o);
         all += __shfl_xor_sync(0xffffffffu, all, o);
     }
-    if ((threadIdx.x & 31) == 0) sums[0][threadIdx.x >> 5] = before, sums[1][threadIdx.x >> 5] = all;
+    if (lane == 0) sums[0][warp] = before, sums[1][warp] = all;
     __syncthreads();
     before = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
     all = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
-    const Seq s = seq_of(a, a.b0 + mine);
-    if (s.cnt == 0 || unit >= tiles_of(a, s, RT) * a.heads) return;
     const int64_t u0 = before + (int64_t)unit * s.cnt, u1 = u0 + s.cnt;
     const int64_t C = active_ctas(all, nw, grid);
     // CTA c takes [all c / C, all (c + 1) / C): the one that holds an item
@@ -810,50 +894,76 @@ __global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ Kv
         while (all * c / C > item) --c;
         return c;
     };
-    const int64_t first = holder(u0), last = holder(u1 - 1);
-    if (first == last) return;
+    const int first = (int)holder(u0), np = (int)holder(u1 - 1) - first + 1;
+    if (np == 1) return;
     const int64_t pf = part_floats<RT>(a.d);
-    const int64_t row0 = kv_rows_of(a.cu, a.b0 + mine, a.tokens, a.max_tokens).x;
-    const int h = unit % a.heads, r0 = unit / a.heads * RT;
-    const int rows = min(RT, s.n * a.group - r0), d4 = a.d / 4;
-    const auto part = [&](int64_t c) {
-        // the first CTA left it open at its end (slot 1) unless it begins exactly with it
-        return a.part_cta + (c * 2 + (all * c / C > u0 ? 0 : 1)) * pf;
-    };
-    for (int e = threadIdx.x; e < rows * d4; e += 128) {
-        const int r = e / d4, c4 = e - r * d4;
-        float m = M_NONE, l = 0.0f;
-        for (int64_t c = first; c <= last; ++c) m = fmaxf(m, part(c)[2 * r]);
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int64_t c = first; c <= last; ++c) {
-            const float *p = part(c);
-            const float w = exp2f(p[2 * r] - m);
-            const float4 v = *reinterpret_cast<const float4 *>(p + part_head<RT>() + r * a.d + 4 * c4);
-            l = fmaf(p[2 * r + 1], w, l);
-            o.x = fmaf(v.x, w, o.x), o.y = fmaf(v.y, w, o.y), o.z = fmaf(v.z, w, o.z), o.w = fmaf(v.w, w, o.w);
-        }
-        const int64_t row = row_index(a, (int)row0, h, r0 + r);
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        kv_store(a.out, row * a.d + 4 * c4, o.x * inv, a.dtype);
-        kv_store(a.out, row * a.d + 4 * c4 + 1, o.y * inv, a.dtype);
-        kv_store(a.out, row * a.d + 4 * c4 + 2, o.z * inv, a.dtype);
-        kv_store(a.out, row * a.d + 4 * c4 + 3, o.w * inv, a.dtype);
-        if (c4 == 0 && a.lse) a.lse[row] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
+    // the first CTA left it open at its end (slot 1), the others found it begun (slot 0)
+    const float *base = a.part_cta + (int64_t)first * 2 * pf;
+    const auto part = [&](int i) { return base + (2 * (int64_t)i + (i == 0 ? 1 : 0)) * pf; };
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    float m = M_NONE;
+    for (int i = tid; i < np; i += 128) m = fmaxf(m, part(i)[2 * r]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) tops[warp] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    float l = 0.0f;
+    for (int i = tid; i < np; i += 128) {
+        const float2 ml = *reinterpret_cast<const float2 *>(part(i) + 2 * r);
+        const float f = ex2(ml.x - m);
+        weight[i] = f;
+        l = fmaf(ml.y, f, l);
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if (lane == 0) sl[warp] = l;
+    __syncthreads();
+    l = sl[0] + sl[1] + sl[2] + sl[3];
+    float4 o[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
+    const int d4 = a.d / 4;
+#pragma unroll 4
+    for (int i = warp; i < np; i += 4) {
+        const float f = weight[i];
+        const float4 *p = reinterpret_cast<const float4 *>(part(i) + part_head<RT>() + r * a.d);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (lane + 32 * k < d4) {
+                const float4 v = p[lane + 32 * k];
+                o[k].x = fmaf(v.x, f, o[k].x), o[k].y = fmaf(v.y, f, o[k].y);
+                o[k].z = fmaf(v.z, f, o[k].z), o[k].w = fmaf(v.w, f, o[k].w);
+            }
+    }
+    if (warp > 0)
+        for (int k = 0; k < 2; ++k) so[warp - 1][lane + 32 * k] = o[k];
+    __syncthreads();
+    if (warp > 0) return;
+    const int64_t row = row_index(a, s, a.by_heads.mod(unit),
+                                  a.by_heads.div(unit) * RT + r);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    for (int k = 0; k < 2; ++k)
+        if (lane + 32 * k < d4) {
+            float4 v = o[k];
+            for (int w = 0; w < 3; ++w) {
+                const float4 x = so[w][lane + 32 * k];
+                v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+            }
+            store_row4(a, row, lane + 32 * k, v, inv);
+        }
+    if (lane == 0 && a.lse) a.lse[row] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
 }
 
 constexpr size_t SMEM_MOST = 226 * 1024;  // the static part aside
 
 template <class Rows, int NW>
 cudaError_t run_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) {
-    auto kern = kv_rows_kernel<Rows, NW>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_MOST);
-    if (e != cudaSuccess) return e;
-    kern<<<(unsigned)p.grid, NW * 32, p.smem, st>>>(a, p.ns);
-    e = launched();
+    static SmemLimit limit;
+    cudaError_t e = limit.launch(kv_rows_kernel<Rows, NW>, SMEM_MOST, [&] {
+        kv_rows_kernel<Rows, NW><<<(unsigned)p.grid, NW * 32, p.smem, st>>>(a, p.ns);
+    });
     if (e != cudaSuccess || p.whole) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)p.units);
+    cfg.gridDim = dim3((unsigned)(p.units * Rows::RT));
     cfg.blockDim = dim3(128);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
@@ -890,11 +1000,20 @@ KvRowsPlan plan_rows(int nb, int heads, int group, int d, int max_tokens, int64_
 #define KV_ROWS_VARIANTS(X)                                                                              \
     X(1, 1, 64, (Fp32Rows<1, 2>), 16) X(1, 1, 128, (Fp32Rows<1, 4>), 16) X(1, 1, 256, (Fp32Rows<1, 8>), 8)  \
     X(1, 4, 64, (Fp32Rows<4, 2>), 16) X(1, 4, 128, (Fp32Rows<4, 4>), 16) X(1, 4, 256, (Fp32Rows<4, 8>), 8)  \
-    X(0, 8, 64, (MmaRows<4, 1>), 16) X(0, 8, 128, (MmaRows<8, 1>), 16) X(0, 8, 256, (MmaRows<16, 1>), 8)    \
-    X(0, 16, 64, (MmaRows<4, 2>), 16) X(0, 16, 128, (MmaRows<8, 2>), 8) X(0, 16, 256, (MmaRows<16, 2>), 8)  \
-    X(0, 32, 64, (MmaRows<4, 4>), 8) X(0, 32, 128, (MmaRows<8, 4>), 8)
+    KV_MMA_VARIANTS(X, true) KV_MMA_VARIANTS(X, false)
+#define KV_MMA_VARIANTS(X, FULL)                                                                            \
+    X(0, 8, 64, (MmaRows<4, 1, FULL>), 16) X(0, 8, 128, (MmaRows<8, 1, FULL>), 16)                          \
+    X(0, 8, 256, (MmaRows<16, 1, FULL>), 8) X(0, 16, 64, (MmaRows<4, 2, FULL>), 16)                         \
+    X(0, 16, 128, (MmaRows<8, 2, FULL>), 8) X(0, 16, 256, (MmaRows<16, 2, FULL>), 8)                        \
+    X(0, 32, 64, (MmaRows<4, 4, FULL>), 8) X(0, 32, 128, (MmaRows<8, 4, FULL>), 8)
 
 #define KV_UNPACK(...) __VA_ARGS__
+
+// variants for one d only come before those that take any
+template <class Rows>
+constexpr bool is_full() {
+    return Rows::ONE_D;
+}
 
 // span: positions that a unit's items may cover
 KvRowsPlan kv_rows_plan(int nb, int heads, int group, int d, int dtype, int max_tokens, int64_t span) {
@@ -915,8 +1034,10 @@ KvRowsPlan kv_rows_plan(int nb, int heads, int group, int d, int dtype, int max_
 
 cudaError_t launch_kv_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) {
     const int dmax = a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256;
+    const bool full = a.d == dmax;
 #define KV_RUN(FP32, RT, D, ROWS, NW) \
-    if (p.fp32 == FP32 && p.rt == RT && dmax == D) return run_rows<KV_UNPACK ROWS, NW>(a, p, st);
+    if (p.fp32 == FP32 && p.rt == RT && dmax == D && (full || !is_full<KV_UNPACK ROWS>())) \
+        return run_rows<KV_UNPACK ROWS, NW>(a, p, st);
     KV_ROWS_VARIANTS(KV_RUN)
 #undef KV_RUN
     return cudaErrorInvalidValue;

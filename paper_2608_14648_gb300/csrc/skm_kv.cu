@@ -214,6 +214,9 @@ int skm_kv_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn
     k.tokens = s->tokens;
     k.max_tokens = most_tokens(s);
     k.group = a->heads_q / c->heads;
+    k.by_heads = FastDiv(k.heads);
+    k.by_group = FastDiv(k.group);
+    k.by_bpp = FastDiv(k.bpp);
     k.causal = a->causal != 0;
     k.window = (int)std::min<int64_t>(a->window, KV_MOST);
     k.dtype = a->dtype;

@@ -1,6 +1,8 @@
 // 8-bit key/value cache: shared by the kernels (k_kv_*.cu) and their entry
 // points (skm_kv.cu).
 #pragma once
+#include <atomic>
+
 #include <cuda_fp16.h>
 
 #include "skm_internal.cuh"
@@ -12,6 +14,19 @@ constexpr int KV_SMS = 152;
 // sequences whose prefix sums one launch keeps in shared memory; larger
 // batches take several launches
 constexpr int KV_MAX_SEQS = 1024;
+
+// n / d for 0 <= n < 2^31 without a division (the divisors of a launch: a
+// division is a chain of some 40 dependent instructions)
+struct FastDiv {
+    uint32_t d, mul, shift;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t n) : d(n), shift(0) {
+        while ((uint64_t(1) << shift) < n) ++shift;
+        mul = (uint32_t)(((uint64_t(1) << 32) * ((uint64_t(1) << shift) - n)) / n + 1);
+    }
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi(mul, (uint32_t)n) + (uint32_t)n) >> shift); }
+    __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
+};
 
 struct KvTokens {
     const void *x;
@@ -39,6 +54,7 @@ struct KvAttnArgs {
     int heads, d, page, pages, bpp, cols, tokens, max_tokens;
     int b0, nb;  // sequences of this launch
     int group, causal, window, dtype;
+    FastDiv by_heads, by_group, by_bpp;
     float scale_log2;
     const void *Q;
     int64_t q_token, q_head;
@@ -70,6 +86,31 @@ struct KvPromptPlan {
 bool kv_prompt_ok(int d, int dtype, int64_t rows);
 KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens, int64_t span);
 cudaError_t launch_kv_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st);
+
+// A kernel's shared-memory limit, raised once a device: the call costs a
+// microsecond, as much as a fifth of a small launch.  A launch that is refused (the
+// device was reset since) raises it again.
+struct SmemLimit {
+    std::atomic<uint64_t> raised{0};
+    template <class Kernel, class Launch>
+    cudaError_t launch(Kernel *kern, size_t bytes, Launch &&go) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = uint64_t(1) << (dev & 63);
+        for (int again = 0;; ++again) {
+            const bool was = dev < 64 && (raised.load(std::memory_order_relaxed) & bit) && !again;
+            if (!was) {
+                e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+                if (e != cudaSuccess) return e;
+                raised.fetch_or(bit, std::memory_order_relaxed);
+            }
+            go();
+            if (!was || cudaPeekAtLastError() != cudaErrorInvalidValue) return launched();
+            cudaGetLastError();
+        }
+    }
+};
 
 // ---- device helpers
 __device__ __forceinline__ float kv_code(uint32_t word, int byte) {

@@ -9,7 +9,7 @@ namespace {
 
 constexpr unsigned long long WAIT_NS = 2000000000ull;
 constexpr float M_NONE = -3.0e38f;  // the reference before the first logit
-constexpr float M_SLACK = 15.0f, M_BELOW = 7.0f;
+constexpr float M_SLACK = 15.0f, M_BELOW = 7.0f, M_MOST = 32768.0f;  // M_MOST = 2^M_SLACK
 constexpr float LN2 = 0.69314718055994531f;
 
 __device__ __forceinline__ float ex2(float x) {  // 2^x, 2 units in the last place, subnormal results 0
@@ -53,11 +53,14 @@ __device__ __forceinline__ void bulk_g2s(uint32_t dst, const void *src, uint32_t
 struct Seq {
     int lo, cnt;  // first block that a row sees, blocks
     int len, n;   // tokens held, rows
+    int row0;     // its first row in the token tensors
 };
 __device__ __forceinline__ Seq seq_of(const KvAttnArgs &a, int b) {
     Seq s;
     s.len = kv_clamp(a.pos[b], 0, a.cols * a.page);
-    s.n = kv_rows_of(a.cu, b, a.tokens, a.max_tokens).y;
+    const int2 rows = kv_rows_of(a.cu, b, a.tokens, a.max_tokens);
+    s.row0 = rows.x;
+    s.n = rows.y;
     s.lo = a.window > 0 ? max(0, s.len - s.n - a.window + 1) / KV_B : 0;
     s.cnt = s.n > 0 ? (s.len + KV_B - 1) / KV_B - s.lo : 0;
     if (s.cnt < 0) s.cnt = 0;
@@ -68,17 +71,17 @@ __device__ __forceinline__ int tiles_of(const KvAttnArgs &a, const Seq &s, int r
 }
 // the last / first position that row r of a sequence may see (last < first: none)
 __device__ __forceinline__ int last_of(const KvAttnArgs &a, const Seq &s, int r) {
-    const int i = r / a.group;
+    const int i = a.by_group.div(r);
     if (i >= s.n) return -1;
     return a.causal ? min(s.len - 1, s.len - s.n + i) : s.len - 1;
 }
 __device__ __forceinline__ int first_of(const KvAttnArgs &a, const Seq &s, int r) {
-    return a.window > 0 ? max(0, s.len - s.n + r / a.group - a.window + 1) : 0;
+    return a.window > 0 ? max(0, s.len - s.n + a.by_group.div(r) - a.window + 1) : 0;
 }
 
 // Where a row's result goes
-__device__ __forceinline__ int64_t row_index(const KvAttnArgs &a, int row0, int h, int r) {
-    return ((int64_t)row0 + r / a.group) * (a.heads * a.group) + h * a.group + r % a.group;
+__device__ __forceinline__ int64_t row_index(const KvAttnArgs &a, const Seq &s, int h, int r) {
+    return ((int64_t)s.row0 + a.by_group.div(r)) * (a.heads * a.group) + h * a.group + a.by_group.mod(r);
 }
 
 // codes of bytes 0, 1 / 2, 3 of a word as two f16: 1024 + u as bits, minus 1152
