@@ -830,7 +830,8 @@ int skm_kv_read(const skm_kv_cache *c, const skm_kv_seqs *s, int dtype, void *K,
  *  out dtype [tokens][heads_q][d], lse float32 [tokens][heads_q] or NULL: contiguous
  * dtype BF16 or F16: products on tensor cores of codes (exact in f16) and of the
  * queries (bf16 rows scaled by a power of two to f16), sums and softmax in fp32,
- * the probabilities rounded to f16; F32: fp32 arithmetic throughout.
+ * the probabilities rounded to f16; F32: fp32 arithmetic throughout.  Value
+ * scales below 2^-80 count as 2^-80.
  *  status: device int32 or NULL; set to 1 when a bounded device wait gave up
  *  (some rows are then NaN or not written), otherwise left alone.
  *  ws: skm_kv_attend_workspace_size(c, s, a) bytes, 256-byte aligned (0 bytes: may be

@@ -474,10 +474,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
             const bool vals = task & KBLK;
             if (!warp_wait(vals ? v_free(st) : k_free(st), ((j / ST) & 1) ^ 1, gone)) break;
             if (!vals) {
-                if (lane == 0)
-                    info[(j & (INFO - 1)) * KBLK + blk] =
-                        at >= 0 ? make_float4(sc.x, sc.y > 0.0f ? log2f(sc.y) : 0.0f, sc.y > 0.0f ? 1.0f / sc.y : 1.0f, 1.0f)
-                                : make_float4(0.0f, 0.0f, 1.0f, 0.0f);
+                if (lane == 0) {
+                    float4 f = value_scale(sc);
+                    f.w = at >= 0 ? 1.0f : 0.0f;
+                    info[(j & (INFO - 1)) * KBLK + blk] = f;
+                }
             }
             if (at >= 0) {
                 const uint32_t base = sm + (vals ? L::v : L::k) + st * L::TILE;

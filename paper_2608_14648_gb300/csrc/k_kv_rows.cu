@@ -99,9 +99,7 @@ __device__ __forceinline__ void window_blocks(const KvAttnArgs &a, Window &w) {
     w.todo = __ballot_sync(0xffffffffu, there);
 }
 __device__ __forceinline__ void window_scales(const Window &w, float4 *mem, int lane) {
-    // a block of zeros has scale 0: any value scale will do
-    const float vs = w.sc.y > 0.0f ? w.sc.y : 1.0f;
-    mem[lane] = make_float4(w.sc.x, log2f(vs), 1.0f / vs, 0.0f);
+    mem[lane] = value_scale(w.sc);
     __syncwarp();
 }
 
@@ -134,12 +132,13 @@ __host__ __device__ __forceinline__ int64_t part_floats(int d) {
 // Merges parts of one unit: the lanes in `same` hold one each, in order.  A
 // warp takes a row: a lane its part's (m, l), then all lanes the row's dims.  To
 // the outputs (dst NULL) or as a part again.
-template <int RT>
+template <int RT, int Q>
 __device__ __forceinline__ void merge_parts(const KvAttnArgs &a, const float *part, uint32_t same, const Seq &s, int unit,
                                             float *dst, int warp, int warps, int lane) {
     const int d4 = a.d / 4, h = a.by_heads.mod(unit), r0 = a.by_heads.div(unit) * RT;
     const int rows = min(RT, s.n * a.group - r0);
     const bool mine = (same >> lane) & 1;
+#pragma unroll 1
     for (int r = warp; r < rows; r += warps) {
         const float2 ml = mine ? *reinterpret_cast<const float2 *>(part + 2 * r) : make_float2(M_NONE, 0.0f);
         float m = ml.x;
@@ -149,7 +148,10 @@ __device__ __forceinline__ void merge_parts(const KvAttnArgs &a, const float *pa
         float l = ml.y * f;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-        float4 o[2] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
+        float4 o[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) o[q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
         for (uint32_t bits = same; bits;) {
             float w[4];
             const float4 *p[4];
@@ -163,7 +165,7 @@ __device__ __forceinline__ void merge_parts(const KvAttnArgs &a, const float *pa
                 bits &= bits - 1;
             }
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
+            for (int q = 0; q < Q; ++q) {
                 if (lane + 32 * q >= d4) break;
                 float4 v[4];
 #pragma unroll
@@ -178,7 +180,7 @@ __device__ __forceinline__ void merge_parts(const KvAttnArgs &a, const float *pa
         const int64_t row = row_index(a, s, h, r0 + r);
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < Q; ++q) {
             if (lane + 32 * q >= d4) break;
             if (dst) reinterpret_cast<float4 *>(dst + part_head<RT>() + r * a.d)[lane + 32 * q] = o[q];
             else store_row4(a, row, lane + 32 * q, o[q], inv);
@@ -190,22 +192,33 @@ __device__ __forceinline__ void merge_parts(const KvAttnArgs &a, const float *pa
     }
 }
 
+// The positions that a tile's rows see, kept by the warp for its masked blocks
+template <int RT>
+constexpr int LIMITS = (8 * RT + 15) & ~15;
+template <int RT>
+__device__ __forceinline__ void limits(const KvAttnArgs &a, const Seq &s, int r0, int2 *lim, int lane) {
+    if (lane < RT) lim[lane] = make_int2(last_of(a, s, r0 + lane), first_of(a, s, r0 + lane));
+}
+
 // Rows of one warp in fp32 on CUDA cores.  Scores: lane = (half, token), a
 // half takes every other 16-dim chunk of the keys; sums: lane = dims lane,
 // lane + 32, ...  q and p pass through the warp's shared memory.
 template <int R, int DPL>
 struct Fp32Rows {
-    static constexpr int RT = R;
+    static constexpr int RT = R, D4 = DPL > 4 ? 2 : 1;
     static constexpr bool ONE_D = false;
-    static size_t __host__ __device__ scratch(int d) { return (size_t)R * (d + KV_B) * 4; }
+    static size_t __host__ __device__ scratch(int d) { return (size_t)R * (d + KV_B) * 4 + LIMITS<R>; }
     float o[R][DPL], m[R], l[R];
     float *q, *p;
+    int2 *lim;
 
     __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int h, int r0, uint8_t *mem,
                                           int lane) {
-        q = reinterpret_cast<float *>(mem);
+        lim = reinterpret_cast<int2 *>(mem);
+        q = reinterpret_cast<float *>(mem + LIMITS<R>);
         p = q + R * a.d;
         __syncwarp();
+        limits<R>(a, s, r0, lim, lane);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             m[r] = M_NONE, l[r] = 0.0f;
@@ -219,8 +232,7 @@ struct Fp32Rows {
         __syncwarp();
     }
 
-    __device__ __forceinline__ void block(const KvAttnArgs &a, const Seq &s, int r0, const uint8_t *K, const uint8_t *V,
-                                          int blk, float ks, float lvs, float ivs, bool mask, int lane) {
+    __device__ __forceinline__ void block(const KvAttnArgs &a, const uint8_t *K, const uint8_t *V, int blk, float ks, float lvs, float ivs, bool mask, int lane) {
         const int t = lane & 15, half = lane >> 4, nc = a.d / KV_B;
         float x[R];
 #pragma unroll
@@ -248,7 +260,7 @@ struct Fp32Rows {
             x[r] = fmaf(x[r], ks, lvs);
             if (mask) {
                 const int j = blk * KV_B + t;
-                if (j > last_of(a, s, r0 + r) || j < first_of(a, s, r0 + r)) x[r] = -INFINITY;
+                if (j > lim[r].x || j < lim[r].y) x[r] = -INFINITY;
             }
             if (__any_sync(0xffffffffu, x[r] > m[r] + M_SLACK)) {
                 float top = x[r];
@@ -349,6 +361,19 @@ __device__ __forceinline__ void codes_a(uint32_t x, uint32_t y, uint32_t (&a)[4]
     a[3] = codes_f16(y, 0x4342);
 }
 
+// 4 values without the alignment of a vector (not inlined: a rare path)
+__device__ __noinline__ uint2 load4(const uint16_t *x) {
+    return make_uint2(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16);
+}
+// two bf16 times a power of two as f16
+__device__ __forceinline__ uint32_t bf16_f16(uint32_t w, float mul) {
+    const __half2 x = __floats2half2_rn(__uint_as_float(w << 16) * mul, __uint_as_float(w & 0xffff0000u) * mul);
+    return *reinterpret_cast<const uint32_t *>(&x);
+}
+__device__ __forceinline__ uint16_t bits16(float v, bool bf) {
+    return bf ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
+}
+
 // Rows of one warp on tensor cores, transposed: S^T = K q^T and o^T = V^T p^T
 // (16 tokens or dims x 8 rows x 16), so a tile of 8 rows wastes nothing when
 // the heads of a group are 8.  Both cache layouts are read by ldmatrix, 512
@@ -362,18 +387,23 @@ __device__ __forceinline__ void codes_a(uint32_t x, uint32_t y, uint32_t (&a)[4]
 template <int DC, int NT, bool FULL>
 struct MmaRows {
     static constexpr int RT = 8 * NT;
+    static constexpr int D4 = DC > 8 ? 2 : 1;
     static constexpr bool ONE_D = FULL;
     static constexpr bool QMEM = NT * DC >= 32;  // the queries' operands wait in shared memory
-    static size_t __host__ __device__ scratch(int) { return QMEM ? (size_t)NT * DC * 2 * 32 * 4 : 0; }
+    static size_t __host__ __device__ scratch(int) { return (QMEM ? (size_t)NT * DC * 2 * 32 * 4 : 0) + LIMITS<RT>; }
     float o[NT][DC][4], m[NT][2], l[NT][2], fac[NT][2];
     uint32_t q[QMEM ? 1 : NT][QMEM ? 1 : DC][2];
     uint2 *qmem;
+    int2 *lim;
 
     __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int h, int r0, uint8_t *mem,
                                           int lane) {
         const int g = lane >> 2, c = lane & 3, nc = FULL ? DC : a.d / KV_B;
-        qmem = reinterpret_cast<uint2 *>(mem);
+        lim = reinterpret_cast<int2 *>(mem);
+        qmem = reinterpret_cast<uint2 *>(mem + LIMITS<RT>);
         __syncwarp();
+        limits<RT>(a, s, r0, lim, lane);
+        const bool bf = a.dtype == SKM_DTYPE_BF16;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int rr = r0 + 8 * t + g;
@@ -381,29 +411,28 @@ struct MmaRows {
             const uint16_t *x = static_cast<const uint16_t *>(a.Q);
             if (in) x += (int64_t)(s.row0 + a.by_group.div(rr)) * a.q_token + (int64_t)(h * a.group + a.by_group.mod(rr)) * a.q_head + 4 * c;
             uint2 raw[DC];
-            float top = 0.0f;
 #pragma unroll
-            for (int w = 0; w < DC; ++w) {
-                raw[w] = make_uint2(0, 0);
-                if (in && w < nc) {
-                    if (a.q_wide) {
-                        raw[w] = *reinterpret_cast<const uint2 *>(x + 16 * w);
-                    } else {
-                        raw[w].x = x[16 * w] | (uint32_t)x[16 * w + 1] << 16;
-                        raw[w].y = x[16 * w + 2] | (uint32_t)x[16 * w + 3] << 16;
-                    }
-                }
+            for (int w = 0; w < DC; ++w) raw[w] = make_uint2(0, 0);
+            if (in && a.q_wide) {
+#pragma unroll
+                for (int w = 0; w < DC; ++w)
+                    if (w < nc) raw[w] = *reinterpret_cast<const uint2 *>(x + 16 * w);
+            } else if (in) {
+#pragma unroll
+                for (int w = 0; w < DC; ++w)
+                    if (w < nc) raw[w] = load4(x + 16 * w);
             }
             float mul = 1.0f, back = 1.0f;
-            if (a.dtype == SKM_DTYPE_BF16) {
+            if (bf) {
+                uint32_t top = 0;  // the largest |x| as bits (of one sign, they order like the numbers)
 #pragma unroll
                 for (int w = 0; w < DC; ++w) {
-                    top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw[w].x << 16)), fabsf(__uint_as_float(raw[w].x & 0xffff0000u))));
-                    top = fmaxf(top, fmaxf(fabsf(__uint_as_float(raw[w].y << 16)), fabsf(__uint_as_float(raw[w].y & 0xffff0000u))));
+                    top = max(max(top, raw[w].x << 16 & 0x7fff0000u), raw[w].x & 0x7fff0000u);
+                    top = max(max(top, raw[w].y << 16 & 0x7fff0000u), raw[w].y & 0x7fff0000u);
                 }
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const uint32_t ex = __float_as_uint(top) >> 23;
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const uint32_t ex = top >> 23;
                 if (ex > 0 && ex < 255) {
                     const uint32_t e = ex > 253 ? 253 : ex;
                     mul = __uint_as_float((254 - e) << 23);
@@ -412,13 +441,7 @@ struct MmaRows {
             }
 #pragma unroll
             for (int w = 0; w < DC; ++w) {
-                uint32_t b0 = raw[w].x, b1 = raw[w].y;
-                if (a.dtype == SKM_DTYPE_BF16) {
-                    const __half2 x0 = __floats2half2_rn(__uint_as_float(b0 << 16) * mul, __uint_as_float(b0 & 0xffff0000u) * mul);
-                    const __half2 x1 = __floats2half2_rn(__uint_as_float(b1 << 16) * mul, __uint_as_float(b1 & 0xffff0000u) * mul);
-                    b0 = *reinterpret_cast<const uint32_t *>(&x0);
-                    b1 = *reinterpret_cast<const uint32_t *>(&x1);
-                }
+                const uint32_t b0 = bf ? bf16_f16(raw[w].x, mul) : raw[w].x, b1 = bf ? bf16_f16(raw[w].y, mul) : raw[w].y;
                 if constexpr (QMEM) qmem[(t * DC + w) * 32 + lane] = make_uint2(b0, b1);
                 else q[t][w][0] = b0, q[t][w][1] = b1;
 #pragma unroll
@@ -435,8 +458,7 @@ struct MmaRows {
         __syncwarp();
     }
 
-    __device__ __forceinline__ void block(const KvAttnArgs &a, const Seq &s, int r0, const uint8_t *K, const uint8_t *V,
-                                          int blk, float ks, float lvs, float ivs, bool mask, int lane) {
+    __device__ __forceinline__ void block(const KvAttnArgs &a, const uint8_t *K, const uint8_t *V, int blk, float ks, float lvs, float ivs, bool mask, int lane) {
         const int g = lane >> 2, c = lane & 3, nc = FULL ? DC : a.d / KV_B;
         float x[NT][4];
 #pragma unroll
@@ -482,8 +504,9 @@ struct MmaRows {
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int j = blk * KV_B + g + 8 * (i >> 1), rr = r0 + 8 * t + 2 * c + (i & 1);
-                    if (j > last_of(a, s, rr) || j < first_of(a, s, rr)) x[t][i] = -INFINITY;
+                    const int j = blk * KV_B + g + 8 * (i >> 1);
+                    const int2 see = lim[8 * t + 2 * c + (i & 1)];
+                    if (j > see.x || j < see.y) x[t][i] = -INFINITY;
                 }
         }
         float p[NT][4];
@@ -576,11 +599,13 @@ struct MmaRows {
                 if (rr >= s.n * a.group) continue;
                 const int64_t row = row_index(a, s, h, rr);
                 const float inv = l[t][i] == 0.0f ? 0.0f : 1.0f / l[t][i];
+                uint16_t *dst = static_cast<uint16_t *>(a.out) + row * a.d + g;
+                const bool bf = a.dtype == SKM_DTYPE_BF16;
 #pragma unroll
                 for (int w = 0; w < DC; ++w) {
                     if (!FULL && w >= a.d / KV_B) break;
-                    kv_store(a.out, row * a.d + 16 * w + g, o[t][w][i] * inv, a.dtype);
-                    kv_store(a.out, row * a.d + 16 * w + g + 8, o[t][w][i + 2] * inv, a.dtype);
+                    dst[16 * w] = bits16(o[t][w][i] * inv, bf);
+                    dst[16 * w + 8] = bits16(o[t][w][i + 2] * inv, bf);
                 }
                 if (g == 0 && a.lse) a.lse[row] = l[t][i] == 0.0f ? -INFINITY : LN2 * (m[t][i] + log2f(l[t][i]));
             }
@@ -807,7 +832,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
                 }
                 const uint8_t *K = ring + take_at * 2 * half;
                 const bool mask = blk * KV_B < safe_first || blk * KV_B + KV_B - 1 > safe_last;
-                rows.block(a, seq[useq], ur0, K, K + half, blk, sc.x, sc.y, sc.z, mask, lane);
+                rows.block(a, K, K + half, blk, sc.x, sc.y, sc.z, mask, lane);
                 __syncwarp();
                 if (++take_at == ns) take_at = 0, phase ^= 1u;
                 --flying;
@@ -852,7 +877,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
         const Seq s = seq[rs];
         const int64_t u0 = cum[rs] + (int64_t)ru * s.cnt, u1 = u0 + s.cnt;
         float *dst = u0 >= c0 && u1 <= c1 ? nullptr : a.part_cta + ((int64_t)blockIdx.x * 2 + (u0 < c0 ? 0 : 1)) * pf;
-        merge_parts<RT>(a, mine.part, same, s, ru, dst, warp, NW, lane);
+        merge_parts<RT, Rows::D4>(a, mine.part, same, s, ru, dst, warp, NW, lane);
     }
 }
 

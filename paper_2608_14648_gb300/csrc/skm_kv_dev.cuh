@@ -84,6 +84,18 @@ __device__ __forceinline__ int64_t row_index(const KvAttnArgs &a, const Seq &s, 
     return ((int64_t)s.row0 + a.by_group.div(r)) * (a.heads * a.group) + h * a.group + a.by_group.mod(r);
 }
 
+// A block's scales as attention uses them: (key scale, log2 of the value scale,
+// 1 / value scale, 0).  Weights carry the value scale, so scales too far apart would push
+// the smaller ones' weights out of fp32: scales below 2^-80 (values below 1e-22,
+// blocks of zeros among them) count as 2^-80.
+__device__ __forceinline__ float4 value_scale(float2 sc) {
+    const float vs = fmaxf(sc.y, 8.271806e-25f);
+    float lg, inv;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lg) : "f"(vs));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(vs));
+    return make_float4(sc.x, lg, inv, 0.0f);
+}
+
 // codes of bytes 0, 1 / 2, 3 of a word as two f16: 1024 + u as bits, minus 1152
 __device__ __forceinline__ uint32_t codes_f16(uint32_t word, uint32_t sel) {
     const uint32_t x = __byte_perm(word, 0x64646464u, sel);

@@ -291,7 +291,7 @@ def attend_ref(held, table, length, cu, Q, group, scale, causal, window, typ):
 
 
 def check_attend(heads, group, d, page, typ, seqs, causal=True, window=0, absent=0.0, scale=None, seed=11, spread=1.0,
-                 strided=False, max_len=None, max_tokens=None):
+                 strided=False, max_len=None, max_tokens=None, spoil=None):
     """seqs: (tokens held before, query rows) of each sequence."""
     import paper_2608_14648_gb300 as skm
 
@@ -301,6 +301,8 @@ def check_attend(heads, group, d, page, typ, seqs, causal=True, window=0, absent
     c = make_cache(heads, d, page, pages, seed)
     table = make_table(len(seqs), cols, pages, seed)
     g = torch.Generator().manual_seed(seed + 1)
+    if spoil:
+        spoil(c)
     if absent:
         gone = torch.rand(table.shape, generator=g) < absent
         table = torch.where(gone, torch.full_like(table, -1), table)
@@ -410,6 +412,19 @@ def test_attend_sharp_rows(cuda_ok, typ, new):
 def test_attend_bf16_queries_beyond_f16(cuda_ok):
     check_attend(1, 4, 64, 16, "bf16", [(90, 1), (50, 100)], spread=1e6, scale=1e-6)
     check_attend(1, 4, 64, 16, "bf16", [(90, 1), (50, 100)], spread=1e-9, scale=1e8)
+
+
+@pytest.mark.parametrize("typ,new", [("bf16", 1), ("f16", 20), ("f16", 100), ("f32", 1)])
+def test_attend_value_scales_far_apart(cuda_ok, typ, new):
+    """Blocks of zeros, of tiny values and of large ones carry weight all the same."""
+    def spoil(c):
+        c.scales[0::5, :, :, 1] = 0.0
+        c.v[0::5] = 128
+        c.scales[1::5, :, :, 1] = 1e-35
+        c.scales[2::5, :, :, 1] = 3e-20
+        c.scales[3::5, :, :, 1] = 50.0
+
+    check_attend(2, 4, 64, 16, typ, [(300, new), (61, new)], spoil=spoil)
 
 
 def test_attend_hints_may_be_larger(cuda_ok):
