@@ -3,26 +3,29 @@
 //
 // A CTA takes 256 query rows (token-major, then the heads of a group) of one
 // sequence and key/value head as two tiles of 128, and walks the keys they see in
-// tiles of 128 positions (8 blocks of the cache).  The codes are exact in f16, so
+// tiles of 64 positions (4 blocks of the cache).  The codes are exact in f16, so
 // both products run in kind::f16 and the block scales stay out of the
 // operands: the key scale multiplies the logits of its block, the value scale
 // is added to them as log2 s_v (o = sum p c_v, l = sum p / s_v; the formulas of
 // k_kv_rows.cu, the running reference m included).
 //
-//   warps 0-3, 4-7  softmax of tile 0 / 1, one thread a row: S from TMEM in
-//                   pieces of a block, p = 2^(s f + c) to f16, P back to TMEM
-//                   over the columns S held (the A operand of the next product)
+//   warps 0-3, 4-7  softmax of tile 0 / 1, one thread a row: 64 logits from
+//                   TMEM, p = 2^(s f + c) to f16, P back to TMEM over the columns
+//                   S held (the A operand of the next product)
 //   warps 8-14      converters: a block of keys (or values) at a time from
 //                   global memory, one block ahead in registers, to f16 in the
 //                   128-byte-swizzled operand layout
-//   warp 15         MMA issuer: P0 V, Q0 K', P1 V, Q1 K' in turn, so the tensor
-//                   cores work on one tile while the other's softmax runs
+//   warp 15         MMA issuer
 //
-// TMEM: S0/P0, S1/P1 (128 columns each), O0, O1 (DH columns each).  The first
-// pass over a tile's logits assumes that m need not move and keeps P in
-// registers; a block whose sum exceeds 2^15 (m has to be set or moved, at a row's first
-// tile and rarely after it) sends the warp through a maximum, a rescaling of O
-// and a second pass.  Shared memory: Q, and rings of K and V tiles.
+// TMEM: two S/P buffers of 64 columns a tile, O0, O1 (DH columns each).  The
+// logits of a key tile are there before the softmax of the one before is done, so a
+// softmax warp never waits for the tensor cores to answer it (with one buffer
+// of 128 keys a tile the chain softmax, P V, Q K' took 5400 clocks for 256 x 128
+// logits where the tensor cores need 2048).  The first pass over a tile's
+// logits assumes that m need not move; a block whose sum exceeds 2^15 (m has to be
+// set or moved, at a row's first tile and rarely after it) sends the warp through a
+// maximum, a rescaling of O and a second pass.  Shared memory: Q, and rings of K and V
+// tiles.
 //
 // Few CTAs (short prompts): the keys are split over CTAs as well, and
 // kv_prompt_join_kernel merges the parts in order.
@@ -32,17 +35,19 @@ namespace skm {
 
 namespace {
 
-constexpr int QT = 128, KT = 128, KBLK = KT / KV_B;  // rows of a tile, keys of a tile, blocks of it
+constexpr int QT = 128, KT = 64, KBLK = KT / KV_B;  // rows of a tile, keys of a tile, blocks of it
 constexpr int CONV = 7, CONV_WARP0 = 8, MMA_WARP = 15, THREADS = 512;
-constexpr int INFO = 8;  // tiles whose scales are kept (more than the K ring holds)
+constexpr int INFO = 8;  // tiles whose scales are kept: those of the K ring and those its softmax still reads
 
+constexpr int ST = 4;  // K and V tiles in flight
 template <int DH>
 struct Lay {
-    static constexpr int STAGES = DH <= 64 ? 4 : 2;
-    static constexpr int TILE = QT * DH * 2;  // bytes of a Q, K or V tile
-    static constexpr int q = 0, k = 2 * TILE, v = k + STAGES * TILE, info = v + STAGES * TILE;
-    static constexpr int bars = info + INFO * KBLK * 16, slots = bars + 8 * (4 * STAGES + 8), total = slots + 16 + 1024;
-    static constexpr uint32_t O = 2 * KT;  // TMEM column of O0
+    static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
+    static constexpr int q = 0, k = 2 * QTILE, v = k + ST * TILE, info = v + ST * TILE;
+    static constexpr int bars = info + INFO * KBLK * 16, slots = bars + 8 * (4 * ST + 12);
+    // one CTA an SM: it takes all of TMEM
+    static constexpr int bytes = slots + 16 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
+    static constexpr uint32_t O = 4 * KT;  // TMEM column of O0
 };
 
 __device__ __forceinline__ void arrive(uint32_t b) {
@@ -72,8 +77,20 @@ __device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, volatile 
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void commit(uint32_t b) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(b) : "memory");
+// The issuing warp runs its loop converged and one elected lane (`one`) takes the
+// tcgen05 instructions by predicate, not by a branch: the operands then stay in
+// uniform registers.
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void commit(uint32_t b, uint32_t one) {
+    asm volatile(
+        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %1, 0;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(b),
+        "r"(one)
+        : "memory");
 }
 // K-major operand, 128-byte swizzle: rows of 128 bytes, groups of 8 rows
 __device__ __forceinline__ uint64_t operand(uint32_t addr) {
@@ -83,21 +100,34 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr) {
 constexpr uint32_t idesc(int n) {  // f16 x f16 -> f32, M = 128, both K-major
     return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(QT >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t add) {
+template <bool ADD>
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t one) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(id), "r"(add)
+        "{\n\t.reg .pred e, p;\n\tsetp.ne.b32 e, %4, 0;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(id), "r"(one), "n"(ADD)
         : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t add, uint32_t one) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d),
-        "r"(a), "l"(b), "r"(id), "r"(add)
+        "{\n\t.reg .pred e, p;\n\tsetp.ne.b32 e, %5, 0;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(id), "r"(add), "r"(one)
         : "memory");
 }
-// 16 columns; valid after ld_wait on the same registers
+// 32 / 16 columns; valid after ld_wait on the same registers
+__device__ __forceinline__ void ld32(uint32_t addr, uint32_t *v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(addr)
+        : "memory");
+}
 __device__ __forceinline__ void ld16(uint32_t addr, uint32_t (&v)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -112,6 +142,16 @@ __device__ __forceinline__ void ld_wait(uint32_t (&v)[16]) {
                  : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
                    "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]),
                    "+r"(v[15])
+                 :
+                 : "memory");
+}
+__device__ __forceinline__ void ld_wait32(uint32_t *v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]),
+                   "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]),
+                   "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]),
+                   "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
                  :
                  : "memory");
 }
@@ -204,7 +244,6 @@ __device__ __forceinline__ float load_row(const KvAttnArgs &a, const uint16_t *x
 template <int DH>
 __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_constant__ KvAttnArgs a, int splits, float *parts) {
     using L = Lay<DH>;
-    constexpr int ST = L::STAGES;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t *smem = smem_raw + ((1024 - (su32(smem_raw) & 1023)) & 1023);  // swizzle atoms
@@ -214,10 +253,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
     const auto k_free = [&](int s) { return bar(ST + s); };
     const auto v_full = [&](int s) { return bar(2 * ST + s); };
     const auto v_free = [&](int s) { return bar(3 * ST + s); };
-    const auto s_full = [&](int q) { return bar(4 * ST + q); };
-    const auto p_full = [&](int q) { return bar(4 * ST + 2 + q); };
-    const auto o_done = [&](int q) { return bar(4 * ST + 4 + q); };
-    const uint32_t q_full = bar(4 * ST + 6), drain = bar(4 * ST + 7);
+    const auto s_full = [&](int q, int buf) { return bar(4 * ST + 2 * q + buf); };
+    const auto p_full = [&](int q, int buf) { return bar(4 * ST + 4 + 2 * q + buf); };
+    const auto o_done = [&](int q) { return bar(4 * ST + 8 + q); };
+    const uint32_t q_full = bar(4 * ST + 10), drain = bar(4 * ST + 11);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::slots);
     volatile int32_t *gone = reinterpret_cast<volatile int32_t *>(smem + L::slots + 4);
     float4 *info = reinterpret_cast<float4 *>(smem + L::info);  // (k scale, log2 v scale, 1 / v scale, there)
@@ -249,8 +288,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(v_free(i)), "r"(1) : "memory");
         }
         for (int q = 0; q < 2; ++q) {
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s_full(q)), "r"(1) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(p_full(q)), "r"(4) : "memory");
+            for (int i = 0; i < 2; ++i) {
+                asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s_full(q, i)), "r"(1) : "memory");
+                asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(p_full(q, i)), "r"(4) : "memory");
+            }
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(o_done(q)), "r"(1) : "memory");
         }
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(q_full), "r"(8) : "memory");
@@ -276,7 +317,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         const bool in = r < rows;
         const uint16_t *x = static_cast<const uint16_t *>(a.Q);
         if (in) x += (int64_t)(s.row0 + a.by_group.div(r)) * a.q_token + (int64_t)(h * a.group + a.by_group.mod(r)) * a.q_head;
-        const float fac = load_row<DH>(a, x, in, sm + L::q + q * L::TILE, row);
+        const float fac = load_row<DH>(a, x, in, sm + L::q + q * L::QTILE, row);
         fence_async();
         __syncwarp();
         if (lane == 0) arrive(q_full);
@@ -284,84 +325,95 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         // rows of the warp see [low, high] whole
         const int high = __shfl_sync(0xffffffffu, hi, 0), low = __reduce_max_sync(0xffffffffu, lo);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t S = tmem + lanes + q * KT, O = tmem + lanes + L::O + q * DH;
+        const uint32_t S0 = tmem + lanes + q * 2 * KT, O = tmem + lanes + L::O + q * DH;
         float m = M_NONE, l = 0.0f;
         bool ok = true;
         for (int j = 0; j < n && q < nq; ++j) {
-            if (!warp_wait(s_full(q), j & 1, gone)) {
+            if (!warp_wait(s_full(q, j & 1), (j >> 1) & 1, gone)) {
                 ok = false;
                 break;
             }
             fence_after();
+            const uint32_t S = S0 + (j & 1) * KT;
             const float4 *inf = info + (j & (INFO - 1)) * KBLK;
             const int c0 = (t0 + j) * KT;
             const bool whole = c0 >= low && c0 + KT - 1 <= high &&
                                __all_sync(0xffffffffu, inf[lane & (KBLK - 1)].w != 0.0f);
             uint32_t P[KT / 2];
-            float add = 0.0f;
+            float add;
             for (int pass = 0;; ++pass) {
-                uint32_t v[2][16];
-                float most = 0.0f;
-                add = 0.0f;
-                ld16(S, v[0]);
+                uint32_t v[KT];
+                ld32(S, v);
+                ld32(S + 32, v + 32);
+                float f[KBLK], c[KBLK], iv[KBLK];
 #pragma unroll
                 for (int k = 0; k < KBLK; ++k) {
-                    ld_wait(v[k & 1]);
-                    if (k + 1 < KBLK) ld16(S + (k + 1) * KV_B, v[(k + 1) & 1]);
                     const float4 f4 = inf[k];
-                    const float f = fac * f4.x, c = f4.y - m;
+                    f[k] = fac * f4.x, c[k] = f4.y - m, iv[k] = f4.z;
+                }
+                ld_wait32(v);
+                ld_wait32(v + 32);
+                float most = 0.0f;
+                add = 0.0f;
+#pragma unroll
+                for (int k = 0; k < KBLK; ++k) {
                     float p[16];
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
-                        const float2 t = fma2(make_float2(__uint_as_float(v[k & 1][i]), __uint_as_float(v[k & 1][i + 1])),
-                                              make_float2(f, f), make_float2(c, c));
+                        const float2 t = fma2(make_float2(__uint_as_float(v[16 * k + i]), __uint_as_float(v[16 * k + i + 1])),
+                                              make_float2(f[k], f[k]), make_float2(c[k], c[k]));
                         p[i] = t.x, p[i + 1] = t.y;
                     }
                     if (!whole) {
                         const int at = c0 + k * KV_B;
-                        const int upto = f4.w != 0.0f ? hi - at : -1, from = lo - at;
+                        const int upto = inf[k].w != 0.0f ? hi - at : -1, from = lo - at;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) p[i] = i <= upto && i >= from ? p[i] : -INFINITY;
                     }
-                    float2 sum = make_float2(0.0f, 0.0f);
+                    float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
                         const float2 e = make_float2(ex2(p[i]), ex2(p[i + 1]));
-                        sum = add2(sum, e);
+                        sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], e);
                         P[k * 8 + i / 2] = pack(e.x, e.y);
                     }
-                    const float all = sum.x + sum.y;
+                    const float2 both = add2(sum[0], sum[1]);
+                    const float all = both.x + both.y;
                     most = fmaxf(most, all);
-                    add = fmaf(all, f4.z, add);
+                    add = fmaf(all, iv[k], add);
                 }
                 if (pass == 1 || !__any_sync(0xffffffffu, most > M_MOST)) break;
                 // the rows' maxima, and with them new references
                 float top = -INFINITY;
+#pragma unroll 1
                 for (int k = 0; k < KBLK; ++k) {
-                    ld16(S + k * KV_B, v[0]);
-                    ld_wait(v[0]);
+                    uint32_t w[16];
+                    ld16(S + k * KV_B, w);
+                    ld_wait(w);
                     const float4 f4 = inf[k];
                     const int at = c0 + k * KV_B, upto = f4.w != 0.0f ? hi - at : -1, from = lo - at;
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (i <= upto && i >= from) top = fmaxf(top, fmaf(__uint_as_float(v[0][i]), fac * f4.x, f4.y));
+                        if (i <= upto && i >= from) top = fmaxf(top, fmaf(__uint_as_float(w[i]), fac * f4.x, f4.y));
                 }
                 const float to = top > m + 8.0f ? top - M_BELOW : m;
-                const float f = ex2(m - to);
+                const float g = ex2(m - to);
                 m = to;
-                l *= f;
+                l *= g;
                 if (j > 0) {
                     if (!warp_wait(o_done(q), (j - 1) & 1, gone)) {
                         ok = false;
                         break;
                     }
                     fence_after();
+#pragma unroll 1
                     for (int k = 0; k < DH / 16; ++k) {
-                        ld16(O + k * 16, v[0]);
-                        ld_wait(v[0]);
+                        uint32_t w[16];
+                        ld16(O + k * 16, w);
+                        ld_wait(w);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) v[0][i] = __float_as_uint(__uint_as_float(v[0][i]) * f);
-                        st16(O + k * 16, v[0]);
+                        for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * g);
+                        st16(O + k * 16, w);
                     }
                     st_wait();
                 }
@@ -373,11 +425,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
             st_wait();
             fence_before();
             __syncwarp();
-            if (lane == 0) arrive(p_full(q));
+            if (lane == 0) arrive(p_full(q, j & 1));
         }
         if (q < nq) {
             if (ok && n > 0) {
-                ok = warp_wait(o_done(q), (n - 1) & 1, gone);
+                // the last two products may both be in flight: one phase after the other
+                ok = n < 2 || warp_wait(o_done(q), n & 1, gone);
+                ok = ok && warp_wait(o_done(q), (n - 1) & 1, gone);
                 fence_after();
             }
             if (!ok) {
@@ -461,8 +515,18 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         for (int i = 0; i < NV; ++i) raw[i] = coming[i] = make_uint4(0, 0, 0, 0);
         int at = __shfl_sync(0xffffffffu, cur.at, 0);
         if (cw < tasks) load(cw, at, raw);
+        // where a lane's vector of 16 codes goes: two 16-byte chunks, the second one next
+        // to the first.  Keys, vector lane + 32 k: chunk of dims lane / 16 + 2 k, token
+        // lane % 16; values: dim lane + 32 k
+        uint32_t to[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int w = (lane >> 4) + 2 * k;
+            to[k] = (w >> 2) * (KT * 128) + (lane & 15) * 128 + (((w & 3) * 2 ^ (lane & 7)) << 4);
+        }
         for (int task = cw, i = 0; task < tasks; task += CONV, ++i) {
-            const int slot = i & 31;
+            const int slot = i & 31, j = task / (2 * KBLK), st = j & (ST - 1), blk = task & (KBLK - 1);
+            const bool vals = task & KBLK;
             const float2 sc = make_float2(__shfl_sync(0xffffffffu, cur.sc.x, slot), __shfl_sync(0xffffffffu, cur.sc.y, slot));
             if (slot == 31) {
                 cur = next;
@@ -470,38 +534,30 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
             }
             const int at_next = __shfl_sync(0xffffffffu, cur.at, (i + 1) & 31);
             if (task + CONV < tasks) load(task + CONV, at_next, coming);
-            const int j = task / (2 * KBLK), st = j % ST, blk = task % KBLK;
-            const bool vals = task & KBLK;
             if (!warp_wait(vals ? v_free(st) : k_free(st), ((j / ST) & 1) ^ 1, gone)) break;
-            if (!vals) {
-                if (lane == 0) {
-                    float4 f = value_scale(sc);
-                    f.w = at >= 0 ? 1.0f : 0.0f;
-                    info[(j & (INFO - 1)) * KBLK + blk] = f;
-                }
+            if (!vals && lane == 0) {
+                float4 f = value_scale(sc);
+                f.w = at >= 0 ? 1.0f : 0.0f;
+                info[(j & (INFO - 1)) * KBLK + blk] = f;
             }
             if (at >= 0) {
-                const uint32_t base = sm + (vals ? L::v : L::k) + st * L::TILE;
+                const uint32_t base = sm + (vals ? L::v + lane * 128 + ((blk * 2 ^ (lane & 7)) << 4) : L::k + blk * 2048) +
+                                      st * L::TILE;
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
-                    const int e = lane + 32 * k;
-                    if (e >= a.d) break;
+                    if (lane + 32 * k >= a.d) break;
                     const uint4 c = raw[k];
                     uint32_t f[8];
                     f[0] = codes_f16(c.x, 0x4140), f[1] = codes_f16(c.x, 0x4342);
                     f[2] = codes_f16(c.y, 0x4140), f[3] = codes_f16(c.y, 0x4342);
                     f[4] = codes_f16(c.z, 0x4140), f[5] = codes_f16(c.z, 0x4342);
                     f[6] = codes_f16(c.w, 0x4140), f[7] = codes_f16(c.w, 0x4342);
-                    if (!vals) {  // e: chunk e / 16 of dims, token e % 16
-                        const int row = blk * KV_B + (e & 15), w = e >> 4, ch = (w & 3) * 2;
-                        const uint32_t p = base + (w >> 2) * (KT * 128) + row * 128;
-                        st_shared(p + ((ch ^ (row & 7)) << 4), f[0], f[1], f[2], f[3]);
-                        st_shared(p + (((ch + 1) ^ (row & 7)) << 4), f[4], f[5], f[6], f[7]);
-                    } else {  // e: dim; even words tokens 0..7, odd 8..15
-                        const int ch = (blk & 3) * 2;
-                        const uint32_t p = base + (blk >> 2) * (DH * 128) + e * 128;
-                        st_shared(p + ((ch ^ (e & 7)) << 4), f[0], f[2], f[4], f[6]);
-                        st_shared(p + (((ch + 1) ^ (e & 7)) << 4), f[1], f[3], f[5], f[7]);
+                    if (!vals) {
+                        st_shared(base + to[k], f[0], f[1], f[2], f[3]);
+                        st_shared((base + to[k]) ^ 16, f[4], f[5], f[6], f[7]);
+                    } else {  // even words tokens 0..7, odd 8..15
+                        st_shared(base + k * 4096, f[0], f[2], f[4], f[6]);
+                        st_shared((base + k * 4096) ^ 16, f[1], f[3], f[5], f[7]);
                     }
                 }
             }
@@ -512,46 +568,52 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
 #pragma unroll
             for (int k = 0; k < NV; ++k) raw[k] = coming[k];
         }
-    } else if (lane == 0 && n > 0) {  // ------------------------------------ MMA issuer
-        bool ok = wait(q_full, 0, gone), issued = false;
-        const auto qk = [&](int q, int st) {
+    } else if (n > 0) {  // ------------------------------------------------ MMA issuer
+        const uint32_t one = elect_one();
+        bool ok = warp_wait(q_full, 0, gone), issued = false;
+        const uint64_t q_op = operand(sm + L::q), k_op = operand(sm + L::k), v_op = operand(sm + L::v);
+        const auto qk = [&](int q, int j) {
+            const uint32_t d = tmem + (2 * q + (j & 1)) * KT;
+            const uint64_t qa = q_op + (uint32_t)q * (L::QTILE >> 4), ka = k_op + (uint32_t)(j & (ST - 1)) * (L::TILE >> 4);
+            mma_ss<false>(d, qa, ka, idesc(KT), one);
 #pragma unroll
-            for (int k = 0; k < DH / 16; ++k)
-                mma_ss(tmem + q * KT, operand(sm + L::q + q * L::TILE + (k >> 2) * (QT * 128)) + 2 * (k & 3),
-                       operand(sm + L::k + st * L::TILE + (k >> 2) * (KT * 128)) + 2 * (k & 3), idesc(KT), k > 0);
+            for (int k = 1; k < DH / 16; ++k)
+                mma_ss<true>(d, qa + ((k >> 2) * (QT * 128 >> 4) + 2 * (k & 3)), ka + ((k >> 2) * (KT * 128 >> 4) + 2 * (k & 3)),
+                             idesc(KT), one);
             issued = true;
-            commit(s_full(q));
+            commit(s_full(q, j & 1), one);
         };
-        if (ok) ok = wait(k_full(0), 0, gone);
-        if (ok) {
+        // the logits of two key tiles ahead
+        for (int j = 0; j < 2 && j < n && ok; ++j) {
+            if (!(ok = warp_wait(k_full(j), 0, gone))) break;
             fence_after();
-            for (int q = 0; q < nq; ++q) qk(q, 0);
-            commit(k_free(0));
+            for (int q = 0; q < nq; ++q) qk(q, j);
+            commit(k_free(j), one);
         }
         for (int j = 0; j < n && ok; ++j) {
-            const int st = j % ST, kst = (j + 1) % ST;
+            const int st = j & (ST - 1);
             for (int q = 0; q < nq; ++q) {
-                if (!(ok = wait(p_full(q), j & 1, gone))) break;
-                if (q == 0 && !(ok = wait(v_full(st), (j / ST) & 1, gone))) break;
+                if (!(ok = warp_wait(p_full(q, j & 1), (j >> 1) & 1, gone))) break;
+                if (q == 0 && !(ok = warp_wait(v_full(st), (j / ST) & 1, gone))) break;
                 fence_after();
+                const uint32_t p = tmem + (2 * q + (j & 1)) * KT, o = tmem + L::O + q * DH;
+                const uint64_t va = v_op + (uint32_t)st * (L::TILE >> 4);
 #pragma unroll
-                for (int k = 0; k < KT / 16; ++k)
-                    mma_ts(tmem + L::O + q * DH, tmem + q * KT + 8 * k,
-                           operand(sm + L::v + st * L::TILE + (k >> 2) * (DH * 128)) + 2 * (k & 3), idesc(DH), j > 0 || k > 0);
-                if (q == nq - 1) commit(v_free(st));
-                commit(o_done(q));  // last, so that nothing arrives after the tile's rows are out
-                if (j + 1 < n) {
+                for (int k = 0; k < KT / 16; ++k) mma_ts(o, p + 8 * k, va + 2 * k, idesc(DH), k > 0 || j > 0, one);
+                if (q == nq - 1) commit(v_free(st), one);
+                commit(o_done(q), one);  // last, so that nothing arrives after the tile's rows are out
+                if (j + 2 < n) {  // over the buffer that P V read, in order behind it
                     if (q == 0) {
-                        if (!(ok = wait(k_full(kst), ((j + 1) / ST) & 1, gone))) break;
+                        if (!(ok = warp_wait(k_full((j + 2) & (ST - 1)), ((j + 2) / ST) & 1, gone))) break;
                         fence_after();
                     }
-                    qk(q, kst);
-                    if (q == nq - 1) commit(k_free(kst));
+                    qk(q, j + 2);
+                    if (q == nq - 1) commit(k_free((j + 2) & (ST - 1)), one);
                 }
             }
         }
         if (!ok && issued) {  // what was issued ends before the memory is given up
-            commit(drain);
+            commit(drain, one);
             bar_wait(drain, 0);
         }
     }
@@ -632,8 +694,8 @@ KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens,
     p.max_tiles = (int)cdiv((int64_t)max_tokens * group, QT);
     p.units = (int64_t)nb * heads * ((p.max_tiles + 1) / 2);
     p.splits = 1;
-    // one CTA an SM: split the keys while CTAs are missing, 4 tiles a split at least
-    const int64_t room = KV_SMS / p.units, worth = span / (4 * KT);
+    // one CTA an SM: split the keys while CTAs are missing, 512 keys a split at least
+    const int64_t room = KV_SMS / p.units, worth = span / 512;
     p.splits = (int)(room < 1 || worth < 1 ? 1 : (room < worth ? room : worth));
     p.part = p.splits > 1 ? (size_t)p.units * p.splits * prompt_part(d) * 4 : 0;
     return p;
