@@ -9,13 +9,14 @@
 // is added to them as log2 s_v (o = sum p c_v, l = sum p / s_v; the formulas of
 // k_kv_rows.cu, the running reference m included).
 //
-//   warps 0-3, 4-7  softmax of tile 0 / 1, one thread a row: 64 logits from
-//                   TMEM, p = 2^(s f + c) to f16, P back to TMEM over the columns
-//                   S held (the A operand of the next product)
-//   warps 8-14      converters: a block of keys (or values) at a time from
+//   warps 0-15      softmax: 8 warps a tile, two threads a row with 32 logits of a
+//                   key tile each (one thread a row left the schedulers idle half the
+//                   time: 377 us where this takes XXX): p = 2^(s f + c) to f16, P back to
+//                   TMEM over the columns S held (the A operand of the next product)
+//   warps 16-22     converters: a block of keys (or values) at a time from
 //                   global memory, one block ahead in registers, to f16 in the
 //                   128-byte-swizzled operand layout
-//   warp 15         MMA issuer
+//   warp 23         MMA issuer
 //
 // TMEM: two S/P buffers of 64 columns a tile, O0, O1 (DH columns each).  The
 // logits of a key tile are there before the softmax of the one before is done, so a
@@ -36,7 +37,8 @@ namespace skm {
 namespace {
 
 constexpr int QT = 128, KT = 64, KBLK = KT / KV_B;  // rows of a tile, keys of a tile, blocks of it
-constexpr int CONV = 7, CONV_WARP0 = 8, MMA_WARP = 15, THREADS = 512;
+constexpr int CONV = 7, CONV_WARP0 = 16, MMA_WARP = 23, THREADS = 768;
+constexpr int HB = KBLK / 2, HK = KT / 2;  // blocks, keys of a half row
 constexpr int INFO = 8;  // tiles whose scales are kept: those of the K ring and those its softmax still reads
 
 constexpr int ST = 4;  // K and V tiles in flight
@@ -44,7 +46,8 @@ template <int DH>
 struct Lay {
     static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
     static constexpr int q = 0, k = 2 * QTILE, v = k + ST * TILE, info = v + ST * TILE;
-    static constexpr int bars = info + INFO * KBLK * 16, slots = bars + 8 * (4 * ST + 12);
+    static constexpr int swap = info + INFO * KBLK * 16;  // a float of either half of each row
+    static constexpr int bars = swap + 2 * 2 * QT * 4, slots = bars + 8 * (4 * ST + 14);
     // one CTA an SM: it takes all of TMEM
     static constexpr int bytes = slots + 16 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
     static constexpr uint32_t O = 4 * KT;  // TMEM column of O0
@@ -73,6 +76,17 @@ __device__ __forceinline__ bool wait(uint32_t b, uint32_t parity, volatile int32
 // by a whole warp, with one answer
 __device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, volatile int32_t *gone) {
     return __all_sync(0xffffffffu, wait(b, parity, gone));
+}
+// whether any thread of two warps says so; a barrier of the two
+__device__ __forceinline__ int pair_or(int bar, int say) {
+    int r;
+    asm volatile(
+        "{\n\t.reg .pred p, r;\n\tsetp.ne.b32 p, %2, 0;\n\t"
+        "barrier.cta.red.or.pred r, %1, 64, p;\n\tselp.b32 %0, 1, 0, r;\n\t}\n"
+        : "=r"(r)
+        : "r"(bar), "r"(say)
+        : "memory");
+    return r;
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -193,10 +207,10 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
 // A part: 256 x (m, l), then 256 rows of d sums
 __host__ __device__ __forceinline__ int64_t prompt_part(int d) { return 2 * QT * (int64_t)(2 + d); }
 
-// A query row to f16 in its tile's operand; returns what its logits are
+// Half of a query row to f16 in its tile's operand; returns what its logits are
 // multiplied by (k_kv_rows.cu: bf16 rows are scaled by a power of two)
 template <int DH>
-__device__ __forceinline__ float load_row(const KvAttnArgs &a, const uint16_t *x, bool in, uint32_t tile, int row) {
+__device__ __forceinline__ float load_row(const KvAttnArgs &a, const uint16_t *x, bool in, uint32_t tile, int row, int half) {
     float top = 0.0f, mul = 1.0f, back = 1.0f;
     const auto get = [&](int i, uint32_t (&w)[4]) {  // dims 8 i .. 8 i + 7
 #pragma unroll
@@ -228,7 +242,7 @@ __device__ __forceinline__ float load_row(const KvAttnArgs &a, const uint16_t *x
         }
     }
 #pragma unroll 4
-    for (int i = 0; i < DH / 8; ++i) {
+    for (int i = half * (DH / 16); i < (half + 1) * (DH / 16); ++i) {
         uint32_t w[4];
         get(i, w);
         if (bf) {
@@ -256,7 +270,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
     const auto s_full = [&](int q, int buf) { return bar(4 * ST + 2 * q + buf); };
     const auto p_full = [&](int q, int buf) { return bar(4 * ST + 4 + 2 * q + buf); };
     const auto o_done = [&](int q) { return bar(4 * ST + 8 + q); };
-    const uint32_t q_full = bar(4 * ST + 10), drain = bar(4 * ST + 11);
+    const auto o_last = [&](int q) { return bar(4 * ST + 10 + q); };
+    const uint32_t q_full = bar(4 * ST + 12), drain = bar(4 * ST + 13);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::slots);
     volatile int32_t *gone = reinterpret_cast<volatile int32_t *>(smem + L::slots + 4);
     float4 *info = reinterpret_cast<float4 *>(smem + L::info);  // (k scale, log2 v scale, 1 / v scale, there)
@@ -290,11 +305,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         for (int q = 0; q < 2; ++q) {
             for (int i = 0; i < 2; ++i) {
                 asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s_full(q, i)), "r"(1) : "memory");
-                asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(p_full(q, i)), "r"(4) : "memory");
+                asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(p_full(q, i)), "r"(8) : "memory");
             }
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(o_done(q)), "r"(1) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(o_last(q)), "r"(1) : "memory");
         }
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(q_full), "r"(8) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(q_full), "r"(16) : "memory");
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(drain), "r"(1) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *gone = 0;
@@ -313,11 +329,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
     const uint32_t tmem = *tmem_slot;
 
     if (warp < CONV_WARP0) {  // ------------------------------------------ softmax
-        const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row;
+        const int q = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row;
         const bool in = r < rows;
         const uint16_t *x = static_cast<const uint16_t *>(a.Q);
         if (in) x += (int64_t)(s.row0 + a.by_group.div(r)) * a.q_token + (int64_t)(h * a.group + a.by_group.mod(r)) * a.q_head;
-        const float fac = load_row<DH>(a, x, in, sm + L::q + q * L::QTILE, row);
+        const float fac = load_row<DH>(a, x, in, sm + L::q + q * L::QTILE, row, half);
         fence_async();
         __syncwarp();
         if (lane == 0) arrive(q_full);
@@ -325,38 +341,36 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         // rows of the warp see [low, high] whole
         const int high = __shfl_sync(0xffffffffu, hi, 0), low = __reduce_max_sync(0xffffffffu, lo);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t S0 = tmem + lanes + q * 2 * KT, O = tmem + lanes + L::O + q * DH;
+        const uint32_t S0 = tmem + lanes + q * 2 * KT + half * HK, O = tmem + lanes + L::O + q * DH;
+        // the two warps of 32 rows: a barrier, a word of each row
+        const int pair_bar = 1 + q * 4 + (warp & 3);
+        float *mine = reinterpret_cast<float *>(smem + L::swap) + (half * 2 + q) * QT + row;
+        const float *other = reinterpret_cast<const float *>(smem + L::swap) + ((half ^ 1) * 2 + q) * QT + row;
         float m = M_NONE, l = 0.0f;
         bool ok = true;
         for (int j = 0; j < n && q < nq; ++j) {
-            if (!warp_wait(s_full(q, j & 1), (j >> 1) & 1, gone)) {
-                ok = false;
-                break;
-            }
+            ok = warp_wait(s_full(q, j & 1), (j >> 1) & 1, gone);
             fence_after();
             const uint32_t S = S0 + (j & 1) * KT;
-            const float4 *inf = info + (j & (INFO - 1)) * KBLK;
-            const int c0 = (t0 + j) * KT;
-            const bool whole = c0 >= low && c0 + KT - 1 <= high &&
-                               __all_sync(0xffffffffu, inf[lane & (KBLK - 1)].w != 0.0f);
-            uint32_t P[KT / 2];
+            const float4 *inf = info + (j & (INFO - 1)) * KBLK + half * HB;
+            const int c0 = (t0 + j) * KT + half * HK;
+            const bool whole = c0 >= low && c0 + HK - 1 <= high && inf[0].w * inf[1].w != 0.0f;
+            uint32_t P[HK / 2];
             float add;
             for (int pass = 0;; ++pass) {
-                uint32_t v[KT];
+                uint32_t v[HK];
                 ld32(S, v);
-                ld32(S + 32, v + 32);
-                float f[KBLK], c[KBLK], iv[KBLK];
+                float f[HB], c[HB], iv[HB];
 #pragma unroll
-                for (int k = 0; k < KBLK; ++k) {
+                for (int k = 0; k < HB; ++k) {
                     const float4 f4 = inf[k];
                     f[k] = fac * f4.x, c[k] = f4.y - m, iv[k] = f4.z;
                 }
                 ld_wait32(v);
-                ld_wait32(v + 32);
                 float most = 0.0f;
                 add = 0.0f;
 #pragma unroll
-                for (int k = 0; k < KBLK; ++k) {
+                for (int k = 0; k < HB; ++k) {
                     float p[16];
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
@@ -382,11 +396,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                     most = fmaxf(most, all);
                     add = fmaf(all, iv[k], add);
                 }
-                if (pass == 1 || !__any_sync(0xffffffffu, most > M_MOST)) break;
+                // either warp's wish is both's; a wait that gave up ends both
+                const int word = pair_or(pair_bar, most > M_MOST || !ok);
+                if (pass == 1 || !word) break;
                 // the rows' maxima, and with them new references
                 float top = -INFINITY;
 #pragma unroll 1
-                for (int k = 0; k < KBLK; ++k) {
+                for (int k = 0; k < HB; ++k) {
                     uint32_t w[16];
                     ld16(S + k * KV_B, w);
                     ld_wait(w);
@@ -396,32 +412,35 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                     for (int i = 0; i < 16; ++i)
                         if (i <= upto && i >= from) top = fmaxf(top, fmaf(__uint_as_float(w[i]), fac * f4.x, f4.y));
                 }
+                ok = ok && (j == 0 || warp_wait(o_done(q), (j - 1) & 1, gone));
+                *mine = ok ? top : NAN;
+                pair_or(pair_bar, 0);
+                const float theirs = *other;
+                pair_or(pair_bar, 0);
+                ok = ok && __any_sync(0xffffffffu, theirs == theirs);
+                if (!ok) break;
+                top = fmaxf(top, theirs);
                 const float to = top > m + 8.0f ? top - M_BELOW : m;
                 const float g = ex2(m - to);
                 m = to;
                 l *= g;
-                if (j > 0) {
-                    if (!warp_wait(o_done(q), (j - 1) & 1, gone)) {
-                        ok = false;
-                        break;
-                    }
+                if (j > 0) {  // each warp half of O
                     fence_after();
 #pragma unroll 1
-                    for (int k = 0; k < DH / 16; ++k) {
+                    for (int k = 0; k < DH / 32; ++k) {
                         uint32_t w[16];
-                        ld16(O + k * 16, w);
+                        ld16(O + half * (DH / 2) + k * 16, w);
                         ld_wait(w);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * g);
-                        st16(O + k * 16, w);
+                        st16(O + half * (DH / 2) + k * 16, w);
                     }
                     st_wait();
                 }
             }
             if (!ok) break;
             l += add;
-#pragma unroll
-            for (int k = 0; k < KT / 2; k += 16) st16(S + k, P + k);
+            st16(S, P);
             st_wait();
             fence_before();
             __syncwarp();
@@ -429,21 +448,23 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         }
         if (q < nq) {
             if (ok && n > 0) {
-                // the last two products may both be in flight: one phase after the other
-                ok = n < 2 || warp_wait(o_done(q), n & 1, gone);
-                ok = ok && warp_wait(o_done(q), (n - 1) & 1, gone);
+                ok = warp_wait(o_last(q), 0, gone);
                 fence_after();
             }
             if (!ok) {
                 l = NAN;
                 if (lane == 0 && a.status) *a.status = 1;
             }
+            *mine = l;
+            pair_or(pair_bar, 0);
+            l += *other;
             float *part = parts ? parts + (int64_t)blockIdx.x * prompt_part(a.d) : nullptr;
             const int pr = q * QT + row;
-            if (part) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);
+            if (part && half == 0) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);
             const int64_t at = in ? row_index(a, s, h, r) : 0;
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            for (int k = 0; k < DH / 16; ++k) {
+#pragma unroll 1
+            for (int k = half * (DH / 32); k < (half + 1) * (DH / 32); ++k) {
                 if (16 * k >= a.d) break;
                 uint32_t v[16];
                 if (ok && n > 0) {
@@ -477,7 +498,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                 dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
                 dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
             }
-            if (in && !part && a.lse) a.lse[at] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
+            if (in && !part && half == 0 && a.lse) a.lse[at] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
         }
     } else if (warp < MMA_WARP) {  // ------------------------------------- converters
         // tasks: per tile 8 blocks of keys, then 8 of values; warp w takes w, w + 7, ...
@@ -599,9 +620,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                 const uint32_t p = tmem + (2 * q + (j & 1)) * KT, o = tmem + L::O + q * DH;
                 const uint64_t va = v_op + (uint32_t)st * (L::TILE >> 4);
 #pragma unroll
-                for (int k = 0; k < KT / 16; ++k) mma_ts(o, p + 8 * k, va + 2 * k, idesc(DH), k > 0 || j > 0, one);
+                for (int k = 0; k < KT / 16; ++k) mma_ts(o, p + (k >> 1) * HK + 8 * (k & 1), va + 2 * k, idesc(DH), k > 0 || j > 0, one);
                 if (q == nq - 1) commit(v_free(st), one);
-                commit(o_done(q), one);  // last, so that nothing arrives after the tile's rows are out
+                commit(o_done(q), one);
+                // a barrier of its own for the last product: the softmax may be up to two
+                // phases of o_done away from it, more than a parity tells apart.  Committed
+                // last, so that nothing arrives after the tile's rows are out
+                if (j == n - 1) commit(o_last(q), one);
                 if (j + 2 < n) {  // over the buffer that P V read, in order behind it
                     if (q == 0) {
                         if (!(ok = warp_wait(k_full((j + 2) & (ST - 1)), ((j + 2) / ST) & 1, gone))) break;
