@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -762,49 +763,58 @@ class KVCache:
         self.heads, self.d, self.page, self.pages = int(heads), int(d), int(page), n
         self.index = k.get_device()
         self.ref = KVCacheRef(self.heads, self.d, self.page, n, k.data_ptr(), v.data_ptr(), scales.data_ptr())
+        self.addr = ctypes.addressof(self.ref)
 
     @property
     def device(self):
         return self.k.device
 
 
+# The structs of a call as packed bytes: the same layouts as KVSeqs and KVAttn
+# at half the cost of building a ctypes.Structure (a call's host time is a few
+# microseconds, and a short decode step's kernel takes not much more).
+_KV_SEQS = struct.Struct("@iiPPPiiixxxx")
+_KV_ATTN = struct.Struct("@iiiifiPqqPPP")
+assert _KV_SEQS.size == ctypes.sizeof(KVSeqs) and _KV_ATTN.size == ctypes.sizeof(KVAttn)
+
+
 def _kv_ints(name, t, n, index):
-    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != index:
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != index:
         raise ValueError(f"{name} must be a contiguous int32 tensor [{n}] on the cache's device")
     return t.data_ptr()
 
 
 def _kv_seqs(cache, table, pos, cu, tokens, max_tokens, max_len=0):
     index = cache.index
+    if index < 0:
+        raise ValueError("the cache is not on a GPU")
     if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_contiguous() or table.get_device() != index:
         raise ValueError("table must be a contiguous int32 tensor [batch, cols] on the cache's device")
     batch, cols = table.shape
-    return KVSeqs(batch, cols, table.data_ptr(), _kv_ints("positions", pos, batch, index),
-                  _kv_ints("cu", cu, batch + 1, index), tokens, max_tokens, max_len)
+    return _KV_SEQS.pack(batch, cols, table.data_ptr(), _kv_ints("positions", pos, batch, index),
+                         _kv_ints("cu", cu, batch + 1, index), tokens, max_tokens, max_len)
 
 
 def _kv_rows(name, t, heads, cache):
-    """The C type of rows [tokens, heads, d]."""
-    shape = t.shape
+    """The C type of rows [tokens, heads, d] and their strides."""
+    shape, strides = t.shape, t.stride()
     if len(shape) != 3 or shape[1] != heads or shape[2] != cache.d or t.get_device() != cache.index:
         raise ValueError(f"{name} must be [tokens, {heads}, {cache.d}] on the cache's device")
     dtype = _KV_DTYPES.get(t.dtype)
     if dtype is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16")
-    if t.stride(2) != 1:
+    if strides[2] != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return dtype
+    return dtype, strides[0], strides[1]
 
 
 def _kv_stream(cache, stream):
     """The raw stream: the current one of the cache's device unless given (the
     lookup without a Stream object, whose construction costs 3 us)."""
-    if cache.index < 0:
-        raise ValueError("the cache is not on a GPU")
     return torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream
 
 
-def _kv_empty(cache, stream, *shape, dtype):
+def _kv_empty(cache, stream, shape, dtype):
     """What a call allocates belongs to the stream that it runs on."""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=cache.k.device)
@@ -816,12 +826,14 @@ def skm_kv_write(cache: KVCache, table, start, cu, K, V, max_tokens, stream=None
     """Quantises rows cu[b]:cu[b + 1] of K and V ([tokens, heads, d], any strides
     with d contiguous) into the cache at positions start[b], start[b] + 1, ... of
     sequence b; table int32 [batch, cols], start [batch], cu [batch + 1]."""
-    dtype = _kv_rows("K", K, cache.heads, cache)
-    if _kv_rows("V", V, cache.heads, cache) != dtype or V.shape[0] != K.shape[0]:
+    dtype, k_token, k_head = _kv_rows("K", K, cache.heads, cache)
+    v_dtype, v_token, v_head = _kv_rows("V", V, cache.heads, cache)
+    tokens = K.shape[0]
+    if v_dtype != dtype or V.shape[0] != tokens:
         raise ValueError("K and V must have one type and length")
-    s = _kv_seqs(cache, table, start, cu, K.shape[0], max_tokens)
-    rc = lib().skm_kv_write(ctypes.byref(cache.ref), ctypes.byref(s), dtype, K.data_ptr(), K.stride(0), K.stride(1),
-                            V.data_ptr(), V.stride(0), V.stride(1), _kv_stream(cache, stream))
+    s = _kv_seqs(cache, table, start, cu, tokens, max_tokens)
+    rc = lib().skm_kv_write(cache.addr, s, dtype, K.data_ptr(), k_token, k_head, V.data_ptr(), v_token, v_head,
+                            _kv_stream(cache, stream))
     if rc:
         _check(rc)
 
@@ -834,24 +846,24 @@ def skm_kv_read(cache: KVCache, table, start, cu, tokens, max_tokens, dtype=DTYP
         t = _KV_TORCH.get(dtype)
         if t is None:
             raise ValueError(f"unknown dtype {dtype}")
-        out = (_kv_empty(cache, stream, tokens, cache.heads, cache.d, dtype=t),
-               _kv_empty(cache, stream, tokens, cache.heads, cache.d, dtype=t))
+        shape = (tokens, cache.heads, cache.d)
+        out = _kv_empty(cache, stream, shape, t), _kv_empty(cache, stream, shape, t)
     else:
         for t in out:
-            if t is not None and (_kv_rows("out", t, cache.heads, cache) != dtype or t.shape[0] != tokens
+            if t is not None and (_kv_rows("out", t, cache.heads, cache)[0] != dtype or t.shape[0] != tokens
                                   or not t.is_contiguous()):
                 raise ValueError("out: contiguous tensors of `tokens` rows and the given dtype")
     K, V = out
     s = _kv_seqs(cache, table, start, cu, tokens, max_tokens)
-    rc = lib().skm_kv_read(ctypes.byref(cache.ref), ctypes.byref(s), dtype, None if K is None else K.data_ptr(),
-                           None if V is None else V.data_ptr(), _kv_stream(cache, stream))
+    rc = lib().skm_kv_read(cache.addr, s, dtype, None if K is None else K.data_ptr(), None if V is None else V.data_ptr(),
+                           _kv_stream(cache, stream))
     if rc:
         _check(rc)
     return out
 
 
 def _kv_ws_bytes(cache, s, a):
-    n = lib().skm_kv_attend_workspace_size(ctypes.byref(cache.ref), ctypes.byref(s), ctypes.byref(a))
+    n = lib().skm_kv_attend_workspace_size(cache.addr, s, a)
     if n == ctypes.c_size_t(-1).value:
         raise SkmError(1, lib().skm_last_error().decode())
     return n
@@ -862,8 +874,8 @@ def kv_workspace(cache: KVCache, batch, heads_q, tokens, max_tokens, max_len, dt
     """A workspace for skm_kv_attend calls of these sizes."""
     cols = -(-max_len // cache.page) if cols is None else cols
     dummy = cache.k.data_ptr()
-    s = KVSeqs(batch, max(cols, 1), dummy, dummy, dummy, tokens, max_tokens, max_len)
-    a = KVAttn(heads_q, dtype, bool(causal), window, 1.0, 0, None, 0, 0, None, None, None)
+    s = _KV_SEQS.pack(batch, max(cols, 1), dummy, dummy, dummy, tokens, max_tokens, max_len)
+    a = _KV_ATTN.pack(heads_q, dtype, bool(causal), window, 1.0, 0, 0, 0, 0, 0, 0, 0)
     return _ws(_kv_ws_bytes(cache, s, a), cache.device)
 
 
@@ -872,26 +884,28 @@ def skm_kv_attend(cache: KVCache, table, length, cu, Q, max_tokens, max_len, sca
     """(out, lse or None): attention of the query rows Q [tokens, heads_q, d]
     over the cache.  length[b]: the tokens the cache holds of sequence b, its
     own query tokens included; scale: 1 / sqrt(d) unless given."""
-    tokens, heads_q = Q.shape[0], Q.shape[1]
-    dtype = _kv_rows("Q", Q, heads_q, cache)
+    shape = Q.shape
+    tokens, heads_q = shape[0], shape[1]
+    dtype, q_token, q_head = _kv_rows("Q", Q, heads_q, cache)
     s = _kv_seqs(cache, table, length, cu, tokens, max_tokens, max_len)
     if out is None:
-        out = _kv_empty(cache, stream, tokens, heads_q, cache.d, dtype=Q.dtype)
-    elif out.shape != Q.shape or out.dtype != Q.dtype or not out.is_contiguous() or out.get_device() != cache.index:
+        out = _kv_empty(cache, stream, shape, Q.dtype)
+    elif out.shape != shape or out.dtype != Q.dtype or not out.is_contiguous() or out.get_device() != cache.index:
         raise ValueError("out: contiguous, of Q's shape, type and device")
+    lse = _kv_empty(cache, stream, (tokens, heads_q), torch.float32) if want_lse else None
     if status is not None and (status.dtype is not torch.int32 or status.get_device() != cache.index or not status.numel()):
         raise ValueError("status must be an int32 tensor on the cache's device")
-    lse = _kv_empty(cache, stream, tokens, heads_q, dtype=torch.float32) if want_lse else None
-    a = KVAttn(heads_q, dtype, bool(causal), window, cache.d ** -0.5 if scale is None else scale, 0, Q.data_ptr(),
-               Q.stride(0), Q.stride(1), out.data_ptr(), None if lse is None else lse.data_ptr(),
-               None if status is None else status.data_ptr())
+    a = _KV_ATTN.pack(heads_q, dtype, bool(causal), window, cache.d ** -0.5 if scale is None else scale, 0, Q.data_ptr(),
+                      q_token, q_head, out.data_ptr(), 0 if lse is None else lse.data_ptr(),
+                      0 if status is None else status.data_ptr())
     if ws is None:
         n = _kv_ws_bytes(cache, s, a)
-        ws = _kv_empty(cache, stream, n, dtype=torch.uint8) if n else None
+        if n:
+            ws = _kv_empty(cache, stream, (n,), torch.uint8)
     elif ws.get_device() != cache.index or not ws.is_contiguous():
         raise ValueError("ws must be contiguous, on the cache's device")
-    rc = lib().skm_kv_attend(ctypes.byref(cache.ref), ctypes.byref(s), ctypes.byref(a), None if ws is None else ws.data_ptr(),
-                             0 if ws is None else ws.nbytes, _kv_stream(cache, stream))
+    rc = lib().skm_kv_attend(cache.addr, s, a, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
+                             _kv_stream(cache, stream))
     if rc:
         _check(rc)
     return out, lse
