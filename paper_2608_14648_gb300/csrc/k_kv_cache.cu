@@ -1,22 +1,29 @@
 // Writing keys and values into the 8-bit cache and reading them back.
 //
 // One warp takes one block (16 tokens) of one head's keys or values: it holds
-// the block's new values in registers, so the largest magnitude, the scale and
-// the codes come from one read of the input.  Both kernels move bytes and
-// nothing else bounds them; a warp needs no other warp, so an append (one
-// token, a warp busy for its memory latencies) and a prompt (thousands of
-// independent 4 KB reads in flight) are the same code.
+// the block's new values in registers as they came, so the largest magnitude,
+// the scale and the codes come from one read of the input.  Both kernels move
+// bytes; a warp needs no other warp, so an append (one token, a warp busy for its
+// memory latencies) and a prompt (thousands of independent 4 KB reads in flight) are
+// the same code.  What bounds writing is how many of those reads are in flight:
+// the input is read before the page is known, and 16-bit values stay packed
+// (64 registers, 32 warps an SM).
 //
 // Lanes: keys, a unit is 16 dims of a token (a 16-byte code store, two 16-byte
 // loads of 16-bit values), consecutive lanes along d; values, whose blocks
 // keep the 16 tokens of a dim together, a unit is 8 dims of the four tokens
 // that share a 32-bit word, so the transposition stays in registers.
 //
+// The largest magnitude is an integer maximum of the values' bits without
+// their sign, in which infinities and NaN come out on top: a warp that finds one
+// goes element by element.
+//
 // Rounding: code = rint(x / scale) with the quotient rounded to fp32.  x times
 // the reciprocal is within 1.6e-5 of x / scale (|quotient| < 128, two roundings
 // of 2^-24 relative), the fp32 quotient within 8e-6, so both round to the same
 // integer unless x times the reciprocal lies within 1e-4 of a half; only those
-// elements (and infinities and NaN) take the division.
+// elements take the division.
+#include <algorithm>
 #include <type_traits>
 
 #include "skm_kv.cuh"
@@ -29,31 +36,48 @@ constexpr int WARPS = 8;
 constexpr float CODE_MAGIC = 12583040.0f;  // 1.5 2^23 + 128: q + this holds rint(q) + 128 in its low byte
 constexpr float NEAR_HALF = 0.4999f;
 
-// 8 consecutive values
 template <typename T>
-__device__ __forceinline__ void load8(const T *p, int wide, float *v) {
-    if (!wide) {
+constexpr int WORDS8 = 8 * sizeof(T) / 4;  // words of 8 values
+template <typename T>
+constexpr uint32_t INF_BITS = std::is_same<T, float>::value ? 0x7f800000u : std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+
+// 8 consecutive values as they are
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int wide, uint32_t *w) {
+    if (wide) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)p[i];
-        return;
-    }
-    if constexpr (std::is_same<T, float>::value) {
-        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-        const uint4 a = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (std::is_same<T, __half>::value) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-                v[2 * i] = f.x, v[2 * i + 1] = f.y;
-            } else {
-                v[2 * i] = __uint_as_float(w[i] << 16);
-                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            }
+        for (int i = 0; i < WORDS8<T>; i += 4) {
+            const uint4 a = reinterpret_cast<const uint4 *>(p)[i / 4];
+            w[i] = a.x, w[i + 1] = a.y, w[i + 2] = a.z, w[i + 3] = a.w;
         }
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+    } else {
+        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
     }
+}
+// value i of words
+template <typename T>
+__device__ __forceinline__ float value(const uint32_t *w, int i) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    const uint32_t x = w[i >> 1];
+    if constexpr (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((uint16_t)(i & 1 ? x >> 16 : x)));
+    return __uint_as_float(i & 1 ? x & 0xffff0000u : x << 16);
+}
+// the larger magnitudes' bits, a 16-bit pair at a time
+template <typename T>
+__device__ __forceinline__ uint32_t larger(uint32_t m, uint32_t w) {
+    if constexpr (sizeof(T) == 4) return max(m, w & 0x7fffffffu);
+    return __vmaxu2(m, w & 0x7fff7fffu);
+}
+template <typename T>
+__device__ __forceinline__ float magnitude(uint32_t bits) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(bits);
+    if constexpr (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((uint16_t)bits));
+    return __uint_as_float(bits << 16);
 }
 
 template <typename T>
@@ -77,32 +101,25 @@ __device__ __forceinline__ void store8(T *p, const float *v) {
     }
 }
 
-__device__ __forceinline__ float warp_max(float m) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    return m;
-}
-
 __device__ __noinline__ uint32_t code_exact(float x, float s) {
     float q = __fdiv_rn(x, s);
     q = q == q ? fminf(fmaxf(rintf(q), -127.0f), 127.0f) : 0.0f;
     return (uint32_t)(int)(q + 128.0f);
 }
 
-// codes of four values in a word, the first in the low byte; quick: the
-// reciprocal of s is a normal number
+// codes of four values in a word, the first in the low byte; quick: they are
+// finite and the reciprocal of s is a normal number
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float s, float inv, bool quick) {
     const float fa = fmaf(a, inv, CODE_MAGIC), fb = fmaf(b, inv, CODE_MAGIC);
     const float fc = fmaf(c, inv, CODE_MAGIC), fd = fmaf(d, inv, CODE_MAGIC);
     const float ra = fmaf(a, inv, CODE_MAGIC - fa), rb = fmaf(b, inv, CODE_MAGIC - fb);
     const float rc = fmaf(c, inv, CODE_MAGIC - fc), rd = fmaf(d, inv, CODE_MAGIC - fd);
-    const float far = fmaxf(fmaxf(fabsf(ra), fabsf(rb)), fmaxf(fabsf(rc), fabsf(rd)));
-    const bool fine = quick && far <= NEAR_HALF && ra == ra && rb == rb && rc == rc && rd == rd;
-    if (fine) {
+    if (quick && fmaxf(fmaxf(fabsf(ra), fabsf(rb)), fmaxf(fabsf(rc), fabsf(rd))) <= NEAR_HALF) {
         const uint32_t lo = __byte_perm(__float_as_uint(fa), __float_as_uint(fb), 0x0040);
         const uint32_t hi = __byte_perm(__float_as_uint(fc), __float_as_uint(fd), 0x0040);
         return __byte_perm(lo, hi, 0x5410);
     }
+    if (!(s > 0.0f)) return 0x80808080u;
     return code_exact(a, s) | code_exact(b, s) << 8 | code_exact(c, s) << 16 | code_exact(d, s) << 24;
 }
 
@@ -114,25 +131,53 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t word, float r) {
     return out;
 }
 
-// The block's scale and what it was: a = the lanes' largest |x| with
-// infinities counted, fine(): the largest finite one (rare)
+// The block's scale: bits = the lane's largest magnitudes, finite(): its
+// largest finite one (rare)
 struct BlockScale {
     float s, inv, ratio;  // ratio: old / s, 1 when the codes held stay as they are
     bool quick;
 };
-template <typename Fine>
-__device__ __forceinline__ BlockScale block_scale(float a, float *where, bool holds, int lane, Fine fine) {
-    a = warp_max(a);
-    if (a == INFINITY) a = warp_max(fine());
-    const float old = holds ? *where : 0.0f;
-    __syncwarp();
+template <typename T, typename Finite>
+__device__ __forceinline__ BlockScale block_scale(uint32_t bits, float old, Finite finite) {
+    if constexpr (sizeof(T) == 2) bits = max(bits & 0xffffu, bits >> 16);
+    bits = __reduce_max_sync(0xffffffffu, bits);
     BlockScale b;
+    b.quick = bits < INF_BITS<T>;
+    float a = magnitude<T>(bits);
+    if (!b.quick) a = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(finite())));
     b.s = fmaxf(old, a * (1.0f / 127.0f));
     b.ratio = old > 0.0f && b.s > old ? __fdiv_rn(old, b.s) : 1.0f;
-    b.quick = b.s > 1e-37f;
+    b.quick = b.quick && b.s > 1e-37f;
     b.inv = b.quick ? __frcp_rn(b.s) : 0.0f;
-    if (lane == 0) *where = b.s;
     return b;
+}
+
+// Which block a warp takes: its sequence and how many blocks after the first.
+// Up to 32 sequences, the blocks there are, in order; more, a row of
+// most_blocks for each.
+struct Place {
+    int b, i;
+};
+__device__ __forceinline__ Place place_of(const KvCacheArgs &a, int64_t u, int most_blocks, int lane) {
+    if (a.batch > 32) {
+        const int b = (int)(u / most_blocks);
+        return Place{b, (int)(u - (int64_t)b * most_blocks)};
+    }
+    int n = 0;
+    if (lane < a.batch) {
+        const int2 rows = kv_rows_of(a.cu, lane, a.tokens, a.max_tokens);
+        const int start = max(a.pos[lane], 0);
+        if (rows.y > 0) n = (start % KV_B + rows.y + KV_B - 1) / KV_B;
+    }
+    int x = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    const uint32_t after = __ballot_sync(0xffffffffu, x > u);  // the first whose blocks reach past u
+    const int b = after ? __ffs(after) - 1 : a.batch;
+    return Place{b, (int)u - __shfl_sync(0xffffffffu, x - n, b & 31)};
 }
 
 // Warps: one a (sequence, block its new rows reach, head, tensor).  NU: units a lane.
@@ -143,52 +188,66 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
     const int tensor = (int)(u & 1);
     u >>= 1;
     const int h = (int)(u % a.heads);
-    u /= a.heads;
-    const int b = (int)(u / most_blocks);
+    const Place at_block = place_of(a, u / a.heads, most_blocks, lane);
+    const int b = at_block.b;
     if (b >= a.batch) return;
     const int2 rows = kv_rows_of(a.cu, b, a.tokens, a.max_tokens);
     const int start = max(a.pos[b], 0);
     const int cap = a.cols * a.page;
     const int end = (int)min((int64_t)start + rows.y, (int64_t)cap);
-    const int blk = start / KV_B + (int)(u % most_blocks);
+    const int blk = start / KV_B + at_block.i;
     const int t0 = blk * KV_B;
     if (t0 >= end) return;
-    const int pg = a.table[(int64_t)b * a.cols + blk / a.bpp];
-    if (pg < 0 || pg >= a.pages) return;
-    const int64_t at = ((int64_t)pg * a.heads + h) * a.bpp + blk % a.bpp;
+    const int pg = a.table[(int64_t)b * a.cols + blk / a.bpp];  // looked at once the input is on its way
     const int nc = a.d / KV_B;
     const KvTokens src = tensor ? a.V : a.K;
     const T *x = static_cast<const T *>(src.x) + (int64_t)(rows.x - start + t0) * src.token + (int64_t)h * src.head;
-    uint8_t *codes = (tensor ? a.v : a.k) + at * (KV_B * a.d);
-    float *where = reinterpret_cast<float *>(a.scales + at) + tensor;
     const bool holds = start > t0;
-    // tokens of the block that are new / held from before
+    // tokens of the block that are new
     const auto is_new = [&](int t) { return t0 + t >= start && t0 + t < end; };
-    float top = 0.0f;
+    uint32_t top = 0;
+    uint8_t *codes = nullptr;
+    float *where = nullptr;
+    const auto find = [&] {  // false: an absent page
+        if (pg < 0 || pg >= a.pages) return false;
+        const int64_t at = ((int64_t)pg * a.heads + h) * a.bpp + blk % a.bpp;
+        codes = (tensor ? a.v : a.k) + at * (KV_B * a.d);
+        where = reinterpret_cast<float *>(a.scales + at) + tensor;
+        return true;
+    };
 
     if (tensor == 0) {
-        float v[NU][16];
+        constexpr int W = 2 * WORDS8<T>;
+        uint32_t v[NU][W];
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
             const int q = lane + 32 * i, t = q / nc, w = q - t * nc;
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[i][j] = 0;
             if (t < KV_B && is_new(t)) {
                 load8(x + (int64_t)t * src.token + 16 * w, src.wide, v[i]);
-                load8(x + (int64_t)t * src.token + 16 * w + 8, src.wide, v[i] + 8);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) v[i][j] = 0.0f;
+                load8(x + (int64_t)t * src.token + 16 * w + 8, src.wide, v[i] + W / 2);
             }
         }
+        if (!find()) return;
+        const float old = holds ? *where : 0.0f;
 #pragma unroll
         for (int i = 0; i < NU; ++i)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) top = fmaxf(top, fabsf(v[i][j]));
-        const BlockScale bs = block_scale(top, where, holds, lane, [&] {
+            for (int j = 0; j < W; ++j) top = larger<T>(top, v[i][j]);
+        const BlockScale bs = block_scale<T>(top, old, [&] {
             float m = 0.0f;
+#pragma unroll
             for (int i = 0; i < NU; ++i)
-                for (int j = 0; j < 16; ++j) m = fmaxf(m, fabsf(v[i][j]) < INFINITY ? fabsf(v[i][j]) : 0.0f);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float y = fabsf(value<T>(v[i], j));
+                    m = y < INFINITY ? fmaxf(m, y) : m;
+                }
             return m;
         });
+        __syncwarp();
+        if (lane == 0) *where = bs.s;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
             const int q = lane + 32 * i, t = q / nc, w = q - t * nc;
@@ -198,9 +257,8 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
                 uint32_t c[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    c[j] = bs.s > 0.0f ? codes4(v[i][4 * j], v[i][4 * j + 1], v[i][4 * j + 2], v[i][4 * j + 3], bs.s,
-                                                bs.inv, bs.quick)
-                                       : 0x80808080u;
+                    c[j] = codes4(value<T>(v[i], 4 * j), value<T>(v[i], 4 * j + 1), value<T>(v[i], 4 * j + 2),
+                                  value<T>(v[i], 4 * j + 3), bs.s, bs.inv, bs.quick);
                 *p = make_uint4(c[0], c[1], c[2], c[3]);
             } else if (t0 + t < start && bs.ratio != 1.0f) {
                 const uint4 c = *p;
@@ -209,8 +267,8 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
             }
         }
     } else {
-        constexpr int NV = (NU + 1) / 2;
-        float v[NV][4][8];
+        constexpr int NV = (NU + 1) / 2, W = WORDS8<T>;
+        uint32_t v[NV][4][W];
         const int last = a.d / 2;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -218,28 +276,34 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int t = 2 * c + (k & 1) + 8 * (k >> 1);
-                if (q < last && is_new(t)) {
-                    load8(x + (int64_t)t * src.token + 8 * e, src.wide, v[i][k]);
-                } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[i][k][j] = 0.0f;
-                }
+                for (int j = 0; j < W; ++j) v[i][k][j] = 0;
+                if (q < last && is_new(t)) load8(x + (int64_t)t * src.token + 8 * e, src.wide, v[i][k]);
             }
         }
+        if (!find()) return;
+        const float old = holds ? *where : 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[i][k][j]));
-        const BlockScale bs = block_scale(top, where, holds, lane, [&] {
+                for (int j = 0; j < W; ++j) top = larger<T>(top, v[i][k][j]);
+        const BlockScale bs = block_scale<T>(top, old, [&] {
             float m = 0.0f;
+#pragma unroll
             for (int i = 0; i < NV; ++i)
+#pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    for (int j = 0; j < 8; ++j)
-                        m = fmaxf(m, fabsf(v[i][k][j]) < INFINITY ? fabsf(v[i][k][j]) : 0.0f);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float y = fabsf(value<T>(v[i][k], j));
+                        m = y < INFINITY ? fmaxf(m, y) : m;
+                    }
             return m;
         });
+        __syncwarp();
+        if (lane == 0) *where = bs.s;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int q = lane + 32 * i, c = q & 3, e = q >> 2;
@@ -255,9 +319,8 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
             uint32_t *p = reinterpret_cast<uint32_t *>(codes + 8 * e * 16 + 4 * c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                uint32_t w = bs.s > 0.0f
-                                 ? codes4(v[i][0][j], v[i][1][j], v[i][2][j], v[i][3][j], bs.s, bs.inv, bs.quick)
-                                 : 0x80808080u;
+                uint32_t w = codes4(value<T>(v[i][0], j), value<T>(v[i][1], j), value<T>(v[i][2], j), value<T>(v[i][3], j),
+                                    bs.s, bs.inv, bs.quick);
                 if (fresh != 0xffffffffu) {
                     const uint32_t was = p[4 * j];
                     const uint32_t kept = bs.ratio != 1.0f ? rescale4(was, bs.ratio) : was;
@@ -272,20 +335,20 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
 // Warps: one a (sequence, block its range reaches, head, tensor).
 template <typename T, int NU>
 __global__ void __launch_bounds__(WARPS * 32) kv_read_kernel(KvCacheArgs a, int most_blocks) {
+    T *dst = static_cast<T *>(blockIdx.x * WARPS + (threadIdx.x >> 5) & 1 ? a.outv : a.outk);
+    if (!dst) return;
     const int lane = threadIdx.x & 31;
     int64_t u = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
     const int tensor = (int)(u & 1);
     u >>= 1;
     const int h = (int)(u % a.heads);
-    u /= a.heads;
-    const int b = (int)(u / most_blocks);
+    const Place at_block = place_of(a, u / a.heads, most_blocks, lane);
+    const int b = at_block.b;
     if (b >= a.batch) return;
-    T *dst = static_cast<T *>(tensor ? a.outv : a.outk);
-    if (!dst) return;
     const int2 rows = kv_rows_of(a.cu, b, a.tokens, a.max_tokens);
     const int start = max(a.pos[b], 0);
     const int64_t end = (int64_t)start + rows.y;
-    const int64_t blk = start / KV_B + u % most_blocks;
+    const int64_t blk = start / KV_B + at_block.i;
     const int64_t t0 = blk * KV_B;
     if (t0 >= end) return;
     const int64_t col = blk / a.bpp;
@@ -351,8 +414,11 @@ __global__ void __launch_bounds__(WARPS * 32) kv_read_kernel(KvCacheArgs a, int 
 // blocks that max_tokens rows reach at most, wherever the first one lies
 int most_blocks_of(const KvCacheArgs &a) { return (int)(((int64_t)a.max_tokens + KV_B - 1 + KV_B - 1) / KV_B); }
 
+// at most: the blocks of a row for each sequence, and those that the tokens fill and touch
 int64_t grid_of(const KvCacheArgs &a) {
-    return cdiv((int64_t)a.batch * most_blocks_of(a) * a.heads * 2, WARPS);
+    int64_t blocks = (int64_t)a.batch * most_blocks_of(a);
+    if (a.batch <= 32) blocks = std::min<int64_t>(blocks, a.tokens / KV_B + 2 * (int64_t)a.batch);
+    return cdiv(blocks * a.heads * 2, WARPS);
 }
 
 }  // namespace
