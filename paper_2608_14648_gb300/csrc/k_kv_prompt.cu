@@ -9,14 +9,14 @@
 // is added to them as log2 s_v (o = sum p c_v, l = sum p / s_v; the formulas of
 // k_kv_rows.cu, the running reference m included).
 //
-//   warps 0-15      softmax: 8 warps a tile, two threads a row with 32 logits of a
-//                   key tile each (one thread a row left the schedulers idle half the
-//                   time: 377 us where this takes XXX): p = 2^(s f + c) to f16, P back to
-//                   TMEM over the columns S held (the A operand of the next product)
-//   warps 16-22     converters: a block of keys (or values) at a time from
+//   warps 0-3, 4-7  softmax of tile 0 / 1, one thread a row: 16 logits at a time
+//                   from TMEM, the next 16 already on their way, p = 2^(s f + c) to
+//                   f16, P back to TMEM over the columns S held (the A operand of
+//                   the next product)
+//   warps 8-14      converters: a block of keys (or values) at a time from
 //                   global memory, one block ahead in registers, to f16 in the
 //                   128-byte-swizzled operand layout
-//   warp 23         MMA issuer
+//   warp 15         MMA issuer
 //
 // TMEM: two S/P buffers of 64 columns a tile, O0, O1 (DH columns each).  The
 // logits of a key tile are there before the softmax of the one before is done, so a
@@ -37,8 +37,7 @@ namespace skm {
 namespace {
 
 constexpr int QT = 128, KT = 64, KBLK = KT / KV_B;  // rows of a tile, keys of a tile, blocks of it
-constexpr int CONV = 7, CONV_WARP0 = 16, MMA_WARP = 23, THREADS = 768;
-constexpr int HB = KBLK / 2, HK = KT / 2;  // blocks, keys of a half row
+constexpr int CONV = 7, CONV_WARP0 = 8, MMA_WARP = 15, THREADS = 512;
 constexpr int INFO = 8;  // tiles whose scales are kept: those of the K ring and those its softmax still reads
 
 constexpr int ST = 4;  // K and V tiles in flight
@@ -46,8 +45,7 @@ template <int DH>
 struct Lay {
     static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
     static constexpr int q = 0, k = 2 * QTILE, v = k + ST * TILE, info = v + ST * TILE;
-    static constexpr int swap = info + INFO * KBLK * 16;  // a float of either half of each row
-    static constexpr int bars = swap + 2 * 2 * QT * 4, slots = bars + 8 * (4 * ST + 14);
+    static constexpr int bars = info + INFO * KBLK * 16, slots = bars + 8 * (4 * ST + 14);
     // one CTA an SM: it takes all of TMEM
     static constexpr int bytes = slots + 16 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
     static constexpr uint32_t O = 4 * KT;  // TMEM column of O0
@@ -76,17 +74,6 @@ __device__ __forceinline__ bool wait(uint32_t b, uint32_t parity, volatile int32
 // by a whole warp, with one answer
 __device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, volatile int32_t *gone) {
     return __all_sync(0xffffffffu, wait(b, parity, gone));
-}
-// whether any thread of two warps says so; a barrier of the two
-__device__ __forceinline__ int pair_or(int bar, int say) {
-    int r;
-    asm volatile(
-        "{\n\t.reg .pred p, r;\n\tsetp.ne.b32 p, %2, 0;\n\t"
-        "barrier.cta.red.or.pred r, %1, 64, p;\n\tselp.b32 %0, 1, 0, r;\n\t}\n"
-        : "=r"(r)
-        : "r"(bar), "r"(say)
-        : "memory");
-    return r;
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -129,19 +116,7 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "r"(a), "l"(b), "r"(id), "r"(add), "r"(one)
         : "memory");
 }
-// 32 / 16 columns; valid after ld_wait on the same registers
-__device__ __forceinline__ void ld32(uint32_t addr, uint32_t *v) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
-          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
-          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-        : "r"(addr)
-        : "memory");
-}
+// 16 columns; valid after ld_wait on the same registers
 __device__ __forceinline__ void ld16(uint32_t addr, uint32_t (&v)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -156,16 +131,6 @@ __device__ __forceinline__ void ld_wait(uint32_t (&v)[16]) {
                  : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
                    "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]),
                    "+r"(v[15])
-                 :
-                 : "memory");
-}
-__device__ __forceinline__ void ld_wait32(uint32_t *v) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
-                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]),
-                   "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]),
-                   "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]),
-                   "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
                  :
                  : "memory");
 }
@@ -207,52 +172,63 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
 // A part: 256 x (m, l), then 256 rows of d sums
 __host__ __device__ __forceinline__ int64_t prompt_part(int d) { return 2 * QT * (int64_t)(2 + d); }
 
-// Half of a query row to f16 in its tile's operand; returns what its logits are
-// multiplied by (k_kv_rows.cu: bf16 rows are scaled by a power of two)
+// 8 values without the alignment of a vector (not inlined: a rare path)
+__device__ __noinline__ uint4 load8(const uint16_t *x) {
+    uint32_t w[4];
+    for (int i = 0; i < 4; ++i) w[i] = x[2 * i] | (uint32_t)x[2 * i + 1] << 16;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint32_t bf16_f16(uint32_t w, float mul) {
+    return pack(__uint_as_float(w << 16) * mul, __uint_as_float(w & 0xffff0000u) * mul);
+}
+
+// A warp's 32 query rows to f16 in their tile's operand, DH / 8 lanes a row, all
+// reads issued before the first is used; returns what the logits of row `lane` are
+// multiplied by (k_kv_rows.cu: bf16 rows are scaled by a power of two).  tile0: the
+// tile's row 0, row0: the warp's first row of it.
 template <int DH>
-__device__ __forceinline__ float load_row(const KvAttnArgs &a, const uint16_t *x, bool in, uint32_t tile, int row, int half) {
-    float top = 0.0f, mul = 1.0f, back = 1.0f;
-    const auto get = [&](int i, uint32_t (&w)[4]) {  // dims 8 i .. 8 i + 7
+__device__ __forceinline__ float load_rows(const KvAttnArgs &a, const Seq &s, int h, int tile0, int row0, uint32_t tile, int lane) {
+    constexpr int LPR = DH / 8, RPI = 32 / LPR, IT = 32 / RPI;
+    const int li = lane % LPR, sub = lane / LPR;
+    uint4 raw[IT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = 0;
-        if (!in || 8 * i >= a.d) return;
-        if (a.q_wide) {
-            const uint2 u = *reinterpret_cast<const uint2 *>(x + 8 * i), v = *reinterpret_cast<const uint2 *>(x + 8 * i + 4);
-            w[0] = u.x, w[1] = u.y, w[2] = v.x, w[3] = v.y;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = x[8 * i + 2 * j] | (uint32_t)x[8 * i + 2 * j + 1] << 16;
-        }
-    };
-    const bool bf = a.dtype == SKM_DTYPE_BF16;
-    if (bf) {
-#pragma unroll 4
-        for (int i = 0; i < DH / 8; ++i) {
-            uint32_t w[4];
-            get(i, w);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[j] << 16)), fabsf(__uint_as_float(w[j] & 0xffff0000u))));
-        }
-        const uint32_t ex = __float_as_uint(top) >> 23;
-        if (ex > 0 && ex < 255) {
-            const uint32_t e = ex > 253 ? 253 : ex;
-            mul = __uint_as_float((254 - e) << 23);
-            back = __uint_as_float(e << 23);
+    for (int i = 0; i < IT; ++i) {
+        const int r = tile0 + row0 + i * RPI + sub;
+        raw[i] = make_uint4(0, 0, 0, 0);
+        if (r < s.n * a.group && 8 * li < a.d) {
+            const int t = a.by_group.div(r);
+            const uint16_t *x = static_cast<const uint16_t *>(a.Q) + (int64_t)(s.row0 + t) * a.q_token +
+                                (int64_t)(h * a.group + r - t * a.group) * a.q_head + 8 * li;
+            if (a.q_wide) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(x), v = *reinterpret_cast<const uint2 *>(x + 4);
+                raw[i] = make_uint4(u.x, u.y, v.x, v.y);
+            } else {
+                raw[i] = load8(x);
+            }
         }
     }
-#pragma unroll 4
-    for (int i = half * (DH / 16); i < (half + 1) * (DH / 16); ++i) {
-        uint32_t w[4];
-        get(i, w);
-        if (bf) {
+    float fac = a.scale_log2;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j] = pack(__uint_as_float(w[j] << 16) * mul, __uint_as_float(w[j] & 0xffff0000u) * mul);
+    for (int i = 0; i < IT; ++i) {
+        const int row = row0 + i * RPI + sub;
+        uint4 w = raw[i];
+        if (a.dtype == SKM_DTYPE_BF16) {
+            uint32_t top = 0;  // the largest |x| as bits
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = max(max(top, u[k] << 16 & 0x7fff0000u), u[k] & 0x7fff0000u);
+#pragma unroll
+            for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const uint32_t ex = top >> 23, e = ex > 253 ? 253 : ex;
+            const bool fine = ex > 0 && ex < 255;
+            const float mul = fine ? __uint_as_float((254 - e) << 23) : 1.0f, back = fine ? __uint_as_float(e << 23) : 1.0f;
+            w = make_uint4(bf16_f16(w.x, mul), bf16_f16(w.y, mul), bf16_f16(w.z, mul), bf16_f16(w.w, mul));
+            const float mine = __shfl_sync(0xffffffffu, back, (lane % RPI) * LPR);
+            if (lane / RPI == i) fac = mine * a.scale_log2;
         }
-        st_shared(tile + (i >> 3) * (QT * 128) + row * 128 + (((i & 7) ^ (row & 7)) << 4), w[0], w[1], w[2], w[3]);
+        st_shared(tile + (li >> 3) * (QT * 128) + row * 128 + (((li & 7) ^ (row & 7)) << 4), w.x, w.y, w.z, w.w);
     }
-    return back * a.scale_log2;
+    return fac;
 }
 
 template <int DH>
@@ -305,19 +281,20 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         for (int q = 0; q < 2; ++q) {
             for (int i = 0; i < 2; ++i) {
                 asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s_full(q, i)), "r"(1) : "memory");
-                asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(p_full(q, i)), "r"(8) : "memory");
+                asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(p_full(q, i)), "r"(4) : "memory");
             }
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(o_done(q)), "r"(1) : "memory");
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(o_last(q)), "r"(1) : "memory");
         }
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(q_full), "r"(16) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(q_full), "r"(8) : "memory");
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(drain), "r"(1) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *gone = 0;
     }
-    // blocks that are not there leave their operand rows as they are: finite
-    for (int i = tid * 16; i < 2 * ST * L::TILE; i += THREADS * 16) st_shared(sm + L::k + i, 0, 0, 0, 0);
-    fence_async();
+    if (a.d < DH) {  // dims from d on are zeros
+        for (int i = tid * 16; i < 2 * ST * L::TILE; i += THREADS * 16) st_shared(sm + L::k + i, 0, 0, 0, 0);
+        fence_async();
+    }
     if (warp == MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(tmem_slot)), "r"(512)
                      : "memory");
@@ -329,11 +306,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
     const uint32_t tmem = *tmem_slot;
 
     if (warp < CONV_WARP0) {  // ------------------------------------------ softmax
-        const int q = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row;
+        const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row;
         const bool in = r < rows;
-        const uint16_t *x = static_cast<const uint16_t *>(a.Q);
-        if (in) x += (int64_t)(s.row0 + a.by_group.div(r)) * a.q_token + (int64_t)(h * a.group + a.by_group.mod(r)) * a.q_head;
-        const float fac = load_row<DH>(a, x, in, sm + L::q + q * L::QTILE, row, half);
+        const float fac = load_rows<DH>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE, lane);
         fence_async();
         __syncwarp();
         if (lane == 0) arrive(q_full);
@@ -341,68 +316,70 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         // rows of the warp see [low, high] whole
         const int high = __shfl_sync(0xffffffffu, hi, 0), low = __reduce_max_sync(0xffffffffu, lo);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t S0 = tmem + lanes + q * 2 * KT + half * HK, O = tmem + lanes + L::O + q * DH;
-        // the two warps of 32 rows: a barrier, a word of each row
-        const int pair_bar = 1 + q * 4 + (warp & 3);
-        float *mine = reinterpret_cast<float *>(smem + L::swap) + (half * 2 + q) * QT + row;
-        const float *other = reinterpret_cast<const float *>(smem + L::swap) + ((half ^ 1) * 2 + q) * QT + row;
+        const uint32_t S0 = tmem + lanes + q * 2 * KT, O = tmem + lanes + L::O + q * DH;
         float m = M_NONE, l = 0.0f;
-        bool ok = true;
+        bool ok = true, loaded = false;  // loaded: v[0] holds (or will) the first logits of tile j
+        uint32_t v[2][16];
         for (int j = 0; j < n && q < nq; ++j) {
-            ok = warp_wait(s_full(q, j & 1), (j >> 1) & 1, gone);
-            fence_after();
             const uint32_t S = S0 + (j & 1) * KT;
-            const float4 *inf = info + (j & (INFO - 1)) * KBLK + half * HB;
-            const int c0 = (t0 + j) * KT + half * HK;
-            const bool whole = c0 >= low && c0 + HK - 1 <= high && inf[0].w * inf[1].w != 0.0f;
-            uint32_t P[HK / 2];
-            float add;
-            for (int pass = 0;; ++pass) {
-                uint32_t v[HK];
-                ld32(S, v);
-                float f[HB], c[HB], iv[HB];
+            if (!loaded) {
+                if (!(ok = warp_wait(s_full(q, j & 1), (j >> 1) & 1, gone))) break;
+                fence_after();
+                ld16(S, v[0]);
+            }
+            const float4 *inf = info + (j & (INFO - 1)) * KBLK;
+            const int c0 = (t0 + j) * KT;
+            const bool whole = c0 >= low && c0 + KT - 1 <= high &&
+                               __all_sync(0xffffffffu, inf[lane & (KBLK - 1)].w != 0.0f);
+            uint32_t P[KT / 2];
+            float most = 0.0f, add = 0.0f;
+            // weights of block k of the tile from 16 logits
+            const auto weigh = [&](const uint32_t (&x)[16], int k) {
+                const float4 f4 = inf[k];
+                const float f = fac * f4.x, c = f4.y - m;
+                float p[16];
 #pragma unroll
-                for (int k = 0; k < HB; ++k) {
-                    const float4 f4 = inf[k];
-                    f[k] = fac * f4.x, c[k] = f4.y - m, iv[k] = f4.z;
+                for (int i = 0; i < 16; i += 2) {
+                    const float2 t = fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), make_float2(f, f),
+                                          make_float2(c, c));
+                    p[i] = t.x, p[i + 1] = t.y;
                 }
-                ld_wait32(v);
-                float most = 0.0f;
-                add = 0.0f;
+                if (!whole) {
+                    const int at = c0 + k * KV_B, upto = f4.w != 0.0f ? hi - at : -1, from = lo - at;
 #pragma unroll
-                for (int k = 0; k < HB; ++k) {
-                    float p[16];
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float2 t = fma2(make_float2(__uint_as_float(v[16 * k + i]), __uint_as_float(v[16 * k + i + 1])),
-                                              make_float2(f[k], f[k]), make_float2(c[k], c[k]));
-                        p[i] = t.x, p[i + 1] = t.y;
-                    }
-                    if (!whole) {
-                        const int at = c0 + k * KV_B;
-                        const int upto = inf[k].w != 0.0f ? hi - at : -1, from = lo - at;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) p[i] = i <= upto && i >= from ? p[i] : -INFINITY;
-                    }
-                    float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float2 e = make_float2(ex2(p[i]), ex2(p[i + 1]));
-                        sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], e);
-                        P[k * 8 + i / 2] = pack(e.x, e.y);
-                    }
-                    const float2 both = add2(sum[0], sum[1]);
-                    const float all = both.x + both.y;
-                    most = fmaxf(most, all);
-                    add = fmaf(all, iv[k], add);
+                    for (int i = 0; i < 16; ++i) p[i] = i <= upto && i >= from ? p[i] : -INFINITY;
                 }
-                // either warp's wish is both's; a wait that gave up ends both
-                const int word = pair_or(pair_bar, most > M_MOST || !ok);
-                if (pass == 1 || !word) break;
-                // the rows' maxima, and with them new references
+                float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float2 e = make_float2(ex2(p[i]), ex2(p[i + 1]));
+                    sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], e);
+                    P[k * 8 + i / 2] = pack(e.x, e.y);
+                }
+                const float2 both = add2(sum[0], sum[1]);
+                const float all = both.x + both.y;
+                most = fmaxf(most, all);
+                add = fmaf(all, f4.z, add);
+            };
+#pragma unroll
+            for (int k = 0; k < KBLK; ++k) {
+                ld_wait(v[k & 1]);
+                if (k + 1 < KBLK) {
+                    ld16(S + (k + 1) * KV_B, v[(k + 1) & 1]);
+                } else {  // the next tile's first logits, if they are there
+                    loaded = j + 1 < n && __all_sync(0xffffffffu, bar_try(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1));
+                    if (loaded) {
+                        fence_after();
+                        ld16(S0 + ((j + 1) & 1) * KT, v[0]);
+                    }
+                }
+                weigh(v[k & 1], k);
+            }
+            if (__any_sync(0xffffffffu, most > M_MOST)) {
+                // the rows' maxima, with them new references, and the weights again
                 float top = -INFINITY;
 #pragma unroll 1
-                for (int k = 0; k < HB; ++k) {
+                for (int k = 0; k < KBLK; ++k) {
                     uint32_t w[16];
                     ld16(S + k * KV_B, w);
                     ld_wait(w);
@@ -412,40 +389,42 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                     for (int i = 0; i < 16; ++i)
                         if (i <= upto && i >= from) top = fmaxf(top, fmaf(__uint_as_float(w[i]), fac * f4.x, f4.y));
                 }
-                ok = ok && (j == 0 || warp_wait(o_done(q), (j - 1) & 1, gone));
-                *mine = ok ? top : NAN;
-                pair_or(pair_bar, 0);
-                const float theirs = *other;
-                pair_or(pair_bar, 0);
-                ok = ok && __any_sync(0xffffffffu, theirs == theirs);
-                if (!ok) break;
-                top = fmaxf(top, theirs);
                 const float to = top > m + 8.0f ? top - M_BELOW : m;
                 const float g = ex2(m - to);
                 m = to;
                 l *= g;
-                if (j > 0) {  // each warp half of O
+                if (j > 0) {
+                    if (!(ok = warp_wait(o_done(q), (j - 1) & 1, gone))) break;
                     fence_after();
 #pragma unroll 1
-                    for (int k = 0; k < DH / 32; ++k) {
+                    for (int k = 0; k < DH / 16; ++k) {
                         uint32_t w[16];
-                        ld16(O + half * (DH / 2) + k * 16, w);
+                        ld16(O + k * 16, w);
                         ld_wait(w);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * g);
-                        st16(O + half * (DH / 2) + k * 16, w);
+                        st16(O + k * 16, w);
                     }
                     st_wait();
                 }
+                add = 0.0f;
+#pragma unroll
+                for (int k = 0; k < KBLK; ++k) {
+                    uint32_t w[16];
+                    ld16(S + k * KV_B, w);
+                    ld_wait(w);
+                    weigh(w, k);
+                }
             }
-            if (!ok) break;
             l += add;
-            st16(S, P);
+#pragma unroll
+            for (int k = 0; k < KT / 2; k += 16) st16(S + k, P + k);
             st_wait();
             fence_before();
             __syncwarp();
             if (lane == 0) arrive(p_full(q, j & 1));
         }
+        if (loaded) ld_wait(v[0]);  // an early end leaves no load in flight
         if (q < nq) {
             if (ok && n > 0) {
                 ok = warp_wait(o_last(q), 0, gone);
@@ -455,18 +434,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                 l = NAN;
                 if (lane == 0 && a.status) *a.status = 1;
             }
-            *mine = l;
-            pair_or(pair_bar, 0);
-            l += *other;
             float *part = parts ? parts + (int64_t)blockIdx.x * prompt_part(a.d) : nullptr;
             const int pr = q * QT + row;
-            if (part && half == 0) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);
+            if (part) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);
             const int64_t at = in ? row_index(a, s, h, r) : 0;
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll 1
-            for (int k = half * (DH / 32); k < (half + 1) * (DH / 32); ++k) {
+            for (int k = 0; k < DH / 16; ++k) {
                 if (16 * k >= a.d) break;
                 uint32_t v[16];
+                __syncwarp();
                 if (ok && n > 0) {
                     ld16(O + k * 16, v);
                     ld_wait(v);
@@ -498,7 +475,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                 dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
                 dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
             }
-            if (in && !part && half == 0 && a.lse) a.lse[at] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
+            if (in && !part && a.lse) a.lse[at] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
         }
     } else if (warp < MMA_WARP) {  // ------------------------------------- converters
         // tasks: per tile 8 blocks of keys, then 8 of values; warp w takes w, w + 7, ...
@@ -527,15 +504,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         const auto load = [&](int task, int at, uint4 (&raw)[NV]) {
             const uint4 *p = reinterpret_cast<const uint4 *>((task & KBLK ? a.v : a.k) + (int64_t)at * (KV_B * a.d));
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i) {
+                raw[i] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);  // absent: zeros
                 if (at >= 0 && lane + 32 * i < a.d) raw[i] = __ldg(p + lane + 32 * i);
+            }
         };
-        Ahead cur = look(cw + CONV * lane), next = look(cw + CONV * (32 + lane));
         uint4 raw[NV], coming[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) raw[i] = coming[i] = make_uint4(0, 0, 0, 0);
+        Ahead cur = look(cw + CONV * lane);
         int at = __shfl_sync(0xffffffffu, cur.at, 0);
-        if (cw < tasks) load(cw, at, raw);
+        load(cw, at, raw);
+        Ahead next = look(cw + CONV * (32 + lane));
         // where a lane's vector of 16 codes goes: two 16-byte chunks, the second one next
         // to the first.  Keys, vector lane + 32 k: chunk of dims lane / 16 + 2 k, token
         // lane % 16; values: dim lane + 32 k
@@ -554,14 +532,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                 next = look(task + CONV * (33 + lane));
             }
             const int at_next = __shfl_sync(0xffffffffu, cur.at, (i + 1) & 31);
-            if (task + CONV < tasks) load(task + CONV, at_next, coming);
+            load(task + CONV, at_next, coming);
             if (!warp_wait(vals ? v_free(st) : k_free(st), ((j / ST) & 1) ^ 1, gone)) break;
             if (!vals && lane == 0) {
                 float4 f = value_scale(sc);
                 f.w = at >= 0 ? 1.0f : 0.0f;
                 info[(j & (INFO - 1)) * KBLK + blk] = f;
             }
-            if (at >= 0) {
+            {
                 const uint32_t base = sm + (vals ? L::v + lane * 128 + ((blk * 2 ^ (lane & 7)) << 4) : L::k + blk * 2048) +
                                       st * L::TILE;
 #pragma unroll
@@ -620,7 +598,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                 const uint32_t p = tmem + (2 * q + (j & 1)) * KT, o = tmem + L::O + q * DH;
                 const uint64_t va = v_op + (uint32_t)st * (L::TILE >> 4);
 #pragma unroll
-                for (int k = 0; k < KT / 16; ++k) mma_ts(o, p + (k >> 1) * HK + 8 * (k & 1), va + 2 * k, idesc(DH), k > 0 || j > 0, one);
+                for (int k = 0; k < KT / 16; ++k) mma_ts(o, p + 8 * k, va + 2 * k, idesc(DH), k > 0 || j > 0, one);
                 if (q == nq - 1) commit(v_free(st), one);
                 commit(o_done(q), one);
                 // a barrier of its own for the last product: the softmax may be up to two
