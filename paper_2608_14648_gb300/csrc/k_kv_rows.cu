@@ -740,6 +740,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
     }
 
     const int64_t i0 = c0 + (c1 - c0) * warp / NW, i1 = c0 + (c1 - c0) * (warp + 1) / NW;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the join waits for this kernel's end all the same
     Rows rows;
     bool open = false, ok = true;
     int useq = 0, uunit = 0;       // the open unit
@@ -858,7 +859,6 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
         }
         open = leave(true);
     }
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // a unit still open leaves its part where the warp's ring was
     const int64_t pf = part_floats<RT>(a.d);
     if (open) {
@@ -886,7 +886,8 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
 template <int RT>
 __global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ KvAttnArgs a, int nw, int64_t grid) {
     __shared__ int64_t sums[2][4];
-    __shared__ float tops[4], sl[4], weight[KV_SMS];
+    __shared__ float tops[4], sl[4];
+    __shared__ float2 ml[KV_SMS];  // (m, l) of the parts, then (weight, .)
     __shared__ float4 so[3][64];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = a.max_tiles * a.heads, r = blockIdx.x % RT;
@@ -912,11 +913,12 @@ __global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ Kv
     all = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
     const int64_t u0 = before + (int64_t)unit * s.cnt, u1 = u0 + s.cnt;
     const int64_t C = active_ctas(all, nw, grid);
-    // CTA c takes [all c / C, all (c + 1) / C): the one that holds an item
+    // CTA c takes [all c / C, all (c + 1) / C): the one that holds an item, with
+    // floor(all c / C) <= item written as all c < C (item + 1)
     const auto holder = [&](int64_t item) {
-        int64_t c = item * C / all;
-        while (all * (c + 1) / C <= item) ++c;
-        while (all * c / C > item) --c;
+        int64_t c = (int64_t)((uint64_t)item * (uint64_t)C / (uint64_t)all);
+        while (all * (c + 1) < C * (item + 1)) ++c;
+        while (all * c >= C * (item + 1)) --c;
         return c;
     };
     const int first = (int)holder(u0), np = (int)holder(u1 - 1) - first + 1;
@@ -927,7 +929,11 @@ __global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ Kv
     const auto part = [&](int i) { return base + (2 * (int64_t)i + (i == 0 ? 1 : 0)) * pf; };
     asm volatile("griddepcontrol.wait;" ::: "memory");
     float m = M_NONE;
-    for (int i = tid; i < np; i += 128) m = fmaxf(m, part(i)[2 * r]);
+    for (int i = tid; i < np; i += 128) {
+        const float2 x = *reinterpret_cast<const float2 *>(part(i) + 2 * r);
+        ml[i] = x;
+        m = fmaxf(m, x.x);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     if (lane == 0) tops[warp] = m;
@@ -935,10 +941,9 @@ __global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ Kv
     m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     float l = 0.0f;
     for (int i = tid; i < np; i += 128) {
-        const float2 ml = *reinterpret_cast<const float2 *>(part(i) + 2 * r);
-        const float f = ex2(ml.x - m);
-        weight[i] = f;
-        l = fmaf(ml.y, f, l);
+        const float f = ex2(ml[i].x - m);
+        l = fmaf(ml[i].y, f, l);
+        ml[i].x = f;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
@@ -949,7 +954,7 @@ __global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ Kv
     const int d4 = a.d / 4;
 #pragma unroll 4
     for (int i = warp; i < np; i += 4) {
-        const float f = weight[i];
+        const float f = ml[i].x;
         const float4 *p = reinterpret_cast<const float4 *>(part(i) + part_head<RT>() + r * a.d);
 #pragma unroll
         for (int k = 0; k < 2; ++k)
@@ -1006,7 +1011,7 @@ KvRowsPlan plan_rows(int nb, int heads, int group, int d, int max_tokens, int64_
     p.rt = Rows::RT;
     p.nw = nw;
     p.units = (int64_t)nb * cdiv((int64_t)max_tokens * group, p.rt) * heads;
-    p.whole = span <= 1024;
+    p.whole = span <= 2048;
     p.ns = 4;
     const int seqs = p.whole ? 1 : nb;
     while (p.ns > 1 && smem_of<Rows>(seqs, d, nw, p.ns).total > SMEM_MOST) --p.ns;
