@@ -38,6 +38,7 @@ namespace {
 
 constexpr int QT = 128, KT = 64, KBLK = KT / KV_B;  // rows of a tile, keys of a tile, blocks of it
 constexpr int CONV = 7, CONV_WARP0 = 8, MMA_WARP = 15, THREADS = 512;
+constexpr int RANKED = 256;
 constexpr int INFO = 8;  // tiles whose scales are kept: those of the K ring and those its softmax still reads
 
 constexpr int ST = 4;  // K and V tiles in flight
@@ -45,9 +46,9 @@ template <int DH>
 struct Lay {
     static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
     static constexpr int q = 0, k = 2 * QTILE, v = k + ST * TILE, info = v + ST * TILE;
-    static constexpr int bars = info + INFO * KBLK * 16, slots = bars + 8 * (4 * ST + 14);
+    static constexpr int bars = info + INFO * KBLK * 16, slots = bars + 8 * (4 * ST + 14);  // TMEM address, a flag, the part's index
     // one CTA an SM: it takes all of TMEM
-    static constexpr int bytes = slots + 16 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
+    static constexpr int bytes = slots + 32 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
     static constexpr uint32_t O = 4 * KT;  // TMEM column of O0
 };
 
@@ -74,6 +75,18 @@ __device__ __forceinline__ bool wait(uint32_t b, uint32_t parity, volatile int32
 // by a whole warp, with one answer
 __device__ __forceinline__ bool warp_wait(uint32_t b, uint32_t parity, volatile int32_t *gone) {
     return __all_sync(0xffffffffu, wait(b, parity, gone));
+}
+// whether a phase is over, without the wait that a try may include
+__device__ __forceinline__ bool bar_test(uint32_t b, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}\n"
+        : "=r"(ok)
+        : "r"(b), "r"(parity)
+        : "memory");
+    return ok != 0;
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -250,16 +263,39 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
     const uint32_t q_full = bar(4 * ST + 12), drain = bar(4 * ST + 13);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::slots);
     volatile int32_t *gone = reinterpret_cast<volatile int32_t *>(smem + L::slots + 4);
-    float4 *info = reinterpret_cast<float4 *>(smem + L::info);  // (k scale, log2 v scale, 1 / v scale, there)
+    float4 *info = reinterpret_cast<float4 *>(smem + L::info);  // a block's value_scale, its log2 -infinity where the block is absent
 
-    // the unit: later rows first (causal: they see the most)
-    const int tiles = (a.max_tiles + 1) / 2;  // pairs of row tiles
+    // the unit: a sequence's pair of row tiles, longest first (few pairs are ranked by
+    // the key tiles they see; of many, the later rows come first), its heads next
+    // to each other
+    const int tiles = (a.max_tiles + 1) / 2, pairs = a.nb * tiles;
     int u = blockIdx.x;
     const int split = u % splits;
     u /= splits;
     const int h = a.by_heads.mod(u);
     u = a.by_heads.div(u);
-    const int bi = u % a.nb, pair = tiles - 1 - u / a.nb, b = a.b0 + bi;
+    if (pairs <= RANKED) {
+        int *length = reinterpret_cast<int *>(smem), *pick = length + RANKED;
+        if (tid < pairs) {
+            const Seq s = seq_of(a, a.b0 + tid / tiles);
+            const int r0 = tid % tiles * 2 * QT, r1 = min(r0 + 2 * QT, s.n * a.group) - 1;
+            length[tid] = r1 < r0 ? -1 : last_of(a, s, r1) / KT - first_of(a, s, r0) / KT;
+        }
+        __syncthreads();
+        if (tid < pairs) {
+            int rank = 0;
+            for (int i = 0; i < pairs; ++i) rank += length[i] > length[tid] || (length[i] == length[tid] && i < tid);
+            if (rank == u) *pick = tid;
+        }
+        __syncthreads();
+        u = *pick;
+        __syncthreads();
+    } else {
+        u = u % a.nb * tiles + tiles - 1 - u / a.nb;
+    }
+    const int bi = u / tiles, pair = u % tiles, b = a.b0 + bi;
+    int64_t *part_index = reinterpret_cast<int64_t *>(smem + L::slots + 8);
+    if (tid == 0) *part_index = ((int64_t)u * a.heads + h) * splits + split;
     const Seq s = seq_of(a, b);
     const int rows = s.n * a.group, r0 = pair * 2 * QT;
     if (r0 >= rows) return;
@@ -329,8 +365,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
             }
             const float4 *inf = info + (j & (INFO - 1)) * KBLK;
             const int c0 = (t0 + j) * KT;
-            const bool whole = c0 >= low && c0 + KT - 1 <= high &&
-                               __all_sync(0xffffffffu, inf[lane & (KBLK - 1)].w != 0.0f);
+            const bool whole = c0 >= low && c0 + KT - 1 <= high;
             uint32_t P[KT / 2];
             float most = 0.0f, add = 0.0f;
             // weights of block k of the tile from 16 logits
@@ -345,7 +380,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                     p[i] = t.x, p[i + 1] = t.y;
                 }
                 if (!whole) {
-                    const int at = c0 + k * KV_B, upto = f4.w != 0.0f ? hi - at : -1, from = lo - at;
+                    int upto = hi - (c0 + k * KV_B), from = lo - (c0 + k * KV_B);
+                    // opaque, so that the comparisons stay in the branch (hoisted, they
+                    // were two integer operations a logit in every tile)
+                    asm volatile("" : "+r"(upto), "+r"(from));
 #pragma unroll
                     for (int i = 0; i < 16; ++i) p[i] = i <= upto && i >= from ? p[i] : -INFINITY;
                 }
@@ -367,7 +405,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                 if (k + 1 < KBLK) {
                     ld16(S + (k + 1) * KV_B, v[(k + 1) & 1]);
                 } else {  // the next tile's first logits, if they are there
-                    loaded = j + 1 < n && __all_sync(0xffffffffu, bar_try(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1));
+                    loaded = j + 1 < n && __all_sync(0xffffffffu, bar_test(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1));
                     if (loaded) {
                         fence_after();
                         ld16(S0 + ((j + 1) & 1) * KT, v[0]);
@@ -384,7 +422,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                     ld16(S + k * KV_B, w);
                     ld_wait(w);
                     const float4 f4 = inf[k];
-                    const int at = c0 + k * KV_B, upto = f4.w != 0.0f ? hi - at : -1, from = lo - at;
+                    const int upto = hi - (c0 + k * KV_B), from = lo - (c0 + k * KV_B);
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         if (i <= upto && i >= from) top = fmaxf(top, fmaf(__uint_as_float(w[i]), fac * f4.x, f4.y));
@@ -434,7 +472,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                 l = NAN;
                 if (lane == 0 && a.status) *a.status = 1;
             }
-            float *part = parts ? parts + (int64_t)blockIdx.x * prompt_part(a.d) : nullptr;
+            float *part = parts ? parts + *part_index * prompt_part(a.d) : nullptr;
             const int pr = q * QT + row;
             if (part) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);
             const int64_t at = in ? row_index(a, s, h, r) : 0;
@@ -536,7 +574,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
             if (!warp_wait(vals ? v_free(st) : k_free(st), ((j / ST) & 1) ^ 1, gone)) break;
             if (!vals && lane == 0) {
                 float4 f = value_scale(sc);
-                f.w = at >= 0 ? 1.0f : 0.0f;
+                if (at < 0) f.y = -INFINITY;  // an absent block: no weight (its codes are zeros)
                 info[(j & (INFO - 1)) * KBLK + blk] = f;
             }
             {
@@ -634,10 +672,8 @@ __global__ void __launch_bounds__(256) kv_prompt_join_kernel(const __grid_consta
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tiles = (a.max_tiles + 1) / 2;
     const int unit = blockIdx.x / (2 * QT / 8), pr = blockIdx.x % (2 * QT / 8) * 8 + (threadIdx.x >> 5);
-    int u = unit;
-    const int h = a.by_heads.mod(u);
-    u = a.by_heads.div(u);
-    const int b = a.b0 + u % a.nb, r = (tiles - 1 - u / a.nb) * 2 * QT + pr;
+    const int h = a.by_heads.mod(unit), u = a.by_heads.div(unit);
+    const int b = a.b0 + u / tiles, r = u % tiles * 2 * QT + pr;
     const Seq s = seq_of(a, b);
     if (r >= s.n * a.group) return;
     const float *base = parts + (int64_t)unit * splits * prompt_part(a.d);
