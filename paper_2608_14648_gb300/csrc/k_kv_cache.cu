@@ -21,7 +21,7 @@
 // Rounding: code = rint(x / scale) with the quotient rounded to fp32.  x times
 // the reciprocal is within 1.6e-5 of x / scale (|quotient| < 128, two roundings
 // of 2^-24 relative), the fp32 quotient within 8e-6, so both round to the same
-// integer unless x times the reciprocal lies within 1e-4 of a half; only those
+// integer unless x times the reciprocal lies within 3e-5 of a half; only those
 // elements take the division.
 #include <algorithm>
 #include <type_traits>
@@ -34,29 +34,34 @@ namespace {
 
 constexpr int WARPS = 8;
 constexpr float CODE_MAGIC = 12583040.0f;  // 1.5 2^23 + 128: q + this holds rint(q) + 128 in its low byte
-constexpr float NEAR_HALF = 0.4999f;
+constexpr float NEAR_HALF = 0.49997f;
 
 template <typename T>
 constexpr int WORDS8 = 8 * sizeof(T) / 4;  // words of 8 values
 template <typename T>
 constexpr uint32_t INF_BITS = std::is_same<T, float>::value ? 0x7f800000u : std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
 
+// 16 bytes without the alignment of a vector (not inlined: the loads would be
+// predicated into the aligned path)
+template <typename T>
+__device__ __noinline__ uint4 load_slowly(const T *p) {
+    uint32_t w[4];
+    if constexpr (sizeof(T) == 4) {
+        for (int i = 0; i < 4; ++i) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+    } else {
+        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+        for (int i = 0; i < 4; ++i) w[i] = h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 // 8 consecutive values as they are
 template <typename T>
 __device__ __forceinline__ void load8(const T *p, int wide, uint32_t *w) {
-    if (wide) {
 #pragma unroll
-        for (int i = 0; i < WORDS8<T>; i += 4) {
-            const uint4 a = reinterpret_cast<const uint4 *>(p)[i / 4];
-            w[i] = a.x, w[i + 1] = a.y, w[i + 2] = a.z, w[i + 3] = a.w;
-        }
-    } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
-    } else {
-        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
+    for (int i = 0; i < WORDS8<T>; i += 4) {
+        const T *q = p + i * (4 / (int)sizeof(T));
+        const uint4 a = wide ? *reinterpret_cast<const uint4 *>(q) : load_slowly(q);
+        w[i] = a.x, w[i + 1] = a.y, w[i + 2] = a.z, w[i + 3] = a.w;
     }
 }
 // value i of words
@@ -110,17 +115,24 @@ __device__ __noinline__ uint32_t code_exact(float x, float s) {
 // codes of four values in a word, the first in the low byte; quick: they are
 // finite and the reciprocal of s is a normal number
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float s, float inv, bool quick) {
+    if (!quick) {
+        if (!(s > 0.0f)) return 0x80808080u;
+        return code_exact(a, s) | code_exact(b, s) << 8 | code_exact(c, s) << 16 | code_exact(d, s) << 24;
+    }
     const float fa = fmaf(a, inv, CODE_MAGIC), fb = fmaf(b, inv, CODE_MAGIC);
     const float fc = fmaf(c, inv, CODE_MAGIC), fd = fmaf(d, inv, CODE_MAGIC);
     const float ra = fmaf(a, inv, CODE_MAGIC - fa), rb = fmaf(b, inv, CODE_MAGIC - fb);
     const float rc = fmaf(c, inv, CODE_MAGIC - fc), rd = fmaf(d, inv, CODE_MAGIC - fd);
-    if (quick && fmaxf(fmaxf(fabsf(ra), fabsf(rb)), fmaxf(fabsf(rc), fabsf(rd))) <= NEAR_HALF) {
-        const uint32_t lo = __byte_perm(__float_as_uint(fa), __float_as_uint(fb), 0x0040);
-        const uint32_t hi = __byte_perm(__float_as_uint(fc), __float_as_uint(fd), 0x0040);
-        return __byte_perm(lo, hi, 0x5410);
+    const uint32_t lo = __byte_perm(__float_as_uint(fa), __float_as_uint(fb), 0x0040);
+    const uint32_t hi = __byte_perm(__float_as_uint(fc), __float_as_uint(fd), 0x0040);
+    uint32_t w = __byte_perm(lo, hi, 0x5410);
+    if (fmaxf(fmaxf(fabsf(ra), fabsf(rb)), fmaxf(fabsf(rc), fabsf(rd))) > NEAR_HALF) {
+        if (fabsf(ra) > NEAR_HALF) w = (w & 0xffffff00u) | code_exact(a, s);
+        if (fabsf(rb) > NEAR_HALF) w = (w & 0xffff00ffu) | code_exact(b, s) << 8;
+        if (fabsf(rc) > NEAR_HALF) w = (w & 0xff00ffffu) | code_exact(c, s) << 16;
+        if (fabsf(rd) > NEAR_HALF) w = (w & 0x00ffffffu) | code_exact(d, s) << 24;
     }
-    if (!(s > 0.0f)) return 0x80808080u;
-    return code_exact(a, s) | code_exact(b, s) << 8 | code_exact(c, s) << 16 | code_exact(d, s) << 24;
+    return w;
 }
 
 // codes of a word of the block's earlier tokens after its scale grew by 1 / r
@@ -158,11 +170,8 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t bits, float old, Fini
 struct Place {
     int b, i;
 };
-__device__ __forceinline__ Place place_of(const KvCacheArgs &a, int64_t u, int most_blocks, int lane) {
-    if (a.batch > 32) {
-        const int b = (int)(u / most_blocks);
-        return Place{b, (int)(u - (int64_t)b * most_blocks)};
-    }
+__device__ __forceinline__ Place place_of(const KvCacheArgs &a, int u, int lane) {
+    if (a.batch > 32) return Place{a.by_most.div(u), a.by_most.mod(u)};
     int n = 0;
     if (lane < a.batch) {
         const int2 rows = kv_rows_of(a.cu, lane, a.tokens, a.max_tokens);
@@ -177,18 +186,16 @@ __device__ __forceinline__ Place place_of(const KvCacheArgs &a, int64_t u, int m
     }
     const uint32_t after = __ballot_sync(0xffffffffu, x > u);  // the first whose blocks reach past u
     const int b = after ? __ffs(after) - 1 : a.batch;
-    return Place{b, (int)u - __shfl_sync(0xffffffffu, x - n, b & 31)};
+    return Place{b, u - __shfl_sync(0xffffffffu, x - n, b & 31)};
 }
 
 // Warps: one a (sequence, block its new rows reach, head, tensor).  NU: units a lane.
 template <typename T, int NU>
-__global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int most_blocks) {
+__global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(const __grid_constant__ KvCacheArgs a) {
     const int lane = threadIdx.x & 31;
-    int64_t u = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
-    const int tensor = (int)(u & 1);
-    u >>= 1;
-    const int h = (int)(u % a.heads);
-    const Place at_block = place_of(a, u / a.heads, most_blocks, lane);
+    const int warp = blockIdx.x * WARPS + (threadIdx.x >> 5), tensor = warp & 1;
+    const int h = a.by_heads.mod(warp >> 1);
+    const Place at_block = place_of(a, a.by_heads.div(warp >> 1), lane);
     const int b = at_block.b;
     if (b >= a.batch) return;
     const int2 rows = kv_rows_of(a.cu, b, a.tokens, a.max_tokens);
@@ -198,30 +205,32 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
     const int blk = start / KV_B + at_block.i;
     const int t0 = blk * KV_B;
     if (t0 >= end) return;
-    const int pg = a.table[(int64_t)b * a.cols + blk / a.bpp];  // looked at once the input is on its way
+    const int pg = a.table[(int64_t)b * a.cols + a.by_bpp.div(blk)];  // looked at once the input is on its way
     const int nc = a.d / KV_B;
     const KvTokens src = tensor ? a.V : a.K;
     const T *x = static_cast<const T *>(src.x) + (int64_t)(rows.x - start + t0) * src.token + (int64_t)h * src.head;
     const bool holds = start > t0;
-    // tokens of the block that are new
-    const auto is_new = [&](int t) { return t0 + t >= start && t0 + t < end; };
+    const bool full = !holds && t0 + KV_B <= end;
     uint32_t top = 0;
     uint8_t *codes = nullptr;
     float *where = nullptr;
     const auto find = [&] {  // false: an absent page
         if (pg < 0 || pg >= a.pages) return false;
-        const int64_t at = ((int64_t)pg * a.heads + h) * a.bpp + blk % a.bpp;
+        const int64_t at = ((int64_t)pg * a.heads + h) * a.bpp + a.by_bpp.mod(blk);
         codes = (tensor ? a.v : a.k) + at * (KV_B * a.d);
         where = reinterpret_cast<float *>(a.scales + at) + tensor;
         return true;
     };
 
-    if (tensor == 0) {
+    // ALL: every token of the block is new
+    const auto keys = [&](auto all) {
+        constexpr bool ALL = decltype(all)::value;
+        const auto is_new = [&](int t) { return ALL || (t0 + t >= start && t0 + t < end); };
         constexpr int W = 2 * WORDS8<T>;
         uint32_t v[NU][W];
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int q = lane + 32 * i, t = q / nc, w = q - t * nc;
+            const int q = lane + 32 * i, t = a.by_chunks.div(q), w = q - t * nc;
 #pragma unroll
             for (int j = 0; j < W; ++j) v[i][j] = 0;
             if (t < KV_B && is_new(t)) {
@@ -250,7 +259,7 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
         if (lane == 0) *where = bs.s;
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int q = lane + 32 * i, t = q / nc, w = q - t * nc;
+            const int q = lane + 32 * i, t = a.by_chunks.div(q), w = q - t * nc;
             if (t >= KV_B) continue;
             uint4 *p = reinterpret_cast<uint4 *>(codes + w * 256 + t * 16);
             if (is_new(t)) {
@@ -266,7 +275,10 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
                                 rescale4(c.w, bs.ratio));
             }
         }
-    } else {
+    };
+    const auto values = [&](auto all) {
+        constexpr bool ALL = decltype(all)::value;
+        const auto is_new = [&](int t) { return ALL || (t0 + t >= start && t0 + t < end); };
         constexpr int NV = (NU + 1) / 2, W = WORDS8<T>;
         uint32_t v[NV][4][W];
         const int last = a.d / 2;
@@ -313,15 +325,15 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
             for (int k = 0; k < 4; ++k) {
                 const int t = 2 * c + (k & 1) + 8 * (k >> 1);
                 if (is_new(t)) fresh |= 0xffu << (8 * k);
-                if (t0 + t < start) held |= 0xffu << (8 * k);
+                if (!ALL && t0 + t < start) held |= 0xffu << (8 * k);
             }
-            if (!fresh && (!held || bs.ratio == 1.0f)) continue;
+            if (!ALL && !fresh && (!held || bs.ratio == 1.0f)) continue;
             uint32_t *p = reinterpret_cast<uint32_t *>(codes + 8 * e * 16 + 4 * c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 uint32_t w = codes4(value<T>(v[i][0], j), value<T>(v[i][1], j), value<T>(v[i][2], j), value<T>(v[i][3], j),
                                     bs.s, bs.inv, bs.quick);
-                if (fresh != 0xffffffffu) {
+                if (!ALL && fresh != 0xffffffffu) {
                     const uint32_t was = p[4 * j];
                     const uint32_t kept = bs.ratio != 1.0f ? rescale4(was, bs.ratio) : was;
                     w = (w & fresh) | (kept & held) | (was & ~(fresh | held));
@@ -329,32 +341,32 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(KvCacheArgs a, int
                 p[4 * j] = w;
             }
         }
-    }
+    };
+    if (tensor == 0) full ? keys(std::true_type{}) : keys(std::false_type{});
+    else full ? values(std::true_type{}) : values(std::false_type{});
 }
 
 // Warps: one a (sequence, block its range reaches, head, tensor).
 template <typename T, int NU>
-__global__ void __launch_bounds__(WARPS * 32) kv_read_kernel(KvCacheArgs a, int most_blocks) {
+__global__ void __launch_bounds__(WARPS * 32) kv_read_kernel(const __grid_constant__ KvCacheArgs a) {
     T *dst = static_cast<T *>(blockIdx.x * WARPS + (threadIdx.x >> 5) & 1 ? a.outv : a.outk);
     if (!dst) return;
     const int lane = threadIdx.x & 31;
-    int64_t u = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
-    const int tensor = (int)(u & 1);
-    u >>= 1;
-    const int h = (int)(u % a.heads);
-    const Place at_block = place_of(a, u / a.heads, most_blocks, lane);
+    const int warp = blockIdx.x * WARPS + (threadIdx.x >> 5), tensor = warp & 1;
+    const int h = a.by_heads.mod(warp >> 1);
+    const Place at_block = place_of(a, a.by_heads.div(warp >> 1), lane);
     const int b = at_block.b;
     if (b >= a.batch) return;
     const int2 rows = kv_rows_of(a.cu, b, a.tokens, a.max_tokens);
     const int start = max(a.pos[b], 0);
     const int64_t end = (int64_t)start + rows.y;
-    const int64_t blk = start / KV_B + at_block.i;
-    const int64_t t0 = blk * KV_B;
+    const int blk = start / KV_B + at_block.i;
+    const int64_t t0 = (int64_t)blk * KV_B;
     if (t0 >= end) return;
-    const int64_t col = blk / a.bpp;
+    const int col = a.by_bpp.div(blk);
     const int pg = col < a.cols ? a.table[(int64_t)b * a.cols + col] : -1;
     const bool there = pg >= 0 && pg < a.pages;
-    const int64_t at = there ? ((int64_t)pg * a.heads + h) * a.bpp + blk % a.bpp : 0;
+    const int64_t at = there ? ((int64_t)pg * a.heads + h) * a.bpp + a.by_bpp.mod(blk) : 0;
     const int nc = a.d / KV_B;
     const uint8_t *codes = (tensor ? a.v : a.k) + at * (KV_B * a.d);
     const float s = there ? reinterpret_cast<const float *>(a.scales + at)[tensor] : 0.0f;
@@ -366,13 +378,13 @@ __global__ void __launch_bounds__(WARPS * 32) kv_read_kernel(KvCacheArgs a, int 
         uint4 c[NU];
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int q = lane + 32 * i, t = q / nc, w = q - t * nc;
+            const int q = lane + 32 * i, t = a.by_chunks.div(q), w = q - t * nc;
             c[i] = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
             if (there && t < KV_B && wanted(t)) c[i] = *reinterpret_cast<const uint4 *>(codes + w * 256 + t * 16);
         }
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-            const int q = lane + 32 * i, t = q / nc, w = q - t * nc;
+            const int q = lane + 32 * i, t = a.by_chunks.div(q), w = q - t * nc;
             if (t >= KV_B || !wanted(t)) continue;
             const uint32_t word[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
             float v[16];
@@ -425,13 +437,22 @@ int64_t grid_of(const KvCacheArgs &a) {
 
 #define KV_BY_TYPE(KERNEL, NU)                                                                              \
     do {                                                                                                    \
-        if (dtype == SKM_DTYPE_F32) KERNEL<float, NU><<<grid, WARPS * 32, 0, st>>>(a, most_blocks_of(a));      \
+        if (dtype == SKM_DTYPE_F32) KERNEL<float, NU><<<grid, WARPS * 32, 0, st>>>(a);      \
         else if (dtype == SKM_DTYPE_BF16)                                                                   \
-            KERNEL<__nv_bfloat16, NU><<<grid, WARPS * 32, 0, st>>>(a, most_blocks_of(a));                   \
-        else KERNEL<__half, NU><<<grid, WARPS * 32, 0, st>>>(a, most_blocks_of(a));                         \
+            KERNEL<__nv_bfloat16, NU><<<grid, WARPS * 32, 0, st>>>(a);                   \
+        else KERNEL<__half, NU><<<grid, WARPS * 32, 0, st>>>(a);                         \
     } while (0)
 
-cudaError_t launch_kv_write(const KvCacheArgs &a, int dtype, cudaStream_t st) {
+static KvCacheArgs with_divisions(KvCacheArgs a) {
+    a.by_heads = FastDiv(a.heads);
+    a.by_bpp = FastDiv(a.bpp);
+    a.by_most = FastDiv(most_blocks_of(a));
+    a.by_chunks = FastDiv(a.d / KV_B);
+    return a;
+}
+
+cudaError_t launch_kv_write(const KvCacheArgs &args, int dtype, cudaStream_t st) {
+    const KvCacheArgs a = with_divisions(args);
     const unsigned grid = (unsigned)grid_of(a);
     if (a.d <= 64) KV_BY_TYPE(kv_write_kernel, 2);
     else if (a.d <= 128) KV_BY_TYPE(kv_write_kernel, 4);
@@ -439,7 +460,8 @@ cudaError_t launch_kv_write(const KvCacheArgs &a, int dtype, cudaStream_t st) {
     return launched();
 }
 
-cudaError_t launch_kv_read(const KvCacheArgs &a, int dtype, cudaStream_t st) {
+cudaError_t launch_kv_read(const KvCacheArgs &args, int dtype, cudaStream_t st) {
+    const KvCacheArgs a = with_divisions(args);
     const unsigned grid = (unsigned)grid_of(a);
     if (a.d <= 64) KV_BY_TYPE(kv_read_kernel, 2);
     else if (a.d <= 128) KV_BY_TYPE(kv_read_kernel, 4);

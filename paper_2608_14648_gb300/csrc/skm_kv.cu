@@ -74,7 +74,7 @@ KvCacheArgs cache_args(const skm_kv_cache *c, const skm_kv_seqs *s) {
 // a launch's warps must fit a grid
 int check_grid(const skm_kv_cache *c, const skm_kv_seqs *s) {
     const int64_t blocks = (most_tokens(s) + 2 * KV_B - 2) / KV_B;
-    if ((double)s->batch * blocks * c->heads > 4e9)
+    if ((double)s->batch * blocks * c->heads > 1e9)
         return set_error(SKM_ERR_UNSUPPORTED, "batch * max_tokens * heads is too large");
     return SKM_OK;
 }

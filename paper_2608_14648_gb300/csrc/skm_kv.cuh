@@ -40,6 +40,7 @@ struct KvCacheArgs {
     const int32_t *table, *pos, *cu;
     int heads, d, page, pages, bpp;  // bpp: blocks of a page
     int batch, cols, tokens, max_tokens;
+    FastDiv by_heads, by_bpp, by_most, by_chunks;  // (set by the launchers) most blocks of a sequence, 16-dim chunks
     KvTokens K, V;    // write: sources
     void *outk, *outv;  // read: destinations
 };
