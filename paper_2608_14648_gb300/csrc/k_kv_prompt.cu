@@ -1,8 +1,9 @@
 // Attention over the 8-bit cache for many query rows (prompt chunks) on
-// tcgen05: 16-bit queries, d <= 128.
+// tcgen05: 16-bit queries.
 //
 // A CTA takes 256 query rows (token-major, then the heads of a group) of one
-// sequence and key/value head as two tiles of 128, and walks the keys they see in
+// sequence and key/value head as two tiles of 128 (d > 128: one tile, so that its
+// sums fit TMEM and its operands shared memory), and walks the keys they see in
 // tiles of 64 positions (4 blocks of the cache).  The codes are exact in f16, so
 // both products run in kind::f16 and the block scales stay out of the
 // operands: the key scale multiplies the logits of its block, the value scale
@@ -16,7 +17,7 @@
 //   warps 8-14      converters: a block of keys (or values) at a time from
 //                   global memory, one block ahead in registers, to f16 in the
 //                   128-byte-swizzled operand layout
-//   warp 15         MMA issuer
+//   warp 15         MMA issuer (d > 128: 4 softmax warps, the others behind them)
 //
 // TMEM: two S/P buffers of 64 columns a tile, O0, O1 (DH columns each).  The
 // logits of a key tile are there before the softmax of the one before is done, so a
@@ -37,19 +38,23 @@ namespace skm {
 namespace {
 
 constexpr int QT = 128, KT = 64, KBLK = KT / KV_B;  // rows of a tile, keys of a tile, blocks of it
-constexpr int CONV = 7, CONV_WARP0 = 8, MMA_WARP = 15, THREADS = 512;
+constexpr int CONV = 7;  // converter warps
 constexpr int RANKED = 256;
 constexpr int INFO = 8;  // tiles whose scales are kept: those of the K ring and those its softmax still reads
 
-constexpr int ST = 4;  // K and V tiles in flight
+// DH: dims, padded to 64, 128 or 256
 template <int DH>
 struct Lay {
+    static constexpr int NQ = DH <= 128 ? 2 : 1;      // row tiles of a CTA
+    static constexpr int ST = DH <= 128 ? 4 : 2;      // K and V tiles in flight
+    static constexpr int ROWS = NQ * QT;
+    static constexpr int CONV_WARP0 = 4 * NQ, MMA_WARP = CONV_WARP0 + CONV, THREADS = 32 * (MMA_WARP + 1);
     static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
-    static constexpr int q = 0, k = 2 * QTILE, v = k + ST * TILE, info = v + ST * TILE;
+    static constexpr int q = 0, k = NQ * QTILE, v = k + ST * TILE, info = v + ST * TILE;
     static constexpr int bars = info + INFO * KBLK * 16, slots = bars + 8 * (4 * ST + 14);  // TMEM address, a flag, the part's index
     // one CTA an SM: it takes all of TMEM
     static constexpr int bytes = slots + 32 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
-    static constexpr uint32_t O = 4 * KT;  // TMEM column of O0
+    static constexpr uint32_t O = NQ * 2 * KT;  // TMEM column of O0
 };
 
 __device__ __forceinline__ void arrive(uint32_t b) {
@@ -182,8 +187,8 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// A part: 256 x (m, l), then 256 rows of d sums
-__host__ __device__ __forceinline__ int64_t prompt_part(int d) { return 2 * QT * (int64_t)(2 + d); }
+// A part: a CTA's rows x (m, l), then its rows of d sums
+__host__ __device__ __forceinline__ int64_t prompt_part(int rows, int d) { return rows * (int64_t)(2 + d); }
 
 // 8 values without the alignment of a vector (not inlined: a rare path)
 __device__ __noinline__ uint4 load8(const uint16_t *x) {
@@ -201,52 +206,56 @@ __device__ __forceinline__ uint32_t bf16_f16(uint32_t w, float mul) {
 // tile's row 0, row0: the warp's first row of it.
 template <int DH>
 __device__ __forceinline__ float load_rows(const KvAttnArgs &a, const Seq &s, int h, int tile0, int row0, uint32_t tile, int lane) {
-    constexpr int LPR = DH / 8, RPI = 32 / LPR, IT = 32 / RPI;
+    constexpr int LPR = DH / 8, RPI = 32 / LPR, IT = 32 / RPI, AT_ONCE = IT < 16 ? IT : 16;
     const int li = lane % LPR, sub = lane / LPR;
-    uint4 raw[IT];
+    float fac = a.scale_log2;
+    for (int i0 = 0; i0 < IT; i0 += AT_ONCE) {
+        uint4 raw[AT_ONCE];
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-        const int r = tile0 + row0 + i * RPI + sub;
-        raw[i] = make_uint4(0, 0, 0, 0);
-        if (r < s.n * a.group && 8 * li < a.d) {
-            const int t = a.by_group.div(r);
-            const uint16_t *x = static_cast<const uint16_t *>(a.Q) + (int64_t)(s.row0 + t) * a.q_token +
-                                (int64_t)(h * a.group + r - t * a.group) * a.q_head + 8 * li;
-            if (a.q_wide) {
-                const uint2 u = *reinterpret_cast<const uint2 *>(x), v = *reinterpret_cast<const uint2 *>(x + 4);
-                raw[i] = make_uint4(u.x, u.y, v.x, v.y);
-            } else {
-                raw[i] = load8(x);
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int r = tile0 + row0 + (i0 + i) * RPI + sub;
+            raw[i] = make_uint4(0, 0, 0, 0);
+            if (r < s.n * a.group && 8 * li < a.d) {
+                const int t = a.by_group.div(r);
+                const uint16_t *x = static_cast<const uint16_t *>(a.Q) + (int64_t)(s.row0 + t) * a.q_token +
+                                    (int64_t)(h * a.group + r - t * a.group) * a.q_head + 8 * li;
+                if (a.q_wide) {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(x), v = *reinterpret_cast<const uint2 *>(x + 4);
+                    raw[i] = make_uint4(u.x, u.y, v.x, v.y);
+                } else {
+                    raw[i] = load8(x);
+                }
             }
         }
-    }
-    float fac = a.scale_log2;
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-        const int row = row0 + i * RPI + sub;
-        uint4 w = raw[i];
-        if (a.dtype == SKM_DTYPE_BF16) {
-            uint32_t top = 0;  // the largest |x| as bits
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int row = row0 + (i0 + i) * RPI + sub;
+            uint4 w = raw[i];
+            if (a.dtype == SKM_DTYPE_BF16) {
+                uint32_t top = 0;  // the largest |x| as bits
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) top = max(max(top, u[k] << 16 & 0x7fff0000u), u[k] & 0x7fff0000u);
+                for (int k = 0; k < 4; ++k) top = max(max(top, u[k] << 16 & 0x7fff0000u), u[k] & 0x7fff0000u);
 #pragma unroll
-            for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const uint32_t ex = top >> 23, e = ex > 253 ? 253 : ex;
-            const bool fine = ex > 0 && ex < 255;
-            const float mul = fine ? __uint_as_float((254 - e) << 23) : 1.0f, back = fine ? __uint_as_float(e << 23) : 1.0f;
-            w = make_uint4(bf16_f16(w.x, mul), bf16_f16(w.y, mul), bf16_f16(w.z, mul), bf16_f16(w.w, mul));
-            const float mine = __shfl_sync(0xffffffffu, back, (lane % RPI) * LPR);
-            if (lane / RPI == i) fac = mine * a.scale_log2;
+                for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const uint32_t ex = top >> 23, e = ex > 253 ? 253 : ex;
+                const bool fine = ex > 0 && ex < 255;
+                const float mul = fine ? __uint_as_float((254 - e) << 23) : 1.0f, back = fine ? __uint_as_float(e << 23) : 1.0f;
+                w = make_uint4(bf16_f16(w.x, mul), bf16_f16(w.y, mul), bf16_f16(w.z, mul), bf16_f16(w.w, mul));
+                const float mine = __shfl_sync(0xffffffffu, back, (lane % RPI) * LPR);
+                if (lane / RPI == i0 + i) fac = mine * a.scale_log2;
+            }
+            st_shared(tile + (li >> 3) * (QT * 128) + row * 128 + (((li & 7) ^ (row & 7)) << 4), w.x, w.y, w.z, w.w);
         }
-        st_shared(tile + (li >> 3) * (QT * 128) + row * 128 + (((li & 7) ^ (row & 7)) << 4), w.x, w.y, w.z, w.w);
     }
     return fac;
 }
 
 template <int DH>
-__global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_constant__ KvAttnArgs a, int splits, float *parts) {
+__global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
+    kv_prompt_kernel(const __grid_constant__ KvAttnArgs a, int splits, float *parts) {
     using L = Lay<DH>;
+    constexpr int ST = L::ST, ROWS = L::ROWS, CONV_WARP0 = L::CONV_WARP0, MMA_WARP = L::MMA_WARP, THREADS = L::THREADS;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t *smem = smem_raw + ((1024 - (su32(smem_raw) & 1023)) & 1023);  // swizzle atoms
@@ -265,10 +274,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
     volatile int32_t *gone = reinterpret_cast<volatile int32_t *>(smem + L::slots + 4);
     float4 *info = reinterpret_cast<float4 *>(smem + L::info);  // a block's value_scale, its log2 -infinity where the block is absent
 
-    // the unit: a sequence's pair of row tiles, longest first (few pairs are ranked by
+    // the unit: ROWS rows of a sequence, longest first (few units are ranked by
     // the key tiles they see; of many, the later rows come first), its heads next
     // to each other
-    const int tiles = (a.max_tiles + 1) / 2, pairs = a.nb * tiles;
+    const int tiles = a.max_tiles, pairs = a.nb * tiles;
     int u = blockIdx.x;
     const int split = u % splits;
     u /= splits;
@@ -278,7 +287,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         int *length = reinterpret_cast<int *>(smem), *pick = length + RANKED;
         if (tid < pairs) {
             const Seq s = seq_of(a, a.b0 + tid / tiles);
-            const int r0 = tid % tiles * 2 * QT, r1 = min(r0 + 2 * QT, s.n * a.group) - 1;
+            const int r0 = tid % tiles * ROWS, r1 = min(r0 + ROWS, s.n * a.group) - 1;
             length[tid] = r1 < r0 ? -1 : last_of(a, s, r1) / KT - first_of(a, s, r0) / KT;
         }
         __syncthreads();
@@ -297,9 +306,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
     int64_t *part_index = reinterpret_cast<int64_t *>(smem + L::slots + 8);
     if (tid == 0) *part_index = ((int64_t)u * a.heads + h) * splits + split;
     const Seq s = seq_of(a, b);
-    const int rows = s.n * a.group, r0 = pair * 2 * QT;
+    const int rows = s.n * a.group, r0 = pair * ROWS;
     if (r0 >= rows) return;
-    const int r1 = min(r0 + 2 * QT, rows) - 1;
+    const int r1 = min(r0 + ROWS, rows) - 1;
     const int nq = r1 - r0 >= QT ? 2 : 1;
     // positions that some row sees, the tiles of them, this split's tiles
     const int first = first_of(a, s, r0), last = last_of(a, s, r1);
@@ -314,7 +323,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(k_free(i)), "r"(1) : "memory");
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(v_free(i)), "r"(1) : "memory");
         }
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < L::NQ; ++q) {
             for (int i = 0; i < 2; ++i) {
                 asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(s_full(q, i)), "r"(1) : "memory");
                 asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(p_full(q, i)), "r"(4) : "memory");
@@ -322,7 +331,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(o_done(q)), "r"(1) : "memory");
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(o_last(q)), "r"(1) : "memory");
         }
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(q_full), "r"(8) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(q_full), "r"(4 * L::NQ) : "memory");
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(drain), "r"(1) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *gone = 0;
@@ -348,12 +357,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
         fence_async();
         __syncwarp();
         if (lane == 0) arrive(q_full);
-        const int hi = in ? last_of(a, s, r) : -1, lo = in ? first_of(a, s, r) : 0;
+        // (rows past the end see everything, with no weight: they slow no one down)
+        const int hi = in ? last_of(a, s, r) : 0x7fffffff, lo = in ? first_of(a, s, r) : 0;
         // rows of the warp see [low, high] whole
         const int high = __shfl_sync(0xffffffffu, hi, 0), low = __reduce_max_sync(0xffffffffu, lo);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t S0 = tmem + lanes + q * 2 * KT, O = tmem + lanes + L::O + q * DH;
-        float m = M_NONE, l = 0.0f;
+        float m = in ? M_NONE : -M_NONE, l = 0.0f;
         bool ok = true, loaded = false;  // loaded: v[0] holds (or will) the first logits of tile j
         uint32_t v[2][16];
         for (int j = 0; j < n && q < nq; ++j) {
@@ -472,7 +482,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                 l = NAN;
                 if (lane == 0 && a.status) *a.status = 1;
             }
-            float *part = parts ? parts + *part_index * prompt_part(a.d) : nullptr;
+            float *part = parts ? parts + *part_index * prompt_part(ROWS, a.d) : nullptr;
             const int pr = q * QT + row;
             if (part) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);
             const int64_t at = in ? row_index(a, s, h, r) : 0;
@@ -491,7 +501,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
                 }
                 if (!in) continue;
                 if (part) {
-                    float4 *dst = reinterpret_cast<float4 *>(part + 4 * QT + (int64_t)pr * a.d + 16 * k);
+                    float4 *dst = reinterpret_cast<float4 *>(part + 2 * ROWS + (int64_t)pr * a.d + 16 * k);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         dst[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
@@ -668,29 +678,30 @@ __global__ void __launch_bounds__(THREADS, 1) kv_prompt_kernel(const __grid_cons
 }
 
 // A CTA takes 8 rows of a unit; the threads of a row its dims.
-__global__ void __launch_bounds__(256) kv_prompt_join_kernel(const __grid_constant__ KvAttnArgs a, int splits, const float *parts) {
+__global__ void __launch_bounds__(256) kv_prompt_join_kernel(const __grid_constant__ KvAttnArgs a, int splits, int unit_rows,
+                                                             const float *parts) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int tiles = (a.max_tiles + 1) / 2;
-    const int unit = blockIdx.x / (2 * QT / 8), pr = blockIdx.x % (2 * QT / 8) * 8 + (threadIdx.x >> 5);
+    const int tiles = a.max_tiles;
+    const int unit = blockIdx.x / (unit_rows / 8), pr = blockIdx.x % (unit_rows / 8) * 8 + (threadIdx.x >> 5);
     const int h = a.by_heads.mod(unit), u = a.by_heads.div(unit);
-    const int b = a.b0 + u / tiles, r = u % tiles * 2 * QT + pr;
+    const int b = a.b0 + u / tiles, r = u % tiles * unit_rows + pr;
     const Seq s = seq_of(a, b);
     if (r >= s.n * a.group) return;
-    const float *base = parts + (int64_t)unit * splits * prompt_part(a.d);
+    const float *base = parts + (int64_t)unit * splits * prompt_part(unit_rows, a.d);
     float m = M_NONE, l = 0.0f;
-    for (int i = 0; i < splits; ++i) m = fmaxf(m, base[i * prompt_part(a.d) + 2 * pr]);
+    for (int i = 0; i < splits; ++i) m = fmaxf(m, base[i * prompt_part(unit_rows, a.d) + 2 * pr]);
     const int64_t row = row_index(a, s, h, r);
     for (int i = 0; i < splits; ++i) {
-        const float *p = base + i * prompt_part(a.d) + 2 * pr;
+        const float *p = base + i * prompt_part(unit_rows, a.d) + 2 * pr;
         l = fmaf(p[1], exp2f(p[0] - m), l);
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     for (int c = threadIdx.x & 31; c < a.d / 4; c += 32) {
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         for (int i = 0; i < splits; ++i) {
-            const float *p = base + i * prompt_part(a.d);
+            const float *p = base + i * prompt_part(unit_rows, a.d);
             const float w = exp2f(p[2 * pr] - m);
-            const float4 v = *reinterpret_cast<const float4 *>(p + 4 * QT + (int64_t)pr * a.d + 4 * c);
+            const float4 v = *reinterpret_cast<const float4 *>(p + 2 * unit_rows + (int64_t)pr * a.d + 4 * c);
             o.x = fmaf(v.x, w, o.x), o.y = fmaf(v.y, w, o.y), o.z = fmaf(v.z, w, o.z), o.w = fmaf(v.w, w, o.w);
         }
         kv_store(a.out, row * a.d + 4 * c, o.x * inv, a.dtype);
@@ -705,12 +716,12 @@ template <int DH>
 cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
     static SmemLimit limit;
     cudaError_t e = limit.launch(kv_prompt_kernel<DH>, Lay<DH>::total, [&] {
-        kv_prompt_kernel<DH><<<(unsigned)(p.units * p.splits), THREADS, Lay<DH>::total, st>>>(
+        kv_prompt_kernel<DH><<<(unsigned)(p.units * p.splits), Lay<DH>::THREADS, Lay<DH>::total, st>>>(
             a, p.splits, p.splits > 1 ? a.part_cta : nullptr);
     });
     if (e != cudaSuccess || p.splits == 1) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.units * (2 * QT / 8)));
+    cfg.gridDim = dim3((unsigned)(p.units * (Lay<DH>::ROWS / 8)));
     cfg.blockDim = dim3(256);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
@@ -718,30 +729,31 @@ cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t 
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kv_prompt_join_kernel, a, p.splits, (const float *)a.part_cta);
+    e = cudaLaunchKernelEx(&cfg, kv_prompt_join_kernel, a, p.splits, Lay<DH>::ROWS, (const float *)a.part_cta);
     return e != cudaSuccess ? e : launched();
 }
 
 }  // namespace
 
-// 16-bit queries with d <= 128 and more rows a sequence than a warp tile of
-// k_kv_rows.cu holds
-bool kv_prompt_ok(int d, int dtype, int64_t rows) { return dtype != SKM_DTYPE_F32 && d <= 128 && rows > 32; }
+// 16-bit queries and more rows a sequence than a warp tile of k_kv_rows.cu
+// holds
+bool kv_prompt_ok(int dtype, int64_t rows) { return dtype != SKM_DTYPE_F32 && rows > 32; }
 
 KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens, int64_t span) {
     KvPromptPlan p = {};
-    p.max_tiles = (int)cdiv((int64_t)max_tokens * group, QT);
-    p.units = (int64_t)nb * heads * ((p.max_tiles + 1) / 2);
+    const int unit_rows = d <= 128 ? Lay<128>::ROWS : Lay<256>::ROWS;
+    p.max_tiles = (int)cdiv((int64_t)max_tokens * group, unit_rows);
+    p.units = (int64_t)nb * heads * p.max_tiles;
     p.splits = 1;
     // one CTA an SM: split the keys while CTAs are missing, 512 keys a split at least
     const int64_t room = KV_SMS / p.units, worth = span / 512;
     p.splits = (int)(room < 1 || worth < 1 ? 1 : (room < worth ? room : worth));
-    p.part = p.splits > 1 ? (size_t)p.units * p.splits * prompt_part(d) * 4 : 0;
+    p.part = p.splits > 1 ? (size_t)p.units * p.splits * prompt_part(unit_rows, d) * 4 : 0;
     return p;
 }
 
 cudaError_t launch_kv_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
-    return a.d <= 64 ? run_prompt<64>(a, p, st) : run_prompt<128>(a, p, st);
+    return a.d <= 64 ? run_prompt<64>(a, p, st) : a.d <= 128 ? run_prompt<128>(a, p, st) : run_prompt<256>(a, p, st);
 }
 
 }  // namespace skm

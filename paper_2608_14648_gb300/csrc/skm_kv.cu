@@ -116,7 +116,7 @@ struct AttendPlan {
 AttendPlan plan_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, Carver &cv) {
     AttendPlan p;
     const int nb = std::min<int>(s->batch, KV_MAX_SEQS), group = a->heads_q / c->heads, most = most_tokens(s);
-    p.prompt = kv_prompt_ok(c->d, a->dtype, (int64_t)most * group);
+    p.prompt = kv_prompt_ok(a->dtype, (int64_t)most * group);
     if (p.prompt) {
         p.many = kv_prompt_plan(nb, c->heads, group, c->d, most, span_of(c, s, a));
         if (p.many.part) p.part_cta = cv.take<float>(p.many.part / 4);
@@ -236,7 +236,7 @@ int skm_kv_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn
         k.nb = std::min(s->batch - k.b0, KV_MAX_SEQS);
         if (p.prompt) {
             KvPromptPlan q = p.many;
-            q.units = (int64_t)k.nb * k.heads * ((k.max_tiles + 1) / 2);
+            q.units = (int64_t)k.nb * k.heads * k.max_tiles;
             SKM_CUDA_TRY(launch_kv_prompt(k, q, S(stream)));
         } else {
             KvRowsPlan q = p.rows;

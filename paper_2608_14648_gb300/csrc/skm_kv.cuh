@@ -78,13 +78,13 @@ struct KvRowsPlan {
 KvRowsPlan kv_rows_plan(int nb, int heads, int group, int d, int dtype, int max_tokens, int64_t span);
 cudaError_t launch_kv_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st);
 
-// Many rows on tcgen05 (k_kv_prompt.cu): max_tiles in tiles of 128 rows, units of 256
+// Many rows on tcgen05 (k_kv_prompt.cu): max_tiles in units of a CTA's rows
 struct KvPromptPlan {
     int max_tiles, splits;
     int64_t units;
     size_t part;  // bytes
 };
-bool kv_prompt_ok(int d, int dtype, int64_t rows);
+bool kv_prompt_ok(int dtype, int64_t rows);
 KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens, int64_t span);
 cudaError_t launch_kv_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st);
 

@@ -357,6 +357,10 @@ ATTENDS = [
     (2, 2, 96, 32, "bf16", [(40, 200)]),
     (1, 5, 80, 16, "f16", [(1, 77), (64, 64)]),
     (1, 2, 256, 64, "bf16", [(10, 90)]),
+    (2, 3, 192, 32, "bf16", [(70, 150), (0, 33)]),
+    (1, 4, 256, 128, "f16", [(300, 260), (1, 7)]),
+    (1, 2, 144, 16, "f16", [(20, 60)]),
+    (1, 8, 16, 16, "bf16", [(60, 40), (0, 1)]),
 ]
 
 
