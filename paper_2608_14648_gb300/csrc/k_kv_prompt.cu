@@ -274,8 +274,8 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     volatile int32_t *gone = reinterpret_cast<volatile int32_t *>(smem + L::slots + 4);
     float4 *info = reinterpret_cast<float4 *>(smem + L::info);  // a block's value_scale, its log2 -infinity where the block is absent
 
-    // the unit: ROWS rows of a sequence, longest first (few units are ranked by
-    // the key tiles they see; of many, the later rows come first), its heads next
+    // the unit: ROWS rows of a sequence, longest first where there is more than one a
+    // SM (few units are ranked by the key tiles they see; of many, the later rows come first), its heads next
     // to each other
     const int tiles = a.max_tiles, pairs = a.nb * tiles;
     int u = blockIdx.x;
@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     u /= splits;
     const int h = a.by_heads.mod(u);
     u = a.by_heads.div(u);
-    if (pairs <= RANKED) {
+    if (pairs <= RANKED && gridDim.x > KV_SMS) {
         int *length = reinterpret_cast<int *>(smem), *pick = length + RANKED;
         if (tid < pairs) {
             const Seq s = seq_of(a, a.b0 + tid / tiles);
@@ -487,7 +487,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             if (part) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);
             const int64_t at = in ? row_index(a, s, h, r) : 0;
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll 1
+#pragma unroll 2
             for (int k = 0; k < DH / 16; ++k) {
                 if (16 * k >= a.d) break;
                 uint32_t v[16];
@@ -745,8 +745,9 @@ KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens,
     p.max_tiles = (int)cdiv((int64_t)max_tokens * group, unit_rows);
     p.units = (int64_t)nb * heads * p.max_tiles;
     p.splits = 1;
-    // one CTA an SM: split the keys while CTAs are missing, 512 keys a split at least
-    const int64_t room = KV_SMS / p.units, worth = span / 512;
+    // one CTA an SM: split the keys while CTAs are missing, 320 keys a split at least
+    // (a second kernel joins the parts: with 256, 96 rows that see 512 keys took 21 us instead of 17)
+    const int64_t room = KV_SMS / p.units, worth = span / 320;
     p.splits = (int)(room < 1 || worth < 1 ? 1 : (room < worth ? room : worth));
     p.part = p.splits > 1 ? (size_t)p.units * p.splits * prompt_part(unit_rows, d) * 4 : 0;
     return p;
