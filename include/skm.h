@@ -835,7 +835,9 @@ int skm_kv_read(const skm_kv_cache *c, const skm_kv_seqs *s, int dtype, void *K,
  *  status: device int32 or NULL; set to 1 when a bounded device wait gave up
  *  (some rows are then NaN or not written), otherwise left alone.
  *  ws: skm_kv_attend_workspace_size(c, s, a) bytes, 256-byte aligned (0 bytes: may be
- *  NULL; it returns (size_t)-1 with skm_last_error() set for invalid arguments).
+ *  NULL; it returns (size_t)-1 with skm_last_error() set for invalid arguments): at
+ *  most 26 MB, and enough for every call with the same heads, d, heads_q and dtype and
+ *  no larger batch, tokens, max_tokens and max_len.
  * The result does not depend on timing.  Asynchronous. */
 typedef struct skm_kv_attn {
     int32_t heads_q;   /* a multiple of the cache's heads */

@@ -869,13 +869,12 @@ def _kv_ws_bytes(cache, s, a):
     return n
 
 
-def kv_workspace(cache: KVCache, batch, heads_q, tokens, max_tokens, max_len, dtype=DTYPE_BF16, cols=None, causal=True,
-                 window=0):
-    """A workspace for skm_kv_attend calls of these sizes."""
+def kv_workspace(cache: KVCache, batch, heads_q, tokens, max_tokens, max_len, dtype=DTYPE_BF16, cols=None):
+    """A workspace for skm_kv_attend calls of at most these sizes."""
     cols = -(-max_len // cache.page) if cols is None else cols
     dummy = cache.k.data_ptr()
     s = _KV_SEQS.pack(batch, max(cols, 1), dummy, dummy, dummy, tokens, max_tokens, max_len)
-    a = _KV_ATTN.pack(heads_q, dtype, bool(causal), window, 1.0, 0, 0, 0, 0, 0, 0, 0)
+    a = _KV_ATTN.pack(heads_q, dtype, 1, 0, 1.0, 0, 0, 0, 0, 0, 0, 0)
     return _ws(_kv_ws_bytes(cache, s, a), cache.device)
 
 

@@ -739,15 +739,22 @@ cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t 
 // holds
 bool kv_prompt_ok(int dtype, int64_t rows) { return dtype != SKM_DTYPE_F32 && rows > 32; }
 
+// Keys a split has at least: a second kernel joins the parts (with 256, 96 rows that
+// see 512 keys took 21 us instead of 17; with 512, 40 rows that see 1045 32 instead of 28)
+constexpr int64_t SPLIT_KEYS = 320;
+
+size_t kv_prompt_part_most(int d, int64_t span) {
+    return span < 2 * SPLIT_KEYS ? 0 : (size_t)KV_SMS * prompt_part(d <= 128 ? Lay<128>::ROWS : Lay<256>::ROWS, d) * 4;
+}
+
 KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens, int64_t span) {
     KvPromptPlan p = {};
     const int unit_rows = d <= 128 ? Lay<128>::ROWS : Lay<256>::ROWS;
     p.max_tiles = (int)cdiv((int64_t)max_tokens * group, unit_rows);
     p.units = (int64_t)nb * heads * p.max_tiles;
     p.splits = 1;
-    // one CTA an SM: split the keys while CTAs are missing, 320 keys a split at least
-    // (a second kernel joins the parts: with 256, 96 rows that see 512 keys took 21 us instead of 17)
-    const int64_t room = KV_SMS / p.units, worth = span / 320;
+    // one CTA an SM: split the keys while CTAs are missing
+    const int64_t room = KV_SMS / p.units, worth = span / SPLIT_KEYS;
     p.splits = (int)(room < 1 || worth < 1 ? 1 : (room < worth ? room : worth));
     p.part = p.splits > 1 ? (size_t)p.units * p.splits * prompt_part(unit_rows, d) * 4 : 0;
     return p;

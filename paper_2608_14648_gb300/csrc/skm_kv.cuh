@@ -86,6 +86,8 @@ struct KvPromptPlan {
 };
 bool kv_prompt_ok(int dtype, int64_t rows);
 KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens, int64_t span);
+// workspace of any call of this d and span at most
+size_t kv_prompt_part_most(int d, int64_t span);
 cudaError_t launch_kv_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st);
 
 // A kernel's shared-memory limit, raised once a device: the call costs a

@@ -123,3 +123,25 @@ def test_binding_checks_its_tensors(skm):
         skm.skm_kv_attend(c, table, pos, cu, torch.zeros(3, 4, 32), 3, 10)
     with pytest.raises(ValueError):
         skm.skm_kv_attend(c, table, pos, cu, K, 3, 10, out=K.half())
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_a_workspace_serves_smaller_calls(skm, d, dtype):
+    # each call is stopped by an injected refusal, whose message says what it needs
+    c = cache(skm, d=d, pages=100000)
+    need_of = skm.lib().skm_kv_attend_workspace_size
+    for group, batch, most, length in [(1, 1, 1, 5000), (1, 40, 3, 700), (8, 3, 2, 90000), (4, 9, 60, 640), (2, 7, 900, 20000)]:
+        sizes = dict(cols=100000, tokens=batch * most)
+        a = attn(skm, heads_q=2 * group, dtype=dtype)
+        need = need_of(ctypes.byref(c), ctypes.byref(seqs(skm, batch=batch, max_tokens=most, max_len=length, **sizes)), ctypes.byref(a))
+        for b in {1, 2, batch // 2, batch - 1, batch} & set(range(1, batch + 1)):
+            for m in {1, 2, 4, 8, 16, 17, 33, most // 2, most} & set(range(1, most + 1)):
+                for n in {1, 600, 641, 2048, 2049, length // 2, length} & set(range(length + 1)):
+                    for window in (0, 50, 2500):
+                        smaller = seqs(skm, batch=b, max_tokens=m, max_len=n, **sizes)
+                        skm.skm_inject_fault(skm.FAULT_WORKSPACE, 1)
+                        rc = call(skm, "attend", c, smaller, attn(skm, heads_q=2 * group, dtype=dtype, window=window))
+                        skm.skm_inject_fault(skm.FAULT_WORKSPACE, 0)
+                        text = skm.lib().skm_last_error().decode()
+                        assert rc == NO_MEMORY and int(text.split(",")[1].split()[0]) <= need, (b, m, n, window, text, need)
