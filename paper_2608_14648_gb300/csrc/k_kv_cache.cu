@@ -199,12 +199,12 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(const __grid_const
     const int b = at_block.b;
     if (b >= a.batch) return;
     const int2 rows = kv_rows_of(a.cu, b, a.tokens, a.max_tokens);
-    const int start = max(a.pos[b], 0);
     const int cap = a.cols * a.page;
+    const int start = kv_clamp(a.pos[b], 0, cap);  // (from cap on there is nothing, and block positions stay below 2^31)
     const int end = (int)min((int64_t)start + rows.y, (int64_t)cap);
     const int blk = start / KV_B + at_block.i;
     const int t0 = blk * KV_B;
-    if (t0 >= end) return;
+    if (t0 >= end || rows.y == 0) return;  // (without rows: its page may be another's by now)
     const int pg = a.table[(int64_t)b * a.cols + a.by_bpp.div(blk)];  // looked at once the input is on its way
     const int nc = a.d / KV_B;
     const KvTokens src = tensor ? a.V : a.K;

@@ -477,3 +477,38 @@ def test_on_another_stream_and_in_a_graph(cuda_ok):
     torch.cuda.synchronize()
     want, _ = skm.skm_kv_attend(c, table, length, cu, Q, 1, 4800)
     assert torch.equal(out, want)
+
+
+def test_write_of_a_sequence_without_rows_touches_nothing(cuda_ok):
+    # 40 sequences: the even ones have no rows, and table rows that name pages of the odd ones
+    import paper_2608_14648_gb300 as skm
+
+    g = torch.Generator().manual_seed(5)
+    for _ in range(5):
+        c = make_cache(2, 64, 16, 40)
+        table = torch.arange(40, dtype=torch.int32).view(40, 1)
+        table[0::2] = table[1::2]
+        n = [b % 2 * 3 for b in range(40)]
+        cu = [0] + torch.tensor(n).cumsum(0).tolist()
+        start = [5 + b % 7 for b in range(40)]
+        K, V = torch.randn(2, cu[-1], 2, 64, generator=g)
+        want = Held(c)
+        odd = [cu[b] for b in range(1, 40, 2)] + [cu[-1]]
+        want.write(table[1::2], start[1::2], odd, K, V)
+        skm.skm_kv_write(c, table.cuda(), i32(start), i32(cu), K.cuda(), V.cuda(), 3)
+        same(c, want)
+
+
+@pytest.mark.parametrize("start", [64, 80, 2**31 - 1, 2**31 - 40, -2**31])
+def test_write_beyond_the_table(cuda_ok, start):
+    # nothing at or past cols * page = 64; a negative position counts as 0
+    import paper_2608_14648_gb300 as skm
+
+    c = make_cache(1, 32, 32, 3)
+    want = Held(c)
+    table = torch.tensor([[2, 0]], dtype=torch.int32)
+    K, V = torch.randn(2, 100, 1, 32, generator=torch.Generator().manual_seed(6))
+    if start < 0:
+        want.write(table, [0], [0, 100], K, V)
+    skm.skm_kv_write(c, table.cuda(), i32([start]), i32([0, 100]), K.cuda(), V.cuda(), 100)
+    same(c, want)
