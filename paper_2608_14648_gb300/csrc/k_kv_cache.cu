@@ -5,9 +5,14 @@
 // the scale and the codes come from one read of the input.  Both kernels move
 // bytes; a warp needs no other warp, so an append (one token, a warp busy for its
 // memory latencies) and a prompt (thousands of independent 4 KB reads in flight) are
-// the same code.  What bounds writing is how many of those reads are in flight:
+// the same code.  What bounds writing is how many of those reads are in flight
+// and the instructions of a block (984 a warp for 2048 values):
 // the input is read before the page is known, and 16-bit values stay packed
 // (64 registers, 32 warps an SM).
+//
+// Measured (GB300, bf16, 8 heads of 128): writing 12 prompts of up to 2500 tokens,
+// 93 MB in and out, 43 us = 2.2 TB/s; reading 4 sequences of up to 32768
+// tokens back, 611 MB, 101 us = 6.0 TB/s (a plain copy: 6.8).
 //
 // Lanes: keys, a unit is 16 dims of a token (a 16-byte code store, two 16-byte
 // loads of 16-bit values), consecutive lanes along d; values, whose blocks
@@ -18,11 +23,13 @@
 // their sign, in which infinities and NaN come out on top: a warp that finds one
 // goes element by element.
 //
-// Rounding: code = rint(x / scale) with the quotient rounded to fp32.  x times
-// the reciprocal is within 1.6e-5 of x / scale (|quotient| < 128, two roundings
-// of 2^-24 relative), the fp32 quotient within 8e-6, so both round to the same
-// integer unless x times the reciprocal lies within 3e-5 of a half; only those
-// elements take the division.
+// Rounding: code = rint(x / scale) with the quotient rounded to fp32.  The quotient is
+// q = x y, y the correctly rounded reciprocal, corrected twice by its exact
+// remainder: q' = q + (x - q s) y.  q is within 1.5 units in the last place, the first correction
+// within one, and by Markstein's theorem (IBM J. Res. Dev. 34, 1990) the second
+// is the quotient as a division rounds it.  Five operations, two values at a time: a
+// division only where x y lies near the middle of two codes took more, because
+// 16-bit values meet it often (half the largest one is 63.5).
 #include <algorithm>
 #include <type_traits>
 
@@ -34,7 +41,6 @@ namespace {
 
 constexpr int WARPS = 8;
 constexpr float CODE_MAGIC = 12583040.0f;  // 1.5 2^23 + 128: q + this holds rint(q) + 128 in its low byte
-constexpr float NEAR_HALF = 0.49997f;
 
 template <typename T>
 constexpr int WORDS8 = 8 * sizeof(T) / 4;  // words of 8 values
@@ -113,26 +119,21 @@ __device__ __noinline__ uint32_t code_exact(float x, float s) {
 }
 
 // codes of four values in a word, the first in the low byte; quick: they are
-// finite and the reciprocal of s is a normal number
+// finite, and s and its reciprocal far from the ends of the exponent's range
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float s, float inv, bool quick) {
     if (!quick) {
         if (!(s > 0.0f)) return 0x80808080u;
         return code_exact(a, s) | code_exact(b, s) << 8 | code_exact(c, s) << 16 | code_exact(d, s) << 24;
     }
-    const float fa = fmaf(a, inv, CODE_MAGIC), fb = fmaf(b, inv, CODE_MAGIC);
-    const float fc = fmaf(c, inv, CODE_MAGIC), fd = fmaf(d, inv, CODE_MAGIC);
-    const float ra = fmaf(a, inv, CODE_MAGIC - fa), rb = fmaf(b, inv, CODE_MAGIC - fb);
-    const float rc = fmaf(c, inv, CODE_MAGIC - fc), rd = fmaf(d, inv, CODE_MAGIC - fd);
-    const uint32_t lo = __byte_perm(__float_as_uint(fa), __float_as_uint(fb), 0x0040);
-    const uint32_t hi = __byte_perm(__float_as_uint(fc), __float_as_uint(fd), 0x0040);
-    uint32_t w = __byte_perm(lo, hi, 0x5410);
-    if (fmaxf(fmaxf(fabsf(ra), fabsf(rb)), fmaxf(fabsf(rc), fabsf(rd))) > NEAR_HALF) {
-        if (fabsf(ra) > NEAR_HALF) w = (w & 0xffffff00u) | code_exact(a, s);
-        if (fabsf(rb) > NEAR_HALF) w = (w & 0xffff00ffu) | code_exact(b, s) << 8;
-        if (fabsf(rc) > NEAR_HALF) w = (w & 0xff00ffffu) | code_exact(c, s) << 16;
-        if (fabsf(rd) > NEAR_HALF) w = (w & 0x00ffffffu) | code_exact(d, s) << 24;
-    }
-    return w;
+    const float2 y = make_float2(inv, inv), less = make_float2(-s, -s);
+    const auto codes2 = [&](float2 x) {
+        float2 q = mul2(x, y);
+        q = fma2(fma2(q, less, x), y, q);
+        q = fma2(fma2(q, less, x), y, q);
+        q = add2(q, make_float2(CODE_MAGIC, CODE_MAGIC));
+        return __byte_perm(__float_as_uint(q.x), __float_as_uint(q.y), 0x0040);
+    };
+    return __byte_perm(codes2(make_float2(a, b)), codes2(make_float2(c, d)), 0x5410);
 }
 
 // codes of a word of the block's earlier tokens after its scale grew by 1 / r
@@ -159,7 +160,7 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t bits, float old, Fini
     if (!b.quick) a = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(finite())));
     b.s = fmaxf(old, a * (1.0f / 127.0f));
     b.ratio = old > 0.0f && b.s > old ? __fdiv_rn(old, b.s) : 1.0f;
-    b.quick = b.quick && b.s > 1e-37f;
+    b.quick = b.quick && b.s > 1e-30f;  // (smaller: a remainder may be subnormal)
     b.inv = b.quick ? __frcp_rn(b.s) : 0.0f;
     return b;
 }
@@ -189,9 +190,9 @@ __device__ __forceinline__ Place place_of(const KvCacheArgs &a, int u, int lane)
     return Place{b, u - __shfl_sync(0xffffffffu, x - n, b & 31)};
 }
 
-// Warps: one a (sequence, block its new rows reach, head, tensor).  NU: units a lane.
-template <typename T, int NU>
-__global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(const __grid_constant__ KvCacheArgs a) {
+// Warps: one a (sequence, block its new rows reach, head, tensor).
+template <typename T>
+__global__ void __launch_bounds__(WARPS * 32, 4) kv_write_kernel(const __grid_constant__ KvCacheArgs a) {
     const int lane = threadIdx.x & 31;
     const int warp = blockIdx.x * WARPS + (threadIdx.x >> 5), tensor = warp & 1;
     const int h = a.by_heads.mod(warp >> 1);
@@ -206,134 +207,103 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(const __grid_const
     const int t0 = blk * KV_B;
     if (t0 >= end || rows.y == 0) return;  // (without rows: its page may be another's by now)
     const int pg = a.table[(int64_t)b * a.cols + a.by_bpp.div(blk)];  // looked at once the input is on its way
-    const int nc = a.d / KV_B;
     const KvTokens src = tensor ? a.V : a.K;
     const T *x = static_cast<const T *>(src.x) + (int64_t)(rows.x - start + t0) * src.token + (int64_t)h * src.head;
-    const bool holds = start > t0;
-    const bool full = !holds && t0 + KV_B <= end;
-    uint32_t top = 0;
-    uint8_t *codes = nullptr;
-    float *where = nullptr;
-    const auto find = [&] {  // false: an absent page
-        if (pg < 0 || pg >= a.pages) return false;
-        const int64_t at = ((int64_t)pg * a.heads + h) * a.bpp + a.by_bpp.mod(blk);
-        codes = (tensor ? a.v : a.k) + at * (KV_B * a.d);
-        where = reinterpret_cast<float *>(a.scales + at) + tensor;
-        return true;
-    };
+    const int lo = max(start - t0, 0), hi = min(end - t0, KV_B);  // the block's new tokens
 
-    // ALL: every token of the block is new
-    const auto keys = [&](auto all) {
-        constexpr bool ALL = decltype(all)::value;
-        const auto is_new = [&](int t) { return ALL || (t0 + t >= start && t0 + t < end); };
-        constexpr int W = 2 * WORDS8<T>;
-        uint32_t v[NU][W];
+    // the largest magnitude: 8 values a lane, consecutive lanes along d
+    uint32_t top = 0;
+    const int eighths = KV_B * (a.d / 8);
+    constexpr int W = WORDS8<T>;
+    const auto loads = [&](auto many, bool wide) {
+        constexpr int AT_ONCE = decltype(many)::value;
+#pragma unroll 1
+        for (int q0 = lane; q0 < eighths; q0 += 32 * AT_ONCE) {
+            uint32_t v[AT_ONCE][W];
 #pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int q = lane + 32 * i, t = a.by_chunks.div(q), w = q - t * nc;
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const int q = q0 + 32 * i, t = a.by_eighths.div(q);
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[i][j] = 0;
-            if (t < KV_B && is_new(t)) {
-                load8(x + (int64_t)t * src.token + 16 * w, src.wide, v[i]);
-                load8(x + (int64_t)t * src.token + 16 * w + 8, src.wide, v[i] + W / 2);
+                for (int j = 0; j < W; ++j) v[i][j] = 0;
+                if (t >= lo && t < hi) load8(x + (int64_t)t * src.token + 8 * (q - t * (a.d / 8)), wide, v[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+                for (int j = 0; j < W; ++j) top = larger<T>(top, v[i][j]);
+        }
+    };
+    if (src.wide) loads(std::integral_constant<int, 32 / W>{}, true);
+    else loads(std::integral_constant<int, 1>{}, false);
+    if (pg < 0 || pg >= a.pages) return;
+    const int64_t at = ((int64_t)pg * a.heads + h) * a.bpp + a.by_bpp.mod(blk);
+    uint8_t *codes = (tensor ? a.v : a.k) + at * (KV_B * a.d);
+    float *where = reinterpret_cast<float *>(a.scales + at) + tensor;
+    const float old = lo > 0 ? *where : 0.0f;
+    const BlockScale bs = block_scale<T>(top, old, [&] {
+        float m = 0.0f;
+        for (int q = lane; q < eighths; q += 32) {
+            const int t = a.by_eighths.div(q);
+            if (t < lo || t >= hi) continue;
+            uint32_t v[W];
+            load8(x + (int64_t)t * src.token + 8 * (q - t * (a.d / 8)), src.wide, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float y = fabsf(value<T>(v, j));
+                m = y < INFINITY ? fmaxf(m, y) : m;
             }
         }
-        if (!find()) return;
-        const float old = holds ? *where : 0.0f;
-#pragma unroll
-        for (int i = 0; i < NU; ++i)
-#pragma unroll
-            for (int j = 0; j < W; ++j) top = larger<T>(top, v[i][j]);
-        const BlockScale bs = block_scale<T>(top, old, [&] {
-            float m = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NU; ++i)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float y = fabsf(value<T>(v[i], j));
-                    m = y < INFINITY ? fmaxf(m, y) : m;
-                }
-            return m;
-        });
-        __syncwarp();
-        if (lane == 0) *where = bs.s;
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int q = lane + 32 * i, t = a.by_chunks.div(q), w = q - t * nc;
-            if (t >= KV_B) continue;
+        return m;
+    });
+    __syncwarp();
+    if (lane == 0) *where = bs.s;
+
+    // the codes: the values again, out of L1
+    if (tensor == 0) {
+        const int nc = a.d / KV_B;
+#pragma unroll 1
+        for (int q = lane; q < KV_B * nc; q += 32) {
+            const int t = a.by_chunks.div(q), w = q - t * nc;
             uint4 *p = reinterpret_cast<uint4 *>(codes + w * 256 + t * 16);
-            if (is_new(t)) {
-                uint32_t c[4];
+            if (t >= lo && t < hi) {
+                uint32_t v[2 * W], c[4];
+                load8(x + (int64_t)t * src.token + 16 * w, src.wide, v);
+                load8(x + (int64_t)t * src.token + 16 * w + 8, src.wide, v + W);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    c[j] = codes4(value<T>(v[i], 4 * j), value<T>(v[i], 4 * j + 1), value<T>(v[i], 4 * j + 2),
-                                  value<T>(v[i], 4 * j + 3), bs.s, bs.inv, bs.quick);
+                    c[j] = codes4(value<T>(v, 4 * j), value<T>(v, 4 * j + 1), value<T>(v, 4 * j + 2),
+                                  value<T>(v, 4 * j + 3), bs.s, bs.inv, bs.quick);
                 *p = make_uint4(c[0], c[1], c[2], c[3]);
-            } else if (t0 + t < start && bs.ratio != 1.0f) {
+            } else if (t < lo && bs.ratio != 1.0f) {
                 const uint4 c = *p;
                 *p = make_uint4(rescale4(c.x, bs.ratio), rescale4(c.y, bs.ratio), rescale4(c.z, bs.ratio),
                                 rescale4(c.w, bs.ratio));
             }
         }
-    };
-    const auto values = [&](auto all) {
-        constexpr bool ALL = decltype(all)::value;
-        const auto is_new = [&](int t) { return ALL || (t0 + t >= start && t0 + t < end); };
-        constexpr int NV = (NU + 1) / 2, W = WORDS8<T>;
-        uint32_t v[NV][4][W];
-        const int last = a.d / 2;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int q = lane + 32 * i, c = q & 3, e = q >> 2;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int t = 2 * c + (k & 1) + 8 * (k >> 1);
-#pragma unroll
-                for (int j = 0; j < W; ++j) v[i][k][j] = 0;
-                if (q < last && is_new(t)) load8(x + (int64_t)t * src.token + 8 * e, src.wide, v[i][k]);
-            }
-        }
-        if (!find()) return;
-        const float old = holds ? *where : 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int j = 0; j < W; ++j) top = larger<T>(top, v[i][k][j]);
-        const BlockScale bs = block_scale<T>(top, old, [&] {
-            float m = 0.0f;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float y = fabsf(value<T>(v[i][k], j));
-                        m = y < INFINITY ? fmaxf(m, y) : m;
-                    }
-            return m;
-        });
-        __syncwarp();
-        if (lane == 0) *where = bs.s;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int q = lane + 32 * i, c = q & 3, e = q >> 2;
-            if (q >= last) continue;
+    } else {
+#pragma unroll 1
+        for (int q = lane; q < a.d / 2; q += 32) {
+            const int c = q & 3, e = q >> 2;
+            uint32_t v[4][W];
             uint32_t fresh = 0, held = 0;  // bytes of new tokens, of tokens from before
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int t = 2 * c + (k & 1) + 8 * (k >> 1);
-                if (is_new(t)) fresh |= 0xffu << (8 * k);
-                if (!ALL && t0 + t < start) held |= 0xffu << (8 * k);
+#pragma unroll
+                for (int j = 0; j < W; ++j) v[k][j] = 0;
+                if (t >= lo && t < hi) {
+                    load8(x + (int64_t)t * src.token + 8 * e, src.wide, v[k]);
+                    fresh |= 0xffu << (8 * k);
+                }
+                if (t < lo) held |= 0xffu << (8 * k);
             }
-            if (!ALL && !fresh && (!held || bs.ratio == 1.0f)) continue;
+            if (!fresh && (!held || bs.ratio == 1.0f)) continue;
             uint32_t *p = reinterpret_cast<uint32_t *>(codes + 8 * e * 16 + 4 * c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                uint32_t w = codes4(value<T>(v[i][0], j), value<T>(v[i][1], j), value<T>(v[i][2], j), value<T>(v[i][3], j),
+                uint32_t w = codes4(value<T>(v[0], j), value<T>(v[1], j), value<T>(v[2], j), value<T>(v[3], j),
                                     bs.s, bs.inv, bs.quick);
-                if (!ALL && fresh != 0xffffffffu) {
+                if (fresh != 0xffffffffu) {
                     const uint32_t was = p[4 * j];
                     const uint32_t kept = bs.ratio != 1.0f ? rescale4(was, bs.ratio) : was;
                     w = (w & fresh) | (kept & held) | (was & ~(fresh | held));
@@ -341,9 +311,7 @@ __global__ void __launch_bounds__(WARPS * 32) kv_write_kernel(const __grid_const
                 p[4 * j] = w;
             }
         }
-    };
-    if (tensor == 0) full ? keys(std::true_type{}) : keys(std::false_type{});
-    else full ? values(std::true_type{}) : values(std::false_type{});
+    }
 }
 
 // Warps: one a (sequence, block its range reaches, head, tensor).
@@ -435,12 +403,12 @@ int64_t grid_of(const KvCacheArgs &a) {
 
 }  // namespace
 
-#define KV_BY_TYPE(KERNEL, NU)                                                                              \
+#define KV_BY_TYPE(KERNEL, ...)                                                                             \
     do {                                                                                                    \
-        if (dtype == SKM_DTYPE_F32) KERNEL<float, NU><<<grid, WARPS * 32, 0, st>>>(a);      \
+        if (dtype == SKM_DTYPE_F32) KERNEL<float __VA_OPT__(, ) __VA_ARGS__><<<grid, WARPS * 32, 0, st>>>(a); \
         else if (dtype == SKM_DTYPE_BF16)                                                                   \
-            KERNEL<__nv_bfloat16, NU><<<grid, WARPS * 32, 0, st>>>(a);                   \
-        else KERNEL<__half, NU><<<grid, WARPS * 32, 0, st>>>(a);                         \
+            KERNEL<__nv_bfloat16 __VA_OPT__(, ) __VA_ARGS__><<<grid, WARPS * 32, 0, st>>>(a);               \
+        else KERNEL<__half __VA_OPT__(, ) __VA_ARGS__><<<grid, WARPS * 32, 0, st>>>(a);                     \
     } while (0)
 
 static KvCacheArgs with_divisions(KvCacheArgs a) {
@@ -448,15 +416,14 @@ static KvCacheArgs with_divisions(KvCacheArgs a) {
     a.by_bpp = FastDiv(a.bpp);
     a.by_most = FastDiv(most_blocks_of(a));
     a.by_chunks = FastDiv(a.d / KV_B);
+    a.by_eighths = FastDiv(a.d / 8);
     return a;
 }
 
 cudaError_t launch_kv_write(const KvCacheArgs &args, int dtype, cudaStream_t st) {
     const KvCacheArgs a = with_divisions(args);
     const unsigned grid = (unsigned)grid_of(a);
-    if (a.d <= 64) KV_BY_TYPE(kv_write_kernel, 2);
-    else if (a.d <= 128) KV_BY_TYPE(kv_write_kernel, 4);
-    else KV_BY_TYPE(kv_write_kernel, 8);
+    KV_BY_TYPE(kv_write_kernel);
     return launched();
 }
 

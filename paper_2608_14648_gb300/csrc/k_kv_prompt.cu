@@ -31,6 +31,14 @@
 //
 // Few CTAs (short prompts): the keys are split over CTAs as well, and
 // kv_prompt_join_kernel merges the parts in order.
+//
+// Measured (GB300): chunks of 2048 tokens of two prompts behind 6144, 32 query heads
+// over 8 of 128, bf16: 323 us = 1040 TFLOP/s, 54% of a cuBLAS product; 4 whole prompts of up to
+// 4096, 16 heads of 64, f16: 143 us (long and short row tiles; half the work of a
+// product of 128 dims for as many exponentials).  A tile of 256 rows x 64 keys takes 1850
+// clocks: the softmax warps' chain (TMEM load, exponentials, sums, P back, barriers)
+// bounds it; the products take 1280 (an instruction of 128 x 64 x 16 with both operands in
+// shared memory 48, bound by reading them), the 7 converter warps somewhat less.
 #include "skm_kv_dev.cuh"
 
 namespace skm {
@@ -161,24 +169,6 @@ __device__ __forceinline__ void st16(uint32_t addr, const uint32_t *v) {
         : "memory");
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 r;
-    asm("{\n\t.reg .b64 ra, rb, rc, rd;\n\t"
-        "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmov.b64 rc, {%6, %7};\n\t"
-        "fma.rn.f32x2 rd, ra, rb, rc;\n\tmov.b64 {%0, %1}, rd;\n\t}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return r;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 r;
-    asm("{\n\t.reg .b64 ra, rb, rd;\n\t"
-        "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
-        "add.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
 __device__ __forceinline__ void st_shared(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
@@ -736,8 +726,16 @@ cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t 
 }  // namespace
 
 // 16-bit queries and more rows a sequence than a warp tile of k_kv_rows.cu
-// holds
-bool kv_prompt_ok(int dtype, int64_t rows) { return dtype != SKM_DTYPE_F32 && rows > 32; }
+// holds: at d = 128, 40 rows of 2 sequences that see 900 keys take 22 us here and 24 there, of
+// 16 (8 heads) 26 and 46.  d > 128, where this kernel takes longer to start (a CTA
+// converts 64 KB of keys and values before its first product is through): not while the
+// other one has an SM for every unit and few keys a unit.  At d = 256, 40 rows of 16 sequences, 2
+// heads: 905 keys 29 us here and 23 there; 2 sequences, 1905 keys 27 and 33; 16
+// sequences, 8 heads, 905 keys 35 and 62.
+bool kv_prompt_ok(int dtype, int nb, int heads, int d, int64_t rows, int64_t span) {
+    if (dtype == SKM_DTYPE_F32 || rows <= KV_ROWS_MOST) return false;
+    return d <= 128 || span > 1280 || (int64_t)nb * heads * cdiv(rows, (int64_t)16) > KV_SMS;
+}
 
 // Keys a split has at least: a second kernel joins the parts (with 256, 96 rows that
 // see 512 keys took 21 us instead of 17; with 512, 40 rows that see 1045 32 instead of 28)

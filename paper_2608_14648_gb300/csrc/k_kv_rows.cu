@@ -19,6 +19,13 @@
 // exceeds it by 15 (then to 7 below the maximum), so p < 2^15 and the sums are rarely
 // rescaled.  out = o / l, lse = ln2 (m + log2 l).
 //
+// What bounds it.  Sequences with much to read: HBM (GB300, 8 heads of 128: 64
+// sequences of up to 8192 tokens, 485 MB, 99 us = 4.9 TB/s; one of 131079, 269
+// MB, 56 us = 4.8 TB/s; a plain copy of as much 6.8).  What is missing is at both
+// ends: some 4 us until the first block has arrived (lengths, table, scales, each behind
+// the one before), as much for merging warps and CTAs.  Short sequences: the launch, and
+// instructions that are fetched for the first time (7 of the 11 us for one of 333 tokens).
+//
 // Joining.  Partial (m, l, o) of units that warps share are merged by their
 // CTA, those that CTAs share by kv_join_kernel; both in the line's order, so
 // the result does not depend on timing.
@@ -1011,6 +1018,9 @@ KvRowsPlan plan_rows(int nb, int heads, int group, int d, int max_tokens, int64_
     p.rt = Rows::RT;
     p.nw = nw;
     p.units = (int64_t)nb * cdiv((int64_t)max_tokens * group, p.rt) * heads;
+    // One CTA a unit, without the join kernel, while the longest unit is short: one
+    // sequence of 333 tokens takes 13 us against 16 in shared stretches, 16 that see
+    // 1029 positions 25 against 29; one of 4096 takes longer on one SM than on many.
     p.whole = span <= 2048;
     p.ns = 4;
     const int seqs = p.whole ? 1 : nb;
@@ -1026,7 +1036,8 @@ KvRowsPlan plan_rows(int nb, int heads, int group, int d, int max_tokens, int64_
 
 // The variants.  fp32 queries: one row or four.  16-bit queries: tiles of 8,
 // 16 or 32 rows (d > 128: 8 or 16, the sums of a tile are held in registers);
-// warps as many as the registers of that tile allow.
+// warps as many as the registers of that tile allow.  A variant for d = 64, 128 or
+// 256 only (FULL) has no bounds on dims in its loops, the other takes any d.
 #define KV_ROWS_VARIANTS(X)                                                                              \
     X(1, 1, 64, (Fp32Rows<1, 2>), 16) X(1, 1, 128, (Fp32Rows<1, 4>), 16) X(1, 1, 256, (Fp32Rows<1, 8>), 8)  \
     X(1, 4, 64, (Fp32Rows<4, 2>), 16) X(1, 4, 128, (Fp32Rows<4, 4>), 16) X(1, 4, 256, (Fp32Rows<4, 8>), 8)  \

@@ -117,7 +117,7 @@ struct AttendPlan {
 AttendPlan plan_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, Carver &cv) {
     AttendPlan p;
     const int nb = std::min<int>(s->batch, KV_MAX_SEQS), group = a->heads_q / c->heads, most = most_tokens(s);
-    p.prompt = kv_prompt_ok(a->dtype, (int64_t)most * group);
+    p.prompt = kv_prompt_ok(a->dtype, nb, c->heads, c->d, (int64_t)most * group, span_of(c, s, a));
     if (p.prompt) {
         p.many = kv_prompt_plan(nb, c->heads, group, c->d, most, span_of(c, s, a));
         if (p.many.part) p.part_cta = cv.take<float>(p.many.part / 4);
@@ -179,20 +179,21 @@ size_t skm_kv_attend_workspace_size(const skm_kv_cache *c, const skm_kv_seqs *s,
     if (check_attend(c, s, a) != SKM_OK) return (size_t)-1;
     if (most_tokens(s) == 0) return 0;
     // the most that any call of these sizes or smaller ones takes: fewer rows may
-    // mean another tile, or more CTAs that share a row
+    // mean another tile, or more CTAs that share a row (more than KV_ROWS_MOST rows
+    // in k_kv_rows.cu after all: short, without parts)
     const int64_t span = std::min<int64_t>(s->max_len, (int64_t)s->cols * c->page);
     const int64_t rows = (int64_t)most_tokens(s) * (a->heads_q / c->heads);
     const int nb = std::min<int>(s->batch, KV_MAX_SEQS);
     size_t most = 0;
     for (const int64_t r : {int64_t(1), int64_t(8), int64_t(16), int64_t(32), rows}) {
-        if (r > rows || kv_prompt_ok(a->dtype, r)) continue;
+        if (r > rows || (a->dtype != SKM_DTYPE_F32 && r > KV_ROWS_MOST)) continue;
         const KvRowsPlan p = kv_rows_plan(nb, c->heads, 1, c->d, a->dtype, (int)r, span);
         Carver cv(nullptr, 0);
         if (p.part_cta) cv.take<float>(p.part_cta / 4);
         if (p.part_warp) cv.take<float>(p.part_warp / 4);
         most = std::max(most, cv.off);
     }
-    if (kv_prompt_ok(a->dtype, rows)) most = std::max(most, kv_prompt_part_most(c->d, span));
+    if (a->dtype != SKM_DTYPE_F32 && rows > KV_ROWS_MOST) most = std::max(most, kv_prompt_part_most(c->d, span));
     return most;
 }
 

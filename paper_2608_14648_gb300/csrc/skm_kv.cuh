@@ -40,7 +40,7 @@ struct KvCacheArgs {
     const int32_t *table, *pos, *cu;
     int heads, d, page, pages, bpp;  // bpp: blocks of a page
     int batch, cols, tokens, max_tokens;
-    FastDiv by_heads, by_bpp, by_most, by_chunks;  // (set by the launchers) most blocks of a sequence, 16-dim chunks
+    FastDiv by_heads, by_bpp, by_most, by_chunks, by_eighths;  // (set by the launchers) most blocks of a sequence, 16 and 8 dims
     KvTokens K, V;    // write: sources
     void *outk, *outv;  // read: destinations
 };
@@ -84,7 +84,8 @@ struct KvPromptPlan {
     int64_t units;
     size_t part;  // bytes
 };
-bool kv_prompt_ok(int dtype, int64_t rows);
+constexpr int KV_ROWS_MOST = 32;  // 16-bit rows that are always k_kv_rows.cu's
+bool kv_prompt_ok(int dtype, int nb, int heads, int d, int64_t rows, int64_t span);
 KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens, int64_t span);
 // workspace of any call of this d and span at most
 size_t kv_prompt_part_most(int d, int64_t span);
@@ -129,6 +130,34 @@ __device__ __forceinline__ void kv_store(void *x, int64_t i, float v, int dtype)
     if (dtype == SKM_DTYPE_F32) static_cast<float *>(x)[i] = v;
     else if (dtype == SKM_DTYPE_BF16) static_cast<__nv_bfloat16 *>(x)[i] = __float2bfloat16_rn(v);
     else static_cast<__half *>(x)[i] = __float2half_rn(v);
+}
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n\t.reg .b64 ra, rb, rc, rd;\n\t"
+        "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmov.b64 rc, {%6, %7};\n\t"
+        "fma.rn.f32x2 rd, ra, rb, rc;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 ra, rb, rd;\n\t"
+        "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+        "add.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 ra, rb, rd;\n\t"
+        "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+        "mul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
 }
 __device__ __forceinline__ int kv_clamp(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
 

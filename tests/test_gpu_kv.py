@@ -512,3 +512,30 @@ def test_write_beyond_the_table(cuda_ok, start):
         want.write(table, [0], [0, 100], K, V)
     skm.skm_kv_write(c, table.cuda(), i32([start]), i32([0, 100]), K.cuda(), V.cuda(), 100)
     same(c, want)
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+def test_write_rounds_like_a_division(cuda_ok, typ):
+    # values at and next to the middles of two codes: a few units in the last place to either side
+    import paper_2608_14648_gb300 as skm
+
+    g = torch.Generator().manual_seed(7)
+    blocks, d = 60, 256
+    c = make_cache(1, d, 16, blocks)
+    table = torch.arange(blocks, dtype=torch.int32).view(1, blocks)
+    top = torch.exp(60 * torch.rand(blocks, 1, 1, generator=g) - 30)
+    top[:6, 0, 0] = torch.tensor([1.0, 127.0, 126.99999, 254.0, 3.0, 0.7])
+    if typ == "f16":
+        top = top.clamp(1e-3, 6e4)
+    s = top.to(DT[typ]).float() * torch.tensor(1.0 / 127)
+    x = s * (torch.randint(-127, 127, (blocks, 16, d), generator=g) + 0.5)
+    if typ == "f32":
+        x = (x.view(torch.int32) + torch.randint(-3, 4, x.shape, generator=g, dtype=torch.int32)).view(torch.float32)
+    x = torch.minimum(torch.maximum(x, -top), top)
+    x[:, 0, 0] = top[:, 0, 0]
+    K = x.to(DT[typ]).view(blocks * 16, 1, d)
+    V = K.flip(2)
+    want = Held(c)
+    want.write(table, [0], [0, blocks * 16], K, V)
+    skm.skm_kv_write(c, table.cuda(), i32([0]), i32([0, blocks * 16]), K.cuda(), V.cuda(), blocks * 16)
+    same(c, want)
