@@ -48,6 +48,7 @@ namespace {
 constexpr int QT = 128, KT = 64, KBLK = KT / KV_B;  // rows of a tile, keys of a tile, blocks of it
 constexpr int CONV = 7;  // converter warps
 constexpr int RANKED = 256;
+constexpr float W_MOST = 65000.0f;  // a block's sum of weights: above it one may pass the largest f16
 constexpr int INFO = 8;  // tiles whose scales are kept: those of the K ring and those its softmax still reads
 
 // DH: dims, padded to 64, 128 or 256
@@ -175,6 +176,29 @@ __device__ __forceinline__ void st_shared(uint32_t addr, uint32_t a, uint32_t b,
 __device__ __forceinline__ uint32_t pack(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// two weights 2^a, 2^b as f16, and added to a pair of sums (the sums as 64 bits, the
+// weights' conversion from the pair that was added: fewer moves between registers)
+__device__ __forceinline__ uint32_t weights2(float a, float b, uint64_t &sum) {
+    uint32_t p;
+    asm("{\n\t.reg .b64 e;\n\t.reg .f32 x, y;\n\t"
+        "ex2.approx.ftz.f32 x, %2;\n\tex2.approx.ftz.f32 y, %3;\n\t"
+        "mov.b64 e, {x, y};\n\tadd.rn.f32x2 %1, %1, e;\n\t"
+        "mov.b64 {x, y}, e;\n\tcvt.rn.f16x2.f32 %0, y, x;\n\t}"
+        : "=r"(p), "+l"(sum)
+        : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float2 halves(uint64_t x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
 }
 
 // A part: a CTA's rows x (m, l), then its rows of d sums
@@ -305,6 +329,12 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     const int t_lo = first / KT, t_all = last >= first ? last / KT + 1 - t_lo : 0;
     const int t0 = t_lo + (int)((int64_t)t_all * split / splits);
     const int n = t_lo + (int)((int64_t)t_all * (split + 1) / splits) - t0;
+    // those that a row tile goes through: the last one all of them, the one before it to its own end
+    const auto tiles_for = [&](int q) {
+        if (q >= nq) return 0;
+        const int its_last = last_of(a, s, min(r0 + (q + 1) * QT - 1, r1));
+        return its_last < first ? 0 : kv_clamp(its_last / KT + 1 - t0, 0, n);
+    };
 
     if (tid == 0) {
         for (int i = 0; i < ST; ++i) {
@@ -341,14 +371,14 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     const uint32_t tmem = *tmem_slot;
 
     if (warp < CONV_WARP0) {  // ------------------------------------------ softmax
-        const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row;
+        const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row, nt = tiles_for(q);
         const bool in = r < rows;
         const float fac = load_rows<DH>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE, lane);
         fence_async();
         __syncwarp();
         if (lane == 0) arrive(q_full);
         // (rows past the end see everything, with no weight: they slow no one down)
-        const int hi = in ? last_of(a, s, r) : 0x7fffffff, lo = in ? first_of(a, s, r) : 0;
+        const int hi = in ? last_of(a, s, r) : 0x7ffffffe, lo = in ? first_of(a, s, r) : 0;
         // rows of the warp see [low, high] whole
         const int high = __shfl_sync(0xffffffffu, hi, 0), low = __reduce_max_sync(0xffffffffu, lo);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -356,18 +386,23 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         float m = in ? M_NONE : -M_NONE, l = 0.0f;
         bool ok = true, loaded = false;  // loaded: v[0] holds (or will) the first logits of tile j
         uint32_t v[2][16];
-        for (int j = 0; j < n && q < nq; ++j) {
+        for (int j = 0; j < nt; ++j) {
             const uint32_t S = S0 + (j & 1) * KT;
             if (!loaded) {
                 if (!(ok = warp_wait(s_full(q, j & 1), (j >> 1) & 1, gone))) break;
                 fence_after();
-                ld16(S, v[0]);
+                if (j > 0) ld16(S, v[0]);
             }
             const float4 *inf = info + (j & (INFO - 1)) * KBLK;
             const int c0 = (t0 + j) * KT;
             const bool whole = c0 >= low && c0 + KT - 1 <= high;
             uint32_t P[KT / 2];
             float most = 0.0f, add = 0.0f;
+            // the positions of block k that the row sees, as bits
+            const auto visible = [&](int k) {
+                const int at = c0 + k * KV_B;
+                return ((1u << kv_clamp(hi + 1 - at, 0, KV_B)) - 1) & ~0u << kv_clamp(lo - at, 0, KV_B);
+            };
             // weights of block k of the tile from 16 logits
             const auto weigh = [&](const uint32_t (&x)[16], int k) {
                 const float4 f4 = inf[k];
@@ -380,52 +415,54 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     p[i] = t.x, p[i + 1] = t.y;
                 }
                 if (!whole) {
-                    int upto = hi - (c0 + k * KV_B), from = lo - (c0 + k * KV_B);
-                    // opaque, so that the comparisons stay in the branch (hoisted, they
-                    // were two integer operations a logit in every tile)
-                    asm volatile("" : "+r"(upto), "+r"(from));
+                    uint32_t sees = visible(k);
+                    // opaque, so that the tests of its bits stay in the branch (hoisted, they
+                    // are an operation a logit in every tile)
+                    asm volatile("" : "+r"(sees));
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) p[i] = i <= upto && i >= from ? p[i] : -INFINITY;
+                    for (int i = 0; i < 16; ++i) p[i] = sees & 1u << i ? p[i] : -INFINITY;
                 }
-                float2 sum[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                uint64_t sum[2] = {0, 0};
 #pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float2 e = make_float2(ex2(p[i]), ex2(p[i + 1]));
-                    sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], e);
-                    P[k * 8 + i / 2] = pack(e.x, e.y);
-                }
-                const float2 both = add2(sum[0], sum[1]);
+                for (int i = 0; i < 16; i += 2) P[k * 8 + i / 2] = weights2(p[i], p[i + 1], sum[(i >> 1) & 1]);
+                const float2 both = halves(add2(sum[0], sum[1]));
                 const float all = both.x + both.y;
                 most = fmaxf(most, all);
                 add = fmaf(all, f4.z, add);
             };
+            bool moves = j == 0;  // the reference: set by the first tile, seldom moved by a later one
+            if (!moves) {
 #pragma unroll
-            for (int k = 0; k < KBLK; ++k) {
-                ld_wait(v[k & 1]);
-                if (k + 1 < KBLK) {
-                    ld16(S + (k + 1) * KV_B, v[(k + 1) & 1]);
-                } else {  // the next tile's first logits, if they are there
-                    loaded = j + 1 < n && __all_sync(0xffffffffu, bar_test(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1));
-                    if (loaded) {
-                        fence_after();
-                        ld16(S0 + ((j + 1) & 1) * KT, v[0]);
-                    }
-                }
-                weigh(v[k & 1], k);
-            }
-            if (__any_sync(0xffffffffu, most > M_MOST)) {
-                // the rows' maxima, with them new references, and the weights again
-                float top = -INFINITY;
-#pragma unroll 1
                 for (int k = 0; k < KBLK; ++k) {
-                    uint32_t w[16];
-                    ld16(S + k * KV_B, w);
-                    ld_wait(w);
+                    ld_wait(v[k & 1]);
+                    if (k + 1 < KBLK) {
+                        ld16(S + (k + 1) * KV_B, v[(k + 1) & 1]);
+                    } else {  // the next tile's first logits, if they are there
+                        loaded = j + 1 < nt && __all_sync(0xffffffffu, bar_test(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1));
+                        if (loaded) {
+                            fence_after();
+                            ld16(S0 + ((j + 1) & 1) * KT, v[0]);
+                        }
+                    }
+                    weigh(v[k & 1], k);
+                }
+                moves = __any_sync(0xffffffffu, most > W_MOST);
+            }
+            if (moves) {
+                // the rows' maxima, with them new references, and the weights (again)
+                uint32_t w[KBLK][16];
+#pragma unroll
+                for (int k = 0; k < KBLK; ++k) ld16(S + k * KV_B, w[k]);
+                float top = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < KBLK; ++k) {
+                    ld_wait(w[k]);
                     const float4 f4 = inf[k];
-                    const int upto = hi - (c0 + k * KV_B), from = lo - (c0 + k * KV_B);
+                    const float f = fac * f4.x;
+                    const uint32_t sees = visible(k);
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (i <= upto && i >= from) top = fmaxf(top, fmaf(__uint_as_float(w[i]), fac * f4.x, f4.y));
+                        if (sees & 1u << i) top = fmaxf(top, fmaf(__uint_as_float(w[k][i]), f, f4.y));
                 }
                 const float to = top > m + 8.0f ? top - M_BELOW : m;
                 const float g = ex2(m - to);
@@ -436,23 +473,18 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     fence_after();
 #pragma unroll 1
                     for (int k = 0; k < DH / 16; ++k) {
-                        uint32_t w[16];
-                        ld16(O + k * 16, w);
-                        ld_wait(w);
+                        uint32_t x[16];
+                        ld16(O + k * 16, x);
+                        ld_wait(x);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * g);
-                        st16(O + k * 16, w);
+                        for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * g);
+                        st16(O + k * 16, x);
                     }
                     st_wait();
                 }
                 add = 0.0f;
 #pragma unroll
-                for (int k = 0; k < KBLK; ++k) {
-                    uint32_t w[16];
-                    ld16(S + k * KV_B, w);
-                    ld_wait(w);
-                    weigh(w, k);
-                }
+                for (int k = 0; k < KBLK; ++k) weigh(w[k], k);
             }
             l += add;
 #pragma unroll
@@ -464,7 +496,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         }
         if (loaded) ld_wait(v[0]);  // an early end leaves no load in flight
         if (q < nq) {
-            if (ok && n > 0) {
+            if (ok && nt > 0) {
                 ok = warp_wait(o_last(q), 0, gone);
                 fence_after();
             }
@@ -482,7 +514,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                 if (16 * k >= a.d) break;
                 uint32_t v[16];
                 __syncwarp();
-                if (ok && n > 0) {
+                if (ok && nt > 0) {
                     ld16(O + k * 16, v);
                     ld_wait(v);
                 } else {
@@ -621,17 +653,22 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             commit(s_full(q, j & 1), one);
         };
         // the logits of two key tiles ahead
+        const int nt[2] = {tiles_for(0), tiles_for(1)};
         for (int j = 0; j < 2 && j < n && ok; ++j) {
             if (!(ok = warp_wait(k_full(j), 0, gone))) break;
             fence_after();
-            for (int q = 0; q < nq; ++q) qk(q, j);
+            for (int q = 0; q < nq; ++q)
+                if (j < nt[q]) qk(q, j);
             commit(k_free(j), one);
         }
         for (int j = 0; j < n && ok; ++j) {
-            const int st = j & (ST - 1);
+            const int st = j & (ST - 1), ahead = (j + 2) & (ST - 1);
+            bool have_v = false, have_k = false;
             for (int q = 0; q < nq; ++q) {
+                if (j >= nt[q]) continue;
                 if (!(ok = warp_wait(p_full(q, j & 1), (j >> 1) & 1, gone))) break;
-                if (q == 0 && !(ok = warp_wait(v_full(st), (j / ST) & 1, gone))) break;
+                if (!have_v && !(ok = warp_wait(v_full(st), (j / ST) & 1, gone))) break;
+                have_v = true;
                 fence_after();
                 const uint32_t p = tmem + (2 * q + (j & 1)) * KT, o = tmem + L::O + q * DH;
                 const uint64_t va = v_op + (uint32_t)st * (L::TILE >> 4);
@@ -642,14 +679,15 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                 // a barrier of its own for the last product: the softmax may be up to two
                 // phases of o_done away from it, more than a parity tells apart.  Committed
                 // last, so that nothing arrives after the tile's rows are out
-                if (j == n - 1) commit(o_last(q), one);
-                if (j + 2 < n) {  // over the buffer that P V read, in order behind it
-                    if (q == 0) {
-                        if (!(ok = warp_wait(k_full((j + 2) & (ST - 1)), ((j + 2) / ST) & 1, gone))) break;
+                if (j == nt[q] - 1) commit(o_last(q), one);
+                if (j + 2 < nt[q]) {  // over the buffer that P V read, in order behind it
+                    if (!have_k) {
+                        if (!(ok = warp_wait(k_full(ahead), ((j + 2) / ST) & 1, gone))) break;
+                        have_k = true;
                         fence_after();
                     }
                     qk(q, j + 2);
-                    if (q == nq - 1) commit(k_free((j + 2) & (ST - 1)), one);
+                    if (q == nq - 1) commit(k_free(ahead), one);
                 }
             }
         }
