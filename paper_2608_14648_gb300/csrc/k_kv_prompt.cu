@@ -398,9 +398,11 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             const bool whole = c0 >= low && c0 + KT - 1 <= high;
             uint32_t P[KT / 2];
             float most = 0.0f, add = 0.0f;
-            // the positions of block k that the row sees, as bits
+            // the positions of block k that the row sees, as bits (opaque, so that it stays in the
+            // branches that ask: hoisted, it ran in every tile)
             const auto visible = [&](int k) {
-                const int at = c0 + k * KV_B;
+                int at = c0 + k * KV_B;
+                asm volatile("" : "+r"(at));
                 return ((1u << kv_clamp(hi + 1 - at, 0, KV_B)) - 1) & ~0u << kv_clamp(lo - at, 0, KV_B);
             };
             // weights of block k of the tile from 16 logits
@@ -415,10 +417,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     p[i] = t.x, p[i + 1] = t.y;
                 }
                 if (!whole) {
-                    uint32_t sees = visible(k);
-                    // opaque, so that the tests of its bits stay in the branch (hoisted, they
-                    // are an operation a logit in every tile)
-                    asm volatile("" : "+r"(sees));
+                    const uint32_t sees = visible(k);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) p[i] = sees & 1u << i ? p[i] : -INFINITY;
                 }
@@ -593,7 +592,8 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             const int w = (lane >> 4) + 2 * k;
             to[k] = (w >> 2) * (KT * 128) + (lane & 15) * 128 + (((w & 3) * 2 ^ (lane & 7)) << 4);
         }
-        for (int task = cw, i = 0; task < tasks; task += CONV, ++i) {
+        // a task from `raw`, the next one's codes on their way to `coming`
+        const auto convert = [&](int task, int i, uint4 (&raw)[NV], uint4 (&coming)[NV]) {
             const int slot = i & 31, j = task / (2 * KBLK), st = j & (ST - 1), blk = task & (KBLK - 1);
             const bool vals = task & KBLK;
             const float2 sc = make_float2(__shfl_sync(0xffffffffu, cur.sc.x, slot), __shfl_sync(0xffffffffu, cur.sc.y, slot));
@@ -603,39 +603,46 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             }
             const int at_next = __shfl_sync(0xffffffffu, cur.at, (i + 1) & 31);
             load(task + CONV, at_next, coming);
-            if (!warp_wait(vals ? v_free(st) : k_free(st), ((j / ST) & 1) ^ 1, gone)) break;
+            if (!warp_wait(vals ? v_free(st) : k_free(st), ((j / ST) & 1) ^ 1, gone)) return false;
             if (!vals && lane == 0) {
                 float4 f = value_scale(sc);
                 if (at < 0) f.y = -INFINITY;  // an absent block: no weight (its codes are zeros)
                 info[(j & (INFO - 1)) * KBLK + blk] = f;
             }
-            {
-                const uint32_t base = sm + (vals ? L::v + lane * 128 + ((blk * 2 ^ (lane & 7)) << 4) : L::k + blk * 2048) +
-                                      st * L::TILE;
+            // (a branch each for keys and values around all of it: their stores take the words in
+            // other groups of four registers)
+            if (!vals) {
+                const uint32_t base = sm + L::k + blk * 2048 + st * L::TILE;
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
                     if (lane + 32 * k >= a.d) break;
                     const uint4 c = raw[k];
-                    uint32_t f[8];
-                    f[0] = codes_f16(c.x, 0x4140), f[1] = codes_f16(c.x, 0x4342);
-                    f[2] = codes_f16(c.y, 0x4140), f[3] = codes_f16(c.y, 0x4342);
-                    f[4] = codes_f16(c.z, 0x4140), f[5] = codes_f16(c.z, 0x4342);
-                    f[6] = codes_f16(c.w, 0x4140), f[7] = codes_f16(c.w, 0x4342);
-                    if (!vals) {
-                        st_shared(base + to[k], f[0], f[1], f[2], f[3]);
-                        st_shared((base + to[k]) ^ 16, f[4], f[5], f[6], f[7]);
-                    } else {  // even words tokens 0..7, odd 8..15
-                        st_shared(base + k * 4096, f[0], f[2], f[4], f[6]);
-                        st_shared((base + k * 4096) ^ 16, f[1], f[3], f[5], f[7]);
-                    }
+                    st_shared(base + to[k], codes_f16(c.x, 0x4140), codes_f16(c.x, 0x4342), codes_f16(c.y, 0x4140),
+                              codes_f16(c.y, 0x4342));
+                    st_shared((base + to[k]) ^ 16, codes_f16(c.z, 0x4140), codes_f16(c.z, 0x4342), codes_f16(c.w, 0x4140),
+                              codes_f16(c.w, 0x4342));
+                }
+            } else {  // even halves of a word tokens 0..7, odd 8..15
+                const uint32_t base = sm + L::v + lane * 128 + ((blk * 2 ^ (lane & 7)) << 4) + st * L::TILE;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    if (lane + 32 * k >= a.d) break;
+                    const uint4 c = raw[k];
+                    st_shared(base + k * 4096, codes_f16(c.x, 0x4140), codes_f16(c.y, 0x4140), codes_f16(c.z, 0x4140),
+                              codes_f16(c.w, 0x4140));
+                    st_shared((base + k * 4096) ^ 16, codes_f16(c.x, 0x4342), codes_f16(c.y, 0x4342), codes_f16(c.z, 0x4342),
+                              codes_f16(c.w, 0x4342));
                 }
             }
             fence_async();
             __syncwarp();
             if (lane == 0) arrive(vals ? v_full(st) : k_full(st));
             at = at_next;
-#pragma unroll
-            for (int k = 0; k < NV; ++k) raw[k] = coming[k];
+            return true;
+        };
+        for (int task = cw, i = 0; task < tasks; task += 2 * CONV, i += 2) {
+            if (!convert(task, i, raw, coming)) break;
+            if (task + CONV >= tasks || !convert(task + CONV, i + 1, coming, raw)) break;
         }
     } else if (n > 0) {  // ------------------------------------------------ MMA issuer
         const uint32_t one = elect_one();
