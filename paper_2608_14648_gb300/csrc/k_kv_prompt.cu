@@ -406,8 +406,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                 return ((1u << kv_clamp(hi + 1 - at, 0, KV_B)) - 1) & ~0u << kv_clamp(lo - at, 0, KV_B);
             };
             // weights of block k of the tile from 16 logits
-            const auto weigh = [&](const uint32_t (&x)[16], int k) {
-                const float4 f4 = inf[k];
+            const auto weigh = [&](const uint32_t (&x)[16], int k, float4 f4) {
                 const float f = fac * f4.x, c = f4.y - m;
                 float p[16];
 #pragma unroll
@@ -431,8 +430,11 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             };
             bool moves = j == 0;  // the reference: set by the first tile, seldom moved by a later one
             if (!moves) {
+                float4 coming;
 #pragma unroll
                 for (int k = 0; k < KBLK; ++k) {
+                    const float4 now = k ? coming : inf[0];
+                    if (k + 1 < KBLK) coming = inf[k + 1];  // (read before the wait, which nothing moves across)
                     ld_wait(v[k & 1]);
                     if (k + 1 < KBLK) {
                         ld16(S + (k + 1) * KV_B, v[(k + 1) & 1]);
@@ -443,7 +445,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                             ld16(S0 + ((j + 1) & 1) * KT, v[0]);
                         }
                     }
-                    weigh(v[k & 1], k);
+                    weigh(v[k & 1], k, now);
                 }
                 moves = __any_sync(0xffffffffu, most > W_MOST);
             }
@@ -483,7 +485,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                 }
                 add = 0.0f;
 #pragma unroll
-                for (int k = 0; k < KBLK; ++k) weigh(w[k], k);
+                for (int k = 0; k < KBLK; ++k) weigh(w[k], k, inf[k]);
             }
             l += add;
 #pragma unroll
