@@ -1,23 +1,25 @@
 // Writing keys and values into the 8-bit cache and reading them back.
 //
-// One warp takes one block (16 tokens) of one head's keys or values: it holds
-// the block's new values in registers as they came, so the largest magnitude,
-// the scale and the codes come from one read of the input.  Both kernels move
-// bytes; a warp needs no other warp, so an append (one token, a warp busy for its
-// memory latencies) and a prompt (thousands of independent 4 KB reads in flight) are
-// the same code.  What bounds writing is how many of those reads are in flight
-// and the instructions of a block (984 a warp for 2048 values):
-// the input is read before the page is known, and 16-bit values stay packed
-// (64 registers, 32 warps an SM).
+// One warp takes one block (16 tokens) of one head's keys or values: a first pass over
+// the block's new values for the largest magnitude, a second one, out of L1, for the
+// codes.  A warp needs no other warp, so an append (one token, a warp busy for its memory
+// latencies) and a prompt (thousands of independent 4 KB reads in flight) are the
+// same code.  What bounds writing is how many of those reads are in flight and the
+// instructions of a block (850 a warp for 2048 values): the input is read before the page is known, eight
+// 16-byte loads a lane at a time, and the second pass is a rolled loop (holding the
+// values in registers instead took an unrolled path for each d, and warps waited for
+// its instructions: 43 us against 37 for the 12 prompts below).  64 registers, 32 warps an
+// SM: with 48 or 40 registers the loads in flight cost more than the warps give (writing and reading
+// back 54, 55 and 59 us).
 //
-// Measured (GB300, bf16, 8 heads of 128): writing 12 prompts of up to 2500 tokens,
-// 93 MB in and out, 43 us = 2.2 TB/s; reading 4 sequences of up to 32768
-// tokens back, 611 MB, 101 us = 6.0 TB/s (a plain copy: 6.8).
+// Measured (GB300, bf16, 8 heads of 128): writing 12 prompts of up to 2500 tokens, 93 MB
+// in and out, 32 us = 2.9 TB/s; reading 4 sequences of up to 32768 tokens back, 611 MB,
+// 101 us = 6.0 TB/s (a plain copy: 6.8).
 //
-// Lanes: keys, a unit is 16 dims of a token (a 16-byte code store, two 16-byte
-// loads of 16-bit values), consecutive lanes along d; values, whose blocks
-// keep the 16 tokens of a dim together, a unit is 8 dims of the four tokens
-// that share a 32-bit word, so the transposition stays in registers.
+// Lanes: the magnitudes and the keys along d (a 16-byte code store, two 16-byte loads
+// of 16-bit values); values, whose blocks keep the 16 tokens of a dim together, 8
+// dims of the four tokens that share a 32-bit word, so the transposition stays in
+// registers.
 //
 // The largest magnitude is an integer maximum of the values' bits without
 // their sign, in which infinities and NaN come out on top: a warp that finds one
@@ -27,9 +29,9 @@
 // q = x y, y the correctly rounded reciprocal, corrected twice by its exact
 // remainder: q' = q + (x - q s) y.  q is within 1.5 units in the last place, the first correction
 // within one, and by Markstein's theorem (IBM J. Res. Dev. 34, 1990) the second
-// is the quotient as a division rounds it.  Five operations, two values at a time: a
-// division only where x y lies near the middle of two codes took more, because
-// 16-bit values meet it often (half the largest one is 63.5).
+// is the quotient as a division rounds it.  Five operations, two values at a time; a
+// division only where x y lies near the middle of two codes took longer (37 us
+// against 32), because 16-bit values meet it often (half the largest one is 63.5).
 #include <algorithm>
 #include <type_traits>
 

@@ -20,25 +20,27 @@
 //   warp 15         MMA issuer (d > 128: 4 softmax warps, the others behind them)
 //
 // TMEM: two S/P buffers of 64 columns a tile, O0, O1 (DH columns each).  The
-// logits of a key tile are there before the softmax of the one before is done, so a
-// softmax warp never waits for the tensor cores to answer it (with one buffer
+// logits of a key tile are under way while the softmax of the one before runs (with one buffer
 // of 128 keys a tile the chain softmax, P V, Q K' took 5400 clocks for 256 x 128
-// logits where the tensor cores need 2048).  The first pass over a tile's
-// logits assumes that m need not move; a block whose sum exceeds 2^15 (m has to be
-// set or moved, at a row's first tile and rarely after it) sends the warp through a
-// maximum, a rescaling of O and a second pass.  Shared memory: Q, and rings of K and V
-// tiles.
+// logits where the tensor cores need 2048).  The pass over a tile's
+// logits assumes that m need not move; the first tile, and a block whose sum exceeds
+// 65000 (seldom), send the warp through the maxima, a rescaling of O and the weights
+// once more.  Shared memory: Q, and rings of K and V tiles.
 //
 // Few CTAs (short prompts): the keys are split over CTAs as well, and
 // kv_prompt_join_kernel merges the parts in order.
 //
 // Measured (GB300): chunks of 2048 tokens of two prompts behind 6144, 32 query heads
-// over 8 of 128, bf16: 323 us = 1040 TFLOP/s, 54% of a cuBLAS product; 4 whole prompts of up to
-// 4096, 16 heads of 64, f16: 143 us (long and short row tiles; half the work of a
-// product of 128 dims for as many exponentials).  A tile of 256 rows x 64 keys takes 1850
-// clocks: the softmax warps' chain (TMEM load, exponentials, sums, P back, barriers)
-// bounds it; the products take 1280 (an instruction of 128 x 64 x 16 with both operands in
-// shared memory 48, bound by reading them), the 7 converter warps somewhat less.
+// over 8 of 128, bf16: 293 us = 1150 TFLOP/s, 60% of a cuBLAS product; 4 whole prompts of up to
+// 4096, 16 heads of 64, f16: 123 us (half the flops a logit, and key tiles on the
+// diagonal).  A tile of 256 rows x 64 keys takes some 2000 clocks.  What bounds it is the
+// softmax warps' chain of latencies, two warps a scheduler: without the
+// exponentials, the conversion of codes or P's way back the time stays within 2%, with three
+// quarters of the products gone it is 276 us, without exponentials and conversion as well
+// 248.  So reads
+// that a wait would hold up come before it (a block's scales: 11 us), the converters
+// leave issue slots free (6 us), and what runs seldom stays in its branch.  More logits a
+// wait (367 us) or asking for the next tile's earlier (311) made it slower.
 #include "skm_kv_dev.cuh"
 
 namespace skm {
