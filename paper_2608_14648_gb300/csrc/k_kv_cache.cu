@@ -5,7 +5,7 @@
 // codes.  A warp needs no other warp, so an append (one token, a warp busy for its memory
 // latencies) and a prompt (thousands of independent 4 KB reads in flight) are the
 // same code.  What bounds writing is how many of those reads are in flight and the
-// instructions of a block (850 a warp for 2048 values): the input is read before the page is known, eight
+// instructions of a block (1095 a warp for 2048 values): the input is read before the page is known, eight
 // 16-byte loads a lane at a time, and the second pass is a rolled loop (holding the
 // values in registers instead took an unrolled path for each d, and warps waited for
 // its instructions: 43 us against 37 for the 12 prompts below).  64 registers, 32 warps an
