@@ -539,3 +539,36 @@ def test_write_rounds_like_a_division(cuda_ok, typ):
     want.write(table, [0], [0, blocks * 16], K, V)
     skm.skm_kv_write(c, table.cuda(), i32([0]), i32([0, blocks * 16]), K.cuda(), V.cuda(), blocks * 16)
     same(c, want)
+
+
+@pytest.mark.parametrize("heads,group,d,page,typ,seqs,window", [
+    (1, 2, 256, 64, "bf16", [(1500, 40)], 0), (2, 3, 192, 32, "f16", [(1400, 150), (0, 33), (70, 1)], 0),
+    (1, 2, 256, 16, "f16", [(1600, 300), (3, 129)], 1350), (8, 16, 256, 64, "bf16", [(5, 40), (0, 17), (60, 3)], 0),
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attend_wide_heads_many_rows(cuda_ok, heads, group, d, page, typ, seqs, window, causal):
+    # long enough, or enough units, for d > 128 to go to the kernel for many rows
+    check_attend(heads, group, d, page, typ, seqs, causal, window if causal else 0)
+
+
+def test_offsets_beyond_32_bits(cuda_ok):
+    # a pool of 5 GB of keys and as much of values: its last pages against a small pool's, bit for bit
+    import paper_2608_14648_gb300 as skm
+
+    heads, d, page, pages, n = 8, 256, 64, 40000, 1500
+    cols = -(-n // page)
+    small, big = (skm.KVCache(heads, d, page, pages=p) for p in (cols, pages))
+    assert big.k.numel() > 1 << 32
+    at = torch.arange(cols, dtype=torch.int32, device="cuda").view(1, cols)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    K, V = torch.randn(2, n, heads, d, generator=g, device="cuda").to(torch.bfloat16)
+    got = []
+    for c, table in ((small, at), (big, at + (pages - cols))):
+        skm.skm_kv_write(c, table, i32([0]), i32([0, n]), K, V, n)
+        res = list(skm.skm_kv_read(c, table, i32([0]), i32([0, n]), n, n))
+        for rows, typ in ((1, torch.bfloat16), (1, torch.float32), (300, torch.float16)):
+            Q = torch.randn(rows, 2 * heads, d, generator=torch.Generator().manual_seed(9)).cuda().to(typ)
+            res += skm.skm_kv_attend(c, table, i32([n]), i32([0, rows]), Q, rows, n, want_lse=True)
+        got.append(res)
+    for x, y in zip(*got):
+        assert torch.isfinite(x).all() and torch.equal(x, y)
