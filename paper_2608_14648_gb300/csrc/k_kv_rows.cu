@@ -28,7 +28,10 @@
 //
 // Joining.  Partial (m, l, o) of units that warps share are merged by their
 // CTA, those that CTAs share by kv_join_kernel; both in the line's order, so
-// the result does not depend on timing.
+// the result does not depend on timing.  A CTA that goes on with a unit notes what there is to
+// join, so the second kernel has a CTA a cut and row, whatever the batch (with one a unit
+// and row, each finding its place, 900 sequences of up to 2501 tokens took 344 us
+// instead of 259).
 #include "skm_kv_dev.cuh"
 
 namespace skm {
@@ -695,6 +698,20 @@ __device__ void line_up(const KvAttnArgs &a, int b0, int nb, int64_t *cum, Seq *
     __syncthreads();
 }
 
+// What the CTA that goes on with a unit first leaves for kv_join_kernel: the unit,
+// the CTAs that hold parts of it (0: not this CTA's to say), its sequence's rows
+struct Cut {
+    int unit, parts, row0, n;
+};
+// The CTA that holds an item, C of them sharing W: CTA c takes [W c / C, W (c + 1) / C),
+// with floor(W c / C) <= item written as W c < C (item + 1)
+__device__ __forceinline__ int64_t holder(int64_t item, int64_t W, int64_t C) {
+    int64_t c = (int64_t)((uint64_t)item * (uint64_t)C / (uint64_t)W);
+    while (W * (c + 1) < C * (item + 1)) ++c;
+    while (W * c >= C * (item + 1)) --c;
+    return c;
+}
+
 template <class Rows, int NW>
 __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_constant__ KvAttnArgs a, int ns) {
     constexpr int RT = Rows::RT;
@@ -876,6 +893,10 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
     }
     __syncthreads();
     const Record mine = lane < 2 * NW ? rec[lane] : Record{0, -1, nullptr};
+    // (by a warp that has no rows to merge)
+    Cut *cut = a.whole || warp != NW - 1 || lane != 0 ? nullptr
+                                                      : reinterpret_cast<Cut *>(a.part_cta + (int64_t)gridDim.x * 2 * pf) + blockIdx.x;
+    if (cut) *cut = Cut{0, 0, 0, 0};
     for (uint32_t left = __ballot_sync(0xffffffffu, mine.unit >= 0); left;) {
         const int f = __ffs(left) - 1;
         const int rs = __shfl_sync(0xffffffffu, mine.seq, f), ru = __shfl_sync(0xffffffffu, mine.unit, f);
@@ -884,57 +905,33 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
         const Seq s = seq[rs];
         const int64_t u0 = cum[rs] + (int64_t)ru * s.cnt, u1 = u0 + s.cnt;
         float *dst = u0 >= c0 && u1 <= c1 ? nullptr : a.part_cta + ((int64_t)blockIdx.x * 2 + (u0 < c0 ? 0 : 1)) * pf;
+        if (cut && u0 < c0) {
+            const int64_t C = active_ctas(W, NW, gridDim.x), c = blockIdx.x;
+            if (u0 >= W * (c - 1) / C) *cut = Cut{ru, (int)(holder(u1 - 1, W, C) - c + 2), s.row0, s.n};
+        }
         merge_parts<RT, Rows::D4>(a, mine.part, same, s, ru, dst, warp, NW, lane);
     }
 }
 
-// One CTA a row of a unit: merges what the CTAs of kv_rows_kernel left of it,
-// a warp every fourth part, then the warps' sums.  grid: that kernel's CTAs.
+// CTA c RT + r: row r of the unit that kv_rows_kernel's CTA c was the first to go on
+// with; merges what the CTAs left of it, a warp every fourth part, then the warps' sums.
 template <int RT>
-__global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ KvAttnArgs a, int nw, int64_t grid) {
-    __shared__ int64_t sums[2][4];
+__global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ KvAttnArgs a, int ctas) {
     __shared__ float tops[4], sl[4];
     __shared__ float2 ml[KV_SMS];  // (m, l) of the parts, then (weight, .)
     __shared__ float4 so[3][64];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = a.max_tiles * a.heads, r = blockIdx.x % RT;
-    const int mine = blockIdx.x / RT / per, unit = blockIdx.x / RT % per;
-    const Seq s = seq_of(a, a.b0 + mine);
-    if (s.cnt == 0 || unit >= tiles_of(a, s, RT) * a.heads || a.by_heads.div(unit) * RT + r >= s.n * a.group) return;
-    // items before this sequence, and all of them
-    int64_t before = 0, all = 0;
-    for (int i = tid; i < a.nb; i += 128) {
-        const Seq q = seq_of(a, a.b0 + i);
-        const int64_t v = (int64_t)q.cnt * tiles_of(a, q, RT) * a.heads;
-        all += v;
-        if (i < mine) before += v;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        before += __shfl_xor_sync(0xffffffffu, before, o);
-        all += __shfl_xor_sync(0xffffffffu, all, o);
-    }
-    if (lane == 0) sums[0][warp] = before, sums[1][warp] = all;
-    __syncthreads();
-    before = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
-    all = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
-    const int64_t u0 = before + (int64_t)unit * s.cnt, u1 = u0 + s.cnt;
-    const int64_t C = active_ctas(all, nw, grid);
-    // CTA c takes [all c / C, all (c + 1) / C): the one that holds an item, with
-    // floor(all c / C) <= item written as all c < C (item + 1)
-    const auto holder = [&](int64_t item) {
-        int64_t c = (int64_t)((uint64_t)item * (uint64_t)C / (uint64_t)all);
-        while (all * (c + 1) < C * (item + 1)) ++c;
-        while (all * c >= C * (item + 1)) --c;
-        return c;
-    };
-    const int first = (int)holder(u0), np = (int)holder(u1 - 1) - first + 1;
-    if (np == 1) return;
+    const int r = blockIdx.x % RT, c = blockIdx.x / RT;
     const int64_t pf = part_floats<RT>(a.d);
-    // the first CTA left it open at its end (slot 1), the others found it begun (slot 0)
-    const float *base = a.part_cta + (int64_t)first * 2 * pf;
-    const auto part = [&](int i) { return base + (2 * (int64_t)i + (i == 0 ? 1 : 0)) * pf; };
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    const Cut cut = reinterpret_cast<const Cut *>(a.part_cta + (int64_t)ctas * 2 * pf)[c];
+    const int unit = cut.unit, np = cut.parts;
+    if (np == 0 || a.by_heads.div(unit) * RT + r >= cut.n * a.group) return;
+    Seq s = {};
+    s.row0 = cut.row0;
+    // the CTA before left it open at its end (slot 1), this one and others found it begun (slot 0)
+    const float *base = a.part_cta + (int64_t)(c - 1) * 2 * pf;
+    const auto part = [&](int i) { return base + (2 * (int64_t)i + (i == 0 ? 1 : 0)) * pf; };
     float m = M_NONE;
     for (int i = tid; i < np; i += 128) {
         const float2 x = *reinterpret_cast<const float2 *>(part(i) + 2 * r);
@@ -1000,7 +997,7 @@ cudaError_t run_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) 
     });
     if (e != cudaSuccess || p.whole) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.units * Rows::RT));
+    cfg.gridDim = dim3((unsigned)(p.grid * Rows::RT));
     cfg.blockDim = dim3(128);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
@@ -1008,7 +1005,7 @@ cudaError_t run_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) 
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kv_join_kernel<Rows::RT>, a, NW, p.grid);
+    e = cudaLaunchKernelEx(&cfg, kv_join_kernel<Rows::RT>, a, (int)p.grid);
     return e != cudaSuccess ? e : launched();
 }
 
@@ -1027,7 +1024,7 @@ KvRowsPlan plan_rows(int nb, int heads, int group, int d, int max_tokens, int64_
     while (p.ns > 1 && smem_of<Rows>(seqs, d, nw, p.ns).total > SMEM_MOST) --p.ns;
     p.smem = smem_of<Rows>(seqs, d, nw, p.ns).total;
     p.grid = p.whole ? p.units : KV_SMS;
-    p.part_cta = p.whole ? 0 : (size_t)p.grid * 2 * part_floats<Rows::RT>(d) * 4;
+    p.part_cta = p.whole ? 0 : (size_t)p.grid * (2 * part_floats<Rows::RT>(d) * 4 + sizeof(Cut));
     p.part_warp = p.whole ? 0 : (size_t)p.grid * nw * part_floats<Rows::RT>(d) * 4;
     return p;
 }
