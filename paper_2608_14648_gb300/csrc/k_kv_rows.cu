@@ -7,7 +7,7 @@
 // tile, head), and each CTA takes an equal stretch of it, each warp an equal
 // stretch of its CTA's: short and long sequences balance without a plan on the
 // host, and a warp crosses at most two cuts.  (With `whole`, a CTA's stretch
-// is one unit: short sequences then need no second kernel.)  A warp runs alone: lane 0
+// is one unit: few short ones then need no second kernel.)  A warp runs alone: lane 0
 // keeps a ring of cp.async.bulk copies (a block's keys and values, 16 d bytes
 // each, contiguous in the cache) going across unit boundaries; the table
 // entries and scales of 32 items are fetched at once, a window ahead.
@@ -32,6 +32,9 @@
 // join, so the second kernel has a CTA a cut and row, whatever the batch (with one a unit
 // and row, each finding its place, 900 sequences of up to 2501 tokens took 344 us
 // instead of 259).
+#include <algorithm>
+#include <initializer_list>
+
 #include "skm_kv_dev.cuh"
 
 namespace skm {
@@ -1009,16 +1012,23 @@ cudaError_t run_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) 
     return e != cudaSuccess ? e : launched();
 }
 
+// One CTA a unit, without the join kernel: where every unit has an SM, and none is so
+// long that it had better be shared.  16-bit queries, 4 heads a group, d = 128
+// (alone in a graph): 8 units of 121 keys take 8 us against 12 in shared stretches,
+// of 1001 both 12, of 1901 16 against 14; 128 units of 1901 17 against 20; 512 units of 121
+// keys, more than a wave, 28 against 13, 192 of 1001 23 against 19.
+constexpr int64_t WHOLE_FEW = 64, WHOLE_KEYS = 1024, WHOLE_KEYS_MANY = 2048;
+bool whole_units(int64_t units, int64_t span) {
+    return units <= KV_SMS && span <= (units <= WHOLE_FEW ? WHOLE_KEYS : WHOLE_KEYS_MANY);
+}
+
 template <class Rows>
 KvRowsPlan plan_rows(int nb, int heads, int group, int d, int max_tokens, int64_t span, int nw) {
     KvRowsPlan p = {};
     p.rt = Rows::RT;
     p.nw = nw;
     p.units = (int64_t)nb * cdiv((int64_t)max_tokens * group, p.rt) * heads;
-    // One CTA a unit, without the join kernel, while the longest unit is short: one
-    // sequence of 333 tokens takes 13 us against 16 in shared stretches, 16 that see
-    // 1029 positions 25 against 29; one of 4096 takes longer on one SM than on many.
-    p.whole = span <= 2048;
+    p.whole = whole_units(p.units, span);
     p.ns = 4;
     const int seqs = p.whole ? 1 : nb;
     while (p.ns > 1 && smem_of<Rows>(seqs, d, nw, p.ns).total > SMEM_MOST) --p.ns;
@@ -1068,6 +1078,21 @@ KvRowsPlan kv_rows_plan(int nb, int heads, int group, int d, int dtype, int max_
     KV_ROWS_VARIANTS(KV_PLAN)
 #undef KV_PLAN
     return KvRowsPlan{};
+}
+
+size_t kv_rows_part_most(int nb, int heads, int d, int dtype, int64_t rows, int64_t span) {
+    // fewer units may share an SM's stretch where more have one each
+    if (span <= WHOLE_KEYS && (int64_t)nb * heads * cdiv(rows, (int64_t)(dtype == SKM_DTYPE_F32 ? 4 : 8)) <= KV_SMS) return 0;
+    size_t most = 0;
+    for (const int r : {1, 2, 9, 17}) {  // the fewest rows of every tile
+        if (r > rows) break;
+        const KvRowsPlan p = kv_rows_plan(KV_SMS + 1, 1, 1, d, dtype, r, WHOLE_KEYS_MANY + 1);
+        Carver cv(nullptr, 0);
+        cv.take<float>(p.part_cta / 4);
+        cv.take<float>(p.part_warp / 4);
+        most = std::max(most, cv.off);
+    }
+    return most;
 }
 
 cudaError_t launch_kv_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) {

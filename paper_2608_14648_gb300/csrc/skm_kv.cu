@@ -1,7 +1,6 @@
 // extern "C" entry points of the 8-bit key/value cache (declared in
 // include/skm.h): argument checks on the host, workspace carving, launches.
 #include <algorithm>
-#include <initializer_list>
 
 #include "skm_kv.cuh"
 
@@ -179,20 +178,10 @@ size_t skm_kv_attend_workspace_size(const skm_kv_cache *c, const skm_kv_seqs *s,
     if (check_attend(c, s, a) != SKM_OK) return (size_t)-1;
     if (most_tokens(s) == 0) return 0;
     // the most that any call of these sizes or smaller ones takes: fewer rows may
-    // mean another tile, or more CTAs that share a row (more than KV_ROWS_MOST rows
-    // in k_kv_rows.cu after all: short, without parts)
+    // mean another tile, or more CTAs that share a row
     const int64_t span = std::min<int64_t>(s->max_len, (int64_t)s->cols * c->page);
     const int64_t rows = (int64_t)most_tokens(s) * (a->heads_q / c->heads);
-    const int nb = std::min<int>(s->batch, KV_MAX_SEQS);
-    size_t most = 0;
-    for (const int64_t r : {int64_t(1), int64_t(8), int64_t(16), int64_t(32), rows}) {
-        if (r > rows || (a->dtype != SKM_DTYPE_F32 && r > KV_ROWS_MOST)) continue;
-        const KvRowsPlan p = kv_rows_plan(nb, c->heads, 1, c->d, a->dtype, (int)r, span);
-        Carver cv(nullptr, 0);
-        if (p.part_cta) cv.take<float>(p.part_cta / 4);
-        if (p.part_warp) cv.take<float>(p.part_warp / 4);
-        most = std::max(most, cv.off);
-    }
+    size_t most = kv_rows_part_most(std::min<int>(s->batch, KV_MAX_SEQS), c->heads, c->d, a->dtype, rows, span);
     if (a->dtype != SKM_DTYPE_F32 && rows > KV_ROWS_MOST) most = std::max(most, kv_prompt_part_most(c->d, span));
     return most;
 }

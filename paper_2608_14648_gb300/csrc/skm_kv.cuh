@@ -76,6 +76,8 @@ struct KvRowsPlan {
     size_t smem, part_cta, part_warp;  // bytes
 };
 KvRowsPlan kv_rows_plan(int nb, int heads, int group, int d, int dtype, int max_tokens, int64_t span);
+// workspace of any call of these sizes or smaller ones at most
+size_t kv_rows_part_most(int nb, int heads, int d, int dtype, int64_t rows, int64_t span);
 cudaError_t launch_kv_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st);
 
 // Many rows on tcgen05 (k_kv_prompt.cu): max_tiles in units of a CTA's rows

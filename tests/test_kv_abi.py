@@ -131,7 +131,8 @@ def test_a_workspace_serves_smaller_calls(skm, d, dtype):
     # each call is stopped by an injected refusal, whose message says what it needs
     c = cache(skm, d=d, pages=100000)
     need_of = skm.lib().skm_kv_attend_workspace_size
-    for group, batch, most, length in [(1, 1, 1, 5000), (1, 40, 3, 700), (8, 3, 2, 90000), (4, 9, 60, 640), (2, 7, 900, 20000)]:
+    for group, batch, most, length in [(1, 1, 1, 5000), (1, 40, 3, 700), (8, 3, 2, 90000), (4, 9, 60, 640), (2, 7, 900, 20000),
+                                       (1, 200, 3, 300), (1, 60, 9, 1024), (3, 30, 6, 1100)]:
         sizes = dict(cols=100000, tokens=batch * most)
         a = attn(skm, heads_q=2 * group, dtype=dtype)
         need = need_of(ctypes.byref(c), ctypes.byref(seqs(skm, batch=batch, max_tokens=most, max_len=length, **sizes)), ctypes.byref(a))
