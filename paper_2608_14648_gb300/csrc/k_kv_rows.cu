@@ -21,10 +21,12 @@
 //
 // What bounds it.  Sequences with much to read: HBM (GB300, 8 heads of 128: 64
 // sequences of up to 8192 tokens, 485 MB, 99 us = 4.9 TB/s; one of 131079, 269
-// MB, 56 us = 4.8 TB/s; a plain copy of as much 6.8).  What is missing is at both
-// ends: some 4 us until the first block has arrived (lengths, table, scales, each behind
-// the one before), as much for merging warps and CTAs.  Short sequences: the launch, and
-// instructions that are fetched for the first time (7 of the 11 us for one of 333 tokens).
+// MB, 56 us = 4.8 TB/s; a plain copy of as much 6.8).  While all
+// warps of the batch run it is read at 6.9 TB/s; they end 62 to 82 us after the start
+// (SMs do not all get the same share), some 4 us pass until the first block has arrived
+// (lengths, table, scales, each behind the one before), and merging takes the rest.  Short
+// sequences: instructions that are fetched for the first time (7 of the 9 us for one of
+// 333 tokens, in a graph).
 //
 // Joining.  Partial (m, l, o) of units that warps share are merged by their
 // CTA, those that CTAs share by kv_join_kernel; both in the line's order, so
