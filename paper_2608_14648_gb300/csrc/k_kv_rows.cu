@@ -140,7 +140,7 @@ __host__ __device__ constexpr int part_head() {
     return (2 * RT + 3) & ~3;
 }
 template <int RT>
-__host__ __device__ __forceinline__ int64_t part_floats(int d) {
+__host__ __device__ __forceinline__ constexpr int64_t part_floats(int d) {
     return part_head<RT>() + (int64_t)RT * d;
 }
 
@@ -222,7 +222,7 @@ template <int R, int DPL>
 struct Fp32Rows {
     static constexpr int RT = R, D4 = DPL > 4 ? 2 : 1;
     static constexpr bool ONE_D = false;
-    static size_t __host__ __device__ scratch(int d) { return (size_t)R * (d + KV_B) * 4 + LIMITS<R>; }
+    static constexpr size_t __host__ __device__ scratch(int d) { return (size_t)R * (d + KV_B) * 4 + LIMITS<R>; }
     float o[R][DPL], m[R], l[R];
     float *q, *p;
     int2 *lim;
@@ -405,7 +405,7 @@ struct MmaRows {
     static constexpr int D4 = DC > 8 ? 2 : 1;
     static constexpr bool ONE_D = FULL;
     static constexpr bool QMEM = NT * DC >= 32;  // the queries' operands wait in shared memory
-    static size_t __host__ __device__ scratch(int) { return (QMEM ? (size_t)NT * DC * 2 * 32 * 4 : 0) + LIMITS<RT>; }
+    static constexpr size_t __host__ __device__ scratch(int) { return (QMEM ? (size_t)NT * DC * 2 * 32 * 4 : 0) + LIMITS<RT>; }
     float o[NT][DC][4], m[NT][2], l[NT][2], fac[NT][2];
     uint32_t q[QMEM ? 1 : NT][QMEM ? 1 : DC][2];
     uint2 *qmem;
@@ -640,9 +640,8 @@ struct Smem {
     size_t cum, seq, rec, win, bars, scratch, ring, warp_ring, total;
 };
 template <class Rows>
-__host__ __device__ __forceinline__ Smem smem_of(int nb, int d, int nw, int ns) {
-    Smem s;
-    s.cum = 0;
+__host__ __device__ __forceinline__ constexpr Smem smem_of(int nb, int d, int nw, int ns) {
+    Smem s = {};
     s.seq = s.cum + 8 * (size_t)(nb + 1);
     s.seq = (s.seq + 15) & ~size_t(15);
     s.rec = (s.seq + sizeof(Seq) * nb + 15) & ~size_t(15);
@@ -1024,11 +1023,23 @@ bool whole_units(int64_t units, int64_t span) {
     return units <= KV_SMS && span <= (units <= WHOLE_FEW ? WHOLE_KEYS : WHOLE_KEYS_MANY);
 }
 
+// Sequences of one launch: their line takes 28 bytes of shared memory each, which 1024 of them have
+// beside the smaller tiles only (32 rows of d = 128: 783; 16 of 256: 856)
 template <class Rows>
-KvRowsPlan plan_rows(int nb, int heads, int group, int d, int max_tokens, int64_t span, int nw) {
+int seqs_that_fit(int nb, int d, int nw) {
+    nb = std::min(nb, KV_MAX_SEQS);
+    while (smem_of<Rows>(nb, d, nw, 1).total > SMEM_MOST) --nb;  // (ends: plan_rows' assertion)
+    return nb;
+}
+
+template <class Rows, int NW, int DMAX>
+KvRowsPlan plan_rows(int nb, int heads, int group, int d, int max_tokens, int64_t span) {
+    static_assert(smem_of<Rows>(1, DMAX, NW, 1).total <= SMEM_MOST, "a CTA's shared memory");
+    constexpr int nw = NW;
     KvRowsPlan p = {};
     p.rt = Rows::RT;
     p.nw = nw;
+    p.seqs = nb = seqs_that_fit<Rows>(nb, d, nw);
     p.units = (int64_t)nb * cdiv((int64_t)max_tokens * group, p.rt) * heads;
     p.whole = whole_units(p.units, span);
     p.ns = 4;
@@ -1073,7 +1084,7 @@ KvRowsPlan kv_rows_plan(int nb, int heads, int group, int d, int dtype, int max_
     const int dmax = d <= 64 ? 64 : d <= 128 ? 128 : 256;
 #define KV_PLAN(FP32, RT, D, ROWS, NW)                                                          \
     if (fp32 == FP32 && rt == RT && dmax == D) {                                                \
-        KvRowsPlan p = plan_rows<KV_UNPACK ROWS>(nb, heads, group, d, max_tokens, span, NW);    \
+        KvRowsPlan p = plan_rows<KV_UNPACK ROWS, NW, D>(nb, heads, group, d, max_tokens, span); \
         p.fp32 = FP32;                                                                          \
         return p;                                                                               \
     }

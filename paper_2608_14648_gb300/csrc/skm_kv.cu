@@ -108,6 +108,7 @@ int64_t span_of(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn *
 // How a call runs, and its parts of the workspace
 struct AttendPlan {
     bool prompt;
+    int seqs;  // of a launch
     KvRowsPlan rows = {};
     KvPromptPlan many = {};
     float *part_cta = nullptr, *part_warp = nullptr;
@@ -115,13 +116,14 @@ struct AttendPlan {
 
 AttendPlan plan_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, Carver &cv) {
     AttendPlan p;
-    const int nb = std::min<int>(s->batch, KV_MAX_SEQS), group = a->heads_q / c->heads, most = most_tokens(s);
+    const int nb = p.seqs = std::min<int>(s->batch, KV_MAX_SEQS), group = a->heads_q / c->heads, most = most_tokens(s);
     p.prompt = kv_prompt_ok(a->dtype, nb, c->heads, c->d, (int64_t)most * group, span_of(c, s, a));
     if (p.prompt) {
         p.many = kv_prompt_plan(nb, c->heads, group, c->d, most, span_of(c, s, a));
         if (p.many.part) p.part_cta = cv.take<float>(p.many.part / 4);
     } else {
         p.rows = kv_rows_plan(nb, c->heads, group, c->d, a->dtype, most, span_of(c, s, a));
+        p.seqs = p.rows.seqs;
         if (p.rows.part_cta) p.part_cta = cv.take<float>(p.rows.part_cta / 4);
         if (p.rows.part_warp) p.part_warp = cv.take<float>(p.rows.part_warp / 4);
     }
@@ -236,8 +238,8 @@ int skm_kv_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn
     k.part_warp = p.part_warp;
     k.max_tiles = p.prompt ? p.many.max_tiles : (int)cdiv((int64_t)k.max_tokens * k.group, p.rows.rt);
     k.whole = p.rows.whole;
-    for (k.b0 = 0; k.b0 < s->batch; k.b0 += KV_MAX_SEQS) {
-        k.nb = std::min(s->batch - k.b0, KV_MAX_SEQS);
+    for (k.b0 = 0; k.b0 < s->batch; k.b0 += p.seqs) {
+        k.nb = std::min(s->batch - k.b0, p.seqs);
         if (p.prompt) {
             KvPromptPlan q = p.many;
             q.units = (int64_t)k.nb * k.heads * k.max_tiles;

@@ -11,7 +11,7 @@ namespace skm {
 
 constexpr int KV_B = SKM_KV_BLOCK;
 constexpr int KV_SMS = 152;
-// sequences whose prefix sums one launch keeps in shared memory; larger
+// sequences whose prefix sums one launch keeps in shared memory at most; larger
 // batches take several launches
 constexpr int KV_MAX_SEQS = 1024;
 
@@ -69,9 +69,9 @@ struct KvAttnArgs {
     int whole;         // one CTA a unit (a sequence's row tile and head)
 };
 
-// How one call is run: rows a tile holds, warps, ring stages, CTAs, workspace.
+// How one call is run: rows a tile holds, warps, ring stages, sequences of a launch, CTAs, workspace.
 struct KvRowsPlan {
-    int fp32, rt, nw, ns, whole;
+    int fp32, rt, nw, ns, whole, seqs;
     int64_t units, grid;
     size_t smem, part_cta, part_warp;  // bytes
 };
