@@ -216,7 +216,12 @@ int skm_version(void); /* major*10000 + minor*100 + patch */
  *  SKM_FAULT_WAIT       a tensor-core assignment launch starts with a 1 ms
  *                       bounded wait on a barrier that nothing arrives on: it
  *                       gives up before loading anything, raises its abort
- *                       flag, and skm_fit reports SKM_ERR_TIMEOUT.
+ *                       flag, and skm_fit reports SKM_ERR_TIMEOUT.  In
+ *                       skm_kv_attend (fp32 queries, or up to 32 rows a
+ *                       sequence), the first keys of one warp, numbered by
+ *                       the occurrences still armed, never count as arrived:
+ *                       its wait ends after 1 ms and the call's status word is
+ *                       set.
  * The environment variable SKM_FAULT=workspace|launch|status|wait arms one
  * occurrence when the library first checks.  Nothing faults the GPU: every
  * injected failure is a status the host reads.  Returns SKM_OK, or
@@ -832,8 +837,9 @@ int skm_kv_read(const skm_kv_cache *c, const skm_kv_seqs *s, int dtype, void *K,
  * queries (bf16 rows scaled by a power of two to f16), sums and softmax in fp32,
  * the probabilities rounded to f16; F32: fp32 arithmetic throughout.  Value
  * scales below 2^-80 count as 2^-80.
- *  status: device int32 or NULL; set to 1 when a bounded device wait gave up
- *  (some rows are then NaN or not written), otherwise left alone.
+ *  status: device int32 or NULL; set to 1 when a bounded device wait (2 s) gave up,
+ *  otherwise left alone.  The rows concerned, and some others, are then NaN; a row that
+ *  is not NaN is right.
  *  ws: skm_kv_attend_workspace_size(c, s, a) bytes, 256-byte aligned (0 bytes: may be
  *  NULL; it returns (size_t)-1 with skm_last_error() set for invalid arguments): at
  *  most 26 MB, and enough for every call with the same heads, d, heads_q and dtype and

@@ -81,7 +81,7 @@ __device__ __forceinline__ bool wait(uint32_t b, uint32_t parity, volatile int32
         if ((i & 63) == 0) {
             if (*gone) return false;
             asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-            if (t - t0 > WAIT_NS) {
+            if (t - t0 > KV_WAIT_NS) {
                 *gone = 1;
                 return false;
             }
@@ -704,7 +704,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         }
         if (!ok && issued) {  // what was issued ends before the memory is given up
             commit(drain, one);
-            bar_wait(drain, 0);
+            bar_wait(drain, 0, KV_WAIT_NS);
         }
     }
     __syncwarp();

@@ -322,10 +322,6 @@ struct Fp32Rows {
 #pragma unroll
             for (int b = 16; b > 0; b >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], b);
     }
-    __device__ __forceinline__ void poison() {
-#pragma unroll
-        for (int r = 0; r < R; ++r) l[r] = NAN;
-    }
     __device__ __forceinline__ void put(const KvAttnArgs &a, float *dst, int lane) const {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -584,10 +580,6 @@ struct MmaRows {
 #pragma unroll
                 for (int b = 4; b < 32; b <<= 1) l[t][i] += __shfl_xor_sync(0xffffffffu, l[t][i], b);
     }
-    __device__ __forceinline__ void poison() {
-#pragma unroll
-        for (int t = 0; t < NT; ++t) l[t][0] = l[t][1] = NAN;
-    }
     __device__ __forceinline__ void put(const KvAttnArgs &a, float *dst, int lane) const {
         const int g = lane >> 2, c = lane & 3;
 #pragma unroll
@@ -716,10 +708,60 @@ __device__ __forceinline__ int64_t holder(int64_t item, int64_t W, int64_t C) {
     return c;
 }
 
+// What this CTA (not the first) says of the unit [u0, u1) of W items that it found begun: parts 0 where
+// another CTA was the first to go on with it
+__device__ __forceinline__ Cut cut_of(int unit, const Seq &s, int64_t u0, int64_t u1, int64_t W, int64_t C) {
+    const int64_t c = blockIdx.x;
+    if (u0 < W * (c - 1) / C) return Cut{0, 0, 0, 0};
+    return Cut{unit, (int)(holder(u1 - 1, W, C) - c + 2), s.row0, s.n};
+}
+// part_cta: [grid][2] parts (of the unit that the CTA found begun, of the one open at its end), [grid] Cuts
+template <int RT>
+__device__ __forceinline__ float *part_of(const KvAttnArgs &a, bool begun) {
+    return a.part_cta + ((int64_t)blockIdx.x * 2 + (begun ? 0 : 1)) * part_floats<RT>(a.d);
+}
+template <int RT>
+__device__ __forceinline__ Cut *cuts_of(const KvAttnArgs &a, int ctas) {
+    return reinterpret_cast<Cut *>(a.part_cta + (int64_t)ctas * 2 * part_floats<RT>(a.d));
+}
+
+// A CTA of which a warp gave up its wait: that warp left items undone without a record, so all units of
+// the CTA's stretch [c0, c1) become NaN, those shared with other CTAs by a part whose l is NaN.
+template <int RT>
+__device__ __noinline__ void give_up(const KvAttnArgs &a, Line line, int64_t c0, int64_t c1) {
+    const int tid = threadIdx.x, n = blockDim.x;
+    const int64_t W = line.cum[line.nb];
+    if (tid == 0) {
+        if (a.status) *a.status = 1;
+        if (!a.whole) cuts_of<RT>(a, gridDim.x)[blockIdx.x] = Cut{0, 0, 0, 0};
+    }
+    for (int64_t item = c0; item < c1;) {
+        const int b = line.find(item);
+        const Seq s = line.seq[b];
+        const int unit = (int)((item - line.cum[b]) / s.cnt);
+        const int64_t u0 = line.cum[b] + (int64_t)unit * s.cnt, u1 = u0 + s.cnt;
+        const int h = a.by_heads.mod(unit), r0 = a.by_heads.div(unit) * RT, rows = min(RT, s.n * a.group - r0);
+        const bool all = u0 >= c0 && u1 <= c1;
+        for (int r = tid; r < rows; r += n) {
+            if (all) {
+                const int64_t row = row_index(a, s, h, r0 + r);
+                for (int i = 0; i < a.d; ++i) kv_store(a.out, row * a.d + i, NAN, a.dtype);
+                if (a.lse) a.lse[row] = NAN;
+            } else {
+                float *part = part_of<RT>(a, u0 < c0);
+                part[2 * r] = M_NONE, part[2 * r + 1] = NAN;
+            }
+        }
+        if (tid == 0 && u0 < c0) cuts_of<RT>(a, gridDim.x)[blockIdx.x] = cut_of(unit, s, u0, u1, W, active_ctas(W, n / 32, gridDim.x));
+        item = u1;
+    }
+}
+
 template <class Rows, int NW>
 __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_constant__ KvAttnArgs a, int ns) {
     constexpr int RT = Rows::RT;
     extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int gave_up;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // the sequences this CTA looks at, and its stretch of their line
     int nb = a.nb, b0 = a.b0, whole_unit = 0;
@@ -741,9 +783,12 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
 
     if (lane == 0)
         for (int i = 0; i < ns; ++i)
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bars + 8 * i), "r"(1) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bars + 8 * i),
+                         "r"(1 + (i == 0 && (int)blockIdx.x * NW + warp == a.stuck))
+                         : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (lane < 2) rec[2 * warp + lane].unit = -1;
+    if (tid == 0) gave_up = 0;
     line_up<RT>(a, b0, nb, cum, seq);
     const Line line{cum, seq, b0, nb};
     const int64_t W = cum[nb];
@@ -819,7 +864,6 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
         const auto leave = [&](bool last) {  // the open unit ends here, for this warp
             const Seq s = seq[useq];
             rows.close(lane);
-            if (!ok) rows.poison();
             const int64_t u0 = cum[useq] + (int64_t)uunit * s.cnt;
             const bool done = u0 >= i0 && u0 + s.cnt <= i1;
             if (done) {
@@ -855,7 +899,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
                 if (!((cur.todo >> i) & 1)) continue;
                 const int blk = ublk + i;
                 const float4 sc = win[32 * side + i];
-                if (!__all_sync(0xffffffffu, bar_wait(bars + 8 * take_at, phase))) {
+                if (!__all_sync(0xffffffffu, bar_wait(bars + 8 * take_at, phase, a.wait_ns))) {
                     ok = false;
                     break;
                 }
@@ -880,12 +924,12 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
         }
         if (!ok) {  // a copy did not arrive: let the others land before the memory is given up
             for (; flying > 0; --flying) {
-                bar_wait(bars + 8 * take_at, phase);
+                bar_wait(bars + 8 * take_at, phase, a.wait_ns);
                 if (++take_at == ns) take_at = 0, phase ^= 1u;
             }
-            if (lane == 0 && a.status) *a.status = 1;
+            if (lane == 0) gave_up = 1;
         }
-        open = leave(true);
+        open = ok && leave(true);
     }
     // a unit still open leaves its part where the warp's ring was
     const int64_t pf = part_floats<RT>(a.d);
@@ -896,10 +940,13 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
         if (lane == 0) rec[2 * warp + 1] = Record{useq, uunit, dst};
     }
     __syncthreads();
+    if (gave_up) {
+        give_up<RT>(a, line, c0, c1);
+        return;
+    }
     const Record mine = lane < 2 * NW ? rec[lane] : Record{0, -1, nullptr};
     // (by a warp that has no rows to merge)
-    Cut *cut = a.whole || warp != NW - 1 || lane != 0 ? nullptr
-                                                      : reinterpret_cast<Cut *>(a.part_cta + (int64_t)gridDim.x * 2 * pf) + blockIdx.x;
+    Cut *cut = a.whole || warp != NW - 1 || lane != 0 ? nullptr : cuts_of<RT>(a, gridDim.x) + blockIdx.x;
     if (cut) *cut = Cut{0, 0, 0, 0};
     for (uint32_t left = __ballot_sync(0xffffffffu, mine.unit >= 0); left;) {
         const int f = __ffs(left) - 1;
@@ -908,11 +955,8 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
         left &= ~same;
         const Seq s = seq[rs];
         const int64_t u0 = cum[rs] + (int64_t)ru * s.cnt, u1 = u0 + s.cnt;
-        float *dst = u0 >= c0 && u1 <= c1 ? nullptr : a.part_cta + ((int64_t)blockIdx.x * 2 + (u0 < c0 ? 0 : 1)) * pf;
-        if (cut && u0 < c0) {
-            const int64_t C = active_ctas(W, NW, gridDim.x), c = blockIdx.x;
-            if (u0 >= W * (c - 1) / C) *cut = Cut{ru, (int)(holder(u1 - 1, W, C) - c + 2), s.row0, s.n};
-        }
+        float *dst = u0 >= c0 && u1 <= c1 ? nullptr : part_of<RT>(a, u0 < c0);
+        if (cut && u0 < c0) *cut = cut_of(ru, s, u0, u1, W, active_ctas(W, NW, gridDim.x));
         merge_parts<RT, Rows::D4>(a, mine.part, same, s, ru, dst, warp, NW, lane);
     }
 }
@@ -928,7 +972,7 @@ __global__ void __launch_bounds__(128) kv_join_kernel(const __grid_constant__ Kv
     const int r = blockIdx.x % RT, c = blockIdx.x / RT;
     const int64_t pf = part_floats<RT>(a.d);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const Cut cut = reinterpret_cast<const Cut *>(a.part_cta + (int64_t)ctas * 2 * pf)[c];
+    const Cut cut = cuts_of<RT>(a, ctas)[c];
     const int unit = cut.unit, np = cut.parts;
     if (np == 0 || a.by_heads.div(unit) * RT + r >= cut.n * a.group) return;
     Seq s = {};

@@ -238,6 +238,12 @@ int skm_kv_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn
     k.part_warp = p.part_warp;
     k.max_tiles = p.prompt ? p.many.max_tiles : (int)cdiv((int64_t)k.max_tokens * k.group, p.rows.rt);
     k.whole = p.rows.whole;
+    k.wait_ns = KV_WAIT_NS;
+    k.stuck = -1;
+    if (!p.prompt && fault_take(SKM_FAULT_WAIT)) {
+        k.wait_ns = KV_WAIT_NS_INJECTED;
+        k.stuck = skm_fault_armed(SKM_FAULT_WAIT);
+    }
     for (k.b0 = 0; k.b0 < s->batch; k.b0 += p.seqs) {
         k.nb = std::min(s->batch - k.b0, p.seqs);
         if (p.prompt) {

@@ -67,7 +67,10 @@ struct KvAttnArgs {
     float *part_warp;  // [grid][warps] rows of the unit that a warp found begun and left
     int max_tiles;     // row tiles of the longest sequence
     int whole;         // one CTA a unit (a sequence's row tile and head)
+    unsigned long long wait_ns;  // k_kv_rows.cu: limit of a wait for copies
+    int stuck;         // ... the warp whose first keys never count as arrived (SKM_FAULT_WAIT), -1: none
 };
+constexpr unsigned long long KV_WAIT_NS = 2000000000ull, KV_WAIT_NS_INJECTED = 1000000ull;
 
 // How one call is run: rows a tile holds, warps, ring stages, sequences of a launch, CTAs, workspace.
 struct KvRowsPlan {

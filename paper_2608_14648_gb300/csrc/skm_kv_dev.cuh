@@ -7,7 +7,6 @@ namespace skm {
 
 namespace {
 
-constexpr unsigned long long WAIT_NS = 2000000000ull;
 constexpr float M_NONE = -3.0e38f;  // the reference before the first logit
 constexpr float M_SLACK = 15.0f, M_BELOW = 7.0f, M_MOST = 32768.0f;  // M_MOST = 2^M_SLACK
 constexpr float LN2 = 0.69314718055994531f;
@@ -29,8 +28,8 @@ __device__ __forceinline__ bool bar_try(uint32_t b, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-// false after WAIT_NS
-__device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity) {
+// false after `limit` ns
+__device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity, unsigned long long limit) {
     if (bar_try(b, parity)) return true;
     unsigned long long t0, t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
@@ -38,7 +37,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t b, uint32_t parity) {
         if (bar_try(b, parity)) return true;
         if ((i & 63) == 0) {
             asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-            if (t - t0 > WAIT_NS) return false;
+            if (t - t0 > limit) return false;
         }
     }
 }
