@@ -63,8 +63,9 @@ struct Lay {
     static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
     static constexpr int q = 0, k = NQ * QTILE, v = k + ST * TILE, info = v + ST * TILE;
     static constexpr int bars = info + INFO * KBLK * 16, slots = bars + 8 * (4 * ST + 14);  // TMEM address, a flag, the part's index
+    static constexpr int wild = slots + 32;  // a byte a row: its query holds infinities or NaN
     // one CTA an SM: it takes all of TMEM
-    static constexpr int bytes = slots + 32 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
+    static constexpr int bytes = wild + ROWS + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
     static constexpr uint32_t O = NQ * 2 * KT;  // TMEM column of O0
 };
 
@@ -219,12 +220,17 @@ __device__ __forceinline__ uint32_t bf16_f16(uint32_t w, float mul) {
 // A warp's 32 query rows to f16 in their tile's operand, DH / 8 lanes a row, all
 // reads issued before the first is used; returns what the logits of row `lane` are
 // multiplied by (k_kv_rows.cu: bf16 rows are scaled by a power of two).  tile0: the
-// tile's row 0, row0: the warp's first row of it.
+// tile's row 0, row0: the warp's first row of it.  Infinities and NaN enter as zeros (with their neighbours)
+// and are noted in `wild`, a byte a row of the tile: such a row becomes NaN at the end if it has seen a key.  (An
+// absent block's keys are zeros here: their products would be NaN where the row sees nothing.)
 template <int DH>
-__device__ __forceinline__ float load_rows(const KvAttnArgs &a, const Seq &s, int h, int tile0, int row0, uint32_t tile, int lane) {
+__device__ __forceinline__ float load_rows(const KvAttnArgs &a, const Seq &s, int h, int tile0, int row0, uint32_t tile, int lane,
+                                            uint8_t *wild) {
     constexpr int LPR = DH / 8, RPI = 32 / LPR, IT = 32 / RPI, AT_ONCE = IT < 16 ? IT : 16;
     const int li = lane % LPR, sub = lane / LPR;
     float fac = a.scale_log2;
+    wild[row0 + lane] = 0;
+    __syncwarp();
     for (int i0 = 0; i0 < IT; i0 += AT_ONCE) {
         uint4 raw[AT_ONCE];
 #pragma unroll
@@ -256,10 +262,20 @@ __device__ __forceinline__ float load_rows(const KvAttnArgs &a, const Seq &s, in
                 for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
                 const uint32_t ex = top >> 23, e = ex > 253 ? 253 : ex;
                 const bool fine = ex > 0 && ex < 255;
+                if (ex == 255) {
+                    w = make_uint4(0, 0, 0, 0);
+                    wild[row] = 1;
+                }
                 const float mul = fine ? __uint_as_float((254 - e) << 23) : 1.0f, back = fine ? __uint_as_float(e << 23) : 1.0f;
                 w = make_uint4(bf16_f16(w.x, mul), bf16_f16(w.y, mul), bf16_f16(w.z, mul), bf16_f16(w.w, mul));
                 const float mine = __shfl_sync(0xffffffffu, back, (lane % RPI) * LPR);
                 if (lane / RPI == i0 + i) fac = mine * a.scale_log2;
+            } else {  // (an exponent of ones carries into the sign's place)
+                const auto ends = [](uint32_t x) { return (x & 0x7c007c00u) + 0x04000400u; };
+                if ((ends(w.x) | ends(w.y) | ends(w.z) | ends(w.w)) & 0x80008000u) {
+                    w = make_uint4(0, 0, 0, 0);
+                    wild[row] = 1;
+                }
             }
             st_shared(tile + (li >> 3) * (QT * 128) + row * 128 + (((li & 7) ^ (row & 7)) << 4), w.x, w.y, w.z, w.w);
         }
@@ -375,7 +391,8 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     if (warp < CONV_WARP0) {  // ------------------------------------------ softmax
         const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row, nt = tiles_for(q);
         const bool in = r < rows;
-        const float fac = load_rows<DH>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE, lane);
+        const float fac = load_rows<DH>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE, lane,
+                                        smem + L::wild + q * QT);
         fence_async();
         __syncwarp();
         if (lane == 0) arrive(q_full);
@@ -507,6 +524,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                 l = NAN;
                 if (lane == 0 && a.status) *a.status = 1;
             }
+            if (smem[L::wild + q * QT + row] && l != 0.0f) l = NAN;
             float *part = parts ? parts + *part_index * prompt_part(ROWS, a.d) : nullptr;
             const int pr = q * QT + row;
             if (part) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);

@@ -1,5 +1,7 @@
 """The 8-bit key/value cache where sizes, values or events are out of the
 ordinary; the bounds are those of test_gpu_kv.py."""
+import math
+
 import pytest
 import torch
 from test_gpu_kv import DT, check_attend, i32, make_cache, make_table
@@ -63,3 +65,47 @@ def test_attend_that_gives_up_says_so(cuda_ok, heads, group, d, typ, rows, most)
     assert hit >= 1
     out, lse, fine = call()  # nothing is left of it
     assert fine == 0 and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("new", [1, 6, 100])
+@pytest.mark.parametrize("what", [math.nan, math.inf])
+def test_attend_rows_that_see_nothing_may_hold_anything(cuda_ok, typ, new, what):
+    """Padded rows: all pages of a sequence absent, or no position left to see, whatever the queries are."""
+    import paper_2608_14648_gb300 as skm
+
+    c = make_cache(2, 64, 16, 40, 31)
+    table = torch.full((4, 13), -1, dtype=torch.int32)
+    table[0], table[2], table[3, 3:] = torch.arange(13), torch.arange(13, 26), torch.arange(26, 36)
+    Q = torch.randn(4 * new, 4, 64, generator=torch.Generator().manual_seed(32)).to(DT[typ])
+    clean = Q.clone()
+    Q[new: 2 * new] = what  # no page
+    Q[2 * new: 3 * new] = what  # no token
+    Q[3 * new: 3 * new + new // 2] = what  # the first pages are absent, and these rows see no others
+    args = table.cuda(), i32([200, 200, 0, 48 + new - new // 2]), i32([0, new, 2 * new, 3 * new, 4 * new])
+    out, lse = skm.skm_kv_attend(c, *args, Q.cuda(), new, 200, want_lse=True)
+    want, want_lse = skm.skm_kv_attend(c, *args, clean.cuda(), new, 200, want_lse=True)
+    nothing = slice(new, 3 * new + new // 2)
+    assert (out[nothing] == 0).all() and torch.isneginf(lse[nothing]).all()
+    assert torch.isfinite(want).all() and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("typ", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("new", [1, 6, 100])
+def test_attend_nan_in_a_query_stays_in_its_row(cuda_ok, typ, new):
+    import paper_2608_14648_gb300 as skm
+
+    c = make_cache(2, 64, 16, 40, 33)
+    table = torch.arange(26, dtype=torch.int32).view(2, 13)
+    table[1, 4] = -1  # an absent page among the others
+    Q = torch.randn(2 * new, 4, 64, generator=torch.Generator().manual_seed(34)).to(DT[typ])
+    args = table.cuda(), i32([200, 150]), i32([0, new, 2 * new])
+    want, want_lse = skm.skm_kv_attend(c, *args, Q.cuda(), new, 200, want_lse=True)
+    hit = torch.zeros(2 * new, 4, dtype=torch.bool)
+    for row, head, dim in ((0, 1, 63), (new, 0, 0), (2 * new - 1, 3, 17)):
+        Q[row, head, dim] = math.nan
+        hit[row, head] = True
+    out, lse = skm.skm_kv_attend(c, *args, Q.cuda(), new, 200, want_lse=True)
+    hit = hit.cuda()
+    assert torch.isnan(out[hit]).all() and torch.isnan(lse[hit]).all()
+    assert torch.equal(out[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
