@@ -834,7 +834,8 @@ int skm_kv_read(const skm_kv_cache *c, const skm_kv_seqs *s, int dtype, void *K,
  *  Q   dtype rows [tokens] of [heads_q][d], d contiguous, strides in elements
  *  out dtype [tokens][heads_q][d], lse float32 [tokens][heads_q] or NULL: contiguous
  * dtype BF16 or F16: products on tensor cores of codes (exact in f16) and of the
- * queries (bf16 rows scaled by a power of two to f16), sums and softmax in fp32,
+ * queries (bf16 rows scaled by a power of two to f16, where elements below 2^-32 of
+ * the row's largest lose bits and those below 2^-40 vanish), sums and softmax in fp32,
  * the probabilities rounded to f16; F32: fp32 arithmetic throughout.  Value
  * scales below 2^-80 count as 2^-80.
  *  status: device int32 or NULL; set to 1 when a bounded device wait (2 s) gave up,

@@ -219,7 +219,7 @@ __device__ __forceinline__ uint32_t bf16_f16(uint32_t w, float mul) {
 
 // A warp's 32 query rows to f16 in their tile's operand, DH / 8 lanes a row, all
 // reads issued before the first is used; returns what the logits of row `lane` are
-// multiplied by (k_kv_rows.cu: bf16 rows are scaled by a power of two).  tile0: the
+// multiplied by (bf16 rows are scaled by a power of two: to_f16).  tile0: the
 // tile's row 0, row0: the warp's first row of it.  Infinities and NaN enter as zeros (with their neighbours)
 // and are noted in `wild`, a byte a row of the tile: such a row becomes NaN at the end if it has seen a key.  (An
 // absent block's keys are zeros here: their products would be NaN where the row sees nothing.)
@@ -260,15 +260,13 @@ __device__ __forceinline__ float load_rows(const KvAttnArgs &a, const Seq &s, in
                 for (int k = 0; k < 4; ++k) top = max(max(top, u[k] << 16 & 0x7fff0000u), u[k] & 0x7fff0000u);
 #pragma unroll
                 for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const uint32_t ex = top >> 23, e = ex > 253 ? 253 : ex;
-                const bool fine = ex > 0 && ex < 255;
-                if (ex == 255) {
+                const Pow2 by = to_f16(top >> 23);
+                if (top >= 0x7f800000u) {
                     w = make_uint4(0, 0, 0, 0);
                     wild[row] = 1;
                 }
-                const float mul = fine ? __uint_as_float((254 - e) << 23) : 1.0f, back = fine ? __uint_as_float(e << 23) : 1.0f;
-                w = make_uint4(bf16_f16(w.x, mul), bf16_f16(w.y, mul), bf16_f16(w.z, mul), bf16_f16(w.w, mul));
-                const float mine = __shfl_sync(0xffffffffu, back, (lane % RPI) * LPR);
+                w = make_uint4(bf16_f16(w.x, by.mul), bf16_f16(w.y, by.mul), bf16_f16(w.z, by.mul), bf16_f16(w.w, by.mul));
+                const float mine = __shfl_sync(0xffffffffu, by.back, (lane % RPI) * LPR);
                 if (lane / RPI == i0 + i) fac = mine * a.scale_log2;
             } else {  // (an exponent of ones carries into the sign's place)
                 const auto ends = [](uint32_t x) { return (x & 0x7c007c00u) + 0x04000400u; };

@@ -392,8 +392,7 @@ __device__ __forceinline__ uint16_t bits16(float v, bool bf) {
 // the dims of a 16-dim chunk, lane column c holds 4c .. 4c + 3 (the queries
 // are laid out to match); of the tokens, the cache's byte order makes it 2c,
 // 2c + 1, 2c + 8, 2c + 9, the operand's own.  p^T comes from S^T by movmatrix.
-// bf16 queries become f16 exactly after scaling a row by a power of two (values
-// below 2^-25 of the row's largest, whose products round away, aside).
+// bf16 queries become f16 after scaling a row by a power of two (to_f16).
 // DC: 16-dim chunks at most (FULL: exactly), NT: tiles of 8 rows.
 template <int DC, int NT, bool FULL>
 struct MmaRows {
@@ -443,12 +442,8 @@ struct MmaRows {
                 }
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const uint32_t ex = top >> 23;
-                if (ex > 0 && ex < 255) {
-                    const uint32_t e = ex > 253 ? 253 : ex;
-                    mul = __uint_as_float((254 - e) << 23);
-                    back = __uint_as_float(e << 23);
-                }
+                const Pow2 by = to_f16(top >> 23);
+                mul = by.mul, back = by.back;
             }
 #pragma unroll
             for (int w = 0; w < DC; ++w) {

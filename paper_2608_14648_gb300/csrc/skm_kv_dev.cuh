@@ -95,6 +95,18 @@ __device__ __forceinline__ float4 value_scale(float2 sc) {
     return make_float4(sc.x, lg, inv, 0.0f);
 }
 
+// A bf16 query row becomes f16 by a power of two that takes its largest element to [2^15, 2^16) (65280 at
+// most, of f16's 65504; the products of 256 dims with codes stay below 2^32).  That is exact for elements of 2^-32 of the
+// largest and more: the eight bits of one lie above 2^-24, f16's smallest number.  ex: the largest
+// element's exponent field
+struct Pow2 {
+    float mul, back;
+};
+__device__ __forceinline__ Pow2 to_f16(uint32_t ex) {
+    const uint32_t e = max(ex, 1u), up = min(e - 1u, 15u);
+    return Pow2{__uint_as_float((254u - e + up) << 23), __uint_as_float((e - up) << 23)};
+}
+
 // codes of bytes 0, 1 / 2, 3 of a word as two f16: 1024 + u as bits, minus 1152
 __device__ __forceinline__ uint32_t codes_f16(uint32_t word, uint32_t sel) {
     const uint32_t x = __byte_perm(word, 0x64646464u, sel);

@@ -109,3 +109,30 @@ def test_attend_nan_in_a_query_stays_in_its_row(cuda_ok, typ, new):
     hit = hit.cuda()
     assert torch.isnan(out[hit]).all() and torch.isnan(lse[hit]).all()
     assert torch.equal(out[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
+
+
+@pytest.mark.parametrize("new", [1, 8, 100])
+@pytest.mark.parametrize("large", [2.0**14, 2.0**20, -1.9921875 * 2.0**21])
+def test_attend_bf16_queries_of_unequal_elements(cuda_ok, monkeypatch, new, large):
+    """An element far above the others, on a dim where all keys are 0: the logits are the others'.  Elements of 2^-32 of the
+    row's largest and more take part exactly, so the bound for exact queries holds."""
+    def spoil(c):
+        c.k.view(c.pages, c.heads, -1, c.d // 16, 16, 16)[..., 0, :, 0] = 128
+
+    draw = torch.randn
+
+    def randn(*size, **kw):
+        x = draw(*size, **kw)
+        x = torch.where(x.abs() < 2.0**-10, torch.full_like(x, 2.0**-10), x)
+        x[..., 0] = large
+        return x
+
+    monkeypatch.setattr(torch, "randn", randn)
+    check_attend(1, 4, 64, 16, "bf16", [(90, new), (50, new)], spoil=spoil)
+
+
+@pytest.mark.parametrize("new", [1, 100])
+@pytest.mark.parametrize("size,scale", [(1e-38, 2e37), (1e-39, 2e38), (3e37, 1e-38), (5e37, 1e-38), (0.0, 1.0)])
+def test_attend_bf16_queries_at_the_ends_of_the_range(cuda_ok, new, size, scale):
+    """Rows of subnormal elements, rows whose largest one is near the largest bf16, rows of zeros."""
+    check_attend(1, 4, 64, 16, "bf16", [(90, new), (50, new)], spread=size, scale=scale)
