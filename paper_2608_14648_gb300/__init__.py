@@ -743,7 +743,8 @@ KV_BLOCK = 16
 class KVCache:
     """The tensors of one skm_kv_cache: uint8 codes k and v [pages, heads,
     page / 16, 16 d] and float32 scales [pages, heads, page / 16, 2] (layouts in
-    include/skm.h), allocated here for `pages` pages unless given."""
+    include/skm.h), allocated here for `pages` pages unless given.  Calls on it
+    are made with its device current (torch.cuda.device)."""
 
     def __init__(self, heads, d, page, k=None, v=None, scales=None, pages=None, device="cuda"):
         if k is None:
@@ -788,6 +789,9 @@ def _kv_seqs(cache, table, pos, cu, tokens, max_tokens, max_len=0):
     index = cache.index
     if index < 0:
         raise ValueError("the cache is not on a GPU")
+    current = torch._C._cuda_getDevice()
+    if current != index:  # the library launches on the current device, where a default stream's handle (0) belongs to it
+        raise ValueError(f"the cache is on cuda:{index}, but the current device is cuda:{current}")
     if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_contiguous() or table.get_device() != index:
         raise ValueError("table must be a contiguous int32 tensor [batch, cols] on the cache's device")
     batch, cols = table.shape

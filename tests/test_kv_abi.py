@@ -146,3 +146,46 @@ def test_a_workspace_serves_smaller_calls(skm, d, dtype):
                         skm.skm_inject_fault(skm.FAULT_WORKSPACE, 0)
                         text = skm.lib().skm_last_error().decode()
                         assert rc == NO_MEMORY and int(text.split(",")[1].split()[0]) <= need, (b, m, n, window, text, need)
+
+
+class OnDevice:
+    """What the binding asks of a tensor, on a device that need not exist."""
+
+    def __init__(self, t, index):
+        self.t, self.index = t, index
+
+    def get_device(self):
+        return self.index
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def test_binding_refuses_another_current_device(skm, monkeypatch):
+    # a launch goes to the current device: with the cache on another one its pointers would be foreign there
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: calls.append(name) or 0
+
+    monkeypatch.setattr(skm, "lib", Library)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    c = skm.KVCache(2, 64, 32, pages=4, device="cpu")
+    c.index = 1
+    on = lambda t: OnDevice(t, 1)  # noqa: E731
+    i32 = lambda *x: on(torch.tensor(x, dtype=torch.int32))  # noqa: E731
+    table, pos, cu = on(torch.tensor([[0, 1]], dtype=torch.int32)), i32(0), i32(0, 3)
+    rows = lambda heads: on(torch.zeros(3, heads, 64))  # noqa: E731
+    ops = [lambda: skm.skm_kv_write(c, table, pos, cu, rows(2), rows(2), 3),
+           lambda: skm.skm_kv_read(c, table, pos, cu, 3, 3, skm.DTYPE_F32, out=(rows(2), None)),
+           lambda: skm.skm_kv_attend(c, table, pos, cu, rows(4), 3, 10, out=rows(4), ws=rows(4))]
+    for current, made in ((0, 0), (1, 3)):
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current, raising=False)
+        for op in ops:
+            if current == 1:
+                op()
+            else:
+                with pytest.raises(ValueError, match="cuda:1.*cuda:0"):
+                    op()
+        assert len(calls) == made
