@@ -166,9 +166,9 @@ int skm_kv_read(const skm_kv_cache *c, const skm_kv_seqs *s, int dtype, void *K,
     SKM_TRY(check_seqs(c, s));
     SKM_TRY(check_dtype(dtype));
     SKM_TRY(check_grid(c, s));
+    if (most_tokens(s) == 0) return SKM_OK;
     if (!K && !V) return set_error(SKM_ERR_INVALID_ARG, "K and V are both NULL");
     if (!aligned(K, 16) || !aligned(V, 16)) return set_error(SKM_ERR_INVALID_ARG, "K and V must be 16-byte aligned");
-    if (most_tokens(s) == 0) return SKM_OK;
     KvCacheArgs a = cache_args(c, s);
     a.outk = K;
     a.outv = V;

@@ -136,3 +136,13 @@ def test_attend_bf16_queries_of_unequal_elements(cuda_ok, monkeypatch, new, larg
 def test_attend_bf16_queries_at_the_ends_of_the_range(cuda_ok, new, size, scale):
     """Rows of subnormal elements, rows whose largest one is near the largest bf16, rows of zeros."""
     check_attend(1, 4, 64, 16, "bf16", [(90, new), (50, new)], spread=size, scale=scale)
+
+
+def test_write_and_read_no_rows(cuda_ok):
+    import paper_2608_14648_gb300 as skm
+
+    c = make_cache(2, 64, 16, 2, 1)
+    table, pos, cu = i32([[0, 1]]), i32([20]), i32([0, 0])
+    skm.skm_kv_write(c, table, pos, cu, *torch.empty(2, 0, 2, 64, device="cuda"), 0)
+    K, V = skm.skm_kv_read(c, table, pos, cu, 0, 0)
+    assert K.shape == V.shape == (0, 2, 64)

@@ -189,3 +189,9 @@ def test_binding_refuses_another_current_device(skm, monkeypatch):
                 with pytest.raises(ValueError, match="cuda:1.*cuda:0"):
                     op()
         assert len(calls) == made
+
+
+def test_reading_no_rows_is_fine_without_tensors(skm):
+    # (an empty tensor has no address)
+    for change in (dict(tokens=0), dict(max_tokens=0)):
+        assert call(skm, "read", cache(skm), seqs(skm, **change), K=None, V=None) == 0
