@@ -87,13 +87,17 @@ class Server:
             self.state.copy_(y)
             self.start.copy_(length)
 
+        # warm up with all pages absent: a token written here could raise the scale of the block that holds a
+        # prompt's last tokens, and their codes would be rounded once more
+        at, pages = self.start.clone(), self.table.clone()
+        self.table.fill_(-1)
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
-        at = self.start.clone()
         with torch.cuda.stream(side):
-            step()  # warm up; the token it appended is overwritten by the first real one
+            step()
         torch.cuda.current_stream().wait_stream(side)
         self.start.copy_(at)
+        self.table.copy_(pages)
         self.graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(self.graph):
             step()

@@ -25,3 +25,20 @@ def test_serving_example(cuda_ok, batch, prompt, chunk, steps):
         d2 = ((keys[:, h] - C.double()[assign.long()]) ** 2).sum()
         assert wcss == pytest.approx(float(d2), rel=1e-4)
         assert wcss <= float(((keys[:, h] - keys[:, h].mean(0)) ** 2).sum()) * (1 + 1e-4)
+
+
+def test_capturing_the_step_leaves_the_caches_as_they_were(cuda_ok):
+    import kv_serve
+
+    lengths = [20, 33, 41]  # last blocks of 4, 1 and 9 tokens
+    server = kv_serve.Server(3, 60)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    server.prompts([torch.randn(n, 256, generator=g, device="cuda").to(torch.bfloat16) for n in lengths], 16)
+    was = [[t.clone() for t in (lay.cache.k, lay.cache.v, lay.cache.scales)] for lay in server.layers]
+    table = server.table.clone()
+    server.capture()
+    torch.cuda.synchronize()
+    assert server.start.tolist() == lengths and torch.equal(server.table, table)
+    for lay, held in zip(server.layers, was):
+        for t, w in zip((lay.cache.k, lay.cache.v, lay.cache.scales), held):
+            assert torch.equal(t.view(torch.uint8), w.view(torch.uint8))
