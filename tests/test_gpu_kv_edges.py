@@ -3,8 +3,9 @@ ordinary; the bounds are those of test_gpu_kv.py."""
 import math
 
 import pytest
+import test_gpu_kv
 import torch
-from test_gpu_kv import DT, check_attend, i32, make_cache, make_table
+from test_gpu_kv import DT, check_attend, i32, make_cache, make_table, same, write_case
 
 pytestmark = pytest.mark.gpu
 
@@ -146,3 +147,87 @@ def test_write_and_read_no_rows(cuda_ok):
     skm.skm_kv_write(c, table, pos, cu, *torch.empty(2, 0, 2, 64, device="cuda"), 0)
     K, V = skm.skm_kv_read(c, table, pos, cu, 0, 0)
     assert K.shape == V.shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("heads,group,d,page,typ,seqs,causal,window", [
+    (20, 1, 64, 16, "f16", [(0, 600), (300, 257), (17, 40)], True, 0),      # 180 units of 9 row tiles, ranked by their lengths
+    (20, 1, 64, 16, "bf16", [(0, 600), (300, 257), (17, 40)], True, 200),
+    (10, 4, 128, 64, "bf16", [(100, 200), (0, 130), (500, 64), (900, 1)], True, 0),  # 160, d = 128
+    (16, 1, 256, 32, "bf16", [(0, 300), (200, 129), (1290, 33)], False, 0),  # 144 of 128 rows
+    (16, 1, 192, 32, "f16", [(0, 300), (200, 129), (1290, 33), (5, 60)], True, 0),
+    (1, 1, 96, 16, "bf16", [(i * 7 % 100, 33 + i % 30) for i in range(300)], True, 0),  # 300 row tiles: too many to rank
+    (1, 2, 64, 16, "f16", [(i * 7 % 50, 1 + i % 20) for i in range(1100)], True, 0),  # two launches
+])
+def test_attend_many_rows_in_several_waves(cuda_ok, heads, group, d, page, typ, seqs, causal, window):
+    check_attend(heads, group, d, page, typ, seqs, causal, window)
+
+
+def test_attend_a_prompt_among_single_tokens(cuda_ok):
+    check_attend(4, 4, 128, 64, "bf16", [(300, 1), (700, 300), (40, 1), (1500, 1), (0, 1)] + [(90 * i, 1) for i in range(30)])
+
+
+@pytest.mark.parametrize("typ,group,new", [("bf16", 8, 1), ("f16", 5, 2), ("f32", 1, 1), ("f32", 2, 3)])
+@pytest.mark.parametrize("d", [144, 192, 256])
+def test_attend_wide_heads_split_over_the_whole_gpu(cuda_ok, typ, group, new, d):
+    """d > 128 in shared stretches: units cut between warps and CTAs, whose sums a lane joins in two vectors."""
+    check_attend(2, group, d, 64, typ, [(6000, new), (0, new), (3111, new), (40, new)])
+    check_attend(1, group, d, 16, typ, [(i * 11 % 70, new) for i in range(160)])
+
+
+class HeldRows(test_gpu_kv.Held):
+    """Held, for sequences of a call that have no rows."""
+
+    def write(self, table, start, cu, K, V):
+        for b, at in enumerate(start):
+            rows = slice(cu[b], cu[b + 1])
+            if cu[b + 1] > cu[b]:
+                super().write(table[b: b + 1], [at], [0, cu[b + 1] - cu[b]], K[rows], V[rows])
+
+
+@pytest.mark.parametrize("heads,d,page,typ", [(8, 128, 64, "bf16"), (3, 96, 32, "f16"), (2, 256, 16, "f32"), (5, 16, 16, "bf16")])
+def test_write_and_read_large_batches(cuda_ok, monkeypatch, heads, d, page, typ):
+    """More than 32 sequences: their blocks are placed in rows of the longest's, one or none reached by the others."""
+    import paper_2608_14648_gb300 as skm
+
+    monkeypatch.setattr(test_gpu_kv, "Held", HeldRows)
+    seqs = [(i * 13 % 50, (i * 29 % 71) * (i % 5 > 0)) for i in range(45)] + [(15, 1), (16, 200), (31, 2)]
+    c, table, start, cu, want, most = write_case(heads, d, page, typ, seqs, fused=True)
+    same(c, want)
+    for dt, code in ((torch.float32, skm.DTYPE_F32), (torch.bfloat16, skm.DTYPE_BF16), (torch.float16, skm.DTYPE_F16)):
+        got = skm.skm_kv_read(c, table.cuda(), i32(start), i32(cu), cu[-1], most, code)
+        for name, x in zip("kv", got):
+            ref = torch.cat([want.values(name, table, b, s, s + n, torch.float32)[0] for b, (s, n) in enumerate(seqs)])
+            assert torch.equal(x.cpu(), ref.to(dt))
+
+
+@pytest.mark.parametrize("grow", [1.0, 1.02, 1.5])
+def test_values_of_a_block_that_grows(cuda_ok, grow):
+    """Single tokens, each up to `grow` times larger: a value read back is within half a step of every scale that it was rounded
+    at, the block's at its own write and each larger one since, and so within (g + 1) / 2 steps of the last one after
+    g growths.  (A scale and a ratio are rounded to fp32, a code of up to 127 by 127 2^-23 of a step in all each time.)"""
+    import paper_2608_14648_gb300 as skm
+
+    heads, d, n = 2, 64, 48
+    c = make_cache(heads, d, 16, 4, 41)
+    table = make_table(1, 4, 4, 41).cuda()
+    g = torch.Generator().manual_seed(42)
+    x = torch.randn(n, 2 * heads, d, generator=g) * grow ** (torch.arange(n) % 16)[:, None, None]
+    dev = x.cuda()
+    bound = torch.zeros(n, 2, heads, dtype=torch.float64)
+    growths = torch.zeros(n, 2, heads)
+    scale = torch.zeros(2, heads, dtype=torch.float64)
+    for t in range(n):
+        skm.skm_kv_write(c, table, i32([t]), i32([0, 1]), dev[t: t + 1, :heads], dev[t: t + 1, heads:], 1)
+        was, scale = scale, c.scales[int(table[0, t // 16]), :, 0].T.cpu().double()
+        step = (0.5 + 127 * 2.0**-23) * scale
+        bound[t] = step
+        if t % 16:
+            grew = scale > was
+            bound[t - t % 16: t] += torch.where(grew, step, torch.zeros(()))
+            growths[t - t % 16: t] += grew
+    got = torch.stack(skm.skm_kv_read(c, table, i32([0]), i32([0, n]), n, n, skm.DTYPE_F32), 1).cpu().double()
+    off = (got - x.view(n, 2, heads, d).double()).abs().amax(-1)
+    assert (off <= bound).all()
+    last = torch.stack([c.scales[int(p), :, 0].T for p in table[0, :3]]).cpu().double().repeat_interleave(16, 0)
+    assert (off <= (growths + 1) * (0.5 + 127 * 2.0**-23) * last).all()
+    assert growths.max() >= 2
