@@ -836,8 +836,11 @@ int skm_kv_read(const skm_kv_cache *c, const skm_kv_seqs *s, int dtype, void *K,
  * dtype BF16 or F16: products on tensor cores of codes (exact in f16) and of the
  * queries (bf16 rows scaled by a power of two to f16, where elements below 2^-32 of
  * the row's largest lose bits and those below 2^-40 vanish), sums and softmax in fp32,
- * the probabilities rounded to f16; F32: fp32 arithmetic throughout.  Value
- * scales below 2^-80 count as 2^-80.
+ * the probabilities rounded to f16; F32: fp32 arithmetic throughout (2^x of weights, log2
+ * and reciprocal of value scales approximate, to 2^-22).  Weights carry the value scale.
+ * So value scales below 2^-80 count as 2^-80, and where a row's value scales, so counted, lie
+ * more than 2^109 apart, the blocks of the smaller ones lose weight: a block of zeros next to
+ * values up to 2^35 has its full weight, next to values of 2^57 it has none.
  *  status: device int32 or NULL; set to 1 when a bounded device wait (2 s) gave up,
  *  otherwise left alone.  The rows concerned, and some others, are then NaN; a row that
  *  is not NaN is right.

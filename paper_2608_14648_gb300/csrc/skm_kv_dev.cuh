@@ -86,7 +86,9 @@ __device__ __forceinline__ int64_t row_index(const KvAttnArgs &a, const Seq &s, 
 // A block's scales as attention uses them: (key scale, log2 of the value scale,
 // 1 / value scale, 0).  Weights carry the value scale, so scales too far apart would push
 // the smaller ones' weights out of fp32: scales below 2^-80 (values below 1e-22,
-// blocks of zeros among them) count as 2^-80.
+// blocks of zeros among them) count as 2^-80.  (The reference lies at least 7 below the row's largest
+// weight, so that one is 2^7 or more; fp32 ends at 2^-126, and weights down to 2^-24 of the largest count
+// in a row's sum: scales may lie 2^(126 + 7 - 24) = 2^109 apart.)
 __device__ __forceinline__ float4 value_scale(float2 sc) {
     const float vs = fmaxf(sc.y, 8.271806e-25f);
     float lg, inv;

@@ -231,3 +231,14 @@ def test_values_of_a_block_that_grows(cuda_ok, grow):
     last = torch.stack([c.scales[int(p), :, 0].T for p in table[0, :3]]).cpu().double().repeat_interleave(16, 0)
     assert (off <= (growths + 1) * (0.5 + 127 * 2.0**-23) * last).all()
     assert growths.max() >= 2
+
+
+@pytest.mark.parametrize("typ,new", [("bf16", 1), ("bf16", 20), ("bf16", 100), ("f32", 1)])
+def test_attend_value_scales_to_the_limit(cuda_ok, typ, new):
+    """Value scales of 2^29 next to blocks of zeros (counted as 2^-80), 2^109 apart: both have their full weights."""
+    def spoil(c):
+        c.scales[0::3, :, :, 1] = 0.0
+        c.v[0::3] = 128
+        c.scales[1::3, :, :, 1] = 2.0**29
+
+    check_attend(2, 4, 64, 16, typ, [(300, new), (61, new)], spoil=spoil)
