@@ -812,7 +812,9 @@ typedef struct skm_kv_seqs {
  * before the first new one, fl32(a fl32(1/127))), code = 128 +
  * clip(round(x / scale), -127, 127) in fp32, rounding half to even (NaN: 128;
  * scale 0: 128).  When the scale of a block that holds tokens grows, their
- * codes become 128 + round((code - 128) fl32(old / scale)).  Positions from
+ * codes become 128 + round((code - 128) fl32(old / scale)): a value read back is within half a scale of
+ * what was written where its block was written at once, and within (g + 1) / 2 scales where the
+ * block's scale has grown g times since (token by token up to 15 times).  Positions from
  * pos[b] on that were written before are overwritten (a rolled back tail).  Two
  * sequences of a call must not write to the same page.  One kernel, no
  * workspace.  Asynchronous. */
@@ -848,7 +850,10 @@ int skm_kv_read(const skm_kv_cache *c, const skm_kv_seqs *s, int dtype, void *K,
  *  NULL; it returns (size_t)-1 with skm_last_error() set for invalid arguments): at
  *  most 26 MB, and enough for every call with the same heads, d, heads_q and dtype and
  *  no larger batch, tokens, max_tokens and max_len.
- * The result does not depend on timing.  Asynchronous. */
+ * The result does not depend on timing.  Asynchronous.
+ * One kernel serves all sequences of a call, chosen by max_tokens and max_len.  A prompt chunk among
+ * single tokens is faster as a call of its own: two calls on the same Q and out, each with its own
+ * part of table, pos and cu (cu's values stay as they are). */
 typedef struct skm_kv_attn {
     int32_t heads_q;   /* a multiple of the cache's heads */
     int32_t dtype;

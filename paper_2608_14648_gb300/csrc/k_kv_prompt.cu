@@ -31,13 +31,14 @@
 // kv_prompt_join_kernel merges the parts in order.
 //
 // Measured (GB300): chunks of 2048 tokens of two prompts behind 6144, 32 query heads
-// over 8 of 128, bf16: 293 us = 1150 TFLOP/s, 60% of a cuBLAS product; 4 whole prompts of up to
-// 4096, 16 heads of 64, f16: 123 us (half the flops a logit, and key tiles on the
+// over 8 of 128, bf16: 298 us = 1130 TFLOP/s, 59% of a cuBLAS product; 4 whole prompts of up to
+// 4096, 16 heads of 64, f16: 124 us (half the flops a logit, and key tiles on the
 // diagonal).  A tile of 256 rows x 64 keys takes some 2000 clocks.  What bounds it is the
-// softmax warps' chain of latencies, two warps a scheduler: without the
+// softmax warps' chain of latencies, two warps a scheduler: in copies of 290 us, without the
 // exponentials, the conversion of codes or P's way back the time stays within 2%, with three
 // quarters of the products gone it is 276 us, without exponentials and conversion as well
-// 248.  So reads
+// 248.  The loops are at the limit of 128 registers, and a few instructions outside them move the time by 2%:
+// noting query rows with infinities or NaN costs 5 us.  So reads
 // that a wait would hold up come before it (a block's scales: 11 us), the converters
 // leave issue slots free (6 us), and what runs seldom stays in its branch.  More logits a
 // wait (367 us) or asking for the next tile's earlier (311) made it slower.
@@ -51,7 +52,9 @@ constexpr int QT = 128, KT = 64, KBLK = KT / KV_B;  // rows of a tile, keys of a
 constexpr int CONV = 7;  // converter warps
 constexpr int RANKED = 256;
 constexpr float W_MOST = 65000.0f;  // a block's sum of weights: above it one may pass the largest f16
-constexpr int INFO = 8;  // tiles whose scales are kept: those of the K ring and those its softmax still reads
+// tiles whose scales are kept.  A K stage is free once its product is through, which is issued when the softmax has
+// handed over the tile two before: tile j + ST (at most 4) comes while it reads tile j - 1 at the earliest, 5 behind
+constexpr int INFO = 8;
 
 // DH: dims, padded to 64, 128 or 256
 template <int DH>
@@ -567,7 +570,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             if (in && !part && a.lse) a.lse[at] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
         }
     } else if (warp < MMA_WARP) {  // ------------------------------------- converters
-        // tasks: per tile 8 blocks of keys, then 8 of values; warp w takes w, w + 7, ...
+        // tasks: per tile KBLK blocks of keys, then KBLK of values; warp w takes w, w + CONV, ...
         const int tasks = n * 2 * KBLK, cw = warp - CONV_WARP0;
         constexpr int NV = DH / 32;
         struct Ahead {  // 32 of the warp's tasks, one a lane
@@ -794,9 +797,10 @@ cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t 
 // holds: at d = 128, 40 rows of 2 sequences that see 900 keys take 22 us here and 24 there, of
 // 16 (8 heads) 26 and 46.  d > 128, where this kernel takes longer to start (a CTA
 // converts 64 KB of keys and values before its first product is through): not while the
-// other one has an SM for every unit and few keys a unit.  At d = 256, 40 rows of 16 sequences, 2
-// heads: 905 keys 29 us here and 23 there; 2 sequences, 1905 keys 27 and 33; 16
-// sequences, 8 heads, 905 keys 35 and 62.
+// other one has an SM for every unit and few keys a unit.  At d = 256 (alone in a graph), 40 rows of 16
+// sequences, 2 heads (96 units there): 905 keys 26.7 us here and 21.7 there, 1280 24.8 and 25.3, 1400 26.1 and
+// 26.3, 1905 28.2 and 32.1; 16 sequences, 8 heads, 905 keys 35 and 62.  Of 12 units the other one stays ahead (1905 keys
+// 24.8 and 18.5, in shared stretches), which the rule does not use.
 bool kv_prompt_ok(int dtype, int nb, int heads, int d, int64_t rows, int64_t span) {
     if (dtype == SKM_DTYPE_F32 || rows <= KV_ROWS_MOST) return false;
     return d <= 128 || span > 1280 || (int64_t)nb * heads * cdiv(rows, (int64_t)16) > KV_SMS;

@@ -1,5 +1,6 @@
 // Attention over the 8-bit cache for few query rows (single tokens, a few
-// tokens): the codes cross HBM once and everything else hides behind them.
+// tokens): one row tile a head, whose codes cross HBM once, and everything else hides behind
+// them.  (More rows than a tile, fp32 ones or 16-bit ones of d > 128: each tile fetches them again.)
 //
 // Work.  A unit is a sequence's tile of RT query rows (token-major, then the
 // heads of one group) and a key/value head; its blocks of 16 tokens are its

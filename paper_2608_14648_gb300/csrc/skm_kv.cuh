@@ -16,7 +16,8 @@ constexpr int KV_SMS = 152;
 constexpr int KV_MAX_SEQS = 1024;
 
 // n / d for 0 <= n < 2^31 without a division (the divisors of a launch: a
-// division is a chain of some 40 dependent instructions)
+// division is a chain of some 40 dependent instructions): Granlund and Montgomery, Division by
+// invariant integers using multiplication, PLDI 1994
 struct FastDiv {
     uint32_t d, mul, shift;
     FastDiv() = default;
