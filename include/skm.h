@@ -873,6 +873,120 @@ size_t skm_kv_attend_workspace_size(const skm_kv_cache *c, const skm_kv_seqs *s,
 int skm_kv_attend(const skm_kv_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws, size_t ws_bytes,
                   void *stream);
 
+/* ------------------------------------------------------------------------
+ * Key/value cache in 4 bits, and attention that computes on its codes: LVQ4
+ * (Section 3.1: a bias and a scale for each vector, 4-bit codes) applied to the
+ * vectors that a language model keeps of a context.  Every token's key and value
+ * of a head is a vector of its own, value = b + s code, codes 0..15: unlike the
+ * 8-bit cache's, a token's codes never change with the tokens written after it.
+ *
+ * Pages, positions, table, absent pages and rows as in the 8-bit cache above.
+ * blocks: uint8 [pages][heads][page / 16][16 d + 128], 16-byte aligned; a block of
+ * 16 tokens is
+ *  keys    [d / 16][8 g][4 c][2 l][2 t]: codes of tokens g + 8 t, dims 4 c + l of the
+ *          chunk of 16 in the low half of a byte, dims 4 c + l + 2 in the high half
+ *  values  [d / 16][8 g][4 c][2 l][2 t]: codes of dims g + 8 t of the chunk, tokens
+ *          2 c + l in the low half, 2 c + l + 8 in the high half
+ *  float16 [16 tokens][4]: key scale, key bias, value scale, value bias
+ * (a 32-bit word holds the eight codes that a lane's tensor-core operand takes).
+ * 16 <= d <= 256 and a multiple of 16, page a multiple of 16; pages * heads *
+ * page / 16 < 2^31.  Nothing needs initialising: only positions that were written
+ * are read.
+ * ------------------------------------------------------------------------ */
+typedef struct skm_kv4_cache {
+    int32_t heads;
+    int32_t d;
+    int32_t page;     /* tokens of a page                                     */
+    int32_t pages;    /* pages of the pool                                    */
+    uint8_t *blocks;
+} skm_kv4_cache;
+
+/* Quantises new keys and values as they enter the cache; arguments as for skm_kv_write.
+ * Per token, head and tensor, with lo and hi the smallest and largest finite element, clipped to
+ * f16's range (0, 0 without a finite one): b the largest f16 not above lo, s the smallest
+ * f16 with b + 15 s >= hi, code = round((x - b) / s), halves to even, of x brought into [lo, hi] (NaN:
+ * lo; s = 0: code 0), all as in exact arithmetic.  A finite value within f16's range that is read back is within
+ * s / 2 of what was written; s <= (hi - lo + 2^-10 |lo| + 2^-24) (1 + 2^-10) / 15 + 2^-24.  Two sequences of a call must
+ * not write to the same page.  One kernel, no workspace.  Asynchronous. */
+int skm_kv4_write(const skm_kv4_cache *c, const skm_kv_seqs *s, int dtype, const void *K, int64_t k_token,
+                  int64_t k_head, const void *V, int64_t v_token, int64_t v_head, void *stream);
+
+/* Values of positions pos[b], pos[b] + 1, ... back, as skm_kv_read: b + s code in fp32 with one
+ * rounding, rounded once more to dtype.  Absent pages and positions past the table's end: zeros.
+ * Asynchronous. */
+int skm_kv4_read(const skm_kv4_cache *c, const skm_kv_seqs *s, int dtype, void *K, void *V, void *stream);
+
+/* Attention of query rows over the cache: rows, masks, outputs, status and workspaces as for
+ * skm_kv_attend (the workspace from skm_kv4_attend_workspace_size).  dtype BF16 or F16: products on
+ * tensor cores, sums and softmax in fp32, weights rounded to f16.  Query rows become f16 by a power of two
+ * a row: elements below 2^-25 (F16) or 2^-28 (BF16) of the row's largest lose bits, those below 2^-36
+ * vanish.  F32: fp32 arithmetic throughout.
+ * The result does not depend on timing.  Asynchronous. */
+size_t skm_kv4_attend_workspace_size(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a);
+int skm_kv4_attend(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws, size_t ws_bytes,
+                   void *stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions (Su et al., RoFormer, 2021) of query and key rows, before they enter
+ * a cache and attend to it.  The first `dims` dims of a head form dims / 2 pairs: (i, i + dims / 2)
+ * (SKM_ROTARY_HALF) or (2 i, 2 i + 1) (SKM_ROTARY_INTERLEAVED).  At position p pair i turns by the angle
+ * p f_i, radians; the dims behind stay as they are:
+ *   y1 = gain (x1 cos - x2 sin),  y2 = gain (x1 sin + x2 cos).
+ *
+ * skm_rotary_turns (host) writes the frequencies as turns a position in units of 2^-64 (so that an angle is
+ * one wrapping integer product, exact at every position) and the gain.  f_i = base^(-2 i / dims), and for
+ * contexts longer than the trained one, with `factor` the ratio:
+ *   LINEAR  f_i / factor (Chen et al., position interpolation, 2023)
+ *   BASE    base factor^(dims / (dims - 2)) in place of base
+ *   INDEX   f_i (1 - w) + f_i / factor w, w rising over the pairs from floor(n(high)) to
+ *           ceil(n(low)) (clipped to 0 and dims - 1), n(t) the index of the pair that turns t times over `trained`
+ *           positions; gain 0.1 ln(factor) + 1 where factor > 1 (Peng et al., YaRN, 2023)
+ *   TURNS   the same with w falling from 1 to 0 as a pair's turns over `trained` positions go from low to
+ *           high; gain 1
+ * base > 1, factor > 0, trained > 0, 0 < low < high.  Frequencies are good to 2^-50 of themselves: angles
+ * to 2^-24 up to position 2^26.
+ * ------------------------------------------------------------------------ */
+enum { SKM_ROTARY_HALF = 0, SKM_ROTARY_INTERLEAVED = 1 };
+enum { SKM_ROTARY_NONE = 0, SKM_ROTARY_LINEAR = 1, SKM_ROTARY_BASE = 2, SKM_ROTARY_INDEX = 3, SKM_ROTARY_TURNS = 4 };
+
+typedef struct skm_rotary_config {
+    int32_t dims;     /* even, 2..1024                                        */
+    int32_t scaling;
+    double base;
+    double factor;    /* not read where scaling is NONE                       */
+    double trained;   /* INDEX, TURNS                                         */
+    double low;
+    double high;
+} skm_rotary_config;
+
+int skm_rotary_turns(const skm_rotary_config *cfg, uint64_t *turns_host, float *gain_host);
+
+typedef struct skm_rotary {
+    int32_t dims;
+    int32_t layout;
+    int32_t transpose;     /* 1: by the angle's negative, what the gradient of the rotated rows becomes */
+    float gain;
+    const uint64_t *turns; /* device [dims / 2] */
+} skm_rotary;
+
+typedef struct skm_rotary_rows {
+    const void *x;         /* dtype rows [tokens] of [heads][d], d contiguous, strides in elements */
+    void *y;               /* may be x (then with its strides); no other overlap */
+    int64_t x_token;
+    int64_t x_head;
+    int64_t y_token;
+    int64_t y_head;
+    int32_t heads;
+    int32_t reserved;
+} skm_rotary_rows;
+
+/* Row i of sequence b stands at position pos[b] + i (skm_kv_write's); of s, table, cols and max_len are
+ * not read.  rows: `count` (1 or 2) tensors, as a step's queries and keys.  Rows that belong to no
+ * sequence are left alone.  fp32 arithmetic, one rounding.  1 <= d <= 1024.  One kernel, no
+ * workspace.  Asynchronous. */
+int skm_kv_rotate(const skm_kv_seqs *s, const skm_rotary *r, int d, int dtype, const skm_rotary_rows *rows, int count,
+                  void *stream);
+
 #ifdef __cplusplus
 }
 #endif

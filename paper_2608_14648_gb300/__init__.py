@@ -22,13 +22,17 @@ __all__ = [
     "skm_update_finalize", "skm_fit", "skm_split_empty", "skm_objective", "skm_sq8_decode", "EXPORTED_SYMBOLS",
     "EMPTY_KEEP", "EMPTY_SPLIT",
     "skm_assign_prune_stats", "DTYPE_F32", "DTYPE_BF16", "DTYPE_F16", "KVCache", "kv_workspace", "skm_kv_write",
-    "skm_kv_read", "skm_kv_attend",
+    "skm_kv_read", "skm_kv_attend", "KVCache4", "kv4_workspace", "skm_kv4_write", "skm_kv4_read", "skm_kv4_attend",
+    "ROTARY_HALF", "ROTARY_INTERLEAVED", "ROTARY_NONE", "ROTARY_LINEAR", "ROTARY_BASE", "ROTARY_INDEX", "ROTARY_TURNS",
+    "Rotary", "skm_rotary_turns", "skm_kv_rotate",
 ]
 
 REPR_F32, REPR_SQ8, REPR_RBQ1, REPR_BF16, REPR_LVQ4 = 0, 1, 2, 3, 4
 FLAG_PRUNE, FLAG_SYMMETRIC, FLAG_WARM, FLAG_PRUNE_CUDA_CORES = 1, 2, 4, 8
 DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 EMPTY_KEEP, EMPTY_SPLIT = 0, 1
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_NONE, ROTARY_LINEAR, ROTARY_BASE, ROTARY_INDEX, ROTARY_TURNS = 0, 1, 2, 3, 4
 OP_ASSIGN, OP_UPDATE, OP_FIT, OP_QUANTIZE, OP_PCA, OP_ASSIGN_SEG = 0, 1, 2, 3, 4, 5
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -49,6 +53,7 @@ EXPORTED_SYMBOLS = [
     "skm_lloyd_step_host", "skm_inject_fault", "skm_fault_armed", "skm_forgy_indices", "skm_column_absmax",
     "skm_mean_scale", "skm_column_sums_fixed", "skm_mean_from_sums", "skm_rbq1_segment_bounds",
     "skm_rbq1_segments", "skm_kv_write", "skm_kv_read", "skm_kv_attend_workspace_size", "skm_kv_attend",
+    "skm_kv4_write", "skm_kv4_read", "skm_kv4_attend_workspace_size", "skm_kv4_attend", "skm_rotary_turns", "skm_kv_rotate",
 ]
 
 
@@ -104,6 +109,13 @@ class KVCacheRef(ctypes.Structure):
                 ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
 
 
+class KVCache4Ref(ctypes.Structure):
+    """skm_kv4_cache (include/skm.h)."""
+
+    _fields_ = [("heads", ctypes.c_int32), ("d", ctypes.c_int32), ("page", ctypes.c_int32), ("pages", ctypes.c_int32),
+                ("blocks", ctypes.c_void_p)]
+
+
 class KVSeqs(ctypes.Structure):
     """skm_kv_seqs (include/skm.h)."""
 
@@ -119,6 +131,27 @@ class KVAttn(ctypes.Structure):
                 ("window", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
                 ("Q", ctypes.c_void_p), ("q_token", ctypes.c_int64), ("q_head", ctypes.c_int64),
                 ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class RotaryConfig(ctypes.Structure):
+    """skm_rotary_config (include/skm.h)."""
+
+    _fields_ = [("dims", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("trained", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class RotaryRef(ctypes.Structure):
+    """skm_rotary (include/skm.h)."""
+
+    _fields_ = [("dims", ctypes.c_int32), ("layout", ctypes.c_int32), ("transpose", ctypes.c_int32), ("gain", ctypes.c_float),
+                ("turns", ctypes.c_void_p)]
+
+
+class RotaryRows(ctypes.Structure):
+    """skm_rotary_rows (include/skm.h)."""
+
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_token", ctypes.c_int64), ("x_head", ctypes.c_int64),
+                ("y_token", ctypes.c_int64), ("y_head", ctypes.c_int64), ("heads", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 EXCHANGE_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p)
@@ -190,6 +223,12 @@ def lib():
             "skm_kv_read": ([vp, vp, i32, vp, vp, vp], i32),
             "skm_kv_attend_workspace_size": ([vp, vp, vp], sz),
             "skm_kv_attend": ([vp, vp, vp, vp, sz, vp], i32),
+            "skm_kv4_write": ([vp, vp, i32, vp, i64, i64, vp, i64, i64, vp], i32),
+            "skm_kv4_read": ([vp, vp, i32, vp, vp, vp], i32),
+            "skm_kv4_attend_workspace_size": ([vp, vp, vp], sz),
+            "skm_kv4_attend": ([vp, vp, vp, vp, sz, vp], i32),
+            "skm_rotary_turns": ([vp, vp, vp], i32),
+            "skm_kv_rotate": ([vp, vp, i32, i32, vp, i32, vp], i32),
             "skm_lloyd_step_host": ([vp, vp, vp, vp, vp, vp, vp, vp, sz, vp], i32),
         }
         for name, (args, res) in sig.items():
@@ -733,7 +772,7 @@ def skm_rbq1_segments(X, m, stream=None):
     return nx2, F, pc
 
 
-# ---- 8-bit key/value cache
+# ---- 8-bit key/value cache (and what the calls of both caches share)
 
 _KV_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
 _KV_TORCH = {v: k for k, v in _KV_DTYPES.items()}
@@ -760,7 +799,7 @@ class KVCache:
                 raise ValueError(f"KVCache: {name} must be contiguous {dt} {list(shape + (last,))}")
             if t.device != k.device:
                 raise ValueError("KVCache: k, v and scales must be on one device")
-        self.k, self.v, self.scales = k, v, scales
+        self.k, self.v, self.scales, self.data = k, v, scales, k
         self.heads, self.d, self.page, self.pages = int(heads), int(d), int(page), n
         self.index = k.get_device()
         self.ref = KVCacheRef(self.heads, self.d, self.page, n, k.data_ptr(), v.data_ptr(), scales.data_ptr())
@@ -821,31 +860,31 @@ def _kv_stream(cache, stream):
 def _kv_empty(cache, stream, shape, dtype):
     """What a call allocates belongs to the stream that it runs on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=cache.k.device)
+        return torch.empty(shape, dtype=dtype, device=cache.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=cache.k.device)
+        return torch.empty(shape, dtype=dtype, device=cache.device)
 
 
-def skm_kv_write(cache: KVCache, table, start, cu, K, V, max_tokens, stream=None):
-    """Quantises rows cu[b]:cu[b + 1] of K and V ([tokens, heads, d], any strides
-    with d contiguous) into the cache at positions start[b], start[b] + 1, ... of
-    sequence b; table int32 [batch, cols], start [batch], cu [batch + 1]."""
+def _write(call, cache, table, start, cu, K, V, max_tokens, stream):
     dtype, k_token, k_head = _kv_rows("K", K, cache.heads, cache)
     v_dtype, v_token, v_head = _kv_rows("V", V, cache.heads, cache)
     tokens = K.shape[0]
     if v_dtype != dtype or V.shape[0] != tokens:
         raise ValueError("K and V must have one type and length")
     s = _kv_seqs(cache, table, start, cu, tokens, max_tokens)
-    rc = lib().skm_kv_write(cache.addr, s, dtype, K.data_ptr(), k_token, k_head, V.data_ptr(), v_token, v_head,
-                            _kv_stream(cache, stream))
+    rc = call(cache.addr, s, dtype, K.data_ptr(), k_token, k_head, V.data_ptr(), v_token, v_head, _kv_stream(cache, stream))
     if rc:
         _check(rc)
 
 
-def skm_kv_read(cache: KVCache, table, start, cu, tokens, max_tokens, dtype=DTYPE_BF16, out=None, stream=None):
-    """(K, V), each [tokens, heads, d]: rows cu[b]:cu[b + 1] are the values at
-    positions start[b], start[b] + 1, ... of sequence b.  out: a pair of
-    contiguous tensors, either may be None (not read)."""
+def skm_kv_write(cache: KVCache, table, start, cu, K, V, max_tokens, stream=None):
+    """Quantises rows cu[b]:cu[b + 1] of K and V ([tokens, heads, d], any strides
+    with d contiguous) into the cache at positions start[b], start[b] + 1, ... of
+    sequence b; table int32 [batch, cols], start [batch], cu [batch + 1]."""
+    _write(lib().skm_kv_write, cache, table, start, cu, K, V, max_tokens, stream)
+
+
+def _read(call, cache, table, start, cu, tokens, max_tokens, dtype, out, stream):
     if out is None:
         t = _KV_TORCH.get(dtype)
         if t is None:
@@ -859,34 +898,41 @@ def skm_kv_read(cache: KVCache, table, start, cu, tokens, max_tokens, dtype=DTYP
                 raise ValueError("out: contiguous tensors of `tokens` rows and the given dtype")
     K, V = out
     s = _kv_seqs(cache, table, start, cu, tokens, max_tokens)
-    rc = lib().skm_kv_read(cache.addr, s, dtype, None if K is None else K.data_ptr(), None if V is None else V.data_ptr(),
-                           _kv_stream(cache, stream))
+    rc = call(cache.addr, s, dtype, None if K is None else K.data_ptr(), None if V is None else V.data_ptr(),
+              _kv_stream(cache, stream))
     if rc:
         _check(rc)
     return out
 
 
-def _kv_ws_bytes(cache, s, a):
-    n = lib().skm_kv_attend_workspace_size(cache.addr, s, a)
+def skm_kv_read(cache: KVCache, table, start, cu, tokens, max_tokens, dtype=DTYPE_BF16, out=None, stream=None):
+    """(K, V), each [tokens, heads, d]: rows cu[b]:cu[b + 1] are the values at
+    positions start[b], start[b] + 1, ... of sequence b.  out: a pair of
+    contiguous tensors, either may be None (not read)."""
+    return _read(lib().skm_kv_read, cache, table, start, cu, tokens, max_tokens, dtype, out, stream)
+
+
+def _kv_ws_bytes(size, cache, s, a):
+    n = size(cache.addr, s, a)
     if n == ctypes.c_size_t(-1).value:
         raise SkmError(1, lib().skm_last_error().decode())
     return n
 
 
-def kv_workspace(cache: KVCache, batch, heads_q, tokens, max_tokens, max_len, dtype=DTYPE_BF16, cols=None):
-    """A workspace for skm_kv_attend calls of at most these sizes."""
+def _workspace(size, cache, batch, heads_q, tokens, max_tokens, max_len, dtype, cols):
     cols = -(-max_len // cache.page) if cols is None else cols
-    dummy = cache.k.data_ptr()
+    dummy = cache.data.data_ptr()
     s = _KV_SEQS.pack(batch, max(cols, 1), dummy, dummy, dummy, tokens, max_tokens, max_len)
     a = _KV_ATTN.pack(heads_q, dtype, 1, 0, 1.0, 0, 0, 0, 0, 0, 0, 0)
-    return _ws(_kv_ws_bytes(cache, s, a), cache.device)
+    return _ws(_kv_ws_bytes(size, cache, s, a), cache.device)
 
 
-def skm_kv_attend(cache: KVCache, table, length, cu, Q, max_tokens, max_len, scale=None, causal=True, window=0,
-                  want_lse=False, out=None, ws=None, status=None, stream=None):
-    """(out, lse or None): attention of the query rows Q [tokens, heads_q, d]
-    over the cache.  length[b]: the tokens the cache holds of sequence b, its
-    own query tokens included; scale: 1 / sqrt(d) unless given."""
+def kv_workspace(cache: KVCache, batch, heads_q, tokens, max_tokens, max_len, dtype=DTYPE_BF16, cols=None):
+    """A workspace for skm_kv_attend calls of at most these sizes."""
+    return _workspace(lib().skm_kv_attend_workspace_size, cache, batch, heads_q, tokens, max_tokens, max_len, dtype, cols)
+
+
+def _attend(call, size, cache, table, length, cu, Q, max_tokens, max_len, scale, causal, window, want_lse, out, ws, status, stream):
     shape = Q.shape
     tokens, heads_q = shape[0], shape[1]
     dtype, q_token, q_head = _kv_rows("Q", Q, heads_q, cache)
@@ -902,13 +948,149 @@ def skm_kv_attend(cache: KVCache, table, length, cu, Q, max_tokens, max_len, sca
                       q_token, q_head, out.data_ptr(), 0 if lse is None else lse.data_ptr(),
                       0 if status is None else status.data_ptr())
     if ws is None:
-        n = _kv_ws_bytes(cache, s, a)
+        n = _kv_ws_bytes(size, cache, s, a)
         if n:
             ws = _kv_empty(cache, stream, (n,), torch.uint8)
     elif ws.get_device() != cache.index or not ws.is_contiguous():
         raise ValueError("ws must be contiguous, on the cache's device")
-    rc = lib().skm_kv_attend(cache.addr, s, a, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
-                             _kv_stream(cache, stream))
+    rc = call(cache.addr, s, a, None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes, _kv_stream(cache, stream))
     if rc:
         _check(rc)
     return out, lse
+
+
+def skm_kv_attend(cache: KVCache, table, length, cu, Q, max_tokens, max_len, scale=None, causal=True, window=0,
+                  want_lse=False, out=None, ws=None, status=None, stream=None):
+    """(out, lse or None): attention of the query rows Q [tokens, heads_q, d]
+    over the cache.  length[b]: the tokens the cache holds of sequence b, its
+    own query tokens included; scale: 1 / sqrt(d) unless given."""
+    L = lib()
+    return _attend(L.skm_kv_attend, L.skm_kv_attend_workspace_size, cache, table, length, cu, Q, max_tokens, max_len, scale,
+                   causal, window, want_lse, out, ws, status, stream)
+
+
+# ---- 4-bit key/value cache
+
+
+class KVCache4:
+    """The tensor of one skm_kv4_cache: uint8 blocks [pages, heads, page / 16, 16 d + 128]
+    (layout in include/skm.h), allocated here for `pages` pages unless given.  Calls
+    on it are made with its device current (torch.cuda.device)."""
+
+    def __init__(self, heads, d, page, blocks=None, pages=None, device="cuda"):
+        heads, d, page = int(heads), int(d), int(page)
+        if blocks is None:
+            blocks = torch.empty(int(pages), heads, page // KV_BLOCK, KV_BLOCK * d + 8 * KV_BLOCK, dtype=torch.uint8, device=device)
+        n = int(blocks.shape[0]) if blocks.dim() else 0
+        shape = (n, heads, page // KV_BLOCK, KV_BLOCK * d + 8 * KV_BLOCK)
+        if blocks.dtype != torch.uint8 or tuple(blocks.shape) != shape or not blocks.is_contiguous():
+            raise ValueError(f"KVCache4: blocks must be contiguous uint8 {list(shape)}")
+        self.blocks = self.data = blocks
+        self.heads, self.d, self.page, self.pages = heads, d, page, n
+        self.index = blocks.get_device()
+        self.ref = KVCache4Ref(heads, d, page, n, blocks.data_ptr())
+        self.addr = ctypes.addressof(self.ref)
+
+    @property
+    def device(self):
+        return self.blocks.device
+
+
+def kv4_workspace(cache: KVCache4, batch, heads_q, tokens, max_tokens, max_len, dtype=DTYPE_BF16, cols=None):
+    """A workspace for skm_kv4_attend calls of at most these sizes."""
+    return _workspace(lib().skm_kv4_attend_workspace_size, cache, batch, heads_q, tokens, max_tokens, max_len, dtype, cols)
+
+
+def skm_kv4_write(cache: KVCache4, table, start, cu, K, V, max_tokens, stream=None):
+    """skm_kv_write for the 4-bit cache."""
+    _write(lib().skm_kv4_write, cache, table, start, cu, K, V, max_tokens, stream)
+
+
+def skm_kv4_read(cache: KVCache4, table, start, cu, tokens, max_tokens, dtype=DTYPE_BF16, out=None, stream=None):
+    """skm_kv_read for the 4-bit cache."""
+    return _read(lib().skm_kv4_read, cache, table, start, cu, tokens, max_tokens, dtype, out, stream)
+
+
+def skm_kv4_attend(cache: KVCache4, table, length, cu, Q, max_tokens, max_len, scale=None, causal=True, window=0,
+                   want_lse=False, out=None, ws=None, status=None, stream=None):
+    """skm_kv_attend for the 4-bit cache."""
+    L = lib()
+    return _attend(L.skm_kv4_attend, L.skm_kv4_attend_workspace_size, cache, table, length, cu, Q, max_tokens, max_len, scale,
+                   causal, window, want_lse, out, ws, status, stream)
+
+
+# ---- rotary positions
+
+
+def skm_rotary_turns(dims, base=10000.0, scaling=ROTARY_NONE, factor=1.0, trained=0.0, low=1.0, high=32.0):
+    """(frequencies, gain): the turns a position of each pair in units of 2^-64, as
+    the bits of an int64 CPU tensor [dims / 2]."""
+    turns = torch.empty(max(int(dims) // 2, 0), dtype=torch.int64)
+    gain = ctypes.c_float(0.0)
+    cfg = RotaryConfig(int(dims), int(scaling), float(base), float(factor), float(trained), float(low), float(high))
+    _check(lib().skm_rotary_turns(ctypes.byref(cfg), _ptr(turns), ctypes.byref(gain)))
+    return turns, gain.value
+
+
+class Rotary:
+    """The frequencies that skm_kv_rotate takes (skm_rotary_turns), on the device; layout
+    ROTARY_HALF or ROTARY_INTERLEAVED."""
+
+    def __init__(self, dims, base=10000.0, layout=ROTARY_HALF, scaling=ROTARY_NONE, factor=1.0, trained=0.0, low=1.0,
+                 high=32.0, device="cuda"):
+        turns, self.gain = skm_rotary_turns(dims, base, scaling, factor, trained, low, high)
+        self.dims, self.layout = int(dims), int(layout)
+        self.turns = turns.to(device)
+        self.index = self.turns.get_device()
+        ref = lambda back: RotaryRef(self.dims, self.layout, back, self.gain, self.turns.data_ptr())  # noqa: E731
+        self.refs = ref(0), ref(1)
+        self.addrs = tuple(ctypes.addressof(r) for r in self.refs)
+
+    @property
+    def device(self):
+        return self.turns.device
+
+
+_ROTARY_ROWS = struct.Struct("@PPqqqqii")  # RotaryRows, packed as the structs above
+assert _ROTARY_ROWS.size == ctypes.sizeof(RotaryRows)
+
+
+def skm_kv_rotate(rotary: Rotary, start, cu, rows, max_tokens, out=None, transpose=False, stream=None):
+    """Rows cu[b]:cu[b + 1] of one tensor [tokens, heads, d] or of two (a step's queries
+    and keys; any strides with d contiguous) turned to positions start[b], start[b] + 1, ...
+    of sequence b; start int32 [batch], cu [batch + 1].  out: new tensors unless given (the
+    rows themselves: in place).  transpose: what a gradient of the result becomes.  Returns
+    out, a tensor or a tuple as rows is."""
+    single = isinstance(rows, torch.Tensor)
+    if single:
+        rows, out = (rows,), None if out is None else (out,)
+    if not 1 <= len(rows) <= 2 or (out is not None and len(out) != len(rows)):
+        raise ValueError("rows: one tensor or two, out: as many")
+    index = rotary.index
+    if index < 0:
+        raise ValueError("the frequencies are not on a GPU")
+    current = torch._C._cuda_getDevice()
+    if current != index:
+        raise ValueError(f"the frequencies are on cuda:{index}, but the current device is cuda:{current}")
+    if start.dim() != 1:
+        raise ValueError("start must be an int32 tensor [batch]")
+    batch, shape, kind = start.shape[0], rows[0].shape, rows[0].dtype
+    dtype = _KV_DTYPES.get(kind)
+    if dtype is None:
+        raise ValueError("rows must be float32, bfloat16 or float16")
+    if out is None:
+        out = tuple(_kv_empty(rotary, stream, x.shape, kind) for x in rows)
+    packed = b""
+    for x, y in zip(rows, out):
+        xs, ys = x.stride(), y.stride()
+        if (x.dim() != 3 or y.shape != x.shape or x.shape[0] != shape[0] or x.shape[2] != shape[2] or x.dtype != kind
+                or y.dtype != kind or xs[2] != 1 or ys[2] != 1 or x.get_device() != index or y.get_device() != index):
+            raise ValueError("rows and out must be [tokens, heads, d] of one type and one number of tokens, d contiguous, "
+                             "on the frequencies' device")
+        packed += _ROTARY_ROWS.pack(x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], x.shape[1], 0)
+    s = _KV_SEQS.pack(batch, 0, 0, _kv_ints("start", start, batch, index), _kv_ints("cu", cu, batch + 1, index), shape[0],
+                      max_tokens, 0)
+    rc = lib().skm_kv_rotate(s, rotary.addrs[bool(transpose)], shape[2], dtype, packed, len(rows), _kv_stream(rotary, stream))
+    if rc:
+        _check(rc)
+    return out[0] if single else out

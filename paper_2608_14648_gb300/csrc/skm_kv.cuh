@@ -11,6 +11,8 @@ namespace skm {
 
 constexpr int KV_B = SKM_KV_BLOCK;
 constexpr int KV_SMS = 152;
+// bytes of a 4-bit block: the codes of 16 keys and values, 16 x (scale, bias) of both in f16
+__host__ __device__ __forceinline__ constexpr int kv4_bytes(int d) { return KV_B * d + 8 * KV_B; }
 // sequences whose prefix sums one launch keeps in shared memory at most; larger
 // batches take several launches
 constexpr int KV_MAX_SEQS = 1024;
@@ -48,6 +50,30 @@ struct KvCacheArgs {
 
 cudaError_t launch_kv_write(const KvCacheArgs &a, int dtype, cudaStream_t st);
 cudaError_t launch_kv_read(const KvCacheArgs &a, int dtype, cudaStream_t st);
+// (4-bit: k points at the blocks, v and scales are not used)
+cudaError_t launch_kv4_write(const KvCacheArgs &a, int dtype, cudaStream_t st);
+cudaError_t launch_kv4_read(const KvCacheArgs &a, int dtype, cudaStream_t st);
+
+// Rotary positions: one or two tensors of rows
+struct RotaryPart {
+    const void *x;
+    void *y;
+    int64_t x_token, x_head, y_token, y_head;
+    int heads;
+};
+struct RotaryArgs {
+    const int32_t *pos, *cu;
+    const uint64_t *turns;
+    int batch, tokens, max_tokens, dims, interleaved;
+    int copied;         // dims behind the rotated ones that a call with other outputs copies
+    int heads;          // of both parts
+    float gain, sine;   // factors of cosine and sine: the sine's is negative for a transposed call
+    RotaryPart part[2];
+    int tile, cuts;     // (set by the launcher) tokens of a CTA, CTAs that share a token's heads
+    FastDiv by_half, by_heads, by_units;
+};
+// vec: elements of a vector that all rows are aligned to
+cudaError_t launch_rotary(const RotaryArgs &a, int dtype, int vec, cudaStream_t st);
 
 struct KvAttnArgs {
     const uint8_t *k, *v;
@@ -83,6 +109,9 @@ KvRowsPlan kv_rows_plan(int nb, int heads, int group, int d, int dtype, int max_
 // workspace of any call of these sizes or smaller ones at most
 size_t kv_rows_part_most(int nb, int heads, int d, int dtype, int64_t rows, int64_t span);
 cudaError_t launch_kv_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st);
+KvRowsPlan kv4_rows_plan(int nb, int heads, int group, int d, int dtype, int max_tokens, int64_t span);
+size_t kv4_rows_part_most(int nb, int heads, int d, int dtype, int64_t rows, int64_t span);
+cudaError_t launch_kv4_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st);
 
 // Many rows on tcgen05 (k_kv_prompt.cu): max_tiles in units of a CTA's rows
 struct KvPromptPlan {
