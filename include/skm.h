@@ -920,7 +920,9 @@ int skm_kv4_read(const skm_kv4_cache *c, const skm_kv_seqs *s, int dtype, void *
  * skm_kv_attend (the workspace from skm_kv4_attend_workspace_size).  dtype BF16 or F16: products on
  * tensor cores, sums and softmax in fp32, weights rounded to f16.  Query rows become f16 by a power of two
  * a row: elements below 2^-25 (F16) or 2^-28 (BF16) of the row's largest lose bits, those below 2^-36
- * vanish.  F32: fp32 arithmetic throughout.
+ * vanish.  Calls of more than 32 rows a sequence (tokens x heads of a group; d > 128: of more keys too)
+ * run on another kernel, which takes keys and values rounded to f16 (2^-11 of each; b + 15 s above f16's
+ * largest number as that number).  F32: fp32 arithmetic throughout.
  * The result does not depend on timing.  Asynchronous. */
 size_t skm_kv4_attend_workspace_size(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a);
 int skm_kv4_attend(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws, size_t ws_bytes,

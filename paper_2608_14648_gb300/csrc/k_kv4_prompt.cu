@@ -1,0 +1,571 @@
+// Attention over the 4-bit cache for many query rows (prompt chunks) on tcgen05: 16-bit
+// queries.
+//
+// As k_kv_prompt.cu: a CTA takes 256 query rows of one sequence and key/value head as two tiles of 128
+// (d > 128: one), and walks the keys they see in tiles of 64 positions; softmax warps of one
+// thread a row, converter warps, one warp that issues the products.  Unlike there the converters
+// make whole keys and values, b + s c in f16 (one rounding of 2^-11), so a row's logits need one
+// factor and no block's scales: p = 2^(f S - m), l = sum p, and a tile's sum tells whether the
+// reference m has to move.
+#include "skm_kv_prompt.cuh"
+
+namespace skm {
+
+namespace {
+
+constexpr int CONV = 7;  // converter warps
+constexpr float TILE_MOST = 65000.0f;  // a tile's sum of weights: above it one may pass the largest f16
+// tiles whose absent blocks are noted.  A K stage is free once its product is through, which is issued when the softmax
+// has handed over the tile two before: tile j + ST (at most 4) comes while it reads tile j - 1 at the earliest, 5 behind
+constexpr int INFO = 8;
+
+// DH: dims, padded to 64, 128 or 256
+template <int DH>
+struct Lay {
+    static constexpr int NQ = DH <= 128 ? 2 : 1;      // row tiles of a CTA
+    static constexpr int ST = DH <= 128 ? 4 : 2;      // K and V tiles in flight
+    static constexpr int ROWS = NQ * QT;
+    static constexpr int CONV_WARP0 = 4 * NQ, MMA_WARP = CONV_WARP0 + CONV, THREADS = 32 * (MMA_WARP + 1);
+    static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
+    static constexpr int q = 0, k = NQ * QTILE, v = k + ST * TILE, bars = v + ST * TILE;
+    static constexpr int slots = bars + 8 * (4 * ST + 14);  // TMEM address, a flag, the part's index
+    static constexpr int wild = slots + 32;    // a byte a row: its query holds infinities or NaN
+    static constexpr int there = wild + ROWS;  // a byte a block of the last INFO tiles: its page is present
+    static constexpr int scales = (there + INFO * KBLK + 63) / 64 * 64;  // [converter warp][value scales, biases of 16 tokens]
+    // one CTA an SM: it takes all of TMEM
+    static constexpr int bytes = scales + CONV * 64 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
+    static constexpr uint32_t O = NQ * 2 * KT;  // TMEM column of O0
+};
+
+__device__ __forceinline__ void ld32(uint32_t addr, uint32_t *v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void ld_wait32(uint32_t *v) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]),
+                   "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]),
+                   "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+                 :
+                 : "memory");
+}
+
+__device__ __forceinline__ __half2 h2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
+__device__ __forceinline__ uint32_t u2(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
+// b + s c of the codes in bits 0..3 and 16..19 of a word, or (HIGH) 4..7 and 20..23: 1024 + c (1024 + 16 c) as f16
+// bits, made c, exactly, then one rounding.  BIG: no more than f16's largest number
+template <bool HIGH, bool BIG>
+__device__ __forceinline__ uint32_t dequant2(uint32_t w, __half2 s, __half2 b) {
+    const __half2 x = h2((w & (HIGH ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u);
+    const __half2 c = HIGH ? __hfma2(x, h2(0x2c002c00u), h2(0xd400d400u)) : __hsub2(x, h2(0x64006400u));
+    const __half2 v = __hfma2(c, s, b);
+    return u2(BIG ? __hmin2(v, h2(0x7bff7bffu)) : v);
+}
+
+template <int DH>
+__global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
+    kv4_prompt_kernel(const __grid_constant__ KvAttnArgs a, int splits, float *parts) {
+    using L = Lay<DH>;
+    constexpr int ST = L::ST, ROWS = L::ROWS, CONV_WARP0 = L::CONV_WARP0, MMA_WARP = L::MMA_WARP, THREADS = L::THREADS;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint8_t *smem = smem_raw + ((1024 - (su32(smem_raw) & 1023)) & 1023);  // swizzle atoms
+    const uint32_t sm = su32(smem);
+    const auto bar = [&](int i) { return sm + L::bars + 8 * i; };
+    const auto k_full = [&](int s) { return bar(s); };
+    const auto k_free = [&](int s) { return bar(ST + s); };
+    const auto v_full = [&](int s) { return bar(2 * ST + s); };
+    const auto v_free = [&](int s) { return bar(3 * ST + s); };
+    const auto s_full = [&](int q, int buf) { return bar(4 * ST + 2 * q + buf); };
+    const auto p_full = [&](int q, int buf) { return bar(4 * ST + 4 + 2 * q + buf); };
+    const auto o_done = [&](int q) { return bar(4 * ST + 8 + q); };
+    const auto o_last = [&](int q) { return bar(4 * ST + 10 + q); };
+    const uint32_t q_full = bar(4 * ST + 12), drain = bar(4 * ST + 13);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::slots);
+    volatile int32_t *gone = reinterpret_cast<volatile int32_t *>(smem + L::slots + 4);
+
+    // the unit: ROWS rows of a sequence, longest first where there is more than one a
+    // SM (few units are ranked by the key tiles they see; of many, the later rows come first), its heads next
+    // to each other
+    const int tiles = a.max_tiles, pairs = a.nb * tiles;
+    int u = blockIdx.x;
+    const int split = u % splits;
+    u /= splits;
+    const int h = a.by_heads.mod(u);
+    u = a.by_heads.div(u);
+    if (pairs <= RANKED && gridDim.x > KV_SMS) {
+        int *length = reinterpret_cast<int *>(smem), *pick = length + RANKED;
+        if (tid < pairs) {
+            const Seq s = seq_of(a, a.b0 + tid / tiles);
+            const int r0 = tid % tiles * ROWS, r1 = min(r0 + ROWS, s.n * a.group) - 1;
+            length[tid] = r1 < r0 ? -1 : last_of(a, s, r1) / KT - first_of(a, s, r0) / KT;
+        }
+        __syncthreads();
+        if (tid < pairs) {
+            int rank = 0;
+            for (int i = 0; i < pairs; ++i) rank += length[i] > length[tid] || (length[i] == length[tid] && i < tid);
+            if (rank == u) *pick = tid;
+        }
+        __syncthreads();
+        u = *pick;
+        __syncthreads();
+    } else {
+        u = u % a.nb * tiles + tiles - 1 - u / a.nb;
+    }
+    const int bi = u / tiles, pair = u % tiles, b = a.b0 + bi;
+    int64_t *part_index = reinterpret_cast<int64_t *>(smem + L::slots + 8);
+    if (tid == 0) *part_index = ((int64_t)u * a.heads + h) * splits + split;
+    const Seq s = seq_of(a, b);
+    const int rows = s.n * a.group, r0 = pair * ROWS;
+    if (r0 >= rows) return;
+    const int r1 = min(r0 + ROWS, rows) - 1;
+    const int nq = r1 - r0 >= QT ? 2 : 1;
+    // positions that some row sees, the tiles of them, this split's tiles
+    const int first = first_of(a, s, r0), last = last_of(a, s, r1);
+    const int t_lo = first / KT, t_all = last >= first ? last / KT + 1 - t_lo : 0;
+    const int t0 = t_lo + (int)((int64_t)t_all * split / splits);
+    const int n = t_lo + (int)((int64_t)t_all * (split + 1) / splits) - t0;
+    // those that a row tile goes through: the last one all of them, the one before it to its own end
+    const auto tiles_for = [&](int q) {
+        if (q >= nq) return 0;
+        const int its_last = last_of(a, s, min(r0 + (q + 1) * QT - 1, r1));
+        return its_last < first ? 0 : kv_clamp(its_last / KT + 1 - t0, 0, n);
+    };
+
+    if (tid == 0) {
+        const auto init = [&](uint32_t b, int count) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(b), "r"(count) : "memory");
+        };
+        for (int i = 0; i < ST; ++i) init(k_full(i), KBLK), init(v_full(i), KBLK), init(k_free(i), 1), init(v_free(i), 1);
+        for (int q = 0; q < L::NQ; ++q) {
+            for (int i = 0; i < 2; ++i) init(s_full(q, i), 1), init(p_full(q, i), 4);
+            init(o_done(q), 1), init(o_last(q), 1);
+        }
+        init(q_full, 4 * L::NQ), init(drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *gone = 0;
+    }
+    if (a.d < DH) {  // dims from d on are zeros
+        for (int i = tid * 16; i < 2 * ST * L::TILE; i += THREADS * 16) st_shared(sm + L::k + i, 0, 0, 0, 0);
+        fence_async();
+    }
+    if (warp == MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(su32(tmem_slot)), "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    // (two row tiles: the softmax threads hold a tile's 64 logits and its weights.  168 and 88 registers for
+    // 256 threads each are the 128 of all 512 that the launch comes with)
+    if constexpr (L::NQ == 2) {
+        if (warp < CONV_WARP0) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    }
+    if (warp < CONV_WARP0) {  // ------------------------------------------ softmax
+        const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row, nt = tiles_for(q);
+        const bool in = r < rows;
+        const float fac = load_rows<DH>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE, lane,
+                                        smem + L::wild + q * QT);
+        fence_async();
+        __syncwarp();
+        if (lane == 0) arrive(q_full);
+        // (rows past the end see everything, with no weight: they slow no one down)
+        const int hi = in ? last_of(a, s, r) : 0x7ffffffe, lo = in ? first_of(a, s, r) : 0;
+        // rows of the warp see [low, high] whole
+        const int high = __shfl_sync(0xffffffffu, hi, 0), low = __reduce_max_sync(0xffffffffu, lo);
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t S0 = tmem + lanes + q * 2 * KT, O = tmem + lanes + L::O + q * DH;
+        float m = in ? M_NONE : -M_NONE, l = 0.0f;
+        bool ok = true;
+        const volatile uint32_t *there = reinterpret_cast<const volatile uint32_t *>(smem + L::there);
+        for (int j = 0; j < nt; ++j) {
+            const uint32_t S = S0 + (j & 1) * KT;
+            if (!(ok = warp_wait(s_full(q, j & 1), (j >> 1) & 1, gone))) break;
+            fence_after();
+            uint32_t v[KT];
+            ld32(S, v);
+            ld32(S + 32, v + 32);
+            const uint32_t blocks = there[j & (INFO - 1)];
+            const int c0 = (t0 + j) * KT;
+            const bool whole = c0 >= low && c0 + KT - 1 <= high && blocks == 0x01010101u;
+            // the positions of half a tile that the row sees, as bits (opaque, so that it stays in the branches that ask)
+            const auto visible = [&](int k0) {
+                uint32_t bits = 0;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    int at = c0 + k0 + k * KV_B;
+                    asm volatile("" : "+r"(at));
+                    const uint32_t sees = ((1u << kv_clamp(hi + 1 - at, 0, KV_B)) - 1) & ~0u << kv_clamp(lo - at, 0, KV_B);
+                    if (blocks >> (k0 / 2 + 8 * k) & 1) bits |= sees << (KV_B * k);
+                }
+                return bits;
+            };
+            uint32_t P[KT / 2];
+            uint64_t sum[4] = {0, 0, 0, 0};
+            // weights of 32 logits
+            const auto weigh = [&](auto masked, const uint32_t *x, uint32_t *p, uint32_t sees) {
+                const float2 f = make_float2(fac, fac), c = make_float2(-m, -m);
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) {
+                    float2 t = fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), f, c);
+                    if constexpr (decltype(masked)::value) {
+                        t.x = sees & 1u << i ? t.x : -INFINITY;
+                        t.y = sees & 2u << i ? t.y : -INFINITY;
+                    }
+                    p[i / 2] = weights2(t.x, t.y, sum[i / 2 & 3]);
+                }
+            };
+            const auto weigh_any = [&](int k0) {
+                if (whole) weigh(std::false_type{}, v + k0, P + k0 / 2, 0u);
+                else weigh(std::true_type{}, v + k0, P + k0 / 2, visible(k0));
+            };
+            const auto total = [&] {
+                const float2 t = halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
+                return t.x + t.y;
+            };
+            bool moves = j == 0;  // the reference: set by the first tile, seldom moved by a later one
+            float add = 0.0f;
+            ld_wait32(v);
+            if (!moves) {
+                weigh_any(0);
+                ld_wait32(v + 32);
+                weigh_any(32);
+                add = total();
+                moves = __any_sync(0xffffffffu, add > TILE_MOST);
+            } else {
+                ld_wait32(v + 32);
+            }
+            if (moves) {
+                // the rows' maxima, with them new references, and the weights (again)
+                float top = -INFINITY;
+#pragma unroll
+                for (int k0 = 0; k0 < KT; k0 += 32) {
+                    const uint32_t sees = visible(k0);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (sees & 1u << i) top = fmaxf(top, __uint_as_float(v[k0 + i]) * fac);
+                }
+                const float to = top > m + 8.0f ? top - M_BELOW : m;
+                const float g = ex2(m - to);
+                m = to;
+                l *= g;
+                if (j > 0) {
+                    if (!(ok = warp_wait(o_done(q), (j - 1) & 1, gone))) break;
+                    fence_after();
+#pragma unroll 1
+                    for (int k = 0; k < DH / 16; ++k) {
+                        uint32_t x[16];
+                        ld16(O + k * 16, x);
+                        ld_wait(x);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * g);
+                        st16(O + k * 16, x);
+                    }
+                    st_wait();
+                }
+                sum[0] = sum[1] = sum[2] = sum[3] = 0;
+                weigh(std::true_type{}, v, P, visible(0));
+                weigh(std::true_type{}, v + 32, P + 16, visible(32));
+                add = total();
+            }
+            l += add;
+#pragma unroll
+            for (int k = 0; k < KT / 2; k += 16) st16(S + k, P + k);
+            st_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(p_full(q, j & 1));
+        }
+        if (q < nq) {
+            if (ok && nt > 0) {
+                ok = warp_wait(o_last(q), 0, gone);
+                fence_after();
+            }
+            if (!ok) {
+                l = NAN;
+                if (lane == 0 && a.status) *a.status = 1;
+            }
+            if (smem[L::wild + q * QT + row] && l != 0.0f) l = NAN;
+            float *part = parts ? parts + *part_index * prompt_part(ROWS, a.d) : nullptr;
+            const int pr = q * QT + row;
+            if (part) reinterpret_cast<float2 *>(part)[pr] = make_float2(m, l);
+            const int64_t at = in ? row_index(a, s, h, r) : 0;
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll 2
+            for (int k = 0; k < DH / 16; ++k) {
+                if (16 * k >= a.d) break;
+                uint32_t v[16];
+                __syncwarp();
+                if (ok && nt > 0) {
+                    ld16(O + k * 16, v);
+                    ld_wait(v);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = 0;
+                }
+                if (!in) continue;
+                if (part) {
+                    float4 *dst = reinterpret_cast<float4 *>(part + 2 * ROWS + (int64_t)pr * a.d + 16 * k);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        dst[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
+                                             __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+                    continue;
+                }
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float x0 = __uint_as_float(v[2 * i]) * inv, x1 = __uint_as_float(v[2 * i + 1]) * inv;
+                    if (a.dtype == SKM_DTYPE_BF16) {
+                        const __nv_bfloat162 y = __floats2bfloat162_rn(x0, x1);
+                        w[i] = *reinterpret_cast<const uint32_t *>(&y);
+                    } else {
+                        w[i] = pack(x0, x1);
+                    }
+                }
+                uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + at * a.d + 16 * k);
+                dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            }
+            if (in && !part && a.lse) a.lse[at] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
+        }
+    } else if (warp < MMA_WARP) {  // ------------------------------------- converters
+        // tasks: per tile KBLK blocks of keys, then KBLK of values; warp w takes w, w + CONV, ...
+        const int tasks = n * 2 * KBLK, cw = warp - CONV_WARP0, bytes = kv4_bytes(a.d);
+        constexpr int NV = DH >= 128 ? DH / 64 : 1;  // 16-byte vectors of a lane: (16-dim chunk lane / 8 + 4 k, g = lane % 8)
+        const int g = lane & 7;
+        uint8_t *mine = smem + L::scales + cw * 64;
+        const auto look = [&](int task) {  // 32 of the warp's tasks, one a lane
+            int at = -1;
+            if (task < tasks) {
+                const int blk = (t0 + task / (2 * KBLK)) * KBLK + task % KBLK;
+                if (blk * KV_B <= last && blk * KV_B + KV_B > first) {
+                    const int pg = a.table[(int64_t)b * a.cols + a.by_bpp.div(blk)];
+                    if (pg >= 0 && pg < a.pages) at = (pg * a.heads + h) * a.bpp + a.by_bpp.mod(blk);
+                }
+            }
+            return at;
+        };
+        // a block's keys or values, and of them the scale and bias of two tokens (keys: g and g + 8; values: lane % 16)
+        struct Raw {
+            uint4 code[NV];
+            uint32_t sb[2];
+        };
+        const auto load = [&](int task, int at, Raw &raw) {
+            const bool vals = task & KBLK;
+            const uint8_t *p = a.k + (int64_t)at * bytes;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                raw.code[k] = make_uint4(0, 0, 0, 0);
+                const int v = lane + 32 * k;
+                if (at >= 0 && 2 * v < a.d) raw.code[k] = __ldg(reinterpret_cast<const uint4 *>(p + (vals ? 8 * a.d : 0)) + v);
+            }
+            raw.sb[0] = raw.sb[1] = 0;
+            if (at < 0) return;
+            // tokens past the sequence's end were never written: zeros
+            const uint32_t *sc = reinterpret_cast<const uint32_t *>(p + KV_B * a.d);
+            const int left = s.len - ((t0 + task / (2 * KBLK)) * KBLK + task % KBLK) * KV_B;
+            if (vals) {
+                if ((lane & 15) < left) raw.sb[0] = __ldg(sc + 2 * (lane & 15) + 1);
+            } else {
+                if (g < left) raw.sb[0] = __ldg(sc + 2 * g);
+                if (g + 8 < left) raw.sb[1] = __ldg(sc + 2 * (g + 8));
+            }
+        };
+        Raw raw, coming;
+        int cur = look(cw + CONV * lane);
+        int at = __shfl_sync(0xffffffffu, cur, 0);
+        load(cw, at, raw);
+        int next = look(cw + CONV * (32 + lane));
+        const auto beyond = [](uint32_t sb) {  // b + 15 s above f16's largest number
+            const float2 x = __half22float2(h2(sb));
+            return fmaf(15.0f, x.x, x.y) > 65504.0f;
+        };
+        // keys: vector (chunk w, g): tokens g and g + 8, 16 dims each: two 16-byte chunks of an operand row of 64
+        // dims.  Values: dims 16 w + g and 16 w + g + 8, 16 tokens each
+        const auto keys = [&](auto big, const Raw &raw, uint32_t base) {
+            constexpr bool BIG = decltype(big)::value;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int w = (lane >> 3) + 4 * k;
+                if (16 * w >= a.d) break;
+                const uint32_t to = base + (w >> 2) * (KT * 128) + g * 128 + (((w & 3) * 2 ^ g) << 4);
+                const uint32_t c[4] = {raw.code[k].x, raw.code[k].y, raw.code[k].z, raw.code[k].w};
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const __half2 s = __low2half2(h2(raw.sb[t])), b = __high2half2(h2(raw.sb[t]));
+                    uint32_t x[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x[2 * i] = dequant2<false, BIG>(c[i] >> 8 * t, s, b);
+                        x[2 * i + 1] = dequant2<true, BIG>(c[i] >> 8 * t, s, b);
+                    }
+                    st_shared(to + t * 1024, x[0], x[1], x[2], x[3]);
+                    st_shared((to + t * 1024) ^ 16, x[4], x[5], x[6], x[7]);
+                }
+            }
+        };
+        const auto values = [&](auto big, const Raw &raw, uint32_t base, int blk) {
+            constexpr bool BIG = decltype(big)::value;
+            const uint4 s0 = *reinterpret_cast<const uint4 *>(mine), s1 = *reinterpret_cast<const uint4 *>(mine + 16);
+            const uint4 b0 = *reinterpret_cast<const uint4 *>(mine + 32), b1 = *reinterpret_cast<const uint4 *>(mine + 48);
+            const uint32_t sl[4] = {s0.x, s0.y, s0.z, s0.w}, sh[4] = {s1.x, s1.y, s1.z, s1.w};
+            const uint32_t bl[4] = {b0.x, b0.y, b0.z, b0.w}, bh[4] = {b1.x, b1.y, b1.z, b1.w};
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int w = (lane >> 3) + 4 * k;
+                if (16 * w >= a.d) break;
+                const uint32_t to = base + (16 * w + g) * 128 + ((blk * 2 ^ g) << 4);
+                const uint32_t c[4] = {raw.code[k].x, raw.code[k].y, raw.code[k].z, raw.code[k].w};
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    uint32_t x[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x[i] = dequant2<false, BIG>(c[i] >> 8 * t, h2(sl[i]), h2(bl[i]));
+                        x[4 + i] = dequant2<true, BIG>(c[i] >> 8 * t, h2(sh[i]), h2(bh[i]));
+                    }
+                    st_shared(to + t * 1024, x[0], x[1], x[2], x[3]);
+                    st_shared((to + t * 1024) ^ 16, x[4], x[5], x[6], x[7]);
+                }
+            }
+        };
+        // a task from `raw`, the next one's codes on their way to `coming`
+        const auto convert = [&](int task, int i, const Raw &raw, Raw &coming) {
+            const int slot = i & 31, j = task / (2 * KBLK), st = j & (ST - 1), blk = task & (KBLK - 1);
+            const bool vals = task & KBLK;
+            if (slot == 31) {
+                cur = next;
+                next = look(task + CONV * (33 + lane));
+            }
+            const int at_next = __shfl_sync(0xffffffffu, cur, (i + 1) & 31);
+            load(task + CONV, at_next, coming);
+            const bool big = __any_sync(0xffffffffu, beyond(raw.sb[0]) || beyond(raw.sb[1]));
+            if (vals) {
+                __syncwarp();
+                if (lane < KV_B) {
+                    reinterpret_cast<uint16_t *>(mine)[lane] = (uint16_t)raw.sb[0];
+                    reinterpret_cast<uint16_t *>(mine)[KV_B + lane] = (uint16_t)(raw.sb[0] >> 16);
+                }
+                __syncwarp();
+            }
+            if (!warp_wait(vals ? v_free(st) : k_free(st), ((j / ST) & 1) ^ 1, gone)) return false;
+            if (!vals) {
+                if (lane == 0) smem[L::there + (j & (INFO - 1)) * KBLK + blk] = at >= 0;
+                const uint32_t base = sm + L::k + st * L::TILE + blk * 2048;
+                if (big) keys(std::true_type{}, raw, base);
+                else keys(std::false_type{}, raw, base);
+            } else {
+                const uint32_t base = sm + L::v + st * L::TILE;
+                if (big) values(std::true_type{}, raw, base, blk);
+                else values(std::false_type{}, raw, base, blk);
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) arrive(vals ? v_full(st) : k_full(st));
+            at = at_next;
+            return true;
+        };
+        for (int task = cw, i = 0; task < tasks; task += 2 * CONV, i += 2) {
+            if (!convert(task, i, raw, coming)) break;
+            if (task + CONV >= tasks || !convert(task + CONV, i + 1, coming, raw)) break;
+        }
+    } else if (n > 0) {  // ------------------------------------------------ MMA issuer
+        const uint32_t one = elect_one();
+        bool ok = warp_wait(q_full, 0, gone), issued = false;
+        const uint64_t q_op = operand(sm + L::q), k_op = operand(sm + L::k), v_op = operand(sm + L::v);
+        const auto qk = [&](int q, int j) {
+            const uint32_t d = tmem + (2 * q + (j & 1)) * KT;
+            const uint64_t qa = q_op + (uint32_t)q * (L::QTILE >> 4), ka = k_op + (uint32_t)(j & (ST - 1)) * (L::TILE >> 4);
+            mma_ss<false>(d, qa, ka, idesc(KT), one);
+#pragma unroll
+            for (int k = 1; k < DH / 16; ++k)
+                mma_ss<true>(d, qa + ((k >> 2) * (QT * 128 >> 4) + 2 * (k & 3)), ka + ((k >> 2) * (KT * 128 >> 4) + 2 * (k & 3)),
+                             idesc(KT), one);
+            issued = true;
+            commit(s_full(q, j & 1), one);
+        };
+        // the logits of two key tiles ahead
+        const int nt[2] = {tiles_for(0), tiles_for(1)};
+        for (int j = 0; j < 2 && j < n && ok; ++j) {
+            if (!(ok = warp_wait(k_full(j), 0, gone))) break;
+            fence_after();
+            for (int q = 0; q < nq; ++q)
+                if (j < nt[q]) qk(q, j);
+            commit(k_free(j), one);
+        }
+        for (int j = 0; j < n && ok; ++j) {
+            const int st = j & (ST - 1), ahead = (j + 2) & (ST - 1);
+            bool have_v = false, have_k = false;
+            for (int q = 0; q < nq; ++q) {
+                if (j >= nt[q]) continue;
+                if (!(ok = warp_wait(p_full(q, j & 1), (j >> 1) & 1, gone))) break;
+                if (!have_v && !(ok = warp_wait(v_full(st), (j / ST) & 1, gone))) break;
+                have_v = true;
+                fence_after();
+                const uint32_t p = tmem + (2 * q + (j & 1)) * KT, o = tmem + L::O + q * DH;
+                const uint64_t va = v_op + (uint32_t)st * (L::TILE >> 4);
+#pragma unroll
+                for (int k = 0; k < KT / 16; ++k) mma_ts(o, p + 8 * k, va + 2 * k, idesc(DH), k > 0 || j > 0, one);
+                if (q == nq - 1) commit(v_free(st), one);
+                commit(o_done(q), one);
+                // a barrier of its own for the last product: the softmax may be up to two
+                // phases of o_done away from it, more than a parity tells apart.  Committed
+                // last, so that nothing arrives after the tile's rows are out
+                if (j == nt[q] - 1) commit(o_last(q), one);
+                if (j + 2 < nt[q]) {  // over the buffer that P V read, in order behind it
+                    if (!have_k) {
+                        if (!(ok = warp_wait(k_full(ahead), ((j + 2) / ST) & 1, gone))) break;
+                        have_k = true;
+                        fence_after();
+                    }
+                    qk(q, j + 2);
+                    if (q == nq - 1) commit(k_free(ahead), one);
+                }
+            }
+        }
+        if (!ok && issued) {  // what was issued ends before the memory is given up
+            commit(drain, one);
+            bar_wait(drain, 0, KV_WAIT_NS);
+        }
+    }
+    __syncwarp();
+    fence_before();
+    __syncthreads();
+    if (warp == MMA_WARP) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+template <int DH>
+cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
+    static SmemLimit limit;
+    cudaError_t e = limit.launch(kv4_prompt_kernel<DH>, Lay<DH>::total, [&] {
+        kv4_prompt_kernel<DH><<<(unsigned)(p.units * p.splits), Lay<DH>::THREADS, Lay<DH>::total, st>>>(
+            a, p.splits, p.splits > 1 ? a.part_cta : nullptr);
+    });
+    if (e != cudaSuccess || p.splits == 1) return e;
+    return run_prompt_join(a, p, Lay<DH>::ROWS, st);
+}
+
+}  // namespace
+
+cudaError_t launch_kv4_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
+    return a.d <= 64 ? run_prompt<64>(a, p, st) : a.d <= 128 ? run_prompt<128>(a, p, st) : run_prompt<256>(a, p, st);
+}
+
+}  // namespace skm

@@ -132,7 +132,7 @@ struct AttendPlan {
 AttendPlan plan_attend(const Cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, Carver &cv) {
     AttendPlan p;
     const int nb = p.seqs = std::min<int>(s->batch, KV_MAX_SEQS), group = a->heads_q / c->heads, most = most_tokens(s);
-    p.prompt = !c->four && kv_prompt_ok(a->dtype, nb, c->heads, c->d, (int64_t)most * group, span_of(c, s, a));
+    p.prompt = kv_prompt_ok(a->dtype, nb, c->heads, c->d, (int64_t)most * group, span_of(c, s, a));
     if (p.prompt) {
         p.many = kv_prompt_plan(nb, c->heads, group, c->d, most, span_of(c, s, a));
         if (p.many.part) p.part_cta = cv.take<float>(p.many.part / 4);
@@ -191,7 +191,7 @@ size_t attend_workspace_size(const Cache *c, const skm_kv_seqs *s, const skm_kv_
     const int64_t span = std::min<int64_t>(s->max_len, (int64_t)s->cols * c->page);
     const int64_t rows = (int64_t)most_tokens(s) * (a->heads_q / c->heads);
     size_t most = (c->four ? kv4_rows_part_most : kv_rows_part_most)(std::min<int>(s->batch, KV_MAX_SEQS), c->heads, c->d, a->dtype, rows, span);
-    if (!c->four && a->dtype != SKM_DTYPE_F32 && rows > KV_ROWS_MOST) most = std::max(most, kv_prompt_part_most(c->d, span));
+    if (a->dtype != SKM_DTYPE_F32 && rows > KV_ROWS_MOST) most = std::max(most, kv_prompt_part_most(c->d, span));
     return most;
 }
 
@@ -255,7 +255,7 @@ int attend(const Cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws,
         if (p.prompt) {
             KvPromptPlan q = p.many;
             q.units = (int64_t)k.nb * k.heads * k.max_tiles;
-            SKM_CUDA_TRY(launch_kv_prompt(k, q, S(stream)));
+            SKM_CUDA_TRY((c->four ? launch_kv4_prompt : launch_kv_prompt)(k, q, S(stream)));
         } else {
             KvRowsPlan q = p.rows;
             q.units = (int64_t)k.nb * k.max_tiles * k.heads;

@@ -545,6 +545,19 @@ def test_attend_values_around_a_far_mean(cuda_ok, typ, new):
     check_attend(2, 4, 64, 16, typ, [(300, new), (61, new)], spoil=spoil)
 
 
+@pytest.mark.parametrize("new", [1, 100])
+def test_attend_values_at_the_ends_of_f16(cuda_ok, new):
+    """Vectors from -65504 to 65504, whose largest code stands for more than f16 holds."""
+    def spoil(c):
+        sc = scales(c)
+        sc[:, :, :, 3::4, 1::2] = -65504.0
+        sc[:, :, :, 3::4, 0::2] = 8736.0  # the smallest with -65504 + 15 s >= 65504
+        c.blocks[..., :16 * c.d] |= c.blocks[..., :16 * c.d] << 1  # (many codes of 15)
+
+    # the bound counts a value of up to 65536, taken as 65504: 2^-11 of it
+    check_attend(2, 4, 64, 16, "bf16", [(300, new), (61, new)], spoil=spoil, scale=1e-6)
+
+
 def test_attend_hints_may_be_larger(cuda_ok):
     check_attend(2, 4, 64, 16, "bf16", [(90, 1), (3, 1)], max_len=5000, max_tokens=4)
     check_attend(2, 4, 64, 16, "bf16", [(90, 20), (3, 7)], max_len=5000, max_tokens=900)
