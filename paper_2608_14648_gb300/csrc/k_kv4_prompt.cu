@@ -13,7 +13,6 @@ namespace skm {
 
 namespace {
 
-constexpr int CONV = 7;  // converter warps
 constexpr float TILE_MOST = 65000.0f;  // a tile's sum of weights: above it one may pass the largest f16
 // tiles whose absent blocks are noted.  A K stage is free once its product is through, which is issued when the softmax
 // has handed over the tile two before: tile j + ST (at most 4) comes while it reads tile j - 1 at the earliest, 5 behind
@@ -25,10 +24,18 @@ struct Lay {
     static constexpr int NQ = DH <= 128 ? 2 : 1;      // row tiles of a CTA
     static constexpr int ST = DH <= 128 ? 4 : 2;      // K and V tiles in flight
     static constexpr int ROWS = NQ * QT;
-    static constexpr int CONV_WARP0 = 4 * NQ, MMA_WARP = CONV_WARP0 + CONV, THREADS = 32 * (MMA_WARP + 1);
+    // converter warps.  A barrier's parity tells a phase from the next one only, so a warp may not come to a stage two rounds
+    // early: from a task to its next one it goes on by no more tiles than there are stages, and it has
+    // waited for the product of the tile ST before the first one's
+    static constexpr int CONV = NQ == 2 ? 10 : 7;
+    static_assert((CONV + KBLK - 1) / KBLK <= ST);
+    static constexpr int CONV_WARP0 = 4 * NQ, MMA_WARP = CONV_WARP0 + CONV, THREADS = 32 * (MMA_WARP + NQ);
+    // two row tiles: registers of a softmax thread and of the others, no more in all than the 96 each that the launch comes with
+    static constexpr int SOFT_REGS = 144, REST_REGS = 64;
+    static_assert(NQ == 1 || CONV_WARP0 * SOFT_REGS + (THREADS / 32 - CONV_WARP0) * REST_REGS <= THREADS / 32 * (65536 / THREADS / 8 * 8));
     static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
     static constexpr int q = 0, k = NQ * QTILE, v = k + ST * TILE, bars = v + ST * TILE;
-    static constexpr int slots = bars + 8 * (4 * ST + 14);  // TMEM address, a flag, the part's index
+    static constexpr int slots = bars + 8 * (4 * ST + 16);  // TMEM address, a flag, the part's index
     static constexpr int wild = slots + 32;    // a byte a row: its query holds infinities or NaN
     static constexpr int there = wild + ROWS;  // a byte a block of the last INFO tiles: its page is present
     static constexpr int scales = (there + INFO * KBLK + 63) / 64 * 64;  // [converter warp][value scales, biases of 16 tokens]
@@ -75,7 +82,7 @@ template <int DH>
 __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     kv4_prompt_kernel(const __grid_constant__ KvAttnArgs a, int splits, float *parts) {
     using L = Lay<DH>;
-    constexpr int ST = L::ST, ROWS = L::ROWS, CONV_WARP0 = L::CONV_WARP0, MMA_WARP = L::MMA_WARP, THREADS = L::THREADS;
+    constexpr int ST = L::ST, CONV = L::CONV, ROWS = L::ROWS, CONV_WARP0 = L::CONV_WARP0, MMA_WARP = L::MMA_WARP, THREADS = L::THREADS;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t *smem = smem_raw + ((1024 - (su32(smem_raw) & 1023)) & 1023);  // swizzle atoms
@@ -89,7 +96,8 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     const auto p_full = [&](int q, int buf) { return bar(4 * ST + 4 + 2 * q + buf); };
     const auto o_done = [&](int q) { return bar(4 * ST + 8 + q); };
     const auto o_last = [&](int q) { return bar(4 * ST + 10 + q); };
-    const uint32_t q_full = bar(4 * ST + 12), drain = bar(4 * ST + 13);
+    const auto q_full = [&](int q) { return bar(4 * ST + 12 + q); };
+    const auto drain = [&](int q) { return bar(4 * ST + 14 + q); };
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::slots);
     volatile int32_t *gone = reinterpret_cast<volatile int32_t *>(smem + L::slots + 4);
 
@@ -145,12 +153,11 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         const auto init = [&](uint32_t b, int count) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(b), "r"(count) : "memory");
         };
-        for (int i = 0; i < ST; ++i) init(k_full(i), KBLK), init(v_full(i), KBLK), init(k_free(i), 1), init(v_free(i), 1);
+        for (int i = 0; i < ST; ++i) init(k_full(i), KBLK), init(v_full(i), KBLK), init(k_free(i), L::NQ), init(v_free(i), L::NQ);
         for (int q = 0; q < L::NQ; ++q) {
             for (int i = 0; i < 2; ++i) init(s_full(q, i), 1), init(p_full(q, i), 4);
-            init(o_done(q), 1), init(o_last(q), 1);
+            init(o_done(q), 1), init(o_last(q), 1), init(q_full(q), 4), init(drain(q), 1);
         }
-        init(q_full, 4 * L::NQ), init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *gone = 0;
     }
@@ -168,11 +175,9 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    // (two row tiles: the softmax threads hold a tile's 64 logits and its weights.  168 and 88 registers for
-    // 256 threads each are the 128 of all 512 that the launch comes with)
     if constexpr (L::NQ == 2) {
-        if (warp < CONV_WARP0) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
-        else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp < CONV_WARP0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFT_REGS));
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::REST_REGS));
     }
     if (warp < CONV_WARP0) {  // ------------------------------------------ softmax
         const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row, nt = tiles_for(q);
@@ -181,7 +186,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                                         smem + L::wild + q * QT);
         fence_async();
         __syncwarp();
-        if (lane == 0) arrive(q_full);
+        if (lane == 0) arrive(q_full(q));
         // (rows past the end see everything, with no weight: they slow no one down)
         const int hi = in ? last_of(a, s, r) : 0x7ffffffe, lo = in ? first_of(a, s, r) : 0;
         // rows of the warp see [low, high] whole
@@ -343,15 +348,15 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             if (in && !part && a.lse) a.lse[at] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
         }
     } else if (warp < MMA_WARP) {  // ------------------------------------- converters
-        // tasks: per tile KBLK blocks of keys, then KBLK of values; warp w takes w, w + CONV, ...
-        const int tasks = n * 2 * KBLK, cw = warp - CONV_WARP0, bytes = kv4_bytes(a.d);
+        // tasks: the blocks of all tiles, keys and values; warp w takes w, w + CONV, ...
+        const int tasks = n * KBLK, cw = warp - CONV_WARP0, bytes = kv4_bytes(a.d);
         constexpr int NV = DH >= 128 ? DH / 64 : 1;  // 16-byte vectors of a lane: (16-dim chunk lane / 8 + 4 k, g = lane % 8)
-        const int g = lane & 7;
+        const int g = lane & 7, w0 = lane >> 3;
         uint8_t *mine = smem + L::scales + cw * 64;
         const auto look = [&](int task) {  // 32 of the warp's tasks, one a lane
             int at = -1;
             if (task < tasks) {
-                const int blk = (t0 + task / (2 * KBLK)) * KBLK + task % KBLK;
+                const int blk = t0 * KBLK + task;
                 if (blk * KV_B <= last && blk * KV_B + KV_B > first) {
                     const int pg = a.table[(int64_t)b * a.cols + a.by_bpp.div(blk)];
                     if (pg >= 0 && pg < a.pages) at = (pg * a.heads + h) * a.bpp + a.by_bpp.mod(blk);
@@ -359,187 +364,163 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             }
             return at;
         };
-        // a block's keys or values, and of them the scale and bias of two tokens (keys: g and g + 8; values: lane % 16)
-        struct Raw {
-            uint4 code[NV];
-            uint32_t sb[2];
-        };
-        const auto load = [&](int task, int at, Raw &raw) {
-            const bool vals = task & KBLK;
-            const uint8_t *p = a.k + (int64_t)at * bytes;
+        // codes of a block's keys or values; of an absent one zeros
+        const auto load = [&](int at, int from, uint4 (&code)[NV]) {
+            const uint4 *p = reinterpret_cast<const uint4 *>(a.k + (int64_t)at * bytes + from) + lane;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                raw.code[k] = make_uint4(0, 0, 0, 0);
-                const int v = lane + 32 * k;
-                if (at >= 0 && 2 * v < a.d) raw.code[k] = __ldg(reinterpret_cast<const uint4 *>(p + (vals ? 8 * a.d : 0)) + v);
-            }
-            raw.sb[0] = raw.sb[1] = 0;
-            if (at < 0) return;
-            // tokens past the sequence's end were never written: zeros
-            const uint32_t *sc = reinterpret_cast<const uint32_t *>(p + KV_B * a.d);
-            const int left = s.len - ((t0 + task / (2 * KBLK)) * KBLK + task % KBLK) * KV_B;
-            if (vals) {
-                if ((lane & 15) < left) raw.sb[0] = __ldg(sc + 2 * (lane & 15) + 1);
-            } else {
-                if (g < left) raw.sb[0] = __ldg(sc + 2 * g);
-                if (g + 8 < left) raw.sb[1] = __ldg(sc + 2 * (g + 8));
+                code[k] = make_uint4(0, 0, 0, 0);
+                if (at >= 0 && 2 * (lane + 32 * k) < a.d) code[k] = __ldg(p + 32 * k);
             }
         };
-        Raw raw, coming;
+        // scale and bias of a token's key (0) or value (1); tokens past the sequence's end were never written: zeros
+        const auto scale = [&](int at, int task, int t, int which) {
+            if (at < 0 || t >= s.len - (t0 * KBLK + task) * KV_B) return 0u;
+            return __ldg(reinterpret_cast<const uint32_t *>(a.k + (int64_t)at * bytes + KV_B * a.d) + 2 * t + which);
+        };
+        uint4 kc[NV], vc[NV];
+        uint32_t ks[2], vs;  // of tokens g and g + 8; of token lane % 16
+        const auto load_keys = [&](int at, int task) {
+            load(at, 0, kc);
+            ks[0] = scale(at, task, g, 0), ks[1] = scale(at, task, g + 8, 0);
+        };
+        const auto load_values = [&](int at, int task) {
+            load(at, 8 * a.d, vc);
+            vs = scale(at, task, lane & 15, 1);
+        };
         int cur = look(cw + CONV * lane);
         int at = __shfl_sync(0xffffffffu, cur, 0);
-        load(cw, at, raw);
-        int next = look(cw + CONV * (32 + lane));
+        load_keys(at, cw);
+        load_values(at, cw);
         const auto beyond = [](uint32_t sb) {  // b + 15 s above f16's largest number
             const float2 x = __half22float2(h2(sb));
             return fmaf(15.0f, x.x, x.y) > 65504.0f;
         };
         // keys: vector (chunk w, g): tokens g and g + 8, 16 dims each: two 16-byte chunks of an operand row of 64
         // dims.  Values: dims 16 w + g and 16 w + g + 8, 16 tokens each
-        const auto keys = [&](auto big, const Raw &raw, uint32_t base) {
+        const uint32_t k_to = sm + L::k + g * 128 + (((w0 & 3) * 2 ^ g) << 4);
+        const uint32_t v_to = sm + L::v + (16 * w0 + g) * 128;
+        const auto keys = [&](auto big, uint32_t to) {
             constexpr bool BIG = decltype(big)::value;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                const int w = (lane >> 3) + 4 * k;
-                if (16 * w >= a.d) break;
-                const uint32_t to = base + (w >> 2) * (KT * 128) + g * 128 + (((w & 3) * 2 ^ g) << 4);
-                const uint32_t c[4] = {raw.code[k].x, raw.code[k].y, raw.code[k].z, raw.code[k].w};
+                if (16 * (w0 + 4 * k) >= a.d) break;
+                const uint32_t c[4] = {kc[k].x, kc[k].y, kc[k].z, kc[k].w};
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const __half2 s = __low2half2(h2(raw.sb[t])), b = __high2half2(h2(raw.sb[t]));
+                    const __half2 s = __low2half2(h2(ks[t])), b = __high2half2(h2(ks[t]));
                     uint32_t x[8];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         x[2 * i] = dequant2<false, BIG>(c[i] >> 8 * t, s, b);
                         x[2 * i + 1] = dequant2<true, BIG>(c[i] >> 8 * t, s, b);
                     }
-                    st_shared(to + t * 1024, x[0], x[1], x[2], x[3]);
-                    st_shared((to + t * 1024) ^ 16, x[4], x[5], x[6], x[7]);
+                    st_shared(to + k * (KT * 128) + t * 1024, x[0], x[1], x[2], x[3]);
+                    st_shared((to + k * (KT * 128) + t * 1024) ^ 16, x[4], x[5], x[6], x[7]);
                 }
             }
         };
-        const auto values = [&](auto big, const Raw &raw, uint32_t base, int blk) {
+        const auto values = [&](auto big, uint32_t to) {
             constexpr bool BIG = decltype(big)::value;
-            const uint4 s0 = *reinterpret_cast<const uint4 *>(mine), s1 = *reinterpret_cast<const uint4 *>(mine + 16);
-            const uint4 b0 = *reinterpret_cast<const uint4 *>(mine + 32), b1 = *reinterpret_cast<const uint4 *>(mine + 48);
-            const uint32_t sl[4] = {s0.x, s0.y, s0.z, s0.w}, sh[4] = {s1.x, s1.y, s1.z, s1.w};
-            const uint32_t bl[4] = {b0.x, b0.y, b0.z, b0.w}, bh[4] = {b1.x, b1.y, b1.z, b1.w};
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int w = (lane >> 3) + 4 * k;
-                if (16 * w >= a.d) break;
-                const uint32_t to = base + (16 * w + g) * 128 + ((blk * 2 ^ g) << 4);
-                const uint32_t c[4] = {raw.code[k].x, raw.code[k].y, raw.code[k].z, raw.code[k].w};
+            for (int half = 0; half < 2; ++half) {  // tokens 0 .. 7, 8 .. 15
+                const uint4 s4 = *reinterpret_cast<const uint4 *>(mine + 16 * half), b4 = *reinterpret_cast<const uint4 *>(mine + 32 + 16 * half);
+                const uint32_t s[4] = {s4.x, s4.y, s4.z, s4.w}, b[4] = {b4.x, b4.y, b4.z, b4.w};
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    uint32_t x[8];
+                for (int k = 0; k < NV; ++k) {
+                    if (16 * (w0 + 4 * k) >= a.d) break;
+                    const uint32_t c[4] = {vc[k].x, vc[k].y, vc[k].z, vc[k].w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x[i] = dequant2<false, BIG>(c[i] >> 8 * t, h2(sl[i]), h2(bl[i]));
-                        x[4 + i] = dequant2<true, BIG>(c[i] >> 8 * t, h2(sh[i]), h2(bh[i]));
+                    for (int t = 0; t < 2; ++t) {
+                        uint32_t x[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            x[i] = half ? dequant2<true, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i])) : dequant2<false, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i]));
+                        st_shared((to + k * 8192 + t * 1024) ^ (16 * half), x[0], x[1], x[2], x[3]);
                     }
-                    st_shared(to + t * 1024, x[0], x[1], x[2], x[3]);
-                    st_shared((to + t * 1024) ^ 16, x[4], x[5], x[6], x[7]);
                 }
             }
         };
-        // a task from `raw`, the next one's codes on their way to `coming`
-        const auto convert = [&](int task, int i, const Raw &raw, Raw &coming) {
-            const int slot = i & 31, j = task / (2 * KBLK), st = j & (ST - 1), blk = task & (KBLK - 1);
-            const bool vals = task & KBLK;
-            if (slot == 31) {
-                cur = next;
-                next = look(task + CONV * (33 + lane));
-            }
+        for (int task = cw, i = 0; task < tasks; task += CONV, ++i) {
+            const int j = task / KBLK, st = j & (ST - 1), blk = task & (KBLK - 1);
+            if ((i & 31) == 31) cur = look(task + CONV * (1 + lane));
             const int at_next = __shfl_sync(0xffffffffu, cur, (i + 1) & 31);
-            load(task + CONV, at_next, coming);
-            const bool big = __any_sync(0xffffffffu, beyond(raw.sb[0]) || beyond(raw.sb[1]));
-            if (vals) {
-                __syncwarp();
-                if (lane < KV_B) {
-                    reinterpret_cast<uint16_t *>(mine)[lane] = (uint16_t)raw.sb[0];
-                    reinterpret_cast<uint16_t *>(mine)[KV_B + lane] = (uint16_t)(raw.sb[0] >> 16);
-                }
-                __syncwarp();
-            }
-            if (!warp_wait(vals ? v_free(st) : k_free(st), ((j / ST) & 1) ^ 1, gone)) return false;
-            if (!vals) {
-                if (lane == 0) smem[L::there + (j & (INFO - 1)) * KBLK + blk] = at >= 0;
-                const uint32_t base = sm + L::k + st * L::TILE + blk * 2048;
-                if (big) keys(std::true_type{}, raw, base);
-                else keys(std::false_type{}, raw, base);
-            } else {
-                const uint32_t base = sm + L::v + st * L::TILE;
-                if (big) values(std::true_type{}, raw, base, blk);
-                else values(std::false_type{}, raw, base, blk);
-            }
+            const bool big = __any_sync(0xffffffffu, beyond(ks[0]) || beyond(ks[1]) || beyond(vs));
+            if (!warp_wait(k_free(st), ((j / ST) & 1) ^ 1, gone)) break;
+            if (lane == 0) smem[L::there + (j & (INFO - 1)) * KBLK + blk] = at >= 0;
+            if (big) keys(std::true_type{}, k_to + st * L::TILE + blk * 2048);
+            else keys(std::false_type{}, k_to + st * L::TILE + blk * 2048);
             fence_async();
             __syncwarp();
-            if (lane == 0) arrive(vals ? v_full(st) : k_full(st));
+            if (lane == 0) arrive(k_full(st));
+            load_keys(at_next, task + CONV);
+            if (lane < KV_B) {
+                reinterpret_cast<uint16_t *>(mine)[lane] = (uint16_t)vs;
+                reinterpret_cast<uint16_t *>(mine)[KV_B + lane] = (uint16_t)(vs >> 16);
+            }
+            __syncwarp();
+            if (!warp_wait(v_free(st), ((j / ST) & 1) ^ 1, gone)) break;
+            if (big) values(std::true_type{}, v_to + st * L::TILE + ((blk * 2 ^ g) << 4));
+            else values(std::false_type{}, v_to + st * L::TILE + ((blk * 2 ^ g) << 4));
+            fence_async();
+            __syncwarp();
+            if (lane == 0) arrive(v_full(st));
+            load_values(at_next, task + CONV);
             at = at_next;
-            return true;
-        };
-        for (int task = cw, i = 0; task < tasks; task += 2 * CONV, i += 2) {
-            if (!convert(task, i, raw, coming)) break;
-            if (task + CONV >= tasks || !convert(task + CONV, i + 1, coming, raw)) break;
         }
-    } else if (n > 0) {  // ------------------------------------------------ MMA issuer
+    } else if (n > 0) {  // ------------------------------------------------ MMA issuer of a row tile
         const uint32_t one = elect_one();
-        bool ok = warp_wait(q_full, 0, gone), issued = false;
-        const uint64_t q_op = operand(sm + L::q), k_op = operand(sm + L::k), v_op = operand(sm + L::v);
-        const auto qk = [&](int q, int j) {
+        const int q = warp - MMA_WARP, nt = tiles_for(q);
+        bool ok = nt == 0 || warp_wait(q_full(q), 0, gone), issued = false;
+        const uint64_t q_op = operand(sm + L::q + q * L::QTILE), k_op = operand(sm + L::k), v_op = operand(sm + L::v);
+        // a stage is free when both row tiles are through with it; a key tile that this one does not go through is waited for all the same
+        const auto skip = [&](uint32_t full, uint32_t parity, uint32_t free) {
+            ok = warp_wait(full, parity, gone);
+            if (ok && lane == 0) arrive(free);
+        };
+        const auto qk = [&](int j) {
+            const int st = j & (ST - 1);
+            if (j >= nt) return skip(k_full(st), (j / ST) & 1, k_free(st));
+            if (!(ok = warp_wait(k_full(st), (j / ST) & 1, gone))) return;
+            fence_after();
             const uint32_t d = tmem + (2 * q + (j & 1)) * KT;
-            const uint64_t qa = q_op + (uint32_t)q * (L::QTILE >> 4), ka = k_op + (uint32_t)(j & (ST - 1)) * (L::TILE >> 4);
-            mma_ss<false>(d, qa, ka, idesc(KT), one);
+            const uint64_t ka = k_op + (uint32_t)st * (L::TILE >> 4);
+            mma_ss<false>(d, q_op, ka, idesc(KT), one);
 #pragma unroll
             for (int k = 1; k < DH / 16; ++k)
-                mma_ss<true>(d, qa + ((k >> 2) * (QT * 128 >> 4) + 2 * (k & 3)), ka + ((k >> 2) * (KT * 128 >> 4) + 2 * (k & 3)),
+                mma_ss<true>(d, q_op + ((k >> 2) * (QT * 128 >> 4) + 2 * (k & 3)), ka + ((k >> 2) * (KT * 128 >> 4) + 2 * (k & 3)),
                              idesc(KT), one);
             issued = true;
             commit(s_full(q, j & 1), one);
+            commit(k_free(st), one);
         };
         // the logits of two key tiles ahead
-        const int nt[2] = {tiles_for(0), tiles_for(1)};
-        for (int j = 0; j < 2 && j < n && ok; ++j) {
-            if (!(ok = warp_wait(k_full(j), 0, gone))) break;
-            fence_after();
-            for (int q = 0; q < nq; ++q)
-                if (j < nt[q]) qk(q, j);
-            commit(k_free(j), one);
-        }
+        for (int j = 0; j < 2 && j < n && ok; ++j) qk(j);
         for (int j = 0; j < n && ok; ++j) {
-            const int st = j & (ST - 1), ahead = (j + 2) & (ST - 1);
-            bool have_v = false, have_k = false;
-            for (int q = 0; q < nq; ++q) {
-                if (j >= nt[q]) continue;
+            const int st = j & (ST - 1);
+            if (j < nt) {
+                if (!(ok = warp_wait(v_full(st), (j / ST) & 1, gone))) break;
                 if (!(ok = warp_wait(p_full(q, j & 1), (j >> 1) & 1, gone))) break;
-                if (!have_v && !(ok = warp_wait(v_full(st), (j / ST) & 1, gone))) break;
-                have_v = true;
                 fence_after();
                 const uint32_t p = tmem + (2 * q + (j & 1)) * KT, o = tmem + L::O + q * DH;
                 const uint64_t va = v_op + (uint32_t)st * (L::TILE >> 4);
 #pragma unroll
                 for (int k = 0; k < KT / 16; ++k) mma_ts(o, p + 8 * k, va + 2 * k, idesc(DH), k > 0 || j > 0, one);
-                if (q == nq - 1) commit(v_free(st), one);
+                commit(v_free(st), one);
                 commit(o_done(q), one);
                 // a barrier of its own for the last product: the softmax may be up to two
                 // phases of o_done away from it, more than a parity tells apart.  Committed
                 // last, so that nothing arrives after the tile's rows are out
-                if (j == nt[q] - 1) commit(o_last(q), one);
-                if (j + 2 < nt[q]) {  // over the buffer that P V read, in order behind it
-                    if (!have_k) {
-                        if (!(ok = warp_wait(k_full(ahead), ((j + 2) / ST) & 1, gone))) break;
-                        have_k = true;
-                        fence_after();
-                    }
-                    qk(q, j + 2);
-                    if (q == nq - 1) commit(k_free(ahead), one);
-                }
+                if (j == nt - 1) commit(o_last(q), one);
+            } else {
+                skip(v_full(st), (j / ST) & 1, v_free(st));
+                if (!ok) break;
             }
+            if (j + 2 < n) qk(j + 2);  // over the buffer that P V read, in order behind it
         }
         if (!ok && issued) {  // what was issued ends before the memory is given up
-            commit(drain, one);
-            bar_wait(drain, 0, KV_WAIT_NS);
+            commit(drain(q), one);
+            bar_wait(drain(q), 0, KV_WAIT_NS);
         }
     }
     __syncwarp();
