@@ -14,8 +14,8 @@ namespace skm {
 namespace {
 
 constexpr float TILE_MOST = 65000.0f;  // a tile's sum of weights: above it one may pass the largest f16
-// tiles whose absent blocks are noted.  A K stage is free once its product is through, which is issued when the softmax
-// has handed over the tile two before: tile j + ST (at most 4) comes while it reads tile j - 1 at the earliest, 5 behind
+// tiles whose absent blocks are noted: a key stage is free once both row tiles' products are through, which are issued
+// when their softmax has handed over the tile two before: tile j + ST comes while it reads tile j - 1 at the earliest, 5 behind
 constexpr int INFO = 8;
 
 // DH: dims, padded to 64, 128 or 256
@@ -25,8 +25,8 @@ struct Lay {
     static constexpr int ST = DH <= 128 ? 4 : 2;      // K and V tiles in flight
     static constexpr int ROWS = NQ * QT;
     // converter warps.  A barrier's parity tells a phase from the next one only, so a warp may not come to a stage two rounds
-    // early: from a task to its next one it goes on by no more tiles than there are stages, and it has
-    // waited for the product of the tile ST before the first one's
+    // early: from a task to its next one it goes on by no more stages than there are, and for the first one it has
+    // waited until its stage was free
     static constexpr int CONV = NQ == 2 ? 10 : 7;
     static_assert((CONV + KBLK - 1) / KBLK <= ST);
     static constexpr int CONV_WARP0 = 4 * NQ, MMA_WARP = CONV_WARP0 + CONV, THREADS = 32 * (MMA_WARP + NQ);
@@ -35,8 +35,8 @@ struct Lay {
     static_assert(NQ == 1 || CONV_WARP0 * SOFT_REGS + (THREADS / 32 - CONV_WARP0) * REST_REGS <= THREADS / 32 * (65536 / THREADS / 8 * 8));
     static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
     static constexpr int q = 0, k = NQ * QTILE, v = k + ST * TILE, bars = v + ST * TILE;
-    static constexpr int slots = bars + 8 * (4 * ST + 16);  // TMEM address, a flag, the part's index
-    static constexpr int wild = slots + 32;    // a byte a row: its query holds infinities or NaN
+    static constexpr int slots = bars + 8 * (6 * ST + 10);  // TMEM address, a flag, the part's index
+    static constexpr int wild = (slots + 24 + 15) / 16 * 16;  // a byte a row: its query holds infinities or NaN
     static constexpr int there = wild + ROWS;  // a byte a block of the last INFO tiles: its page is present
     static constexpr int scales = (there + INFO * KBLK + 63) / 64 * 64;  // [converter warp][value scales, biases of 16 tokens]
     // one CTA an SM: it takes all of TMEM
@@ -88,16 +88,15 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     uint8_t *smem = smem_raw + ((1024 - (su32(smem_raw) & 1023)) & 1023);  // swizzle atoms
     const uint32_t sm = su32(smem);
     const auto bar = [&](int i) { return sm + L::bars + 8 * i; };
-    const auto k_full = [&](int s) { return bar(s); };
-    const auto k_free = [&](int s) { return bar(ST + s); };
-    const auto v_full = [&](int s) { return bar(2 * ST + s); };
-    const auto v_free = [&](int s) { return bar(3 * ST + s); };
-    const auto s_full = [&](int q, int buf) { return bar(4 * ST + 2 * q + buf); };
-    const auto p_full = [&](int q, int buf) { return bar(4 * ST + 4 + 2 * q + buf); };
-    const auto o_done = [&](int q) { return bar(4 * ST + 8 + q); };
-    const auto o_last = [&](int q) { return bar(4 * ST + 10 + q); };
-    const auto q_full = [&](int q) { return bar(4 * ST + 12 + q); };
-    const auto drain = [&](int q) { return bar(4 * ST + 14 + q); };
+    // Everything that the products of step (row tile q, key tile j) wait for arrives at one barrier: the weights of (q, j),
+    // the values of tile j, the keys of tile j + 2.  Logits of (q, j) there: and P V of tile j - 2, in order before them
+    const auto k_first = [&](int j) { return bar(j); };  // the keys of the first two tiles
+    const auto k_free = [&](int q, int s) { return bar(2 + q * ST + s); };
+    const auto v_free = [&](int q, int s) { return bar(2 + 2 * ST + q * ST + s); };
+    const auto ready = [&](int q, int s) { return bar(2 + 4 * ST + q * ST + s); };
+    const auto s_full = [&](int q, int buf) { return bar(2 + 6 * ST + 2 * q + buf); };
+    const auto q_full = [&](int q) { return bar(6 + 6 * ST + q); };
+    const auto drain = [&](int q) { return bar(8 + 6 * ST + q); };
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::slots);
     volatile int32_t *gone = reinterpret_cast<volatile int32_t *>(smem + L::slots + 4);
 
@@ -153,10 +152,10 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         const auto init = [&](uint32_t b, int count) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(b), "r"(count) : "memory");
         };
-        for (int i = 0; i < ST; ++i) init(k_full(i), KBLK), init(v_full(i), KBLK), init(k_free(i), L::NQ), init(v_free(i), L::NQ);
+        for (int i = 0; i < 2; ++i) init(k_first(i), KBLK);
         for (int q = 0; q < L::NQ; ++q) {
-            for (int i = 0; i < 2; ++i) init(s_full(q, i), 1), init(p_full(q, i), 4);
-            init(o_done(q), 1), init(o_last(q), 1), init(q_full(q), 4), init(drain(q), 1);
+            for (int i = 0; i < ST; ++i) init(k_free(q, i), 1), init(v_free(q, i), 1), init(ready(q, i), 4 + 2 * KBLK);
+            init(s_full(q, 0), 1), init(s_full(q, 1), 1), init(q_full(q), 4), init(drain(q), 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *gone = 0;
@@ -268,7 +267,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                 m = to;
                 l *= g;
                 if (j > 0) {
-                    if (!(ok = warp_wait(o_done(q), (j - 1) & 1, gone))) break;
+                    if (!(ok = warp_wait(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1, gone))) break;  // P V of tile j - 1 is through
                     fence_after();
 #pragma unroll 1
                     for (int k = 0; k < DH / 16; ++k) {
@@ -292,11 +291,11 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             st_wait();
             fence_before();
             __syncwarp();
-            if (lane == 0) arrive(p_full(q, j & 1));
+            if (lane == 0) arrive(ready(q, j % ST));
         }
         if (q < nq) {
             if (ok && nt > 0) {
-                ok = warp_wait(o_last(q), 0, gone);
+                ok = warp_wait(s_full(q, (nt + 1) & 1), ((nt + 1) >> 1) & 1, gone);
                 fence_after();
             }
             if (!ok) {
@@ -441,84 +440,83 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                 }
             }
         };
+        // A stage is free when the row tiles that go through its tile are through with it: even lanes ask the first one's
+        // barrier, odd ones the second's
+        const int ask = nq == 2 ? lane & 1 : 0, nt0 = tiles_for(0);
         for (int task = cw, i = 0; task < tasks; task += CONV, ++i) {
-            const int j = task / KBLK, st = j & (ST - 1), blk = task & (KBLK - 1);
+            const int j = task / KBLK, st = j % ST, blk = task & (KBLK - 1);
             if ((i & 31) == 31) cur = look(task + CONV * (1 + lane));
             const int at_next = __shfl_sync(0xffffffffu, cur, (i + 1) & 31);
             const bool big = __any_sync(0xffffffffu, beyond(ks[0]) || beyond(ks[1]) || beyond(vs));
-            if (!warp_wait(k_free(st), ((j / ST) & 1) ^ 1, gone)) break;
+            const int whose = j - ST < nt0 ? ask : nq - 1;
+            if (!warp_wait(k_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
             if (lane == 0) smem[L::there + (j & (INFO - 1)) * KBLK + blk] = at >= 0;
             if (big) keys(std::true_type{}, k_to + st * L::TILE + blk * 2048);
             else keys(std::false_type{}, k_to + st * L::TILE + blk * 2048);
             fence_async();
             __syncwarp();
-            if (lane == 0) arrive(k_full(st));
+            if (j < 2) {
+                if (lane == 0) arrive(k_first(j));
+            } else if (lane < L::NQ) {
+                arrive(ready(lane, (j - 2) % ST));
+            }
             load_keys(at_next, task + CONV);
             if (lane < KV_B) {
                 reinterpret_cast<uint16_t *>(mine)[lane] = (uint16_t)vs;
                 reinterpret_cast<uint16_t *>(mine)[KV_B + lane] = (uint16_t)(vs >> 16);
             }
             __syncwarp();
-            if (!warp_wait(v_free(st), ((j / ST) & 1) ^ 1, gone)) break;
+            if (!warp_wait(v_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
             if (big) values(std::true_type{}, v_to + st * L::TILE + ((blk * 2 ^ g) << 4));
             else values(std::false_type{}, v_to + st * L::TILE + ((blk * 2 ^ g) << 4));
             fence_async();
             __syncwarp();
-            if (lane == 0) arrive(v_full(st));
+            // (the last two tiles' steps wait for no keys: once more in their place)
+            if (lane < L::NQ) {
+                arrive(ready(lane, st));
+                if (j + 2 >= n) arrive(ready(lane, st));
+            }
             load_values(at_next, task + CONV);
             at = at_next;
         }
-    } else if (n > 0) {  // ------------------------------------------------ MMA issuer of a row tile
-        const uint32_t one = elect_one();
+    } else {  // -------------------------------------------------------- MMA issuer of a row tile
+        // (one a row tile: between its products a warp waits, commits and counts for as long as the products take)
         const int q = warp - MMA_WARP, nt = tiles_for(q);
-        bool ok = nt == 0 || warp_wait(q_full(q), 0, gone), issued = false;
+        const uint32_t one = elect_one();
+        bool ok = nt > 0 && warp_wait(q_full(q), 0, gone), issued = false;
         const uint64_t q_op = operand(sm + L::q + q * L::QTILE), k_op = operand(sm + L::k), v_op = operand(sm + L::v);
-        // a stage is free when both row tiles are through with it; a key tile that this one does not go through is waited for all the same
-        const auto skip = [&](uint32_t full, uint32_t parity, uint32_t free) {
-            ok = warp_wait(full, parity, gone);
-            if (ok && lane == 0) arrive(free);
-        };
+        const uint32_t S = tmem + 2 * q * KT, O = tmem + L::O + q * DH;
         const auto qk = [&](int j) {
-            const int st = j & (ST - 1);
-            if (j >= nt) return skip(k_full(st), (j / ST) & 1, k_free(st));
-            if (!(ok = warp_wait(k_full(st), (j / ST) & 1, gone))) return;
-            fence_after();
-            const uint32_t d = tmem + (2 * q + (j & 1)) * KT;
-            const uint64_t ka = k_op + (uint32_t)st * (L::TILE >> 4);
+            const uint32_t d = S + (j & 1) * KT;
+            const uint64_t ka = k_op + (uint32_t)(j % ST) * (L::TILE >> 4);
             mma_ss<false>(d, q_op, ka, idesc(KT), one);
 #pragma unroll
             for (int k = 1; k < DH / 16; ++k)
                 mma_ss<true>(d, q_op + ((k >> 2) * (QT * 128 >> 4) + 2 * (k & 3)), ka + ((k >> 2) * (KT * 128 >> 4) + 2 * (k & 3)),
                              idesc(KT), one);
             issued = true;
-            commit(s_full(q, j & 1), one);
-            commit(k_free(st), one);
+            commit(k_free(q, j % ST), one);
         };
         // the logits of two key tiles ahead
-        for (int j = 0; j < 2 && j < n && ok; ++j) qk(j);
-        for (int j = 0; j < n && ok; ++j) {
-            const int st = j & (ST - 1);
-            if (j < nt) {
-                if (!(ok = warp_wait(v_full(st), (j / ST) & 1, gone))) break;
-                if (!(ok = warp_wait(p_full(q, j & 1), (j >> 1) & 1, gone))) break;
-                fence_after();
-                const uint32_t p = tmem + (2 * q + (j & 1)) * KT, o = tmem + L::O + q * DH;
-                const uint64_t va = v_op + (uint32_t)st * (L::TILE >> 4);
-#pragma unroll
-                for (int k = 0; k < KT / 16; ++k) mma_ts(o, p + 8 * k, va + 2 * k, idesc(DH), k > 0 || j > 0, one);
-                commit(v_free(st), one);
-                commit(o_done(q), one);
-                // a barrier of its own for the last product: the softmax may be up to two
-                // phases of o_done away from it, more than a parity tells apart.  Committed
-                // last, so that nothing arrives after the tile's rows are out
-                if (j == nt - 1) commit(o_last(q), one);
-            } else {
-                skip(v_full(st), (j / ST) & 1, v_free(st));
-                if (!ok) break;
-            }
-            if (j + 2 < n) qk(j + 2);  // over the buffer that P V read, in order behind it
+        for (int j = 0; j < 2 && j < nt && ok; ++j) {
+            if (!(ok = warp_wait(k_first(j), 0, gone))) break;
+            fence_after();
+            qk(j);
+            commit(s_full(q, j), one);
         }
-        if (!ok && issued) {  // what was issued ends before the memory is given up
+#pragma unroll 1
+        for (int j = 0; j < nt && ok; ++j) {
+            if (!(ok = warp_wait(ready(q, j % ST), (j / ST) & 1, gone))) break;
+            fence_after();
+            const uint32_t p = S + (j & 1) * KT;
+            const uint64_t va = v_op + (uint32_t)(j % ST) * (L::TILE >> 4);
+#pragma unroll
+            for (int k = 0; k < KT / 16; ++k) mma_ts(O, p + 8 * k, va + 2 * k, idesc(DH), k > 0 || j > 0, one);
+            commit(v_free(q, j % ST), one);
+            if (j + 2 < nt) qk(j + 2);  // over the buffer that P V read, in order behind it
+            commit(s_full(q, j & 1), one);
+        }
+        if (nt > 0 && !ok && issued) {  // what was issued ends before the memory is given up
             commit(drain(q), one);
             bar_wait(drain(q), 0, KV_WAIT_NS);
         }
