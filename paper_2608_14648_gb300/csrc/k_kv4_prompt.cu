@@ -66,6 +66,33 @@ __device__ __forceinline__ void ld_wait32(uint32_t *v) {
                  : "memory");
 }
 
+// Bounded, cut short when another role gave up, by a whole warp with one answer.  Suspended meanwhile, a millisecond at a
+// time (a loop of short tries took a sixth of the kernel's issue slots)
+__device__ __forceinline__ bool warp_sleep(uint32_t b, uint32_t parity, volatile int32_t *gone) {
+    const auto there = [&](uint32_t ns) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}\n"
+            : "=r"(ok)
+            : "r"(b), "r"(parity), "r"(ns)
+            : "memory");
+        return __all_sync(0xffffffffu, ok);
+    };
+    if (there(1000000)) return true;
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    while (!there(1000000)) {
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+        if (__any_sync(0xffffffffu, *gone || t - t0 > KV_WAIT_NS)) {
+            *gone = 1;
+            return false;
+        }
+    }
+    return true;
+}
+
 __device__ __forceinline__ __half2 h2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
 __device__ __forceinline__ uint32_t u2(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
 // b + s c of the codes in bits 0..3 and 16..19 of a word, or (HIGH) 4..7 and 20..23: 1024 + c (1024 + 16 c) as f16
@@ -84,7 +111,8 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     using L = Lay<DH>;
     constexpr int ST = L::ST, CONV = L::CONV, ROWS = L::ROWS, CONV_WARP0 = L::CONV_WARP0, MMA_WARP = L::MMA_WARP, THREADS = L::THREADS;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // (a warp's number from one lane: the issuing warps' operands then are in uniform registers)
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     uint8_t *smem = smem_raw + ((1024 - (su32(smem_raw) & 1023)) & 1023);  // swizzle atoms
     const uint32_t sm = su32(smem);
     const auto bar = [&](int i) { return sm + L::bars + 8 * i; };
@@ -172,7 +200,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     fence_before();
     __syncthreads();
     fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
 
     if constexpr (L::NQ == 2) {
         if (warp < CONV_WARP0) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFT_REGS));
@@ -197,7 +225,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         const volatile uint32_t *there = reinterpret_cast<const volatile uint32_t *>(smem + L::there);
         for (int j = 0; j < nt; ++j) {
             const uint32_t S = S0 + (j & 1) * KT;
-            if (!(ok = warp_wait(s_full(q, j & 1), (j >> 1) & 1, gone))) break;
+            if (!(ok = warp_sleep(s_full(q, j & 1), (j >> 1) & 1, gone))) break;
             fence_after();
             uint32_t v[KT];
             ld32(S, v);
@@ -267,7 +295,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                 m = to;
                 l *= g;
                 if (j > 0) {
-                    if (!(ok = warp_wait(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1, gone))) break;  // P V of tile j - 1 is through
+                    if (!(ok = warp_sleep(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1, gone))) break;  // P V of tile j - 1 is through
                     fence_after();
 #pragma unroll 1
                     for (int k = 0; k < DH / 16; ++k) {
@@ -295,7 +323,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         }
         if (q < nq) {
             if (ok && nt > 0) {
-                ok = warp_wait(s_full(q, (nt + 1) & 1), ((nt + 1) >> 1) & 1, gone);
+                ok = warp_sleep(s_full(q, (nt + 1) & 1), ((nt + 1) >> 1) & 1, gone);
                 fence_after();
             }
             if (!ok) {
@@ -449,7 +477,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             const int at_next = __shfl_sync(0xffffffffu, cur, (i + 1) & 31);
             const bool big = __any_sync(0xffffffffu, beyond(ks[0]) || beyond(ks[1]) || beyond(vs));
             const int whose = j - ST < nt0 ? ask : nq - 1;
-            if (!warp_wait(k_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
+            if (!warp_sleep(k_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
             if (lane == 0) smem[L::there + (j & (INFO - 1)) * KBLK + blk] = at >= 0;
             if (big) keys(std::true_type{}, k_to + st * L::TILE + blk * 2048);
             else keys(std::false_type{}, k_to + st * L::TILE + blk * 2048);
@@ -466,7 +494,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                 reinterpret_cast<uint16_t *>(mine)[KV_B + lane] = (uint16_t)(vs >> 16);
             }
             __syncwarp();
-            if (!warp_wait(v_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
+            if (!warp_sleep(v_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
             if (big) values(std::true_type{}, v_to + st * L::TILE + ((blk * 2 ^ g) << 4));
             else values(std::false_type{}, v_to + st * L::TILE + ((blk * 2 ^ g) << 4));
             fence_async();
@@ -483,7 +511,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         // (one a row tile: between its products a warp waits, commits and counts for as long as the products take)
         const int q = warp - MMA_WARP, nt = tiles_for(q);
         const uint32_t one = elect_one();
-        bool ok = nt > 0 && warp_wait(q_full(q), 0, gone), issued = false;
+        bool ok = nt > 0 && warp_sleep(q_full(q), 0, gone), issued = false;
         const uint64_t q_op = operand(sm + L::q + q * L::QTILE), k_op = operand(sm + L::k), v_op = operand(sm + L::v);
         const uint32_t S = tmem + 2 * q * KT, O = tmem + L::O + q * DH;
         const auto qk = [&](int j) {
@@ -499,14 +527,14 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         };
         // the logits of two key tiles ahead
         for (int j = 0; j < 2 && j < nt && ok; ++j) {
-            if (!(ok = warp_wait(k_first(j), 0, gone))) break;
+            if (!(ok = warp_sleep(k_first(j), 0, gone))) break;
             fence_after();
             qk(j);
             commit(s_full(q, j), one);
         }
 #pragma unroll 1
         for (int j = 0; j < nt && ok; ++j) {
-            if (!(ok = warp_wait(ready(q, j % ST), (j / ST) & 1, gone))) break;
+            if (!(ok = warp_sleep(ready(q, j % ST), (j / ST) & 1, gone))) break;
             fence_after();
             const uint32_t p = S + (j & 1) * KT;
             const uint64_t va = v_op + (uint32_t)(j % ST) * (L::TILE >> 4);
