@@ -96,14 +96,23 @@ __device__ __forceinline__ bool warp_sleep(uint32_t b, uint32_t parity, volatile
 __device__ __forceinline__ __half2 h2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
 __device__ __forceinline__ uint32_t u2(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
 // b + s c of the codes in bits 0..3 and 16..19 of a word, or (HIGH) 4..7 and 20..23: 1024 + c (1024 + 16 c) as f16
-// bits, made c, exactly, then one rounding.  BIG: no more than f16's largest number
-template <bool HIGH, bool BIG>
-__device__ __forceinline__ uint32_t dequant2(uint32_t w, __half2 s, __half2 b) {
-    const __half2 x = h2((w & (HIGH ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u);
-    const __half2 c = HIGH ? __hfma2(x, h2(0x2c002c00u), h2(0xd400d400u)) : __hsub2(x, h2(0x64006400u));
-    const __half2 v = __hfma2(c, s, b);
-    return u2(BIG ? __hmin2(v, h2(0x7bff7bffu)) : v);
-}
+// bits, made c, exactly, then one rounding.  BIG: no more than f16's largest number.  The constants in registers: as immediates
+// the two of one logical operation make it two (a third of the converters' logical operations)
+struct Dequant {
+    uint32_t up, down, part, less;  // f16 pairs: 1024, -1024, 1/16, -64
+    __device__ __forceinline__ Dequant() {
+        asm volatile("mov.b32 %0, 0x64006400;\n\tmov.b32 %1, 0xe400e400;\n\tmov.b32 %2, 0x2c002c00;\n\tmov.b32 %3, 0xd400d400;"
+                     : "=r"(up), "=r"(down), "=r"(part), "=r"(less));
+    }
+    template <bool HIGH, bool BIG>
+    __device__ __forceinline__ uint32_t two(uint32_t w, __half2 s, __half2 b) const {
+        uint32_t x;
+        asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x) : "r"(w), "n"(HIGH ? 0x00f000f0 : 0x000f000f), "r"(up));  // and, or
+        const __half2 c = HIGH ? __hfma2(h2(x), h2(part), h2(less)) : __hadd2(h2(x), h2(down));
+        const __half2 v = __hfma2(c, s, b);
+        return u2(BIG ? __hmin2(v, h2(0x7bff7bffu)) : v);
+    }
+};
 
 template <int DH>
 __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
@@ -423,6 +432,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             const float2 x = __half22float2(h2(sb));
             return fmaf(15.0f, x.x, x.y) > 65504.0f;
         };
+        const Dequant dq;
         // keys: vector (chunk w, g): tokens g and g + 8, 16 dims each: two 16-byte chunks of an operand row of 64
         // dims.  Values: dims 16 w + g and 16 w + g + 8, 16 tokens each
         const uint32_t k_to = sm + L::k + g * 128 + (((w0 & 3) * 2 ^ g) << 4);
@@ -439,8 +449,8 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     uint32_t x[8];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        x[2 * i] = dequant2<false, BIG>(c[i] >> 8 * t, s, b);
-                        x[2 * i + 1] = dequant2<true, BIG>(c[i] >> 8 * t, s, b);
+                        x[2 * i] = dq.two<false, BIG>(c[i] >> 8 * t, s, b);
+                        x[2 * i + 1] = dq.two<true, BIG>(c[i] >> 8 * t, s, b);
                     }
                     st_shared(to + k * (KT * 128) + t * 1024, x[0], x[1], x[2], x[3]);
                     st_shared((to + k * (KT * 128) + t * 1024) ^ 16, x[4], x[5], x[6], x[7]);
@@ -462,7 +472,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                         uint32_t x[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            x[i] = half ? dequant2<true, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i])) : dequant2<false, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i]));
+                            x[i] = half ? dq.two<true, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i])) : dq.two<false, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i]));
                         st_shared((to + k * 8192 + t * 1024) ^ (16 * half), x[0], x[1], x[2], x[3]);
                     }
                 }
