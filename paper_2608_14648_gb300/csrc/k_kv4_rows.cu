@@ -69,6 +69,11 @@ struct Fp32Rows4 {
         __syncwarp();
     }
 
+    __device__ __forceinline__ void item(const KvAttnArgs &a, const uint8_t *rec, int pair, bool mask, uint32_t have, int lane) {
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i)
+            if (have >> i & 1) block(a, rec + i * kv4_bytes(a.d), 2 * pair + i, mask, lane);
+    }
     __device__ __forceinline__ void block(const KvAttnArgs &a, const uint8_t *rec, int blk, bool mask, int lane) {
         const int t = lane & 15, half = lane >> 4, nc = a.d / KV_B;
         const uint8_t *K = rec, *V = rec + 8 * a.d;
@@ -284,76 +289,101 @@ struct MmaRows4 {
         __syncwarp();
     }
 
-    __device__ __forceinline__ void block(const KvAttnArgs &a, const uint8_t *rec, int blk, bool mask, int lane) {
-        const int g = lane >> 2, c = lane & 3, nc = FULL ? DC : a.d / KV_B;
-        TokenScales s0 = token_scales(rec, a.d, g), s1 = token_scales(rec, a.d, g + 8);
-        s0.ks *= CODES_UP, s1.ks *= CODES_UP;
-        float x[NT][4];
+    // Two blocks at once where the rows are one tile: twice the independent products and half the tests of the
+    // reference (decode batch below: 138 us with one at a time)
+    __device__ __forceinline__ void item(const KvAttnArgs &a, const uint8_t *rec, int pair, bool mask, uint32_t have, int lane) {
+        if (NT == 1 && have == 3) {
+            blocks<2>(a, rec, 2 * pair, mask, lane);
+            return;
+        }
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i)
+            if (have >> i & 1) blocks<1>(a, rec + i * kv4_bytes(a.d), 2 * pair + i, mask, lane);
+    }
+    template <int NB>
+    __device__ __forceinline__ void blocks(const KvAttnArgs &a, const uint8_t *rec, int blk, bool mask, int lane) {
+        const int g = lane >> 2, c = lane & 3, nc = FULL ? DC : a.d / KV_B, bytes = kv4_bytes(FULL ? 16 * DC : a.d);
+        float x[NB][NT][4];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[t][i] = 0.0f;
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[n][t][i] = 0.0f;
         const uint32_t ka = su32(rec) + lane * 16, va = ka + 8 * a.d;
 #pragma unroll
         for (int w0 = 0; w0 < DC; w0 += 4) {
             if (w0 >= nc) break;
-            uint32_t r[4], f[4];
-            ldsm4(ka + w0 * 128, r);  // (of the last chunks what lies behind them is not used)
+            uint32_t r[NB][4], f[4];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) ldsm4(ka + n * bytes + w0 * 128, r[n]);  // (of the last chunks what lies behind them is not used)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int w = w0 + i;
                 if (w >= DC || w >= nc) break;
-                codes4_a(r[i], f);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    if constexpr (QMEM) {
-                        const uint2 b = qmem[(t * DC + w) * 32 + lane];
-                        mma16816(x[t], f, b.x, b.y);
-                    } else {
-                        mma16816(x[t], f, q[t][w][0], q[t][w][1]);
+                for (int n = 0; n < NB; ++n) {
+                    codes4_a(r[n][i], f);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        if constexpr (QMEM) {
+                            const uint2 b = qmem[(t * DC + w) * 32 + lane];
+                            mma16816(x[n][t], f, b.x, b.y);
+                        } else {
+                            mma16816(x[n][t], f, q[t][w][0], q[t][w][1]);
+                        }
                     }
                 }
             }
         }
-        // log2 and reciprocal of the value scales, biases over scales
-        const float v0 = fmaxf(s0.vs, SCALE_LEAST), v1 = fmaxf(s1.vs, SCALE_LEAST);
-        float lv0, lv1, iv0, iv1;
-        asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lv0) : "f"(v0));
-        asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lv1) : "f"(v1));
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(iv0) : "f"(v0));
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(iv1) : "f"(v1));
-        float bv0 = s0.vb * iv0, bv1 = s1.vb * iv1;
+        // log2 and reciprocal of the value scales, biases over scales, of tokens g and g + 8
+        float iv[NB][2], bv[NB][2];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                x[t][i] = fmaf(x[t][i], fac[t][i] * s0.ks, fmaf(qs[t][i], s0.kb, lv0));
-                x[t][i + 2] = fmaf(x[t][i + 2], fac[t][i] * s1.ks, fmaf(qs[t][i], s1.kb, lv1));
+            for (int k = 0; k < 2; ++k) {
+                const TokenScales sc = token_scales(rec + n * bytes, a.d, g + 8 * k);
+                const float ks = sc.ks * CODES_UP, v = fmaxf(sc.vs, SCALE_LEAST);
+                float lv;
+                asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lv) : "f"(v));
+                asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(iv[n][k]) : "f"(v));
+                bv[n][k] = sc.vb * iv[n][k];
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        x[n][t][2 * k + i] = fmaf(x[n][t][2 * k + i], fac[t][i] * ks, fmaf(qs[t][i], sc.kb, lv));
             }
         if (mask) {
-            bool seen[2] = {false, false};
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int n = 0; n < NB; ++n) {
+                bool seen[2] = {false, false};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int j = blk * KV_B + g + 8 * (i >> 1);
-                    const int2 see = lim[8 * t + 2 * c + (i & 1)];
-                    if (j > see.x || j < see.y) x[t][i] = -INFINITY;
-                    else seen[i >> 1] = true;
-                }
-            // a token that none of the lane's rows sees has no weight, but may never have been written
-            if (!seen[0]) iv0 = bv0 = 0.0f;
-            if (!seen[1]) iv1 = bv1 = 0.0f;
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = (blk + n) * KV_B + g + 8 * (i >> 1);
+                        const int2 see = lim[8 * t + 2 * c + (i & 1)];
+                        if (j > see.x || j < see.y) x[n][t][i] = -INFINITY;
+                        else seen[i >> 1] = true;
+                    }
+                // a token that none of the lane's rows sees has no weight, but may never have been written
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (!seen[k]) iv[n][k] = bv[n][k] = 0.0f;
+            }
         }
-        float p[NT][4];
+        float p[NB][NT][4];
         const auto weigh = [&] {  // weights, and the largest sum of two
             float most = 0.0f;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[t][i] = ex2(x[t][i] - m[t][i & 1]);
-                most = fmaxf(most, fmaxf(p[t][0] + p[t][2], p[t][1] + p[t][3]));
-            }
+                for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[n][t][i] = ex2(x[n][t][i] - m[t][i & 1]);
+                    most = fmaxf(most, fmaxf(p[n][t][0] + p[n][t][2], p[n][t][1] + p[n][t][3]));
+                }
             return most;
         };
         if (__any_sync(0xffffffffu, weigh() > M_MOST)) {
@@ -361,7 +391,9 @@ struct MmaRows4 {
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float top = fmaxf(x[t][i], x[t][i + 2]);
+                    float top = fmaxf(x[0][t][i], x[0][t][i + 2]);
+#pragma unroll
+                    for (int n = 1; n < NB; ++n) top = fmaxf(top, fmaxf(x[n][t][i], x[n][t][i + 2]));
 #pragma unroll
                     for (int b = 4; b < 32; b <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, b));
                     const float to = top > m[t][i] + M_BELOW ? top - M_BELOW : m[t][i];
@@ -374,31 +406,36 @@ struct MmaRows4 {
                 }
             weigh();
         }
-        uint32_t pb[NT][2];
+        uint32_t pb[NB][NT][2];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                l[t][i] = fmaf(p[t][i + 2], iv1, fmaf(p[t][i], iv0, l[t][i]));
-                ob[t][i] = fmaf(p[t][i + 2], bv1, fmaf(p[t][i], bv0, ob[t][i]));
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    l[t][i] = fmaf(p[n][t][i + 2], iv[n][1], fmaf(p[n][t][i], iv[n][0], l[t][i]));
+                    ob[t][i] = fmaf(p[n][t][i + 2], bv[n][1], fmaf(p[n][t][i], bv[n][0], ob[t][i]));
+                }
+                const __half2 lo = __floats2half2_rn(p[n][t][0], p[n][t][1]), hi = __floats2half2_rn(p[n][t][2] * 0.0625f, p[n][t][3] * 0.0625f);
+                pb[n][t][0] = transpose8x8(*reinterpret_cast<const uint32_t *>(&lo));
+                pb[n][t][1] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hi));
             }
-            const __half2 lo = __floats2half2_rn(p[t][0], p[t][1]), hi = __floats2half2_rn(p[t][2] * 0.0625f, p[t][3] * 0.0625f);
-            pb[t][0] = transpose8x8(*reinterpret_cast<const uint32_t *>(&lo));
-            pb[t][1] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hi));
-        }
 #pragma unroll
         for (int w0 = 0; w0 < DC; w0 += 4) {
             if (w0 >= nc) break;
-            uint32_t r[4], f[4];
-            ldsm4(va + w0 * 128, r);
+            uint32_t r[NB][4], f[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int w = w0 + i;
-                if (w >= DC || w >= nc) break;
-                codes4_a(r[i], f);
+            for (int n = 0; n < NB; ++n) ldsm4(va + n * bytes + w0 * 128, r[n]);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mma16816(o[t][w], f, pb[t][0], pb[t][1]);
-            }
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int w = w0 + i;
+                    if (w >= DC || w >= nc) break;
+                    codes4_a(r[n][i], f);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) mma16816(o[t][w], f, pb[n][t][0], pb[n][t][1]);
+                }
         }
     }
 

@@ -50,18 +50,19 @@ __device__ __forceinline__ void bulk_g2s(uint32_t dst, const void *src, uint32_t
 
 // ---- a sequence as this launch sees it
 struct Seq {
-    int lo, cnt;  // first block that a row sees, blocks
+    int lo, cnt;  // first block (of T tokens) that a row sees, blocks
     int len, n;   // tokens held, rows
     int row0;     // its first row in the token tensors
 };
+template <int T = KV_B>
 __device__ __forceinline__ Seq seq_of(const KvAttnArgs &a, int b) {
     Seq s;
     s.len = kv_clamp(a.pos[b], 0, a.cols * a.page);
     const int2 rows = kv_rows_of(a.cu, b, a.tokens, a.max_tokens);
     s.row0 = rows.x;
     s.n = rows.y;
-    s.lo = a.window > 0 ? max(0, s.len - s.n - a.window + 1) / KV_B : 0;
-    s.cnt = s.n > 0 ? (s.len + KV_B - 1) / KV_B - s.lo : 0;
+    s.lo = a.window > 0 ? max(0, s.len - s.n - a.window + 1) / T : 0;
+    s.cnt = s.n > 0 ? (s.len + T - 1) / T - s.lo : 0;
     if (s.cnt < 0) s.cnt = 0;
     return s;
 }

@@ -33,29 +33,37 @@ __host__ __device__ __forceinline__ int64_t active_ctas(int64_t W, int nw, int64
     return c < 1 ? 1 : (c > grid ? grid : c);
 }
 
-// A block in a warp's ring: its keys and values (8-bit: their scales come with the window
-// below; 4-bit: the block's record, scales and biases included)
+// An item is a block of 16 tokens; of the 4-bit cache, whose blocks are half as large, two blocks: its tokens,
+// and its bytes in a warp's ring (8-bit: the scales come with the window below; 4-bit: two records, scales and
+// biases included)
+template <class Rows>
+constexpr int TOKENS = Rows::FOUR ? 2 * KV_B : KV_B;
 template <class Rows>
 __host__ __device__ __forceinline__ constexpr int ring_bytes(int d) {
-    return Rows::FOUR ? kv4_bytes(d) : 2 * KV_B * d;
+    return Rows::FOUR ? 2 * kv4_bytes(d) : 2 * KV_B * d;
 }
 
 // 32 items, one a lane.  Three steps, so that the two dependent loads behind
 // an item (its page, then the block's scales) are waited for long after they
 // were issued: where the item is, its block, its scales to shared memory.
+template <bool FOUR>
 struct Window {
     int pg, at;  // page; block of the pool, -1: nothing to do
     int blk, seq, unit;
-    float2 sc;
+    float2 sc;           // (8-bit)
+    int pg2, at2;        // (4-bit) of the item's second block
     uint32_t todo, starts;  // (all lanes the same) items with work, items that begin a unit
+    uint32_t have, have2;   // (4-bit) items whose first, second block there is
     int n;
 };
 
-template <int RT>
+template <class Rows>
 __device__ __forceinline__ void window_pages(const KvAttnArgs &a, const Line &ln, int64_t base, int64_t end, int lane,
-                                             Window &w) {
+                                             Window<Rows::FOUR> &w) {
+    constexpr int RT = Rows::RT, T = TOKENS<Rows>;
     w.n = end - base > 32 ? 32 : (int)(end > base ? end - base : 0);
     w.pg = -1;
+    if constexpr (Rows::FOUR) w.pg2 = -1;
     w.blk = w.seq = w.unit = 0;
     bool starts = false;
     if (lane < w.n) {
@@ -76,22 +84,48 @@ __device__ __forceinline__ void window_pages(const KvAttnArgs &a, const Line &ln
         w.unit = (int)u;
         w.blk = s.lo + (int)k;
         const int r0 = a.by_heads.div((int)u) * RT, r1 = min(r0 + RT, s.n * a.group) - 1;
-        if (w.blk * KV_B <= last_of(a, s, r1) && w.blk * KV_B + KV_B > first_of(a, s, r0))
-            w.pg = a.table[(int64_t)(ln.b0 + b) * a.cols + a.by_bpp.div(w.blk)];
+        const int first = first_of(a, s, r0), last = last_of(a, s, r1);
+        const auto page = [&](int blk) {
+            if (blk * KV_B > last || blk * KV_B + KV_B <= first) return -1;
+            return a.table[(int64_t)(ln.b0 + b) * a.cols + a.by_bpp.div(blk)];
+        };
+        w.pg = page(w.blk * (T / KV_B));
+        if constexpr (Rows::FOUR) w.pg2 = page(w.blk * 2 + 1);
     }
     w.starts = __ballot_sync(0xffffffffu, starts);
     w.todo = 0;
 }
 template <bool FOUR>
-__device__ __forceinline__ void window_blocks(const KvAttnArgs &a, Window &w) {
-    const bool there = w.pg >= 0 && w.pg < a.pages;
-    w.at = there ? (w.pg * a.heads + a.by_heads.mod(w.unit)) * a.bpp + a.by_bpp.mod(w.blk) : -1;
-    if constexpr (!FOUR) w.sc = there ? a.scales[w.at] : make_float2(0.0f, 0.0f);
-    w.todo = __ballot_sync(0xffffffffu, there);
+__device__ __forceinline__ void window_blocks(const KvAttnArgs &a, Window<FOUR> &w) {
+    const auto block = [&](int pg, int blk) {
+        return pg >= 0 && pg < a.pages ? (pg * a.heads + a.by_heads.mod(w.unit)) * a.bpp + a.by_bpp.mod(blk) : -1;
+    };
+    w.at = block(w.pg, FOUR ? 2 * w.blk : w.blk);
+    if constexpr (FOUR) {
+        w.at2 = block(w.pg2, 2 * w.blk + 1);
+        w.have = __ballot_sync(0xffffffffu, w.at >= 0);
+        w.have2 = __ballot_sync(0xffffffffu, w.at2 >= 0);
+        w.todo = w.have | w.have2;
+    } else {
+        w.sc = w.at >= 0 ? a.scales[w.at] : make_float2(0.0f, 0.0f);
+        w.todo = __ballot_sync(0xffffffffu, w.at >= 0);
+    }
 }
-__device__ __forceinline__ void window_scales(const Window &w, float4 *mem, int lane) {
+__device__ __forceinline__ void window_scales(const Window<false> &w, float4 *mem, int lane) {
     mem[lane] = value_scale(w.sc);
     __syncwarp();
+}
+
+// The wait of a whole warp, without branches of single lanes
+__device__ __forceinline__ bool warp_bar_wait(uint32_t b, uint32_t parity, unsigned long long limit) {
+    if (__all_sync(0xffffffffu, bar_try(b, parity))) return true;
+    unsigned long long t0, t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    while (!__all_sync(0xffffffffu, bar_try(b, parity))) {
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+        if (__any_sync(0xffffffffu, t - t0 > limit)) return false;
+    }
+    return true;
 }
 
 // dims 4 c .. 4 c + 3 of an output row
@@ -271,15 +305,15 @@ __device__ __forceinline__ int64_t scan_add(int64_t x, int lane) {  // inclusive
 
 // cum and seq of the launch's sequences (one sequence with `whole`); ends with
 // a barrier
-template <int RT>
+template <class Rows>
 __device__ void line_up(const KvAttnArgs &a, int b0, int nb, int64_t *cum, Seq *seq) {
     __shared__ int64_t warp_sum[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = blockDim.x >> 5;
     const auto items = [&](int i) {
         if (i >= nb) return int64_t(0);
-        const Seq s = seq_of(a, b0 + i);
+        const Seq s = seq_of<TOKENS<Rows>>(a, b0 + i);
         seq[i] = s;
-        return (int64_t)s.cnt * tiles_of(a, s, RT) * a.heads;
+        return (int64_t)s.cnt * tiles_of(a, s, Rows::RT) * a.heads;
     };
     if (nb <= 32) {
         if (warp == 0) {
@@ -371,7 +405,7 @@ __device__ __noinline__ void give_up(const KvAttnArgs &a, Line line, int64_t c0,
 
 template <class Rows, int NW>
 __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_constant__ KvAttnArgs a, int ns) {
-    constexpr int RT = Rows::RT;
+    constexpr int RT = Rows::RT, T = TOKENS<Rows>;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ int gave_up;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -402,7 +436,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (lane < 2) rec[2 * warp + lane].unit = -1;
     if (tid == 0) gave_up = 0;
-    line_up<RT>(a, b0, nb, cum, seq);
+    line_up<Rows>(a, b0, nb, cum, seq);
     const Line line{cum, seq, b0, nb};
     const int64_t W = cum[nb];
     int64_t c0, c1;  // this CTA's items
@@ -436,21 +470,29 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
     if (i1 > i0) {
         float4 *win = reinterpret_cast<float4 *>(smem + sm.win) + 64 * warp;
         int side = 0;  // half of win that holds cur's scales
-        Window cur, next;
-        window_pages<RT>(a, line, i0, i1, lane, cur);
-        window_blocks<Rows::FOUR>(a, cur);
+        Window<Rows::FOUR> cur, next;
+        window_pages<Rows>(a, line, i0, i1, lane, cur);
+        window_blocks(a, cur);
         int64_t base = i0;
         uint32_t to_issue = cur.todo, flying = 0;
         bool ahead = false, known = false;  // to_issue belongs to `next`; next's blocks are known
         int put_at = 0, take_at = 0;
         uint32_t phase = 0;  // parity of the stage taken next
-        const auto issue = [&](int at) {
+        const auto issue = [&](int at, int at2) {
             if (lane == 0) {
                 const uint32_t b = bars + 8 * put_at, dst = ring_u + put_at * bytes;
-                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(bytes) : "memory");
                 if constexpr (Rows::FOUR) {
-                    bulk_g2s(dst, a.k + (int64_t)at * bytes, bytes, b);
+                    const int rec = bytes / 2;
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(at >= 0 && at2 >= 0 ? bytes : rec)
+                                 : "memory");
+                    if (at >= 0 && at2 == at + 1) {
+                        bulk_g2s(dst, a.k + (int64_t)at * rec, bytes, b);
+                    } else {
+                        if (at >= 0) bulk_g2s(dst, a.k + (int64_t)at * rec, rec, b);
+                        if (at2 >= 0) bulk_g2s(dst + rec, a.k + (int64_t)at2 * rec, rec, b);
+                    }
                 } else {
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(bytes) : "memory");
                     bulk_g2s(dst, a.k + (int64_t)at * half, half, b);
                     bulk_g2s(dst + half, a.v + (int64_t)at * half, half, b);
                 }
@@ -461,7 +503,9 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
         while (to_issue && flying < (uint32_t)ns) {  // the first copies go out before the next window is known
             const int i = __ffs(to_issue) - 1;
             to_issue &= to_issue - 1;
-            issue(__shfl_sync(0xffffffffu, cur.at, i));
+            const int at = __shfl_sync(0xffffffffu, cur.at, i);
+            if constexpr (Rows::FOUR) issue(at, __shfl_sync(0xffffffffu, cur.at2, i));
+            else issue(at, -1);
         }
         const auto fill_ring = [&] {
             while (flying < (uint32_t)ns) {
@@ -473,10 +517,12 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
                 }
                 const int i = __ffs(to_issue) - 1;
                 to_issue &= to_issue - 1;
-                issue(__shfl_sync(0xffffffffu, ahead ? next.at : cur.at, i));
+                const int at = __shfl_sync(0xffffffffu, ahead ? next.at : cur.at, i);
+                if constexpr (Rows::FOUR) issue(at, __shfl_sync(0xffffffffu, ahead ? next.at2 : cur.at2, i));
+                else issue(at, -1);
             }
         };
-        window_pages<RT>(a, line, base + 32, i1, lane, next);
+        window_pages<Rows>(a, line, base + 32, i1, lane, next);
         if constexpr (!Rows::FOUR) window_scales(cur, win, lane);
         const auto leave = [&](bool last) {  // the open unit ends here, for this warp
             const Seq s = seq[useq];
@@ -496,7 +542,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
             // next: its blocks a few items into this window, its scales some later
             for (int i = 0; i < cur.n; ++i) {
                 if (i == 8) {
-                    window_blocks<Rows::FOUR>(a, next);
+                    window_blocks(a, next);
                     known = true;
                     fill_ring();
                 }
@@ -518,13 +564,12 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
                 const int blk = ublk + i;
                 float4 sc;
                 if constexpr (!Rows::FOUR) sc = win[32 * side + i];
-                if (!__all_sync(0xffffffffu, bar_wait(bars + 8 * take_at, phase, a.wait_ns))) {
-                    ok = false;
-                    break;
-                }
+                if constexpr (Rows::FOUR) ok = warp_bar_wait(bars + 8 * take_at, phase, a.wait_ns);
+                else ok = __all_sync(0xffffffffu, bar_wait(bars + 8 * take_at, phase, a.wait_ns));
+                if (!ok) break;
                 const uint8_t *K = ring + take_at * bytes;
-                const bool mask = blk * KV_B < safe_first || blk * KV_B + KV_B - 1 > safe_last;
-                if constexpr (Rows::FOUR) rows.block(a, K, blk, mask, lane);
+                const bool mask = blk * T < safe_first || blk * T + T - 1 > safe_last;
+                if constexpr (Rows::FOUR) rows.item(a, K, blk, mask, (cur.have >> i & 1) | (cur.have2 >> i & 1) << 1, lane);
                 else rows.block(a, K, K + half, blk, sc.x, sc.y, sc.z, mask, lane);
                 __syncwarp();
                 if (++take_at == ns) take_at = 0, phase ^= 1u;
@@ -539,7 +584,7 @@ __global__ void __launch_bounds__(NW * 32, 1) kv_rows_kernel(const __grid_consta
             if (ahead) ahead = false;
             else to_issue = cur.todo;
             known = false;
-            window_pages<RT>(a, line, base + 32, i1, lane, next);
+            window_pages<Rows>(a, line, base + 32, i1, lane, next);
             fill_ring();
         }
         if (!ok) {  // a copy did not arrive: let the others land before the memory is given up
