@@ -213,7 +213,7 @@ struct MmaRows4 {
     static constexpr int RT = 8 * NT;
     static constexpr int D4 = DC > 8 ? 2 : 1;
     static constexpr bool ONE_D = FULL, FOUR = true;
-    static constexpr bool QMEM = NT * DC >= 32;  // the queries' operands wait in shared memory
+    static constexpr bool QMEM = NT * DC >= 8;  // the queries' operands wait in shared memory (decode batch 118 us, in registers 129)
     static constexpr size_t __host__ __device__ scratch(int) { return (QMEM ? (size_t)NT * DC * 2 * 32 * 4 : 0) + LIMITS<RT>; }
     float o[NT][DC][4], m[NT][2], l[NT][2], ob[NT][2], fac[NT][2], qs[NT][2];
     uint32_t q[QMEM ? 1 : NT][QMEM ? 1 : DC][2];
