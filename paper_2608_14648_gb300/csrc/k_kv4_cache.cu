@@ -75,21 +75,6 @@ __device__ __forceinline__ Range range8(const uint32_t *w) {
 }
 __device__ __forceinline__ bool ordinary(Range r) { return r.lo >= -F16_MOST && r.hi <= F16_MOST; }
 
-// Vectors that are not: the range of their finite elements, clipped to f16's
-template <typename T>
-__device__ __noinline__ float2 finite8(const uint32_t *w, float2 r) {
-    for (int i = 0; i < 4; ++i) {
-        const float2 p = value2<T>(w, i);
-        if (fabsf(p.x) < INFINITY) r.x = fminf(r.x, p.x), r.y = fmaxf(r.y, p.x);
-        if (fabsf(p.y) < INFINITY) r.x = fminf(r.x, p.y), r.y = fmaxf(r.y, p.y);
-    }
-    return r;
-}
-__device__ __forceinline__ Range clipped(float2 r) {
-    if (r.x > r.y) return Range{0.0f, 0.0f};  // no finite element
-    return Range{fminf(fmaxf(r.x, -F16_MOST), F16_MOST), fminf(fmaxf(r.y, -F16_MOST), F16_MOST)};
-}
-
 struct Lvq {
     float b, s, inv;
 };
@@ -114,44 +99,37 @@ __device__ __forceinline__ uint32_t held(const Lvq &v) {  // (scale, bias)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// the code of a value that fp32 leaves open, near the middle of two
-__device__ __noinline__ float code_near(float x, float b, float s) {
-    const float k = floorf((x - b) / s);
-    const double over = (double)x - (double)b, mid = ((double)k + 0.5) * (double)s;
+// the code of a value within its vector's range, in 64 bits where fp32 leaves it open
+__device__ __forceinline__ float code_of(float x, const Lvq &v) {
+    const float q = (x - v.b) * v.inv, c = rintf(q);
+    if (fabsf(q - c) <= NEAR) return c;
+    const float k = floorf(q);  // near k + 1/2
+    const double over = (double)x - (double)v.b, mid = ((double)k + 0.5) * (double)v.s;
     return over > mid || (over == mid && ((int)k & 1)) ? k + 1.0f : k;
 }
-// codes of 8 values as floats
+// codes of two values as floats; far: the largest distance of a quotient from its code
 template <typename T>
-__device__ __forceinline__ void codes8(const uint32_t *w, const Lvq &v, float2 *c) {
-    float far = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 q = mul2(add2(value2<T>(w, i), make_float2(-v.b, -v.b)), make_float2(v.inv, v.inv));
-        c[i] = add2(add2(q, make_float2(MAGIC, MAGIC)), make_float2(-MAGIC, -MAGIC));
-        far = fmaxf(far, fmaxf(fabsf(q.x - c[i].x), fabsf(q.y - c[i].y)));
-    }
-    if (far > NEAR) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 x = value2<T>(w, i);
-            if (fabsf((x.x - v.b) * v.inv - c[i].x) > NEAR) c[i].x = code_near(x.x, v.b, v.s);
-            if (fabsf((x.y - v.b) * v.inv - c[i].y) > NEAR) c[i].y = code_near(x.y, v.b, v.s);
-        }
-    }
+__device__ __forceinline__ float2 codes2(const uint32_t *w, int i, const Lvq &v, float &far) {
+    const float2 q = mul2(add2(value2<T>(w, i), make_float2(-v.b, -v.b)), make_float2(v.inv, v.inv));
+    const float2 c = add2(add2(q, make_float2(MAGIC, MAGIC)), make_float2(-MAGIC, -MAGIC));
+    far = fmaxf(far, fmaxf(fabsf(q.x - c.x), fabsf(q.y - c.y)));
+    return c;
 }
-// ... of a vector that is not ordinary: its elements taken into its range, NaN to the smallest
+// the same where some are near the middle of two: one code in a nibble each (by value and not inlined: what is rare
+// costs the ordinary path no registers)
 template <typename T>
-__device__ __noinline__ void codes8_clipped(const uint32_t *w, Lvq v, float lo, float hi, float2 *c) {
+struct Eight {
+    uint32_t w[WORDS8<T>];
+};
+template <typename T>
+__device__ __noinline__ uint32_t codes8_near(Eight<T> x, float b, float s, float inv) {
+    const Lvq v{b, s, inv};
+    uint32_t c = 0;
     for (int i = 0; i < 4; ++i) {
-        const float2 p = value2<T>(w, i);
-        float x[2] = {p.x, p.y};
-        for (int k = 0; k < 2; ++k) {
-            x[k] = x[k] == x[k] ? fminf(fmaxf(x[k], lo), hi) : lo;
-            const float q = (x[k] - v.b) * v.inv, r = rintf(q);
-            x[k] = fabsf(q - r) > NEAR ? code_near(x[k], v.b, v.s) : r;
-        }
-        c[i] = make_float2(x[0], x[1]);
+        const float2 p = value2<T>(x.w, i);
+        c |= (uint32_t)code_of(p.x, v) << (8 * i) | (uint32_t)code_of(p.y, v) << (8 * i + 4);
     }
+    return c;
 }
 
 __device__ __forceinline__ float2 pack2(float2 a, float2 b, float up) { return fma2(b, make_float2(up, up), a); }
@@ -161,9 +139,56 @@ __device__ __forceinline__ uint32_t word_of(float lo, float hi) {
 }
 __device__ __forceinline__ uint32_t merged(uint32_t was, uint32_t now, uint32_t mask) { return (was & ~mask) | (now & mask); }
 
+// A block's new tokens one after the other, whatever they hold, by the definition: for blocks with infinities, NaN,
+// values beyond f16 (left out, or clipped, of a vector's range and taken into it: NaN to its smallest), and for
+// rows that no wide load may read.
+template <typename T>
+__device__ __noinline__ void block_slowly(const T *x, int64_t step, int d, int tensor, int lo, int hi, uint8_t *rec, int lane) {
+    for (int t = lo; t < hi; ++t) {
+        const T *row = x + t * step;
+        const auto at = [&](int dim) {
+            if constexpr (std::is_same<T, float>::value) return row[dim];
+            else if constexpr (std::is_same<T, __half>::value) return __half2float(row[dim]);
+            else return __bfloat162float(row[dim]);
+        };
+        float least = INFINITY, most = -INFINITY;
+        for (int i = lane; i < d; i += 32) {
+            const float y = at(i);
+            if (fabsf(y) < INFINITY) least = fminf(least, y), most = fmaxf(most, y);
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        }
+        Range r{0.0f, 0.0f};  // without a finite element
+        if (least <= most) r = Range{fminf(fmaxf(least, -F16_MOST), F16_MOST), fminf(fmaxf(most, -F16_MOST), F16_MOST)};
+        const Lvq v = lvq_of(r);
+        const auto code = [&](int dim) -> uint32_t {
+            float y = at(dim);
+            y = y == y ? fminf(fmaxf(y, r.lo), r.hi) : r.lo;
+            return (uint32_t)code_of(y, v);
+        };
+        if (tensor == 0) {
+            for (int i = lane; i < d / 2; i += 32) {  // a byte: two dims of the token
+                const int w = i >> 3, c = (i >> 1) & 3, l = i & 1, dim = 16 * w + 4 * c + l;
+                rec[128 * w + 16 * (t & 7) + 4 * c + 2 * l + (t >> 3)] = (uint8_t)(code(dim) | code(dim + 2) << 4);
+            }
+        } else {
+            for (int dim = lane; dim < d; dim += 32) {  // half a byte
+                uint8_t *p = rec + 8 * d + 128 * (dim >> 4) + 16 * (dim & 7) + 4 * ((t & 7) >> 1) + 2 * (t & 1) + ((dim >> 3) & 1);
+                const int up = 4 * (t >> 3);
+                *p = (uint8_t)((*p & ~(15u << up)) | code(dim) << up);
+            }
+        }
+        if (lane == 0) *reinterpret_cast<uint32_t *>(rec + KV_B * d + 8 * t + 4 * tensor) = held(v);
+    }
+}
+
 // Warps: one a (sequence, block its new rows reach, head, tensor).  D: dims at most
 template <typename T, int D>
-__global__ void __launch_bounds__(WARPS * 32) kv4_write_kernel(const __grid_constant__ KvCacheArgs a) {
+__global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 4 : sizeof(T) * D <= 512 ? 2 : 1)
+    kv4_write_kernel(const __grid_constant__ KvCacheArgs a) {
     constexpr int W = WORDS8<T>;
     const int lane = threadIdx.x & 31;
     const int warp = blockIdx.x * WARPS + (threadIdx.x >> 5), tensor = warp & 1;
@@ -183,8 +208,22 @@ __global__ void __launch_bounds__(WARPS * 32) kv4_write_kernel(const __grid_cons
     const T *x = static_cast<const T *>(src.x) + (int64_t)(rows.x - start + t0) * src.token + (int64_t)h * src.head;
     const int lo = max(start - t0, 0), hi = min(end - t0, KV_B);  // the block's new tokens
     const bool there = pg >= 0 && pg < a.pages;
-    uint8_t *rec = a.k + (((int64_t)pg * a.heads + h) * a.bpp + a.by_bpp.mod(blk)) * kv4_bytes(a.d);
-
+    uint8_t *rec = a.k + (((int64_t)(there ? pg : 0) * a.heads + h) * a.bpp + a.by_bpp.mod(blk)) * kv4_bytes(a.d);
+    // 8 values of a token, zeros if it is not new; where wide loads are not possible all blocks go the slow way
+    const auto get = [&](int t, int dim, uint32_t *w) {
+        const uint4 *p = reinterpret_cast<const uint4 *>(x + (int64_t)t * src.token + dim);
+        const bool in = t >= lo && t < hi;
+#pragma unroll
+        for (int i = 0; i < W; i += 4) {
+            const uint4 v = in ? __ldg(p + i / 4) : make_uint4(0, 0, 0, 0);
+            w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+        }
+    };
+    if (!src.wide) {
+        if (there) block_slowly(x, src.token, a.d, tensor, lo, hi, rec, lane);
+        return;
+    }
+    bool fine = true;
     if (tensor == 0) {
         constexpr int NP = D / 32;
         const int g = lane >> 2, c = lane & 3;
@@ -194,67 +233,65 @@ __global__ void __launch_bounds__(WARPS * 32) kv4_write_kernel(const __grid_cons
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 // (dims past the last: the first ones once more, which does not change the range)
-                const int t = g + 8 * k, dim = 32 * p + 8 * c, from = dim < a.d ? dim : 8 * (c & 1);
-#pragma unroll
-                for (int i = 0; i < W; ++i) raw[p][k][i] = 0;
-                if (t >= lo && t < hi) load8(x + (int64_t)t * src.token + from, src.wide, raw[p][k]);
+                const int dim = 32 * p + 8 * c;
+                get(g + 8 * k, dim < a.d ? dim : 8 * (c & 1), raw[p][k]);
             }
         if (!there) return;
         Lvq v[2];
-        Range r[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            r[k] = range8<T>(raw[0][k]);
+            Range r = range8<T>(raw[0][k]);
 #pragma unroll
-            for (int p = 1; p < NP; ++p) r[k] = both(r[k], range8<T>(raw[p][k]));
-            r[k] = across(across(r[k], 1), 2);
+            for (int p = 1; p < NP; ++p) r = both(r, range8<T>(raw[p][k]));
+            r = across(across(r, 1), 2);
+            fine = fine && ordinary(r);
+            v[k] = lvq_of(r);
         }
-        const bool clip = !__all_sync(0xffffffffu, ordinary(r[0]) && ordinary(r[1]));
-        if (clip) {
+        if (__all_sync(0xffffffffu, fine)) {
+            uint32_t fresh = 0;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                float2 f = make_float2(INFINITY, -INFINITY);
+                const int t = g + 8 * k;
+                const bool in = t >= lo && t < hi;
+                fresh |= in ? 0x00ff00ffu << (8 * k) : 0u;
+                if (in && c == 0) *reinterpret_cast<uint32_t *>(rec + KV_B * a.d + 8 * t) = held(v[k]);
+            }
 #pragma unroll
-                for (int p = 0; p < NP; ++p) f = finite8<T>(raw[p][k], f);
+            for (int p = 0; p < NP; ++p) {
+                uint32_t w[2];
+                float far = 0.0f;
 #pragma unroll
-                for (int o = 1; o < 4; o <<= 1) {
-                    f.x = fminf(f.x, __shfl_xor_sync(0xffffffffu, f.x, o));
-                    f.y = fmaxf(f.y, __shfl_xor_sync(0xffffffffu, f.y, o));
+                for (int i = 0; i < 2; ++i) {
+                    float2 n[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+                        n[k] = pack2(codes2<T>(raw[p][k], 2 * i, v[k], far), codes2<T>(raw[p][k], 2 * i + 1, v[k], far), 16.0f);
+                    const float2 u = pack2(n[0], n[1], 256.0f);
+                    w[i] = word_of(u.x, u.y);
                 }
-                r[k] = clipped(f);
-            }
-        }
-        uint32_t fresh = 0;
+                if (far > NEAR) {
+                    w[0] = w[1] = 0;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int t = g + 8 * k;
-            v[k] = lvq_of(r[k]);
-            if (t < lo || t >= hi) continue;
-            fresh |= 0x00ff00ffu << (8 * k);
-            if (c == 0) *reinterpret_cast<uint32_t *>(rec + KV_B * a.d + 8 * t) = held(v[k]);
-        }
-        if (!fresh) return;
+                    for (int k = 0; k < 2; ++k) {
+                        Eight<T> x8;
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            if (32 * p + 8 * c >= a.d) break;
-            float2 n[2][4];
+                        for (int j = 0; j < W; ++j) x8.w[j] = raw[p][k][j];
+                        const uint32_t n8 = codes8_near<T>(x8, v[k].b, v[k].s, v[k].inv);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if (clip) codes8_clipped<T>(raw[p][k], v[k], r[k].lo, r[k].hi, n[k]);
-                else codes8<T>(raw[p][k], v[k], n[k]);
+                        for (int i = 0; i < 2; ++i) {  // dims 0, 2 of a word's four in its low half, 1, 3 in the high one
+                            const uint32_t n4 = n8 >> (16 * i);
+                            w[i] |= ((n4 & 15) | (n4 >> 4 & 0xf0) | (n4 & 0xf0) << 12 | (n4 & 0xf000) << 8) << (8 * k);
+                        }
+                    }
+                }
+                if (32 * p + 8 * c >= a.d || !fresh) continue;
+                uint2 *dst = reinterpret_cast<uint2 *>(rec + (2 * p + (c >> 1)) * 128 + g * 16 + (c & 1) * 8);
+                if (fresh != 0xffffffffu) {
+                    const uint2 was = *dst;
+                    w[0] = merged(was.x, w[0], fresh), w[1] = merged(was.y, w[1], fresh);
+                }
+                *dst = make_uint2(w[0], w[1]);
             }
-            uint32_t w[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float2 u = pack2(pack2(n[0][2 * i], n[0][2 * i + 1], 16.0f), pack2(n[1][2 * i], n[1][2 * i + 1], 16.0f), 256.0f);
-                w[i] = word_of(u.x, u.y);
-            }
-            uint2 *dst = reinterpret_cast<uint2 *>(rec + (2 * p + (c >> 1)) * 128 + g * 16 + (c & 1) * 8);
-            if (fresh != 0xffffffffu) {
-                const uint2 was = *dst;
-                w[0] = merged(was.x, w[0], fresh), w[1] = merged(was.y, w[1], fresh);
-            }
-            *dst = make_uint2(w[0], w[1]);
         }
     } else {
         constexpr int NI = (D + 63) / 64;
@@ -264,77 +301,70 @@ __global__ void __launch_bounds__(WARPS * 32) kv4_write_kernel(const __grid_cons
         for (int i = 0; i < NI; ++i)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int t = 2 * c + (k & 1) + 8 * (k >> 1), e = (lane >> 2) + 8 * i, from = 8 * (8 * e < a.d ? e : e & 1);
-#pragma unroll
-                for (int j = 0; j < W; ++j) raw[i][k][j] = 0;
-                if (t >= lo && t < hi) load8(x + (int64_t)t * src.token + from, src.wide, raw[i][k]);
+                const int e = (lane >> 2) + 8 * i;
+                get(2 * c + (k & 1) + 8 * (k >> 1), 8 * (8 * e < a.d ? e : e & 1), raw[i][k]);
             }
         if (!there) return;
-        Range r[4];
-        bool fine = true;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            r[k] = range8<T>(raw[0][k]);
-#pragma unroll
-            for (int i = 1; i < NI; ++i) r[k] = both(r[k], range8<T>(raw[i][k]));
-            r[k] = across(across(across(r[k], 4), 8), 16);
-            fine = fine && ordinary(r[k]);
-        }
-        const bool clip = !__all_sync(0xffffffffu, fine);
-        if (clip) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float2 f = make_float2(INFINITY, -INFINITY);
-#pragma unroll
-                for (int i = 0; i < NI; ++i) f = finite8<T>(raw[i][k], f);
-#pragma unroll
-                for (int o = 4; o < 32; o <<= 1) {
-                    f.x = fminf(f.x, __shfl_xor_sync(0xffffffffu, f.x, o));
-                    f.y = fmaxf(f.y, __shfl_xor_sync(0xffffffffu, f.y, o));
-                }
-                r[k] = clipped(f);
-            }
-        }
         Lvq v[4];
-        uint32_t fresh = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int t = 2 * c + (k & 1) + 8 * (k >> 1);
-            v[k] = lvq_of(r[k]);
-            if (t < lo || t >= hi) continue;
-            fresh |= 0x0f0fu << (16 * (k & 1) + 4 * (k >> 1));
-            if (lane < 4) *reinterpret_cast<uint32_t *>(rec + KV_B * a.d + 8 * t + 4) = held(v[k]);
-        }
+            Range r = range8<T>(raw[0][k]);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-            const int e = (lane >> 2) + 8 * i, odd = e & 1;
-            float2 n[4][4];
+            for (int i = 1; i < NI; ++i) r = both(r, range8<T>(raw[i][k]));
+            r = across(across(across(r, 4), 8), 16);
+            fine = fine && ordinary(r);
+            v[k] = lvq_of(r);
+        }
+        if (__all_sync(0xffffffffu, fine)) {
+            uint32_t fresh = 0;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (clip) codes8_clipped<T>(raw[i][k], v[k], r[k].lo, r[k].hi, n[k]);
-                else codes8<T>(raw[i][k], v[k], n[k]);
+                const int t = 2 * c + (k & 1) + 8 * (k >> 1);
+                const bool in = t >= lo && t < hi;
+                fresh |= in ? 0x0f0fu << (16 * (k & 1) + 4 * (k >> 1)) : 0u;
+                if (in && lane < 4) *reinterpret_cast<uint32_t *>(rec + KV_B * a.d + 8 * t + 4) = held(v[k]);
             }
-            // dim 8 e + j: bytes 0 and 2 of its word (e even) or 1 and 3
-            uint32_t part[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 u = pack2(n[0][j], n[2][j], 16.0f), w = pack2(n[1][j], n[3][j], 16.0f);
-                part[2 * j] = word_of(u.x, w.x) << (8 * odd);
-                part[2 * j + 1] = word_of(u.y, w.y) << (8 * odd);
-            }
-            // of the eight words the two lanes share, the even one stores four, the odd one four
+            for (int i = 0; i < NI; ++i) {
+                const int e = (lane >> 2) + 8 * i, odd = e & 1;
+                // dim 8 e + j: bytes 0 and 2 of its word (e even) or 1 and 3
+                uint32_t part[8];
+                float far = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t give = odd ? part[j] : part[j + 4];
-                const uint32_t got = __shfl_xor_sync(0xffffffffu, give, 4);
-                uint32_t w = (odd ? part[j + 4] : part[j]) | got;
-                if (8 * e >= a.d || !fresh) continue;
-                uint32_t *dst = reinterpret_cast<uint32_t *>(rec + 8 * a.d + (e >> 1) * 128 + (j + 4 * odd) * 16 + 4 * c);
-                if (fresh != 0xffffffffu) w = merged(*dst, w, fresh);
-                *dst = w;
+                for (int j = 0; j < 4; ++j) {
+                    const float2 u = pack2(codes2<T>(raw[i][0], j, v[0], far), codes2<T>(raw[i][2], j, v[2], far), 16.0f);
+                    const float2 w = pack2(codes2<T>(raw[i][1], j, v[1], far), codes2<T>(raw[i][3], j, v[3], far), 16.0f);
+                    part[2 * j] = word_of(u.x, w.x) << (8 * odd);
+                    part[2 * j + 1] = word_of(u.y, w.y) << (8 * odd);
+                }
+                if (far > NEAR) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) part[j] = 0;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        Eight<T> x8;
+#pragma unroll
+                        for (int j = 0; j < W; ++j) x8.w[j] = raw[i][k][j];
+                        const uint32_t n8 = codes8_near<T>(x8, v[k].b, v[k].s, v[k].inv);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) part[j] |= (n8 >> (4 * j) & 15) << (16 * (k & 1) + 4 * (k >> 1) + 8 * odd);
+                    }
+                }
+                // of the eight words the two lanes share, the even one stores four, the odd one four
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t give = odd ? part[j] : part[j + 4];
+                    const uint32_t got = __shfl_xor_sync(0xffffffffu, give, 4);
+                    uint32_t w = (odd ? part[j + 4] : part[j]) | got;
+                    if (8 * e >= a.d || !fresh) continue;
+                    uint32_t *dst = reinterpret_cast<uint32_t *>(rec + 8 * a.d + (e >> 1) * 128 + (j + 4 * odd) * 16 + 4 * c);
+                    if (fresh != 0xffffffffu) w = merged(*dst, w, fresh);
+                    *dst = w;
+                }
             }
         }
     }
+    if (!__all_sync(0xffffffffu, fine)) block_slowly(x, src.token, a.d, tensor, lo, hi, rec, lane);
 }
 
 // the codes in bits 0..3, 16..19 of a word as floats

@@ -59,10 +59,46 @@ struct alignas(sizeof(T) * V) Vec {
     T v[V];
 };
 
+// A vector of neighbours (NEXT), or one of each half of the dims
+template <typename T, int E, int V, bool NEXT>
+struct Unit {
+    Vec<T, E> p, q;
+    __device__ __forceinline__ void load(const T *x, int half, bool copy) {
+#pragma unroll
+        for (int k = 0; k < E; k += V)
+            if (k == 0 || !copy) *reinterpret_cast<Vec<T, V> *>(p.v + k) = *reinterpret_cast<const Vec<T, V> *>(x + k);
+        if (!NEXT && !copy) q = *reinterpret_cast<const Vec<T, E> *>(x + half);
+    }
+    __device__ __forceinline__ void store(T *y, int half, bool copy) const {
+#pragma unroll
+        for (int k = 0; k < E; k += V)
+            if (k == 0 || !copy) *reinterpret_cast<Vec<T, V> *>(y + k) = *reinterpret_cast<const Vec<T, V> *>(p.v + k);
+        if (!NEXT && !copy) *reinterpret_cast<Vec<T, E> *>(y + half) = q;
+    }
+    __device__ __forceinline__ void turn(const float2 *cs) {
+        constexpr int N = NEXT ? E / 2 : E;  // pairs; their angles two at a time (an even number from an even one on)
+#pragma unroll
+        for (int k = 0; k < N; k += 2) {
+            const float4 two = N > 1 ? *reinterpret_cast<const float4 *>(cs + k) : make_float4(cs[k].x, cs[k].y, 0.0f, 0.0f);
+#pragma unroll
+            for (int i = k; i < k + 2 && i < N; ++i) {
+                const float2 one = i == k ? make_float2(two.x, two.y) : make_float2(two.z, two.w);
+                if constexpr (NEXT) pair(p.v[2 * i], p.v[2 * i + 1], one);
+                else pair(p.v[i], q.v[i], one);
+            }
+        }
+    }
+    __device__ __forceinline__ static void pair(T &x1, T &x2, float2 cs) {
+        const float a = as_float(x1), b = as_float(x2);
+        x1 = as_type<T>(a * cs.x - b * cs.y);
+        x2 = as_type<T>(a * cs.y + b * cs.x);
+    }
+};
+
 // V: elements of a vector
 template <typename T, int V, bool NEXT>
 __global__ void __launch_bounds__(THREADS) rotary_kernel(const __grid_constant__ RotaryArgs a) {
-    extern __shared__ float2 angles[];  // [tokens][dims / 2] cosine, sine
+    extern __shared__ __align__(16) float2 angles[];  // [tokens][dims / 2] cosine, sine
     __shared__ int there[TOKENS_MOST];
     const int tid = threadIdx.x, lane = tid & 31, half = a.dims / 2;
     const int tok0 = blockIdx.x / a.cuts * a.tile, cut = blockIdx.x % a.cuts, nt = min(a.tile, a.tokens - tok0);
@@ -94,47 +130,43 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(const __grid_constant__
     }
     __syncthreads();
     // units: per token and head the vectors of a rotated head (NEXT: pairs of neighbours, a vector a
-    // unit; else a vector of the first half and one of the second), then those copied
+    // unit; else a vector of the first half and one of the second), then those copied.  A thread keeps to one unit
+    // and goes from row to row (token, head), so that its addresses are additions
     constexpr int E = NEXT && V == 1 ? 2 : V;  // elements of a unit's vector, loaded one at a time where V is 1
     const int turned = NEXT ? a.dims / E : half / V, units = turned + a.copied / V;
-    const int h0 = (int)((int64_t)a.heads * cut / a.cuts), nh = (int)((int64_t)a.heads * (cut + 1) / a.cuts) - h0;
-    for (int i = tid; i < nt * nh * units; i += THREADS) {
-        const int row = a.by_units.div(i), u = i - row * units;
-        const int t = a.tile == 1 ? 0 : a.by_heads.div(row), head = h0 + row - t * nh;  // (heads are cut where a tile is one token)
-        if (!there[t]) continue;
-        const bool second = head >= a.part[0].heads;
-        const RotaryPart &part = a.part[second];
-        const int hh = second ? head - a.part[0].heads : head;
-        const T *x = static_cast<const T *>(part.x) + (int64_t)(tok0 + t) * part.x_token + (int64_t)hh * part.x_head;
-        T *y = static_cast<T *>(part.y) + (int64_t)(tok0 + t) * part.y_token + (int64_t)hh * part.y_head;
-        using Vector = Vec<T, V>;
-        if (u >= turned) {
-            const int dim = a.dims + (u - turned) * V;
-            *reinterpret_cast<Vector *>(y + dim) = *reinterpret_cast<const Vector *>(x + dim);
-        } else if constexpr (NEXT) {
-            Vec<T, E> p;
-#pragma unroll
-            for (int k = 0; k < E; k += V) *reinterpret_cast<Vector *>(p.v + k) = *reinterpret_cast<const Vector *>(x + u * E + k);
-#pragma unroll
-            for (int k = 0; k < E / 2; ++k) {
-                const float2 cs = angles[t * half + u * (E / 2) + k];
-                const float x1 = as_float(p.v[2 * k]), x2 = as_float(p.v[2 * k + 1]);
-                p.v[2 * k] = as_type<T>(x1 * cs.x - x2 * cs.y);
-                p.v[2 * k + 1] = as_type<T>(x1 * cs.y + x2 * cs.x);
+    const int step = max(THREADS / units, 1), first = a.by_units.div(tid);
+    if (units <= THREADS && first >= step) return;
+    for (int u = tid - (units <= THREADS ? first * units : 0); u < units; u += THREADS) {
+        const bool copy = u >= turned;
+        const int dim = copy ? a.dims + (u - turned) * V : u * E;
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+            const RotaryPart &part = a.part[k];
+            const int h0 = part.heads * cut / a.cuts, nh = part.heads * (cut + 1) / a.cuts - h0;
+            if (nh == 0) continue;
+            int row = units <= THREADS ? first : 0, t = row / nh, head = row - t * nh;
+            const T *x = static_cast<const T *>(part.x) + (int64_t)(tok0 + t) * part.x_token + (int64_t)(h0 + head) * part.x_head + dim;
+            T *y = static_cast<T *>(part.y) + (int64_t)(tok0 + t) * part.y_token + (int64_t)(h0 + head) * part.y_head + dim;
+            const int64_t x_step = step * part.x_head, y_step = step * part.y_head;
+            const int64_t x_wrap = part.x_token - nh * part.x_head, y_wrap = part.y_token - nh * part.y_head;
+            // the next row's vectors are read before this one's are used
+            Unit<T, E, V, NEXT> now, next;
+            bool in = t < nt && there[t];
+            if (in) now.load(x, half, copy);
+            while (t < nt) {
+                const int t_now = t;
+                const bool in_now = in;
+                T *y_now = y;
+                head += step, x += x_step, y += y_step;
+                while (head >= nh) head -= nh, x += x_wrap, y += y_wrap, ++t;
+                in = t < nt && there[t];
+                if (in) next.load(x, half, copy);
+                if (in_now) {
+                    if (!copy) now.turn(angles + t_now * half + (NEXT ? dim / 2 : dim));
+                    now.store(y_now, half, copy);
+                }
+                now = next;
             }
-#pragma unroll
-            for (int k = 0; k < E; k += V) *reinterpret_cast<Vector *>(y + u * E + k) = *reinterpret_cast<const Vector *>(p.v + k);
-        } else {
-            Vector p = *reinterpret_cast<const Vector *>(x + u * V), q = *reinterpret_cast<const Vector *>(x + half + u * V);
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float2 cs = angles[t * half + u * V + k];
-                const float x1 = as_float(p.v[k]), x2 = as_float(q.v[k]);
-                p.v[k] = as_type<T>(x1 * cs.x - x2 * cs.y);
-                q.v[k] = as_type<T>(x1 * cs.y + x2 * cs.x);
-            }
-            *reinterpret_cast<Vector *>(y + u * V) = p;
-            *reinterpret_cast<Vector *>(y + half + u * V) = q;
         }
     }
 }
@@ -146,7 +178,6 @@ cudaError_t run(RotaryArgs a, cudaStream_t st) {
     a.tile = std::max(1, std::min({THREADS / half, TOKENS_MOST, a.tokens / (4 * KV_SMS)}));
     a.cuts = (int)std::max<int64_t>(1, std::min<int64_t>(a.heads, 2 * KV_SMS / a.tokens));
     a.by_half = FastDiv(half);
-    a.by_heads = FastDiv(a.heads);
     a.by_units = FastDiv((NEXT ? a.dims / (V == 1 ? 2 : V) : half / V) + a.copied / V);
     const int64_t grid = cdiv(a.tokens, a.tile) * a.cuts;
     rotary_kernel<T, V, NEXT><<<(unsigned)grid, THREADS, (size_t)a.tile * half * sizeof(float2), st>>>(a);

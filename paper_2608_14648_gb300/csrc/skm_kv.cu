@@ -395,13 +395,13 @@ int skm_kv_rotate(const skm_kv_seqs *s, const skm_rotary *r, int d, int dtype, c
         narrow((int64_t)(reinterpret_cast<uintptr_t>(p.y) / e));
         for (const int64_t stride : {p.x_token, p.x_head, p.y_token, p.y_head}) narrow(stride);
         a.part[i] = RotaryPart{p.x, p.y, p.x_token, p.x_head, p.y_token, p.y_head, p.heads};
-        a.heads += p.heads;
+        a.heads = std::max(a.heads, p.heads);
     }
     if (most_tokens(s) == 0) return SKM_OK;
     a.copied = in_place ? 0 : d - r->dims;  // (a tensor that is in place beside one that is not: its dims onto themselves)
     narrow(r->layout == SKM_ROTARY_HALF ? r->dims / 2 : r->dims);
     narrow(a.copied);
-    if ((double)s->tokens * a.heads > 1e9) return set_error(SKM_ERR_UNSUPPORTED, "tokens * heads is too large");
+    if ((double)s->tokens * a.heads > 5e8) return set_error(SKM_ERR_UNSUPPORTED, "tokens * heads is too large");
     a.pos = s->pos;
     a.cu = s->cu;
     a.turns = r->turns;

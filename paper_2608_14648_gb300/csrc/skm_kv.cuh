@@ -66,11 +66,11 @@ struct RotaryArgs {
     const uint64_t *turns;
     int batch, tokens, max_tokens, dims, interleaved;
     int copied;         // dims behind the rotated ones that a call with other outputs copies
-    int heads;          // of both parts
+    int heads;          // of the part with more
     float gain, sine;   // factors of cosine and sine: the sine's is negative for a transposed call
     RotaryPart part[2];
     int tile, cuts;     // (set by the launcher) tokens of a CTA, CTAs that share a token's heads
-    FastDiv by_half, by_heads, by_units;
+    FastDiv by_half, by_units;
 };
 // vec: elements of a vector that all rows are aligned to
 cudaError_t launch_rotary(const RotaryArgs &a, int dtype, int vec, cudaStream_t st);
