@@ -6,14 +6,16 @@
 // it in registers, so the input is read once: smallest and largest in registers and over a few lanes, then
 // the codes.  A vector's codes depend on nothing else: what the block holds is never rounded again.
 //
-// Lanes.  Keys: (g, c), tokens g and g + 8, of every 32 dims the eight from 8 c on: a token's 32 dims
+// Lanes.  Ranges, and keys' codes: (g, c), tokens g and g + 8, of every 32 dims the eight from 8 c on: a token's 32 dims
 // are 64 consecutive bytes of 16-bit input, and the lane's codes are two neighbouring words.
 // Values: (e, c), dims 8 e .. of the four tokens 2c, 2c + 1, 2c + 8, 2c + 9 that share a word; the
 // other dims of a word are those of the lane next to it in e.
 //
-// Rounding.  q = (x - b) (1 / s) in fp32 takes three roundings of 2^-24 on the way to a number below
-// 16, so it is within 3 2^-20 of the quotient, whose nearest integer is q's unless q lies within 2^-18 of
-// the middle of two: then x - b is compared with (k + 1/2) s in 64 bits.
+// Rounding.  q = d y, d = x - b and y the correctly rounded reciprocal of s, corrected by its exact remainder: q' = q + (d -
+// q s) y.  q' is within 2^-20 of the quotient (half a unit in the last place, and d's rounding), so its
+// nearest integer is the quotient's unless it lies within 2^-18 of the middle of two.  It often is the middle itself (16-bit
+// values, biases and scales have few bits: one value in 2500 of a bf16 input): then the
+// remainder is 0, d is exact, and half to even is right; else x - b is compared with (k + 1/2) s in 64 bits.
 // Codes become words by multiply-adds of integers as floats (below 2^16, exact), two at a time.
 #include "skm_kv_cache.cuh"
 
@@ -107,16 +109,7 @@ __device__ __forceinline__ float code_of(float x, const Lvq &v) {
     const double over = (double)x - (double)v.b, mid = ((double)k + 0.5) * (double)v.s;
     return over > mid || (over == mid && ((int)k & 1)) ? k + 1.0f : k;
 }
-// codes of two values as floats; far: the largest distance of a quotient from its code
-template <typename T>
-__device__ __forceinline__ float2 codes2(const uint32_t *w, int i, const Lvq &v, float &far) {
-    const float2 q = mul2(add2(value2<T>(w, i), make_float2(-v.b, -v.b)), make_float2(v.inv, v.inv));
-    const float2 c = add2(add2(q, make_float2(MAGIC, MAGIC)), make_float2(-MAGIC, -MAGIC));
-    far = fmaxf(far, fmaxf(fabsf(q.x - c.x), fabsf(q.y - c.y)));
-    return c;
-}
-// the same where some are near the middle of two: one code in a nibble each (by value and not inlined: what is rare
-// costs the ordinary path no registers)
+// the same of 8 values, in a nibble each (by value and not inlined: what is rare costs the ordinary path no registers)
 template <typename T>
 struct Eight {
     uint32_t w[WORDS8<T>];
@@ -130,6 +123,42 @@ __device__ __noinline__ uint32_t codes8_near(Eight<T> x, float b, float s, float
         c |= (uint32_t)code_of(p.x, v) << (8 * i) | (uint32_t)code_of(p.y, v) << (8 * i + 4);
     }
     return c;
+}
+// x - b without a rounding error (Knuth's exact sum)
+__device__ __forceinline__ bool exact_less(float x, float b, float d) {
+    const float z = __fadd_rn(d, -x);
+    return __fadd_rn(__fadd_rn(x, -__fadd_rn(d, -z)), __fadd_rn(-b, -z)) == 0.0f;
+}
+// codes of 8 values as floats
+template <typename T>
+__device__ __forceinline__ void codes8(const Eight<T> &x, const Lvq &v, float2 (&c)[4]) {
+    const float2 less = make_float2(-v.b, -v.b), by = make_float2(v.inv, v.inv), s = make_float2(-v.s, -v.s);
+    const float2 up = make_float2(MAGIC, MAGIC), down = make_float2(-MAGIC, -MAGIC);
+    const auto quotient = [&](float2 d) {
+        const float2 q = mul2(d, by);
+        return fma2(fma2(q, s, d), by, q);
+    };
+    float far = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 q = quotient(add2(value2<T>(x.w, i), less));
+        c[i] = add2(add2(q, up), down);
+        far = fmaxf(far, fmaxf(fabsf(q.x - c[i].x), fabsf(q.y - c[i].y)));
+    }
+    if (far <= NEAR) return;
+    bool open = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 y = value2<T>(x.w, i), d = add2(y, less), q = quotient(d), r = fma2(q, s, d);
+        const float ex = fabsf(q.x - c[i].x), ey = fabsf(q.y - c[i].y);
+        open = open || (ex > NEAR && !(ex == 0.5f && r.x == 0.0f && exact_less(y.x, v.b, d.x)));
+        open = open || (ey > NEAR && !(ey == 0.5f && r.y == 0.0f && exact_less(y.y, v.b, d.y)));
+    }
+    if (open) {
+        const uint32_t n = codes8_near<T>(x, v.b, v.s, v.inv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = make_float2((float)(n >> (8 * i) & 15), (float)(n >> (8 * i + 4) & 15));
+    }
 }
 
 __device__ __forceinline__ float2 pack2(float2 a, float2 b, float up) { return fma2(b, make_float2(up, up), a); }
@@ -210,161 +239,126 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 4 : sizeof(
     const bool there = pg >= 0 && pg < a.pages;
     uint8_t *rec = a.k + (((int64_t)(there ? pg : 0) * a.heads + h) * a.bpp + a.by_bpp.mod(blk)) * kv4_bytes(a.d);
     // 8 values of a token, zeros if it is not new; where wide loads are not possible all blocks go the slow way
-    const auto get = [&](int t, int dim, uint32_t *w) {
+    const auto get = [&](int t, int dim) {
         const uint4 *p = reinterpret_cast<const uint4 *>(x + (int64_t)t * src.token + dim);
         const bool in = t >= lo && t < hi;
+        Eight<T> e;
 #pragma unroll
         for (int i = 0; i < W; i += 4) {
-            const uint4 v = in ? __ldg(p + i / 4) : make_uint4(0, 0, 0, 0);
-            w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+            const uint4 y = in ? __ldg(p + i / 4) : make_uint4(0, 0, 0, 0);
+            e.w[i] = y.x, e.w[i + 1] = y.y, e.w[i + 2] = y.z, e.w[i + 3] = y.w;
         }
+        return e;
     };
     if (!src.wide) {
         if (there) block_slowly(x, src.token, a.d, tensor, lo, hi, rec, lane);
         return;
     }
-    bool fine = true;
-    if (tensor == 0) {
-        constexpr int NP = D / 32;
-        const int g = lane >> 2, c = lane & 3;
-        uint32_t raw[NP][2][W];
+    // the range of each token, in lanes (g, c) of either tensor: tokens g and g + 8, of every 32 dims the eight from 8 c on
+    const int g = lane >> 2, c = lane & 3;
+    constexpr int NP = D / 32;
+    Range r[2];
+    {
+        Eight<T> raw[NP][2];
 #pragma unroll
         for (int p = 0; p < NP; ++p)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 // (dims past the last: the first ones once more, which does not change the range)
                 const int dim = 32 * p + 8 * c;
-                get(g + 8 * k, dim < a.d ? dim : 8 * (c & 1), raw[p][k]);
+                raw[p][k] = get(g + 8 * k, dim < a.d ? dim : 8 * (c & 1));
             }
         if (!there) return;
-        Lvq v[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            Range r = range8<T>(raw[0][k]);
+            r[k] = range8<T>(raw[0][k].w);
 #pragma unroll
-            for (int p = 1; p < NP; ++p) r = both(r, range8<T>(raw[p][k]));
-            r = across(across(r, 1), 2);
-            fine = fine && ordinary(r);
-            v[k] = lvq_of(r);
+            for (int p = 1; p < NP; ++p) r[k] = both(r[k], range8<T>(raw[p][k].w));
+            r[k] = across(across(r[k], 1), 2);
         }
-        if (__all_sync(0xffffffffu, fine)) {
-            uint32_t fresh = 0;
+    }
+    if (!__all_sync(0xffffffffu, ordinary(r[0]) && ordinary(r[1]))) {
+        block_slowly(x, src.token, a.d, tensor, lo, hi, rec, lane);
+        return;
+    }
+    Lvq v[2];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int t = g + 8 * k;
-                const bool in = t >= lo && t < hi;
-                fresh |= in ? 0x00ff00ffu << (8 * k) : 0u;
-                if (in && c == 0) *reinterpret_cast<uint32_t *>(rec + KV_B * a.d + 8 * t) = held(v[k]);
+    for (int k = 0; k < 2; ++k) {
+        const int t = g + 8 * k;
+        v[k] = lvq_of(r[k]);
+        if (c == 0 && t >= lo && t < hi) *reinterpret_cast<uint32_t *>(rec + KV_B * a.d + 8 * t + 4 * tensor) = held(v[k]);
+    }
+    // the codes: the values again, out of L1, in rolled loops (unrolled, with the values in registers, warps waited for
+    // their instructions most of all: writing and reading back 87 us)
+    if (tensor == 0) {
+        uint32_t fresh = 0;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) fresh |= g + 8 * k >= lo && g + 8 * k < hi ? 0x00ff00ffu << (8 * k) : 0u;
+        if (!fresh) return;
+#pragma unroll 1
+        for (int dim = 8 * c; dim < a.d; dim += 32) {
+            float2 n[2][4];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) codes8<T>(get(g + 8 * k, dim), v[k], n[k]);
+            uint32_t w[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float2 u = pack2(pack2(n[0][2 * i], n[0][2 * i + 1], 16.0f), pack2(n[1][2 * i], n[1][2 * i + 1], 16.0f), 256.0f);
+                w[i] = word_of(u.x, u.y);
             }
-#pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                uint32_t w[2];
-                float far = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float2 n[2];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        n[k] = pack2(codes2<T>(raw[p][k], 2 * i, v[k], far), codes2<T>(raw[p][k], 2 * i + 1, v[k], far), 16.0f);
-                    const float2 u = pack2(n[0], n[1], 256.0f);
-                    w[i] = word_of(u.x, u.y);
-                }
-                if (far > NEAR) {
-                    w[0] = w[1] = 0;
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        Eight<T> x8;
-#pragma unroll
-                        for (int j = 0; j < W; ++j) x8.w[j] = raw[p][k][j];
-                        const uint32_t n8 = codes8_near<T>(x8, v[k].b, v[k].s, v[k].inv);
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {  // dims 0, 2 of a word's four in its low half, 1, 3 in the high one
-                            const uint32_t n4 = n8 >> (16 * i);
-                            w[i] |= ((n4 & 15) | (n4 >> 4 & 0xf0) | (n4 & 0xf0) << 12 | (n4 & 0xf000) << 8) << (8 * k);
-                        }
-                    }
-                }
-                if (32 * p + 8 * c >= a.d || !fresh) continue;
-                uint2 *dst = reinterpret_cast<uint2 *>(rec + (2 * p + (c >> 1)) * 128 + g * 16 + (c & 1) * 8);
-                if (fresh != 0xffffffffu) {
-                    const uint2 was = *dst;
-                    w[0] = merged(was.x, w[0], fresh), w[1] = merged(was.y, w[1], fresh);
-                }
-                *dst = make_uint2(w[0], w[1]);
+            uint2 *dst = reinterpret_cast<uint2 *>(rec + (dim >> 4) * 128 + g * 16 + (c & 1) * 8);
+            if (fresh != 0xffffffffu) {
+                const uint2 was = *dst;
+                w[0] = merged(was.x, w[0], fresh), w[1] = merged(was.y, w[1], fresh);
             }
+            *dst = make_uint2(w[0], w[1]);
         }
     } else {
-        constexpr int NI = (D + 63) / 64;
-        const int c = lane & 3;
-        uint32_t raw[NI][4][W];
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int e = (lane >> 2) + 8 * i;
-                get(2 * c + (k & 1) + 8 * (k >> 1), 8 * (8 * e < a.d ? e : e & 1), raw[i][k]);
-            }
-        if (!there) return;
-        Lvq v[4];
+        // lanes (e, c): dims 8 e .. of the four tokens that share a word; their vectors from the lanes above
+        Lvq u[4];
+        uint32_t fresh = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            Range r = range8<T>(raw[0][k]);
-#pragma unroll
-            for (int i = 1; i < NI; ++i) r = both(r, range8<T>(raw[i][k]));
-            r = across(across(across(r, 4), 8), 16);
-            fine = fine && ordinary(r);
-            v[k] = lvq_of(r);
+            const int t = 2 * c + (k & 1) + 8 * (k >> 1), from = 4 * (2 * c + (k & 1));
+            u[k].b = __shfl_sync(0xffffffffu, v[k >> 1].b, from);
+            u[k].s = __shfl_sync(0xffffffffu, v[k >> 1].s, from);
+            u[k].inv = __shfl_sync(0xffffffffu, v[k >> 1].inv, from);
+            fresh |= t >= lo && t < hi ? 0x0f0fu << (16 * (k & 1) + 4 * (k >> 1)) : 0u;
         }
-        if (__all_sync(0xffffffffu, fine)) {
-            uint32_t fresh = 0;
+        const int odd = g & 1;
+#pragma unroll 1
+        for (int e0 = 0; 8 * e0 < a.d; e0 += 8) {
+            const int e = e0 + g;
+            const bool in = 8 * e < a.d && fresh;
+            // dim 8 e + j: bytes 0 and 2 of its word (e even) or 1 and 3
+            float2 n[2][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int t = 2 * c + (k & 1) + 8 * (k >> 1);
-                const bool in = t >= lo && t < hi;
-                fresh |= in ? 0x0f0fu << (16 * (k & 1) + 4 * (k >> 1)) : 0u;
-                if (in && lane < 4) *reinterpret_cast<uint32_t *>(rec + KV_B * a.d + 8 * t + 4) = held(v[k]);
+            for (int k = 0; k < 2; ++k) {
+                float2 first[4], second[4];
+                codes8<T>(get(2 * c + k, in ? 8 * e : 0), u[k], first);
+                codes8<T>(get(2 * c + k + 8, in ? 8 * e : 0), u[k + 2], second);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) n[k][j] = pack2(first[j], second[j], 16.0f);
             }
+            uint32_t part[8];
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int e = (lane >> 2) + 8 * i, odd = e & 1;
-                // dim 8 e + j: bytes 0 and 2 of its word (e even) or 1 and 3
-                uint32_t part[8];
-                float far = 0.0f;
+            for (int j = 0; j < 4; ++j) {
+                part[2 * j] = word_of(n[0][j].x, n[1][j].x) << (8 * odd);
+                part[2 * j + 1] = word_of(n[0][j].y, n[1][j].y) << (8 * odd);
+            }
+            // of the eight words the two lanes share, the even one stores four, the odd one four
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 u = pack2(codes2<T>(raw[i][0], j, v[0], far), codes2<T>(raw[i][2], j, v[2], far), 16.0f);
-                    const float2 w = pack2(codes2<T>(raw[i][1], j, v[1], far), codes2<T>(raw[i][3], j, v[3], far), 16.0f);
-                    part[2 * j] = word_of(u.x, w.x) << (8 * odd);
-                    part[2 * j + 1] = word_of(u.y, w.y) << (8 * odd);
-                }
-                if (far > NEAR) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) part[j] = 0;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        Eight<T> x8;
-#pragma unroll
-                        for (int j = 0; j < W; ++j) x8.w[j] = raw[i][k][j];
-                        const uint32_t n8 = codes8_near<T>(x8, v[k].b, v[k].s, v[k].inv);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) part[j] |= (n8 >> (4 * j) & 15) << (16 * (k & 1) + 4 * (k >> 1) + 8 * odd);
-                    }
-                }
-                // of the eight words the two lanes share, the even one stores four, the odd one four
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t give = odd ? part[j] : part[j + 4];
-                    const uint32_t got = __shfl_xor_sync(0xffffffffu, give, 4);
-                    uint32_t w = (odd ? part[j + 4] : part[j]) | got;
-                    if (8 * e >= a.d || !fresh) continue;
-                    uint32_t *dst = reinterpret_cast<uint32_t *>(rec + 8 * a.d + (e >> 1) * 128 + (j + 4 * odd) * 16 + 4 * c);
-                    if (fresh != 0xffffffffu) w = merged(*dst, w, fresh);
-                    *dst = w;
-                }
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t give = odd ? part[j] : part[j + 4];
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, give, 4);
+                uint32_t w = (odd ? part[j + 4] : part[j]) | got;
+                if (!in) continue;
+                uint32_t *dst = reinterpret_cast<uint32_t *>(rec + 8 * a.d + (e >> 1) * 128 + (j + 4 * odd) * 16 + 4 * c);
+                if (fresh != 0xffffffffu) w = merged(*dst, w, fresh);
+                *dst = w;
             }
         }
     }
-    if (!__all_sync(0xffffffffu, fine)) block_slowly(x, src.token, a.d, tensor, lo, hi, rec, lane);
 }
 
 // the codes in bits 0..3, 16..19 of a word as floats
