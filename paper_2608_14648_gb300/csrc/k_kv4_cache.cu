@@ -216,7 +216,7 @@ __device__ __noinline__ void block_slowly(const T *x, int64_t step, int d, int t
 
 // Warps: one a (sequence, block its new rows reach, head, tensor).  D: dims at most
 template <typename T, int D>
-__global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 4 : sizeof(T) * D <= 512 ? 2 : 1)
+__global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 3 : sizeof(T) * D <= 512 ? 2 : 1)
     kv4_write_kernel(const __grid_constant__ KvCacheArgs a) {
     constexpr int W = WORDS8<T>;
     const int lane = threadIdx.x & 31;

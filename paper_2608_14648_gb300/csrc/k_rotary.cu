@@ -42,56 +42,98 @@ __device__ __forceinline__ int sequence_of(const int32_t *cu, int batch, int tok
     return lo < batch ? lo : -1;
 }
 
-template <typename T>
-__device__ __forceinline__ float as_float(T x) {
-    if constexpr (sizeof(T) == 4) return x;
-    else if constexpr (std::is_same<T, __half>::value) return __half2float(x);
-    else return __bfloat162float(x);
-}
-template <typename T>
-__device__ __forceinline__ T as_type(float x) {
-    if constexpr (sizeof(T) == 4) return x;
-    else if constexpr (std::is_same<T, __half>::value) return __float2half_rn(x);
-    else return __float2bfloat16_rn(x);
+// V elements as words (one 16-bit element: in a word's low half)
+template <typename T, int V>
+constexpr int WORDS = sizeof(T) * V < 4 ? 1 : sizeof(T) * V / 4;
+template <typename T, int V>
+__device__ __forceinline__ void load_words(const T *x, uint32_t *w) {
+    constexpr int BYTES = sizeof(T) * V;
+    if constexpr (BYTES == 2) {
+        w[0] = *reinterpret_cast<const uint16_t *>(x);
+    } else if constexpr (BYTES == 4) {
+        w[0] = *reinterpret_cast<const uint32_t *>(x);
+    } else if constexpr (BYTES == 8) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(x);
+        w[0] = v.x, w[1] = v.y;
+    } else {
+        static_assert(BYTES == 16);
+        const uint4 v = *reinterpret_cast<const uint4 *>(x);
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    }
 }
 template <typename T, int V>
-struct alignas(sizeof(T) * V) Vec {
-    T v[V];
-};
+__device__ __forceinline__ void store_words(T *y, const uint32_t *w) {
+    constexpr int BYTES = sizeof(T) * V;
+    if constexpr (BYTES == 2) *reinterpret_cast<uint16_t *>(y) = (uint16_t)w[0];
+    else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t *>(y) = w[0];
+    else if constexpr (BYTES == 8) *reinterpret_cast<uint2 *>(y) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint4 *>(y) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+// elements 2 i and 2 i + 1 (of one element: it and anything)
+template <typename T>
+__device__ __forceinline__ float2 two_of(const uint32_t *w, int i) {
+    if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    else if constexpr (std::is_same<T, __half>::value) return __half22float2(*reinterpret_cast<const __half2 *>(w + i));
+    else return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+}
+template <typename T>
+__device__ __forceinline__ void put_two(uint32_t *w, int i, float2 v) {
+    if constexpr (sizeof(T) == 4) {
+        w[2 * i] = __float_as_uint(v.x), w[2 * i + 1] = __float_as_uint(v.y);
+    } else if constexpr (std::is_same<T, __half>::value) {
+        const __half2 h = __floats2half2_rn(v.x, v.y);
+        w[i] = *reinterpret_cast<const uint32_t *>(&h);
+    } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+        w[i] = *reinterpret_cast<const uint32_t *>(&h);
+    }
+}
 
-// A vector of neighbours (NEXT), or one of each half of the dims
-template <typename T, int E, int V, bool NEXT>
+// What a thread takes of a row: a vector of V elements, neighbours in pairs (NEXT; with V = 1 two elements, one at a time), or one
+// of each half of the dims
+template <typename T, int V, bool NEXT>
 struct Unit {
-    Vec<T, E> p, q;
+    static constexpr int E = NEXT && V == 1 ? 2 : V, N = (E + 1) / 2;  // elements of p, twos of them
+    uint32_t p[N * 2 * sizeof(T) / 4], q[N * 2 * sizeof(T) / 4];
     __device__ __forceinline__ void load(const T *x, int half, bool copy) {
-#pragma unroll
-        for (int k = 0; k < E; k += V)
-            if (k == 0 || !copy) *reinterpret_cast<Vec<T, V> *>(p.v + k) = *reinterpret_cast<const Vec<T, V> *>(x + k);
-        if (!NEXT && !copy) q = *reinterpret_cast<const Vec<T, E> *>(x + half);
-    }
-    __device__ __forceinline__ void store(T *y, int half, bool copy) const {
-#pragma unroll
-        for (int k = 0; k < E; k += V)
-            if (k == 0 || !copy) *reinterpret_cast<Vec<T, V> *>(y + k) = *reinterpret_cast<const Vec<T, V> *>(p.v + k);
-        if (!NEXT && !copy) *reinterpret_cast<Vec<T, E> *>(y + half) = q;
-    }
-    __device__ __forceinline__ void turn(const float2 *cs) {
-        constexpr int N = NEXT ? E / 2 : E;  // pairs; their angles two at a time (an even number from an even one on)
-#pragma unroll
-        for (int k = 0; k < N; k += 2) {
-            const float4 two = N > 1 ? *reinterpret_cast<const float4 *>(cs + k) : make_float4(cs[k].x, cs[k].y, 0.0f, 0.0f);
-#pragma unroll
-            for (int i = k; i < k + 2 && i < N; ++i) {
-                const float2 one = i == k ? make_float2(two.x, two.y) : make_float2(two.z, two.w);
-                if constexpr (NEXT) pair(p.v[2 * i], p.v[2 * i + 1], one);
-                else pair(p.v[i], q.v[i], one);
-            }
+        if constexpr (E > V) {
+            uint32_t a[1], b[1] = {0};
+            load_words<T, 1>(x, a);
+            if (!copy) load_words<T, 1>(x + 1, b);
+            if constexpr (sizeof(T) == 4) p[0] = a[0], p[1] = b[0];
+            else p[0] = a[0] | b[0] << 16;
+        } else {
+            load_words<T, V>(x, p);
+            if constexpr (!NEXT)
+                if (!copy) load_words<T, V>(x + half, q);
         }
     }
-    __device__ __forceinline__ static void pair(T &x1, T &x2, float2 cs) {
-        const float a = as_float(x1), b = as_float(x2);
-        x1 = as_type<T>(a * cs.x - b * cs.y);
-        x2 = as_type<T>(a * cs.y + b * cs.x);
+    __device__ __forceinline__ void store(T *y, int half, bool copy) const {
+        if constexpr (E > V) {
+            const uint32_t b = sizeof(T) == 4 ? p[sizeof(T) / 4] : p[0] >> 16;
+            store_words<T, 1>(y, p);
+            if (!copy) store_words<T, 1>(y + 1, &b);
+        } else {
+            store_words<T, V>(y, p);
+            if constexpr (!NEXT)
+                if (!copy) store_words<T, V>(y + half, q);
+        }
+    }
+    __device__ __forceinline__ void turn(const float2 *cs) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float2 a = two_of<T>(p, i);
+            if constexpr (NEXT) {
+                const float2 r = cs[i];
+                put_two<T>(p, i, make_float2(a.x * r.x - a.y * r.y, a.x * r.y + a.y * r.x));
+            } else {
+                const float2 b = two_of<T>(q, i);
+                // (cosine, sine) of two pairs at once: an even number of pairs from an even one on
+                const float4 r = E > 1 ? *reinterpret_cast<const float4 *>(cs + 2 * i) : make_float4(cs[0].x, cs[0].y, 0.0f, 0.0f);
+                put_two<T>(p, i, make_float2(a.x * r.x - b.x * r.y, a.y * r.z - b.y * r.w));
+                put_two<T>(q, i, make_float2(a.x * r.y + b.x * r.x, a.y * r.w + b.y * r.z));
+            }
+        }
     }
 };
 
@@ -132,7 +174,7 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(const __grid_constant__
     // units: per token and head the vectors of a rotated head (NEXT: pairs of neighbours, a vector a
     // unit; else a vector of the first half and one of the second), then those copied.  A thread keeps to one unit
     // and goes from row to row (token, head), so that its addresses are additions
-    constexpr int E = NEXT && V == 1 ? 2 : V;  // elements of a unit's vector, loaded one at a time where V is 1
+    constexpr int E = Unit<T, V, NEXT>::E;
     const int turned = NEXT ? a.dims / E : half / V, units = turned + a.copied / V;
     const int step = max(THREADS / units, 1), first = a.by_units.div(tid);
     if (units <= THREADS && first >= step) return;
@@ -150,7 +192,7 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(const __grid_constant__
             const int64_t x_step = step * part.x_head, y_step = step * part.y_head;
             const int64_t x_wrap = part.x_token - nh * part.x_head, y_wrap = part.y_token - nh * part.y_head;
             // the next row's vectors are read before this one's are used
-            Unit<T, E, V, NEXT> now, next;
+            Unit<T, V, NEXT> now, next;
             bool in = t < nt && there[t];
             if (in) now.load(x, half, copy);
             while (t < nt) {
