@@ -145,19 +145,19 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(const __grid_constant__
     const int tid = threadIdx.x, lane = tid & 31, half = a.dims / 2;
     const int tok0 = blockIdx.x / a.cuts * a.tile, cut = blockIdx.x % a.cuts, nt = min(a.tile, a.tokens - tok0);
     __shared__ int64_t at[TOKENS_MOST];
+    bool mine = true;
     for (int i = tid >> 5; i < nt; i += THREADS / 32) {
         const int b = sequence_of(a.cu, a.batch, tok0 + i, lane);
+        int2 rows = make_int2(0, 0);
+        if (b >= 0) rows = kv_rows_of(a.cu, b, a.tokens, a.max_tokens);
+        const bool in = tok0 + i >= rows.x && tok0 + i < rows.x + rows.y;
+        mine = mine && in;
         if (lane == 0) {
-            bool in = false;
-            if (b >= 0) {
-                const int2 rows = kv_rows_of(a.cu, b, a.tokens, a.max_tokens);
-                in = tok0 + i >= rows.x && tok0 + i < rows.x + rows.y;
-                at[i] = (int64_t)a.pos[b] + (tok0 + i - rows.x);
-            }
             there[i] = in;
+            if (in) at[i] = (int64_t)a.pos[b] + (tok0 + i - rows.x);
         }
     }
-    __syncthreads();
+    const bool all = __syncthreads_and(mine);  // (rows that belong to no sequence are left alone)
     for (int i = tid; i < nt * half; i += THREADS) {
         const int t = a.by_half.div(i), pair = i - t * half;
         if (!there[t]) continue;
@@ -191,23 +191,25 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(const __grid_constant__
             T *y = static_cast<T *>(part.y) + (int64_t)(tok0 + t) * part.y_token + (int64_t)(h0 + head) * part.y_head + dim;
             const int64_t x_step = step * part.x_head, y_step = step * part.y_head;
             const int64_t x_wrap = part.x_token - nh * part.x_head, y_wrap = part.y_token - nh * part.y_head;
-            // the next row's vectors are read before this one's are used
-            Unit<T, V, NEXT> now, next;
-            bool in = t < nt && there[t];
-            if (in) now.load(x, half, copy);
+            // two rows at a time: both are read before either is used
             while (t < nt) {
-                const int t_now = t;
-                const bool in_now = in;
-                T *y_now = y;
-                head += step, x += x_step, y += y_step;
-                while (head >= nh) head -= nh, x += x_wrap, y += y_wrap, ++t;
-                in = t < nt && there[t];
-                if (in) next.load(x, half, copy);
-                if (in_now) {
-                    if (!copy) now.turn(angles + t_now * half + (NEXT ? dim / 2 : dim));
-                    now.store(y_now, half, copy);
+                Unit<T, V, NEXT> unit[2];
+                T *to[2];
+                int of[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    to[i] = y;
+                    of[i] = t < nt && (all || there[t]) ? t : -1;
+                    if (of[i] >= 0) unit[i].load(x, half, copy);
+                    head += step, x += x_step, y += y_step;
+                    while (head >= nh) head -= nh, x += x_wrap, y += y_wrap, ++t;
                 }
-                now = next;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (of[i] < 0) continue;
+                    if (!copy) unit[i].turn(angles + of[i] * half + (NEXT ? dim / 2 : dim));
+                    unit[i].store(to[i], half, copy);
+                }
             }
         }
     }
