@@ -1041,14 +1041,11 @@ class Rotary:
         turns, self.gain = skm_rotary_turns(dims, base, scaling, factor, trained, low, high)
         self.dims, self.layout = int(dims), int(layout)
         self.turns = turns.to(device)
+        self.device = self.turns.device
         self.index = self.turns.get_device()
         ref = lambda back: RotaryRef(self.dims, self.layout, back, self.gain, self.turns.data_ptr())  # noqa: E731
         self.refs = ref(0), ref(1)
         self.addrs = tuple(ctypes.addressof(r) for r in self.refs)
-
-    @property
-    def device(self):
-        return self.turns.device
 
 
 _ROTARY_ROWS = struct.Struct("@PPqqqqii")  # RotaryRows, packed as the structs above
@@ -1072,25 +1069,31 @@ def skm_kv_rotate(rotary: Rotary, start, cu, rows, max_tokens, out=None, transpo
     current = torch._C._cuda_getDevice()
     if current != index:
         raise ValueError(f"the frequencies are on cuda:{index}, but the current device is cuda:{current}")
-    if start.dim() != 1:
-        raise ValueError("start must be an int32 tensor [batch]")
-    batch, shape, kind = start.shape[0], rows[0].shape, rows[0].dtype
+    if start.dim() != 1 or rows[0].dim() != 3:
+        raise ValueError("start must be an int32 tensor [batch], rows [tokens, heads, d]")
+    batch, (tokens, _, d), kind = start.shape[0], rows[0].shape, rows[0].dtype
     dtype = _KV_DTYPES.get(kind)
     if dtype is None:
         raise ValueError("rows must be float32, bfloat16 or float16")
-    if out is None:
-        out = tuple(_kv_empty(rotary, stream, x.shape, kind) for x in rows)
-    packed = b""
-    for x, y in zip(rows, out):
-        xs, ys = x.stride(), y.stride()
-        if (x.dim() != 3 or y.shape != x.shape or x.shape[0] != shape[0] or x.shape[2] != shape[2] or x.dtype != kind
-                or y.dtype != kind or xs[2] != 1 or ys[2] != 1 or x.get_device() != index or y.get_device() != index):
-            raise ValueError("rows and out must be [tokens, heads, d] of one type and one number of tokens, d contiguous, "
-                             "on the frequencies' device")
-        packed += _ROTARY_ROWS.pack(x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], x.shape[1], 0)
-    s = _KV_SEQS.pack(batch, 0, 0, _kv_ints("start", start, batch, index), _kv_ints("cu", cu, batch + 1, index), shape[0],
-                      max_tokens, 0)
-    rc = lib().skm_kv_rotate(s, rotary.addrs[bool(transpose)], shape[2], dtype, packed, len(rows), _kv_stream(rotary, stream))
+    outs, packed = [], b""
+    for i, x in enumerate(rows):
+        shape, x_at = x.shape, x.stride()
+        if len(shape) != 3 or shape[0] != tokens or shape[2] != d or x_at[2] != 1 or x.dtype is not kind or x.get_device() != index:
+            raise ValueError("rows must be [tokens, heads, d] of one type and number of tokens, d contiguous, on the frequencies' device")
+        heads = shape[1]
+        if out is None:
+            y = _kv_empty(rotary, stream, shape, kind)
+            y_token, y_head = heads * d, d
+        else:
+            y = out[i]
+            y_at = y.stride()
+            if y.shape != shape or y_at[2] != 1 or y.dtype is not kind or y.get_device() != index:
+                raise ValueError("out must be of the rows' shape, type and device, d contiguous")
+            y_token, y_head = y_at[0], y_at[1]
+        outs.append(y)
+        packed += _ROTARY_ROWS.pack(x.data_ptr(), y.data_ptr(), x_at[0], x_at[1], y_token, y_head, heads, 0)
+    s = _KV_SEQS.pack(batch, 0, 0, _kv_ints("start", start, batch, index), _kv_ints("cu", cu, batch + 1, index), tokens, max_tokens, 0)
+    rc = lib().skm_kv_rotate(s, rotary.addrs[bool(transpose)], d, dtype, packed, len(rows), _kv_stream(rotary, stream))
     if rc:
         _check(rc)
-    return out[0] if single else out
+    return outs[0] if single else tuple(outs)
