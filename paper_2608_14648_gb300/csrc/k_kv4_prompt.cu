@@ -3,10 +3,14 @@
 //
 // As k_kv_prompt.cu: a CTA takes 256 query rows of one sequence and key/value head as two tiles of 128
 // (d > 128: one), and walks the keys they see in tiles of 64 positions; softmax warps of one
-// thread a row, converter warps, one warp that issues the products.  Unlike there the converters
-// make whole keys and values, b + s c in f16 (one rounding of 2^-11), so a row's logits need one
-// factor and no block's scales: p = 2^(f S - m), l = sum p, and a tile's sum tells whether the
-// reference m has to move.
+// thread a row, converter warps, a warp for each row tile that issues its products.  Unlike there the
+// values' operand holds whole values, b + s c with one rounding to f16 (2^-11), so l = sum p, and a tile's sum of weights
+// tells whether the reference m has to move.  Keys take one of two forms.  For bf16 outputs without log-sum-exps they are rounded
+// like values, p = 2^(f S - m).  Where that rounding would show (f16 outputs 2.3 times as far from exact
+// ones as rounded exact ones, log-sum-exps off by 3e-4) the operand holds codes less 8, exact, and a key's scale
+// and bias enter its logit,
+//   t = f (s <q, c - 8> + (b + 8 s) sum q),  p = 2^(t - m),
+// two more operations a logit (prompt chunk below 360 us in place of 270; then 1.4 times and 1e-6).
 #include "skm_kv_prompt.cuh"
 
 namespace skm {
@@ -38,7 +42,8 @@ struct Lay {
     static constexpr int slots = bars + 8 * (6 * ST + 10);  // TMEM address, a flag, the part's index
     static constexpr int wild = (slots + 24 + 15) / 16 * 16;  // a byte a row: its query holds infinities or NaN
     static constexpr int there = wild + ROWS;  // a byte a block of the last INFO tiles: its page is present
-    static constexpr int scales = (there + INFO * KBLK + 63) / 64 * 64;  // [converter warp][value scales, biases of 16 tokens]
+    static constexpr int keys = (there + INFO * KBLK + 63) / 64 * 64;  // [INFO][key scale, key at code 8][64 keys]
+    static constexpr int scales = keys + INFO * 2 * KT * 4;  // [converter warp][value scales, biases of 16 tokens]
     // one CTA an SM: it takes all of TMEM
     static constexpr int bytes = scales + CONV * 64 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
     static constexpr uint32_t O = NQ * 2 * KT;  // TMEM column of O0
@@ -95,26 +100,40 @@ __device__ __forceinline__ bool warp_sleep(uint32_t b, uint32_t parity, volatile
 
 __device__ __forceinline__ __half2 h2(uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); }
 __device__ __forceinline__ uint32_t u2(__half2 x) { return *reinterpret_cast<const uint32_t *>(&x); }
-// b + s c of the codes in bits 0..3 and 16..19 of a word, or (HIGH) 4..7 and 20..23: 1024 + c (1024 + 16 c) as f16
-// bits, made c, exactly, then one rounding.  BIG: no more than f16's largest number.  The constants in registers: as immediates
-// the two of one logical operation make it two (a third of the converters' logical operations)
+// The codes in bits 0..3 and 16..19 of a word, or (HIGH) 4..7 and 20..23, from f16 bits: 1024 + c (1024 + 16 c).  The
+// constants in registers: as immediates the two of one logical operation make it two (a third of the
+// converters' logical operations)
 struct Dequant {
-    uint32_t up, down, part, less;  // f16 pairs: 1024, -1024, 1/16, -64
+    uint32_t up, down, part, less, mid, mid_part;  // f16 pairs: 1024, -1024, 1/16, -64, -1032, -72
     __device__ __forceinline__ Dequant() {
-        asm volatile("mov.b32 %0, 0x64006400;\n\tmov.b32 %1, 0xe400e400;\n\tmov.b32 %2, 0x2c002c00;\n\tmov.b32 %3, 0xd400d400;"
-                     : "=r"(up), "=r"(down), "=r"(part), "=r"(less));
+        asm volatile("mov.b32 %0, 0x64006400;\n\tmov.b32 %1, 0xe400e400;\n\tmov.b32 %2, 0x2c002c00;\n\tmov.b32 %3, 0xd400d400;\n\t"
+                     "mov.b32 %4, 0xe408e408;\n\tmov.b32 %5, 0xd480d480;"
+                     : "=r"(up), "=r"(down), "=r"(part), "=r"(less), "=r"(mid), "=r"(mid_part));
     }
-    template <bool HIGH, bool BIG>
-    __device__ __forceinline__ uint32_t two(uint32_t w, __half2 s, __half2 b) const {
+    template <bool HIGH>
+    __device__ __forceinline__ __half2 bits(uint32_t w) const {
         uint32_t x;
         asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(x) : "r"(w), "n"(HIGH ? 0x00f000f0 : 0x000f000f), "r"(up));  // and, or
-        const __half2 c = HIGH ? __hfma2(h2(x), h2(part), h2(less)) : __hadd2(h2(x), h2(down));
+        return h2(x);
+    }
+    // c - 8, exactly
+    template <bool HIGH>
+    __device__ __forceinline__ uint32_t codes(uint32_t w) const {
+        const __half2 x = bits<HIGH>(w);
+        return u2(HIGH ? __hfma2(x, h2(part), h2(mid_part)) : __hadd2(x, h2(mid)));
+    }
+    // b + s c with one rounding.  BIG: no more than f16's largest number
+    template <bool HIGH, bool BIG>
+    __device__ __forceinline__ uint32_t values(uint32_t w, __half2 s, __half2 b) const {
+        const __half2 x = bits<HIGH>(w);
+        const __half2 c = HIGH ? __hfma2(x, h2(part), h2(less)) : __hadd2(x, h2(down));
         const __half2 v = __hfma2(c, s, b);
         return u2(BIG ? __hmin2(v, h2(0x7bff7bffu)) : v);
     }
 };
 
-template <int DH>
+// EXACT: keys as codes, scales and biases in the logits; otherwise keys rounded to f16 like values
+template <int DH, bool EXACT>
 __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     kv4_prompt_kernel(const __grid_constant__ KvAttnArgs a, int splits, float *parts) {
     using L = Lay<DH>;
@@ -218,8 +237,10 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     if (warp < CONV_WARP0) {  // ------------------------------------------ softmax
         const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row, nt = tiles_for(q);
         const bool in = r < rows;
-        const float fac = load_rows<DH>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE, lane,
-                                        smem + L::wild + q * QT);
+        float row_sum = 0.0f;  // (EXACT) of the row's elements
+        const float fac = load_rows<DH, EXACT>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE, lane,
+                                              smem + L::wild + q * QT, &row_sum);
+        row_sum *= fac;
         fence_async();
         __syncwarp();
         if (lane == 0) arrive(q_full(q));
@@ -256,22 +277,43 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             };
             uint32_t P[KT / 2];
             uint64_t sum[4] = {0, 0, 0, 0};
+            // (EXACT) a key's scale and its value at code 8
+            const float *scale = reinterpret_cast<const float *>(smem + L::keys) + (j & (INFO - 1)) * 2 * KT;
             // weights of 32 logits
-            const auto weigh = [&](auto masked, const uint32_t *x, uint32_t *p, uint32_t sees) {
-                const float2 f = make_float2(fac, fac), c = make_float2(-m, -m);
+            const auto weigh = [&](auto masked, int k0, uint32_t sees) {
+                const float2 f = make_float2(fac, fac), qs = make_float2(row_sum, row_sum), c = make_float2(-m, -m);
+                float4 s4[2], b4[2];  // of four keys, read while the four before are weighed
+                if constexpr (EXACT) s4[0] = *reinterpret_cast<const float4 *>(scale + k0), b4[0] = *reinterpret_cast<const float4 *>(scale + KT + k0);
 #pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    float2 t = fma2(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), f, c);
-                    if constexpr (decltype(masked)::value) {
-                        t.x = sees & 1u << i ? t.x : -INFINITY;
-                        t.y = sees & 2u << i ? t.y : -INFINITY;
+                for (int i = k0; i < k0 + 32; i += 4) {
+                    const int now = (i >> 2) & 1;
+                    if constexpr (EXACT)
+                        if (i + 4 < k0 + 32) {
+                            s4[now ^ 1] = *reinterpret_cast<const float4 *>(scale + i + 4);
+                            b4[now ^ 1] = *reinterpret_cast<const float4 *>(scale + KT + i + 4);
+                        }
+#pragma unroll
+                    for (int k = 0; k < 4; k += 2) {
+                        const float2 x = make_float2(__uint_as_float(v[i + k]), __uint_as_float(v[i + k + 1]));
+                        float2 t;
+                        if constexpr (EXACT) {
+                            const float2 s2 = k ? make_float2(s4[now].z, s4[now].w) : make_float2(s4[now].x, s4[now].y);
+                            const float2 b2 = k ? make_float2(b4[now].z, b4[now].w) : make_float2(b4[now].x, b4[now].y);
+                            t = fma2(x, mul2(s2, f), fma2(qs, b2, c));
+                        } else {
+                            t = fma2(x, f, c);
+                        }
+                        if constexpr (decltype(masked)::value) {
+                            t.x = sees & 1u << (i + k - k0) ? t.x : -INFINITY;
+                            t.y = sees & 2u << (i + k - k0) ? t.y : -INFINITY;
+                        }
+                        P[(i + k) / 2] = weights2(t.x, t.y, sum[(i + k) / 2 & 3]);
                     }
-                    p[i / 2] = weights2(t.x, t.y, sum[i / 2 & 3]);
                 }
             };
             const auto weigh_any = [&](int k0) {
-                if (whole) weigh(std::false_type{}, v + k0, P + k0 / 2, 0u);
-                else weigh(std::true_type{}, v + k0, P + k0 / 2, visible(k0));
+                if (whole) weigh(std::false_type{}, k0, 0u);
+                else weigh(std::true_type{}, k0, visible(k0));
             };
             const auto total = [&] {
                 const float2 t = halves(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
@@ -297,7 +339,10 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     const uint32_t sees = visible(k0);
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
-                        if (sees & 1u << i) top = fmaxf(top, __uint_as_float(v[k0 + i]) * fac);
+                        if (sees & 1u << i) {
+                            const float x = __uint_as_float(v[k0 + i]);
+                            top = fmaxf(top, EXACT ? fmaf(x, scale[k0 + i] * fac, row_sum * scale[KT + k0 + i]) : x * fac);
+                        }
                 }
                 const float to = top > m + 8.0f ? top - M_BELOW : m;
                 const float g = ex2(m - to);
@@ -318,8 +363,8 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     st_wait();
                 }
                 sum[0] = sum[1] = sum[2] = sum[3] = 0;
-                weigh(std::true_type{}, v, P, visible(0));
-                weigh(std::true_type{}, v + 32, P + 16, visible(32));
+                weigh(std::true_type{}, 0, visible(0));
+                weigh(std::true_type{}, 32, visible(32));
                 add = total();
             }
             l += add;
@@ -449,8 +494,8 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     uint32_t x[8];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        x[2 * i] = dq.two<false, BIG>(c[i] >> 8 * t, s, b);
-                        x[2 * i + 1] = dq.two<true, BIG>(c[i] >> 8 * t, s, b);
+                        x[2 * i] = EXACT ? dq.codes<false>(c[i] >> 8 * t) : dq.values<false, BIG>(c[i] >> 8 * t, s, b);
+                        x[2 * i + 1] = EXACT ? dq.codes<true>(c[i] >> 8 * t) : dq.values<true, BIG>(c[i] >> 8 * t, s, b);
                     }
                     st_shared(to + k * (KT * 128) + t * 1024, x[0], x[1], x[2], x[3]);
                     st_shared((to + k * (KT * 128) + t * 1024) ^ 16, x[4], x[5], x[6], x[7]);
@@ -472,7 +517,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                         uint32_t x[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            x[i] = half ? dq.two<true, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i])) : dq.two<false, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i]));
+                            x[i] = half ? dq.values<true, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i])) : dq.values<false, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i]));
                         st_shared((to + k * 8192 + t * 1024) ^ (16 * half), x[0], x[1], x[2], x[3]);
                     }
                 }
@@ -485,11 +530,20 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             const int j = task / KBLK, st = j % ST, blk = task & (KBLK - 1);
             if ((i & 31) == 31) cur = look(task + CONV * (1 + lane));
             const int at_next = __shfl_sync(0xffffffffu, cur, (i + 1) & 31);
-            const bool big = __any_sync(0xffffffffu, beyond(ks[0]) || beyond(ks[1]) || beyond(vs));
+            const bool big = __any_sync(0xffffffffu, beyond(vs) || (!EXACT && (beyond(ks[0]) || beyond(ks[1]))));
             const int whose = j - ST < nt0 ? ask : nq - 1;
             if (!warp_sleep(k_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
             if (lane == 0) smem[L::there + (j & (INFO - 1)) * KBLK + blk] = at >= 0;
-            if (big) keys(std::true_type{}, k_to + st * L::TILE + blk * 2048);
+            if (EXACT && lane < 8) {
+                float *scale = reinterpret_cast<float *>(smem + L::keys) + (j & (INFO - 1)) * 2 * KT + blk * KV_B + g;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const float2 sb = __half22float2(h2(ks[t]));
+                    scale[8 * t] = sb.x;
+                    scale[KT + 8 * t] = fmaf(8.0f, sb.x, sb.y);
+                }
+            }
+            if (!EXACT && big) keys(std::true_type{}, k_to + st * L::TILE + blk * 2048);
             else keys(std::false_type{}, k_to + st * L::TILE + blk * 2048);
             fence_async();
             __syncwarp();
@@ -568,11 +622,11 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     }
 }
 
-template <int DH>
+template <int DH, bool EXACT>
 cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
     static SmemLimit limit;
-    cudaError_t e = limit.launch(kv4_prompt_kernel<DH>, Lay<DH>::total, [&] {
-        kv4_prompt_kernel<DH><<<(unsigned)(p.units * p.splits), Lay<DH>::THREADS, Lay<DH>::total, st>>>(
+    cudaError_t e = limit.launch(kv4_prompt_kernel<DH, EXACT>, Lay<DH>::total, [&] {
+        kv4_prompt_kernel<DH, EXACT><<<(unsigned)(p.units * p.splits), Lay<DH>::THREADS, Lay<DH>::total, st>>>(
             a, p.splits, p.splits > 1 ? a.part_cta : nullptr);
     });
     if (e != cudaSuccess || p.splits == 1) return e;
@@ -582,7 +636,10 @@ cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t 
 }  // namespace
 
 cudaError_t launch_kv4_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
-    return a.d <= 64 ? run_prompt<64>(a, p, st) : a.d <= 128 ? run_prompt<128>(a, p, st) : run_prompt<256>(a, p, st);
+    // bf16 outputs hide the rounding of keys (both 1.7e-3 off); f16 ones and log-sum-exps would show it
+    if (a.dtype == SKM_DTYPE_BF16 && !a.lse)
+        return a.d <= 64 ? run_prompt<64, false>(a, p, st) : a.d <= 128 ? run_prompt<128, false>(a, p, st) : run_prompt<256, false>(a, p, st);
+    return a.d <= 64 ? run_prompt<64, true>(a, p, st) : a.d <= 128 ? run_prompt<128, true>(a, p, st) : run_prompt<256, true>(a, p, st);
 }
 
 }  // namespace skm

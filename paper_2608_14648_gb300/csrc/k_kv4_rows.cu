@@ -8,8 +8,11 @@
 //   o = sum e s_v c + sum e b_v,   l = sum e:
 // the codes are multiplied as they are, scales and biases cost a few operations a
 // token and row.  In the 16-bit form the value scale enters the logits as log2 s_v (as in
-// k_kv_rows.cu: the weights that become f16 then are e s_v, kept below 2^15 by the
-// reference m), l = sum p / s_v and the biases' sum is sum p (b_v / s_v) in fp32.
+// k_kv_rows.cu: the weights that become f16 then are p = e s_v, kept below 2^15 by the
+// reference m) and l = sum p / s_v in fp32.  The rounding of p to f16 is an error of the codes' size, so
+// o = sum p (c - 8) + sum p (b_v / s_v + 8): the first sum from products of rounded weights p' (with one more product,
+// by ones, for 8 sum p'), the second in fp32 from the weights themselves.  (With codes 0..15 in the first, 262151 keys'
+// mean was off by 1.1e-3 of itself in f16, now 2.5e-4.)
 //
 // A code as an operand of the tensor cores costs half an instruction: four bits under a mask
 // are the f16 numbers 2^-24 c (bits 0..3) or 2^-20 c (bits 4..7), subnormal and
@@ -200,6 +203,7 @@ __device__ __forceinline__ void codes4_a(uint32_t w, uint32_t (&a)[4]) {
     a[3] = w & 0x00f000f0u;
 }
 constexpr float CODES_UP = 16777216.0f;   // 2^24
+constexpr float MIDDLE = 8.0f;
 constexpr float SCALE_LEAST = 5.9604645e-8f;  // 2^-24, the smallest f16 above 0: a scale of 0 (then all codes are 0) counts as it
 
 // Rows of one warp on tensor cores, transposed as in k_kv_rows.cu: S^T = K q^T and o^T =
@@ -347,7 +351,7 @@ struct MmaRows4 {
                 float lv;
                 asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lv) : "f"(v));
                 asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(iv[n][k]) : "f"(v));
-                bv[n][k] = sc.vb * iv[n][k];
+                bv[n][k] = fmaf(sc.vb, iv[n][k], MIDDLE);
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -419,6 +423,13 @@ struct MmaRows4 {
                 const __half2 lo = __floats2half2_rn(p[n][t][0], p[n][t][1]), hi = __floats2half2_rn(p[n][t][2] * 0.0625f, p[n][t][3] * 0.0625f);
                 pb[n][t][0] = transpose8x8(*reinterpret_cast<const uint32_t *>(&lo));
                 pb[n][t][1] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hi));
+                // codes around their middle: less its share of the weights as the products have them (every row of the
+                // product is their sum, and ob is summed over the 8 lanes of a column)
+                float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                const uint32_t ones[4] = {0x00010001u, 0x00010001u, 0x00100010u, 0x00100010u};
+                mma16816(z, ones, pb[n][t][0], pb[n][t][1]);
+                ob[t][0] = fmaf(z[0], -MIDDLE / 8 * CODES_UP, ob[t][0]);
+                ob[t][1] = fmaf(z[1], -MIDDLE / 8 * CODES_UP, ob[t][1]);
             }
 #pragma unroll
         for (int w0 = 0; w0 < DC; w0 += 4) {

@@ -167,9 +167,10 @@ __device__ __forceinline__ uint32_t bf16_f16(uint32_t w, float mul) {
 // tile's row 0, row0: the warp's first row of it.  Infinities and NaN enter as zeros (with their neighbours)
 // and are noted in `wild`, a byte a row of the tile: such a row becomes NaN at the end if it has seen a key.  (An
 // absent block's keys are zeros here: their products would be NaN where the row sees nothing.)
-template <int DH>
+// SUM: row `lane`'s sum as the operand has it, too.
+template <int DH, bool SUM = false>
 __device__ __forceinline__ float load_rows(const KvAttnArgs &a, const Seq &s, int h, int tile0, int row0, uint32_t tile, int lane,
-                                            uint8_t *wild) {
+                                            uint8_t *wild, float *sum = nullptr) {
     constexpr int LPR = DH / 8, RPI = 32 / LPR, IT = 32 / RPI, AT_ONCE = IT < 16 ? IT : 16;
     const int li = lane % LPR, sub = lane / LPR;
     float fac = a.scale_log2;
@@ -218,6 +219,19 @@ __device__ __forceinline__ float load_rows(const KvAttnArgs &a, const Seq &s, in
                     w = make_uint4(0, 0, 0, 0);
                     wild[row] = 1;
                 }
+            }
+            if constexpr (SUM) {
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+                float x = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(u + k));
+                    x += y.x + y.y;
+                }
+#pragma unroll
+                for (int o = LPR / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+                x = __shfl_sync(0xffffffffu, x, (lane % RPI) * LPR);
+                if (lane / RPI == i0 + i) *sum = x;
             }
             st_shared(tile + (li >> 3) * (QT * 128) + row * 128 + (((li & 7) ^ (row & 7)) << 4), w.x, w.y, w.z, w.w);
         }

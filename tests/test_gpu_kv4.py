@@ -6,14 +6,14 @@ really holds, elementwise within
 
   u |ref| + (w + 2 e) A + n 2^-28 M,
 
-u the rounding of the output type (2^-8 bf16, 2^-11 f16, 2^-24 f32), A = sum_j p_j (|b_j| + s_j c_j) (codes and biases
-are summed apart), M the largest |b| + 15 s; w the relative error of a weight and of the sums that carry it (f16 weights:
-2^-11 and fp32 sums that tensor cores may truncate, n 2^-23; the value scales' approximate logarithm and
-reciprocal, 2^-20; f32: n + 16 roundings of 2^-24), e the error of a logit: fp32 products of d terms in any order,
-(d + 16) 2^-23 scale sum |q| (|b| + s c), plus 2^-22 |logit| for the base-2 form.  The last term covers weights that
+u the rounding of the output type (2^-8 bf16, 2^-11 f16, 2^-24 f32), A = sum_j p_j (|b_j| + s_j (c_j + 16)) (codes less 8 and
+values at code 8, or codes and biases, are summed apart: s |c - 8| + |b + 8 s| at most), M the largest |b| + 15 s; w the relative error of a weight
+and of the sums that carry it (f16 weights: 2^-11 and fp32 sums that tensor cores may truncate, n 2^-23; the value scales'
+approximate logarithm and reciprocal, 2^-20; f32: n + 16 roundings of 2^-24), e the error of a logit: fp32 products of d terms in
+any order, (d + 16) 2^-23 scale sum |q| (|b| + s (c + 16)), plus 2^-22 |logit| for the base-2 form.  The last term covers weights that
 underflow in f16: of half a block's tokens the weight is held divided by 16, so it is off by at most 2^-21 (half of f16's smallest
-step, 2^-25, times 16), its code at most 15, and the row's largest weight times scale at least 2^7.  Kernels for many rows take keys
-and values as f16: with `rounded`, 2^-11 of a key's and a value's size (2^-25 where they are subnormal) on top.  lse: e and
+step, 2^-25, times 16), its code at most 15, and the row's largest weight times scale at least 2^7.  The kernel for many rows takes
+values as f16: with `rounded`, 2^-11 of a value's size (2^-25 where it is subnormal) on top.  lse: e and
 2^-22 of its size, and the sums' error w without the f16 weights' 2^-11 (sums are of the weights in fp32)."""
 import math
 
@@ -86,7 +86,7 @@ class Held4:
                     self.scale[pg, :, p % self.page, 2 * t + 1] = bias
 
     def values(self, t, table, b, lo, hi):
-        """float64 values [hi - lo, heads, d] of keys (0) or values (1), zeros where the page is absent; |b| + s c; s; which are there."""
+        """float64 values [hi - lo, heads, d] of keys (0) or values (1), zeros where the page is absent; |b| + s (c + 16); s; which are there."""
         val = np.zeros((hi - lo, self.heads, self.d))
         size, step = np.zeros_like(val), np.zeros((hi - lo, self.heads))
         there = np.zeros(hi - lo, bool)
@@ -98,7 +98,7 @@ class Held4:
             at, to = slice(a - p * self.page, z - p * self.page), slice(a - lo, z - lo)
             s, o = (self.scale[pg, :, at, 2 * t + i].astype(np.float64).T[..., None] for i in (0, 1))
             c = self.code[t][pg, :, at].transpose(1, 0, 2)
-            val[to], size[to], step[to], there[to] = o + s * c, abs(o) + s * c, s[..., 0], True
+            val[to], size[to], step[to], there[to] = o + s * c, abs(o) + s * (c + 16), s[..., 0], True
         return (torch.from_numpy(x) for x in (val, size, step, there))
 
     def read(self, t, table, b, lo, hi):
@@ -393,8 +393,6 @@ def attend_ref(held, table, length, cu, Q, group, scale, causal, window, typ, ro
             most = lambda k: (abs(scale) * (q.abs() @ k.T)).masked_fill(~see, 0).amax(1)  # noqa: E731
             big = S.abs().masked_fill(~see, 0).amax(1)
             e = (d + 16) * 2.0**-23 * most(K_size[:, kv]) + 2.0**-22 * big
-            if rounded:
-                e = e + most(2.0**-11 * K[:, kv].abs() + 2.0**-25)
             l = torch.logsumexp(S, 1)
             w = torch.where(any_[:, None], torch.exp(S - l[:, None]), torch.zeros((), dtype=torch.float64)).nan_to_num()
             o, A = w @ V[:, kv], w @ V_size[:, kv]
