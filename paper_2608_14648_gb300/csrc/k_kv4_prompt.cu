@@ -22,30 +22,37 @@ constexpr float TILE_MOST = 65000.0f;  // a tile's sum of weights: above it one 
 // when their softmax has handed over the tile two before: tile j + ST comes while it reads tile j - 1 at the earliest, 5 behind
 constexpr int INFO = 8;
 
+// The forms that keys take (above)
+enum Keys { ROUNDED, SPLIT, SCALED };
+
 // DH: dims, padded to 64, 128 or 256
-template <int DH>
+template <int DH, Keys KEYS>
 struct Lay {
     static constexpr int NQ = DH <= 128 ? 2 : 1;      // row tiles of a CTA
-    static constexpr int ST = DH <= 128 ? 4 : 2;      // K and V tiles in flight
+    static constexpr int ST = DH == 64 || (DH == 128 && KEYS != SPLIT) ? 4 : 2;  // K and V tiles in flight
     static constexpr int ROWS = NQ * QT;
     // converter warps.  A barrier's parity tells a phase from the next one only, so a warp may not come to a stage two rounds
     // early: from a task to its next one it goes on by no more stages than there are, and for the first one it has
-    // waited until its stage was free
-    static constexpr int CONV = NQ == 2 ? 10 : 7;
-    static_assert((CONV + KBLK - 1) / KBLK <= ST);
+    // waited until its stage was free.  (And no fewer than two stages: a warp's values of tile j would wait for the product
+    // of tile j - 1, that one for the keys of tile j + 1, which come after.)
+    static constexpr int CONV = NQ == 1 ? 7 : ST == 4 ? 10 : 6;
+    static_assert(ST >= 2 && (CONV + KBLK - 1) / KBLK <= ST);
     static constexpr int CONV_WARP0 = 4 * NQ, MMA_WARP = CONV_WARP0 + CONV, THREADS = 32 * (MMA_WARP + NQ);
-    // two row tiles: registers of a softmax thread and of the others, no more in all than the 96 each that the launch comes with
-    static constexpr int SOFT_REGS = 144, REST_REGS = 64;
+    // two row tiles: registers of a softmax thread and of the others, no more in all than the 96 or 128 each that the launch comes with
+    static constexpr int SOFT_REGS = THREADS == 640 ? 144 : 168, REST_REGS = THREADS == 640 ? 64 : 88;
     static_assert(NQ == 1 || CONV_WARP0 * SOFT_REGS + (THREADS / 32 - CONV_WARP0) * REST_REGS <= THREADS / 32 * (65536 / THREADS / 8 * 8));
-    static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
-    static constexpr int q = 0, k = NQ * QTILE, v = k + ST * TILE, bars = v + ST * TILE;
+    static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a V tile
+    // SPLIT: a row's sum beside Q, a key's rests and its bias beside it, in 16 of 64 dims
+    static constexpr int QMORE = KEYS == SPLIT ? QT * 128 : 0, KTILE = KEYS == SPLIT ? 2 * TILE + KT * 128 : TILE;
+    static constexpr int q = 0, more = NQ * QTILE, k = more + NQ * QMORE, v = k + ST * KTILE, bars = v + ST * TILE;
     static constexpr int slots = bars + 8 * (6 * ST + 10);  // TMEM address, a flag, the part's index
     static constexpr int wild = (slots + 24 + 15) / 16 * 16;  // a byte a row: its query holds infinities or NaN
     static constexpr int there = wild + ROWS;  // a byte a block of the last INFO tiles: its page is present
-    static constexpr int keys = (there + INFO * KBLK + 63) / 64 * 64;  // [INFO][key scale, key at code 8][64 keys]
-    static constexpr int scales = keys + INFO * 2 * KT * 4;  // [converter warp][value scales, biases of 16 tokens]
+    static constexpr int keys = (there + INFO * KBLK + 63) / 64 * 64;  // (SCALED) [INFO][key scale, key at code 8][64 keys]
+    static constexpr int scales = keys + (KEYS == SCALED ? INFO * 2 * KT * 4 : 0);  // [converter warp][value scales, biases of 16 tokens]
     // one CTA an SM: it takes all of TMEM
     static constexpr int bytes = scales + CONV * 64 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
+    static_assert(total <= 227 * 1024);
     static constexpr uint32_t O = NQ * 2 * KT;  // TMEM column of O0
 };
 
@@ -132,11 +139,10 @@ struct Dequant {
     }
 };
 
-// EXACT: keys as codes, scales and biases in the logits; otherwise keys rounded to f16 like values
-template <int DH, bool EXACT>
-__global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
+template <int DH, Keys KEYS>
+__global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
     kv4_prompt_kernel(const __grid_constant__ KvAttnArgs a, int splits, float *parts) {
-    using L = Lay<DH>;
+    using L = Lay<DH, KEYS>;
     constexpr int ST = L::ST, CONV = L::CONV, ROWS = L::ROWS, CONV_WARP0 = L::CONV_WARP0, MMA_WARP = L::MMA_WARP, THREADS = L::THREADS;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     // (a warp's number from one lane: the issuing warps' operands then are in uniform registers)
@@ -217,7 +223,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         *gone = 0;
     }
     if (a.d < DH) {  // dims from d on are zeros
-        for (int i = tid * 16; i < 2 * ST * L::TILE; i += THREADS * 16) st_shared(sm + L::k + i, 0, 0, 0, 0);
+        for (int i = tid * 16; i < ST * (L::KTILE + L::TILE); i += THREADS * 16) st_shared(sm + L::k + i, 0, 0, 0, 0);
         fence_async();
     }
     if (warp == MMA_WARP) {
@@ -237,9 +243,16 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     if (warp < CONV_WARP0) {  // ------------------------------------------ softmax
         const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row, nt = tiles_for(q);
         const bool in = r < rows;
-        float row_sum = 0.0f;  // (EXACT) of the row's elements
-        const float fac = load_rows<DH, EXACT>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE, lane,
-                                              smem + L::wild + q * QT, &row_sum);
+        // SPLIT: rows of at most 2^7, so that their sums are f16's
+        float row_sum = 0.0f;
+        const float fac = load_rows<DH, KEYS != ROUNDED, KEYS == SPLIT ? 6 : 15>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE,
+                                                                                 lane, smem + L::wild + q * QT, &row_sum);
+        if constexpr (KEYS == SPLIT) {  // the sum in two f16, three times each, for (b, 4 s, 4 s) of a key twice
+            const __half top = __float2half_rn(row_sum), rest = __float2half_rn(row_sum - __half2float(top));
+            const uint32_t to = sm + L::more + q * L::QMORE + row * 128;
+            st_shared(to + ((row & 7) << 4), u2(__halves2half2(top, top)), u2(__halves2half2(top, rest)), u2(__halves2half2(rest, rest)), 0);
+            st_shared(to + ((1 ^ (row & 7)) << 4), 0, 0, 0, 0);
+        }
         row_sum *= fac;
         fence_async();
         __syncwarp();
@@ -277,17 +290,17 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             };
             uint32_t P[KT / 2];
             uint64_t sum[4] = {0, 0, 0, 0};
-            // (EXACT) a key's scale and its value at code 8
+            // (SCALED) a key's scale and its value at code 8
             const float *scale = reinterpret_cast<const float *>(smem + L::keys) + (j & (INFO - 1)) * 2 * KT;
             // weights of 32 logits
             const auto weigh = [&](auto masked, int k0, uint32_t sees) {
                 const float2 f = make_float2(fac, fac), qs = make_float2(row_sum, row_sum), c = make_float2(-m, -m);
                 float4 s4[2], b4[2];  // of four keys, read while the four before are weighed
-                if constexpr (EXACT) s4[0] = *reinterpret_cast<const float4 *>(scale + k0), b4[0] = *reinterpret_cast<const float4 *>(scale + KT + k0);
+                if constexpr (KEYS == SCALED) s4[0] = *reinterpret_cast<const float4 *>(scale + k0), b4[0] = *reinterpret_cast<const float4 *>(scale + KT + k0);
 #pragma unroll
                 for (int i = k0; i < k0 + 32; i += 4) {
                     const int now = (i >> 2) & 1;
-                    if constexpr (EXACT)
+                    if constexpr (KEYS == SCALED)
                         if (i + 4 < k0 + 32) {
                             s4[now ^ 1] = *reinterpret_cast<const float4 *>(scale + i + 4);
                             b4[now ^ 1] = *reinterpret_cast<const float4 *>(scale + KT + i + 4);
@@ -296,7 +309,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     for (int k = 0; k < 4; k += 2) {
                         const float2 x = make_float2(__uint_as_float(v[i + k]), __uint_as_float(v[i + k + 1]));
                         float2 t;
-                        if constexpr (EXACT) {
+                        if constexpr (KEYS == SCALED) {
                             const float2 s2 = k ? make_float2(s4[now].z, s4[now].w) : make_float2(s4[now].x, s4[now].y);
                             const float2 b2 = k ? make_float2(b4[now].z, b4[now].w) : make_float2(b4[now].x, b4[now].y);
                             t = fma2(x, mul2(s2, f), fma2(qs, b2, c));
@@ -341,7 +354,7 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     for (int i = 0; i < 32; ++i)
                         if (sees & 1u << i) {
                             const float x = __uint_as_float(v[k0 + i]);
-                            top = fmaxf(top, EXACT ? fmaf(x, scale[k0 + i] * fac, row_sum * scale[KT + k0 + i]) : x * fac);
+                            top = fmaxf(top, KEYS == SCALED ? fmaf(x, scale[k0 + i] * fac, row_sum * scale[KT + k0 + i]) : x * fac);
                         }
                 }
                 const float to = top > m + 8.0f ? top - M_BELOW : m;
@@ -473,9 +486,9 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         int at = __shfl_sync(0xffffffffu, cur, 0);
         load_keys(at, cw);
         load_values(at, cw);
-        const auto beyond = [](uint32_t sb) {  // b + 15 s above f16's largest number
+        const auto beyond = [](uint32_t sb) {  // b + 15 s or 8 s above f16's largest number
             const float2 x = __half22float2(h2(sb));
-            return fmaf(15.0f, x.x, x.y) > 65504.0f;
+            return fmaxf(fmaf(15.0f, x.x, x.y), 8.0f * x.x) > 65504.0f;
         };
         const Dequant dq;
         // keys: vector (chunk w, g): tokens g and g + 8, 16 dims each: two 16-byte chunks of an operand row of 64
@@ -494,8 +507,25 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     uint32_t x[8];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        x[2 * i] = EXACT ? dq.codes<false>(c[i] >> 8 * t) : dq.values<false, BIG>(c[i] >> 8 * t, s, b);
-                        x[2 * i + 1] = EXACT ? dq.codes<true>(c[i] >> 8 * t) : dq.values<true, BIG>(c[i] >> 8 * t, s, b);
+                        if constexpr (KEYS == ROUNDED) {
+                            x[2 * i] = dq.values<false, BIG>(c[i] >> 8 * t, s, b);
+                            x[2 * i + 1] = dq.values<true, BIG>(c[i] >> 8 * t, s, b);
+                        } else {
+                            x[2 * i] = dq.codes<false>(c[i] >> 8 * t);
+                            x[2 * i + 1] = dq.codes<true>(c[i] >> 8 * t);
+                        }
+                    }
+                    if constexpr (KEYS == SPLIT) {  // s (c - 8) in f16, and what its rounding left (s c at most twice f16's range)
+                        uint32_t rest[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            __half2 y = __hmul2(h2(x[i]), s);
+                            if constexpr (BIG) y = __hmax2(__hmin2(y, h2(0x7bff7bffu)), h2(0xfbfffbffu));
+                            rest[i] = u2(__hfma2(h2(x[i]), s, __hneg2(y)));
+                            x[i] = u2(y);
+                        }
+                        st_shared(to + L::TILE + k * (KT * 128) + t * 1024, rest[0], rest[1], rest[2], rest[3]);
+                        st_shared((to + L::TILE + k * (KT * 128) + t * 1024) ^ 16, rest[4], rest[5], rest[6], rest[7]);
                     }
                     st_shared(to + k * (KT * 128) + t * 1024, x[0], x[1], x[2], x[3]);
                     st_shared((to + k * (KT * 128) + t * 1024) ^ 16, x[4], x[5], x[6], x[7]);
@@ -530,11 +560,18 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
             const int j = task / KBLK, st = j % ST, blk = task & (KBLK - 1);
             if ((i & 31) == 31) cur = look(task + CONV * (1 + lane));
             const int at_next = __shfl_sync(0xffffffffu, cur, (i + 1) & 31);
-            const bool big = __any_sync(0xffffffffu, beyond(vs) || (!EXACT && (beyond(ks[0]) || beyond(ks[1]))));
+            const bool big = __any_sync(0xffffffffu, beyond(vs) || (KEYS != SCALED && (beyond(ks[0]) || beyond(ks[1]))));
             const int whose = j - ST < nt0 ? ask : nq - 1;
             if (!warp_sleep(k_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
             if (lane == 0) smem[L::there + (j & (INFO - 1)) * KBLK + blk] = at >= 0;
-            if (EXACT && lane < 8) {
+            if (KEYS == SPLIT && lane < KV_B) {  // (b, 4 s, 4 s) twice: eight s, but in f16's range
+                const __half2 sb = h2(ks[lane >> 3]);
+                const __half b = __high2half(sb), s4 = __hmul(__low2half(sb), __ushort_as_half(0x4400));
+                const uint32_t to = sm + L::k + st * L::KTILE + 2 * L::TILE + (blk * KV_B + lane) * 128;
+                st_shared(to + ((lane & 7) << 4), u2(__halves2half2(b, s4)), u2(__halves2half2(s4, b)), u2(__halves2half2(s4, s4)), 0);
+                st_shared(to + ((1 ^ (lane & 7)) << 4), 0, 0, 0, 0);
+            }
+            if (KEYS == SCALED && lane < 8) {
                 float *scale = reinterpret_cast<float *>(smem + L::keys) + (j & (INFO - 1)) * 2 * KT + blk * KV_B + g;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -543,8 +580,8 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
                     scale[KT + 8 * t] = fmaf(8.0f, sb.x, sb.y);
                 }
             }
-            if (!EXACT && big) keys(std::true_type{}, k_to + st * L::TILE + blk * 2048);
-            else keys(std::false_type{}, k_to + st * L::TILE + blk * 2048);
+            if (KEYS != SCALED && big) keys(std::true_type{}, k_to + st * L::KTILE + blk * 2048);
+            else keys(std::false_type{}, k_to + st * L::KTILE + blk * 2048);
             fence_async();
             __syncwarp();
             if (j < 2) {
@@ -580,12 +617,19 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
         const uint32_t S = tmem + 2 * q * KT, O = tmem + L::O + q * DH;
         const auto qk = [&](int j) {
             const uint32_t d = S + (j & 1) * KT;
-            const uint64_t ka = k_op + (uint32_t)(j % ST) * (L::TILE >> 4);
-            mma_ss<false>(d, q_op, ka, idesc(KT), one);
+            const uint64_t ka = k_op + (uint32_t)(j % ST) * (L::KTILE >> 4);
+            const auto dims = [&](auto add, uint64_t kb) {
+                mma_ss<decltype(add)::value>(d, q_op, kb, idesc(KT), one);
 #pragma unroll
-            for (int k = 1; k < DH / 16; ++k)
-                mma_ss<true>(d, q_op + ((k >> 2) * (QT * 128 >> 4) + 2 * (k & 3)), ka + ((k >> 2) * (KT * 128 >> 4) + 2 * (k & 3)),
-                             idesc(KT), one);
+                for (int k = 1; k < DH / 16; ++k)
+                    mma_ss<true>(d, q_op + ((k >> 2) * (QT * 128 >> 4) + 2 * (k & 3)), kb + ((k >> 2) * (KT * 128 >> 4) + 2 * (k & 3)),
+                                 idesc(KT), one);
+            };
+            dims(std::false_type{}, ka);
+            if constexpr (KEYS == SPLIT) {
+                dims(std::true_type{}, ka + (L::TILE >> 4));
+                mma_ss<true>(d, operand(sm + L::more + q * L::QMORE), ka + (2 * L::TILE >> 4), idesc(KT), one);
+            }
             issued = true;
             commit(k_free(q, j % ST), one);
         };
@@ -622,15 +666,15 @@ __global__ void __launch_bounds__(Lay<DH>::THREADS, 1)
     }
 }
 
-template <int DH, bool EXACT>
+template <int DH, Keys KEYS>
 cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
     static SmemLimit limit;
-    cudaError_t e = limit.launch(kv4_prompt_kernel<DH, EXACT>, Lay<DH>::total, [&] {
-        kv4_prompt_kernel<DH, EXACT><<<(unsigned)(p.units * p.splits), Lay<DH>::THREADS, Lay<DH>::total, st>>>(
+    cudaError_t e = limit.launch(kv4_prompt_kernel<DH, KEYS>, Lay<DH, KEYS>::total, [&] {
+        kv4_prompt_kernel<DH, KEYS><<<(unsigned)(p.units * p.splits), Lay<DH, KEYS>::THREADS, Lay<DH, KEYS>::total, st>>>(
             a, p.splits, p.splits > 1 ? a.part_cta : nullptr);
     });
     if (e != cudaSuccess || p.splits == 1) return e;
-    return run_prompt_join(a, p, Lay<DH>::ROWS, st);
+    return run_prompt_join(a, p, Lay<DH, KEYS>::ROWS, st);
 }
 
 }  // namespace
@@ -638,8 +682,8 @@ cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t 
 cudaError_t launch_kv4_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st) {
     // bf16 outputs hide the rounding of keys (both 1.7e-3 off); f16 ones and log-sum-exps would show it
     if (a.dtype == SKM_DTYPE_BF16 && !a.lse)
-        return a.d <= 64 ? run_prompt<64, false>(a, p, st) : a.d <= 128 ? run_prompt<128, false>(a, p, st) : run_prompt<256, false>(a, p, st);
-    return a.d <= 64 ? run_prompt<64, true>(a, p, st) : a.d <= 128 ? run_prompt<128, true>(a, p, st) : run_prompt<256, true>(a, p, st);
+        return a.d <= 64 ? run_prompt<64, ROUNDED>(a, p, st) : a.d <= 128 ? run_prompt<128, ROUNDED>(a, p, st) : run_prompt<256, ROUNDED>(a, p, st);
+    return a.d <= 64 ? run_prompt<64, SPLIT>(a, p, st) : a.d <= 128 ? run_prompt<128, SPLIT>(a, p, st) : run_prompt<256, SCALED>(a, p, st);
 }
 
 }  // namespace skm

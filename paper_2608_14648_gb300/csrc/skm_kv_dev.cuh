@@ -105,8 +105,8 @@ __device__ __forceinline__ float4 value_scale(float2 sc) {
 struct Pow2 {
     float mul, back;
 };
-__device__ __forceinline__ Pow2 to_f16(uint32_t ex) {
-    const uint32_t e = max(ex, 1u), up = min(e - 1u, 15u);
+__device__ __forceinline__ Pow2 to_f16(uint32_t ex, uint32_t most = 15u) {
+    const uint32_t e = max(ex, 1u), up = min(e - 1u, most);
     return Pow2{__uint_as_float((254u - e + up) << 23), __uint_as_float((e - up) << 23)};
 }
 

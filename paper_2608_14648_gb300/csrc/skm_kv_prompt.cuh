@@ -167,8 +167,9 @@ __device__ __forceinline__ uint32_t bf16_f16(uint32_t w, float mul) {
 // tile's row 0, row0: the warp's first row of it.  Infinities and NaN enter as zeros (with their neighbours)
 // and are noted in `wild`, a byte a row of the tile: such a row becomes NaN at the end if it has seen a key.  (An
 // absent block's keys are zeros here: their products would be NaN where the row sees nothing.)
-// SUM: row `lane`'s sum as the operand has it, too.
-template <int DH, bool SUM = false>
+// UP: the largest element's exponent, both types scaled (15 or less; F16 rows as they are where it is 15).  SUM: row `lane`'s sum as the
+// operand has it.
+template <int DH, bool SUM = false, uint32_t UP = 15>
 __device__ __forceinline__ float load_rows(const KvAttnArgs &a, const Seq &s, int h, int tile0, int row0, uint32_t tile, int lane,
                                             uint8_t *wild, float *sum = nullptr) {
     constexpr int LPR = DH / 8, RPI = 32 / LPR, IT = 32 / RPI, AT_ONCE = IT < 16 ? IT : 16;
@@ -198,14 +199,35 @@ __device__ __forceinline__ float load_rows(const KvAttnArgs &a, const Seq &s, in
         for (int i = 0; i < AT_ONCE; ++i) {
             const int row = row0 + (i0 + i) * RPI + sub;
             uint4 w = raw[i];
-            if (a.dtype == SKM_DTYPE_BF16) {
+            if (UP < 15 && a.dtype != SKM_DTYPE_BF16) {
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+                float2 y[4];
+                uint32_t top = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    y[k] = __half22float2(*reinterpret_cast<const __half2 *>(u + k));
+                    top = max(max(top, __float_as_uint(y[k].x) & 0x7fffffffu), __float_as_uint(y[k].y) & 0x7fffffffu);
+                }
+#pragma unroll
+                for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const Pow2 by = to_f16(top >> 23, UP);
+                if (top >= 0x7f800000u) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) y[k] = make_float2(0.0f, 0.0f);
+                    wild[row] = 1;
+                }
+                w = make_uint4(pack(y[0].x * by.mul, y[0].y * by.mul), pack(y[1].x * by.mul, y[1].y * by.mul), pack(y[2].x * by.mul, y[2].y * by.mul),
+                               pack(y[3].x * by.mul, y[3].y * by.mul));
+                const float mine = __shfl_sync(0xffffffffu, by.back, (lane % RPI) * LPR);
+                if (lane / RPI == i0 + i) fac = mine * a.scale_log2;
+            } else if (a.dtype == SKM_DTYPE_BF16) {
                 uint32_t top = 0;  // the largest |x| as bits
                 const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) top = max(max(top, u[k] << 16 & 0x7fff0000u), u[k] & 0x7fff0000u);
 #pragma unroll
                 for (int o = LPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const Pow2 by = to_f16(top >> 23);
+                const Pow2 by = to_f16(top >> 23, UP);
                 if (top >= 0x7f800000u) {
                     w = make_uint4(0, 0, 0, 0);
                     wild[row] = 1;

@@ -13,7 +13,8 @@ approximate logarithm and reciprocal, 2^-20; f32: n + 16 roundings of 2^-24), e 
 any order, (d + 16) 2^-23 scale sum |q| (|b| + s (c + 16)), plus 2^-22 |logit| for the base-2 form.  The last term covers weights that
 underflow in f16: of half a block's tokens the weight is held divided by 16, so it is off by at most 2^-21 (half of f16's smallest
 step, 2^-25, times 16), its code at most 15, and the row's largest weight times scale at least 2^7.  The kernel for many rows takes
-values as f16: with `rounded`, 2^-11 of a value's size (2^-25 where it is subnormal) on top.  lse: e and
+values as f16: with `rounded`, 2^-11 of a value's size (2^-25 where it is subnormal) on top; and for bf16 outputs without lse keys
+too: their logits are off by up to scale sum |q| (2^-11 |k| + 2^-25) more.  lse: e and
 2^-22 of its size, and the sums' error w without the f16 weights' 2^-11 (sums are of the weights in fp32)."""
 import math
 
@@ -366,12 +367,12 @@ def test_write_and_read_no_rows(cuda_ok):
 
 
 def attend_ref(held, table, length, cu, Q, group, scale, causal, window, typ, rounded):
-    """(out, lse, tolerance of out, tolerance of lse) in 64 bits."""
+    """(out, lse, tolerance of out, tolerance of lse, tolerance of out with rounded keys) in 64 bits."""
     heads, d = held.heads, held.d
     T = Q.shape[0]
     out = torch.zeros(T, heads * group, d, dtype=torch.float64)
     lse = torch.full((T, heads * group), -math.inf, dtype=torch.float64)
-    tol, ltol = torch.zeros_like(out), torch.zeros_like(lse)
+    tol, ltol, ktol = torch.zeros_like(out), torch.zeros_like(lse), torch.zeros_like(out)
     u = {"bf16": 2.0**-8, "f16": 2.0**-11, "f32": 2.0**-24}[typ]
     for b in range(table.shape[0]):
         n, L = cu[b + 1] - cu[b], length[b]
@@ -403,8 +404,10 @@ def attend_ref(held, table, length, cu, Q, group, scale, causal, window, typ, ro
                           + L * 2.0**-28 * (V_size[:, kv].amax() + 15 * V_step[:, kv].amax()))
             if rounded:
                 tol[sl, h] += 2.0**-11 * (w @ V[:, kv].abs()) + 2.0**-25
+                # exp(2 e) - 1, as these logits are off by more
+                ktol[sl, h] = tol[sl, h] + torch.expm1(2 * most(2.0**-11 * K[:, kv].abs() + 2.0**-25))[:, None] * A * 1.01
             ltol[sl, h] = e + sums + 2.0**-22 * l.abs().nan_to_num(posinf=0)
-    return out, lse, tol, ltol
+    return out, lse, tol, ltol, ktol
 
 
 def check_attend(heads, group, d, page, typ, seqs, causal=True, window=0, absent=0.0, scale=None, seed=11, spread=1.0,
@@ -446,7 +449,7 @@ def check_attend(heads, group, d, page, typ, seqs, causal=True, window=0, absent
     torch.cuda.synchronize()
     assert int(status) == 0
     rounded = typ != "f32" and (max_tokens or max(n for _, n in seqs)) * group > 32
-    out, ref, tol, ltol = attend_ref(held, table, length, cu, Q, group, d**-0.5 if scale is None else scale, causal, window, typ, rounded)
+    out, ref, tol, ltol, ktol = attend_ref(held, table, length, cu, Q, group, d**-0.5 if scale is None else scale, causal, window, typ, rounded)
     got, lse = got.cpu().double(), lse.cpu().double()
     assert torch.equal(torch.isneginf(lse), torch.isneginf(ref))
     fine = ~torch.isneginf(ref)
@@ -456,6 +459,12 @@ def check_attend(heads, group, d, page, typ, seqs, causal=True, window=0, absent
     assert over <= 0, f"out is off by {float((got - out).abs().max()):.3g}, over the bound by {float(over):.3g}"
     if fine.any():
         assert ((lse - ref).abs() - ltol)[fine].amax() <= 0
+    if rounded and typ == "bf16":  # without log-sum-exps keys may be rounded as well
+        alone, _ = skm.skm_kv4_attend(c, table.cuda(), i32(length), i32(cu), dev, max_tokens or max(n for _, n in seqs),
+                                      max(length) if max_len is None else max_len, scale=scale, causal=causal, window=window, status=status)
+        alone = alone.cpu().double()
+        assert int(status) == 0 and torch.isfinite(alone).all() and (alone[~fine] == 0).all()
+        assert ((alone - out).abs() - ktol).amax() <= 0
     return got
 
 
