@@ -5,12 +5,20 @@
 // (d > 128: one), and walks the keys they see in tiles of 64 positions; softmax warps of one
 // thread a row, converter warps, a warp for each row tile that issues its products.  Unlike there the
 // values' operand holds whole values, b + s c with one rounding to f16 (2^-11), so l = sum p, and a tile's sum of weights
-// tells whether the reference m has to move.  Keys take one of two forms.  For bf16 outputs without log-sum-exps they are rounded
-// like values, p = 2^(f S - m).  Where that rounding would show (f16 outputs 2.3 times as far from exact
-// ones as rounded exact ones, log-sum-exps off by 3e-4) the operand holds codes less 8, exact, and a key's scale
-// and bias enter its logit,
-//   t = f (s <q, c - 8> + (b + 8 s) sum q),  p = 2^(t - m),
-// two more operations a logit (prompt chunk below 360 us in place of 270; then 1.4 times and 1e-6).
+// tells whether the reference m has to move.  Keys take one of three forms:
+//   ROUNDED  like values (bf16 outputs without log-sum-exps, which do not show it): p = 2^(f S - m)
+//   SPLIT    s (c - 8) as the sum of two f16, a second operand beside the first, and b + 8 s as b + 4 s + 4 s in 16
+//            dims more, beside the row's sum in two f16: exact, for twice the products Q K' and no more softmax
+//   SCALED   (d > 128, where SPLIT has no room) codes less 8, exact, and t = f (s <q, c - 8> + (b + 8 s) sum q) in the
+//            softmax, two more operations a logit
+// Whole prompts of up to 4096, 16 heads of 64, f16: 113 us ROUNDED, 127 SPLIT, 175 SCALED; ROUNDED log-sum-exps were 2e-5
+// off and f16 outputs by more than the 1.6 times an f16 computation's error that is left (values and weights in f16).
+//
+// What bounds it: the tensor cores, and what keeps them waiting.  A tile of 128 rows and 64 keys of 128 dims takes
+// 4 MFLOP; chunks of 2048 before 16384 tokens, 32 rows heads on 8, 128 dims, bf16: 270 us, 66% of cuBLAS's bf16 rate.  A
+// step's waits were most of what could be gained: one barrier for all that its products need (299 -> 296 us), waits that
+// suspend instead of spinning in the schedulers that convert (296 -> 276), constants in registers (276 -> 270).  Exact
+// bytes are no bound: 136 a token and head of 64 dims.
 #include "skm_kv_prompt.cuh"
 
 namespace skm {
@@ -295,11 +303,11 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
             // weights of 32 logits
             const auto weigh = [&](auto masked, int k0, uint32_t sees) {
                 const float2 f = make_float2(fac, fac), qs = make_float2(row_sum, row_sum), c = make_float2(-m, -m);
-                float4 s4[2], b4[2];  // of four keys, read while the four before are weighed
+                [[maybe_unused]] float4 s4[2], b4[2];  // of four keys, read while the four before are weighed
                 if constexpr (KEYS == SCALED) s4[0] = *reinterpret_cast<const float4 *>(scale + k0), b4[0] = *reinterpret_cast<const float4 *>(scale + KT + k0);
 #pragma unroll
                 for (int i = k0; i < k0 + 32; i += 4) {
-                    const int now = (i >> 2) & 1;
+                    [[maybe_unused]] const int now = (i >> 2) & 1;
                     if constexpr (KEYS == SCALED)
                         if (i + 4 < k0 + 32) {
                             s4[now ^ 1] = *reinterpret_cast<const float4 *>(scale + i + 4);
@@ -496,7 +504,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
         const uint32_t k_to = sm + L::k + g * 128 + (((w0 & 3) * 2 ^ g) << 4);
         const uint32_t v_to = sm + L::v + (16 * w0 + g) * 128;
         const auto keys = [&](auto big, uint32_t to) {
-            constexpr bool BIG = decltype(big)::value;
+            [[maybe_unused]] constexpr bool BIG = decltype(big)::value;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 if (16 * (w0 + 4 * k) >= a.d) break;

@@ -9,16 +9,23 @@
 // the codes are multiplied as they are, scales and biases cost a few operations a
 // token and row.  In the 16-bit form the value scale enters the logits as log2 s_v (as in
 // k_kv_rows.cu: the weights that become f16 then are p = e s_v, kept below 2^15 by the
-// reference m) and l = sum p / s_v in fp32.  The rounding of p to f16 is an error of the codes' size, so
-// o = sum p (c - 8) + sum p (b_v / s_v + 8): the first sum from products of rounded weights p' (with one more product,
-// by ones, for 8 sum p'), the second in fp32 from the weights themselves.  (With codes 0..15 in the first, 262151 keys'
-// mean was off by 1.1e-3 of itself in f16, now 2.5e-4.)
+// reference m), l = sum p / s_v and the biases' sum is sum p (b_v / s_v), in fp32.
+//
+// For f16 outputs the second product has codes less 8 (and b_v / s_v + 8): the weights' rounding is an error of the
+// codes' size, and tensor cores cut their sums off, which shows where values nearly cancel (the mean of 262151 keys: 6 times
+// as far off as its rounding to f16 with codes 0..15).  bf16 outputs hide both.
 //
 // A code as an operand of the tensor cores costs half an instruction: four bits under a mask
 // are the f16 numbers 2^-24 c (bits 0..3) or 2^-20 c (bits 4..7), subnormal and
 // exact, so a word's eight codes are four operands after one shift and four masks.  The factor
 // 16 between the two lies on the other operand (half of a query's dims and half of a
 // block's weights carry 2^-4), 2^24 on the results.
+//
+// What bounds it: HBM from a batch that fills the machine on; next to it issue slots, of which a code takes half.  96
+// sequences of up to 10001 tokens, 8 heads of 128 dims, 4 query rows each, bf16: 118 us, 67% of a copy's rate (79.9 us for
+// the bytes).  Items of two blocks share masks, maxima and the walk (138 -> 129 us), queries' operands lie in shared
+// memory where registers would spill (129 -> 118).  A long sequence, f16, 262151 tokens: 66 us (42.2), of which codes
+// less 8 are 4.
 #include "skm_kv_rows.cuh"
 
 namespace skm {
@@ -34,6 +41,10 @@ __device__ __forceinline__ TokenScales token_scales(const uint8_t *rec, int d, i
     const float2 k = __half22float2(*reinterpret_cast<const __half2 *>(&w.x)), v = __half22float2(*reinterpret_cast<const __half2 *>(&w.y));
     return TokenScales{k.x, k.y, v.x, v.y};
 }
+
+constexpr float MIDDLE = 8.0f;
+// the code in bits 0..3, less 8
+__device__ __forceinline__ float code(uint32_t u) { return __uint_as_float((u & 15u) | 0x4b000000u) - (8388608.0f + MIDDLE); }
 
 // Rows of one warp in fp32 on CUDA cores.  Scores: lane = (half, token), a half takes every
 // other 16-dim chunk of the keys; sums: lane = dims lane, lane + 32, ...  q and the
@@ -81,6 +92,7 @@ struct Fp32Rows4 {
         const int t = lane & 15, half = lane >> 4, nc = a.d / KV_B;
         const uint8_t *K = rec, *V = rec + 8 * a.d;
         TokenScales sc = token_scales(rec, a.d, t);
+        sc.kb = fmaf(MIDDLE, sc.ks, sc.kb), sc.vb = fmaf(MIDDLE, sc.vs, sc.vb);  // codes around their middle: smaller sums
         float x[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) x[r] = 0.0f;
@@ -90,7 +102,7 @@ struct Fp32Rows4 {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t u = word[i] >> (t & 8);  // codes of the token's dims 4 i, + 2, . , . , + 1, + 3
-                const float k0 = (float)(u & 15), k2 = (float)(u >> 4 & 15), k1 = (float)(u >> 16 & 15), k3 = (float)(u >> 20 & 15);
+                const float k0 = code(u), k2 = code(u >> 4), k1 = code(u >> 16), k3 = code(u >> 20);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const float4 qq = *reinterpret_cast<const float4 *>(q + r * a.d + 16 * w + 4 * i);
@@ -143,7 +155,7 @@ struct Fp32Rows4 {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 const uint32_t u = word[w] >> (dim & 8);  // codes of tokens 2 w, + 8, . , . , + 1, + 9
-                const float v0 = (float)(u & 15), v8 = (float)(u >> 4 & 15), v1 = (float)(u >> 16 & 15), v9 = (float)(u >> 20 & 15);
+                const float v0 = code(u), v8 = code(u >> 4), v1 = code(u >> 16), v9 = code(u >> 20);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const float2 lo = *reinterpret_cast<const float2 *>(p + r * KV_B + 2 * w);
@@ -203,7 +215,26 @@ __device__ __forceinline__ void codes4_a(uint32_t w, uint32_t (&a)[4]) {
     a[3] = w & 0x00f000f0u;
 }
 constexpr float CODES_UP = 16777216.0f;   // 2^24
-constexpr float MIDDLE = 8.0f;
+// the same codes less 8, exact, from the f16 numbers 1024 + c and 1024 + 16 c (up: 1024 twice, in a register: with two
+// immediates the logical operation would be two)
+__device__ __forceinline__ void codes4_mid(uint32_t w, uint32_t up, uint32_t (&a)[4]) {
+    const auto half2 = [](uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); };
+    const auto low = [&](uint32_t x) {
+        uint32_t y;
+        asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(y) : "r"(x), "r"(up));  // and, or
+        const __half2 r = __hadd2(half2(y), half2(0xe408e408u));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    };
+    const auto high = [&](uint32_t x) {
+        uint32_t y;
+        asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xea;" : "=r"(y) : "r"(x), "r"(up));
+        const __half2 r = __hfma2(half2(y), half2(0x2c002c00u), half2(0xd480d480u));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    };
+    a[0] = low(w), a[2] = high(w);
+    w >>= 8;
+    a[1] = low(w), a[3] = high(w);
+}
 constexpr float SCALE_LEAST = 5.9604645e-8f;  // 2^-24, the smallest f16 above 0: a scale of 0 (then all codes are 0) counts as it
 
 // Rows of one warp on tensor cores, transposed as in k_kv_rows.cu: S^T = K q^T and o^T =
@@ -223,8 +254,10 @@ struct MmaRows4 {
     uint32_t q[QMEM ? 1 : NT][QMEM ? 1 : DC][2];
     uint2 *qmem;
     int2 *lim;
+    bool fine;  // f16 outputs
 
     __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int h, int r0, uint8_t *mem, int lane) {
+        fine = a.dtype == SKM_DTYPE_F16;
         const int g = lane >> 2, c = lane & 3, nc = FULL ? DC : a.d / KV_B;
         lim = reinterpret_cast<int2 *>(mem);
         qmem = reinterpret_cast<uint2 *>(mem + LIMITS<RT>);
@@ -351,7 +384,7 @@ struct MmaRows4 {
                 float lv;
                 asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lv) : "f"(v));
                 asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(iv[n][k]) : "f"(v));
-                bv[n][k] = fmaf(sc.vb, iv[n][k], MIDDLE);
+                bv[n][k] = fmaf(sc.vb, iv[n][k], fine ? MIDDLE : 0.0f);
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -420,37 +453,39 @@ struct MmaRows4 {
                     l[t][i] = fmaf(p[n][t][i + 2], iv[n][1], fmaf(p[n][t][i], iv[n][0], l[t][i]));
                     ob[t][i] = fmaf(p[n][t][i + 2], bv[n][1], fmaf(p[n][t][i], bv[n][0], ob[t][i]));
                 }
-                const __half2 lo = __floats2half2_rn(p[n][t][0], p[n][t][1]), hi = __floats2half2_rn(p[n][t][2] * 0.0625f, p[n][t][3] * 0.0625f);
+                const float down = fine ? 1.0f : 0.0625f;
+                const __half2 lo = __floats2half2_rn(p[n][t][0], p[n][t][1]), hi = __floats2half2_rn(p[n][t][2] * down, p[n][t][3] * down);
                 pb[n][t][0] = transpose8x8(*reinterpret_cast<const uint32_t *>(&lo));
                 pb[n][t][1] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hi));
-                // codes around their middle: less its share of the weights as the products have them (every row of the
-                // product is their sum, and ob is summed over the 8 lanes of a column)
-                float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                const uint32_t ones[4] = {0x00010001u, 0x00010001u, 0x00100010u, 0x00100010u};
-                mma16816(z, ones, pb[n][t][0], pb[n][t][1]);
-                ob[t][0] = fmaf(z[0], -MIDDLE / 8 * CODES_UP, ob[t][0]);
-                ob[t][1] = fmaf(z[1], -MIDDLE / 8 * CODES_UP, ob[t][1]);
             }
+        uint32_t up;
+        asm volatile("mov.b32 %0, 0x64006400;" : "=r"(up));
+        const auto sums = [&](auto exact) {
 #pragma unroll
-        for (int w0 = 0; w0 < DC; w0 += 4) {
-            if (w0 >= nc) break;
-            uint32_t r[NB][4], f[4];
+            for (int w0 = 0; w0 < DC; w0 += 4) {
+                if (w0 >= nc) break;
+                uint32_t r[NB][4], f[4];
 #pragma unroll
-            for (int n = 0; n < NB; ++n) ldsm4(va + n * bytes + w0 * 128, r[n]);
+                for (int n = 0; n < NB; ++n) ldsm4(va + n * bytes + w0 * 128, r[n]);
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+                for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int w = w0 + i;
-                    if (w >= DC || w >= nc) break;
-                    codes4_a(r[n][i], f);
+                    for (int i = 0; i < 4; ++i) {
+                        const int w = w0 + i;
+                        if (w >= DC || w >= nc) break;
+                        if constexpr (decltype(exact)::value) codes4_mid(r[n][i], up, f);
+                        else codes4_a(r[n][i], f);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) mma16816(o[t][w], f, pb[n][t][0], pb[n][t][1]);
-                }
-        }
+                        for (int t = 0; t < NT; ++t) mma16816(o[t][w], f, pb[n][t][0], pb[n][t][1]);
+                    }
+            }
+        };
+        if (fine) sums(std::true_type{});
+        else sums(std::false_type{});
     }
 
     __device__ __forceinline__ void close(int) {
+        const float up = fine ? 1.0f : CODES_UP;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -462,8 +497,8 @@ struct MmaRows4 {
                 }
 #pragma unroll
                 for (int w = 0; w < DC; ++w) {
-                    o[t][w][i] = fmaf(o[t][w][i], CODES_UP, ob[t][i]);
-                    o[t][w][i + 2] = fmaf(o[t][w][i + 2], CODES_UP, ob[t][i]);
+                    o[t][w][i] = fmaf(o[t][w][i], up, ob[t][i]);
+                    o[t][w][i + 2] = fmaf(o[t][w][i + 2], up, ob[t][i]);
                 }
             }
     }
