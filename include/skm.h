@@ -217,8 +217,8 @@ int skm_version(void); /* major*10000 + minor*100 + patch */
  *                       bounded wait on a barrier that nothing arrives on: it
  *                       gives up before loading anything, raises its abort
  *                       flag, and skm_fit reports SKM_ERR_TIMEOUT.  In
- *                       skm_kv_attend (fp32 queries, or up to 32 rows a
- *                       sequence), the first keys of one warp, numbered by
+ *                       skm_kv_attend and skm_kv4_attend (fp32 queries, or up to 32
+ *                       rows a sequence), the first keys of one warp, numbered by
  *                       the occurrences still armed, never count as arrived:
  *                       its wait ends after 1 ms and the call's status word is
  *                       set.
@@ -921,8 +921,10 @@ int skm_kv4_read(const skm_kv4_cache *c, const skm_kv_seqs *s, int dtype, void *
  * tensor cores, sums and softmax in fp32, weights rounded to f16.  Query rows become f16 by a power of two
  * a row: elements below 2^-25 (F16) or 2^-28 (BF16) of the row's largest lose bits, those below 2^-36
  * vanish.  Calls of more than 32 rows a sequence (tokens x heads of a group; d > 128: of more keys too)
- * run on another kernel, which takes keys and values rounded to f16 (2^-11 of each; b + 15 s above f16's
- * largest number as that number).  F32: fp32 arithmetic throughout.
+ * run on another kernel: it takes values rounded to f16 (2^-11 of each; b + 15 s above f16's largest number as
+ * that number), keys too where the output is BF16 and no lse is asked for; where one is, or the output is F16,
+ * and d <= 128, elements of a query row below 2^-20 (F16) or 2^-23 (BF16) of its largest lose bits and those
+ * below 2^-32 vanish.  F32: fp32 arithmetic throughout.
  * The result does not depend on timing.  Asynchronous. */
 size_t skm_kv4_attend_workspace_size(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a);
 int skm_kv4_attend(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws, size_t ws_bytes,
