@@ -11,19 +11,19 @@
 // Values: (e, c), dims 8 e .. of the four tokens 2c, 2c + 1, 2c + 8, 2c + 9 that share a word; the
 // other dims of a word are those of the lane next to it in e.
 //
-// Rounding.  q = d y, d = x - b and y the correctly rounded reciprocal of s, corrected by its exact remainder: q' = q + (d -
-// q s) y.  q' is within 2^-20 of the quotient (half a unit in the last place, and d's rounding), so its
-// nearest integer is the quotient's unless it lies within 2^-18 of the middle of two.  It often is the middle itself (16-bit
-// values, biases and scales have few bits: one value in 2500 of a bf16 input): then the
-// remainder is 0, d is exact, and half to even is right; else x - b is compared with (k + 1/2) s in 64 bits.
-// Codes become words by multiply-adds of integers as floats (below 2^16, exact), two at a time.
+// Rounding.  q = d y, d = x - b and y the correctly rounded reciprocal of s: three roundings, so q, 15 at most, is within
+// 45 2^-24 of the quotient and its nearest integer is the quotient's unless it lies within 2^-18 of the middle of two.  It
+// often is the middle itself (16-bit values, biases and scales have few bits: one value in 2500 of a bf16 input): then q
+// corrected by its remainder, q + (d - q s) y, is k + 1/2, the remainder of that is 0, d is exact, and half to even is
+// right; else x - b is compared with (k + 1/2) s in 64 bits.  2^23 + q is an integer, rounded half to even; codes become
+// words by multiply-adds of integers as floats (below 2^16 beside 2^23, exact), two at a time.
 #include "skm_kv_cache.cuh"
 
 namespace skm {
 
 namespace {
 
-constexpr float MAGIC = 12582912.0f;  // 1.5 2^23: x + this, less this, is rint(x)
+constexpr float MAGIC = 8388608.0f;  // 2^23: x + this, for x from 0 to 2^22, is rint(x) + this
 constexpr float NEAR = 0.5f - 3.8146973e-6f;  // 1/2 - 2^-18
 constexpr float F16_MOST = 65504.0f;
 
@@ -129,42 +129,46 @@ __device__ __forceinline__ bool exact_less(float x, float b, float d) {
     const float z = __fadd_rn(d, -x);
     return __fadd_rn(__fadd_rn(x, -__fadd_rn(d, -z)), __fadd_rn(-b, -z)) == 0.0f;
 }
-// codes of 8 values as floats
-template <typename T>
+// codes of 8 values as floats, pairs i with bit i of UP + 2^23
+template <int UP, typename T>
 __device__ __forceinline__ void codes8(const Eight<T> &x, const Lvq &v, float2 (&c)[4]) {
-    const float2 less = make_float2(-v.b, -v.b), by = make_float2(v.inv, v.inv), s = make_float2(-v.s, -v.s);
+    const float2 less = make_float2(-v.b, -v.b), by = make_float2(v.inv, v.inv);
     const float2 up = make_float2(MAGIC, MAGIC), down = make_float2(-MAGIC, -MAGIC);
-    const auto quotient = [&](float2 d) {
-        const float2 q = mul2(d, by);
-        return fma2(fma2(q, s, d), by, q);
-    };
     float far = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 q = quotient(add2(value2<T>(x.w, i), less));
-        c[i] = add2(add2(q, up), down);
-        far = fmaxf(far, fmaxf(fabsf(q.x - c[i].x), fabsf(q.y - c[i].y)));
+        const float2 q = mul2(add2(value2<T>(x.w, i), less), by), t = add2(q, up), n = add2(t, down);
+        const float2 off = fma2(n, make_float2(-1.0f, -1.0f), q);
+        far = fmaxf(far, fmaxf(fabsf(off.x), fabsf(off.y)));
+        c[i] = UP >> i & 1 ? t : n;
     }
     if (far <= NEAR) return;
+    // every value once more, from the corrected quotient: a middle counts where it is one exactly
+    const float2 s = make_float2(-v.s, -v.s);
     bool open = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 y = value2<T>(x.w, i), d = add2(y, less), q = quotient(d), r = fma2(q, s, d);
-        const float ex = fabsf(q.x - c[i].x), ey = fabsf(q.y - c[i].y);
+        const float2 y = value2<T>(x.w, i), d = add2(y, less), q0 = mul2(d, by), q = fma2(fma2(q0, s, d), by, q0), r = fma2(q, s, d);
+        const float2 t = add2(q, up), n = add2(t, down);
+        const float ex = fabsf(q.x - n.x), ey = fabsf(q.y - n.y);
         open = open || (ex > NEAR && !(ex == 0.5f && r.x == 0.0f && exact_less(y.x, v.b, d.x)));
         open = open || (ey > NEAR && !(ey == 0.5f && r.y == 0.0f && exact_less(y.y, v.b, d.y)));
+        c[i] = UP >> i & 1 ? t : n;
     }
     if (open) {
         const uint32_t n = codes8_near<T>(x, v.b, v.s, v.inv);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = make_float2((float)(n >> (8 * i) & 15), (float)(n >> (8 * i + 4) & 15));
+        for (int i = 0; i < 4; ++i) {
+            const float more = UP >> i & 1 ? MAGIC : 0.0f;
+            c[i] = make_float2((float)(n >> (8 * i) & 15) + more, (float)(n >> (8 * i + 4) & 15) + more);
+        }
     }
 }
 
 __device__ __forceinline__ float2 pack2(float2 a, float2 b, float up) { return fma2(b, make_float2(up, up), a); }
-// two integers below 2^16 as the halves of a word
+// two integers below 2^16, each + 2^23, as the halves of a word
 __device__ __forceinline__ uint32_t word_of(float lo, float hi) {
-    return __byte_perm(__float_as_uint(lo + 8388608.0f), __float_as_uint(hi + 8388608.0f), 0x5410);
+    return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410);
 }
 __device__ __forceinline__ uint32_t merged(uint32_t was, uint32_t now, uint32_t mask) { return (was & ~mask) | (now & mask); }
 
@@ -216,7 +220,7 @@ __device__ __noinline__ void block_slowly(const T *x, int64_t step, int d, int t
 
 // Warps: one a (sequence, block its new rows reach, head, tensor).  D: dims at most
 template <typename T, int D>
-__global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 3 : sizeof(T) * D <= 512 ? 2 : 1)
+__global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 12 : sizeof(T) * D <= 512 ? 8 : 4)
     kv4_write_kernel(const __grid_constant__ KvCacheArgs a) {
     constexpr int W = WORDS8<T>;
     const int lane = threadIdx.x & 31;
@@ -238,14 +242,15 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 3 : sizeof(
     const int lo = max(start - t0, 0), hi = min(end - t0, KV_B);  // the block's new tokens
     const bool there = pg >= 0 && pg < a.pages;
     uint8_t *rec = a.k + (((int64_t)(there ? pg : 0) * a.heads + h) * a.bpp + a.by_bpp.mod(blk)) * kv4_bytes(a.d);
-    // 8 values of a token, zeros if it is not new; where wide loads are not possible all blocks go the slow way
-    const auto get = [&](int t, int dim) {
-        const uint4 *p = reinterpret_cast<const uint4 *>(x + (int64_t)t * src.token + dim);
-        const bool in = t >= lo && t < hi;
+    // 8 values of a token (if it is not new, of the new one next to it, whose codes are not stored for it); where wide
+    // loads are not possible all blocks go the slow way
+    const auto row_of = [&](int t) { return x + (int64_t)min(max(t, lo), hi - 1) * src.token; };
+    const auto get = [&](const T *row, int dim) {
+        const uint4 *p = reinterpret_cast<const uint4 *>(row + dim);
         Eight<T> e;
 #pragma unroll
         for (int i = 0; i < W; i += 4) {
-            const uint4 y = in ? __ldg(p + i / 4) : make_uint4(0, 0, 0, 0);
+            const uint4 y = __ldg(p + i / 4);
             e.w[i] = y.x, e.w[i + 1] = y.y, e.w[i + 2] = y.z, e.w[i + 3] = y.w;
         }
         return e;
@@ -258,6 +263,7 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 3 : sizeof(
     const int g = lane >> 2, c = lane & 3;
     constexpr int NP = D / 32;
     Range r[2];
+    const T *const row[2] = {row_of(g), row_of(g + 8)};
     {
         Eight<T> raw[NP][2];
 #pragma unroll
@@ -266,7 +272,7 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 3 : sizeof(
             for (int k = 0; k < 2; ++k) {
                 // (dims past the last: the first ones once more, which does not change the range)
                 const int dim = 32 * p + 8 * c;
-                raw[p][k] = get(g + 8 * k, dim < a.d ? dim : 8 * (c & 1));
+                raw[p][k] = get(row[k], dim < a.d ? dim : 8 * (c & 1));
             }
         if (!there) return;
 #pragma unroll
@@ -299,7 +305,10 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 3 : sizeof(
         for (int dim = 8 * c; dim < a.d; dim += 32) {
             float2 n[2][4];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) codes8<T>(get(g + 8 * k, dim), v[k], n[k]);
+            for (int k = 0; k < 2; ++k) {
+                if (k) codes8<0>(get(row[k], dim), v[k], n[k]);
+                else codes8<5>(get(row[k], dim), v[k], n[k]);
+            }
             uint32_t w[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -326,6 +335,7 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 3 : sizeof(
             fresh |= t >= lo && t < hi ? 0x0f0fu << (16 * (k & 1) + 4 * (k >> 1)) : 0u;
         }
         const int odd = g & 1;
+        const T *const from[4] = {row_of(2 * c), row_of(2 * c + 1), row_of(2 * c + 8), row_of(2 * c + 9)};
 #pragma unroll 1
         for (int e0 = 0; 8 * e0 < a.d; e0 += 8) {
             const int e = e0 + g;
@@ -335,8 +345,8 @@ __global__ void __launch_bounds__(WARPS * 32, sizeof(T) * D <= 256 ? 3 : sizeof(
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 float2 first[4], second[4];
-                codes8<T>(get(2 * c + k, in ? 8 * e : 0), u[k], first);
-                codes8<T>(get(2 * c + k + 8, in ? 8 * e : 0), u[k + 2], second);
+                codes8<15>(get(from[k], in ? 8 * e : 0), u[k], first);
+                codes8<0>(get(from[k + 2], in ? 8 * e : 0), u[k + 2], second);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) n[k][j] = pack2(first[j], second[j], 16.0f);
             }
