@@ -7,8 +7,12 @@
 // as an integer too, and sincospi sees at most an eighth of a turn.
 //
 // A CTA takes the rows of a few tokens: first their angles, a sine and a cosine a pair and token to
-// shared memory (one a thread where there are 256), then heads and vectors, all with the same angles.  Work is
-// cut finer, by heads, where there are few tokens.  What bounds it is HBM: a value is read and written once.
+// shared memory (one a thread where there are that many), then heads and vectors, all with the same angles.  Work is
+// cut finer, by heads, where there are few tokens.
+//
+// What bounds it is HBM, a value is read and written once, and what keeps it from that are reads in flight and instructions.
+// Gradients of 12 prompts of up to 2500 tokens, 40 heads of 128 dims, 64 of them turned, bf16: 60 us, 84% of a copy's rate
+// (CTAs of 256 threads 66, two rows at a time 66, both 68, eight rows 65; a vector as words 72 -> 68 and 77 -> 72 before).
 #include <algorithm>
 #include <type_traits>
 
@@ -18,7 +22,7 @@ namespace skm {
 
 namespace {
 
-constexpr int THREADS = 256, TOKENS_MOST = 16;
+constexpr int THREADS = 128, TOKENS_MOST = 16, AT_ONCE = 4;  // AT_ONCE: rows that a thread reads before it uses the first
 
 // The sequence that row `tok` belongs to, -1 for none: the last of cu[0 .. batch] that is
 // not above it.  By a whole warp, four entries a lane and round.
@@ -191,13 +195,13 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(const __grid_constant__
             T *y = static_cast<T *>(part.y) + (int64_t)(tok0 + t) * part.y_token + (int64_t)(h0 + head) * part.y_head + dim;
             const int64_t x_step = step * part.x_head, y_step = step * part.y_head;
             const int64_t x_wrap = part.x_token - nh * part.x_head, y_wrap = part.y_token - nh * part.y_head;
-            // two rows at a time: both are read before either is used
+            // a few rows at a time: all are read before one is used
             while (t < nt) {
-                Unit<T, V, NEXT> unit[2];
-                T *to[2];
-                int of[2];
+                Unit<T, V, NEXT> unit[AT_ONCE];
+                T *to[AT_ONCE];
+                int of[AT_ONCE];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < AT_ONCE; ++i) {
                     to[i] = y;
                     of[i] = t < nt && (all || there[t]) ? t : -1;
                     if (of[i] >= 0) unit[i].load(x, half, copy);
@@ -205,7 +209,7 @@ __global__ void __launch_bounds__(THREADS) rotary_kernel(const __grid_constant__
                     while (head >= nh) head -= nh, x += x_wrap, y += y_wrap, ++t;
                 }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < AT_ONCE; ++i) {
                     if (of[i] < 0) continue;
                     if (!copy) unit[i].turn(angles + of[i] * half + (NEXT ? dim / 2 : dim));
                     unit[i].store(to[i], half, copy);
