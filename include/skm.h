@@ -975,7 +975,7 @@ typedef struct skm_rotary {
 
 typedef struct skm_rotary_rows {
     const void *x;         /* dtype rows [tokens] of [heads][d], d contiguous, strides in elements */
-    void *y;               /* may be x (then with its strides); no other overlap */
+    void *y;               /* may be x (then with its strides); no other overlap, no stride of 0 */
     int64_t x_token;
     int64_t x_head;
     int64_t y_token;

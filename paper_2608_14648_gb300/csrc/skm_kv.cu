@@ -390,6 +390,10 @@ int skm_kv_rotate(const skm_kv_seqs *s, const skm_rotary *r, int d, int dtype, c
         if (!aligned(p.x, e) || !aligned(p.y, e)) return set_error(SKM_ERR_INVALID_ARG, "x and y must be aligned to their elements");
         if (p.x == p.y && (p.x_token != p.y_token || p.x_head != p.y_head))
             return set_error(SKM_ERR_INVALID_ARG, "in place, x and y must have the same strides");
+        if ((s->tokens > 1 && p.y_token == 0) || (p.heads > 1 && p.y_head == 0))
+            return set_error(SKM_ERR_INVALID_ARG, "y's strides must not be 0");
+        if (i == 1 && (p.y == rows[0].y || p.y == rows[0].x || p.x == rows[0].y))
+            return set_error(SKM_ERR_INVALID_ARG, "y of one tensor is x or y of the other");
         if (p.x != p.y) in_place = false;
         narrow((int64_t)(reinterpret_cast<uintptr_t>(p.x) / e));
         narrow((int64_t)(reinterpret_cast<uintptr_t>(p.y) / e));

@@ -187,6 +187,11 @@ def test_rotation_is_checked(skm):  # noqa: F811
                    dict(y=FAKE, y_token=512), dict(y=FAKE, y_head=32)):
         assert rotate(skm, rows=[part(skm, **change)]) == INVALID
         assert rotate(skm, rows=[part(skm), part(skm, **change)]) == INVALID
+    # rows that would be written twice: no stride, the other tensor's
+    for change in (dict(y_token=0), dict(y_head=0)):
+        assert rotate(skm, rows=[part(skm, **change)]) == INVALID
+    for other in (dict(x=3 * FAKE), dict(x=2 * FAKE, y=3 * FAKE), dict(x=3 * FAKE, y=FAKE)):
+        assert rotate(skm, rows=[part(skm), part(skm, **other)]) == INVALID
     assert rotate(skm, d=0) == INVALID and rotate(skm, d=1025) == INVALID and rotate(skm, dtype=3) == INVALID
     assert rotate(skm, count=0) == INVALID and rotate(skm, rows=[part(skm)] * 3) == INVALID
     assert rotate(skm, s=seqs(skm, tokens=1 << 29, max_tokens=1)) == UNSUPPORTED
