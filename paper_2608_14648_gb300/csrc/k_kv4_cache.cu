@@ -17,6 +17,12 @@
 // corrected by its remainder, q + (d - q s) y, is k + 1/2, the remainder of that is 0, d is exact, and half to even is
 // right; else x - b is compared with (k + 1/2) s in 64 bits.  2^23 + q is an integer, rounded half to even; codes become
 // words by multiply-adds of integers as floats (below 2^16 beside 2^23, exact), two at a time.
+//
+// What bounds them.  Writing: instructions (a value's code takes 10 in packed pairs, its place in a word 2 more; issue
+// slots 57% taken) and reads that not enough warps wait for; 12 prompts of up to 2500 tokens, 8 heads of 128 dims, bf16: 42
+// us and 2.6 TB/s of the kernel, 65 us with reading back.  Quotients as divisions, or corrected everywhere, and zeros for rows
+// that are not new took 71; two, four and eight heads a warp with the next one's rows prefetched 69, 72 and 78 (their
+// loop's registers are too many).  Reading: HBM; 4 sequences of up to 32768 tokens, 82 us, 93% of a copy's rate.
 #include "skm_kv_cache.cuh"
 
 namespace skm {

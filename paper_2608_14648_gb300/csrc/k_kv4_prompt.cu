@@ -49,10 +49,13 @@ struct Lay {
     // two row tiles: registers of a softmax thread and of the others, no more in all than the 96 or 128 each that the launch comes with
     static constexpr int SOFT_REGS = THREADS == 640 ? 144 : 168, REST_REGS = THREADS == 640 ? 64 : 88;
     static_assert(NQ == 1 || CONV_WARP0 * SOFT_REGS + (THREADS / 32 - CONV_WARP0) * REST_REGS <= THREADS / 32 * (65536 / THREADS / 8 * 8));
-    static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a V tile
-    // SPLIT: a row's sum beside Q, a key's rests and its bias beside it, in 16 of 64 dims
-    static constexpr int QMORE = KEYS == SPLIT ? QT * 128 : 0, KTILE = KEYS == SPLIT ? 2 * TILE + KT * 128 : TILE;
-    static constexpr int q = 0, more = NQ * QTILE, k = more + NQ * QMORE, v = k + ST * KTILE, bars = v + ST * TILE;
+    static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of an operand of rows, of keys or values
+    // SPLIT: rests of keys and values behind them; rows' sums and keys' biases in 16 of 64 dims, those of the two row
+    // tiles and of the stages in the same rows
+    static constexpr int QMORE = KEYS == SPLIT ? QT * 128 : 0, KMORE = KEYS == SPLIT ? KT * 128 : 0;
+    static constexpr int KTILE = KEYS == SPLIT ? 2 * TILE : TILE, VTILE = KTILE;
+    static_assert(KEYS != SPLIT || (NQ <= 4 && ST <= 4));
+    static constexpr int q = 0, more = NQ * QTILE, kmore = more + QMORE, k = kmore + KMORE, v = k + ST * KTILE, bars = v + ST * VTILE;
     static constexpr int slots = bars + 8 * (6 * ST + 10);  // TMEM address, a flag, the part's index
     static constexpr int wild = (slots + 24 + 15) / 16 * 16;  // a byte a row: its query holds infinities or NaN
     static constexpr int there = wild + ROWS;  // a byte a block of the last INFO tiles: its page is present
@@ -231,7 +234,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
         *gone = 0;
     }
     if (a.d < DH) {  // dims from d on are zeros
-        for (int i = tid * 16; i < ST * (L::KTILE + L::TILE); i += THREADS * 16) st_shared(sm + L::k + i, 0, 0, 0, 0);
+        for (int i = tid * 16; i < ST * (L::KTILE + L::VTILE); i += THREADS * 16) st_shared(sm + L::k + i, 0, 0, 0, 0);
         fence_async();
     }
     if (warp == MMA_WARP) {
@@ -257,9 +260,9 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                                                                                  lane, smem + L::wild + q * QT, &row_sum);
         if constexpr (KEYS == SPLIT) {  // the sum in two f16, three times each, for (b, 4 s, 4 s) of a key twice
             const __half top = __float2half_rn(row_sum), rest = __float2half_rn(row_sum - __half2float(top));
-            const uint32_t to = sm + L::more + q * L::QMORE + row * 128;
-            st_shared(to + ((row & 7) << 4), u2(__halves2half2(top, top)), u2(__halves2half2(top, rest)), u2(__halves2half2(rest, rest)), 0);
-            st_shared(to + ((1 ^ (row & 7)) << 4), 0, 0, 0, 0);
+            const uint32_t to = sm + L::more + row * 128;
+            st_shared(to + ((2 * q ^ (row & 7)) << 4), u2(__halves2half2(top, top)), u2(__halves2half2(top, rest)), u2(__halves2half2(rest, rest)), 0);
+            st_shared(to + (((2 * q + 1) ^ (row & 7)) << 4), 0, 0, 0, 0);
         }
         row_sum *= fac;
         fence_async();
@@ -553,9 +556,22 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         uint32_t x[4];
+                        if constexpr (KEYS == SPLIT) {  // s (c - 8) in f16; what is left, exactly, and the value at code 8 in one
+                            uint32_t rest[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            x[i] = half ? dq.values<true, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i])) : dq.values<false, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i]));
+                            for (int i = 0; i < 4; ++i) {
+                                const __half2 u = h2(half ? dq.codes<true>(c[i] >> 8 * t) : dq.codes<false>(c[i] >> 8 * t));
+                                __half2 y = __hmul2(u, h2(s[i]));
+                                if constexpr (BIG) y = __hmax2(__hmin2(y, h2(0x7bff7bffu)), h2(0xfbfffbffu));
+                                rest[i] = u2(__hadd2(__hfma2(u, h2(s[i]), __hneg2(y)), h2(b[i])));
+                                x[i] = u2(y);
+                            }
+                            st_shared((to + L::TILE + k * 8192 + t * 1024) ^ (16 * half), rest[0], rest[1], rest[2], rest[3]);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                x[i] = half ? dq.values<true, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i])) : dq.values<false, BIG>(c[i] >> 8 * t, h2(s[i]), h2(b[i]));
+                        }
                         st_shared((to + k * 8192 + t * 1024) ^ (16 * half), x[0], x[1], x[2], x[3]);
                     }
                 }
@@ -575,9 +591,9 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
             if (KEYS == SPLIT && lane < KV_B) {  // (b, 4 s, 4 s) twice: eight s, but in f16's range
                 const __half2 sb = h2(ks[lane >> 3]);
                 const __half b = __high2half(sb), s4 = __hmul(__low2half(sb), __ushort_as_half(0x4400));
-                const uint32_t to = sm + L::k + st * L::KTILE + 2 * L::TILE + (blk * KV_B + lane) * 128;
-                st_shared(to + ((lane & 7) << 4), u2(__halves2half2(b, s4)), u2(__halves2half2(s4, b)), u2(__halves2half2(s4, s4)), 0);
-                st_shared(to + ((1 ^ (lane & 7)) << 4), 0, 0, 0, 0);
+                const uint32_t to = sm + L::kmore + (blk * KV_B + lane) * 128;
+                st_shared(to + ((2 * st ^ (lane & 7)) << 4), u2(__halves2half2(b, s4)), u2(__halves2half2(s4, b)), u2(__halves2half2(s4, s4)), 0);
+                st_shared(to + (((2 * st + 1) ^ (lane & 7)) << 4), 0, 0, 0, 0);
             }
             if (KEYS == SCALED && lane < 8) {
                 float *scale = reinterpret_cast<float *>(smem + L::keys) + (j & (INFO - 1)) * 2 * KT + blk * KV_B + g;
@@ -599,13 +615,15 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
             }
             load_keys(at_next, task + CONV);
             if (lane < KV_B) {
+                __half bias = __high2half(h2(vs));
+                if constexpr (KEYS == SPLIT) bias = __hmin(__hfma(__low2half(h2(vs)), __ushort_as_half(0x4800), bias), __ushort_as_half(0x7bff));  // + 8 s
                 reinterpret_cast<uint16_t *>(mine)[lane] = (uint16_t)vs;
-                reinterpret_cast<uint16_t *>(mine)[KV_B + lane] = (uint16_t)(vs >> 16);
+                reinterpret_cast<__half *>(mine)[KV_B + lane] = bias;
             }
             __syncwarp();
             if (!warp_sleep(v_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
-            if (big) values(std::true_type{}, v_to + st * L::TILE + ((blk * 2 ^ g) << 4));
-            else values(std::false_type{}, v_to + st * L::TILE + ((blk * 2 ^ g) << 4));
+            if (big) values(std::true_type{}, v_to + st * L::VTILE + ((blk * 2 ^ g) << 4));
+            else values(std::false_type{}, v_to + st * L::VTILE + ((blk * 2 ^ g) << 4));
             fence_async();
             __syncwarp();
             // (the last two tiles' steps wait for no keys: once more in their place)
@@ -636,7 +654,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
             dims(std::false_type{}, ka);
             if constexpr (KEYS == SPLIT) {
                 dims(std::true_type{}, ka + (L::TILE >> 4));
-                mma_ss<true>(d, operand(sm + L::more + q * L::QMORE), ka + (2 * L::TILE >> 4), idesc(KT), one);
+                mma_ss<true>(d, operand(sm + L::more) + 2 * q, operand(sm + L::kmore) + 2 * (j % ST), idesc(KT), one);
             }
             issued = true;
             commit(k_free(q, j % ST), one);
@@ -653,9 +671,13 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
             if (!(ok = warp_sleep(ready(q, j % ST), (j / ST) & 1, gone))) break;
             fence_after();
             const uint32_t p = S + (j & 1) * KT;
-            const uint64_t va = v_op + (uint32_t)(j % ST) * (L::TILE >> 4);
+            const uint64_t va = v_op + (uint32_t)(j % ST) * (L::VTILE >> 4);
 #pragma unroll
             for (int k = 0; k < KT / 16; ++k) mma_ts(O, p + 8 * k, va + 2 * k, idesc(DH), k > 0 || j > 0, one);
+            if constexpr (KEYS == SPLIT) {
+#pragma unroll
+                for (int k = 0; k < KT / 16; ++k) mma_ts(O, p + 8 * k, va + (L::TILE >> 4) + 2 * k, idesc(DH), 1, one);
+            }
             commit(v_free(q, j % ST), one);
             if (j + 2 < nt) qk(j + 2);  // over the buffer that P V read, in order behind it
             commit(s_full(q, j & 1), one);
