@@ -300,6 +300,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                 return bits;
             };
             uint32_t P[KT / 2];
+            [[maybe_unused]] uint32_t low_bits[KEYS == SCALED ? KT / 2 : 1];  // what the weights' rounding left
             uint64_t sum[4] = {0, 0, 0, 0};
             // (SCALED) a key's scale and its value at code 8
             const float *scale = reinterpret_cast<const float *>(smem + L::keys) + (j & (INFO - 1)) * 2 * KT;
@@ -331,7 +332,16 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                             t.x = sees & 1u << (i + k - k0) ? t.x : -INFINITY;
                             t.y = sees & 2u << (i + k - k0) ? t.y : -INFINITY;
                         }
-                        P[(i + k) / 2] = weights2(t.x, t.y, sum[(i + k) / 2 & 3]);
+                        if constexpr (KEYS == SCALED) {
+                            const float2 p = make_float2(ex2(t.x), ex2(t.y));
+                            sum[(i + k) / 2 & 3] = add2(sum[(i + k) / 2 & 3], joined(p));
+                            const __half2 y = __floats2half2_rn(p.x, p.y);
+                            const float2 z = __half22float2(y);
+                            P[(i + k) / 2] = u2(y);
+                            low_bits[(i + k) / 2] = pack(p.x - z.x, p.y - z.y);
+                        } else {
+                            P[(i + k) / 2] = weights2(t.x, t.y, sum[(i + k) / 2 & 3]);
+                        }
                     }
                 }
             };
@@ -393,7 +403,10 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
             }
             l += add;
 #pragma unroll
-            for (int k = 0; k < KT / 2; k += 16) st16(S + k, P + k);
+            for (int k = 0; k < KT / 2; k += 16) {
+                st16(S + k, P + k);
+                if constexpr (KEYS == SCALED) st16(S + KT / 2 + k, low_bits + k);
+            }
             st_wait();
             fence_before();
             __syncwarp();
@@ -674,9 +687,10 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
             const uint64_t va = v_op + (uint32_t)(j % ST) * (L::VTILE >> 4);
 #pragma unroll
             for (int k = 0; k < KT / 16; ++k) mma_ts(O, p + 8 * k, va + 2 * k, idesc(DH), k > 0 || j > 0, one);
-            if constexpr (KEYS == SPLIT) {
+            if constexpr (KEYS != ROUNDED) {  // SPLIT: the values' rests; SCALED: the weights'
 #pragma unroll
-                for (int k = 0; k < KT / 16; ++k) mma_ts(O, p + 8 * k, va + (L::TILE >> 4) + 2 * k, idesc(DH), 1, one);
+                for (int k = 0; k < KT / 16; ++k)
+                    mma_ts(O, p + (KEYS == SCALED ? KT / 2 : 0) + 8 * k, va + (KEYS == SPLIT ? L::TILE >> 4 : 0) + 2 * k, idesc(DH), 1, one);
             }
             commit(v_free(q, j % ST), one);
             if (j + 2 < nt) qk(j + 2);  // over the buffer that P V read, in order behind it

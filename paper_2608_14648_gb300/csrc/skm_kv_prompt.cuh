@@ -148,6 +148,12 @@ __device__ __forceinline__ float2 halves(uint64_t x) {
     return r;
 }
 
+__device__ __forceinline__ uint64_t joined(float2 x) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x.x), "f"(x.y));
+    return r;
+}
+
 // A part: a CTA's rows x (m, l), then its rows of d sums
 __host__ __device__ __forceinline__ int64_t prompt_part(int rows, int d) { return rows * (int64_t)(2 + d); }
 
