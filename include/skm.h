@@ -921,10 +921,11 @@ int skm_kv4_read(const skm_kv4_cache *c, const skm_kv_seqs *s, int dtype, void *
  * tensor cores, sums and softmax in fp32, weights rounded to f16.  Query rows become f16 by a power of two
  * a row: elements below 2^-25 (F16) or 2^-28 (BF16) of the row's largest lose bits, those below 2^-36
  * vanish.  Calls of more than 32 rows a sequence (tokens x heads of a group; d > 128: of more keys too)
- * run on another kernel: it takes values rounded to f16 (2^-11 of each; b + 15 s above f16's largest number as
- * that number), keys too where the output is BF16 and no lse is asked for; where one is, or the output is F16,
- * and d <= 128, elements of a query row below 2^-20 (F16) or 2^-23 (BF16) of its largest lose bits and those
- * below 2^-32 vanish.  F32: fp32 arithmetic throughout.
+ * run on another kernel.  For BF16 outputs without lse it takes keys and values rounded to f16 (2^-11 of each; b + 15 s above
+ * f16's largest number as that number).  Otherwise it takes keys as they are and, d <= 128, values with b + 8 s rounded to
+ * f16 and a rounding of 2^-11 of that, d > 128, values rounded to f16 and weights to 2^-22; d <= 128: elements of a query
+ * row below 2^-20 (F16) or 2^-23 (BF16) of its largest lose bits there and those below 2^-32 vanish.  F32: fp32 arithmetic
+ * throughout.
  * The result does not depend on timing.  Asynchronous. */
 size_t skm_kv4_attend_workspace_size(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a);
 int skm_kv4_attend(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws, size_t ws_bytes,

@@ -4,21 +4,26 @@
 // As k_kv_prompt.cu: a CTA takes 256 query rows of one sequence and key/value head as two tiles of 128
 // (d > 128: one), and walks the keys they see in tiles of 64 positions; softmax warps of one
 // thread a row, converter warps, a warp for each row tile that issues its products.  Unlike there the
-// values' operand holds whole values, b + s c with one rounding to f16 (2^-11), so l = sum p, and a tile's sum of weights
-// tells whether the reference m has to move.  Keys take one of three forms:
-//   ROUNDED  like values (bf16 outputs without log-sum-exps, which do not show it): p = 2^(f S - m)
-//   SPLIT    s (c - 8) as the sum of two f16, a second operand beside the first, and b + 8 s as b + 4 s + 4 s in 16
-//            dims more, beside the row's sum in two f16: exact, for twice the products Q K' and no more softmax
-//   SCALED   (d > 128, where SPLIT has no room) codes less 8, exact, and t = f (s <q, c - 8> + (b + 8 s) sum q) in the
-//            softmax, two more operations a logit
-// Whole prompts of up to 4096, 16 heads of 64, f16: 113 us ROUNDED, 127 SPLIT, 175 SCALED; ROUNDED log-sum-exps were 2e-5
-// off and f16 outputs by more than the 1.6 times an f16 computation's error that is left (values and weights in f16).
+// values' operands hold whole values, so l = sum p, and a tile's sum of weights
+// tells whether the reference m has to move.  Keys and values take one of three forms:
+//   ROUNDED  b + s c with one rounding to f16, 2^-11 (bf16 outputs without log-sum-exps, which do not show it): p = 2^(f S - m)
+//   SPLIT    s (c - 8) as the sum of two f16, a second operand beside the first.  Keys: b + 8 s as b + 4 s + 4 s in 16
+//            dims more, beside the row's sum in two f16: exact.  Values: b + 8 s rounded to f16 and added to the second
+//            operand with a rounding.  Twice the products and no more softmax
+//   SCALED   (d > 128, where SPLIT has no room) keys: codes less 8, exact, and t = f (s <q, c - 8> + (b + 8 s) sum q) in the
+//            softmax, two more operations a logit; values as in ROUNDED, but weights in two f16, a second operand too
+// f16 weights and f16 values are each as far off as an f16 output: SPLIT has the one, SCALED the other left.
+// Prompts of up to 4096, 16 heads of 64, f16: 113 us ROUNDED, 131 SPLIT, 175 SCALED (with weights in one f16); f16 outputs 1.4
+// times as far off an exact result as its rounding (with values in one f16 127 us, 1.6 times); log-sum-exps 1e-6 off (ROUNDED 2e-5).
+// 4 x 2048 tokens, 32 query heads on 8 of 128 dims: 176 us ROUNDED, 333 SPLIT (six converter warps and two stages, as shared
+// memory allows, make twice the operands); 16 on 8 of 192 dims: 263 ROUNDED, 312 SCALED.
 //
 // What bounds it: the tensor cores, and what keeps them waiting.  A tile of 128 rows and 64 keys of 128 dims takes
-// 4 MFLOP; chunks of 2048 before 16384 tokens, 32 rows heads on 8, 128 dims, bf16: 270 us, 66% of cuBLAS's bf16 rate.  A
+// 4 MFLOP; chunks of up to 2048 tokens behind 6144 (two sequences), 32 query heads on 8 of 128 dims, bf16: 270 us, 66% of cuBLAS's bf16 rate.  A
 // step's waits were most of what could be gained: one barrier for all that its products need (299 -> 296 us), waits that
-// suspend instead of spinning in the schedulers that convert (296 -> 276), constants in registers (276 -> 270).  Exact
-// bytes are no bound: 136 a token and head of 64 dims.
+// suspend instead of spinning in the schedulers that convert (296 -> 276), constants in registers (276 -> 270).  The
+// products alone, issued without a pause, take 82% of that time: one with 64 keys as its columns takes 48 clocks where 32
+// would do, and tiles of 128 keys find no room in TMEM beside two row tiles' sums and next logits.
 #include "skm_kv_prompt.cuh"
 
 namespace skm {
@@ -48,7 +53,9 @@ struct Lay {
     static constexpr int CONV_WARP0 = 4 * NQ, MMA_WARP = CONV_WARP0 + CONV, THREADS = 32 * (MMA_WARP + NQ);
     // two row tiles: registers of a softmax thread and of the others, no more in all than the 96 or 128 each that the launch comes with
     static constexpr int SOFT_REGS = THREADS == 640 ? 144 : 168, REST_REGS = THREADS == 640 ? 64 : 88;
-    static_assert(NQ == 1 || CONV_WARP0 * SOFT_REGS + (THREADS / 32 - CONV_WARP0) * REST_REGS <= THREADS / 32 * (65536 / THREADS / 8 * 8));
+    // (a quarter of the SM holds a quarter of the warps, rounded up, so a launch of 18 warps comes with the registers of one of 20)
+    static constexpr int LAUNCH_REGS = 65536 / ((THREADS + 127) / 128 * 128) / 8 * 8;
+    static_assert(NQ == 1 || CONV_WARP0 * SOFT_REGS + (THREADS / 32 - CONV_WARP0) * REST_REGS <= THREADS / 32 * LAUNCH_REGS);
     static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of an operand of rows, of keys or values
     // SPLIT: rests of keys and values behind them; rows' sums and keys' biases in 16 of 64 dims, those of the two row
     // tiles and of the stages in the same rows

@@ -13,7 +13,7 @@ approximate logarithm and reciprocal, 2^-20; f32: n + 16 roundings of 2^-24), e 
 any order, (d + 16) 2^-23 scale sum |q| (|b| + s (c + 16)), plus 2^-22 |logit| for the base-2 form.  The last term covers weights that
 underflow in f16: of half a block's tokens the weight is held divided by 16, so it is off by at most 2^-21 (half of f16's smallest
 step, 2^-25, times 16), its code at most 15, and the row's largest weight times scale at least 2^7.  The kernel for many rows takes
-values as f16: with `rounded`, 2^-11 of a value's size (2^-25 where it is subnormal) on top; and for bf16 outputs without lse keys
+values as f16 at worst: with `rounded`, 2^-11 of a value's size (2^-25 where it is subnormal) on top; and for bf16 outputs without lse keys
 too: their logits are off by up to scale sum |q| (2^-11 |k| + 2^-25) more.  lse: e and
 2^-22 of its size, and the sums' error w without the f16 weights' 2^-11 (sums are of the weights in fp32)."""
 import math
