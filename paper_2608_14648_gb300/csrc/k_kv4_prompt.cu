@@ -22,7 +22,7 @@
 // 4 MFLOP; chunks of up to 2048 tokens behind 6144 (two sequences), 32 query heads on 8 of 128 dims, bf16: 270 us, 66% of cuBLAS's bf16 rate.  A
 // step's waits were most of what could be gained: one barrier for all that its products need (299 -> 296 us), waits that
 // suspend instead of spinning in the schedulers that convert (296 -> 276), constants in registers (276 -> 270).  The
-// products alone, issued without a pause, take 82% of that time: one with 64 keys as its columns takes 48 clocks where 32
+// products alone, issued without a pause, take 74% of that time: one with 64 keys as its columns takes 48 clocks where 32
 // would do, and tiles of 128 keys find no room in TMEM beside two row tiles' sums and next logits.
 #include "skm_kv_prompt.cuh"
 
