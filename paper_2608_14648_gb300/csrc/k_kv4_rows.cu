@@ -21,11 +21,11 @@
 // 16 between the two lies on the other operand (half of a query's dims and half of a
 // block's weights carry 2^-4), 2^24 on the results.
 //
-// What bounds it: HBM from a batch that fills the machine on; next to it issue slots, of which a code takes half.  96
-// sequences of up to 10001 tokens, 8 heads of 128 dims, 4 query rows each, bf16: 118 us, 67% of a copy's rate (79.9 us for
-// the bytes).  Items of two blocks share masks, maxima and the walk (138 -> 129 us), queries' operands lie in shared
-// memory where registers would spill (129 -> 118).  A long sequence, f16, 262151 tokens: 66 us (42.2), of which codes
-// less 8 are 4.
+// What bounds it, with a batch that fills the machine: the latencies of four warps a scheduler (issue slots 57%, ALU 53%
+// taken) before HBM.  96 sequences of up to 10001 tokens, 8 heads of 128 dims, 4 query rows each, bf16: 119 us, 67% of a
+// copy's rate (79.9 us for the bytes); 546 instructions an item of two blocks, 160 of them make operands of codes, 32 are
+// products.  Items of two blocks share masks, maxima and the walk (138 -> 129 us), queries' operands lie in shared memory
+// where registers would spill (129 -> 118).  A long sequence, f16, 262151 tokens: 66 us (42.2), of which codes less 8 are 4.
 #include "skm_kv_rows.cuh"
 
 namespace skm {
