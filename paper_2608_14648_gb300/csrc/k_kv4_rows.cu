@@ -11,15 +11,15 @@
 // k_kv_rows.cu: the weights that become f16 then are p = e s_v, kept below 2^15 by the
 // reference m), l = sum p / s_v and the biases' sum is sum p (b_v / s_v), in fp32.
 //
-// For f16 outputs the second product has codes less 8 (and b_v / s_v + 8): the weights' rounding is an error of the
-// codes' size, and tensor cores cut their sums off, which shows where values nearly cancel (the mean of 262151 keys: 6 times
-// as far off as its rounding to f16 with codes 0..15).  bf16 outputs hide both.
+// The second product has codes less 8 (and b_v / s_v + 8): the weights' rounding is an error of the
+// codes' size, and tensor cores cut their sums off at every product, always downward for codes 0..15.  The mean of values that
+// nearly cancel lost all its bits so (1024 sequences of a million tokens: 2.7e-3 off where it was 2.0e-3, in any output type).
 //
-// A code as an operand of the tensor cores costs half an instruction: four bits under a mask
+// A key's code as an operand of the tensor cores costs half an instruction: four bits under a mask
 // are the f16 numbers 2^-24 c (bits 0..3) or 2^-20 c (bits 4..7), subnormal and
 // exact, so a word's eight codes are four operands after one shift and four masks.  The factor
-// 16 between the two lies on the other operand (half of a query's dims and half of a
-// block's weights carry 2^-4), 2^24 on the results.
+// 16 between the two lies on the other operand (half of a query's dims carry 2^-4), 2^24 on the
+// results.  A logit has at most 16 such products.
 //
 // What bounds it, with a batch that fills the machine: the latencies of four warps a scheduler (issue slots 57%, ALU 53%
 // taken) before HBM.  96 sequences of up to 10001 tokens, 8 heads of 128 dims, 4 query rows each, bf16: 119 us, 67% of a
@@ -254,10 +254,8 @@ struct MmaRows4 {
     uint32_t q[QMEM ? 1 : NT][QMEM ? 1 : DC][2];
     uint2 *qmem;
     int2 *lim;
-    bool fine;  // f16 outputs
 
     __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int h, int r0, uint8_t *mem, int lane) {
-        fine = a.dtype == SKM_DTYPE_F16;
         const int g = lane >> 2, c = lane & 3, nc = FULL ? DC : a.d / KV_B;
         lim = reinterpret_cast<int2 *>(mem);
         qmem = reinterpret_cast<uint2 *>(mem + LIMITS<RT>);
@@ -384,7 +382,7 @@ struct MmaRows4 {
                 float lv;
                 asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lv) : "f"(v));
                 asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(iv[n][k]) : "f"(v));
-                bv[n][k] = fmaf(sc.vb, iv[n][k], fine ? MIDDLE : 0.0f);
+                bv[n][k] = fmaf(sc.vb, iv[n][k], MIDDLE);
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -453,39 +451,32 @@ struct MmaRows4 {
                     l[t][i] = fmaf(p[n][t][i + 2], iv[n][1], fmaf(p[n][t][i], iv[n][0], l[t][i]));
                     ob[t][i] = fmaf(p[n][t][i + 2], bv[n][1], fmaf(p[n][t][i], bv[n][0], ob[t][i]));
                 }
-                const float down = fine ? 1.0f : 0.0625f;
-                const __half2 lo = __floats2half2_rn(p[n][t][0], p[n][t][1]), hi = __floats2half2_rn(p[n][t][2] * down, p[n][t][3] * down);
+                const __half2 lo = __floats2half2_rn(p[n][t][0], p[n][t][1]), hi = __floats2half2_rn(p[n][t][2], p[n][t][3]);
                 pb[n][t][0] = transpose8x8(*reinterpret_cast<const uint32_t *>(&lo));
                 pb[n][t][1] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hi));
             }
         uint32_t up;
         asm volatile("mov.b32 %0, 0x64006400;" : "=r"(up));
-        const auto sums = [&](auto exact) {
 #pragma unroll
-            for (int w0 = 0; w0 < DC; w0 += 4) {
-                if (w0 >= nc) break;
-                uint32_t r[NB][4], f[4];
+        for (int w0 = 0; w0 < DC; w0 += 4) {
+            if (w0 >= nc) break;
+            uint32_t r[NB][4], f[4];
 #pragma unroll
-                for (int n = 0; n < NB; ++n) ldsm4(va + n * bytes + w0 * 128, r[n]);
+            for (int n = 0; n < NB; ++n) ldsm4(va + n * bytes + w0 * 128, r[n]);
 #pragma unroll
-                for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int w = w0 + i;
-                        if (w >= DC || w >= nc) break;
-                        if constexpr (decltype(exact)::value) codes4_mid(r[n][i], up, f);
-                        else codes4_a(r[n][i], f);
+                for (int i = 0; i < 4; ++i) {
+                    const int w = w0 + i;
+                    if (w >= DC || w >= nc) break;
+                    codes4_mid(r[n][i], up, f);
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) mma16816(o[t][w], f, pb[n][t][0], pb[n][t][1]);
-                    }
-            }
-        };
-        if (fine) sums(std::true_type{});
-        else sums(std::false_type{});
+                    for (int t = 0; t < NT; ++t) mma16816(o[t][w], f, pb[n][t][0], pb[n][t][1]);
+                }
+        }
     }
 
     __device__ __forceinline__ void close(int) {
-        const float up = fine ? 1.0f : CODES_UP;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -497,8 +488,8 @@ struct MmaRows4 {
                 }
 #pragma unroll
                 for (int w = 0; w < DC; ++w) {
-                    o[t][w][i] = fmaf(o[t][w][i], up, ob[t][i]);
-                    o[t][w][i + 2] = fmaf(o[t][w][i + 2], up, ob[t][i]);
+                    o[t][w][i] += ob[t][i];
+                    o[t][w][i + 2] += ob[t][i];
                 }
             }
     }
