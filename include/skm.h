@@ -912,8 +912,8 @@ int skm_kv4_write(const skm_kv4_cache *c, const skm_kv_seqs *s, int dtype, const
                   int64_t k_head, const void *V, int64_t v_token, int64_t v_head, void *stream);
 
 /* Values of positions pos[b], pos[b] + 1, ... back, as skm_kv_read: b + s code in fp32 with one
- * rounding, rounded once more to dtype.  Absent pages and positions past the table's end: zeros.
- * Asynchronous. */
+ * rounding, rounded once more to dtype (F16: values above f16's largest number, which b + 15 s may be, to that
+ * number).  Absent pages and positions past the table's end: zeros.  Asynchronous. */
 int skm_kv4_read(const skm_kv4_cache *c, const skm_kv_seqs *s, int dtype, void *K, void *V, void *stream);
 
 /* Attention of query rows over the cache: rows, masks, outputs, status and workspaces as for
@@ -925,7 +925,7 @@ int skm_kv4_read(const skm_kv4_cache *c, const skm_kv_seqs *s, int dtype, void *
  * f16's largest number as that number).  Otherwise it takes keys as they are and, d <= 128, values with b + 8 s rounded to
  * f16 and a rounding of 2^-11 of that, d > 128, values rounded to f16 and weights to 2^-22; d <= 128: elements of a query
  * row below 2^-20 (F16) or 2^-23 (BF16) of its largest lose bits there and those below 2^-32 vanish.  F32: fp32 arithmetic
- * throughout.
+ * throughout.  F16 outputs beyond f16's largest numbers are those.
  * The result does not depend on timing.  Asynchronous. */
 size_t skm_kv4_attend_workspace_size(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a);
 int skm_kv4_attend(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws, size_t ws_bytes,

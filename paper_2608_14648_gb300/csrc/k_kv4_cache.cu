@@ -383,6 +383,18 @@ __device__ __forceinline__ float2 low_codes(uint32_t u) {
     return add2(make_float2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442))),
                 make_float2(-8388608.0f, -8388608.0f));
 }
+// 8 values; f16's end at its largest number (which a vector's largest code may stand for more than: -65504 to 65504 gives 65536)
+template <typename T>
+__device__ __forceinline__ void store8_within(T *p, const float *v) {
+    if constexpr (std::is_same<T, __half>::value) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
+        *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        store8(p, v);
+    }
+}
 __device__ __forceinline__ float2 scaled(float2 n, float2 sb) { return fma2(n, make_float2(sb.x, sb.x), make_float2(sb.y, sb.y)); }
 
 // Warps: one a (sequence, block its range reaches, head, tensor).
@@ -434,7 +446,7 @@ __global__ void __launch_bounds__(WARPS * 32) kv4_read_kernel(const __grid_const
                 const uint32_t u = w[p].x >> (8 * k), y = w[p].y >> (8 * k);
                 const float2 v[4] = {scaled(low_codes(u), sb), scaled(low_codes(u >> 4), sb), scaled(low_codes(y), sb),
                                      scaled(low_codes(y >> 4), sb)};
-                store8(dst + t * step + 32 * p + 8 * c, reinterpret_cast<const float *>(v));
+                store8_within(dst + t * step + 32 * p + 8 * c, reinterpret_cast<const float *>(v));
             }
         }
     } else {
@@ -468,8 +480,8 @@ __global__ void __launch_bounds__(WARPS * 32) kv4_read_kernel(const __grid_const
                     const float2 y = fma2(low_codes(w[i][j] >> (4 * k)), s, o);
                     v0[j] = y.x, v1[j] = y.y;
                 }
-                if (first) store8(dst + t * step + 8 * e, v0);
-                if (second) store8(dst + (t + 1) * step + 8 * e, v1);
+                if (first) store8_within(dst + t * step + 8 * e, v0);
+                if (second) store8_within(dst + (t + 1) * step + 8 * e, v1);
             }
         }
     }

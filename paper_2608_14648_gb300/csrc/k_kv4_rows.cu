@@ -524,8 +524,9 @@ struct MmaRows4 {
 #pragma unroll
                 for (int w = 0; w < DC; ++w) {
                     if (!FULL && w >= a.d / KV_B) break;
-                    dst[16 * w] = bits16(o[t][w][i] * inv, bf);
-                    dst[16 * w + 8] = bits16(o[t][w][i + 2] * inv, bf);
+                    const float x = o[t][w][i] * inv, y = o[t][w][i + 2] * inv;
+                    dst[16 * w] = bits16(bf ? x : kv_within(x, a.most), bf);
+                    dst[16 * w + 8] = bits16(bf ? y : kv_within(y, a.most), bf);
                 }
                 if (g == 0 && a.lse) a.lse[row] = l[t][i] == 0.0f ? -INFINITY : LN2 * (m[t][i] + log2f(l[t][i]));
             }

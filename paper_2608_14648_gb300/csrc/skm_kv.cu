@@ -240,6 +240,8 @@ int attend(const Cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws,
     k.out = a->out;
     k.lse = a->lse;
     k.status = a->status;
+    // a 4-bit vector's largest code may stand for more than f16 holds, and so may a mean of them
+    k.most = c->four ? 65504.0f : INFINITY;
     k.part_cta = p.part_cta;
     k.part_warp = p.part_warp;
     k.max_tiles = p.prompt ? p.many.max_tiles : (int)cdiv((int64_t)k.max_tokens * k.group, p.rows.rt);

@@ -90,6 +90,7 @@ struct KvAttnArgs {
     void *out;
     float *lse;
     int32_t *status;
+    float most;        // largest magnitude of an f16 output (skm_kv.cu)
     float *part_cta;   // [grid][2] partial rows of units that CTAs share
     float *part_warp;  // [grid][warps] rows of the unit that a warp found begun and left
     int max_tiles;     // row tiles of the longest sequence
@@ -168,6 +169,8 @@ __device__ __forceinline__ void kv_store(void *x, int64_t i, float v, int dtype)
     else if (dtype == SKM_DTYPE_BF16) static_cast<__nv_bfloat16 *>(x)[i] = __float2bfloat16_rn(v);
     else static_cast<__half *>(x)[i] = __float2half_rn(v);
 }
+// brought into [-most, most]; NaN stays
+__device__ __forceinline__ float kv_within(float x, float most) { return x > most ? most : x < -most ? -most : x; }
 // two fp32 operations in one instruction
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     float2 r;

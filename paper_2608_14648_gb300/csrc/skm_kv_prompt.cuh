@@ -294,10 +294,11 @@ __global__ void __launch_bounds__(256) kv_prompt_join_kernel(const __grid_consta
             const float4 v = *reinterpret_cast<const float4 *>(p + 2 * unit_rows + (int64_t)pr * a.d + 4 * c);
             o.x = fmaf(v.x, w, o.x), o.y = fmaf(v.y, w, o.y), o.z = fmaf(v.z, w, o.z), o.w = fmaf(v.w, w, o.w);
         }
-        kv_store(a.out, row * a.d + 4 * c, o.x * inv, a.dtype);
-        kv_store(a.out, row * a.d + 4 * c + 1, o.y * inv, a.dtype);
-        kv_store(a.out, row * a.d + 4 * c + 2, o.z * inv, a.dtype);
-        kv_store(a.out, row * a.d + 4 * c + 3, o.w * inv, a.dtype);
+        const float most = a.dtype == SKM_DTYPE_F16 ? a.most : INFINITY;
+        kv_store(a.out, row * a.d + 4 * c, kv_within(o.x * inv, most), a.dtype);
+        kv_store(a.out, row * a.d + 4 * c + 1, kv_within(o.y * inv, most), a.dtype);
+        kv_store(a.out, row * a.d + 4 * c + 2, kv_within(o.z * inv, most), a.dtype);
+        kv_store(a.out, row * a.d + 4 * c + 3, kv_within(o.w * inv, most), a.dtype);
     }
     if ((threadIdx.x & 31) == 0 && a.lse) a.lse[row] = l == 0.0f ? -INFINITY : LN2 * (m + log2f(l));
 }

@@ -138,6 +138,7 @@ __device__ __forceinline__ void store_row4(const KvAttnArgs &a, int64_t row, int
         reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row * a.d)[c] =
             make_uint2(*reinterpret_cast<const uint32_t *>(&x), *reinterpret_cast<const uint32_t *>(&y));
     } else {
+        o = make_float4(kv_within(o.x, a.most), kv_within(o.y, a.most), kv_within(o.z, a.most), kv_within(o.w, a.most));
         const __half2 x = __floats2half2_rn(o.x, o.y), y = __floats2half2_rn(o.z, o.w);
         reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row * a.d)[c] =
             make_uint2(*reinterpret_cast<const uint32_t *>(&x), *reinterpret_cast<const uint32_t *>(&y));

@@ -1,8 +1,8 @@
-"""The 4-bit key/value cache where weighted sums cancel."""
+"""The 4-bit key/value cache where weighted sums cancel and where its values end."""
 import pytest
 import torch
-from test_gpu_kv import DT
-from test_gpu_kv4 import scales
+from test_gpu_kv import DT, i32
+from test_gpu_kv4 import make_cache, scales
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +39,50 @@ def test_long_sums_keep_their_precision(cuda_ok, typ):
     adds = 2 * batch * n // (152 * 16) // 16
     tol = 2.0**-9 * (u + 2 * adds * 2.0**-24) + 2.0**-20 * 3
     assert (out.double() - 2.0**-9).abs().max() <= tol
+
+
+# ---- values at f16's ends
+
+WIDE = 8736.0  # the smallest f16 s with -65504 + 15 s >= 65504: the largest code stands for 65536
+
+
+@pytest.mark.parametrize("typ", ["f16", "f32"])
+@pytest.mark.parametrize("back", ["f16", "bf16", "f32"])
+def test_vectors_from_end_to_end_read_back(cuda_ok, typ, back):
+    """Within half a scale of what was written and the type's rounding, in f16 too."""
+    import paper_2608_14648_gb300 as skm
+
+    x = (2 * torch.rand(20, 4, 48, generator=torch.Generator().manual_seed(1)) - 1) * 65504
+    x[..., 5], x[..., 40] = -65504.0, 65504.0
+    x = x.to(DT[typ])
+    c, table, dev = make_cache(2, 48, 16, 2), i32([[1, 0]]), x.cuda()
+    skm.skm_kv4_write(c, table, i32([3]), i32([0, 20]), dev[:, :2], dev[:, 2:], 20)
+    got = skm.skm_kv4_read(c, table, i32([3]), i32([0, 20]), 20, 20, {"f32": 0, "bf16": 1, "f16": 2}[back])
+    u = {"bf16": 2.0**-8, "f16": 2.0**-11, "f32": 2.0**-24}[back]
+    for y, want in zip(got, (x[:, :2], x[:, 2:])):
+        assert y.dtype == DT[back] and torch.isfinite(y).all()
+        assert (y.cpu().double() - want.double()).abs().max() <= WIDE / 2 + u * 65536
+
+
+@pytest.mark.parametrize("d", [64, 128, 192])
+@pytest.mark.parametrize("batch,length,new", [(1, 300, 1), (1, 40000, 1), (40, 3000, 1), (3, 300, 5), (1, 400, 100), (1, 6000, 100)])
+def test_attention_over_values_at_the_ends(cuda_ok, d, batch, length, new):
+    """Means of 65536 and of -65504 in f16, in every way that a row's result is put together.  A mean is off by its weights'
+    rounding and sums, 2^-11 + length 2^-23 of 65536, and f16's steps there are 32."""
+    import paper_2608_14648_gb300 as skm
+
+    cols = -(-length // 64)
+    c = make_cache(1, d, 64, cols)
+    c.blocks[..., 8 * d:16 * d] = 0
+    sc = scales(c)
+    sc[..., 2], sc[..., 3] = WIDE, -65504.0
+    top = c.blocks[..., 8 * d:16 * d].unflatten(-1, (d // 16, 8, 16))  # codes of dims g and g + 8: the even g are 15
+    top[..., 0::2, :] = 255
+    table = torch.arange(cols, dtype=torch.int32, device="cuda").expand(batch, cols).contiguous()
+    cu = i32([i * new for i in range(batch + 1)])
+    Q = torch.randn(batch * new, 4, d, generator=torch.Generator().manual_seed(2)).to(torch.float16).cuda()
+    out, _ = skm.skm_kv4_attend(c, table, i32([length] * batch), cu, Q, new, length, causal=False, scale=1e-3)
+    want = torch.full((d,), -65504.0, dtype=torch.float64)
+    want.view(d // 16, 2, 8)[..., 0::2] = 65504.0
+    assert torch.isfinite(out).all()
+    assert (out.cpu().double() - want).abs().max() <= (2.0**-11 + length * 2.0**-23) * 65536 + 32
