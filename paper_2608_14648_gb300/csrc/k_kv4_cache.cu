@@ -15,8 +15,9 @@
 // 45 2^-24 of the quotient and its nearest integer is the quotient's unless it lies within 2^-18 of the middle of two.  It
 // often is the middle itself (16-bit values, biases and scales have few bits: one value in 2500 of a bf16 input): then q
 // corrected by its remainder, q + (d - q s) y, is k + 1/2, the remainder of that is 0, d is exact, and half to even is
-// right; else x - b is compared with (k + 1/2) s in 64 bits.  2^23 + q is an integer, rounded half to even; codes become
-// words by multiply-adds of integers as floats (below 2^16 beside 2^23, exact), two at a time.
+// right; else x - b is compared with (k + 1/2) s in 64 bits, and where the two are equal what x - b was rounded by decides.
+// 2^23 + q is an integer, rounded half to even; codes become words by multiply-adds of integers as floats (below 2^16
+// beside 2^23, exact), two at a time.
 //
 // What bounds them.  Writing: instructions (a value's code takes 10 in packed pairs, its place in a word 2 more; issue
 // slots 57% taken) and reads that not enough warps wait for; 12 prompts of up to 2500 tokens, 8 heads of 128 dims, bf16: 42
@@ -107,13 +108,16 @@ __device__ __forceinline__ uint32_t held(const Lvq &v) {  // (scale, bias)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// the code of a value within its vector's range, in 64 bits where fp32 leaves it open
+// the code of a value within its vector's range, by an exact comparison where fp32 leaves it open
 __device__ __forceinline__ float code_of(float x, const Lvq &v) {
     const float q = (x - v.b) * v.inv, c = rintf(q);
     if (fabsf(q - c) <= NEAR) return c;
     const float k = floorf(q);  // near k + 1/2
     const double over = (double)x - (double)v.b, mid = ((double)k + 0.5) * (double)v.s;
-    return over > mid || (over == mid && ((int)k & 1)) ? k + 1.0f : k;
+    if (over != mid) return over > mid ? k + 1.0f : k;
+    // what the difference was rounded by (Knuth's exact sum): x next to 0 and b are further apart than 53 bits
+    const double z = __dadd_rn(over, -(double)x), rest = __dadd_rn(__dadd_rn((double)x, -__dadd_rn(over, -z)), __dadd_rn(-(double)v.b, -z));
+    return rest > 0.0 || (rest == 0.0 && ((int)k & 1)) ? k + 1.0f : k;
 }
 // the same of 8 values, in a nibble each (by value and not inlined: what is rare costs the ordinary path no registers)
 template <typename T>

@@ -1,8 +1,10 @@
-"""The 4-bit key/value cache where weighted sums cancel and where its values end."""
+"""The 4-bit key/value cache where weighted sums cancel, where its values end, and where codes lie next to the middle of two."""
+from fractions import Fraction
+
 import pytest
 import torch
 from test_gpu_kv import DT, i32
-from test_gpu_kv4 import make_cache, scales
+from test_gpu_kv4 import Held4, make_cache, scales
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +88,38 @@ def test_attention_over_values_at_the_ends(cuda_ok, d, batch, length, new):
     want.view(d // 16, 2, 8)[..., 0::2] = 65504.0
     assert torch.isfinite(out).all()
     assert (out.cpu().double() - want).abs().max() <= (2.0**-11 + length * 2.0**-23) * 65536 + 32
+
+
+# ---- codes at the middle of two
+
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("slow", [False, True])
+def test_codes_next_to_a_middle_are_exact(cuda_ok, typ, slow):
+    """b = -(k + 1/2) s puts the middle of codes k and k + 1 at 0, where elements come as close to it as the type's smallest
+    numbers: the code is that of exact rational arithmetic.  slow: an infinity among the elements, left out."""
+    import paper_2608_14648_gb300 as skm
+
+    near = [0.0, 1e-20, -1e-20, 1e-30, -1e-30, 1e-38, -1e-38, 1e-44, -1e-44, 3e-8, -3e-8, 6e-8, -6e-8, 1e-5, -1e-5]
+    steps = [2.0, 0.5, 2.0**-10, 4096.0, 0.75, 1.25]
+    rows, scale = [], []
+    for s in steps:
+        for k in range(15):
+            b = -(k + 0.5) * s
+            row = [b, b + 15 * s] + [v * max(s, 1.0) for v in near] + [b + 15 * s] * 15
+            row[-1] = float("inf") if slow else b
+            rows.append(row)
+            scale.append((s, k))
+    x = torch.tensor(rows, dtype=torch.float64).to(DT[typ])  # (ends are exact in all three types)
+    n, d = x.shape
+    c = make_cache(1, d, 16, -(-n // 16))
+    table = torch.arange(-(-n // 16), dtype=torch.int32).view(1, -1)
+    K = x.view(n, 1, d)
+    V = K.flip(2)
+    skm.skm_kv4_write(c, table.cuda(), i32([0]), i32([0, n]), K.cuda(), V.cuda(), n)
+    held = Held4(c)
+    for t, X in enumerate((K, V)):
+        code, sc = (h.reshape(-1, h.shape[-1])[:n] for h in (held.code[t], held.scale))
+        for r, (s, k) in enumerate(scale):
+            assert sc[r, 2 * t] == s and sc[r, 2 * t + 1] == -(k + 0.5) * s
+            exact = [15 if v == float("inf") else round((Fraction(v) + Fraction((k + 0.5) * s)) / Fraction(s)) for v in X[r, 0].tolist()]
+            assert code[r].tolist() == exact, (s, k)
