@@ -976,7 +976,7 @@ typedef struct skm_rotary {
 
 typedef struct skm_rotary_rows {
     const void *x;         /* dtype rows [tokens] of [heads][d], d contiguous, strides in elements */
-    void *y;               /* may be x (then with its strides); no other overlap, no stride of 0 */
+    void *y;               /* may be x (then with its strides); no other overlap, nor of its rows with each other */
     int64_t x_token;
     int64_t x_head;
     int64_t y_token;
@@ -987,8 +987,8 @@ typedef struct skm_rotary_rows {
 
 /* Row i of sequence b stands at position pos[b] + i (skm_kv_write's); of s, table, cols and max_len are
  * not read.  rows: `count` (1 or 2) tensors, as a step's queries and keys.  Rows that belong to no
- * sequence are left alone.  fp32 arithmetic, one rounding.  1 <= d <= 1024.  One kernel, no
- * workspace.  Asynchronous. */
+ * sequence are left alone.  fp32 arithmetic, one rounding.  1 <= d <= 1024, heads <= 65536, tokens x heads (of the
+ * tensor with more) <= 5e8.  One kernel, no workspace.  Asynchronous. */
 int skm_kv_rotate(const skm_kv_seqs *s, const skm_rotary *r, int d, int dtype, const skm_rotary_rows *rows, int count,
                   void *stream);
 

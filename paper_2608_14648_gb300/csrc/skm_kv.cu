@@ -278,6 +278,22 @@ auto with(const C *c, F &&f) {
 
 constexpr int ROTARY_D_MOST = 1024;
 
+// Whether two of a tensor's rows (tokens x heads, d elements each) share an element.  Rows (t, h) and (t + i, h + j) do where
+// |i token + j head| < d: of each j >= 0 the i on either side of -j head / token are looked at, unless one stride spans
+// all that the other does
+bool rows_overlap(int64_t tokens, int64_t heads, int64_t token, int64_t head, int64_t d) {
+    using Wide = __int128;
+    const auto size = [](Wide x) { return x < 0 ? -x : x; };
+    const Wide t = tokens > 1 ? size(token) : 0, h = heads > 1 ? size(head) : 0;
+    if ((tokens > 1 && t < d) || (heads > 1 && h < d)) return true;
+    if (tokens == 1 || heads == 1 || t >= (heads - 1) * h + d || h >= (tokens - 1) * t + d) return false;
+    for (int64_t j = 1; j < heads; ++j) {  // (the sign of either stride only mirrors the rows)
+        const Wide i = j * h / t;
+        if ((i < tokens && j * h - i * t < d) || (i + 1 < tokens && (i + 1) * t - j * h < d)) return true;
+    }
+    return false;
+}
+
 }  // namespace
 
 }  // namespace skm
@@ -392,8 +408,8 @@ int skm_kv_rotate(const skm_kv_seqs *s, const skm_rotary *r, int d, int dtype, c
         if (!aligned(p.x, e) || !aligned(p.y, e)) return set_error(SKM_ERR_INVALID_ARG, "x and y must be aligned to their elements");
         if (p.x == p.y && (p.x_token != p.y_token || p.x_head != p.y_head))
             return set_error(SKM_ERR_INVALID_ARG, "in place, x and y must have the same strides");
-        if ((s->tokens > 1 && p.y_token == 0) || (p.heads > 1 && p.y_head == 0))
-            return set_error(SKM_ERR_INVALID_ARG, "y's strides must not be 0");
+        if (rows_overlap(s->tokens, p.heads, p.y_token, p.y_head, d))
+            return set_error(SKM_ERR_INVALID_ARG, "y's rows overlap: strides %lld and %lld for rows of %d", (long long)p.y_token, (long long)p.y_head, d);
         if (i == 1 && (p.y == rows[0].y || p.y == rows[0].x || p.x == rows[0].y))
             return set_error(SKM_ERR_INVALID_ARG, "y of one tensor is x or y of the other");
         if (p.x != p.y) in_place = false;

@@ -1,0 +1,46 @@
+"""Rotary positions: what the host decides (no GPU: the device pointers are fake and never dereferenced)."""
+import itertools
+
+import pytest
+from test_kv4_abi import part, rotate, rotary
+from test_kv_abi import FAKE, INVALID, UNSUPPORTED, seqs, skm  # noqa: F401
+
+
+# ---- outputs whose rows share elements
+
+@pytest.mark.parametrize("y_token,y_head", [(256, 63), (63, 4096), (255, 64), (64, 65), (128, 64), (-256, 32), (96, 64), (64 * 2, 64 * 3), (1, 1)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_outputs_that_overlap_are_refused(skm, y_token, y_head, sign):  # noqa: F811
+    # 4 heads of 64 dims, 10 tokens
+    s = seqs(skm, tokens=10, max_tokens=10)
+    assert rotate(skm, s=s, rows=[part(skm, y_token=sign * y_token, y_head=y_head)]) == INVALID
+    assert b"overlap" in skm.lib().skm_last_error()
+    assert rotate(skm, s=s, rows=[part(skm), part(skm, x=5 * FAKE, y=7 * FAKE, y_token=y_token, y_head=sign * y_head)]) == INVALID
+    # in place too
+    assert rotate(skm, s=s, rows=[part(skm, y=FAKE, x_token=y_token, x_head=y_head, y_token=y_token, y_head=y_head)]) == INVALID
+
+
+def reaches_launch(skm, s, rows, d=64):  # noqa: F811
+    """Whether only the last check, of tokens x heads, refuses the call."""
+    return rotate(skm, s=s, rows=rows, d=d) == UNSUPPORTED
+
+
+def test_outputs_that_do_not_overlap_pass(skm):  # noqa: F811
+    # every pair of small strides against the definition: the elements of all rows, counted
+    tokens, heads, d = 5, 4, 3
+    s, r = seqs(skm, tokens=tokens, max_tokens=tokens), rotary(skm, dims=2)
+    for y_token, y_head in itertools.product(range(-16, 17), repeat=2):
+        at = [t * y_token + h * y_head + i for t in range(tokens) for h in range(heads) for i in range(d)]
+        y = part(skm, y_token=y_token, y_head=y_head, heads=heads)
+        got = rotate(skm, s=s, r=r, rows=[y, part(skm, x=None)], d=d)  # the second tensor is refused in any case
+        assert got == INVALID
+        assert (b"overlap" in skm.lib().skm_last_error()) == (len(set(at)) < len(at)), (y_token, y_head)
+
+
+def test_limits_of_sizes(skm):  # noqa: F811
+    assert rotate(skm, rows=[part(skm, heads=65537)]) == INVALID
+    wide = dict(x_token=1 << 30, y_token=1 << 30, heads=65536)
+    assert reaches_launch(skm, seqs(skm, tokens=7630, max_tokens=1), [part(skm, **wide)])
+    for token in (1 << 62, -(1 << 62)):  # no stride is too large for the check
+        assert reaches_launch(skm, seqs(skm, tokens=7630, max_tokens=1), [part(skm, **(wide | dict(y_token=token)))])
+    assert not rotate(skm, s=seqs(skm, tokens=0), rows=[part(skm, y_token=1)])  # nothing to do
