@@ -1056,8 +1056,9 @@ def skm_kv_rotate(rotary: Rotary, start, cu, rows, max_tokens, out=None, transpo
     """Rows cu[b]:cu[b + 1] of one tensor [tokens, heads, d] or of two (a step's queries
     and keys; any strides with d contiguous) turned to positions start[b], start[b] + 1, ...
     of sequence b; start int32 [batch], cu [batch + 1].  out: new tensors unless given (the
-    rows themselves: in place).  transpose: what a gradient of the result becomes.  Returns
-    out, a tensor or a tuple as rows is."""
+    rows themselves: in place).  transpose: what a gradient of the result becomes; no history
+    is recorded, so rows that require a gradient are refused outside torch.no_grad().
+    Returns out, a tensor or a tuple as rows is."""
     single = isinstance(rows, torch.Tensor)
     if single:
         rows, out = (rows,), None if out is None else (out,)
@@ -1075,7 +1076,7 @@ def skm_kv_rotate(rotary: Rotary, start, cu, rows, max_tokens, out=None, transpo
     dtype = _KV_DTYPES.get(kind)
     if dtype is None:
         raise ValueError("rows must be float32, bfloat16 or float16")
-    outs, packed = [], b""
+    outs, packed, history = [], b"", torch.is_grad_enabled()
     for i, x in enumerate(rows):
         shape, x_at = x.shape, x.stride()
         if len(shape) != 3 or shape[0] != tokens or shape[2] != d or x_at[2] != 1 or x.dtype is not kind or x.get_device() != index:
@@ -1090,6 +1091,8 @@ def skm_kv_rotate(rotary: Rotary, start, cu, rows, max_tokens, out=None, transpo
             if y.shape != shape or y_at[2] != 1 or y.dtype is not kind or y.get_device() != index:
                 raise ValueError("out must be of the rows' shape, type and device, d contiguous")
             y_token, y_head = y_at[0], y_at[1]
+        if history and (x.requires_grad or y.requires_grad):
+            raise ValueError("the call records no history: rotate under torch.no_grad(), and gradients with transpose=True")
         outs.append(y)
         packed += _ROTARY_ROWS.pack(x.data_ptr(), y.data_ptr(), x_at[0], x_at[1], y_token, y_head, heads, 0)
     s = _KV_SEQS.pack(batch, 0, 0, _kv_ints("start", start, batch, index), _kv_ints("cu", cu, batch + 1, index), tokens, max_tokens, 0)

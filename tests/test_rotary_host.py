@@ -2,8 +2,9 @@
 import itertools
 
 import pytest
+import torch
 from test_kv4_abi import part, rotate, rotary
-from test_kv_abi import FAKE, INVALID, UNSUPPORTED, seqs, skm  # noqa: F401
+from test_kv_abi import FAKE, INVALID, UNSUPPORTED, OnDevice, seqs, skm  # noqa: F401
 
 
 # ---- outputs whose rows share elements
@@ -44,3 +45,41 @@ def test_limits_of_sizes(skm):  # noqa: F811
     for token in (1 << 62, -(1 << 62)):  # no stride is too large for the check
         assert reaches_launch(skm, seqs(skm, tokens=7630, max_tokens=1), [part(skm, **(wide | dict(y_token=token)))])
     assert not rotate(skm, s=seqs(skm, tokens=0), rows=[part(skm, y_token=1)])  # nothing to do
+
+
+# ---- rows that require a gradient
+
+class Library:
+    """Stands in for the library, whose calls it counts."""
+
+    def __init__(self):
+        self.calls = 0
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls += 1
+            return 0
+        return call
+
+
+@pytest.mark.parametrize("which", ["x", "y", "out"])
+def test_rows_that_require_a_gradient_are_refused(skm, monkeypatch, which):  # noqa: F811
+    library = Library()
+    monkeypatch.setattr(skm, "lib", lambda: library)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    rot = skm.Rotary.__new__(skm.Rotary)
+    rot.index, rot.addrs = 0, (0, 0)
+    on = lambda t: OnDevice(t, 0)  # noqa: E731
+    ints = lambda *v: on(torch.tensor(v, dtype=torch.int32))  # noqa: E731
+    tensor = {n: torch.zeros(3, 2, 64, requires_grad=n == which) for n in ("x", "y", "out")}
+    x, y, out = (on(tensor[n]) for n in ("x", "y", "out"))
+    args = ints(0), ints(0, 3), (x, y), 3
+    with pytest.raises(ValueError, match="history"):
+        skm.skm_kv_rotate(rot, *args, out=(out, x))
+    assert library.calls == 0
+    with torch.no_grad():
+        skm.skm_kv_rotate(rot, *args, out=(out, x))
+    with torch.inference_mode():
+        skm.skm_kv_rotate(rot, *args, out=(out, x))
+    assert library.calls == 2
