@@ -948,8 +948,10 @@ int skm_kv4_attend(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_at
  *           positions; gain 0.1 ln(factor) + 1 where factor > 1 (Peng et al., YaRN, 2023)
  *   TURNS   the same with w falling from 1 to 0 as a pair's turns over `trained` positions go from low to
  *           high; gain 1
- * base > 1, factor > 0, trained > 0, 0 < low < high.  Frequencies are good to 2^-50 of themselves: angles
- * to 2^-24 up to position 2^26.
+ * base > 1, factor > 0, trained > 0, 0 < low < high.  A frequency is off by 2^-65 turns a position (half a unit, which is
+ * 2^-40 of the slowest pair's at base 1e7) and, with NONE, LINEAR and BASE, by (|ln f_i| + 6) 2^-53 of itself (BASE: and
+ * (|ln factor| dims / (dims - 2) + 3) 2^-53): angles to 2^-24 up to position 2^26 for NONE, and for LINEAR where factor >= 1.
+ * INDEX and TURNS are their formulas in 64-bit floating point, w's rounding included.
  * ------------------------------------------------------------------------ */
 enum { SKM_ROTARY_HALF = 0, SKM_ROTARY_INTERLEAVED = 1 };
 enum { SKM_ROTARY_NONE = 0, SKM_ROTARY_LINEAR = 1, SKM_ROTARY_BASE = 2, SKM_ROTARY_INDEX = 3, SKM_ROTARY_TURNS = 4 };

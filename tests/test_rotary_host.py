@@ -1,9 +1,10 @@
 """Rotary positions: what the host decides (no GPU: the device pointers are fake and never dereferenced)."""
 import itertools
+from decimal import Decimal, localcontext
 
 import pytest
 import torch
-from test_kv4_abi import part, rotate, rotary
+from test_kv4_abi import part, rotate, rotary, turns
 from test_kv_abi import FAKE, INVALID, UNSUPPORTED, OnDevice, seqs, skm  # noqa: F401
 
 
@@ -83,3 +84,46 @@ def test_rows_that_require_a_gradient_are_refused(skm, monkeypatch, which):  # n
     with torch.inference_mode():
         skm.skm_kv_rotate(rot, *args, out=(out, x))
     assert library.calls == 2
+
+
+# ---- frequencies
+
+PI = Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211707")
+
+
+@pytest.mark.parametrize("dims,base", [(2, 10000.0), (64, 10000.0), (128, 500000.0), (80, 1e7), (1024, 1.5)])
+@pytest.mark.parametrize("kind,factor", [("none", 1.0), ("linear", 8.0), ("linear", 0.3), ("base", 8.0), ("base", 0.7)])
+def test_frequencies_to_their_bound(skm, dims, base, kind, factor):  # noqa: F811
+    """Against 40 digits.  Half a unit of 2^-64, and of the frequency: the exponent's rounding, |ln f| 2^-53, pow 2^-52, the
+    divisions by factor and 2 pi and its constant 2^-53 each; a scaled base of relative error (|ln factor| dims / (dims - 2) + 3)
+    2^-53 moves f by 2 i / dims of that."""
+    scaling = {"none": skm.ROTARY_NONE, "linear": skm.ROTARY_LINEAR, "base": skm.ROTARY_BASE}[kind]
+    rc, got, gain = turns(skm, dims=dims, base=base, scaling=scaling, factor=factor)
+    assert rc == 0 and gain == 1.0
+    with localcontext() as ctx:
+        ctx.prec = 40
+        lnb, lnfactor = Decimal(base).ln(), Decimal(factor).ln()
+        if kind == "base" and dims > 2:
+            lnb += lnfactor * dims / (dims - 2)
+        eps, worst = Decimal(2) ** -53, Decimal(0)
+        for i, t in enumerate(got):
+            lnf = -lnb * 2 * i / dims
+            f = lnf.exp() / (Decimal(factor) if kind == "linear" else 1)
+            turn = f / (2 * PI)
+            off = abs((Decimal(t) / 2**64 - turn + Decimal(1) / 2) % 1 - Decimal(1) / 2)  # (of a circle)
+            bound = Decimal(2) ** -65 + turn * eps * (abs(lnf) + 6)
+            if kind == "base":
+                bound += turn * eps * Decimal(2 * i) / dims * (abs(lnfactor) * dims / max(dims - 2, 1) + 3)
+            assert off <= bound, (i, off / bound)
+            worst = max(worst, off * 2 * PI * 2**26)
+        if kind == "none" or (kind == "linear" and factor >= 1):
+            assert worst <= Decimal(2) ** -24  # the angle at position 2^26
+
+
+def test_slow_frequencies_are_not_good_to_their_last_bits(skm):  # noqa: F811
+    # what the units leave of them: a relative bound would not hold
+    rc, got, _ = turns(skm, dims=80, base=1e7)
+    with localcontext() as ctx:
+        ctx.prec = 40
+        turn = (-Decimal(1e7).ln() * 78 / 80).exp() / (2 * PI)
+        assert Decimal(2) ** -50 < abs(Decimal(got[39]) / 2**64 / turn - 1) <= Decimal(2) ** -65 / turn + Decimal(2) ** -48
