@@ -8,13 +8,15 @@
 // instructions of a block (1095 a warp for 2048 values): the input is read before the page is known, eight
 // 16-byte loads a lane at a time, and the second pass is a rolled loop (holding the
 // values in registers instead took an unrolled path for each d, and warps waited for
-// its instructions: 43 us against 37 for the 12 prompts below).  64 registers, 32 warps an
-// SM: with 48 or 40 registers the loads in flight cost more than the warps give (writing and reading
-// back 54, 55 and 59 us).
+// its instructions: 43 us against 37 for the 12 prompts below).  Registers for 32 warps an SM of 16-bit input: without the
+// limit they are 68 for 28 warps, and 900 sequences that append a token take 27.0 us instead of 24.8 (prompts 32 both); with
+// 48 or 40 the loads in flight cost more than the warps give (writing and reading back 54, 55 and 59 us).  For 28 of fp32:
+// 12 prompts of up to 2500 tokens 57.7 us, 900 appends 28.2, 40 chunks of 70 tokens 14.5; for 32 warps 61.2, 26.6 and 16.1 (108 bytes
+// spilled), for 24 59.4, 29.3 and 13.4.
 //
 // Measured (GB300, bf16, 8 heads of 128): writing 12 prompts of up to 2500 tokens, 93 MB
 // in and out, 32 us = 2.9 TB/s; reading 4 sequences of up to 32768 tokens back, 611 MB,
-// 101 us = 6.0 TB/s (a plain copy: 6.8).
+// 96 us = 6.4 TB/s (a plain copy: 6.8).
 //
 // Lanes: the magnitudes and the keys along d (a 16-byte code store, two 16-byte loads
 // of 16-bit values); values, whose blocks keep the 16 tokens of a dim together, 8
@@ -119,7 +121,7 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t bits, float old, Fini
 
 // Warps: one a (sequence, block its new rows reach, head, tensor).
 template <typename T>
-__global__ void __launch_bounds__(WARPS * 32, 4) kv_write_kernel(const __grid_constant__ KvCacheArgs a) {
+__global__ void __launch_bounds__(WARPS * 32, (sizeof(T) == 4 ? 28 : 32) / WARPS) kv_write_kernel(const __grid_constant__ KvCacheArgs a) {
     const int lane = threadIdx.x & 31;
     const int warp = blockIdx.x * WARPS + (threadIdx.x >> 5), tensor = warp & 1;
     const int h = a.by_heads.mod(warp >> 1);
