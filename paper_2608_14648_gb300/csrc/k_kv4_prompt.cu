@@ -44,6 +44,7 @@ struct Lay {
     static constexpr int NQ = DH <= 128 ? 2 : 1;      // row tiles of a CTA
     static constexpr int ST = DH == 64 || (DH == 128 && KEYS != SPLIT) ? 4 : 2;  // K and V tiles in flight
     static constexpr int ROWS = NQ * QT;
+    static_assert(ROWS == prompt_rows(DH));
     // converter warps.  A barrier's parity tells a phase from the next one only, so a warp may not come to a stage two rounds
     // early: from a task to its next one it goes on by no more stages than there are, and for the first one it has
     // waited until its stage was free.  (And no fewer than two stages: a warp's values of tile j would wait for the product

@@ -60,6 +60,7 @@ struct Lay {
     static constexpr int NQ = DH <= 128 ? 2 : 1;      // row tiles of a CTA
     static constexpr int ST = DH <= 128 ? 4 : 2;      // K and V tiles in flight
     static constexpr int ROWS = NQ * QT;
+    static_assert(ROWS == prompt_rows(DH));
     static constexpr int CONV_WARP0 = 4 * NQ, MMA_WARP = CONV_WARP0 + CONV, THREADS = 32 * (MMA_WARP + 1);
     static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of a Q tile, of a K or V tile
     static constexpr int q = 0, k = NQ * QTILE, v = k + ST * TILE, info = v + ST * TILE;
@@ -552,12 +553,12 @@ bool kv_prompt_ok(int dtype, int nb, int heads, int d, int64_t rows, int64_t spa
 constexpr int64_t SPLIT_KEYS = 320;
 
 size_t kv_prompt_part_most(int d, int64_t span) {
-    return span < 2 * SPLIT_KEYS ? 0 : (size_t)KV_SMS * prompt_part(d <= 128 ? Lay<128>::ROWS : Lay<256>::ROWS, d) * 4;
+    return span < 2 * SPLIT_KEYS ? 0 : (size_t)KV_SMS * prompt_part(prompt_rows(d), d) * 4;
 }
 
 KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens, int64_t span) {
     KvPromptPlan p = {};
-    const int unit_rows = d <= 128 ? Lay<128>::ROWS : Lay<256>::ROWS;
+    const int unit_rows = prompt_rows(d);
     p.max_tiles = (int)cdiv((int64_t)max_tokens * group, unit_rows);
     p.units = (int64_t)nb * heads * p.max_tiles;
     p.splits = 1;

@@ -126,7 +126,7 @@ KvPromptPlan kv_prompt_plan(int nb, int heads, int group, int d, int max_tokens,
 // workspace of any call of this d and span at most
 size_t kv_prompt_part_most(int d, int64_t span);
 cudaError_t launch_kv_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st);
-// (4-bit: planned like the 8-bit cache's)
+// (4-bit: chosen and planned by the 8-bit cache's functions; both kernels assert the rows of a CTA that they count on)
 cudaError_t launch_kv4_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t st);
 
 // A kernel's shared-memory limit, raised once a device: the call costs a

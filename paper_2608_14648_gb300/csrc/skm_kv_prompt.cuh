@@ -12,6 +12,9 @@ namespace {
 
 constexpr int QT = 128, KT = 64, KBLK = KT / KV_B;  // rows of a tile, keys of a tile, blocks of it
 constexpr int RANKED = 256;
+// rows of a CTA: two row tiles, above 128 dims one.  Units, parts and workspaces of both caches' kernels are planned with it
+// (kv_prompt_plan, kv_prompt_part_most)
+__host__ __device__ constexpr int prompt_rows(int d) { return d <= 128 ? 2 * QT : QT; }
 
 __device__ __forceinline__ void arrive(uint32_t b) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(b) : "memory");
