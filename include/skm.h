@@ -221,7 +221,8 @@ int skm_version(void); /* major*10000 + minor*100 + patch */
  *                       rows a sequence), the first keys of one warp, numbered by
  *                       the occurrences still armed, never count as arrived:
  *                       its wait ends after 1 ms and the call's status word is
- *                       set.
+ *                       set; in skm_kv4_attend of more rows the first (an even
+ *                       number) or second tile of keys of the CTA of half that number.
  * The environment variable SKM_FAULT=workspace|launch|status|wait arms one
  * occurrence when the library first checks.  Nothing faults the GPU: every
  * injected failure is a status the host reads.  Returns SKM_OK, or

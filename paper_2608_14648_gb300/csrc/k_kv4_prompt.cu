@@ -99,7 +99,7 @@ __device__ __forceinline__ void ld_wait32(uint32_t *v) {
 
 // Bounded, cut short when another role gave up, by a whole warp with one answer.  Suspended meanwhile, a millisecond at a
 // time (a loop of short tries took a sixth of the kernel's issue slots)
-__device__ __forceinline__ bool warp_sleep(uint32_t b, uint32_t parity, volatile int32_t *gone) {
+__device__ __forceinline__ bool warp_sleep(uint32_t b, uint32_t parity, volatile int32_t *gone, const KvAttnArgs &a) {
     const auto there = [&](uint32_t ns) {
         uint32_t ok;
         asm volatile(
@@ -116,7 +116,7 @@ __device__ __forceinline__ bool warp_sleep(uint32_t b, uint32_t parity, volatile
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
     while (!there(1000000)) {
         asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-        if (__any_sync(0xffffffffu, *gone || t - t0 > KV_WAIT_NS)) {
+        if (__any_sync(0xffffffffu, *gone || t - t0 > a.wait_ns)) {
             *gone = 1;
             return false;
         }
@@ -233,7 +233,8 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
         const auto init = [&](uint32_t b, int count) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(b), "r"(count) : "memory");
         };
-        for (int i = 0; i < 2; ++i) init(k_first(i), KBLK);
+        // (one arrival more where a test wants the wait to run out)
+        for (int i = 0; i < 2; ++i) init(k_first(i), KBLK + (2 * (int)blockIdx.x + i == a.stuck));
         for (int q = 0; q < L::NQ; ++q) {
             for (int i = 0; i < ST; ++i) init(k_free(q, i), 1), init(v_free(q, i), 1), init(ready(q, i), 4 + 2 * KBLK);
             init(s_full(q, 0), 1), init(s_full(q, 1), 1), init(q_full(q), 4), init(drain(q), 1);
@@ -287,7 +288,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
         const volatile uint32_t *there = reinterpret_cast<const volatile uint32_t *>(smem + L::there);
         for (int j = 0; j < nt; ++j) {
             const uint32_t S = S0 + (j & 1) * KT;
-            if (!(ok = warp_sleep(s_full(q, j & 1), (j >> 1) & 1, gone))) break;
+            if (!(ok = warp_sleep(s_full(q, j & 1), (j >> 1) & 1, gone, a))) break;
             fence_after();
             uint32_t v[KT];
             ld32(S, v);
@@ -391,7 +392,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                 m = to;
                 l *= g;
                 if (j > 0) {
-                    if (!(ok = warp_sleep(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1, gone))) break;  // P V of tile j - 1 is through
+                    if (!(ok = warp_sleep(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1, gone, a))) break;  // P V of tile j - 1 is through
                     fence_after();
 #pragma unroll 1
                     for (int k = 0; k < DH / 16; ++k) {
@@ -422,7 +423,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
         }
         if (q < nq) {
             if (ok && nt > 0) {
-                ok = warp_sleep(s_full(q, (nt + 1) & 1), ((nt + 1) >> 1) & 1, gone);
+                ok = warp_sleep(s_full(q, (nt + 1) & 1), ((nt + 1) >> 1) & 1, gone, a);
                 fence_after();
             }
             if (!ok) {
@@ -607,7 +608,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
             const int at_next = __shfl_sync(0xffffffffu, cur, (i + 1) & 31);
             const bool big = __any_sync(0xffffffffu, beyond(vs) || (KEYS != SCALED && (beyond(ks[0]) || beyond(ks[1]))));
             const int whose = j - ST < nt0 ? ask : nq - 1;
-            if (!warp_sleep(k_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
+            if (!warp_sleep(k_free(whose, st), ((j / ST) & 1) ^ 1, gone, a)) break;
             if (lane == 0) smem[L::there + (j & (INFO - 1)) * KBLK + blk] = at >= 0;
             if (KEYS == SPLIT && lane < KV_B) {  // (b, 4 s, 4 s) twice: eight s, but in f16's range
                 const __half2 sb = h2(ks[lane >> 3]);
@@ -642,7 +643,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                 reinterpret_cast<__half *>(mine)[KV_B + lane] = bias;
             }
             __syncwarp();
-            if (!warp_sleep(v_free(whose, st), ((j / ST) & 1) ^ 1, gone)) break;
+            if (!warp_sleep(v_free(whose, st), ((j / ST) & 1) ^ 1, gone, a)) break;
             if (big) values(std::true_type{}, v_to + st * L::VTILE + ((blk * 2 ^ g) << 4));
             else values(std::false_type{}, v_to + st * L::VTILE + ((blk * 2 ^ g) << 4));
             fence_async();
@@ -659,7 +660,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
         // (one a row tile: between its products a warp waits, commits and counts for as long as the products take)
         const int q = warp - MMA_WARP, nt = tiles_for(q);
         const uint32_t one = elect_one();
-        bool ok = nt > 0 && warp_sleep(q_full(q), 0, gone), issued = false;
+        bool ok = nt > 0 && warp_sleep(q_full(q), 0, gone, a), issued = false;
         const uint64_t q_op = operand(sm + L::q + q * L::QTILE), k_op = operand(sm + L::k), v_op = operand(sm + L::v);
         const uint32_t S = tmem + 2 * q * KT, O = tmem + L::O + q * DH;
         const auto qk = [&](int j) {
@@ -682,14 +683,14 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
         };
         // the logits of two key tiles ahead
         for (int j = 0; j < 2 && j < nt && ok; ++j) {
-            if (!(ok = warp_sleep(k_first(j), 0, gone))) break;
+            if (!(ok = warp_sleep(k_first(j), 0, gone, a))) break;
             fence_after();
             qk(j);
             commit(s_full(q, j), one);
         }
 #pragma unroll 1
         for (int j = 0; j < nt && ok; ++j) {
-            if (!(ok = warp_sleep(ready(q, j % ST), (j / ST) & 1, gone))) break;
+            if (!(ok = warp_sleep(ready(q, j % ST), (j / ST) & 1, gone, a))) break;
             fence_after();
             const uint32_t p = S + (j & 1) * KT;
             const uint64_t va = v_op + (uint32_t)(j % ST) * (L::VTILE >> 4);

@@ -248,7 +248,7 @@ int attend(const Cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws,
     k.whole = p.rows.whole;
     k.wait_ns = KV_WAIT_NS;
     k.stuck = -1;
-    if (!p.prompt && fault_take(SKM_FAULT_WAIT)) {
+    if ((!p.prompt || c->four) && fault_take(SKM_FAULT_WAIT)) {
         k.wait_ns = KV_WAIT_NS_INJECTED;
         k.stuck = skm_fault_armed(SKM_FAULT_WAIT);
     }

@@ -95,8 +95,9 @@ struct KvAttnArgs {
     float *part_warp;  // [grid][warps] rows of the unit that a warp found begun and left
     int max_tiles;     // row tiles of the longest sequence
     int whole;         // one CTA a unit (a sequence's row tile and head)
-    unsigned long long wait_ns;  // k_kv_rows.cu: limit of a wait for copies
-    int stuck;         // ... the warp whose first keys never count as arrived (SKM_FAULT_WAIT), -1: none
+    unsigned long long wait_ns;  // skm_kv_rows.cuh, k_kv4_prompt.cu: limit of a wait
+    int stuck;         // (SKM_FAULT_WAIT) the warp whose first keys never count as arrived, k_kv4_prompt.cu: the CTA and its first or second
+                       // tile of keys, 2 CTA + tile; -1: none
 };
 constexpr unsigned long long KV_WAIT_NS = 2000000000ull, KV_WAIT_NS_INJECTED = 1000000ull;
 

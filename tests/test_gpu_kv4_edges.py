@@ -1,10 +1,11 @@
-"""The 4-bit key/value cache where weighted sums cancel, where its values end, and where codes lie next to the middle of two."""
+"""The 4-bit key/value cache where weighted sums cancel, where its values end, where codes lie next to the middle of two, and
+where a wait runs out."""
 from fractions import Fraction
 
 import pytest
 import torch
 from test_gpu_kv import DT, i32
-from test_gpu_kv4 import Held4, make_cache, scales
+from test_gpu_kv4 import Held4, make_cache, make_table, scales
 
 pytestmark = pytest.mark.gpu
 
@@ -123,3 +124,48 @@ def test_codes_next_to_a_middle_are_exact(cuda_ok, typ, slow):
             assert sc[r, 2 * t] == s and sc[r, 2 * t + 1] == -(k + 0.5) * s
             exact = [15 if v == float("inf") else round((Fraction(v) + Fraction((k + 0.5) * s)) / Fraction(s)) for v in X[r, 0].tolist()]
             assert code[r].tolist() == exact, (s, k)
+
+
+# ---- waits that run out
+
+@pytest.mark.parametrize("heads,group,d,typ,lse,rows,most", [
+    (8, 4, 64, "bf16", False, [100, 70, 90], 500), (4, 2, 128, "f16", True, [300, 40], 900), (2, 4, 128, "bf16", False, [64], 20000),
+    (2, 1, 192, "bf16", True, [130, 40, 35], 700), (1, 2, 256, "f16", False, [50], 9000), (1, 1, 64, "f16", True, [33] * 1100, 90),
+])
+def test_many_rows_that_give_up_say_so(cuda_ok, heads, group, d, typ, lse, rows, most):
+    """A tile of keys that never counts as arrived (SKM_FAULT_WAIT, 1 ms), the first of a CTA or, with products in flight, the second:
+    the status is set, and every row is NaN or what it is without the fault."""
+    import paper_2608_14648_gb300 as skm
+
+    batch = len(rows)
+    g = torch.Generator().manual_seed(21)
+    length = [max(n, most - int(torch.randint(0, most // 2, (), generator=g))) for n in rows]
+    cols = -(-max(length) // 16)
+    c = make_cache(heads, d, 16, batch * cols, 22)
+    table = make_table(batch, cols, batch * cols, 23).cuda()
+    cu = [0] + torch.tensor(rows).cumsum(0).tolist()
+    Q = torch.randn(cu[-1], heads * group, d, generator=g).to(DT[typ]).cuda()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def call():
+        status.zero_()
+        out, l = skm.skm_kv4_attend(c, table, i32(length), i32(cu), Q, max(rows), max(length), want_lse=lse, out=torch.full_like(Q, 77.0), status=status)
+        return out, l, int(status)
+
+    want, want_lse, fine = call()
+    assert fine == 0 and torch.isfinite(want).all()
+    hits = set()
+    for stuck in (0, 1, 2, 7, 20, 45, 46):
+        skm.skm_inject_fault(skm.FAULT_WAIT, stuck + 1)
+        out, l, gave_up = call()
+        skm.skm_inject_fault(skm.FAULT_WAIT, 0)
+        bad = torch.isnan(out).all(-1)
+        assert (bad | (out == want).all(-1)).all()
+        if lse:
+            assert (torch.isnan(l) == bad).all() and torch.equal(l[~bad], want_lse[~bad])
+        assert gave_up == int(bad.any())
+        if gave_up:
+            hits.add(stuck % 2)
+    assert hits == {0, 1}
+    out, l, fine = call()  # nothing is left of it
+    assert fine == 0 and torch.equal(out, want) and (l is None or torch.equal(l, want_lse))
