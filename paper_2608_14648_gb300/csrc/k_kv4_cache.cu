@@ -393,7 +393,7 @@ __device__ __forceinline__ void store8_within(T *p, const float *v) {
     if constexpr (std::is_same<T, __half>::value) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
+        for (int i = 0; i < 4; ++i) w[i] = kv_f16_within(v[2 * i], v[2 * i + 1]);
         *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
         store8(p, v);

@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                         const __nv_bfloat162 y = __floats2bfloat162_rn(x0, x1);
                         w[i] = *reinterpret_cast<const uint32_t *>(&y);
                     } else {
-                        w[i] = pack(kv_within(x0, a.most), kv_within(x1, a.most));
+                        w[i] = kv_f16_within(x0, x1);
                     }
                 }
                 uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.out) + at * a.d + 16 * k);

@@ -525,8 +525,9 @@ struct MmaRows4 {
                 for (int w = 0; w < DC; ++w) {
                     if (!FULL && w >= a.d / KV_B) break;
                     const float x = o[t][w][i] * inv, y = o[t][w][i + 2] * inv;
-                    dst[16 * w] = bits16(bf ? x : kv_within(x, a.most), bf);
-                    dst[16 * w + 8] = bits16(bf ? y : kv_within(y, a.most), bf);
+                    const uint32_t u = kv_f16_within(x, y);
+                    dst[16 * w] = bf ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : (uint16_t)u;
+                    dst[16 * w + 8] = bf ? __bfloat16_as_ushort(__float2bfloat16_rn(y)) : (uint16_t)(u >> 16);
                 }
                 if (g == 0 && a.lse) a.lse[row] = l[t][i] == 0.0f ? -INFINITY : LN2 * (m[t][i] + log2f(l[t][i]));
             }

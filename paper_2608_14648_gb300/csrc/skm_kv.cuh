@@ -170,6 +170,12 @@ __device__ __forceinline__ void kv_store(void *x, int64_t i, float v, int dtype)
     else if (dtype == SKM_DTYPE_BF16) static_cast<__nv_bfloat16 *>(x)[i] = __float2bfloat16_rn(v);
     else static_cast<__half *>(x)[i] = __float2half_rn(v);
 }
+// two f16, beyond f16's largest numbers those; NaN stays
+__device__ __forceinline__ uint32_t kv_f16_within(float a, float b) {
+    uint32_t r;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
+}
 // brought into [-most, most]; NaN stays
 __device__ __forceinline__ float kv_within(float x, float most) { return x > most ? most : x < -most ? -most : x; }
 // two fp32 operations in one instruction
