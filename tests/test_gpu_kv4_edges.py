@@ -1,5 +1,5 @@
-"""The 4-bit key/value cache where weighted sums cancel, where its values end, where codes lie next to the middle of two, and
-where a wait runs out."""
+"""The 4-bit key/value cache where weighted sums cancel, where its values end, where codes lie next to the middle of two,
+where a wait runs out, and what the two operands of prompts' products hold."""
 from fractions import Fraction
 
 import pytest
@@ -169,3 +169,61 @@ def test_many_rows_that_give_up_say_so(cuda_ok, heads, group, d, typ, lse, rows,
     assert hits == {0, 1}
     out, l, fine = call()  # nothing is left of it
     assert fine == 0 and torch.equal(out, want) and (l is None or torch.equal(l, want_lse))
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("typ,lse", [("f16", False), ("f16", True), ("bf16", True)])
+def test_prompts_have_their_values_exactly(cuda_ok, d, typ, lse):
+    """Up to 128 dims: s (c - 8) as the sum of two f16.  Equal weights, three codes of 15 for seven of 5 and b = -8 s: the mean is
+    0, and what one f16 would leave of 7 s and of 3 s does not cancel.  Exact otherwise but for sums that tensor cores may truncate:
+    of n / 16 blocks and two operands, 17 terms each within 2^-23 of a partial sum, 70 s a weight at most."""
+    import paper_2608_14648_gb300 as skm
+
+    n, rows = 640, 48
+    s = torch.tensor(0.2998).half().double()
+    tol = float(2 / 16 * 17 * 2.0**-23 * 70 * s)
+    left = lambda k: float((k * s).half().double() - k * s)  # noqa: E731
+    assert abs(3 * left(7) + 7 * left(-3)) / 10 > 3 * tol  # one operand would be seen
+    c = make_cache(1, d, 64, n // 64)
+    code = torch.where(torch.arange(n) % 10 < 3, 15, 5).to(torch.uint8).view(n // 16, 16)
+    two = (code[:, :8] | code[:, 8:] << 4).view(n // 64, 1, 4, 1, 1, 4, 2, 1)  # [page][head][block][16 dims][g][token pair][token % 2][dim / 8]
+    c.blocks[..., 8 * d:16 * d].unflatten(-1, (d // 16, 8, 4, 2, 2)).copy_(two.cuda())
+    sc = scales(c)
+    sc[..., 2], sc[..., 3] = float(s), float(-8 * s)
+    Q = torch.zeros(rows, 1, d, dtype=DT[typ], device="cuda")
+    table = torch.arange(n // 64, dtype=torch.int32, device="cuda").view(1, -1)
+    assert Held4(c).code[1].reshape(-1, d)[:20].T.tolist() == [code.flatten()[:20].tolist()] * d
+    out, _ = skm.skm_kv4_attend(c, table, i32([n]), i32([0, rows]), Q, rows, n, causal=False, want_lse=lse)
+    assert out.double().abs().max() <= tol + 2.0**-25
+
+
+@pytest.mark.parametrize("d", [144, 192, 256])
+@pytest.mark.parametrize("typ,lse", [("f16", False), ("f16", True), ("bf16", True)])
+def test_prompts_of_wide_heads_have_their_weights_in_two_parts(cuda_ok, d, typ, lse):
+    """Above 128 dims: weights as the sum of two f16.  Tokens of equal elements (f16 numbers) and three weights, whose sums
+    cancel; bound: logits to 2^-20 (key and bias around 8 apart before they meet), 2^x to 2^-22, weights to 2^-22, and as above."""
+    import paper_2608_14648_gb300 as skm
+
+    n, rows, size = 768, 48, 0.55
+    # the keys' first dim has codes 0, 1, 2: logits 0, size, 2 size
+    x = torch.tensor([0.0, size, 2 * size], dtype=torch.float64).to(DT["f32"]).double()
+    p = torch.exp(x - x[2])
+    v = torch.tensor([1.0, 0, 0], dtype=torch.float64)
+    v[1] = (-v[0] * p[0] / p[1]).half()
+    v[2] = (-(v[0] * p[0] + v[1] * p[1]) / p[2]).half()
+    ref, A = float((p * v).sum() / p.sum()), float((p * v.abs()).sum() / p.sum())
+    tol = 2.0**-18 * A + 2 / 16 * 17 * 2.0**-23 + abs(ref) * 2.0**-8 + 2.0**-25
+    one = float(((128 * p).half().double() * v).sum() / (128 * p.sum()))
+    assert abs(one - ref) > 3 * tol  # weights in one f16 would be seen
+    c = make_cache(1, d, 64, n // 64)
+    c.blocks[..., :16 * d] = 0
+    kind = (torch.arange(n) % 3).view(n // 16, 16)
+    keys = c.blocks[..., :8 * d].view(n // 16, d // 16, 8, 4, 2, 2)
+    keys[:, 0, :, 0, 0, 0], keys[:, 0, :, 0, 0, 1] = kind[:, :8].to(torch.uint8).cuda(), kind[:, 8:].to(torch.uint8).cuda()
+    sc = scales(c).view(n // 16, 16, 4)
+    sc[..., 0], sc[..., 1], sc[..., 2], sc[..., 3] = 1.0, 0.0, 0.0, v[kind].half().cuda()
+    Q = torch.zeros(rows, 1, d, dtype=DT[typ], device="cuda")
+    Q[..., 0] = 1.0
+    table = torch.arange(n // 64, dtype=torch.int32, device="cuda").view(1, -1)
+    out, _ = skm.skm_kv4_attend(c, table, i32([n]), i32([0, rows]), Q, rows, n, causal=False, want_lse=lse, scale=size)
+    assert (out.double() - ref).abs().max() <= tol
