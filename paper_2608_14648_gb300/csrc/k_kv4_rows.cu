@@ -11,9 +11,10 @@
 // k_kv_rows.cu: the weights that become f16 then are p = e s_v, kept below 2^15 by the
 // reference m), l = sum p / s_v and the biases' sum is sum p (b_v / s_v), in fp32.
 //
-// The second product has codes less 8 (and b_v / s_v + 8): the weights' rounding is an error of the
-// codes' size, and tensor cores cut their sums off at every product, always downward for codes 0..15.  The mean of values that
-// nearly cancel lost all its bits so (1024 sequences of a million tokens: 2.7e-3 off where it was 2.0e-3, in any output type).
+// The second product has codes less 7.5 (and b_v / s_v + 7.5): the weights' rounding is an error of the codes' size.  Tensor
+// cores cut a sum off towards 0 at every product, by some 2^-20 of it, so an item's products start from 0 and are added to the
+// rows' sums in fp32 with rounding: a sum that every product of a stretch goes into loses 2^-20 of itself every 16 tokens, and with
+// codes 0..15 the mean of a million values that nearly cancel was 2.7e-3 off where it is 2.0e-3 (codes less 8: 3.1e-5).
 //
 // A key's code as an operand of the tensor cores costs half an instruction: four bits under a mask
 // are the f16 numbers 2^-24 c (bits 0..3) or 2^-20 c (bits 4..7), subnormal and
@@ -215,25 +216,17 @@ __device__ __forceinline__ void codes4_a(uint32_t w, uint32_t (&a)[4]) {
     a[3] = w & 0x00f000f0u;
 }
 constexpr float CODES_UP = 16777216.0f;   // 2^24
-// the same codes less 8, exact, from the f16 numbers 1024 + c and 1024 + 16 c (up: 1024 twice, in a register: with two
-// immediates the logical operation would be two)
-__device__ __forceinline__ void codes4_mid(uint32_t w, uint32_t up, uint32_t (&a)[4]) {
+// 2^-9 times the same codes less 7.5, exact: subnormal as they are, one fused multiply-add each
+constexpr float CENTRE = 7.5f, CENTRED_UP = 512.0f;  // 2^9
+__device__ __forceinline__ void codes4_centred(uint32_t w, uint32_t (&a)[4]) {
     const auto half2 = [](uint32_t x) { return *reinterpret_cast<const __half2 *>(&x); };
-    const auto low = [&](uint32_t x) {
-        uint32_t y;
-        asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(y) : "r"(x), "r"(up));  // and, or
-        const __half2 r = __hadd2(half2(y), half2(0xe408e408u));
+    const auto less = [&](uint32_t x, uint32_t up) {  // up: 2^15 or 2^11; 0xa380: -7.5 2^-9
+        const __half2 r = __hfma2(half2(x), half2(up), half2(0xa380a380u));
         return *reinterpret_cast<const uint32_t *>(&r);
     };
-    const auto high = [&](uint32_t x) {
-        uint32_t y;
-        asm("lop3.b32 %0, %1, 0x00f000f0, %2, 0xea;" : "=r"(y) : "r"(x), "r"(up));
-        const __half2 r = __hfma2(half2(y), half2(0x2c002c00u), half2(0xd480d480u));
-        return *reinterpret_cast<const uint32_t *>(&r);
-    };
-    a[0] = low(w), a[2] = high(w);
+    a[0] = less(w & 0x000f000fu, 0x78007800u), a[2] = less(w & 0x00f000f0u, 0x68006800u);
     w >>= 8;
-    a[1] = low(w), a[3] = high(w);
+    a[1] = less(w & 0x000f000fu, 0x78007800u), a[3] = less(w & 0x00f000f0u, 0x68006800u);
 }
 constexpr float SCALE_LEAST = 5.9604645e-8f;  // 2^-24, the smallest f16 above 0: a scale of 0 (then all codes are 0) counts as it
 
@@ -382,7 +375,7 @@ struct MmaRows4 {
                 float lv;
                 asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lv) : "f"(v));
                 asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(iv[n][k]) : "f"(v));
-                bv[n][k] = fmaf(sc.vb, iv[n][k], MIDDLE);
+                bv[n][k] = fmaf(sc.vb, iv[n][k], CENTRE);
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -455,8 +448,6 @@ struct MmaRows4 {
                 pb[n][t][0] = transpose8x8(*reinterpret_cast<const uint32_t *>(&lo));
                 pb[n][t][1] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hi));
             }
-        uint32_t up;
-        asm volatile("mov.b32 %0, 0x64006400;" : "=r"(up));
 #pragma unroll
         for (int w0 = 0; w0 < DC; w0 += 4) {
             if (w0 >= nc) break;
@@ -464,15 +455,27 @@ struct MmaRows4 {
 #pragma unroll
             for (int n = 0; n < NB; ++n) ldsm4(va + n * bytes + w0 * 128, r[n]);
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+            for (int i = 0; i < 4; ++i) {
+                const int w = w0 + i;
+                if (w >= DC || w >= nc) break;
+                float x[NT][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int w = w0 + i;
-                    if (w >= DC || w >= nc) break;
-                    codes4_mid(r[n][i], up, f);
+                for (int n = 0; n < NB; ++n) {
+                    codes4_centred(r[n][i], f);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) mma16816(o[t][w], f, pb[n][t][0], pb[n][t][1]);
+                    for (int t = 0; t < NT; ++t) {
+                        if (n == 0) x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.0f;
+                        mma16816(x[t], f, pb[n][t][0], pb[n][t][1]);
+                    }
                 }
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int k = 0; k < 4; k += 2) {
+                        const float2 y = add2(make_float2(o[t][w][k], o[t][w][k + 1]), make_float2(x[t][k], x[t][k + 1]));
+                        o[t][w][k] = y.x, o[t][w][k + 1] = y.y;
+                    }
+            }
         }
     }
 
@@ -488,8 +491,8 @@ struct MmaRows4 {
                 }
 #pragma unroll
                 for (int w = 0; w < DC; ++w) {
-                    o[t][w][i] += ob[t][i];
-                    o[t][w][i + 2] += ob[t][i];
+                    o[t][w][i] = fmaf(o[t][w][i], CENTRED_UP, ob[t][i]);
+                    o[t][w][i + 2] = fmaf(o[t][w][i + 2], CENTRED_UP, ob[t][i]);
                 }
             }
     }

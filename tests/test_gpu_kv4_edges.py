@@ -44,6 +44,34 @@ def test_long_sums_keep_their_precision(cuda_ok, typ):
     assert (out.double() - 2.0**-9).abs().max() <= tol
 
 
+@pytest.mark.parametrize("typ", ["bf16", "f16"])
+def test_long_sums_of_any_codes_keep_their_precision(cuda_ok, typ):
+    """As above with codes c and 15 - c of neighbouring tokens: a mean of b + 7.5 s = 2^-9, and sums of codes less 7.5 that are 0 after
+    every block (of codes less 8, half a code a token).  Above, of codes less 7.5, half a code a token too: no sum may lose bits to
+    every product that it takes."""
+    import paper_2608_14648_gb300 as skm
+
+    page, cols, d, batch = 16384, 64, 16, 1024
+    n = page * cols
+    c = skm.KVCache4(1, d, page, pages=cols)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    rand = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=g, dtype=torch.uint8, device="cuda")  # noqa: E731
+    c.blocks[..., :8 * d].view(-1, 8, 4, 2, 2).copy_(rand(0, 16, n // 16, 4, 1, 1, 2).repeat_interleave(2, 1) * 17)
+    values, two = c.blocks[..., 8 * d:16 * d].view(-1, 8, 4, 2, 2), rand(0, 256, n // 16, 8, 4, 2)
+    values[:, :, :, 0], values[:, :, :, 1] = two, 255 - two
+    sc = scales(c)
+    sc[..., 0], sc[..., 1], sc[..., 2], sc[..., 3] = 0.11, 0.0, 0.125, -0.9375 + 2.0**-9
+    Q = torch.zeros(batch, 4, d, dtype=DT[typ], device="cuda")
+    Q[..., 0] = torch.tensor([0.3, 1.0, -1.0, 2.0])
+    table = torch.arange(cols, dtype=torch.int32, device="cuda").expand(batch, cols).contiguous()
+    length, cu = torch.full((batch,), n, dtype=torch.int32, device="cuda"), torch.arange(batch + 1, dtype=torch.int32, device="cuda")
+    out, _ = skm.skm_kv4_attend(c, table, length, cu, Q, 1, n, scale=1.0)
+    u = {"bf16": 2.0**-8, "f16": 2.0**-11}[typ]
+    adds = 2 * batch * n // (152 * 16) // 16
+    tol = 2.0**-9 * (u + 2 * adds * 2.0**-24) + 2.0**-20 * 3
+    assert (out.double() - 2.0**-9).abs().max() <= tol
+
+
 # ---- values at f16's ends
 
 WIDE = 8736.0  # the smallest f16 s with -65504 + 15 s >= 65504: the largest code stands for 65536
