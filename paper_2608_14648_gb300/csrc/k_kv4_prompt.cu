@@ -5,18 +5,21 @@
 // (d > 128: one), and walks the keys they see in tiles of 64 positions; softmax warps of one
 // thread a row, converter warps, a warp for each row tile that issues its products.  Unlike there the
 // values' operands hold whole values, so l = sum p, and a tile's sum of weights
-// tells whether the reference m has to move.  Keys and values take one of three forms:
+// tells whether the reference m has to move.  Operands take one of four forms:
 //   ROUNDED  b + s c with one rounding to f16, 2^-11 (bf16 outputs without log-sum-exps, which do not show it): p = 2^(f S - m)
-//   SPLIT    s (c - 8) as the sum of two f16, a second operand beside the first.  Keys: b + 8 s as b + 4 s + 4 s in 16
-//            dims more, beside the row's sum in two f16: exact.  Values: b + 8 s rounded to f16 and added to the second
-//            operand with a rounding.  Twice the products and no more softmax
+//   SPLIT    (bf16 with log-sum-exps, d <= 128) s (c - 8) as the sum of two f16, a second operand beside the first.  Keys: b + 8 s
+//            as b + 4 s + 4 s in 16 dims more, beside the row's sum in two f16: exact.  Values: b + 8 s rounded to f16 and added to
+//            the second operand with a rounding.  Twice the products and no more softmax
+//   FINE     (f16 outputs, d <= 128) keys as in SPLIT; values s (c - 7.5) in two f16, and b + 7.5 s in fp32, p times it summed in
+//            the softmax; weights in two f16, a third product for the second
 //   SCALED   (d > 128, where SPLIT has no room) keys: codes less 8, exact, and t = f (s <q, c - 8> + (b + 8 s) sum q) in the
 //            softmax, two more operations a logit; values as in ROUNDED, but weights in two f16, a second operand too
-// f16 weights and f16 values are each as far off as an f16 output: SPLIT has the one, SCALED the other left.
-// Prompts of up to 4096, 16 heads of 64, f16: 113 us ROUNDED, 131 SPLIT, 175 SCALED (with weights in one f16); f16 outputs 1.4
-// times as far off an exact result as its rounding (with values in one f16 127 us, 1.6 times); log-sum-exps 1e-6 off (ROUNDED 2e-5).
-// 4 x 2048 tokens, 32 query heads on 8 of 128 dims: 176 us ROUNDED, 333 SPLIT (six converter warps and two stages, as shared
-// memory allows, make twice the operands); 16 on 8 of 192 dims: 263 ROUNDED, 312 SCALED.
+// f16 weights and f16 values are each as far off as an f16 output.  Off an exact result, in units of the output's rounding to f16
+// (1000 keys; 16000 in one CTA): FINE 1.01 and 1.13, SCALED 1.36 and 1.48, SPLIT for f16 outputs 1.41 and 1.44.  What grows with the
+// keys are the sums on tensor cores, which lose half a last bit to every product; codes less 7.5 keep them around 0 (less 8: 2.8 at 16000).
+// Prompts of up to 4096, 16 heads of 64: 113 us ROUNDED, 131 SPLIT, 170 FINE, 175 SCALED (with weights in one f16).  4 x 2048 tokens, 32
+// query heads on 8 of 128 dims: 176 us ROUNDED, 329 SPLIT (six converter warps and two stages, as shared memory allows, make
+// twice the operands), 391 FINE, 288 SCALED, whose values are rounded; 16 on 8 of 192 dims: 263 ROUNDED, 312 SCALED.
 //
 // What bounds it: the tensor cores, and what keeps them waiting.  A tile of 128 rows and 64 keys of 128 dims takes
 // 4 MFLOP; chunks of up to 2048 tokens behind 6144 (two sequences), 32 query heads on 8 of 128 dims, bf16: 270 us, 66% of cuBLAS's bf16 rate.  A
@@ -35,14 +38,16 @@ constexpr float TILE_MOST = 65000.0f;  // a tile's sum of weights: above it one 
 // when their softmax has handed over the tile two before: tile j + ST comes while it reads tile j - 1 at the earliest, 5 behind
 constexpr int INFO = 8;
 
-// The forms that keys take (above)
-enum Keys { ROUNDED, SPLIT, SCALED };
+// The forms of operands (above)
+enum Keys { ROUNDED, SPLIT, FINE, SCALED };
 
 // DH: dims, padded to 64, 128 or 256
 template <int DH, Keys KEYS>
 struct Lay {
     static constexpr int NQ = DH <= 128 ? 2 : 1;      // row tiles of a CTA
-    static constexpr int ST = DH == 64 || (DH == 128 && KEYS != SPLIT) ? 4 : 2;  // K and V tiles in flight
+    static constexpr bool TWO = KEYS == SPLIT || KEYS == FINE;  // keys and values in two operands
+    static constexpr bool LOW = KEYS == FINE || KEYS == SCALED;  // weights in two
+    static constexpr int ST = DH == 64 || (DH == 128 && !TWO) ? 4 : 2;  // K and V tiles in flight
     static constexpr int ROWS = NQ * QT;
     static_assert(ROWS == prompt_rows(DH));
     // converter warps.  A barrier's parity tells a phase from the next one only, so a warp may not come to a stage two rounds
@@ -58,17 +63,19 @@ struct Lay {
     static constexpr int LAUNCH_REGS = 65536 / ((THREADS + 127) / 128 * 128) / 8 * 8;
     static_assert(NQ == 1 || CONV_WARP0 * SOFT_REGS + (THREADS / 32 - CONV_WARP0) * REST_REGS <= THREADS / 32 * LAUNCH_REGS);
     static constexpr int QTILE = QT * DH * 2, TILE = KT * DH * 2;  // bytes of an operand of rows, of keys or values
-    // SPLIT: rests of keys and values behind them; rows' sums and keys' biases in 16 of 64 dims, those of the two row
+    // TWO: rests of keys and values behind them; rows' sums and keys' biases in 16 of 64 dims, those of the two row
     // tiles and of the stages in the same rows
-    static constexpr int QMORE = KEYS == SPLIT ? QT * 128 : 0, KMORE = KEYS == SPLIT ? KT * 128 : 0;
-    static constexpr int KTILE = KEYS == SPLIT ? 2 * TILE : TILE, VTILE = KTILE;
-    static_assert(KEYS != SPLIT || (NQ <= 4 && ST <= 4));
+    static constexpr int QMORE = TWO ? QT * 128 : 0, KMORE = TWO ? KT * 128 : 0;
+    static constexpr int KTILE = TWO ? 2 * TILE : TILE, VTILE = KTILE;
+    static_assert(!TWO || (NQ <= 4 && ST <= 4));
     static constexpr int q = 0, more = NQ * QTILE, kmore = more + QMORE, k = kmore + KMORE, v = k + ST * KTILE, bars = v + ST * VTILE;
     static constexpr int slots = bars + 8 * (6 * ST + 10);  // TMEM address, a flag, the part's index
     static constexpr int wild = (slots + 24 + 15) / 16 * 16;  // a byte a row: its query holds infinities or NaN
     static constexpr int there = wild + ROWS;  // a byte a block of the last INFO tiles: its page is present
-    static constexpr int keys = (there + INFO * KBLK + 63) / 64 * 64;  // (SCALED) [INFO][key scale, key at code 8][64 keys]
-    static constexpr int scales = keys + (KEYS == SCALED ? INFO * 2 * KT * 4 : 0);  // [converter warp][value scales, biases of 16 tokens]
+    // [INFO][64 keys]: (SCALED) the key's scale and its value at code 8, (FINE) the value at code 7.5
+    static constexpr int KEYED = KEYS == SCALED ? 2 * KT : KEYS == FINE ? KT : 0;
+    static constexpr int keys = (there + INFO * KBLK + 63) / 64 * 64;
+    static constexpr int scales = keys + INFO * KEYED * 4;  // [converter warp][value scales, biases of 16 tokens]
     // one CTA an SM: it takes all of TMEM
     static constexpr int bytes = scales + CONV * 64 + 1024, total = bytes > 120 * 1024 ? bytes : 120 * 1024;
     static_assert(total <= 227 * 1024);
@@ -130,11 +137,11 @@ __device__ __forceinline__ uint32_t u2(__half2 x) { return *reinterpret_cast<con
 // constants in registers: as immediates the two of one logical operation make it two (a third of the
 // converters' logical operations)
 struct Dequant {
-    uint32_t up, down, part, less, mid, mid_part;  // f16 pairs: 1024, -1024, 1/16, -64, -1032, -72
+    uint32_t up, down, part, less, mid, mid_part, centre, centre_part;  // f16 pairs: 1024, -1024, 1/16, -64, -1032, -72, -7.5, -71.5
     __device__ __forceinline__ Dequant() {
         asm volatile("mov.b32 %0, 0x64006400;\n\tmov.b32 %1, 0xe400e400;\n\tmov.b32 %2, 0x2c002c00;\n\tmov.b32 %3, 0xd400d400;\n\t"
-                     "mov.b32 %4, 0xe408e408;\n\tmov.b32 %5, 0xd480d480;"
-                     : "=r"(up), "=r"(down), "=r"(part), "=r"(less), "=r"(mid), "=r"(mid_part));
+                     "mov.b32 %4, 0xe408e408;\n\tmov.b32 %5, 0xd480d480;\n\tmov.b32 %6, 0xc780c780;\n\tmov.b32 %7, 0xd478d478;"
+                     : "=r"(up), "=r"(down), "=r"(part), "=r"(less), "=r"(mid), "=r"(mid_part), "=r"(centre), "=r"(centre_part));
     }
     template <bool HIGH>
     __device__ __forceinline__ __half2 bits(uint32_t w) const {
@@ -147,6 +154,12 @@ struct Dequant {
     __device__ __forceinline__ uint32_t codes(uint32_t w) const {
         const __half2 x = bits<HIGH>(w);
         return u2(HIGH ? __hfma2(x, h2(part), h2(mid_part)) : __hadd2(x, h2(mid)));
+    }
+    // c - 7.5, exactly
+    template <bool HIGH>
+    __device__ __forceinline__ uint32_t centred(uint32_t w) const {
+        const __half2 x = bits<HIGH>(w);
+        return u2(HIGH ? __hfma2(x, h2(part), h2(centre_part)) : __hadd2(__hadd2(x, h2(down)), h2(centre)));
     }
     // b + s c with one rounding.  BIG: no more than f16's largest number
     template <bool HIGH, bool BIG>
@@ -263,11 +276,11 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
     if (warp < CONV_WARP0) {  // ------------------------------------------ softmax
         const int q = warp >> 2, row = (warp & 3) * 32 + lane, r = r0 + q * QT + row, nt = tiles_for(q);
         const bool in = r < rows;
-        // SPLIT: rows of at most 2^7, so that their sums are f16's
+        // TWO: rows of at most 2^7, so that their sums are f16's
         float row_sum = 0.0f;
-        const float fac = load_rows<DH, KEYS != ROUNDED, KEYS == SPLIT ? 6 : 15>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE,
+        const float fac = load_rows<DH, KEYS != ROUNDED, L::TWO ? 6 : 15>(a, s, h, r0 + q * QT, (warp & 3) * 32, sm + L::q + q * L::QTILE,
                                                                                  lane, smem + L::wild + q * QT, &row_sum);
-        if constexpr (KEYS == SPLIT) {  // the sum in two f16, three times each, for (b, 4 s, 4 s) of a key twice
+        if constexpr (L::TWO) {  // the sum in two f16, three times each, for (b, 4 s, 4 s) of a key twice
             const __half top = __float2half_rn(row_sum), rest = __float2half_rn(row_sum - __half2float(top));
             const uint32_t to = sm + L::more + row * 128;
             st_shared(to + ((2 * q ^ (row & 7)) << 4), u2(__halves2half2(top, top)), u2(__halves2half2(top, rest)), u2(__halves2half2(rest, rest)), 0);
@@ -284,6 +297,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t S0 = tmem + lanes + q * 2 * KT, O = tmem + lanes + L::O + q * DH;
         float m = in ? M_NONE : -M_NONE, l = 0.0f;
+        [[maybe_unused]] float ob = 0.0f;  // (FINE) the sum of weights times values at code 7.5
         bool ok = true;
         const volatile uint32_t *there = reinterpret_cast<const volatile uint32_t *>(smem + L::there);
         for (int j = 0; j < nt; ++j) {
@@ -309,23 +323,24 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                 return bits;
             };
             uint32_t P[KT / 2];
-            [[maybe_unused]] uint32_t low_bits[KEYS == SCALED ? KT / 2 : 1];  // what the weights' rounding left
+            [[maybe_unused]] uint32_t low_bits[L::LOW ? KT / 2 : 1];  // what the weights' rounding left
             uint64_t sum[4] = {0, 0, 0, 0};
-            // (SCALED) a key's scale and its value at code 8
-            const float *scale = reinterpret_cast<const float *>(smem + L::keys) + (j & (INFO - 1)) * 2 * KT;
+            [[maybe_unused]] float2 mids = make_float2(0.0f, 0.0f);
+            // (SCALED) a key's scale and its value at code 8; (FINE) a value's at code 7.5
+            const float *scale = reinterpret_cast<const float *>(smem + L::keys) + (j & (INFO - 1)) * L::KEYED;
             // weights of 32 logits
             const auto weigh = [&](auto masked, int k0, uint32_t sees) {
                 const float2 f = make_float2(fac, fac), qs = make_float2(row_sum, row_sum), c = make_float2(-m, -m);
                 [[maybe_unused]] float4 s4[2], b4[2];  // of four keys, read while the four before are weighed
-                if constexpr (KEYS == SCALED) s4[0] = *reinterpret_cast<const float4 *>(scale + k0), b4[0] = *reinterpret_cast<const float4 *>(scale + KT + k0);
+                if constexpr (L::KEYED > 0) s4[0] = *reinterpret_cast<const float4 *>(scale + k0);
+                if constexpr (KEYS == SCALED) b4[0] = *reinterpret_cast<const float4 *>(scale + KT + k0);
 #pragma unroll
                 for (int i = k0; i < k0 + 32; i += 4) {
                     [[maybe_unused]] const int now = (i >> 2) & 1;
-                    if constexpr (KEYS == SCALED)
-                        if (i + 4 < k0 + 32) {
-                            s4[now ^ 1] = *reinterpret_cast<const float4 *>(scale + i + 4);
-                            b4[now ^ 1] = *reinterpret_cast<const float4 *>(scale + KT + i + 4);
-                        }
+                    if (i + 4 < k0 + 32) {
+                        if constexpr (L::KEYED > 0) s4[now ^ 1] = *reinterpret_cast<const float4 *>(scale + i + 4);
+                        if constexpr (KEYS == SCALED) b4[now ^ 1] = *reinterpret_cast<const float4 *>(scale + KT + i + 4);
+                    }
 #pragma unroll
                     for (int k = 0; k < 4; k += 2) {
                         const float2 x = make_float2(__uint_as_float(v[i + k]), __uint_as_float(v[i + k + 1]));
@@ -341,17 +356,22 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                             t.x = sees & 1u << (i + k - k0) ? t.x : -INFINITY;
                             t.y = sees & 2u << (i + k - k0) ? t.y : -INFINITY;
                         }
-                        if constexpr (KEYS == SCALED) {
+                        if constexpr (L::LOW) {
                             const float2 p = make_float2(ex2(t.x), ex2(t.y));
                             sum[(i + k) / 2 & 3] = add2(sum[(i + k) / 2 & 3], joined(p));
-                            const __half2 y = __floats2half2_rn(p.x, p.y);
-                            const float2 z = __half22float2(y);
-                            P[(i + k) / 2] = u2(y);
+                            // (the upper part cut off, not rounded: a logical operation on the way to what is left)
+                            const float2 z = make_float2(__uint_as_float(__float_as_uint(p.x) & 0xffffe000u), __uint_as_float(__float_as_uint(p.y) & 0xffffe000u));
+                            P[(i + k) / 2] = pack(z.x, z.y);
                             low_bits[(i + k) / 2] = pack(p.x - z.x, p.y - z.y);
+                            if constexpr (KEYS == FINE) mids = fma2(p, k ? make_float2(s4[now].z, s4[now].w) : make_float2(s4[now].x, s4[now].y), mids);
                         } else {
                             P[(i + k) / 2] = weights2(t.x, t.y, sum[(i + k) / 2 & 3]);
                         }
                     }
+                }
+                if constexpr (L::LOW) {  // at once, while the other half's logits wait in registers
+                    st16(S + k0 / 2, P + k0 / 2);
+                    st16(S + KT / 2 + k0 / 2, low_bits + k0 / 2);
                 }
             };
             const auto weigh_any = [&](int k0) {
@@ -391,6 +411,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                 const float g = ex2(m - to);
                 m = to;
                 l *= g;
+                if constexpr (KEYS == FINE) ob *= g;
                 if (j > 0) {
                     if (!(ok = warp_sleep(s_full(q, (j + 1) & 1), ((j + 1) >> 1) & 1, gone, a))) break;  // P V of tile j - 1 is through
                     fence_after();
@@ -405,16 +426,18 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                     }
                     st_wait();
                 }
+                if constexpr (L::LOW) st_wait();  // (over the weights that are there)
                 sum[0] = sum[1] = sum[2] = sum[3] = 0;
+                mids = make_float2(0.0f, 0.0f);
                 weigh(std::true_type{}, 0, visible(0));
                 weigh(std::true_type{}, 32, visible(32));
                 add = total();
             }
             l += add;
+            if constexpr (KEYS == FINE) ob += mids.x + mids.y;
+            if constexpr (!L::LOW) {
 #pragma unroll
-            for (int k = 0; k < KT / 2; k += 16) {
-                st16(S + k, P + k);
-                if constexpr (KEYS == SCALED) st16(S + KT / 2 + k, low_bits + k);
+                for (int k = 0; k < KT / 2; k += 16) st16(S + k, P + k);
             }
             st_wait();
             fence_before();
@@ -447,6 +470,10 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                 } else {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] = 0;
+                }
+                if constexpr (KEYS == FINE) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + ob);
                 }
                 if (!in) continue;
                 if (part) {
@@ -548,7 +575,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                             x[2 * i + 1] = dq.codes<true>(c[i] >> 8 * t);
                         }
                     }
-                    if constexpr (KEYS == SPLIT) {  // s (c - 8) in f16, and what its rounding left (s c at most twice f16's range)
+                    if constexpr (L::TWO) {  // s (c - 8) in f16, and what its rounding left (s c at most twice f16's range)
                         uint32_t rest[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -578,14 +605,16 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         uint32_t x[4];
-                        if constexpr (KEYS == SPLIT) {  // s (c - 8) in f16; what is left, exactly, and the value at code 8 in one
+                        if constexpr (L::TWO) {  // s (c - 8) in f16; what is left, exactly, and the value at code 8 in one.  FINE: s (c - 7.5), exactly
                             uint32_t rest[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const __half2 u = h2(half ? dq.codes<true>(c[i] >> 8 * t) : dq.codes<false>(c[i] >> 8 * t));
+                                const uint32_t w = c[i] >> 8 * t;
+                                const __half2 u = h2(KEYS == FINE ? (half ? dq.centred<true>(w) : dq.centred<false>(w)) : half ? dq.codes<true>(w) : dq.codes<false>(w));
                                 __half2 y = __hmul2(u, h2(s[i]));
                                 if constexpr (BIG) y = __hmax2(__hmin2(y, h2(0x7bff7bffu)), h2(0xfbfffbffu));
-                                rest[i] = u2(__hadd2(__hfma2(u, h2(s[i]), __hneg2(y)), h2(b[i])));
+                                const __half2 left = __hfma2(u, h2(s[i]), __hneg2(y));
+                                rest[i] = u2(KEYS == SPLIT ? __hadd2(left, h2(b[i])) : left);
                                 x[i] = u2(y);
                             }
                             st_shared((to + L::TILE + k * 8192 + t * 1024) ^ (16 * half), rest[0], rest[1], rest[2], rest[3]);
@@ -610,12 +639,16 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
             const int whose = j - ST < nt0 ? ask : nq - 1;
             if (!warp_sleep(k_free(whose, st), ((j / ST) & 1) ^ 1, gone, a)) break;
             if (lane == 0) smem[L::there + (j & (INFO - 1)) * KBLK + blk] = at >= 0;
-            if (KEYS == SPLIT && lane < KV_B) {  // (b, 4 s, 4 s) twice: eight s, but in f16's range
+            if (L::TWO && lane < KV_B) {  // (b, 4 s, 4 s) twice: eight s, but in f16's range
                 const __half2 sb = h2(ks[lane >> 3]);
                 const __half b = __high2half(sb), s4 = __hmul(__low2half(sb), __ushort_as_half(0x4400));
                 const uint32_t to = sm + L::kmore + (blk * KV_B + lane) * 128;
                 st_shared(to + ((2 * st ^ (lane & 7)) << 4), u2(__halves2half2(b, s4)), u2(__halves2half2(s4, b)), u2(__halves2half2(s4, s4)), 0);
                 st_shared(to + (((2 * st + 1) ^ (lane & 7)) << 4), 0, 0, 0, 0);
+            }
+            if (KEYS == FINE && lane < KV_B) {
+                const float2 sb = __half22float2(h2(vs));
+                reinterpret_cast<float *>(smem + L::keys)[(j & (INFO - 1)) * L::KEYED + blk * KV_B + lane] = fmaf(7.5f, sb.x, sb.y);
             }
             if (KEYS == SCALED && lane < 8) {
                 float *scale = reinterpret_cast<float *>(smem + L::keys) + (j & (INFO - 1)) * 2 * KT + blk * KV_B + g;
@@ -674,7 +707,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                                  idesc(KT), one);
             };
             dims(std::false_type{}, ka);
-            if constexpr (KEYS == SPLIT) {
+            if constexpr (L::TWO) {
                 dims(std::true_type{}, ka + (L::TILE >> 4));
                 mma_ss<true>(d, operand(sm + L::more) + 2 * q, operand(sm + L::kmore) + 2 * (j % ST), idesc(KT), one);
             }
@@ -696,11 +729,12 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
             const uint64_t va = v_op + (uint32_t)(j % ST) * (L::VTILE >> 4);
 #pragma unroll
             for (int k = 0; k < KT / 16; ++k) mma_ts(O, p + 8 * k, va + 2 * k, idesc(DH), k > 0 || j > 0, one);
-            if constexpr (KEYS != ROUNDED) {  // SPLIT: the values' rests; SCALED: the weights'
+            const auto more = [&](uint32_t w, uint64_t v) {
 #pragma unroll
-                for (int k = 0; k < KT / 16; ++k)
-                    mma_ts(O, p + (KEYS == SCALED ? KT / 2 : 0) + 8 * k, va + (KEYS == SPLIT ? L::TILE >> 4 : 0) + 2 * k, idesc(DH), 1, one);
-            }
+                for (int k = 0; k < KT / 16; ++k) mma_ts(O, p + w + 8 * k, v + 2 * k, idesc(DH), 1, one);
+            };
+            if constexpr (L::TWO) more(0, va + (L::TILE >> 4));  // the values' rests
+            if constexpr (L::LOW) more(KT / 2, va);  // the weights'
             commit(v_free(q, j % ST), one);
             if (j + 2 < nt) qk(j + 2);  // over the buffer that P V read, in order behind it
             commit(s_full(q, j & 1), one);
@@ -736,7 +770,9 @@ cudaError_t launch_kv4_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaSt
     // bf16 outputs hide the rounding of keys (both 1.7e-3 off); f16 ones and log-sum-exps would show it
     if (a.dtype == SKM_DTYPE_BF16 && !a.lse)
         return a.d <= 64 ? run_prompt<64, ROUNDED>(a, p, st) : a.d <= 128 ? run_prompt<128, ROUNDED>(a, p, st) : run_prompt<256, ROUNDED>(a, p, st);
-    return a.d <= 64 ? run_prompt<64, SPLIT>(a, p, st) : a.d <= 128 ? run_prompt<128, SPLIT>(a, p, st) : run_prompt<256, SCALED>(a, p, st);
+    if (a.d > 128) return run_prompt<256, SCALED>(a, p, st);
+    if (a.dtype == SKM_DTYPE_BF16) return a.d <= 64 ? run_prompt<64, SPLIT>(a, p, st) : run_prompt<128, SPLIT>(a, p, st);
+    return a.d <= 64 ? run_prompt<64, FINE>(a, p, st) : run_prompt<128, FINE>(a, p, st);
 }
 
 }  // namespace skm
