@@ -15,6 +15,8 @@
 // cores cut a sum off towards 0 at every product, by some 2^-20 of it, so an item's products start from 0 and are added to the
 // rows' sums in fp32 with rounding: a sum that every product of a stretch goes into loses 2^-20 of itself every 16 tokens, and with
 // codes 0..15 the mean of a million values that nearly cancel was 2.7e-3 off where it is 2.0e-3 (codes less 8: 3.1e-5).
+// For f16 outputs weights are two f16, a second product with the same codes: with one they are 1.1 to 1.56 times as far off an
+// exact result as their rounding (60 cases of any sizes), with two 1.00 times.  bf16 outputs hide the rounding of one (1.01 times).
 //
 // A key's code as an operand of the tensor cores costs half an instruction: four bits under a mask
 // are the f16 numbers 2^-24 c (bits 0..3) or 2^-20 c (bits 4..7), subnormal and
@@ -22,11 +24,12 @@
 // 16 between the two lies on the other operand (half of a query's dims carry 2^-4), 2^24 on the
 // results.  A logit has at most 16 such products.
 //
-// What bounds it, with a batch that fills the machine: the latencies of four warps a scheduler (issue slots 57%, ALU 53%
-// taken) before HBM.  96 sequences of up to 10001 tokens, 8 heads of 128 dims, 4 query rows each, bf16: 119 us, 67% of a
-// copy's rate (79.9 us for the bytes); 546 instructions an item of two blocks, 160 of them make operands of codes, 32 are
-// products.  Items of two blocks share masks, maxima and the walk (138 -> 129 us), queries' operands lie in shared memory
-// where registers would spill (129 -> 118).  A long sequence, f16, 262151 tokens: 66 us (42.2), of which codes less 8 are 4.
+// What bounds it, with a batch that fills the machine: the latencies of four warps a scheduler before HBM.
+// 96 sequences of up to 10001 tokens, 8 heads of 128 dims, 4 query rows each, bf16: 127 us, 63% of a
+// copy's rate (79.9 us for the bytes); with codes 0..15 summed without a rounding 119 us, codes less 7.5 cost 5 of the difference, the
+// additions 2, and the f16 form's registers 1.5.  Items of two blocks share masks, maxima and the walk (138 -> 129 us), queries'
+// operands lie in shared memory where registers would spill (129 -> 118).  A long sequence, f16, 262151 tokens: 74 us (42.2), with weights
+// in one f16 66.
 #include "skm_kv_rows.cuh"
 
 namespace skm {
@@ -247,8 +250,10 @@ struct MmaRows4 {
     uint32_t q[QMEM ? 1 : NT][QMEM ? 1 : DC][2];
     uint2 *qmem;
     int2 *lim;
+    bool fine;  // f16 outputs
 
     __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int h, int r0, uint8_t *mem, int lane) {
+        fine = a.dtype == SKM_DTYPE_F16;
         const int g = lane >> 2, c = lane & 3, nc = FULL ? DC : a.d / KV_B;
         lim = reinterpret_cast<int2 *>(mem);
         qmem = reinterpret_cast<uint2 *>(mem + LIMITS<RT>);
@@ -434,49 +439,68 @@ struct MmaRows4 {
                 }
             weigh();
         }
-        uint32_t pb[NB][NT][2];
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     l[t][i] = fmaf(p[n][t][i + 2], iv[n][1], fmaf(p[n][t][i], iv[n][0], l[t][i]));
                     ob[t][i] = fmaf(p[n][t][i + 2], bv[n][1], fmaf(p[n][t][i], bv[n][0], ob[t][i]));
                 }
-                const __half2 lo = __floats2half2_rn(p[n][t][0], p[n][t][1]), hi = __floats2half2_rn(p[n][t][2], p[n][t][3]);
-                pb[n][t][0] = transpose8x8(*reinterpret_cast<const uint32_t *>(&lo));
-                pb[n][t][1] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hi));
-            }
+        const auto sums = [&](auto two) {
+            constexpr bool TWO = decltype(two)::value;
+            uint32_t pb[NB][NT][2];
+            [[maybe_unused]] uint32_t pl[TWO ? NB : 1][NT][2];
 #pragma unroll
-        for (int w0 = 0; w0 < DC; w0 += 4) {
-            if (w0 >= nc) break;
-            uint32_t r[NB][4], f[4];
-#pragma unroll
-            for (int n = 0; n < NB; ++n) ldsm4(va + n * bytes + w0 * 128, r[n]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int w = w0 + i;
-                if (w >= DC || w >= nc) break;
-                float x[NT][4];
-#pragma unroll
-                for (int n = 0; n < NB; ++n) {
-                    codes4_centred(r[n][i], f);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        if (n == 0) x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.0f;
-                        mma16816(x[t], f, pb[n][t][0], pb[n][t][1]);
-                    }
-                }
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int k = 0; k < 4; k += 2) {
-                        const float2 y = add2(make_float2(o[t][w][k], o[t][w][k + 1]), make_float2(x[t][k], x[t][k + 1]));
-                        o[t][w][k] = y.x, o[t][w][k + 1] = y.y;
+                    for (int k = 0; k < 2; ++k) {
+                        float2 y = make_float2(p[n][t][2 * k], p[n][t][2 * k + 1]);
+                        if constexpr (TWO) {  // the upper part cut off, and what is left
+                            const float2 z = make_float2(__uint_as_float(__float_as_uint(y.x) & 0xffffe000u), __uint_as_float(__float_as_uint(y.y) & 0xffffe000u));
+                            const __half2 rest = __floats2half2_rn(y.x - z.x, y.y - z.y);
+                            pl[n][t][k] = transpose8x8(*reinterpret_cast<const uint32_t *>(&rest));
+                            y = z;
+                        }
+                        const __half2 w = __floats2half2_rn(y.x, y.y);
+                        pb[n][t][k] = transpose8x8(*reinterpret_cast<const uint32_t *>(&w));
                     }
+#pragma unroll
+            for (int w0 = 0; w0 < DC; w0 += 4) {
+                if (w0 >= nc) break;
+                uint32_t r[NB][4], f[4];
+#pragma unroll
+                for (int n = 0; n < NB; ++n) ldsm4(va + n * bytes + w0 * 128, r[n]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int w = w0 + i;
+                    if (w >= DC || w >= nc) break;
+                    float x[NT][4];
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        codes4_centred(r[n][i], f);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            if (n == 0) x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.0f;
+                            mma16816(x[t], f, pb[n][t][0], pb[n][t][1]);
+                            if constexpr (TWO) mma16816(x[t], f, pl[n][t][0], pl[n][t][1]);
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int k = 0; k < 4; k += 2) {
+                            const float2 y = add2(make_float2(o[t][w][k], o[t][w][k + 1]), make_float2(x[t][k], x[t][k + 1]));
+                            o[t][w][k] = y.x, o[t][w][k + 1] = y.y;
+                        }
+                }
             }
-        }
+        };
+        if (fine) sums(std::true_type{});
+        else sums(std::false_type{});
     }
 
     __device__ __forceinline__ void close(int) {

@@ -289,3 +289,38 @@ def test_f16_prompts_have_their_weights_in_two_f16(cuda_ok, d, n, group, rows):
     table = torch.arange(n // 16, dtype=torch.int32, device="cuda").view(1, -1)
     out, _ = skm.skm_kv4_attend(c, table, i32([n]), i32([0, rows]), Q, rows, n, causal=False, scale=size)
     assert (out.double() - ref).abs().max() <= tol
+
+
+@pytest.mark.parametrize("d", [16, 64, 96, 128, 144, 256])
+@pytest.mark.parametrize("n,group,rows", [(768, 1, 1), (768, 4, 3), (3840, 8, 1), (48, 1, 1), (768, 8, 4), (48000, 4, 2)])
+def test_f16_rows_have_their_weights_in_two_f16(cuda_ok, d, n, group, rows):
+    """As above for few rows, whose weights carry the value's scale: the scales' logarithms and reciprocals are good to 2^-22 more,
+    b / s + 7.5 to 2^-23 of 7.5, which is within 2^-18 of sum p |v| still."""
+    import paper_2608_14648_gb300 as skm
+
+    size = 0.55
+    x = torch.tensor([0.0, size, 2 * size], dtype=torch.float64).float().double()
+    p = torch.exp(x - x[2])
+    v = torch.tensor([1.0, 0, 0], dtype=torch.float64)
+    v[1] = (-v[0] * p[0] / p[1]).half()
+    v[2] = (-(v[0] * p[0] + v[1] * p[1]) / p[2]).half()
+    ref, A = float((p * v).sum() / p.sum()), float((p * v.abs()).sum() / p.sum())
+    tol = 2.0**-18 * A + 2 / 16 * 17 * 2.0**-23 + abs(ref) * 2.0**-11 + 2.0**-25
+    w = p * v.abs()
+    one = (w * 128 / w.max()).half().double() * w.max() / 128  # the largest is 2^7
+    assert abs(float((one * v.sign()).sum() / p.sum()) - ref) > 3 * tol  # weights in one f16 would be seen
+    c = make_cache(1, d, 16, n // 16)
+    c.blocks[..., :8 * d] = 0
+    kind = (torch.arange(n) % 3).view(n // 16, 16)
+    keys = c.blocks[..., :8 * d].view(n // 16, d // 16, 8, 4, 2, 2)
+    keys[:, 0, :, 0, 0, 0], keys[:, 0, :, 0, 0, 1] = kind[:, :8].to(torch.uint8).cuda(), kind[:, 8:].to(torch.uint8).cuda()
+    code = torch.where(v > 0, 9, 7)[kind].to(torch.uint8)
+    two = (code[:, :8] | code[:, 8:] << 4).view(n // 16, 1, 1, 4, 2, 1).cuda()  # [block][16 dims][g][token pair][token % 2][dim / 8]
+    c.blocks[..., 8 * d:16 * d].view(n // 16, d // 16, 8, 4, 2, 2).copy_(two)
+    sc, s = scales(c).view(n // 16, 16, 4), v.abs()[kind].half().cuda()
+    sc[..., 0], sc[..., 1], sc[..., 2], sc[..., 3] = 1.0, 0.0, s, -8 * s
+    Q = torch.zeros(rows, group, d, dtype=torch.float16, device="cuda")
+    Q[..., 0] = 1.0
+    table = torch.arange(n // 16, dtype=torch.int32, device="cuda").view(1, -1)
+    out, _ = skm.skm_kv4_attend(c, table, i32([n]), i32([0, rows]), Q, rows, n, causal=False, scale=size)
+    assert (out.double() - ref).abs().max() <= tol
