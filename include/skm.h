@@ -919,14 +919,15 @@ int skm_kv4_read(const skm_kv4_cache *c, const skm_kv_seqs *s, int dtype, void *
 
 /* Attention of query rows over the cache: rows, masks, outputs, status and workspaces as for
  * skm_kv_attend (the workspace from skm_kv4_attend_workspace_size).  dtype BF16 or F16: products on
- * tensor cores, sums and softmax in fp32, weights rounded to f16.  Query rows become f16 by a power of two
- * a row: elements below 2^-25 (F16) or 2^-28 (BF16) of the row's largest lose bits, those below 2^-36
+ * tensor cores, sums and softmax in fp32, weights rounded to f16 (BF16) or to 2^-21 of themselves (F16).  Query rows become f16 by a
+ * power of two a row: elements below 2^-25 (F16) or 2^-28 (BF16) of the row's largest lose bits, those below 2^-36
  * vanish.  Calls of more than 32 rows a sequence (tokens x heads of a group; d > 128: of more keys too)
  * run on another kernel.  For BF16 outputs without lse it takes keys and values rounded to f16 (2^-11 of each; b + 15 s above
- * f16's largest number as that number).  Otherwise it takes keys as they are and, d <= 128, values with b + 8 s rounded to
- * f16 and a rounding of 2^-11 of that, d > 128, values rounded to f16 and weights to 2^-22; d <= 128: elements of a query
- * row below 2^-20 (F16) or 2^-23 (BF16) of its largest lose bits there and those below 2^-32 vanish.  F32: fp32 arithmetic
- * throughout.  F16 outputs beyond f16's largest numbers are those.
+ * f16's largest number as that number).  Otherwise it takes keys as they are and, d <= 128, values as they are (F16) or
+ * with b + 8 s rounded to f16 and a rounding of 2^-11 of that (BF16), d > 128, values rounded to f16 and weights to 2^-21; d <= 128:
+ * elements of a query row below 2^-20 (F16) or 2^-23 (BF16) of its largest lose bits there and those below 2^-32 vanish.  So lse changes
+ * a BF16 prompt's last bits, and its time: up to twice as long.  Sums of many rows lose up to 2^-24 of themselves to every 16 keys
+ * that a CTA takes.  F32: fp32 arithmetic throughout.  F16 outputs beyond f16's largest numbers are those.
  * The result does not depend on timing.  Asynchronous. */
 size_t skm_kv4_attend_workspace_size(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a);
 int skm_kv4_attend(const skm_kv4_cache *c, const skm_kv_seqs *s, const skm_kv_attn *a, void *ws, size_t ws_bytes,

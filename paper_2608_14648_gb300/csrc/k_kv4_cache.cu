@@ -2,9 +2,9 @@
 //
 // A token's key (or value) of a head is one LVQ vector: bias b, the largest f16 not above its
 // smallest element, scale s, the smallest f16 with b + 15 s not below its largest, codes
-// rint((x - b) / s).  One warp takes one block (16 tokens) of one head's keys or values and holds
-// it in registers, so the input is read once: smallest and largest in registers and over a few lanes, then
-// the codes.  A vector's codes depend on nothing else: what the block holds is never rounded again.
+// rint((x - b) / s).  One warp takes one block (16 tokens) of one head's keys or values: a first pass for smallest and
+// largest, in registers and over a few lanes, a second one, out of L1, for the codes (HBM is read once).
+// A vector's codes depend on nothing else: what the block holds is never rounded again.
 //
 // Lanes.  Ranges, and keys' codes: (g, c), tokens g and g + 8, of every 32 dims the eight from 8 c on: a token's 32 dims
 // are 64 consecutive bytes of 16-bit input, and the lane's codes are two neighbouring words.
@@ -20,7 +20,7 @@
 // beside 2^23, exact), two at a time.
 //
 // What bounds them.  Writing: instructions (a value's code takes 10 in packed pairs, its place in a word 2 more; issue
-// slots 57% taken) and reads that not enough warps wait for; 12 prompts of up to 2500 tokens, 8 heads of 128 dims, bf16: 42
+// slots 55% taken) and reads that not enough warps wait for; 12 prompts of up to 2500 tokens, 8 heads of 128 dims, bf16: 42
 // us and 2.6 TB/s of the kernel, 65 us with reading back.  Quotients as divisions, or corrected everywhere, and zeros for rows
 // that are not new took 71; two, four and eight heads a warp with the next one's rows prefetched 69, 72 and 78 (their
 // loop's registers are too many).  Reading: HBM; 4 sequences of up to 32768 tokens, 82 us, 93% of a copy's rate.

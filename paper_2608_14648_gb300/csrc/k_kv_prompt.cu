@@ -542,14 +542,17 @@ cudaError_t run_prompt(const KvAttnArgs &a, const KvPromptPlan &p, cudaStream_t 
 // other one has an SM for every unit and few keys a unit.  At d = 256 (alone in a graph), 40 rows of 16
 // sequences, 2 heads (96 units there): 905 keys 26.7 us here and 21.7 there, 1280 24.8 and 25.3, 1400 26.1 and
 // 26.3, 1905 28.2 and 32.1; 16 sequences, 8 heads, 905 keys 35 and 62.  Of 12 units the other one stays ahead (1905 keys
-// 24.8 and 18.5, in shared stretches), which the rule does not use.
+// 24.8 and 18.5, in shared stretches), which the rule does not use.  The 4-bit cache, bf16, 192 and 256 dims, 40 rows, 32 units: 640 keys 23
+// us here and 18.5 there, 1280 24.4 and 24.5, 2560 32 and 39; 8 units 1280 22.8 and 22.7, 2560 24.9 and 22.3; one unit 2560 24.4 and 22.4.
 bool kv_prompt_ok(int dtype, int nb, int heads, int d, int64_t rows, int64_t span) {
     if (dtype == SKM_DTYPE_F32 || rows <= KV_ROWS_MOST) return false;
     return d <= 128 || span > 1280 || (int64_t)nb * heads * cdiv(rows, (int64_t)16) > KV_SMS;
 }
 
 // Keys a split has at least: a second kernel joins the parts (with 256, 96 rows that
-// see 512 keys took 21 us instead of 17; with 512, 40 rows that see 1045 32 instead of 28)
+// see 512 keys took 21 us instead of 17; with 512, 40 rows that see 1045 32 instead of 28).  The 4-bit cache's kernel takes it
+// over: 2 units of 40 and 96 rows, bf16, 64 and 128 dims, that see 512 keys take 11.2 to 14.4 us with 320 and 12.0 to 15.7 with 160, that see
+// 1045 13.4 to 17.3, with 160 12.4 to 16.1, with 640 15.9 to 19.7.  Its exact forms would rather have 160: 512 keys 22.7 and 18.3.
 constexpr int64_t SPLIT_KEYS = 320;
 
 size_t kv_prompt_part_most(int d, int64_t span) {

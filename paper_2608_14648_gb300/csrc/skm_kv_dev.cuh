@@ -1,5 +1,5 @@
 // Device helpers of the attention kernels over the 8-bit cache (k_kv_rows.cu,
-// k_kv_prompt.cu).
+// k_kv_prompt.cu) and the 4-bit one (k_kv4_rows.cu, k_kv4_prompt.cu).
 #pragma once
 #include "skm_kv.cuh"
 

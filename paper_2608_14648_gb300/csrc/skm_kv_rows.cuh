@@ -727,7 +727,9 @@ cudaError_t run_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) 
 // long that it had better be shared.  16-bit queries, 4 heads a group, d = 128
 // (alone in a graph): 8 units of 121 keys take 8 us against 12 in shared stretches,
 // of 1001 both 12, of 1901 16 against 14; 128 units of 1901 17 against 20; 512 units of 121
-// keys, more than a wave, 28 against 13, 192 of 1001 23 against 19.
+// keys, more than a wave, 28 against 13, 192 of 1001 23 against 19.  Over the 4-bit cache: 8 to 128 units of 121, 500 and 1001
+// keys 9, 10 and 11.5 against 17, 13 and 12.5, of 1901 14.5 both, 128 of them 15 against 19; 512 of 121, 500 and 1001 31, 35
+// and 42 against 18, 22 and 28.
 constexpr int64_t WHOLE_FEW = 64, WHOLE_KEYS = 1024, WHOLE_KEYS_MANY = 2048;
 bool whole_units(int64_t units, int64_t span) {
     return units <= KV_SMS && span <= (units <= WHOLE_FEW ? WHOLE_KEYS : WHOLE_KEYS_MANY);
