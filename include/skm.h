@@ -923,7 +923,7 @@ int skm_kv4_read(const skm_kv4_cache *c, const skm_kv_seqs *s, int dtype, void *
  * power of two a row: elements below 2^-25 (F16) or 2^-28 (BF16) of the row's largest lose bits, those below 2^-36
  * vanish.  Calls of more than 32 rows a sequence (tokens x heads of a group; d > 128: of more keys too)
  * run on another kernel.  For BF16 outputs without lse it takes keys and values rounded to f16 (2^-11 of each; b + 15 s above
- * f16's largest number as that number).  Otherwise it takes keys as they are and, d <= 128, values as they are (F16) or
+ * f16's largest number as that number).  Otherwise it takes keys as they are and, d <= 128, values as they are (F16, to 2^-25) or
  * with b + 8 s rounded to f16 and a rounding of 2^-11 of that (BF16), d > 128, values rounded to f16 and weights to 2^-21; d <= 128:
  * elements of a query row below 2^-20 (F16) or 2^-23 (BF16) of its largest lose bits there and those below 2^-32 vanish.  So lse changes
  * a BF16 prompt's last bits, and its time: up to twice as long.  Sums of many rows lose up to 2^-24 of themselves to every 16 keys

@@ -15,7 +15,7 @@
 //   SCALED   (d > 128, where SPLIT has no room) keys: codes less 8, exact, and t = f (s <q, c - 8> + (b + 8 s) sum q) in the
 //            softmax, two more operations a logit; values as in ROUNDED, but weights in two f16, a second operand too
 // f16 weights and f16 values are each as far off as an f16 output.  Off an exact result, in units of the output's rounding to f16
-// (1000 keys; 16000 in one CTA): FINE 1.01 and 1.13, SCALED 1.36 and 1.48, SPLIT for f16 outputs 1.41 and 1.44.  What grows with the
+// (1000 keys; 16000 in one CTA): FINE 1.00 and 1.04, SCALED 1.36 and 1.49, SPLIT for f16 outputs 1.41 and 1.44.  What grows with the
 // keys are the sums on tensor cores, which lose half a last bit to every product; codes less 7.5 keep them around 0 (less 8: 2.8 at 16000).
 // Prompts of up to 4096, 16 heads of 64: 113 us ROUNDED, 131 SPLIT, 170 FINE, 175 SCALED (with weights in one f16).  4 x 2048 tokens, 32
 // query heads on 8 of 128 dims: 176 us ROUNDED, 329 SPLIT (six converter warps and two stages, as shared memory allows, make
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
                 return bits;
             };
             uint32_t P[KT / 2];
-            [[maybe_unused]] uint32_t low_bits[L::LOW ? KT / 2 : 1];  // what the weights' rounding left
+            [[maybe_unused]] uint32_t low_bits[L::LOW ? KT / 2 : 1];  // what is left of the weights
             uint64_t sum[4] = {0, 0, 0, 0};
             [[maybe_unused]] float2 mids = make_float2(0.0f, 0.0f);
             // (SCALED) a key's scale and its value at code 8; (FINE) a value's at code 7.5
@@ -605,7 +605,8 @@ __global__ void __launch_bounds__(Lay<DH, KEYS>::THREADS, 1)
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         uint32_t x[4];
-                        if constexpr (L::TWO) {  // s (c - 8) in f16; what is left, exactly, and the value at code 8 in one.  FINE: s (c - 7.5), exactly
+                        if constexpr (L::TWO) {  // s (c - 8) in f16; what is left, exactly, and the value at code 8 in one.  FINE: s (c - 7.5),
+                                                // exactly but for 2^-25 where s is below 2^-13
                             uint32_t rest[4];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
