@@ -25,9 +25,9 @@
 // results.  A logit has at most 16 such products.
 //
 // What bounds it, with a batch that fills the machine: the latencies of four warps a scheduler before HBM.
-// 96 sequences of up to 10001 tokens, 8 heads of 128 dims, 4 query rows each, bf16: 127 us, 63% of a
-// copy's rate (79.9 us for the bytes); with codes 0..15 summed without a rounding 119 us, codes less 7.5 cost 5 of the difference, the
-// additions 2, and the f16 form's registers 1.5.  Items of two blocks share masks, maxima and the walk (138 -> 129 us), queries'
+// 96 sequences of up to 10001 tokens, 8 heads of 128 dims, 4 query rows each, bf16: 124 us, 65% of a
+// copy's rate (79.9 us for the bytes), 119 with codes 0..15 summed without a rounding.  bf16 and f16 are kernels of their own: in one, the
+// second weights' registers cost bf16 calls 2 to 10% (20 rows 73 us, 66 now).  Items of two blocks share masks, maxima and the walk (138 -> 129 us), queries'
 // operands lie in shared memory where registers would spill (129 -> 118).  A long sequence, f16, 262151 tokens: 74 us (42.2), with weights
 // in one f16 66.
 #include "skm_kv_rows.cuh"
@@ -56,7 +56,7 @@ __device__ __forceinline__ float code(uint32_t u) { return __uint_as_float((u & 
 template <int R, int DPL>
 struct Fp32Rows4 {
     static constexpr int RT = R, D4 = DPL > 4 ? 2 : 1;
-    static constexpr bool ONE_D = false, FOUR = true;
+    static constexpr bool ONE_D = false, FOUR = true, HALF = false;
     static constexpr size_t __host__ __device__ scratch(int d) { return (size_t)R * (d + KV_B) * 4 + LIMITS<R>; }
     float o[R][DPL], m[R], l[R], ob[R], qs[R];  // ob: the biases' sum, qs: the query's
     float *q, *p;
@@ -238,31 +238,28 @@ constexpr float SCALE_LEAST = 5.9604645e-8f;  // 2^-24, the smallest f16 above 0
 // brings the words of four chunks.  Queries, of either type, become f16 after scaling a row by a power of two
 // that takes its largest element to [2^15, 2^16) (to_f16), dims 4c + 2, 4c + 3 with 2^-4 on top: bf16
 // elements down to 2^-28 of the row's largest and f16 ones down to 2^-25 take part exactly.
-// DC: 16-dim chunks at most (FULL: exactly), NT: tiles of 8 rows.
-template <int DC, int NT, bool FULL>
+// DC: 16-dim chunks at most (FULL: exactly), NT: tiles of 8 rows, F16: queries and outputs are f16, else bf16.
+template <int DC, int NT, bool FULL, bool F16>
 struct MmaRows4 {
     static constexpr int RT = 8 * NT;
     static constexpr int D4 = DC > 8 ? 2 : 1;
-    static constexpr bool ONE_D = FULL, FOUR = true;
+    static constexpr bool ONE_D = FULL, FOUR = true, HALF = F16;
     static constexpr bool QMEM = NT * DC >= 8;  // the queries' operands wait in shared memory (decode batch 118 us, in registers 129)
     static constexpr size_t __host__ __device__ scratch(int) { return (QMEM ? (size_t)NT * DC * 2 * 32 * 4 : 0) + LIMITS<RT>; }
     float o[NT][DC][4], m[NT][2], l[NT][2], ob[NT][2], fac[NT][2], qs[NT][2];
     uint32_t q[QMEM ? 1 : NT][QMEM ? 1 : DC][2];
     uint2 *qmem;
     int2 *lim;
-    bool fine;  // f16 outputs
 
     __device__ __forceinline__ void begin(const KvAttnArgs &a, const Seq &s, int h, int r0, uint8_t *mem, int lane) {
-        fine = a.dtype == SKM_DTYPE_F16;
         const int g = lane >> 2, c = lane & 3, nc = FULL ? DC : a.d / KV_B;
         lim = reinterpret_cast<int2 *>(mem);
         qmem = reinterpret_cast<uint2 *>(mem + LIMITS<RT>);
         __syncwarp();
         limits<RT>(a, s, r0, lim, lane);
-        const bool bf = a.dtype == SKM_DTYPE_BF16;
         const auto pair = [&](uint32_t w) {
-            if (bf) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-            return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+            if constexpr (!F16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+            else return __half22float2(*reinterpret_cast<const __half2 *>(&w));
         };
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -448,59 +445,54 @@ struct MmaRows4 {
                     l[t][i] = fmaf(p[n][t][i + 2], iv[n][1], fmaf(p[n][t][i], iv[n][0], l[t][i]));
                     ob[t][i] = fmaf(p[n][t][i + 2], bv[n][1], fmaf(p[n][t][i], bv[n][0], ob[t][i]));
                 }
-        const auto sums = [&](auto two) {
-            constexpr bool TWO = decltype(two)::value;
-            uint32_t pb[NB][NT][2];
-            [[maybe_unused]] uint32_t pl[TWO ? NB : 1][NT][2];
+        uint32_t pb[NB][NT][2];
+        [[maybe_unused]] uint32_t pl[F16 ? NB : 1][NT][2];
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float2 y = make_float2(p[n][t][2 * k], p[n][t][2 * k + 1]);
+                    if constexpr (F16) {  // the upper part cut off, and what is left
+                        const float2 z = make_float2(__uint_as_float(__float_as_uint(y.x) & 0xffffe000u), __uint_as_float(__float_as_uint(y.y) & 0xffffe000u));
+                        const __half2 rest = __floats2half2_rn(y.x - z.x, y.y - z.y);
+                        pl[n][t][k] = transpose8x8(*reinterpret_cast<const uint32_t *>(&rest));
+                        y = z;
+                    }
+                    const __half2 w = __floats2half2_rn(y.x, y.y);
+                    pb[n][t][k] = transpose8x8(*reinterpret_cast<const uint32_t *>(&w));
+                }
+#pragma unroll
+        for (int w0 = 0; w0 < DC; w0 += 4) {
+            if (w0 >= nc) break;
+            uint32_t r[NB][4], f[4];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) ldsm4(va + n * bytes + w0 * 128, r[n]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int w = w0 + i;
+                if (w >= DC || w >= nc) break;
+                float x[NT][4];
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
+                    codes4_centred(r[n][i], f);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        if (n == 0) x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.0f;
+                        mma16816(x[t], f, pb[n][t][0], pb[n][t][1]);
+                        if constexpr (F16) mma16816(x[t], f, pl[n][t][0], pl[n][t][1]);
+                    }
+                }
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        float2 y = make_float2(p[n][t][2 * k], p[n][t][2 * k + 1]);
-                        if constexpr (TWO) {  // the upper part cut off, and what is left
-                            const float2 z = make_float2(__uint_as_float(__float_as_uint(y.x) & 0xffffe000u), __uint_as_float(__float_as_uint(y.y) & 0xffffe000u));
-                            const __half2 rest = __floats2half2_rn(y.x - z.x, y.y - z.y);
-                            pl[n][t][k] = transpose8x8(*reinterpret_cast<const uint32_t *>(&rest));
-                            y = z;
-                        }
-                        const __half2 w = __floats2half2_rn(y.x, y.y);
-                        pb[n][t][k] = transpose8x8(*reinterpret_cast<const uint32_t *>(&w));
+                    for (int k = 0; k < 4; k += 2) {
+                        const float2 y = add2(make_float2(o[t][w][k], o[t][w][k + 1]), make_float2(x[t][k], x[t][k + 1]));
+                        o[t][w][k] = y.x, o[t][w][k + 1] = y.y;
                     }
-#pragma unroll
-            for (int w0 = 0; w0 < DC; w0 += 4) {
-                if (w0 >= nc) break;
-                uint32_t r[NB][4], f[4];
-#pragma unroll
-                for (int n = 0; n < NB; ++n) ldsm4(va + n * bytes + w0 * 128, r[n]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int w = w0 + i;
-                    if (w >= DC || w >= nc) break;
-                    float x[NT][4];
-#pragma unroll
-                    for (int n = 0; n < NB; ++n) {
-                        codes4_centred(r[n][i], f);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            if (n == 0) x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.0f;
-                            mma16816(x[t], f, pb[n][t][0], pb[n][t][1]);
-                            if constexpr (TWO) mma16816(x[t], f, pl[n][t][0], pl[n][t][1]);
-                        }
-                    }
-#pragma unroll
-                    for (int t = 0; t < NT; ++t)
-#pragma unroll
-                        for (int k = 0; k < 4; k += 2) {
-                            const float2 y = add2(make_float2(o[t][w][k], o[t][w][k + 1]), make_float2(x[t][k], x[t][k + 1]));
-                            o[t][w][k] = y.x, o[t][w][k + 1] = y.y;
-                        }
-                }
             }
-        };
-        if (fine) sums(std::true_type{});
-        else sums(std::false_type{});
+        }
     }
 
     __device__ __forceinline__ void close(int) {
@@ -547,14 +539,16 @@ struct MmaRows4 {
                 const int64_t row = row_index(a, s, h, rr);
                 const float inv = l[t][i] == 0.0f ? 0.0f : 1.0f / l[t][i];
                 uint16_t *dst = static_cast<uint16_t *>(a.out) + row * a.d + g;
-                const bool bf = a.dtype == SKM_DTYPE_BF16;
 #pragma unroll
                 for (int w = 0; w < DC; ++w) {
                     if (!FULL && w >= a.d / KV_B) break;
                     const float x = o[t][w][i] * inv, y = o[t][w][i + 2] * inv;
-                    const uint32_t u = kv_f16_within(x, y);
-                    dst[16 * w] = bf ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : (uint16_t)u;
-                    dst[16 * w + 8] = bf ? __bfloat16_as_ushort(__float2bfloat16_rn(y)) : (uint16_t)(u >> 16);
+                    if constexpr (F16) {
+                        const uint32_t u = kv_f16_within(x, y);
+                        dst[16 * w] = (uint16_t)u, dst[16 * w + 8] = (uint16_t)(u >> 16);
+                    } else {
+                        dst[16 * w] = __bfloat16_as_ushort(__float2bfloat16_rn(x)), dst[16 * w + 8] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+                    }
                 }
                 if (g == 0 && a.lse) a.lse[row] = l[t][i] == 0.0f ? -INFINITY : LN2 * (m[t][i] + log2f(l[t][i]));
             }
@@ -567,12 +561,12 @@ struct MmaRows4 {
 #define KV4_ROWS_VARIANTS(X)                                                                                  \
     X(1, 1, 64, (Fp32Rows4<1, 2>), 16) X(1, 1, 128, (Fp32Rows4<1, 4>), 16) X(1, 1, 256, (Fp32Rows4<1, 8>), 8)  \
     X(1, 4, 64, (Fp32Rows4<4, 2>), 16) X(1, 4, 128, (Fp32Rows4<4, 4>), 16) X(1, 4, 256, (Fp32Rows4<4, 8>), 8)  \
-    KV4_MMA_VARIANTS(X, true) KV4_MMA_VARIANTS(X, false)
-#define KV4_MMA_VARIANTS(X, FULL)                                                                             \
-    X(0, 8, 64, (MmaRows4<4, 1, FULL>), 16) X(0, 8, 128, (MmaRows4<8, 1, FULL>), 16)                          \
-    X(0, 8, 256, (MmaRows4<16, 1, FULL>), 8) X(0, 16, 64, (MmaRows4<4, 2, FULL>), 16)                         \
-    X(0, 16, 128, (MmaRows4<8, 2, FULL>), 8) X(0, 16, 256, (MmaRows4<16, 2, FULL>), 8)                        \
-    X(0, 32, 64, (MmaRows4<4, 4, FULL>), 8) X(0, 32, 128, (MmaRows4<8, 4, FULL>), 8)
+    KV4_MMA_VARIANTS(X, true, false) KV4_MMA_VARIANTS(X, false, false) KV4_MMA_VARIANTS(X, true, true) KV4_MMA_VARIANTS(X, false, true)
+#define KV4_MMA_VARIANTS(X, FULL, F16)                                                                        \
+    X(0, 8, 64, (MmaRows4<4, 1, FULL, F16>), 16) X(0, 8, 128, (MmaRows4<8, 1, FULL, F16>), 16)                \
+    X(0, 8, 256, (MmaRows4<16, 1, FULL, F16>), 8) X(0, 16, 64, (MmaRows4<4, 2, FULL, F16>), 16)               \
+    X(0, 16, 128, (MmaRows4<8, 2, FULL, F16>), 8) X(0, 16, 256, (MmaRows4<16, 2, FULL, F16>), 8)              \
+    X(0, 32, 64, (MmaRows4<4, 4, FULL, F16>), 8) X(0, 32, 128, (MmaRows4<8, 4, FULL, F16>), 8)
 
 #define KV_UNPACK(...) __VA_ARGS__
 
@@ -598,9 +592,9 @@ size_t kv4_rows_part_most(int nb, int heads, int d, int dtype, int64_t rows, int
 
 cudaError_t launch_kv4_rows(const KvAttnArgs &a, const KvRowsPlan &p, cudaStream_t st) {
     const int dmax = a.d <= 64 ? 64 : a.d <= 128 ? 128 : 256;
-    const bool full = a.d == dmax;
+    const bool full = a.d == dmax, half = a.dtype == SKM_DTYPE_F16;
 #define KV4_RUN(FP32, RT, D, ROWS, NW)                                                             \
-    if (p.fp32 == FP32 && p.rt == RT && dmax == D && (full || !KV_UNPACK ROWS::ONE_D)) \
+    if (p.fp32 == FP32 && p.rt == RT && dmax == D && (full || !KV_UNPACK ROWS::ONE_D) && half == KV_UNPACK ROWS::HALF) \
         return run_rows<KV_UNPACK ROWS, NW>(a, p, st);
     KV4_ROWS_VARIANTS(KV4_RUN)
 #undef KV4_RUN

@@ -121,7 +121,7 @@ struct KvPromptPlan {
     int64_t units;
     size_t part;  // bytes
 };
-// 16-bit rows that are always the few-row kernels'.  (Over the 4-bit cache, up to 128 dims, 20 rows of 128 units that see 5000 keys take 73 us
+// 16-bit rows that are always the few-row kernels'.  (Over the 4-bit cache, up to 128 dims, 20 rows of 128 units that see 5000 keys take 66 us
 // there and 58 in the kernel for many rows, of 2 units 23 and 18; f16 92 and 172, 26 and 27; 12 rows, bf16, 44 and 58, 15.6 and 18)
 constexpr int KV_ROWS_MOST = 32;
 bool kv_prompt_ok(int dtype, int nb, int heads, int d, int64_t rows, int64_t span);
